@@ -472,6 +472,209 @@ reskv_status reskv_decode_attn_noalloc(const reskv_device_cache* c, const void* 
  */
 reskv_status reskv_noalloc_check_status(void* stream, int32_t* last_kernel);
 
+/*
+ * ---------------------------------------------------------------------------
+ * The full cache before compression: rotary positions, a paged cache held in 4
+ * bits, attention over it, and its rows as input of reskv_build_cache (no
+ * counterpart in the paper, which starts from a prefilled cache).
+ *
+ * These calls own no memory: tensors, pages and workspace are the caller's.
+ * They allocate nothing and may be captured into CUDA graphs.  Device-side
+ * faults (a position, sequence or page outside its range) touch no memory out
+ * of range: the row is skipped or left as stated, and RESKV codes are ORed into
+ * the caller's status word (2 = index out of range, 1 = a bounded wait gave up).
+ * ---------------------------------------------------------------------------
+ */
+
+enum { RESKV_BF16 = 0, RESKV_F16 = 1, RESKV_F32 = 2 };
+
+/* Rows of one tensor: row (t, h) starts at data + t * token_stride + h *
+ * head_stride elements, the elements of a row lie side by side.  data is
+ * aligned to its element size; 16-byte aligned rows are moved in 16-byte words.
+ * Rows may overlap in no other way than being the same row. */
+typedef struct reskv_heads {
+  void* data;
+  int64_t token_stride, head_stride;   /* in elements                         */
+  int32_t n_heads;
+  int32_t dtype;                       /* RESKV_BF16, RESKV_F16 or RESKV_F32  */
+} reskv_heads;
+
+/* The rotation: cos and sin of every position and pair, as reskv_rope_table
+ * writes them or the caller computed them. */
+typedef struct reskv_rotation {
+  const float* table;                  /* device fp32 [n_positions, rot_dim/2, 2] */
+  int64_t n_positions;
+  int32_t rot_dim;                     /* R: the first R dims of a row turn,
+                                          even, 2 <= R <= head_dim            */
+  int32_t interleaved;                 /* 0: pair i is dims (i, i + R/2);
+                                          1: dims (2i, 2i + 1)                */
+} reskv_rotation;
+
+/* Scaling of the frequencies f_i = base^(-2i/R) for contexts longer than the
+ * original_positions (L0) a model was trained on.
+ *   NONE        f_i
+ *   LINEAR      f_i / factor (positions interpolated)
+ *   BASE        base * factor^(R/(R-2)) in place of base
+ *   WAVELENGTH  by the turns L0 f_i / 2pi within L0: f_i at high_freq turns or
+ *               more, f_i / factor at low_freq or fewer, linear between
+ *   YARN        by the pair index: f_i below the pair that makes beta_fast
+ *               turns within L0, f_i / factor above the one that makes
+ *               beta_slow, linear between (bounds rounded outwards)        */
+enum { RESKV_ROPE_NONE = 0, RESKV_ROPE_LINEAR = 1, RESKV_ROPE_BASE = 2,
+       RESKV_ROPE_WAVELENGTH = 3, RESKV_ROPE_YARN = 4 };
+typedef struct reskv_rope_config {
+  int32_t rot_dim;                     /* R, even, 2..512                     */
+  int32_t scaling;                     /* RESKV_ROPE_*                        */
+  double base;
+  double factor;                       /* >= 1                                */
+  double original_positions;           /* L0 (WAVELENGTH, YARN)               */
+  double low_freq, high_freq;          /* WAVELENGTH: 1 and 4                 */
+  double beta_fast, beta_slow;         /* YARN: 32 and 1                      */
+  double magnitude;                    /* multiplies cos and sin; 0: 1, or
+                                          0.1 ln(factor) + 1 with YARN        */
+} reskv_rope_config;
+
+/* base 500000, no scaling, factor 1, low/high 1 and 4, beta 32 and 1, magnitude 0. */
+void reskv_rope_config_default(reskv_rope_config* cfg);
+
+/* table[p, i] = magnitude * (cos, sin)(p * f_i) for p < n_positions: angles and
+ * functions in fp64, rounded once to fp32.  table: device fp32 [n_positions,
+ * R/2, 2], 8-byte aligned. */
+reskv_status reskv_rope_table(const reskv_rope_config* cfg, int64_t n_positions, float* table,
+                              void* stream);
+
+/*
+ * Rotate the rows of n_tensors (1 or 2, e.g. queries and keys) tensors by their
+ * tokens' positions, in one launch:
+ *   (a, b) -> (a cos - b sin, b cos + a sin)   for every pair of the first R dims,
+ * dims R.. are copied.  backward != 0 is the gradient: the transposed map (sin
+ * negated).  Products and sums in fp32, one rounding to y's type.
+ *
+ *   positions : device int32 [n_tokens].  A negative position marks padding: the
+ *               row is copied.  One >= n_positions also, and reports a fault.
+ *   x[i], y[i]: device [n_tokens, n_heads, head_dim], same n_heads and dtype; y
+ *               may be x itself (in place) but must not overlap it otherwise
+ *   status    : device word for faults, or NULL
+ * head_dim even, 2..512.  n_tokens = 0 does nothing.
+ */
+reskv_status reskv_rope(const reskv_rotation* rot, const int32_t* positions, int64_t n_tokens,
+                        int32_t head_dim, int32_t n_tensors, const reskv_heads* x,
+                        const reskv_heads* y, int32_t backward, uint32_t* status, void* stream);
+
+/*
+ * A paged cache held in 4 bits.  Position p of sequence b lies in page
+ * page_table[b, p / page_tokens].  A page holds page_tokens tokens of every KV
+ * head: per head page_tokens / 16 tiles, one after the other.  A tile is 16
+ * tokens (rows) of d = head_dim dims and NG = d / quant_group groups:
+ *
+ *   K codes   16 rows of d/2 bytes.  The 32-bit word of dims 8w .. 8w+7 (dim
+ *             8w + j in bits 4j .. 4j+3) lies at word (w % 4) * (d/32) + w / 4
+ *   K scales  16 rows of NG bf16 scales, then NG bf16 minima
+ *   V codes   8 rows of d bytes for two tokens 2r, 2r+1 each, in 8 chunks of d/8
+ *             bytes.  Chunk g (dims 32c + 4g .. 32c + 4g + 3, c < d/32) lies at
+ *             place g ^ z, z = 2 (r % 4) for d = 128 and 4 (r/2 % 2) for d = 64;
+ *             it holds, for every c, token 2r's 16-bit unit (dim 32c + 4g + i in
+ *             bits 4i .. 4i+3), then token 2r+1's
+ *   V scales  as K scales
+ *
+ * so that a warp reads whole matrix fragments from a tile without bank
+ * conflicts and a tile is one bulk copy.  A group of values x (fp32) is held as
+ *   s = bf16((max - min) / 15), m = bf16(min), n = min(15, max(0, rint((x - m) / s)))
+ * (quotients rounded to nearest, rint to even; s below 2^-126 is held as 0 with
+ * n = 0) and stands for s n + m.  A group with a NaN or infinity, or whose s
+ * or m overflow, is held as s = m = NaN and stands for NaN.
+ */
+typedef struct reskv_paged_kv {
+  void* pages;                         /* device, n_pages * n_kv_heads *
+                                          reskv_paged_head_bytes(), 16-byte aligned */
+  int64_t n_pages;
+  const int32_t* page_table;           /* device int32 [batch, table_pages]   */
+  int32_t batch, table_pages;
+  int32_t page_tokens;                 /* multiple of 16, 16..1024            */
+  int32_t n_kv_heads;
+  int32_t head_dim;                    /* 64 or 128                           */
+  int32_t quant_group;                 /* 32, 64 or 128, divides head_dim     */
+  uint32_t* status;                    /* device word for faults, or NULL     */
+} reskv_paged_kv;
+
+/* Bytes of one KV head of one page; 0 for a shape that is not supported. */
+int64_t reskv_paged_head_bytes(int32_t page_tokens, int32_t head_dim, int32_t quant_group);
+
+/*
+ * Append tokens to the cache: token i's key is rotated (rot != NULL) and held,
+ * with its value, at positions[i] of sequence seqs[i].  With q, the same launch
+ * writes the tokens' rotated queries to q_out (reskv_rope's map; q_out may be q).
+ *
+ *   seqs, positions : device int32 [n_tokens]; a negative position marks padding:
+ *                     nothing is held, q's row is copied.  Each (sequence,
+ *                     position) at most once a call.  A sequence or position
+ *                     outside the table, a page outside the pages, or a position
+ *                     >= n_positions is a fault: nothing is held, q is copied.
+ *   k, v            : device [n_tokens, n_kv_heads, head_dim], one dtype
+ *   q, q_out        : device [n_tokens, any heads, head_dim] of any dtype, or NULL
+ */
+reskv_status reskv_paged_append(const reskv_paged_kv* kv, int64_t n_tokens, const int32_t* seqs,
+                                const int32_t* positions, const reskv_rotation* rot,
+                                const reskv_heads* k, const reskv_heads* v, const reskv_heads* q,
+                                const reskv_heads* q_out, void* stream);
+
+/* Output rows of reskv_paged_gather: row (b, h, i) at data + b * batch_stride +
+ * h * head_stride + i * token_stride elements. */
+typedef struct reskv_rows {
+  void* data;
+  int64_t batch_stride, head_stride, token_stride;
+  int32_t dtype;
+} reskv_rows;
+
+/*
+ * The values held at positions starts[b] .. starts[b] + n - 1 of every sequence
+ * (starts NULL: from 0), as rows of k and v: with starts NULL and contiguous
+ * [batch, n_kv_heads, n, d] outputs, a layer's input of reskv_build_cache.  Rows at
+ * positions >= lens[b] are zero.  A page outside the pages is a fault and gives
+ * zero rows.  Either of k and v may be NULL, and both have one dtype.
+ *   starts, lens : device int32 [batch]
+ */
+reskv_status reskv_paged_gather(const reskv_paged_kv* kv, const int32_t* starts, const int32_t* lens,
+                                int64_t n, const reskv_rows* k, const reskv_rows* v, void* stream);
+
+/*
+ * Attention of every sequence's newest tokens over the sequence's cache (their
+ * own keys and values already appended).  Sequence b holds lens[b] tokens, its
+ * n_b query tokens are the last of them: query i of n_b stands at position
+ * p = lens[b] - n_b + i and sees positions max(0, p - window + 1) .. p (window 0:
+ * from 0).  Query head h attends with KV head h / (heads / n_kv_heads):
+ *   o = sum_t softmax_t(scale <q, k_t>) v_t
+ * over the held values k_t, v_t.  A query that sees nothing (p < 0) gets o = 0.
+ * Sums and softmax statistics in fp32.
+ */
+typedef struct reskv_paged_attn_args {
+  reskv_heads q;                       /* [n_tokens, heads, d] bf16 or fp16; heads a
+                                          multiple of n_kv_heads, at most 64 per KV head */
+  reskv_heads o;                       /* the same shape, q's dtype or fp32; not
+                                          overlapping q                        */
+  float* lse;                          /* device fp32 [n_tokens, heads] or NULL:
+                                          ln sum exp(scale <q, k>), -inf where
+                                          nothing is seen                      */
+  const int32_t* q_begin;              /* device int32 [batch + 1], ascending: query
+                                          tokens q_begin[b] .. q_begin[b+1] - 1 are
+                                          sequence b's; NULL: n_tokens / batch each */
+  const int32_t* lens;                 /* device int32 [batch]                 */
+  int64_t n_tokens;
+  float scale;                         /* 0: 1 / sqrt(head_dim)                */
+  int32_t window;                      /* 0: none                              */
+  void* workspace;                     /* device, 256-byte aligned, zero before its
+                                          first use and left ready for the next
+                                          call; calls that share one must be ordered */
+  size_t workspace_bytes;              /* at least reskv_paged_attn_workspace() */
+} reskv_paged_attn_args;
+
+/* Workspace bytes of a call; depends on the head shape, batch and n_tokens (an
+ * upper bound over fewer), not on the lengths. */
+size_t reskv_paged_attn_workspace(const reskv_paged_kv* kv, const reskv_paged_attn_args* args);
+
+reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* args,
+                              void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -31,6 +31,9 @@ RESKV_DEBUG_UNIT_CANDIDATES = 4
 RESKV_BUDGET_UNIFORM, RESKV_BUDGET_ADAKV = 0, 1
 RESKV_TEST_FAIL_FIRST_WAIT, RESKV_TEST_FAIL_ALLOC = 1, 2
 RESKV_APPEND_FAIL, RESKV_APPEND_RING_DROP, RESKV_APPEND_RING_FOLD = 0, 1, 2
+RESKV_BF16, RESKV_F16, RESKV_F32 = 0, 1, 2
+(RESKV_ROPE_NONE, RESKV_ROPE_LINEAR, RESKV_ROPE_BASE, RESKV_ROPE_WAVELENGTH,
+ RESKV_ROPE_YARN) = 0, 1, 2, 3, 4
 MAX_GRID = 8
 
 
@@ -88,6 +91,46 @@ class reskv_device_cache(ctypes.Structure):
                 ("g_min", ctypes.c_float), ("g_fixed", ctypes.c_float)]
 
 
+class reskv_heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("n_heads", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class reskv_rotation(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("n_positions", ctypes.c_int64),
+                ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class reskv_rope_config(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("original_positions", ctypes.c_double),
+                ("low_freq", ctypes.c_double), ("high_freq", ctypes.c_double),
+                ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double),
+                ("magnitude", ctypes.c_double)]
+
+
+class reskv_paged_kv(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
+                ("page_table", ctypes.c_void_p), ("batch", ctypes.c_int32),
+                ("table_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("quant_group", ctypes.c_int32), ("status", ctypes.c_void_p)]
+
+
+class reskv_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("dtype", ctypes.c_int32)]
+
+
+class reskv_paged_attn_args(ctypes.Structure):
+    _fields_ = [("q", reskv_heads), ("o", reskv_heads), ("lse", ctypes.c_void_p),
+                ("q_begin", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("n_tokens", ctypes.c_int64),
+                ("scale", ctypes.c_float), ("window", ctypes.c_int32), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
 _lib = None
 
 
@@ -138,6 +181,26 @@ def load_library():
     lib.reskv_noalloc_check_status.restype = i32
     lib.reskv_test_inject.argtypes = [i32, ctypes.c_int64]
     lib.reskv_test_inject.restype = i32
+    ropep, headsp = ctypes.POINTER(reskv_rope_config), ctypes.POINTER(reskv_heads)
+    rotp, kvp = ctypes.POINTER(reskv_rotation), ctypes.POINTER(reskv_paged_kv)
+    rowsp, attnp = ctypes.POINTER(reskv_rows), ctypes.POINTER(reskv_paged_attn_args)
+    i64 = ctypes.c_int64
+    lib.reskv_rope_config_default.argtypes = [ropep]
+    lib.reskv_rope_config_default.restype = None
+    lib.reskv_rope_table.argtypes = [ropep, i64, vp, vp]
+    lib.reskv_rope_table.restype = i32
+    lib.reskv_rope.argtypes = [rotp, vp, i64, i32, i32, headsp, headsp, i32, vp, vp]
+    lib.reskv_rope.restype = i32
+    lib.reskv_paged_head_bytes.argtypes = [i32, i32, i32]
+    lib.reskv_paged_head_bytes.restype = i64
+    lib.reskv_paged_append.argtypes = [kvp, i64, vp, vp, rotp, headsp, headsp, headsp, headsp, vp]
+    lib.reskv_paged_append.restype = i32
+    lib.reskv_paged_gather.argtypes = [kvp, vp, vp, i64, rowsp, rowsp, vp]
+    lib.reskv_paged_gather.restype = i32
+    lib.reskv_paged_attn_workspace.argtypes = [kvp, attnp]
+    lib.reskv_paged_attn_workspace.restype = sz
+    lib.reskv_paged_attn.argtypes = [kvp, attnp, vp]
+    lib.reskv_paged_attn.restype = i32
     _lib = lib
     return lib
 
@@ -483,3 +546,250 @@ def reskv_noalloc_check_status(stream=None) -> int:
     k = ctypes.c_int32(0)
     _check(load_library().reskv_noalloc_check_status(_stream(stream), ctypes.byref(k)))
     return int(k.value)
+
+
+# ---------------------------------------------------------------------------
+# the full cache before compression: rotary positions and 4-bit pages
+# ---------------------------------------------------------------------------
+
+_dtypes = {}
+
+
+def _code(t, what: str) -> int:
+    """RESKV_BF16, RESKV_F16 or RESKV_F32 of a tensor."""
+    if not _dtypes:
+        import torch
+        _dtypes.update({torch.bfloat16: RESKV_BF16, torch.float16: RESKV_F16,
+                        torch.float32: RESKV_F32})
+    c = _dtypes.get(t.dtype)
+    if c is None:
+        raise ValueError(f"{what} must be bfloat16, float16 or float32, got {t.dtype}")
+    return c
+
+
+def _heads(t, what: str, tokens: int, heads: Optional[int], dim: int) -> reskv_heads:
+    """reskv_heads of a CUDA tensor [tokens, heads, dim] with neighbouring elements in a row."""
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor")
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != tokens or shape[2] != dim or (heads is not None and shape[1] != heads):
+        raise ValueError(f"{what} must be [{tokens}, {'heads' if heads is None else heads}, {dim}], "
+                         f"got {tuple(shape)}")
+    s = t.stride()
+    if s[2] != 1:
+        raise ValueError(f"{what}: the elements of a row must lie side by side")
+    return reskv_heads(t.data_ptr(), s[0], s[1], shape[1], _code(t, what))
+
+
+def _ints(t, what: str, n: int) -> int:
+    """Pointer of a contiguous int32 CUDA tensor of n elements."""
+    if t.numel() != n:
+        raise ValueError(f"{what} must hold {n} elements, got {t.numel()}")
+    return _dptr(t, "torch.int32", what).value
+
+
+def _rotation(table, interleaved: bool) -> reskv_rotation:
+    if table.dim() != 3 or table.shape[2] != 2:
+        raise ValueError(f"table must be [positions, rot_dim / 2, 2], got {tuple(table.shape)}")
+    return reskv_rotation(_dptr(table, "torch.float32", "table").value, table.shape[0],
+                          2 * table.shape[1], 1 if interleaved else 0)
+
+
+def reskv_rope_config_default(**fields) -> reskv_rope_config:
+    """reskv_rope_config with the defaults, then ``fields`` applied."""
+    cfg = reskv_rope_config()
+    load_library().reskv_rope_config_default(ctypes.byref(cfg))
+    for k, v in fields.items():
+        setattr(cfg, k, v)
+    return cfg
+
+
+def reskv_rope_table(cfg: reskv_rope_config, n_positions: int, stream=None):
+    """float32 [n_positions, rot_dim / 2, 2] cos and sin of every position on the
+    current device."""
+    import torch
+    table = torch.empty((int(n_positions), cfg.rot_dim // 2, 2), dtype=torch.float32, device="cuda")
+    _check(load_library().reskv_rope_table(ctypes.byref(cfg), int(n_positions),
+                                           ctypes.c_void_p(table.data_ptr()), _stream(stream)))
+    return table
+
+
+def reskv_rope(q, q_out, positions, table, k=None, k_out=None, interleaved: bool = False,
+               backward: bool = False, status=None, stream=None) -> None:
+    """Rotate q (and k, in the same launch) by their tokens' positions, or with
+    ``backward`` their gradients by the transposed map.
+
+    q, q_out: [T, H, d] bf16, f16 or f32, any token and head strides; q_out may be
+    q.  k, k_out likewise with their own heads.  positions: int32 [T]; negative
+    ones mark padding (rows copied).  table: float32 [positions, rot_dim / 2, 2]
+    (reskv_rope_table); rot_dim < d rotates a part of every head.  status: int32
+    [1] that a position outside the table sets to 2.
+    """
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out go together")
+    if q.dim() != 3:
+        raise ValueError(f"q must be [tokens, heads, dim], got {tuple(q.shape)}")
+    T, H, d = q.shape
+    n = 1 if k is None else 2
+    x, y = (reskv_heads * n)(), (reskv_heads * n)()
+    x[0], y[0] = _heads(q, "q", T, None, d), _heads(q_out, "q_out", T, H, d)
+    if k is not None:
+        x[1] = _heads(k, "k", T, None, d)
+        y[1] = _heads(k_out, "k_out", T, x[1].n_heads, d)
+    rot = _rotation(table, interleaved)
+    _check(load_library().reskv_rope(ctypes.byref(rot), _ints(positions, "positions", T), T, d, n, x, y,
+                                     1 if backward else 0,
+                                     None if status is None else _ints(status, "status", 1),
+                                     _stream(stream)))
+
+
+def reskv_paged_head_bytes(page_tokens: int, head_dim: int, quant_group: int) -> int:
+    """Bytes of one KV head of one page."""
+    n = load_library().reskv_paged_head_bytes(int(page_tokens), int(head_dim), int(quant_group))
+    if n == 0:
+        raise ValueError(f"no page of {page_tokens} tokens, head_dim {head_dim}, quant_group {quant_group}")
+    return n
+
+
+def reskv_paged_pages(n_pages: int, n_kv_heads: int, page_tokens: int = 64, head_dim: int = 128,
+                      quant_group: int = 32):
+    """Zeroed pages on the current device: uint8 [n_pages, n_kv_heads, bytes]."""
+    import torch
+    return torch.zeros((n_pages, n_kv_heads, reskv_paged_head_bytes(page_tokens, head_dim, quant_group)),
+                       dtype=torch.uint8, device="cuda")
+
+
+class PagedKV:
+    """One layer's paged 4-bit cache: the caller's pages and page table, their
+    shape, and a status word that device faults are ORed into.
+
+    pages: uint8, n_pages * n_kv_heads * reskv_paged_head_bytes() bytes;
+    page_table: int32 [batch, table_pages], read by every call as it then is.
+    """
+
+    def __init__(self, pages, page_table, page_tokens: int, n_kv_heads: int, head_dim: int = 128,
+                 quant_group: int = 32, status=None):
+        import torch
+        per = n_kv_heads * reskv_paged_head_bytes(page_tokens, head_dim, quant_group)
+        if pages.numel() % per or pages.numel() == 0:
+            raise ValueError(f"pages must hold a multiple of {per} bytes, got {pages.numel()}")
+        if page_table.dim() != 2:
+            raise ValueError(f"page_table must be [batch, pages], got {tuple(page_table.shape)}")
+        self.pages, self.page_table = pages, page_table
+        self.batch, self.table_pages = page_table.shape
+        self.page_tokens, self.n_kv_heads, self.head_dim, self.quant_group = (
+            int(page_tokens), int(n_kv_heads), int(head_dim), int(quant_group))
+        self.status = torch.zeros(1, dtype=torch.int32, device=pages.device) if status is None else status
+        self.struct = reskv_paged_kv(
+            pages=_dptr(pages, "torch.uint8", "pages").value, n_pages=pages.numel() // per,
+            page_table=_dptr(page_table, "torch.int32", "page_table").value, batch=self.batch,
+            table_pages=self.table_pages, page_tokens=self.page_tokens, n_kv_heads=self.n_kv_heads,
+            head_dim=self.head_dim, quant_group=self.quant_group,
+            status=_ints(self.status, "status", 1))
+
+    def check_status(self) -> None:
+        """Read and clear the status word (synchronises); raises if a fault was recorded."""
+        word = int(self.status.item())
+        if word:
+            self.status.zero_()
+            raise ReskvError(RESKV_ERR_DEVICE_STATUS, f"paged cache status word {word} (1 = bounded wait "
+                                                      "timed out, 2 = index out of range)")
+
+
+def reskv_paged_append(kv: PagedKV, k, v, seqs, positions, table=None, interleaved: bool = False,
+                       q=None, q_out=None, stream=None) -> None:
+    """Hold token i's key (rotated by its position, with ``table``) and value at
+    positions[i] of sequence seqs[i]; with q, rotate the tokens' queries into
+    q_out in the same call.
+
+    k, v: [T, n_kv_heads, d], one of bf16, f16, f32; seqs, positions: int32 [T],
+    negative positions mark padding; q, q_out: [T, heads, d].
+    """
+    T = k.shape[0]
+    kh = _heads(k, "k", T, kv.n_kv_heads, kv.head_dim)
+    vh = _heads(v, "v", T, kv.n_kv_heads, kv.head_dim)
+    qh = qo = None
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if q is not None:
+        qh = _heads(q, "q", T, None, kv.head_dim)
+        qo = _heads(q_out, "q_out", T, qh.n_heads, kv.head_dim)
+    rot = None if table is None else _rotation(table, interleaved)
+    _check(load_library().reskv_paged_append(kv.struct, T, _ints(seqs, "seqs", T),
+                                             _ints(positions, "positions", T), rot, kh, vh, qh, qo,
+                                             _stream(stream)))
+
+
+def _rows(t, what: str, kv: PagedKV, n: int) -> reskv_rows:
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor")
+    if tuple(t.shape) != (kv.batch, kv.n_kv_heads, n, kv.head_dim) or t.stride(3) != 1:
+        raise ValueError(f"{what} must be [{kv.batch}, {kv.n_kv_heads}, {n}, {kv.head_dim}] with neighbouring "
+                         f"elements in a row, got {tuple(t.shape)}")
+    return reskv_rows(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2), _code(t, what))
+
+
+def reskv_paged_gather(kv: PagedKV, lens, k_out=None, v_out=None, starts=None, stream=None) -> None:
+    """The values held at positions starts[b] .. starts[b] + n - 1 (starts None:
+    from 0) into k_out, v_out [batch, n_kv_heads, n, d] bf16, f16 or f32; rows at
+    positions >= lens[b] are zero.  starts, lens: int32 [batch]."""
+    if k_out is None and v_out is None:
+        raise ValueError("k_out or v_out is needed")
+    n = (v_out if k_out is None else k_out).shape[2]
+    kr = None if k_out is None else _rows(k_out, "k_out", kv, n)
+    vr = None if v_out is None else _rows(v_out, "v_out", kv, n)
+    _check(load_library().reskv_paged_gather(kv.struct,
+                                             None if starts is None else _ints(starts, "starts", kv.batch),
+                                             _ints(lens, "lens", kv.batch), n, kr, vr, _stream(stream)))
+
+
+_workspaces = {}
+
+
+def _workspace(device, stream: int, nbytes: int):
+    """A zeroed workspace per device and stream, kept and grown; what it grew from
+    is kept too (a captured graph may hold its address)."""
+    import torch
+    held = _workspaces.setdefault((device, stream), [])
+    if not held or held[-1].numel() < nbytes:
+        held.append(torch.zeros(max(nbytes, 2 * held[-1].numel() if held else 0), dtype=torch.uint8,
+                                device=device))
+        torch.cuda.current_stream(device).synchronize()
+    return held[-1]
+
+
+def reskv_paged_attn(kv: PagedKV, q, lens, o, q_begin=None, scale: Optional[float] = None, window: int = 0,
+                     lse=None, workspace=None, stream=None) -> None:
+    """Attention of every sequence's newest tokens over its cache.
+
+    q: bf16 or f16 [T, heads, d], sequence b's query tokens rows q_begin[b] ..
+    q_begin[b + 1] - 1 (int32 [batch + 1]; None: T / batch each), the last of the
+    lens[b] tokens it holds; o: [T, heads, d] of q's dtype or float32.  window:
+    positions a query sees, itself included (0: all).  lse: float32 [T, heads]
+    for ln sum exp, or None.  workspace: zeroed uint8 tensor of at least
+    reskv_paged_attn_workspace() bytes (None: one kept per stream).
+    """
+    T = q.shape[0]
+    qh = _heads(q, "q", T, None, kv.head_dim)
+    a = reskv_paged_attn_args(q=qh, o=_heads(o, "o", T, qh.n_heads, kv.head_dim),
+                              lens=_ints(lens, "lens", kv.batch), n_tokens=T,
+                              scale=0.0 if scale is None else scale, window=window)
+    if lse is not None:
+        if lse.numel() != T * qh.n_heads:
+            raise ValueError(f"lse must hold {T * qh.n_heads} elements, got {lse.numel()}")
+        a.lse = _dptr(lse, "torch.float32", "lse").value
+    if q_begin is not None:
+        a.q_begin = _ints(q_begin, "q_begin", kv.batch + 1)
+    s = _stream(stream)
+    lib = load_library()
+    if workspace is None:
+        workspace = _workspace(q.device, s.value or 0, lib.reskv_paged_attn_workspace(kv.struct, a))
+    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    _check(lib.reskv_paged_attn(kv.struct, a, s))
+
+
+def reskv_paged_attn_workspace(kv: PagedKV, n_tokens: int, heads: int) -> int:
+    """Workspace bytes of a reskv_paged_attn call over n_tokens query tokens."""
+    a = reskv_paged_attn_args(n_tokens=n_tokens)
+    a.q.n_heads = heads
+    return load_library().reskv_paged_attn_workspace(kv.struct, a)
