@@ -2,142 +2,488 @@
 // (reskv_paged_attn).
 #include <cmath>
 
-#include "paged.cuh"
+#include "paged_attn.cuh"
 
 namespace reskv {
 namespace {
 
-struct AttnParams {
-  const void* q;
-  void* o;
-  float* lse;
-  int64_t q_token, q_head, o_token, o_head;
-  const int32_t* q_begin;
-  const int32_t* lens;
-  const int32_t* page_table;
-  const uint8_t* pages;
-  uint32_t* status;
-  int64_t n_pages, n_tokens;
-  int32_t batch, table_pages, page_tokens, kv_heads, heads;
-  int32_t window, o_f32;
-  float scale2;                   // scale * log2 e
+// --- few query rows: one warp, one block of 8 rows ---------------------------
+//
+// A call's work is a list of units, one per (sequence, block of 8 query rows, KV
+// head), each a run of 16-token tiles.  The tiles of all units, laid end to end,
+// are cut into equal pieces, one per warp, whatever the sequences' lengths: a
+// warp finishes the units that lie in its piece, a unit cut between warps of a
+// CTA is joined in shared memory, one cut between CTAs by the last of them to
+// arrive (records in order, so the result does not depend on the arrival).  Every CTA
+// works the cut out for itself from the lengths, which only the device knows.
+//
+// One more warp feeds all the others: its lane w keeps warp w's ring of tiles
+// full, one bulk copy per tile, so that page lookups and copies cost the tile
+// step nothing.
+constexpr int kAttnWarps = 15;                      // computing; with the feeding warp 16, of 128 registers
+constexpr int kAttnStages = 3;
+constexpr int kMinTiles = 2;                      // of a piece, before more CTAs are used
+constexpr int kRows = 8;                          // query rows of a unit
+
+struct RecordInfo {
+  int64_t start;                                  // first tile of the record's unit
+  int tiles, b, r0, h;
+  int present;
 };
 
-// One warp per (query token, query head), one position at a time, lane l
-// holding dims 4l .. 4l+3 (two halves of the warp on neighbouring positions for
-// d = 64): the running maximum m, sum l and weighted sum of the softmax.
-template <typename T, int D, int kGroup>
-__global__ void __launch_bounds__(128) k_paged_attn(const __grid_constant__ AttnParams p) {
-  constexpr int L = D / 4, NG = D / kGroup, S = 32 / L;
-  constexpr TileShape ts{D, NG};
-  const int lane = threadIdx.x % 32, u = lane % L, sub = lane / L;
-  const int64_t row = int64_t(blockIdx.x) * 4 + threadIdx.x / 32;
-  if (row >= p.n_tokens * p.heads) return;
-  const int64_t tok = row / p.heads;
-  const int head = int(row - tok * p.heads), h = head / (p.heads / p.kv_heads);
-  int b;
-  int64_t first, count;
-  if (p.q_begin) {
-    int lo = 0, hi = p.batch;                         // last b with q_begin[b] <= tok
+__host__ __device__ constexpr int record_stride(int d) { return d + 4; }          // floats of a row: spreads rows over banks
+__host__ __device__ constexpr int record_floats(int d) { return kRows * record_stride(d); }
+
+template <int D, int NG>
+struct AttnSmem {
+  static constexpr int ring = kAttnWarps * kAttnStages * TileShape{D, NG}.bytes();
+  static constexpr int heads = kAttnWarps * record_floats(D) * 4;
+  static constexpr int refs = 2 * kAttnWarps * kRows * 4;
+  static constexpr int info = 2 * kAttnWarps * int(sizeof(RecordInfo));
+  static constexpr int bars = 2 * kAttnWarps * kAttnStages * 8;
+  static constexpr int skips = kAttnWarps * kAttnStages * 4;
+  static constexpr int fixed = (ring + heads + refs + info + bars + skips + 16 + 15) / 16 * 16;
+  static_assert((ring + heads + refs) % 8 == 0 && (ring + heads + refs + info) % 8 == 0 && ring % 16 == 0, "alignment");
+  static_assert(kAttnStages * TileShape{D, NG}.bytes() >= record_floats(D) * 4, "a drained ring holds a record");
+  static int bytes(int batch) { return fixed + (batch + 1) * 8; }
+};
+
+struct Cursor {
+  int b, r0, h, tile;                             // tile: within the unit
+  Sequence s;
+  RowBlock k;
+  int64_t start;                                  // the unit's first tile among all
+
+  __device__ __forceinline__ void block(const AttnParams& p) {
+    const int rows = s.count * p.group;
+    k = row_block(p, s, r0, min(r0 + kRows, rows));
+  }
+  __device__ void locate(const AttnParams& p, const int64_t* prefix, int64_t x) {
+    int lo = 0, hi = p.batch;                     // prefix[lo] <= x < prefix[hi]
     while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (p.q_begin[mid] <= tok) lo = mid;
+      const int mid = (lo + hi) >> 1;
+      if (prefix[mid] <= x) lo = mid;
       else hi = mid;
     }
     b = lo;
-    first = p.q_begin[b];
-    count = p.q_begin[b + 1] - first;
-    if (tok < first || tok >= first + count) return;
+    s = sequence_of(p, b);
+    int64_t left = x - prefix[b];
+    for (r0 = 0;; r0 += kRows) {
+      block(p);
+      const int64_t n = int64_t(k.tiles) * p.kv_heads;
+      if (left < n || r0 + kRows >= s.count * p.group) break;
+      left -= n;
+    }
+    h = min(int(left / k.tiles), p.kv_heads - 1);
+    tile = int(left - int64_t(h) * k.tiles);
+    start = x - tile;
+  }
+  __device__ void next(const AttnParams& p, const int64_t* prefix) {
+    start += k.tiles;
+    tile = 0;
+    if (++h < p.kv_heads) return;
+    h = 0;
+    r0 += kRows;
+    if (r0 >= s.count * p.group) {
+      do ++b; while (b < p.batch && prefix[b + 1] == prefix[b]);
+      if (b >= p.batch) return;
+      s = sequence_of(p, b);
+      r0 = 0;
+    }
+    block(p);
+  }
+};
+
+// Output row r of a sequence, dims 4u .. 4u + 3.
+__device__ __forceinline__ void store_out(const AttnParams& p, const Sequence& s, int h, int r, int u, float4 v) {
+  const int64_t tok = s.q0 + r / p.group;
+  const int64_t at = tok * p.o_token + int64_t(h * p.group + r % p.group) * p.o_head + 4 * u;
+  const float f[4] = {v.x, v.y, v.z, v.w};
+  if (p.o_f32) {
+    float* y = static_cast<float*>(p.o) + at;
+    if (p.o_wide) {
+      *reinterpret_cast<float4*>(y) = v;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = f[i];
+    }
+    return;
+  }
+  uint16_t* y = static_cast<uint16_t*>(p.o) + at;
+  uint16_t e[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    e[i] = p.q_f16 ? __half_as_ushort(__float2half_rn(f[i])) : __bfloat16_as_ushort(__float2bfloat16_rn(f[i]));
+  if (p.o_wide) {
+    *reinterpret_cast<uint2*>(y) = make_uint2(e[0] | uint32_t(e[1]) << 16, e[2] | uint32_t(e[3]) << 16);
   } else {
-    count = p.n_tokens / p.batch;
-    b = int(tok / count);
-    first = b * count;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = e[i];
   }
-  const int64_t room = int64_t(p.table_pages) * p.page_tokens;
-  int64_t len = p.lens[b];
-  if (len < 0 || len > room) {
-    if (lane == 0) report_status(p.status, kStatusBadIndex);
-    len = len < 0 ? 0 : room;
-  }
-  const int64_t pos = len - count + (tok - first);
-  const int64_t from = p.window > 0 && pos - p.window + 1 > 0 ? pos - p.window + 1 : 0;
-  const T* q = static_cast<const T*>(p.q) + tok * p.q_token + head * p.q_head + 4 * u;
-  float qx[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) qx[i] = to_f32(q[i]) * p.scale2;
-  float m = -INFINITY, l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int64_t t0 = from; t0 <= pos; t0 += S) {
-    const int64_t t = t0 + sub;
-    bool see = t <= pos;
-    const int64_t pg = t / p.page_tokens;
-    int page = 0;
-    if (see) {
-      page = p.page_table[int64_t(b) * p.table_pages + pg];
-      if (page < 0 || page >= p.n_pages) {
-        if (u == 0) report_status(p.status, kStatusBadIndex);
-        see = false;
-      }
-    }
-    float x = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (see) {
-      const int slot = int(t - pg * p.page_tokens), r = slot % kTile;
-      const uint8_t* tile =
-          p.pages + ((int64_t(page) * p.kv_heads + h) * (p.page_tokens / kTile) + slot / kTile) * ts.bytes();
-      const uint32_t kc = *reinterpret_cast<const uint16_t*>(tile + ts.k_unit(r, u));
-      const uint32_t vc = *reinterpret_cast<const uint16_t*>(tile + ts.v_codes() + ts.v_unit(r, u));
-      const uint16_t* km = reinterpret_cast<const uint16_t*>(tile + ts.k_meta()) + r * 2 * NG + 4 * u / kGroup;
-      const uint16_t* vm = reinterpret_cast<const uint16_t*>(tile + ts.v_meta()) + r * 2 * NG + 4 * u / kGroup;
-      const float ks = __uint_as_float(uint32_t(km[0]) << 16), kmin = __uint_as_float(uint32_t(km[NG]) << 16);
-      const float vs = __uint_as_float(uint32_t(vm[0]) << 16), vmin = __uint_as_float(uint32_t(vm[NG]) << 16);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x = fmaf(qx[i], fmaf(ks, float((kc >> (4 * i)) & 15u), kmin), x);
-        v[i] = fmaf(vs, float((vc >> (4 * i)) & 15u), vmin);
-      }
-    }
-#pragma unroll
-    for (int o = 1; o < L; o *= 2) x += __shfl_xor_sync(0xffffffffu, x, o);
-    if (see) {
-      const float top = x > m || x != x ? x : m;
-      const float keep = m == -INFINITY ? 0.f : exp2f(m - top), w = top == -INFINITY ? 0.f : exp2f(x - top);
-      l = l * keep + w;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] = acc[i] * keep + w * v[i];
-      m = top;
-    }
-  }
-  if (S == 2) {                                       // join the two halves
-    const float m2 = __shfl_xor_sync(0xffffffffu, m, 16), l2 = __shfl_xor_sync(0xffffffffu, l, 16);
-    const float top = m > m2 ? m : m2;
-    const float a = m == -INFINITY ? 0.f : exp2f(m - top), c = m2 == -INFINITY ? 0.f : exp2f(m2 - top);
-    l = l * a + l2 * c;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float y = __shfl_xor_sync(0xffffffffu, acc[i], 16);
-      acc[i] = acc[i] * a + y * c;
-    }
-    m = top;
-  }
-  const float inv = l != 0.f ? 1.f / l : 0.f;
-  if (sub == 0) {
-    const int64_t at = tok * p.o_token + head * p.o_head + 4 * u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (p.o_f32) static_cast<float*>(p.o)[at + i] = acc[i] * inv;
-      else static_cast<T*>(p.o)[at + i] = from_f32<T>(acc[i] * inv);
-    }
-  }
-  if (lane == 0 && p.lse) p.lse[tok * p.heads + head] = l != 0.f ? (m + log2f(l)) * 0.69314718056f : -INFINITY;
 }
 
-template <typename T>
-void dispatch_attn(const AttnParams& p, int d, int group, cudaStream_t s) {
-  const unsigned blocks = unsigned((p.n_tokens * p.heads + 3) / 4);
-  if (d == 128 && group == 32) k_paged_attn<T, 128, 32><<<blocks, 128, 0, s>>>(p);
-  else if (d == 128 && group == 64) k_paged_attn<T, 128, 64><<<blocks, 128, 0, s>>>(p);
-  else if (d == 128) k_paged_attn<T, 128, 128><<<blocks, 128, 0, s>>>(p);
-  else if (group == 32) k_paged_attn<T, 64, 32><<<blocks, 128, 0, s>>>(p);
-  else k_paged_attn<T, 64, 64><<<blocks, 128, 0, s>>>(p);
+__device__ __forceinline__ void store_lse(const AttnParams& p, const Sequence& s, int h, int r, float ref) {
+  if (p.lse) p.lse[(s.q0 + r / p.group) * int64_t(p.heads) + h * p.group + r % p.group] = ref * 0.693147180559945f;
+}
+
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+  return ok != 0;
+}
+
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
+// one tile, read once: first out of L2
+__device__ __forceinline__ void copy_tile(void* dst, const void* src, uint32_t bytes, uint64_t* bar, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::
+          "r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy)
+      : "memory");
+}
+
+template <int D, int NG, bool kTwoPlanes>
+__global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __grid_constant__ AttnParams p) {
+  using S = AttnSmem<D, NG>;
+  constexpr TileShape ts{D, NG};
+  constexpr int TB = ts.bytes(), RS = record_stride(D), RF = record_floats(D);
+  extern __shared__ __align__(128) uint8_t smem[];
+  uint8_t* ring = smem;
+  float* heads = reinterpret_cast<float*>(smem + S::ring);
+  float* refs = reinterpret_cast<float*>(smem + S::ring + S::heads);
+  RecordInfo* info = reinterpret_cast<RecordInfo*>(smem + S::ring + S::heads + S::refs);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::ring + S::heads + S::refs + S::info);
+  uint64_t* vacant = full + kAttnWarps * kAttnStages;
+  int* skips = reinterpret_cast<int*>(vacant + kAttnWarps * kAttnStages);
+  int* shared_int = skips + kAttnWarps * kAttnStages;                 // [4]
+  int64_t* prefix = reinterpret_cast<int64_t*>(smem + S::fixed);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  // the tiles of every sequence, and what they sum up to
+  for (int b = threadIdx.x; b < p.batch; b += blockDim.x) {
+    const Sequence s = sequence_of(p, b);
+    const int rows = s.count * p.group;
+    int64_t n = 0;
+    for (int r0 = 0; r0 < rows; r0 += kRows) n += row_block(p, s, r0, min(r0 + kRows, rows)).tiles;
+    prefix[b + 1] = n * p.kv_heads;
+  }
+  if (threadIdx.x < 2 * kAttnWarps) info[threadIdx.x].present = 0;
+  if (threadIdx.x < kAttnWarps * kAttnStages) {
+    mbar_init(&full[threadIdx.x], 1);
+    mbar_init(&vacant[threadIdx.x], 1);
+  }
+  fence_mbar_init();
+  __syncthreads();
+  if (warp == 0) {
+    int64_t sum = 0;
+    if (lane == 0) prefix[0] = 0;
+    for (int b = 0; b < p.batch; b += 32) {
+      int64_t v = b + lane < p.batch ? prefix[b + lane + 1] : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o *= 2) {
+        const int64_t u = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += u;
+      }
+      if (b + lane < p.batch) prefix[b + lane + 1] = sum + v;
+      sum += __shfl_sync(0xffffffffu, v, 31);
+    }
+  }
+  __syncthreads();
+  const int64_t N = prefix[p.batch];
+  if (N == 0) return;
+  const int64_t want = (N + kAttnWarps * kMinTiles - 1) / (kAttnWarps * kMinTiles);
+  const int64_t ctas = want < gridDim.x ? want : gridDim.x;
+  const int64_t cta = blockIdx.x;
+  if (cta >= ctas) return;
+  const int64_t c0 = cta * N / ctas, c1 = (cta + 1) * N / ctas;         // this CTA's tiles
+  auto piece = [&](int w) { return c0 + (c1 - c0) * w / kAttnWarps; };
+
+  if (warp == kAttnWarps) {
+    // --- the feeding warp: lane w for warp w ---
+    const int w = lane;
+    int64_t x = 0, end = 0;
+    Cursor c{};
+    if (w < kAttnWarps) {
+      x = piece(w);
+      end = piece(w + 1);
+      if (x < end) c.locate(p, prefix, x);
+    }
+    uint64_t policy;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+    const int tpp = p.page_tokens / kTile;        // tiles of a page
+    int k = 0;                                    // tiles fed
+    int pg = -1, page = 0;                        // page index held in `page`
+    int64_t pg_b = -1;
+    long long t0 = clock64();
+    while (__any_sync(0xffffffffu, x < end)) {
+      bool fed = false;
+      if (x < end) {
+        const int st = k % kAttnStages;
+        uint64_t* bar = &full[w * kAttnStages + st];
+        if (k < kAttnStages || mbar_test(&vacant[w * kAttnStages + st], (k / kAttnStages - 1) & 1)) {
+          const int tile = c.k.first + c.tile;
+          bool ok = !c.k.empty;
+          if (ok) {
+            const int at = tile / tpp;
+            if (at != pg || c.b != pg_b) {
+              pg = at;
+              pg_b = c.b;
+              page = p.page_table[int64_t(c.b) * p.table_pages + at];
+            }
+            if (page < 0 || page >= p.n_pages) {
+              report_status(p.status, kStatusBadIndex);
+              ok = false;
+            }
+          }
+          skips[w * kAttnStages + st] = !ok;
+          if (ok) {
+            const uint8_t* src = p.pages + ((int64_t(page) * p.kv_heads + c.h) * tpp + (tile - pg * tpp)) * int64_t(TB);
+            mbar_arrive_expect_tx(bar, TB);
+            copy_tile(ring + (w * kAttnStages + st) * TB, src, TB, bar, policy);
+          } else {
+            mbar_arrive(bar);
+          }
+          ++k;
+          ++x;
+          if (++c.tile == c.k.tiles && x < end) c.next(p, prefix);
+          fed = true;
+        }
+      }
+      if (__any_sync(0xffffffffu, fed)) {
+        t0 = clock64();
+        continue;
+      }
+      __nanosleep(64);
+      if (clock64() - t0 > kWaitLimitCycles) {
+        // a warp stopped taking tiles: let the copies in flight land, feed no more
+        if (lane == 0) report_status(p.status, kStatusWaitTimeout);
+        if (w < kAttnWarps)
+          for (int i = k > kAttnStages ? k - kAttnStages : 0; i < k; ++i)
+            mbar_wait_bounded(&full[w * kAttnStages + i % kAttnStages], (i / kAttnStages) & 1);
+        break;
+      }
+    }
+  } else {
+    // --- a computing warp ---
+    const int g = lane >> 2, t = lane & 3;
+    int64_t x = piece(warp);
+    const int64_t end = piece(warp + 1);
+    Cursor c{};
+    if (x < end) c.locate(p, prefix, x);
+    TileStep<D, NG, kTwoPlanes> st;
+    int k = 0;
+    bool failed = false;
+    while (x < end && !failed) {
+      const int n = int(min(int64_t(c.k.tiles - c.tile), end - x));
+      const int rows = c.s.count * p.group;
+      {
+        const int r = c.r0 + g;
+        const void* row = nullptr;
+        if (r < rows)
+          row = static_cast<const uint16_t*>(p.q) + (c.s.q0 + r / p.group) * p.q_token +
+                int64_t(c.h * p.group + r % p.group) * p.q_head;
+        st.load_q(p, row, t, lane);
+      }
+      // positions the lane's columns see; rows that do not exist see what the last one does
+      int lo[2], hi[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        hi[j] = c.s.len - c.s.count + min(c.r0 + 2 * t + j, rows - 1) / p.group;
+        lo[j] = p.window > 0 ? max(0, hi[j] - p.window + 1) : 0;
+      }
+      const int all_hi = c.s.len - c.s.count + c.r0 / p.group;
+      const int last = c.s.len - c.s.count + min(c.r0 + kRows - 1, rows - 1) / p.group;
+      const int all_lo = p.window > 0 ? max(0, last - p.window + 1) : 0;
+      st.reset();
+      for (int i = 0; i < n; ++i, ++k) {
+        const int stage = warp * kAttnStages + k % kAttnStages;
+        if (!__all_sync(0xffffffffu, mbar_wait_bounded(&full[stage], (k / kAttnStages) & 1))) {
+          failed = true;
+          break;
+        }
+        if (!skips[stage]) {
+          const int pos = (c.k.first + c.tile + i) * kTile;
+          const uint8_t* tile = ring + stage * TB;
+          bool see[2][2] = {{true, true}, {true, true}};
+          if (pos >= all_lo && pos + kTile - 1 <= all_hi) {
+            st.template step<false>(tile, g, t, see);
+          } else {
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) see[r][j] = pos + g + 8 * r >= lo[j] && pos + g + 8 * r <= hi[j];
+            st.template step<true>(tile, g, t, see);
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&vacant[stage]);
+      }
+      if (failed) {
+        if (lane == 0) report_status(p.status, kStatusWaitTimeout);
+        break;
+      }
+      st.finish();
+      if (c.tile == 0 && n == c.k.tiles) {        // the whole unit
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int r = c.r0 + 2 * t + j;
+          if (r >= rows) continue;
+#pragma unroll
+          for (int b = 0; b < D / 32; ++b)
+            store_out(p, c.s, c.h, r, 8 * b + g, make_float4(st.x(b, 0, j), st.x(b, 1, j), st.x(b, 2, j), st.x(b, 3, j)));
+          if (g == 0) store_lse(p, c.s, c.h, r, st.ref[j]);
+        }
+      } else {                                    // a record: begun before this piece, or cut off at its end
+        const int slot = c.tile > 0 ? 0 : 1;
+        float* rec = slot == 0 ? heads + warp * RF : reinterpret_cast<float*>(ring + warp * kAttnStages * TB);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int b = 0; b < D / 32; ++b)
+            *reinterpret_cast<float4*>(rec + (2 * t + j) * RS + 32 * b + 4 * g) =
+                make_float4(st.x(b, 0, j), st.x(b, 1, j), st.x(b, 2, j), st.x(b, 3, j));
+          if (g == 0) refs[(2 * warp + slot) * kRows + 2 * t + j] = st.ref[j];
+        }
+        if (lane == 0) info[2 * warp + slot] = RecordInfo{c.start, c.k.tiles, c.b, c.r0, c.h, 1};
+      }
+      x += n;
+      if (x < end) c.next(p, prefix);
+    }
+  }
+  __syncthreads();
+
+  // --- join the records: runs of one unit, in order ---
+  const bool present = lane < 2 * kAttnWarps && info[lane].present;
+  const int64_t start = present ? info[lane].start : -1;
+  const uint32_t have = __ballot_sync(0xffffffffu, present);
+  const uint32_t below = have & ((1u << lane) - 1);
+  const int64_t before = __shfl_sync(0xffffffffu, start, below ? 31 - __clz(below) : lane);
+  const uint32_t heads_of_runs = __ballot_sync(0xffffffffu, present && (!below || before != start));
+  const int runs = __popc(heads_of_runs);
+  const int u = lane;                             // dims 4u .. 4u + 3
+  for (int item = warp; item < runs * kRows; item += kAttnWarps + 1) {
+    const int run = item / kRows, row = item % kRows;
+    const int first = int(__fns(heads_of_runs, 0, run + 1));
+    const int stop = run + 1 < runs ? int(__fns(heads_of_runs, 0, run + 2)) : 32;
+    const RecordInfo ri = info[first];
+    const Sequence s = sequence_of(p, ri.b);
+    const bool inside = ri.start >= c0 && ri.start + ri.tiles <= c1;
+    if (ri.r0 + row >= s.count * p.group) continue;
+    float top = -INFINITY;
+    for (int e = first; e < stop; ++e)
+      if ((have >> e) & 1) top = fmaxf(top, refs[e * kRows + row]);
+    float sum = 0.f;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int e = first; e < stop; ++e) {
+      if (!((have >> e) & 1)) continue;
+      const float r = refs[e * kRows + row];
+      const float f = r == -INFINITY ? 0.f : exp2f(r - top);
+      sum += f;
+      if (u < D / 4 && f != 0.f) {
+        const float* rec = (e & 1) ? reinterpret_cast<const float*>(ring + (e >> 1) * kAttnStages * TB) : heads + (e >> 1) * RF;
+        const float4 v = *reinterpret_cast<const float4*>(rec + row * RS + 4 * u);
+        a.x = fmaf(f, v.x, a.x);
+        a.y = fmaf(f, v.y, a.y);
+        a.z = fmaf(f, v.z, a.z);
+        a.w = fmaf(f, v.w, a.w);
+      }
+    }
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    a = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+    const float ref = sum != 0.f ? top + log2f(sum) : -INFINITY;
+    if (inside) {
+      if (u < D / 4) store_out(p, s, ri.h, ri.r0 + row, u, a);
+      if (lane == 0) store_lse(p, s, ri.h, ri.r0 + row, ref);
+    } else {
+      float* rec = p.partials + (cta * 2 + (ri.start >= c0 ? 1 : 0)) * (RF + kRows);
+      if (u < D / 4) *reinterpret_cast<float4*>(rec + row * RS + 4 * u) = a;
+      if (lane == 0) rec[RF + row] = ref;
+      __threadfence();
+    }
+  }
+  __syncthreads();
+  // units cut between CTAs: at most the first and the last run
+  for (int run = 0; run < runs; ++run) {
+    const RecordInfo ri = info[__fns(heads_of_runs, 0, run + 1)];
+    if (ri.start >= c0 && ri.start + ri.tiles <= c1) continue;
+    const int64_t a0 = ((ri.start + 1) * ctas - 1) / N, a1 = ((ri.start + ri.tiles) * ctas - 1) / N;
+    if (threadIdx.x == 0) {
+      __threadfence();
+      const int n = atomicAdd(&p.tickets[a0], 1) + 1;
+      shared_int[0] = n == int(a1 - a0 + 1);
+      if (shared_int[0]) p.tickets[a0] = 0;
+      __threadfence();
+    }
+    __syncthreads();
+    const bool last = shared_int[0];
+    __syncthreads();
+    if (!last) continue;
+    const Sequence s = sequence_of(p, ri.b);
+    for (int row = warp; row < kRows; row += kAttnWarps + 1) {
+      if (ri.r0 + row >= s.count * p.group) continue;
+      float top = -INFINITY;
+      for (int64_t a = a0; a <= a1; ++a)
+        top = fmaxf(top, __ldcg(p.partials + (a * 2 + (a == a0 ? 1 : 0)) * (RF + kRows) + RF + row));
+      float sum = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int64_t a = a0; a <= a1; ++a) {
+        const float* rec = p.partials + (a * 2 + (a == a0 ? 1 : 0)) * (RF + kRows);
+        const float r = __ldcg(rec + RF + row);
+        const float f = r == -INFINITY ? 0.f : exp2f(r - top);
+        sum += f;
+        if (u < D / 4 && f != 0.f) {
+          const float4 v = __ldcg(reinterpret_cast<const float4*>(rec + row * RS + 4 * u));
+          acc.x = fmaf(f, v.x, acc.x);
+          acc.y = fmaf(f, v.y, acc.y);
+          acc.z = fmaf(f, v.z, acc.z);
+          acc.w = fmaf(f, v.w, acc.w);
+        }
+      }
+      const float inv = sum != 0.f ? 1.f / sum : 0.f;
+      if (u < D / 4) store_out(p, s, ri.h, ri.r0 + row, u, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+      if (lane == 0) store_lse(p, s, ri.h, ri.r0 + row, sum != 0.f ? top + log2f(sum) : -INFINITY);
+    }
+  }
+}
+
+// SMs of the current device (0: not known); no launch, no allocation
+int sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+  return n;
+}
+
+constexpr int kMaxCtas = 256;                     // of a launch; the workspace holds as many records
+constexpr int kMaxBatch = 2048;                   // the cut is worked out in shared memory
+constexpr size_t kTicketBytes = kMaxCtas * 4;
+
+cudaError_t allow_shared(const void* kernel, int bytes) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
+template <int D, int NG, bool kTwoPlanes>
+cudaError_t launch_rows(const AttnParams& p, int ctas, cudaStream_t s) {
+  const cudaError_t err = allow_shared(reinterpret_cast<const void*>(k_attn_rows<D, NG, kTwoPlanes>),
+                                       AttnSmem<D, NG>::bytes(kMaxBatch));
+  if (err != cudaSuccess) return err;
+  k_attn_rows<D, NG, kTwoPlanes><<<ctas, (kAttnWarps + 1) * 32, AttnSmem<D, NG>::bytes(p.batch), s>>>(p);
+  return cudaSuccess;
+}
+
+template <bool kTwoPlanes>
+cudaError_t dispatch_rows(const AttnParams& p, int d, int group, int ctas, cudaStream_t s) {
+  if (d == 128 && group == 32) return launch_rows<128, 4, kTwoPlanes>(p, ctas, s);
+  if (d == 128 && group == 64) return launch_rows<128, 2, kTwoPlanes>(p, ctas, s);
+  if (d == 128) return launch_rows<128, 1, kTwoPlanes>(p, ctas, s);
+  if (group == 32) return launch_rows<64, 2, kTwoPlanes>(p, ctas, s);
+  return launch_rows<64, 1, kTwoPlanes>(p, ctas, s);
 }
 
 std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
@@ -153,6 +499,7 @@ std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a)
   if (a->q.n_heads % kv->n_kv_heads || a->q.n_heads / kv->n_kv_heads > 64)
     return "q's heads must be a multiple of n_kv_heads, at most 64 per KV head";
   if (!a->lens) return "lens is NULL";
+  if (kv->batch > kMaxBatch) return "at most 2048 sequences a call";
   if (a->n_tokens < 0 || double(a->n_tokens) * a->q.n_heads >= double(int64_t(1) << 31))
     return "n_tokens must not be negative, n_tokens * heads below 2^31";
   if (!a->q_begin && a->n_tokens % kv->batch) return "n_tokens must be a multiple of batch without q_begin";
@@ -169,9 +516,8 @@ std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a)
 using namespace reskv;
 
 extern "C" size_t reskv_paged_attn_workspace(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
-  (void)kv;
-  (void)a;
-  return 256;
+  if (!kv || !a || (kv->head_dim != 64 && kv->head_dim != 128)) return 0;
+  return kTicketBytes + size_t(kMaxCtas) * 2 * (record_floats(kv->head_dim) + kRows) * 4;
 }
 
 extern "C" reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a, void* stream) {
@@ -201,8 +547,20 @@ extern "C" reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_p
   p.window = a->window;
   p.o_f32 = a->o.dtype == RESKV_F32;
   p.scale2 = (a->scale != 0.f ? a->scale : 1.f / std::sqrt(float(kv->head_dim))) * kLog2e;
+  p.group = p.heads / p.kv_heads;
+  p.q_f16 = a->q.dtype == RESKV_F16;
+  p.q_wide = rows_aligned(a->q, 16);
+  p.o_wide = rows_aligned(a->o, size_t(4 * dtype_size(a->o.dtype)));
+  p.tickets = static_cast<int32_t*>(a->workspace);
+  p.partials = reinterpret_cast<float*>(static_cast<char*>(a->workspace) + kTicketBytes);
+  int ctas = sm_count();
+  if (ctas < 1) return launch_status("reading the SM count");
+  if (ctas > kMaxCtas) ctas = kMaxCtas;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (a->q.dtype == RESKV_F16) dispatch_attn<__half>(p, kv->head_dim, kv->quant_group, s);
-  else dispatch_attn<__nv_bfloat16>(p, kv->head_dim, kv->quant_group, s);
+  // bf16 outputs: weights in one fp16 plane (2^-11) are finer than the output's 2^-8
+  const cudaError_t err = a->o.dtype == RESKV_BF16 ? dispatch_rows<false>(p, kv->head_dim, kv->quant_group, ctas, s)
+                                                   : dispatch_rows<true>(p, kv->head_dim, kv->quant_group, ctas, s);
+  if (err != cudaSuccess)
+    return paged_fail(RESKV_ERR_CUDA, std::string("paged attention: ") + cudaGetErrorString(err));
   return launch_status("paged attention");
 }

@@ -1,0 +1,441 @@
+// Attention over the paged 4-bit cache: parameters, the split of a call's work
+// and the matrix step of one 16-token tile, shared by the kernels of
+// paged_attn*.cu.
+#pragma once
+#include "paged.cuh"
+
+namespace reskv {
+
+struct AttnParams {
+  const void* q;
+  void* o;
+  float* lse;
+  int64_t q_token, q_head, o_token, o_head;
+  const int32_t* q_begin;
+  const int32_t* lens;
+  const int32_t* page_table;
+  const uint8_t* pages;
+  uint32_t* status;
+  float* partials;                // [CTAs][2][record]
+  int32_t* tickets;               // [CTAs], zero between calls
+  int64_t n_pages, n_tokens;
+  int32_t batch, table_pages, page_tokens, kv_heads, heads, group;
+  int32_t window, q_f16, o_f32, q_wide, o_wide;
+  float scale2;                   // scale * log2 e
+};
+
+// One block of query rows of one sequence: row r of the sequence is query token
+// r / group, head r % group of the KV head.  Its tiles are those any of its rows
+// sees; one that sees nothing still counts one (empty) tile.
+struct RowBlock {
+  int first, tiles;               // first tile of the sequence's positions; count
+  bool empty;
+};
+
+struct Sequence {
+  int len, count, q0;             // held tokens, query tokens, first query token
+};
+
+__device__ __forceinline__ Sequence sequence_of(const AttnParams& p, int b) {
+  Sequence s;
+  if (p.q_begin) {
+    const int64_t lo = min(max(int64_t(p.q_begin[b]), int64_t(0)), p.n_tokens);
+    const int64_t hi = min(max(int64_t(p.q_begin[b + 1]), lo), p.n_tokens);
+    s.q0 = int(lo);
+    s.count = int(hi - lo);
+  } else {
+    s.count = int(p.n_tokens / p.batch);
+    s.q0 = b * s.count;
+  }
+  const int room = p.table_pages * p.page_tokens;      // below 2^31
+  const int len = p.lens[b];
+  if (len < 0 || len > room) report_status(p.status, kStatusBadIndex);
+  s.len = min(max(len, 0), room);
+  return s;
+}
+
+// Rows [r0, r1) of a sequence.
+__device__ __forceinline__ RowBlock row_block(const AttnParams& p, const Sequence& s, int r0, int r1) {
+  const int lo = s.len - s.count + r0 / p.group, hi = s.len - s.count + (r1 - 1) / p.group;
+  RowBlock b;
+  b.empty = hi < 0;
+  const int from = p.window > 0 ? max(0, lo - p.window + 1) : 0;
+  b.first = from / kTile;
+  b.tiles = b.empty ? 1 : hi / kTile - b.first + 1;
+  return b;
+}
+
+// --- matrix instructions -----------------------------------------------------
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                        uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+      "{%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                         uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+      "{%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+
+// what pack_f16 left over
+__device__ __forceinline__ uint32_t rest_f16(float lo, float hi, uint32_t packed) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&packed));
+  return pack_f16(lo - f.x, hi - f.y);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {          // 2^-inf = 0
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// Four 32-bit words (two for d = 64) of shared memory.
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t (&w)[N], const void* p) {
+  if constexpr (N == 4) {
+    const uint4 v = *static_cast<const uint4*>(p);
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+  } else if constexpr (N == 2) {
+    const uint2 v = *static_cast<const uint2*>(p);
+    w[0] = v.x; w[1] = v.y;
+  } else {
+    w[0] = *static_cast<const uint32_t*>(p);
+  }
+}
+
+// A row's scales and minima from its 4 NG bytes.
+template <int NG>
+__device__ __forceinline__ void load_meta(float (&s)[NG], float (&m)[NG], const uint8_t* row) {
+  uint32_t w[NG];
+  load_words<NG>(w, row);
+  if constexpr (NG == 4) {
+    s[0] = low_bf16(w[0]); s[1] = high_bf16(w[0]); s[2] = low_bf16(w[1]); s[3] = high_bf16(w[1]);
+    m[0] = low_bf16(w[2]); m[1] = high_bf16(w[2]); m[2] = low_bf16(w[3]); m[3] = high_bf16(w[3]);
+  } else if constexpr (NG == 2) {
+    s[0] = low_bf16(w[0]); s[1] = high_bf16(w[0]);
+    m[0] = low_bf16(w[1]); m[1] = high_bf16(w[1]);
+  } else {
+    s[0] = low_bf16(w[0]);
+    m[0] = high_bf16(w[0]);
+  }
+}
+
+// --- the tile step -----------------------------------------------------------
+
+// Eight query rows (columns c of the transposed logits) of one warp against
+// tiles of 16 tokens.  In units of log2, with lane = 4 g + t:
+//
+//   logits  S^T[16 tokens x 8] = sum over groups  scale * (codes Q^T) + minimum * sum Q
+//   output  O^T[dims x 8]     += codes^T (scale * P)^T,  and minima * P apart in fp32
+//
+// The codes enter the products as they lie: a masked word holds two 4-bit codes
+// n as the fp16 subnormals n 2^-24 (n 2^-20 from the odd places), which the
+// tensor cores multiply exactly, so that unpacking eight codes takes five
+// integer instructions and no conversion.  A group's scale is applied to the
+// fp32 products of the logits, and to the weights P before they are rounded to
+// fp16 (two planes, 22 bits, unless the output is bf16).  Queries are scaled by a
+// power of two to fp16's top, weights by the running reference: it follows the
+// largest logit + log2 of the token's largest value scale, so that P * scale
+// stays in fp16's range for value scales between 2^-96 and 2^96.
+//
+// The reference moves only when it is passed by more than 8 (2^14 of fp16's
+// range, where 2^6 stands for a weight of one).
+constexpr float kNoRef = -3.0e38f;
+
+template <int D, int NG, bool kTwoPlanes>
+struct TileStep {
+  static constexpr int C = D / 32;               // 32-dim blocks
+  static constexpr int PG = C / NG;              // of one group
+
+  // this lane's share of the query operand: column g
+  uint32_t qb[C][2][2];
+  uint32_t qs[2];                                // sums over groups, three bf16 planes
+  float cq[2];                                   // logit scale of columns 2t, 2t + 1
+  // running state of columns 2t, 2t + 1
+  float ref[2], l[2];
+  float o[2 * C][4];                             // m-tile j: dims 4g + 2 (j % 2), + 1 of block j / 2
+  float om[NG][2];
+
+  __device__ __forceinline__ void reset() {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      ref[i] = kNoRef;
+      l[i] = 0.f;
+#pragma unroll
+      for (int k = 0; k < NG; ++k) om[k][i] = 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < 2 * C; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[j][i] = 0.f;
+  }
+
+  // Query row of column g (NULL: no such row).  Lane t takes dims 8 (4c + t) .. + 7.
+  __device__ __forceinline__ void load_q(const AttnParams& p, const void* row, int t, int lane) {
+    float x[C][8];
+    float top = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int at = 8 * (4 * c + t);
+      if (!row) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[c][i] = 0.f;
+      } else if (p.q_wide) {
+        const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(row) + at);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 f = p.q_f16 ? __half22float2(*reinterpret_cast<const __half2*>(&w[i])) : bf16x2_to_float2(w[i]);
+          x[c][2 * i] = f.x;
+          x[c][2 * i + 1] = f.y;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          x[c][i] = p.q_f16 ? to_f32(static_cast<const __half*>(row)[at + i])
+                            : to_f32(static_cast<const __nv_bfloat16*>(row)[at + i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[c][i]));
+    }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    // 2^e * |x| < 2^15; two factors, as 2^e may pass fp32's range
+    const int e = top > 0.f && top <= 3.4e38f ? 14 - ilogbf(top) : 0;
+    const float f1 = ldexpf(1.f, e / 2), f2 = ldexpf(1.f, e - e / 2);
+    float sum[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      sum[c] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[c][i] = x[c][i] * f1 * f2;
+        sum[c] += x[c][i];
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        qb[c][j][0] = pack_f16(x[c][2 * j], x[c][4 + 2 * j]);
+        qb[c][j][1] = pack_f16(x[c][2 * j + 1] * 0.0625f, x[c][5 + 2 * j] * 0.0625f);
+      }
+      sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 1);
+      sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 2);
+    }
+    // group sums in units of the products, n 2^-24
+    float gs[NG];
+#pragma unroll
+    for (int k = 0; k < NG; ++k) {
+      gs[k] = 0.f;
+#pragma unroll
+      for (int c = 0; c < PG; ++c) gs[k] += sum[k * PG + c];
+      gs[k] *= 5.9604644775390625e-8f;
+    }
+    float plane[NG][3];
+#pragma unroll
+    for (int k = 0; k < NG; ++k) {
+      float r = gs[k];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        plane[k][i] = __bfloat162float(__float2bfloat16_rn(r));
+        r -= plane[k][i];
+      }
+    }
+    auto two = [](float lo, float hi) {            // both exact bf16
+      return (__float_as_uint(lo) >> 16) | (__float_as_uint(hi) & 0xffff0000u);
+    };
+    // k columns of the minima's product: lane t supplies columns 2t, 2t+1 and 2t+8, 2t+9
+    if constexpr (NG == 4) {
+      const int k = 2 * (t & 1), i = t >> 1;       // hi (t 0, 1), mid (t 2, 3); lo (t 0, 1)
+      qs[0] = k == 0 ? (i == 0 ? two(plane[0][0], plane[1][0]) : two(plane[0][1], plane[1][1]))
+                     : (i == 0 ? two(plane[2][0], plane[3][0]) : two(plane[2][1], plane[3][1]));
+      qs[1] = i != 0 ? 0u : k == 0 ? two(plane[0][2], plane[1][2]) : two(plane[2][2], plane[3][2]);
+    } else if constexpr (NG == 2) {
+      qs[0] = t == 0 ? two(plane[0][0], plane[1][0]) : t == 1 ? two(plane[0][1], plane[1][1])
+              : t == 2 ? two(plane[0][2], plane[1][2]) : 0u;
+      qs[1] = 0u;
+    } else {                                       // pairs (scale, minimum): zero against the scale
+      qs[0] = t == 0 ? two(0.f, plane[0][0]) : t == 1 ? two(0.f, plane[0][1]) : t == 2 ? two(0.f, plane[0][2]) : 0u;
+      qs[1] = 0u;
+    }
+    const float c = p.scale2 * 16777216.f * ldexpf(1.f, -(e / 2)) * ldexpf(1.f, -(e - e / 2));
+    cq[0] = __shfl_sync(0xffffffffu, c, 8 * (lane & 3));
+    cq[1] = __shfl_sync(0xffffffffu, c, 8 * (lane & 3) + 4);
+  }
+
+  // One tile in shared memory.  With kMask, row i (token g, g + 8) of column j
+  // takes part only where see[i][j].
+  template <bool kMask>
+  __device__ __forceinline__ void step(const uint8_t* tile, int g, int t, const bool (&see)[2][2]) {
+    constexpr TileShape ts{D, NG};
+    uint32_t kw[2][C];
+    load_words<C>(kw[0], tile + g * (D / 2) + t * (D / 8));
+    load_words<C>(kw[1], tile + (g + 8) * (D / 2) + t * (D / 8));
+    const uint8_t* kmeta = tile + ts.k_meta();
+    uint32_t r0[NG], r1[NG];
+    load_words<NG>(r0, kmeta + g * 4 * NG);
+    load_words<NG>(r1, kmeta + (g + 8) * 4 * NG);
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (NG == 4) {
+      const uint32_t m0 = (t & 1) ? r0[3] : r0[2], m1 = (t & 1) ? r1[3] : r1[2];
+      mma_bf16(acc, m0, m1, m0, m1, qs[0], qs[1]);
+    } else {
+      mma_bf16(acc, r0[NG - 1], r1[NG - 1], 0u, 0u, qs[0], 0u);
+    }
+#pragma unroll
+    for (int k = 0; k < NG; ++k) {
+      float a[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = k * PG; c < (k + 1) * PG; ++c) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t w0 = j ? kw[0][c] >> 8 : kw[0][c], w1 = j ? kw[1][c] >> 8 : kw[1][c];
+          mma_f16(a, w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, qb[c][j][0], qb[c][j][1]);
+        }
+      }
+      const float s0 = (k & 1) ? high_bf16(r0[k / 2]) : low_bf16(r0[k / 2]);
+      const float s1 = (k & 1) ? high_bf16(r1[k / 2]) : low_bf16(r1[k / 2]);
+      acc[0] = fmaf(s0, a[0], acc[0]);
+      acc[1] = fmaf(s0, a[1], acc[1]);
+      acc[2] = fmaf(s1, a[2], acc[2]);
+      acc[3] = fmaf(s1, a[3], acc[3]);
+    }
+    float vs[2][NG], vm[2][NG];
+    const uint8_t* vmeta = tile + ts.v_meta();
+    load_meta<NG>(vs[0], vm[0], vmeta + g * 4 * NG);
+    load_meta<NG>(vs[1], vm[1], vmeta + (g + 8) * 4 * NG);
+    // about log2 of each token's largest value scale (the bits of a float)
+    float sg[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float top = vs[i][0];
+#pragma unroll
+      for (int k = 1; k < NG; ++k) top = fmaxf(top, vs[i][k]);
+      sg[i] = fmaxf(fmaf(float(__float_as_int(top)), 1.1920928955078125e-7f, -127.f), -96.f);
+    }
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y[i] = fmaf(acc[i], cq[i & 1], -ref[i & 1]);
+      if (kMask && !see[i >> 1][i & 1]) y[i] = -INFINITY;
+    }
+    const float over = fmaxf(fmaxf(y[0], y[1]) + sg[0], fmaxf(y[2], y[3]) + sg[1]);
+    if (__any_sync(0xffffffffu, over > 14.f)) {
+      // a column's reference: 6 below its largest logit + log2 scale
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float top = kNoRef;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float sc = sg[i] > 128.f ? -96.f : fminf(sg[i], 96.f);     // above 128: NaN, whose rows decide nothing
+          const float x = acc[2 * i + j] * cq[j] + sc;
+          if (!kMask || see[i][j]) top = fmaxf(top, x);
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+        const float now = fmaxf(ref[j], top - 6.f);
+        const float keep = exp2f(ref[j] - now);
+        ref[j] = now;
+        l[j] *= keep;
+#pragma unroll
+        for (int k = 0; k < NG; ++k) om[k][j] *= keep;
+#pragma unroll
+        for (int m = 0; m < 2 * C; ++m) {
+          o[m][j] *= keep;
+          o[m][2 + j] *= keep;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        y[i] = fmaf(acc[i], cq[i & 1], -ref[i & 1]);
+        if (kMask && !see[i >> 1][i & 1]) y[i] = -INFINITY;
+      }
+    }
+    float w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[i] = exp2_fast(y[i]);
+      l[i & 1] += w[i];
+    }
+    uint32_t b[NG][2], b2[NG][2];
+#pragma unroll
+    for (int k = 0; k < NG; ++k) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float x0 = w[2 * i] * vs[i][k], x1 = w[2 * i + 1] * vs[i][k];
+        float m0 = w[2 * i] * vm[i][k], m1 = w[2 * i + 1] * vm[i][k];
+        if constexpr (kMask) {                   // what is not seen may be NaN
+          if (!see[i][0]) x0 = m0 = 0.f;
+          if (!see[i][1]) x1 = m1 = 0.f;
+        }
+        om[k][0] += m0;
+        om[k][1] += m1;
+        const uint32_t h = pack_f16(x0, x1);
+        b[k][i] = transpose8x8(h);
+        if constexpr (kTwoPlanes) b2[k][i] = transpose8x8(rest_f16(x0, x1, h));
+      }
+    }
+    uint32_t v0[C], v1[C];
+    const uint8_t* codes = tile + ts.v_codes();
+    load_words<C>(v0, codes + t * D + ts.v_place(t, g) * (D / 8));
+    load_words<C>(v1, codes + (t + 4) * D + ts.v_place(t + 4, g) * (D / 8));
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int k = c / PG;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t w0 = j ? v0[c] >> 8 : v0[c], w1 = j ? v1[c] >> 8 : v1[c];
+        const uint32_t a0 = w0 & 0x000f000fu, a1 = w0 & 0x00f000f0u, a2 = w1 & 0x000f000fu, a3 = w1 & 0x00f000f0u;
+        mma_f16(o[2 * c + j], a0, a1, a2, a3, b[k][0], b[k][1]);
+        if constexpr (kTwoPlanes) mma_f16(o[2 * c + j], a0, a1, a2, a3, b2[k][0], b2[k][1]);
+      }
+    }
+  }
+
+  // Sums over the lanes of a column; then o, l hold whole columns, normalised:
+  // x(c, i, j) below is the softmax's output at dim 32c + 4g + i of column 2t + j,
+  // ref its log2 of the sum of 2^logit (-inf: nothing seen).
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+      for (int s = 4; s < 32; s *= 2) {
+        l[j] += __shfl_xor_sync(0xffffffffu, l[j], s);
+#pragma unroll
+        for (int k = 0; k < NG; ++k) om[k][j] += __shfl_xor_sync(0xffffffffu, om[k][j], s);
+      }
+      const bool seen = ref[j] != kNoRef || l[j] != 0.f;
+      const float inv = seen ? 1.f / l[j] : 0.f;
+      ref[j] = seen ? ref[j] + log2f(l[j]) : -INFINITY;
+      l[j] = inv;
+    }
+  }
+  __device__ __forceinline__ float x(int c, int i, int j) const {
+    const float v = o[2 * c + i / 2][2 * (i & 1) + j] * ((i & 1) ? 1048576.f : 16777216.f);
+    return (v + om[c / PG][j]) * l[j];
+  }
+};
+
+}  // namespace reskv
