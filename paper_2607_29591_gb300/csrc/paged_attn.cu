@@ -21,13 +21,14 @@ namespace {
 // full, one bulk copy per tile, so that page lookups and copies cost the tile
 // step nothing.
 constexpr int kAttnWarps = 15;                      // computing; with the feeding warp 16, of 128 registers
-constexpr int kAttnStages = 3;
+constexpr int kAttnStages = 4;
 constexpr int kMinTiles = 2;                      // of a piece, before more CTAs are used
 constexpr int kRows = 8;                          // query rows of a unit
 
 struct RecordInfo {
   int64_t start;                                  // first tile of the record's unit
-  int tiles, b, r0, h;
+  Sequence s;
+  int tiles, r0, h;
   int present;
 };
 
@@ -47,6 +48,18 @@ struct AttnSmem {
   static_assert(kAttnStages * TileShape{D, NG}.bytes() >= record_floats(D) * 4, "a drained ring holds a record");
   static int bytes(int batch) { return fixed + (batch + 1) * 8; }
 };
+
+// floor(i * n / parts), in 32 bits where they hold (an issue of instructions: every
+// CTA works this out before its first copy).
+__device__ __forceinline__ int64_t part_begin(int64_t i, int64_t n, int parts) {
+  if (n < (1 << 22)) return int64_t(uint32_t(i) * uint32_t(n) / uint32_t(parts));
+  return i * n / parts;
+}
+// The part that holds x.
+__device__ __forceinline__ int part_of(int64_t x, int64_t n, int parts) {
+  if (n < (1 << 22)) return int((uint32_t(x + 1) * uint32_t(parts) - 1) / uint32_t(n));
+  return int(((x + 1) * parts - 1) / n);
+}
 
 struct Cursor {
   int b, r0, h, tile;                             // tile: within the unit
@@ -74,7 +87,7 @@ struct Cursor {
       if (left < n || r0 + kRows >= s.count * p.group) break;
       left -= n;
     }
-    h = min(int(left / k.tiles), p.kv_heads - 1);
+    h = min(left < (int64_t(1) << 32) ? int(uint32_t(left) / uint32_t(k.tiles)) : int(left / k.tiles), p.kv_heads - 1);
     tile = int(left - int64_t(h) * k.tiles);
     start = x - tile;
   }
@@ -148,6 +161,28 @@ __device__ __forceinline__ void copy_tile(void* dst, const void* src, uint32_t b
       : "memory");
 }
 
+// The softmaxes of up to 32 records joined: each lane's weight for its record's
+// output, from their log2 sums (-inf: an empty or no record), and the joint sum.
+struct Joined {
+  float weight, ref;
+};
+__device__ __forceinline__ Joined join_weights(float ref) {
+  float top = ref;
+#pragma unroll
+  for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const float f = ref == -INFINITY ? 0.f : exp2f(ref - top);
+  float sum = f;
+#pragma unroll
+  for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return sum != 0.f ? Joined{f / sum, top + log2f(sum)} : Joined{0.f, -INFINITY};
+}
+__device__ __forceinline__ void add_scaled(float4& a, float f, float4 v) {
+  a.x = fmaf(f, v.x, a.x);
+  a.y = fmaf(f, v.y, a.y);
+  a.z = fmaf(f, v.z, a.z);
+  a.w = fmaf(f, v.w, a.w);
+}
+
 template <int D, int NG, bool kTwoPlanes>
 __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __grid_constant__ AttnParams p) {
   using S = AttnSmem<D, NG>;
@@ -198,11 +233,11 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
   const int64_t N = prefix[p.batch];
   if (N == 0) return;
   const int64_t want = (N + kAttnWarps * kMinTiles - 1) / (kAttnWarps * kMinTiles);
-  const int64_t ctas = want < gridDim.x ? want : gridDim.x;
-  const int64_t cta = blockIdx.x;
+  const int ctas = want < gridDim.x ? int(want) : int(gridDim.x);
+  const int cta = blockIdx.x;
   if (cta >= ctas) return;
-  const int64_t c0 = cta * N / ctas, c1 = (cta + 1) * N / ctas;         // this CTA's tiles
-  auto piece = [&](int w) { return c0 + (c1 - c0) * w / kAttnWarps; };
+  const int64_t c0 = part_begin(cta, N, ctas), c1 = part_begin(cta + 1, N, ctas);      // this CTA's tiles
+  auto piece = [&](int w) { return c0 + part_begin(w, c1 - c0, kAttnWarps); };
 
   if (warp == kAttnWarps) {
     // --- the feeding warp: lane w for warp w ---
@@ -217,41 +252,64 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     uint64_t policy;
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
     const int tpp = p.page_tokens / kTile;        // tiles of a page
+    const int64_t head_bytes = int64_t(tpp) * TB;
+    const uint8_t* src = p.pages;                 // the next tile
+    int in_unit = 0, in_page = 0;                 // tiles left of the unit and of the page, the next one included
+    bool ok = false;                              // the page exists
+    int page = 0;                                 // the page after this one, asked for a page ahead
+    const int32_t* ask = p.page_table;
+    auto turn_page = [&](int first) {             // to `page`, from its tile `first`
+      ok = page >= 0 && page < p.n_pages;
+      if (!ok) report_status(p.status, kStatusBadIndex);
+      src = p.pages + (int64_t(ok ? page : 0) * p.kv_heads + c.h) * head_bytes + first * TB;
+      in_page = tpp - first;
+      ++ask;
+      if (in_unit > in_page) page = *ask;
+    };
+    auto begin_unit = [&]() {
+      in_unit = c.k.tiles - c.tile;
+      if (c.k.empty) {
+        ok = false;
+        in_page = in_unit;
+        return;
+      }
+      const int tile = c.k.first + c.tile;
+      ask = p.page_table + int64_t(c.b) * p.table_pages + tile / tpp;
+      page = *ask;
+      turn_page(tile % tpp);
+    };
+    if (x < end) begin_unit();
+    int st = 0;                                   // stage of the next tile
+    uint32_t round = 0;                           // times the ring has gone round
     int k = 0;                                    // tiles fed
-    int pg = -1, page = 0;                        // page index held in `page`
-    int64_t pg_b = -1;
     long long t0 = clock64();
     while (__any_sync(0xffffffffu, x < end)) {
       bool fed = false;
       if (x < end) {
-        const int st = k % kAttnStages;
-        uint64_t* bar = &full[w * kAttnStages + st];
-        if (k < kAttnStages || mbar_test(&vacant[w * kAttnStages + st], (k / kAttnStages - 1) & 1)) {
-          const int tile = c.k.first + c.tile;
-          bool ok = !c.k.empty;
+        const int at = w * kAttnStages + st;
+        if (round == 0 || mbar_test(&vacant[at], (round - 1) & 1)) {
+          skips[at] = !ok;
           if (ok) {
-            const int at = tile / tpp;
-            if (at != pg || c.b != pg_b) {
-              pg = at;
-              pg_b = c.b;
-              page = p.page_table[int64_t(c.b) * p.table_pages + at];
-            }
-            if (page < 0 || page >= p.n_pages) {
-              report_status(p.status, kStatusBadIndex);
-              ok = false;
-            }
-          }
-          skips[w * kAttnStages + st] = !ok;
-          if (ok) {
-            const uint8_t* src = p.pages + ((int64_t(page) * p.kv_heads + c.h) * tpp + (tile - pg * tpp)) * int64_t(TB);
-            mbar_arrive_expect_tx(bar, TB);
-            copy_tile(ring + (w * kAttnStages + st) * TB, src, TB, bar, policy);
+            mbar_arrive_expect_tx(&full[at], TB);
+            copy_tile(ring + at * TB, src, TB, &full[at], policy);
           } else {
-            mbar_arrive(bar);
+            mbar_arrive(&full[at]);
           }
+          src += TB;
           ++k;
           ++x;
-          if (++c.tile == c.k.tiles && x < end) c.next(p, prefix);
+          if (++st == kAttnStages) {
+            st = 0;
+            ++round;
+          }
+          if (--in_unit == 0) {
+            if (x < end) {
+              c.next(p, prefix);
+              begin_unit();
+            }
+          } else if (--in_page == 0) {
+            turn_page(0);
+          }
           fed = true;
         }
       }
@@ -259,7 +317,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
         t0 = clock64();
         continue;
       }
-      __nanosleep(64);
+      __nanosleep(32);
       if (clock64() - t0 > kWaitLimitCycles) {
         // a warp stopped taking tiles: let the copies in flight land, feed no more
         if (lane == 0) report_status(p.status, kStatusWaitTimeout);
@@ -350,7 +408,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
                 make_float4(st.x(b, 0, j), st.x(b, 1, j), st.x(b, 2, j), st.x(b, 3, j));
           if (g == 0) refs[(2 * warp + slot) * kRows + 2 * t + j] = st.ref[j];
         }
-        if (lane == 0) info[2 * warp + slot] = RecordInfo{c.start, c.k.tiles, c.b, c.r0, c.h, 1};
+        if (lane == 0) info[2 * warp + slot] = RecordInfo{c.start, c.s, c.k.tiles, c.r0, c.h, 1};
       }
       x += n;
       if (x < end) c.next(p, prefix);
@@ -358,97 +416,97 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
   }
   __syncthreads();
 
-  // --- join the records: runs of one unit, in order ---
+  // --- join the records: runs of one unit, in order; eight rows to eight warps ---
   const bool present = lane < 2 * kAttnWarps && info[lane].present;
   const int64_t start = present ? info[lane].start : -1;
   const uint32_t have = __ballot_sync(0xffffffffu, present);
   const uint32_t below = have & ((1u << lane) - 1);
   const int64_t before = __shfl_sync(0xffffffffu, start, below ? 31 - __clz(below) : lane);
-  const uint32_t heads_of_runs = __ballot_sync(0xffffffffu, present && (!below || before != start));
-  const int runs = __popc(heads_of_runs);
+  const uint32_t begins = __ballot_sync(0xffffffffu, present && (!below || before != start));
+  if (!begins) return;                            // the same in every warp
+  auto cut = [&](const RecordInfo& r) { return r.start < c0 || r.start + r.tiles > c1; };
+  const int row = warp & (kRows - 1);
   const int u = lane;                             // dims 4u .. 4u + 3
-  for (int item = warp; item < runs * kRows; item += kAttnWarps + 1) {
-    const int run = item / kRows, row = item % kRows;
-    const int first = int(__fns(heads_of_runs, 0, run + 1));
-    const int stop = run + 1 < runs ? int(__fns(heads_of_runs, 0, run + 2)) : 32;
-    const RecordInfo ri = info[first];
-    const Sequence s = sequence_of(p, ri.b);
-    const bool inside = ri.start >= c0 && ri.start + ri.tiles <= c1;
-    if (ri.r0 + row >= s.count * p.group) continue;
-    float top = -INFINITY;
-    for (int e = first; e < stop; ++e)
-      if ((have >> e) & 1) top = fmaxf(top, refs[e * kRows + row]);
-    float sum = 0.f;
+  int turn_of = 0;
+  for (uint32_t m = begins; m; m &= m - 1, turn_of ^= 1) {
+    if (turn_of != warp >> 3) continue;
+    const int first = __ffs(m) - 1;
+    const uint32_t after = m & (m - 1);
+    const uint32_t mine = have & ~((1u << first) - 1) & (after ? (1u << (__ffs(after) - 1)) - 1 : ~0u);
+    const RecordInfo& ri = info[first];
+    if (ri.r0 + row >= ri.s.count * p.group) continue;
+    const float ref = (mine >> lane) & 1 ? refs[lane * kRows + row] : -INFINITY;
+    const Joined j = join_weights(ref);
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int e = first; e < stop; ++e) {
-      if (!((have >> e) & 1)) continue;
-      const float r = refs[e * kRows + row];
-      const float f = r == -INFINITY ? 0.f : exp2f(r - top);
-      sum += f;
-      if (u < D / 4 && f != 0.f) {
-        const float* rec = (e & 1) ? reinterpret_cast<const float*>(ring + (e >> 1) * kAttnStages * TB) : heads + (e >> 1) * RF;
-        const float4 v = *reinterpret_cast<const float4*>(rec + row * RS + 4 * u);
-        a.x = fmaf(f, v.x, a.x);
-        a.y = fmaf(f, v.y, a.y);
-        a.z = fmaf(f, v.z, a.z);
-        a.w = fmaf(f, v.w, a.w);
-      }
+    for (uint32_t e = mine; e; e &= e - 1) {
+      const int i = __ffs(e) - 1;
+      const float f = __shfl_sync(0xffffffffu, j.weight, i);
+      const float* rec = (i & 1) ? reinterpret_cast<const float*>(ring + (i >> 1) * kAttnStages * TB) : heads + (i >> 1) * RF;
+      if (u < D / 4 && f != 0.f) add_scaled(a, f, *reinterpret_cast<const float4*>(rec + row * RS + 4 * u));
     }
-    const float inv = sum != 0.f ? 1.f / sum : 0.f;
-    a = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
-    const float ref = sum != 0.f ? top + log2f(sum) : -INFINITY;
-    if (inside) {
-      if (u < D / 4) store_out(p, s, ri.h, ri.r0 + row, u, a);
-      if (lane == 0) store_lse(p, s, ri.h, ri.r0 + row, ref);
+    if (!cut(ri)) {
+      if (u < D / 4) store_out(p, ri.s, ri.h, ri.r0 + row, u, a);
+      if (lane == 0) store_lse(p, ri.s, ri.h, ri.r0 + row, j.ref);
     } else {
       float* rec = p.partials + (cta * 2 + (ri.start >= c0 ? 1 : 0)) * (RF + kRows);
       if (u < D / 4) *reinterpret_cast<float4*>(rec + row * RS + 4 * u) = a;
-      if (lane == 0) rec[RF + row] = ref;
-      __threadfence();
+      if (lane == 0) rec[RF + row] = j.ref;
     }
   }
-  __syncthreads();
   // units cut between CTAs: at most the first and the last run
-  for (int run = 0; run < runs; ++run) {
-    const RecordInfo ri = info[__fns(heads_of_runs, 0, run + 1)];
-    if (ri.start >= c0 && ri.start + ri.tiles <= c1) continue;
-    const int64_t a0 = ((ri.start + 1) * ctas - 1) / N, a1 = ((ri.start + ri.tiles) * ctas - 1) / N;
-    if (threadIdx.x == 0) {
-      __threadfence();
-      const int n = atomicAdd(&p.tickets[a0], 1) + 1;
-      shared_int[0] = n == int(a1 - a0 + 1);
-      if (shared_int[0]) p.tickets[a0] = 0;
+  const int run_a = __ffs(begins) - 1, run_b = 31 - __clz(begins);
+  const bool cut_a = cut(info[run_a]), cut_b = run_b != run_a && cut(info[run_b]);
+  if (!cut_a && !cut_b) return;
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    const RecordInfo& ri = info[threadIdx.x ? run_b : run_a];
+    int last = 0;
+    if (threadIdx.x ? cut_b : cut_a) {
+      const int a0 = part_of(ri.start, N, ctas), a1 = part_of(ri.start + ri.tiles - 1, N, ctas);
+      __threadfence();                            // the CTA's records, ordered by the barrier
+      last = atomicAdd(&p.tickets[a0], 1) == a1 - a0;
+      if (last) p.tickets[a0] = 0;
       __threadfence();
     }
-    __syncthreads();
-    const bool last = shared_int[0];
-    __syncthreads();
-    if (!last) continue;
-    const Sequence s = sequence_of(p, ri.b);
-    for (int row = warp; row < kRows; row += kAttnWarps + 1) {
-      if (ri.r0 + row >= s.count * p.group) continue;
-      float top = -INFINITY;
-      for (int64_t a = a0; a <= a1; ++a)
-        top = fmaxf(top, __ldcg(p.partials + (a * 2 + (a == a0 ? 1 : 0)) * (RF + kRows) + RF + row));
-      float sum = 0.f;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int64_t a = a0; a <= a1; ++a) {
-        const float* rec = p.partials + (a * 2 + (a == a0 ? 1 : 0)) * (RF + kRows);
-        const float r = __ldcg(rec + RF + row);
-        const float f = r == -INFINITY ? 0.f : exp2f(r - top);
-        sum += f;
-        if (u < D / 4 && f != 0.f) {
-          const float4 v = __ldcg(reinterpret_cast<const float4*>(rec + row * RS + 4 * u));
-          acc.x = fmaf(f, v.x, acc.x);
-          acc.y = fmaf(f, v.y, acc.y);
-          acc.z = fmaf(f, v.z, acc.z);
-          acc.w = fmaf(f, v.w, acc.w);
-        }
+    shared_int[threadIdx.x] = last;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int which = 0; which < 2; ++which) {
+    if (!shared_int[which]) continue;
+    const RecordInfo& ri = info[which ? run_b : run_a];
+    if (warp >= kRows || ri.r0 + row >= ri.s.count * p.group) continue;
+    const int a0 = part_of(ri.start, N, ctas), n = part_of(ri.start + ri.tiles - 1, N, ctas) - a0 + 1;
+    // record i of the unit: the CTA it begins in keeps it second, the others first
+    auto record = [&](int i) { return p.partials + ((a0 + i) * 2 + (i == 0 ? 1 : 0)) * (RF + kRows); };
+    Joined all{0.f, -INFINITY};
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = 0; i0 < n; i0 += 32) {
+      const float ref = i0 + lane < n ? __ldcg(record(i0 + lane) + RF + row) : -INFINITY;
+      const Joined j = join_weights(ref);
+      float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+      const int stop = min(32, n - i0);
+#pragma unroll 4
+      for (int i = 0; i < stop; ++i) {
+        const float f = __shfl_sync(0xffffffffu, j.weight, i);
+        const float4 v = u < D / 4 ? __ldcg(reinterpret_cast<const float4*>(record(i0 + i) + row * RS + 4 * u))
+                                   : make_float4(0.f, 0.f, 0.f, 0.f);
+        add_scaled(b, f, f != 0.f ? v : make_float4(0.f, 0.f, 0.f, 0.f));
       }
-      const float inv = sum != 0.f ? 1.f / sum : 0.f;
-      if (u < D / 4) store_out(p, s, ri.h, ri.r0 + row, u, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-      if (lane == 0) store_lse(p, s, ri.h, ri.r0 + row, sum != 0.f ? top + log2f(sum) : -INFINITY);
+      if (n <= 32) {
+        a = b;
+        all = j;
+      } else {                                    // join the 32 with those before
+        const float two = lane == 0 ? all.ref : lane == 1 ? j.ref : -INFINITY;
+        const Joined k = join_weights(two);
+        const float fa = __shfl_sync(0xffffffffu, k.weight, 0), fb = __shfl_sync(0xffffffffu, k.weight, 1);
+        a = make_float4(a.x * fa, a.y * fa, a.z * fa, a.w * fa);
+        add_scaled(a, fb, b);
+        all = k;
+      }
     }
+    if (u < D / 4) store_out(p, ri.s, ri.h, ri.r0 + row, u, a);
+    if (lane == 0) store_lse(p, ri.s, ri.h, ri.r0 + row, all.ref);
   }
 }
 
@@ -461,7 +519,7 @@ int sm_count() {
 }
 
 constexpr int kMaxCtas = 256;                     // of a launch; the workspace holds as many records
-constexpr int kMaxBatch = 2048;                   // the cut is worked out in shared memory
+constexpr int kMaxBatch = 1024;                   // the cut is worked out in shared memory
 constexpr size_t kTicketBytes = kMaxCtas * 4;
 
 cudaError_t allow_shared(const void* kernel, int bytes) {
@@ -499,7 +557,7 @@ std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a)
   if (a->q.n_heads % kv->n_kv_heads || a->q.n_heads / kv->n_kv_heads > 64)
     return "q's heads must be a multiple of n_kv_heads, at most 64 per KV head";
   if (!a->lens) return "lens is NULL";
-  if (kv->batch > kMaxBatch) return "at most 2048 sequences a call";
+  if (kv->batch > kMaxBatch) return "at most 1024 sequences a call";
   if (a->n_tokens < 0 || double(a->n_tokens) * a->q.n_heads >= double(int64_t(1) << 31))
     return "n_tokens must not be negative, n_tokens * heads below 2^31";
   if (!a->q_begin && a->n_tokens % kv->batch) return "n_tokens must be a multiple of batch without q_begin";

@@ -69,7 +69,7 @@ __device__ __forceinline__ RowBlock row_block(const AttnParams& p, const Sequenc
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                         uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
       "{%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -78,7 +78,7 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                          uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
       "{%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -87,7 +87,7 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
 
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   uint32_t d;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
   return d;
 }
 
@@ -223,9 +223,9 @@ struct TileStep {
     }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    // 2^e * |x| < 2^15; two factors, as 2^e may pass fp32's range
-    const int e = top > 0.f && top <= 3.4e38f ? 14 - ilogbf(top) : 0;
-    const float f1 = ldexpf(1.f, e / 2), f2 = ldexpf(1.f, e - e / 2);
+    // 2^e |x| < 2^15; two factors, as 2^e may pass fp32's range
+    const int e = 141 - min(max(__float_as_int(top) >> 23, 1), 254), e1 = e >> 1, e2 = e - e1;
+    const float f1 = __int_as_float((127 + e1) << 23), f2 = __int_as_float((127 + e2) << 23);
     float sum[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -279,7 +279,7 @@ struct TileStep {
       qs[0] = t == 0 ? two(0.f, plane[0][0]) : t == 1 ? two(0.f, plane[0][1]) : t == 2 ? two(0.f, plane[0][2]) : 0u;
       qs[1] = 0u;
     }
-    const float c = p.scale2 * 16777216.f * ldexpf(1.f, -(e / 2)) * ldexpf(1.f, -(e - e / 2));
+    const float c = p.scale2 * 16777216.f * __int_as_float((127 - e1) << 23) * __int_as_float((127 - e2) << 23);
     cq[0] = __shfl_sync(0xffffffffu, c, 8 * (lane & 3));
     cq[1] = __shfl_sync(0xffffffffu, c, 8 * (lane & 3) + 4);
   }
