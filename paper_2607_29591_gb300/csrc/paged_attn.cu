@@ -1,5 +1,6 @@
 // Attention of every sequence's newest tokens over its paged 4-bit cache
 // (reskv_paged_attn).
+#include <atomic>
 #include <cmath>
 
 #include "paged_attn.cuh"
@@ -510,11 +511,15 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
   }
 }
 
-// SMs of the current device (0: not known); no launch, no allocation
-int sm_count() {
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+// SMs of a device; asked once a device (a decode step makes this call per layer)
+int sm_count(int dev) {
+  static std::atomic<int> known[64];
+  std::atomic<int>* k = dev >= 0 && dev < 64 ? &known[dev] : nullptr;
+  int n = k ? k->load(std::memory_order_relaxed) : 0;
+  if (n == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    if (k) k->store(n, std::memory_order_relaxed);
+  }
   return n;
 }
 
@@ -522,26 +527,29 @@ constexpr int kMaxCtas = 256;                     // of a launch; the workspace 
 constexpr int kMaxBatch = 1024;                   // the cut is worked out in shared memory
 constexpr size_t kTicketBytes = kMaxCtas * 4;
 
-cudaError_t allow_shared(const void* kernel, int bytes) {
-  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-}
-
 template <int D, int NG, bool kTwoPlanes>
-cudaError_t launch_rows(const AttnParams& p, int ctas, cudaStream_t s) {
-  const cudaError_t err = allow_shared(reinterpret_cast<const void*>(k_attn_rows<D, NG, kTwoPlanes>),
-                                       AttnSmem<D, NG>::bytes(kMaxBatch));
-  if (err != cudaSuccess) return err;
+cudaError_t launch_rows(const AttnParams& p, int dev, int ctas, cudaStream_t s) {
+  // the kernel's shared memory limit, raised once a device
+  static std::atomic<uint64_t> raised{0};
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+  if (!(raised.load(std::memory_order_relaxed) & bit) || !bit) {
+    const cudaError_t err = cudaFuncSetAttribute(k_attn_rows<D, NG, kTwoPlanes>,
+                                                 cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 AttnSmem<D, NG>::bytes(kMaxBatch));
+    if (err != cudaSuccess) return err;
+    raised.fetch_or(bit, std::memory_order_relaxed);
+  }
   k_attn_rows<D, NG, kTwoPlanes><<<ctas, (kAttnWarps + 1) * 32, AttnSmem<D, NG>::bytes(p.batch), s>>>(p);
   return cudaSuccess;
 }
 
 template <bool kTwoPlanes>
-cudaError_t dispatch_rows(const AttnParams& p, int d, int group, int ctas, cudaStream_t s) {
-  if (d == 128 && group == 32) return launch_rows<128, 4, kTwoPlanes>(p, ctas, s);
-  if (d == 128 && group == 64) return launch_rows<128, 2, kTwoPlanes>(p, ctas, s);
-  if (d == 128) return launch_rows<128, 1, kTwoPlanes>(p, ctas, s);
-  if (group == 32) return launch_rows<64, 2, kTwoPlanes>(p, ctas, s);
-  return launch_rows<64, 1, kTwoPlanes>(p, ctas, s);
+cudaError_t dispatch_rows(const AttnParams& p, int d, int group, int dev, int ctas, cudaStream_t s) {
+  if (d == 128 && group == 32) return launch_rows<128, 4, kTwoPlanes>(p, dev, ctas, s);
+  if (d == 128 && group == 64) return launch_rows<128, 2, kTwoPlanes>(p, dev, ctas, s);
+  if (d == 128) return launch_rows<128, 1, kTwoPlanes>(p, dev, ctas, s);
+  if (group == 32) return launch_rows<64, 2, kTwoPlanes>(p, dev, ctas, s);
+  return launch_rows<64, 1, kTwoPlanes>(p, dev, ctas, s);
 }
 
 std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
@@ -611,13 +619,15 @@ extern "C" reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_p
   p.o_wide = rows_aligned(a->o, size_t(4 * dtype_size(a->o.dtype)));
   p.tickets = static_cast<int32_t*>(a->workspace);
   p.partials = reinterpret_cast<float*>(static_cast<char*>(a->workspace) + kTicketBytes);
-  int ctas = sm_count();
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return launch_status("reading the device");
+  int ctas = sm_count(dev);
   if (ctas < 1) return launch_status("reading the SM count");
   if (ctas > kMaxCtas) ctas = kMaxCtas;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // bf16 outputs: weights in one fp16 plane (2^-11) are finer than the output's 2^-8
-  const cudaError_t err = a->o.dtype == RESKV_BF16 ? dispatch_rows<false>(p, kv->head_dim, kv->quant_group, ctas, s)
-                                                   : dispatch_rows<true>(p, kv->head_dim, kv->quant_group, ctas, s);
+  const cudaError_t err = a->o.dtype == RESKV_BF16 ? dispatch_rows<false>(p, kv->head_dim, kv->quant_group, dev, ctas, s)
+                                                   : dispatch_rows<true>(p, kv->head_dim, kv->quant_group, dev, ctas, s);
   if (err != cudaSuccess)
     return paged_fail(RESKV_ERR_CUDA, std::string("paged attention: ") + cudaGetErrorString(err));
   return launch_status("paged attention");

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -552,47 +553,82 @@ def reskv_noalloc_check_status(stream=None) -> int:
 # the full cache before compression: rotary positions and 4-bit pages
 # ---------------------------------------------------------------------------
 
+# A decode step makes these calls once per layer and token, so their arguments are
+# checked in few steps and packed into the C structs' bytes directly.
+_pack_heads = struct.Struct("Pqqii").pack            # reskv_heads
+_pack_rotation = struct.Struct("Pqii").pack          # reskv_rotation
+_pack_rows = struct.Struct("Pqqqi4x").pack           # reskv_rows
+_pack_attn = struct.Struct("PqqiiPqqiiPPPqfiPQ").pack  # reskv_paged_attn_args
 _dtypes = {}
+_direct = None
 
 
-def _code(t, what: str) -> int:
-    """RESKV_BF16, RESKV_F16 or RESKV_F32 of a tensor."""
-    if not _dtypes:
+def _calls():
+    """The paged calls with every struct passed as an address or packed bytes."""
+    global _direct
+    if _direct is None:
         import torch
-        _dtypes.update({torch.bfloat16: RESKV_BF16, torch.float16: RESKV_F16,
-                        torch.float32: RESKV_F32})
-    c = _dtypes.get(t.dtype)
-    if c is None:
-        raise ValueError(f"{what} must be bfloat16, float16 or float32, got {t.dtype}")
-    return c
+        load_library()
+        _dtypes.update({torch.bfloat16: RESKV_BF16, torch.float16: RESKV_F16, torch.float32: RESKV_F32})
+        lib = ctypes.CDLL(LIB_PATH)
+        vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+        lib.reskv_rope.argtypes = [vp, vp, i64, i32, i32, vp, vp, i32, vp, vp]
+        lib.reskv_paged_append.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+        lib.reskv_paged_gather.argtypes = [vp, vp, vp, i64, vp, vp, vp]
+        lib.reskv_paged_attn.argtypes = [vp, vp, vp]
+        for f in (lib.reskv_rope, lib.reskv_paged_append, lib.reskv_paged_gather, lib.reskv_paged_attn):
+            f.restype = i32
+        _direct = lib
+    return _direct
 
 
-def _heads(t, what: str, tokens: int, heads: Optional[int], dim: int) -> reskv_heads:
-    """reskv_heads of a CUDA tensor [tokens, heads, dim] with neighbouring elements in a row."""
+def _stream_of(stream, t) -> int:
+    """Address of the stream, by default torch's current one on the tensor's device."""
+    if stream is None:
+        import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return raw(t.device.index) if raw else torch.cuda.current_stream(t.device).cuda_stream
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _bad_heads(t, what: str, tokens: int, heads: Optional[int], dim: int):
     if not t.is_cuda:
         raise ValueError(f"{what} must be a CUDA tensor")
-    shape = t.shape
-    if len(shape) != 3 or shape[0] != tokens or shape[2] != dim or (heads is not None and shape[1] != heads):
-        raise ValueError(f"{what} must be [{tokens}, {'heads' if heads is None else heads}, {dim}], "
-                         f"got {tuple(shape)}")
-    s = t.stride()
-    if s[2] != 1:
+    if t.dtype not in _dtypes:
+        raise ValueError(f"{what} must be bfloat16, float16 or float32, got {t.dtype}")
+    if t.dim() == 3 and t.stride(2) != 1 and t.shape[2] == dim:
         raise ValueError(f"{what}: the elements of a row must lie side by side")
-    return reskv_heads(t.data_ptr(), s[0], s[1], shape[1], _code(t, what))
+    raise ValueError(f"{what} must be [{tokens}, {'heads' if heads is None else heads}, {dim}], "
+                     f"got {tuple(t.shape)}")
+
+
+def _heads(t, what: str, tokens: int, heads: Optional[int], dim: int):
+    """The fields of a reskv_heads: a CUDA tensor [tokens, heads, dim] with neighbouring elements in a row."""
+    shape, s, code = t.shape, t.stride(), _dtypes.get(t.dtype)
+    if (len(s) != 3 or s[2] != 1 or code is None or shape[0] != tokens or shape[2] != dim
+            or (heads is not None and shape[1] != heads) or not t.is_cuda):
+        _bad_heads(t, what, tokens, heads, dim)
+    return t.data_ptr(), s[0], s[1], shape[1], code
 
 
 def _ints(t, what: str, n: int) -> int:
-    """Pointer of a contiguous int32 CUDA tensor of n elements."""
+    """Address of a contiguous int32 CUDA tensor of n elements."""
     if t.numel() != n:
         raise ValueError(f"{what} must hold {n} elements, got {t.numel()}")
-    return _dptr(t, "torch.int32", what).value
+    import torch
+    if t.dtype is not torch.int32 or not t.is_cuda or not t.is_contiguous():
+        return _dptr(t, "torch.int32", what).value
+    return t.data_ptr()
 
 
-def _rotation(table, interleaved: bool) -> reskv_rotation:
-    if table.dim() != 3 or table.shape[2] != 2:
-        raise ValueError(f"table must be [positions, rot_dim / 2, 2], got {tuple(table.shape)}")
-    return reskv_rotation(_dptr(table, "torch.float32", "table").value, table.shape[0],
-                          2 * table.shape[1], 1 if interleaved else 0)
+def _rotation(table, interleaved: bool) -> bytes:
+    shape = table.shape
+    if len(shape) != 3 or shape[2] != 2:
+        raise ValueError(f"table must be [positions, rot_dim / 2, 2], got {tuple(shape)}")
+    import torch
+    if table.dtype is not torch.float32 or not table.is_cuda or not table.is_contiguous():
+        _dptr(table, "torch.float32", "table")
+    return _pack_rotation(table.data_ptr(), shape[0], 2 * shape[1], 1 if interleaved else 0)
 
 
 def reskv_rope_config_default(**fields) -> reskv_rope_config:
@@ -629,18 +665,17 @@ def reskv_rope(q, q_out, positions, table, k=None, k_out=None, interleaved: bool
         raise ValueError("k and k_out go together")
     if q.dim() != 3:
         raise ValueError(f"q must be [tokens, heads, dim], got {tuple(q.shape)}")
+    lib = _calls()
     T, H, d = q.shape
-    n = 1 if k is None else 2
-    x, y = (reskv_heads * n)(), (reskv_heads * n)()
-    x[0], y[0] = _heads(q, "q", T, None, d), _heads(q_out, "q_out", T, H, d)
+    n, x, y = 1, _pack_heads(*_heads(q, "q", T, None, d)), _pack_heads(*_heads(q_out, "q_out", T, H, d))
     if k is not None:
-        x[1] = _heads(k, "k", T, None, d)
-        y[1] = _heads(k_out, "k_out", T, x[1].n_heads, d)
-    rot = _rotation(table, interleaved)
-    _check(load_library().reskv_rope(ctypes.byref(rot), _ints(positions, "positions", T), T, d, n, x, y,
-                                     1 if backward else 0,
-                                     None if status is None else _ints(status, "status", 1),
-                                     _stream(stream)))
+        kh = _heads(k, "k", T, None, d)
+        n, x, y = 2, x + _pack_heads(*kh), y + _pack_heads(*_heads(k_out, "k_out", T, kh[3], d))
+    st = lib.reskv_rope(_rotation(table, interleaved), _ints(positions, "positions", T), T, d, n, x, y,
+                        1 if backward else 0, None if status is None else _ints(status, "status", 1),
+                        _stream_of(stream, q))
+    if st:
+        _check(st)
 
 
 def reskv_paged_head_bytes(page_tokens: int, head_dim: int, quant_group: int) -> int:
@@ -686,6 +721,8 @@ class PagedKV:
             table_pages=self.table_pages, page_tokens=self.page_tokens, n_kv_heads=self.n_kv_heads,
             head_dim=self.head_dim, quant_group=self.quant_group,
             status=_ints(self.status, "status", 1))
+        self.address = ctypes.addressof(self.struct)
+        self.attn_workspace = load_library().reskv_paged_attn_workspace(self.struct, reskv_paged_attn_args())
 
     def check_status(self) -> None:
         """Read and clear the status word (synchronises); raises if a fault was recorded."""
@@ -705,28 +742,31 @@ def reskv_paged_append(kv: PagedKV, k, v, seqs, positions, table=None, interleav
     k, v: [T, n_kv_heads, d], one of bf16, f16, f32; seqs, positions: int32 [T],
     negative positions mark padding; q, q_out: [T, heads, d].
     """
-    T = k.shape[0]
-    kh = _heads(k, "k", T, kv.n_kv_heads, kv.head_dim)
-    vh = _heads(v, "v", T, kv.n_kv_heads, kv.head_dim)
-    qh = qo = None
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
+    lib = _calls()
+    T, heads, d = k.shape[0], kv.n_kv_heads, kv.head_dim
+    kh = _pack_heads(*_heads(k, "k", T, heads, d))
+    vh = _pack_heads(*_heads(v, "v", T, heads, d))
+    qh = qo = None
     if q is not None:
-        qh = _heads(q, "q", T, None, kv.head_dim)
-        qo = _heads(q_out, "q_out", T, qh.n_heads, kv.head_dim)
-    rot = None if table is None else _rotation(table, interleaved)
-    _check(load_library().reskv_paged_append(kv.struct, T, _ints(seqs, "seqs", T),
-                                             _ints(positions, "positions", T), rot, kh, vh, qh, qo,
-                                             _stream(stream)))
+        f = _heads(q, "q", T, None, d)
+        qh, qo = _pack_heads(*f), _pack_heads(*_heads(q_out, "q_out", T, f[3], d))
+    st = lib.reskv_paged_append(kv.address, T, _ints(seqs, "seqs", T), _ints(positions, "positions", T),
+                                None if table is None else _rotation(table, interleaved), kh, vh, qh, qo,
+                                _stream_of(stream, k))
+    if st:
+        _check(st)
 
 
-def _rows(t, what: str, kv: PagedKV, n: int) -> reskv_rows:
-    if not t.is_cuda:
-        raise ValueError(f"{what} must be a CUDA tensor")
-    if tuple(t.shape) != (kv.batch, kv.n_kv_heads, n, kv.head_dim) or t.stride(3) != 1:
+def _rows(t, what: str, kv: PagedKV, n: int) -> bytes:
+    s, code = t.stride(), _dtypes.get(t.dtype)
+    if not t.is_cuda or code is None:
+        raise ValueError(f"{what} must be a CUDA tensor of bfloat16, float16 or float32")
+    if t.shape != (kv.batch, kv.n_kv_heads, n, kv.head_dim) or s[3] != 1:
         raise ValueError(f"{what} must be [{kv.batch}, {kv.n_kv_heads}, {n}, {kv.head_dim}] with neighbouring "
                          f"elements in a row, got {tuple(t.shape)}")
-    return reskv_rows(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2), _code(t, what))
+    return _pack_rows(t.data_ptr(), s[0], s[1], s[2], code)
 
 
 def reskv_paged_gather(kv: PagedKV, lens, k_out=None, v_out=None, starts=None, stream=None) -> None:
@@ -735,27 +775,28 @@ def reskv_paged_gather(kv: PagedKV, lens, k_out=None, v_out=None, starts=None, s
     positions >= lens[b] are zero.  starts, lens: int32 [batch]."""
     if k_out is None and v_out is None:
         raise ValueError("k_out or v_out is needed")
+    lib = _calls()
     n = (v_out if k_out is None else k_out).shape[2]
-    kr = None if k_out is None else _rows(k_out, "k_out", kv, n)
-    vr = None if v_out is None else _rows(v_out, "v_out", kv, n)
-    _check(load_library().reskv_paged_gather(kv.struct,
-                                             None if starts is None else _ints(starts, "starts", kv.batch),
-                                             _ints(lens, "lens", kv.batch), n, kr, vr, _stream(stream)))
+    st = lib.reskv_paged_gather(kv.address, None if starts is None else _ints(starts, "starts", kv.batch),
+                                _ints(lens, "lens", kv.batch), n,
+                                None if k_out is None else _rows(k_out, "k_out", kv, n),
+                                None if v_out is None else _rows(v_out, "v_out", kv, n),
+                                _stream_of(stream, kv.pages))
+    if st:
+        _check(st)
 
 
 _workspaces = {}
 
 
 def _workspace(device, stream: int, nbytes: int):
-    """A zeroed workspace per device and stream, kept and grown; what it grew from
-    is kept too (a captured graph may hold its address)."""
+    """Zeroed workspaces of a device and stream, the last the largest; what one
+    grew from is kept (a captured graph may hold its address)."""
     import torch
-    held = _workspaces.setdefault((device, stream), [])
-    if not held or held[-1].numel() < nbytes:
-        held.append(torch.zeros(max(nbytes, 2 * held[-1].numel() if held else 0), dtype=torch.uint8,
-                                device=device))
-        torch.cuda.current_stream(device).synchronize()
-    return held[-1]
+    held = _workspaces.setdefault((device.index, stream), [])
+    held.append(torch.zeros(nbytes, dtype=torch.uint8, device=device))
+    torch.cuda.current_stream(device).synchronize()
+    return held
 
 
 def reskv_paged_attn(kv: PagedKV, q, lens, o, q_begin=None, scale: Optional[float] = None, window: int = 0,
@@ -769,23 +810,24 @@ def reskv_paged_attn(kv: PagedKV, q, lens, o, q_begin=None, scale: Optional[floa
     for ln sum exp, or None.  workspace: zeroed uint8 tensor of at least
     reskv_paged_attn_workspace() bytes (None: one kept per stream).
     """
-    T = q.shape[0]
-    qh = _heads(q, "q", T, None, kv.head_dim)
-    a = reskv_paged_attn_args(q=qh, o=_heads(o, "o", T, qh.n_heads, kv.head_dim),
-                              lens=_ints(lens, "lens", kv.batch), n_tokens=T,
-                              scale=0.0 if scale is None else scale, window=window)
-    if lse is not None:
-        if lse.numel() != T * qh.n_heads:
-            raise ValueError(f"lse must hold {T * qh.n_heads} elements, got {lse.numel()}")
-        a.lse = _dptr(lse, "torch.float32", "lse").value
-    if q_begin is not None:
-        a.q_begin = _ints(q_begin, "q_begin", kv.batch + 1)
-    s = _stream(stream)
-    lib = load_library()
+    lib = _calls()
+    T, d, B = q.shape[0], kv.head_dim, kv.batch
+    qh = _heads(q, "q", T, None, d)
+    oh = _heads(o, "o", T, qh[3], d)
+    if lse is not None and lse.numel() != T * qh[3]:
+        raise ValueError(f"lse must hold {T * qh[3]} elements, got {lse.numel()}")
+    s = _stream_of(stream, q)
     if workspace is None:
-        workspace = _workspace(q.device, s.value or 0, lib.reskv_paged_attn_workspace(kv.struct, a))
-    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    _check(lib.reskv_paged_attn(kv.struct, a, s))
+        held = _workspaces.get((q.device.index, s))
+        if held is None or held[-1].numel() < kv.attn_workspace:
+            held = _workspace(q.device, s, kv.attn_workspace)
+        workspace = held[-1]
+    st = lib.reskv_paged_attn(kv.address, _pack_attn(
+        *qh, *oh, 0 if lse is None else _dptr(lse, "torch.float32", "lse").value,
+        0 if q_begin is None else _ints(q_begin, "q_begin", B + 1), _ints(lens, "lens", B), T,
+        0.0 if scale is None else scale, window, workspace.data_ptr(), workspace.numel()), s)
+    if st:
+        _check(st)
 
 
 def reskv_paged_attn_workspace(kv: PagedKV, n_tokens: int, heads: int) -> int:

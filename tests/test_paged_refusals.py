@@ -36,6 +36,12 @@ def test_struct_layouts_match_c(lib, tmp_path):
     assert got == want
 
 
+def test_packed_structs_have_the_structs_sizes():
+    import struct
+    for f, s in (("Pqqii", R.reskv_heads), ("Pqii", R.reskv_rotation), ("Pqqqi4x", R.reskv_rows), ("PqqiiPqqiiPPPqfiPQ", R.reskv_paged_attn_args)):
+        assert struct.calcsize(f) == ctypes.sizeof(s)
+
+
 def refused(lib, status, word, st=R.RESKV_ERR_INVALID_ARG):
     assert status == st and word in R.reskv_last_error(), (status, R.reskv_last_error())
 
