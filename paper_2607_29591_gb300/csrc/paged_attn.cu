@@ -8,7 +8,7 @@
 namespace reskv {
 namespace {
 
-// --- few query rows: one warp, one block of 8 rows ---------------------------
+// --- few query rows: one warp, one block of rows ---------------------------
 //
 // A call's work is a list of units, one per (sequence, block of 8 query rows, KV
 // head), each a run of 16-token tiles.  The tiles of all units, laid end to end,
@@ -24,7 +24,7 @@ namespace {
 constexpr int kAttnWarps = 15;                      // computing; with the feeding warp 16, of 128 registers
 constexpr int kAttnStages = 4;
 constexpr int kMinTiles = 2;                      // of a piece, before more CTAs are used
-constexpr int kRows = 8;                          // query rows of a unit
+constexpr int kWholeTiles = 135;                  // 9 a warp
 
 struct RecordInfo {
   int64_t start;                                  // first tile of the record's unit
@@ -34,19 +34,19 @@ struct RecordInfo {
 };
 
 __host__ __device__ constexpr int record_stride(int d) { return d + 4; }          // floats of a row: spreads rows over banks
-__host__ __device__ constexpr int record_floats(int d) { return kRows * record_stride(d); }
+__host__ __device__ constexpr int record_floats(int d, int rows) { return rows * record_stride(d); }
 
-template <int D, int NG>
+template <int D, int NG, int R>
 struct AttnSmem {
   static constexpr int ring = kAttnWarps * kAttnStages * TileShape{D, NG}.bytes();
-  static constexpr int heads = kAttnWarps * record_floats(D) * 4;
-  static constexpr int refs = 2 * kAttnWarps * kRows * 4;
+  static constexpr int heads = kAttnWarps * record_floats(D, R) * 4;
+  static constexpr int refs = 2 * kAttnWarps * R * 4;
   static constexpr int info = 2 * kAttnWarps * int(sizeof(RecordInfo));
   static constexpr int bars = 2 * kAttnWarps * kAttnStages * 8;
   static constexpr int skips = kAttnWarps * kAttnStages * 4;
   static constexpr int fixed = (ring + heads + refs + info + bars + skips + 16 + 15) / 16 * 16;
   static_assert((ring + heads + refs) % 8 == 0 && (ring + heads + refs + info) % 8 == 0 && ring % 16 == 0, "alignment");
-  static_assert(kAttnStages * TileShape{D, NG}.bytes() >= record_floats(D) * 4, "a drained ring holds a record");
+  static_assert(kAttnStages * TileShape{D, NG}.bytes() >= record_floats(D, R) * 4, "a drained ring holds a record");
   static int bytes(int batch) { return fixed + (batch + 1) * 8; }
 };
 
@@ -62,7 +62,13 @@ __device__ __forceinline__ int part_of(int64_t x, int64_t n, int parts) {
   return int(((x + 1) * parts - 1) / n);
 }
 
-struct Cursor {
+// Tiles and units of all sequences before one, in one word.
+constexpr int kUnitBits = 24;
+__device__ __forceinline__ int64_t tiles_of(int64_t x) { return x >> kUnitBits; }
+__device__ __forceinline__ int64_t units_of(int64_t x) { return x & ((int64_t(1) << kUnitBits) - 1); }
+
+template <int R>
+struct RowCursor {
   int b, r0, h, tile;                             // tile: within the unit
   Sequence s;
   RowBlock k;
@@ -70,36 +76,56 @@ struct Cursor {
 
   __device__ __forceinline__ void block(const AttnParams& p) {
     const int rows = s.count * p.group;
-    k = row_block(p, s, r0, min(r0 + kRows, rows));
+    k = row_block(p, s, r0, min(r0 + R, rows));
   }
   __device__ void locate(const AttnParams& p, const int64_t* prefix, int64_t x) {
-    int lo = 0, hi = p.batch;                     // prefix[lo] <= x < prefix[hi]
+    int lo = 0, hi = p.batch;                     // tiles before lo <= x < tiles before hi
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (prefix[mid] <= x) lo = mid;
+      if (tiles_of(prefix[mid]) <= x) lo = mid;
       else hi = mid;
     }
     b = lo;
     s = sequence_of(p, b);
-    int64_t left = x - prefix[b];
-    for (r0 = 0;; r0 += kRows) {
+    int64_t left = x - tiles_of(prefix[b]);
+    for (r0 = 0;; r0 += R) {
       block(p);
       const int64_t n = int64_t(k.tiles) * p.kv_heads;
-      if (left < n || r0 + kRows >= s.count * p.group) break;
+      if (left < n || r0 + R >= s.count * p.group) break;
       left -= n;
     }
     h = min(left < (int64_t(1) << 32) ? int(uint32_t(left) / uint32_t(k.tiles)) : int(left / k.tiles), p.kv_heads - 1);
     tile = int(left - int64_t(h) * k.tiles);
     start = x - tile;
   }
+  // first tile of unit i
+  static __device__ int64_t unit_start(const AttnParams& p, const int64_t* prefix, int64_t i) {
+    if (i >= units_of(prefix[p.batch])) return tiles_of(prefix[p.batch]);
+    int lo = 0, hi = p.batch;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (units_of(prefix[mid]) <= i) lo = mid;
+      else hi = mid;
+    }
+    RowCursor c;
+    c.b = lo;
+    c.s = sequence_of(p, lo);
+    int left = int(i - units_of(prefix[lo]));
+    int64_t x = tiles_of(prefix[lo]);
+    for (c.r0 = 0;; c.r0 += R, left -= p.kv_heads) {
+      c.block(p);
+      if (left < p.kv_heads) return x + int64_t(left) * c.k.tiles;
+      x += int64_t(c.k.tiles) * p.kv_heads;
+    }
+  }
   __device__ void next(const AttnParams& p, const int64_t* prefix) {
     start += k.tiles;
     tile = 0;
     if (++h < p.kv_heads) return;
     h = 0;
-    r0 += kRows;
+    r0 += R;
     if (r0 >= s.count * p.group) {
-      do ++b; while (b < p.batch && prefix[b + 1] == prefix[b]);
+      do ++b; while (b < p.batch && prefix[b + 1] == prefix[b]);        // without queries
       if (b >= p.batch) return;
       s = sequence_of(p, b);
       r0 = 0;
@@ -184,11 +210,13 @@ __device__ __forceinline__ void add_scaled(float4& a, float f, float4 v) {
   a.w = fmaf(f, v.w, a.w);
 }
 
-template <int D, int NG, bool kTwoPlanes>
+template <int D, int NG, bool kTwoPlanes, int R>
 __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __grid_constant__ AttnParams p) {
-  using S = AttnSmem<D, NG>;
+  using S = AttnSmem<D, NG, R>;
+  using Cursor = RowCursor<R>;
+  constexpr int kRows = R;
   constexpr TileShape ts{D, NG};
-  constexpr int TB = ts.bytes(), RS = record_stride(D), RF = record_floats(D);
+  constexpr int TB = ts.bytes(), RS = record_stride(D), RF = record_floats(D, R);
   extern __shared__ __align__(128) uint8_t smem[];
   uint8_t* ring = smem;
   float* heads = reinterpret_cast<float*>(smem + S::ring);
@@ -200,14 +228,23 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
   int* shared_int = skips + kAttnWarps * kAttnStages;                 // [4]
   int64_t* prefix = reinterpret_cast<int64_t*>(smem + S::fixed);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) shared_int[2] = 0;
+  if (p.batch > 1) __syncthreads();
 
   // the tiles of every sequence, and what they sum up to
   for (int b = threadIdx.x; b < p.batch; b += blockDim.x) {
     const Sequence s = sequence_of(p, b);
     const int rows = s.count * p.group;
     int64_t n = 0;
-    for (int r0 = 0; r0 < rows; r0 += kRows) n += row_block(p, s, r0, min(r0 + kRows, rows)).tiles;
-    prefix[b + 1] = n * p.kv_heads;
+    int longest = 0;
+    for (int r0 = 0; r0 < rows; r0 += kRows) {
+      const int k = row_block(p, s, r0, min(r0 + kRows, rows)).tiles;
+      n += k;
+      longest = max(longest, k);
+    }
+    prefix[b + 1] = (n * p.kv_heads << kUnitBits) + int64_t((rows + kRows - 1) / kRows) * p.kv_heads;
+    if (p.batch == 1) shared_int[2] = longest;
+    else atomicMax(&shared_int[2], longest);
   }
   if (threadIdx.x < 2 * kAttnWarps) info[threadIdx.x].present = 0;
   if (threadIdx.x < kAttnWarps * kAttnStages) {
@@ -231,13 +268,27 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     }
   }
   __syncthreads();
-  const int64_t N = prefix[p.batch];
+  const int64_t N = tiles_of(prefix[p.batch]);
   if (N == 0) return;
-  const int64_t want = (N + kAttnWarps * kMinTiles - 1) / (kAttnWarps * kMinTiles);
-  const int ctas = want < gridDim.x ? int(want) : int(gridDim.x);
+  int ctas = gridDim.x;
+  if (N < int64_t(ctas) * kAttnWarps * kMinTiles) ctas = (int(N) + kAttnWarps * kMinTiles - 1) / (kAttnWarps * kMinTiles);
   const int cta = blockIdx.x;
+  // Whole units to every CTA where that costs it few tiles more than equal pieces:
+  // joining records across CTAs takes about the time of kWholeTiles tiles.
+  const int units = int(units_of(prefix[p.batch]));
+  const int whole_ctas = min(units, int(gridDim.x));
+  const int64_t most = int64_t((units + whole_ctas - 1) / whole_ctas) * shared_int[2];
+  const bool whole = most <= part_begin(1, N, ctas) + kWholeTiles;
+  if (whole) ctas = whole_ctas;
   if (cta >= ctas) return;
-  const int64_t c0 = part_begin(cta, N, ctas), c1 = part_begin(cta + 1, N, ctas);      // this CTA's tiles
+  int64_t c0, c1;                                 // this CTA's tiles
+  if (whole) {
+    c0 = Cursor::unit_start(p, prefix, part_begin(cta, units, ctas));
+    c1 = Cursor::unit_start(p, prefix, part_begin(cta + 1, units, ctas));
+  } else {
+    c0 = part_begin(cta, N, ctas);
+    c1 = part_begin(cta + 1, N, ctas);
+  }
   auto piece = [&](int w) { return c0 + part_begin(w, c1 - c0, kAttnWarps); };
 
   if (warp == kAttnWarps) {
@@ -330,30 +381,30 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     }
   } else {
     // --- a computing warp ---
-    const int g = lane >> 2, t = lane & 3;
     int64_t x = piece(warp);
     const int64_t end = piece(warp + 1);
     Cursor c{};
     if (x < end) c.locate(p, prefix, x);
-    TileStep<D, NG, kTwoPlanes> st;
+    TileStep<D, NG, kTwoPlanes, R> st;
+    st.init(lane);
     int k = 0;
     bool failed = false;
     while (x < end && !failed) {
       const int n = int(min(int64_t(c.k.tiles - c.tile), end - x));
       const int rows = c.s.count * p.group;
       {
-        const int r = c.r0 + g;
+        const int r = c.r0 + (st.g & (R - 1));
         const void* row = nullptr;
         if (r < rows)
           row = static_cast<const uint16_t*>(p.q) + (c.s.q0 + r / p.group) * p.q_token +
                 int64_t(c.h * p.group + r % p.group) * p.q_head;
-        st.load_q(p, row, t, lane);
+        st.load_q(p, row);
       }
       // positions the lane's columns see; rows that do not exist see what the last one does
       int lo[2], hi[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        hi[j] = c.s.len - c.s.count + min(c.r0 + 2 * t + j, rows - 1) / p.group;
+        hi[j] = c.s.len - c.s.count + min(c.r0 + st.row(j), rows - 1) / p.group;
         lo[j] = p.window > 0 ? max(0, hi[j] - p.window + 1) : 0;
       }
       const int all_hi = c.s.len - c.s.count + c.r0 / p.group;
@@ -371,13 +422,13 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
           const uint8_t* tile = ring + stage * TB;
           bool see[2][2] = {{true, true}, {true, true}};
           if (pos >= all_lo && pos + kTile - 1 <= all_hi) {
-            st.template step<false>(tile, g, t, see);
+            st.template step<false>(tile, see);
           } else {
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
-              for (int j = 0; j < 2; ++j) see[r][j] = pos + g + 8 * r >= lo[j] && pos + g + 8 * r <= hi[j];
-            st.template step<true>(tile, g, t, see);
+              for (int j = 0; j < 2; ++j) see[r][j] = pos + st.g + 8 * r >= lo[j] && pos + st.g + 8 * r <= hi[j];
+            st.template step<true>(tile, see);
           }
         }
         __syncwarp();
@@ -388,36 +439,33 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
         break;
       }
       st.finish();
-      if (c.tile == 0 && n == c.k.tiles) {        // the whole unit
+      const bool unit = c.tile == 0 && n == c.k.tiles;
+      // else a record: begun before this piece, or cut off at its end
+      const int slot = c.tile > 0 ? 0 : 1;
+      float* rec = slot == 0 ? heads + warp * RF : reinterpret_cast<float*>(ring + warp * kAttnStages * TB);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int r = c.r0 + 2 * t + j;
-          if (r >= rows) continue;
+      for (int j = 0; j < 2; ++j) {
+        const int r = st.row(j);
 #pragma unroll
-          for (int b = 0; b < D / 32; ++b)
-            store_out(p, c.s, c.h, r, 8 * b + g, make_float4(st.x(b, 0, j), st.x(b, 1, j), st.x(b, 2, j), st.x(b, 3, j)));
-          if (g == 0) store_lse(p, c.s, c.h, r, st.ref[j]);
+        for (int b = 0; b < st.H; ++b) {
+          const float4 v = make_float4(st.out(b, 0, j), st.out(b, 1, j), st.out(b, 2, j), st.out(b, 3, j));
+          const int u = 8 * st.block(b) + st.g;
+          if (!unit) *reinterpret_cast<float4*>(rec + r * RS + 4 * u) = v;
+          else if (c.r0 + r < rows) store_out(p, c.s, c.h, c.r0 + r, u, v);
         }
-      } else {                                    // a record: begun before this piece, or cut off at its end
-        const int slot = c.tile > 0 ? 0 : 1;
-        float* rec = slot == 0 ? heads + warp * RF : reinterpret_cast<float*>(ring + warp * kAttnStages * TB);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-#pragma unroll
-          for (int b = 0; b < D / 32; ++b)
-            *reinterpret_cast<float4*>(rec + (2 * t + j) * RS + 32 * b + 4 * g) =
-                make_float4(st.x(b, 0, j), st.x(b, 1, j), st.x(b, 2, j), st.x(b, 3, j));
-          if (g == 0) refs[(2 * warp + slot) * kRows + 2 * t + j] = st.ref[j];
+        if (st.g == 0 && st.half == 0) {
+          if (!unit) refs[(2 * warp + slot) * kRows + r] = st.ref[j];
+          else if (c.r0 + r < rows) store_lse(p, c.s, c.h, c.r0 + r, st.ref[j]);
         }
-        if (lane == 0) info[2 * warp + slot] = RecordInfo{c.start, c.s, c.k.tiles, c.r0, c.h, 1};
       }
+      if (!unit && lane == 0) info[2 * warp + slot] = RecordInfo{c.start, c.s, c.k.tiles, c.r0, c.h, 1};
       x += n;
       if (x < end) c.next(p, prefix);
     }
   }
   __syncthreads();
 
-  // --- join the records: runs of one unit, in order; eight rows to eight warps ---
+  // --- join the records: runs of one unit, in order; its rows to as many warps ---
   const bool present = lane < 2 * kAttnWarps && info[lane].present;
   const int64_t start = present ? info[lane].start : -1;
   const uint32_t have = __ballot_sync(0xffffffffu, present);
@@ -429,8 +477,8 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
   const int row = warp & (kRows - 1);
   const int u = lane;                             // dims 4u .. 4u + 3
   int turn_of = 0;
-  for (uint32_t m = begins; m; m &= m - 1, turn_of ^= 1) {
-    if (turn_of != warp >> 3) continue;
+  for (uint32_t m = begins; m; m &= m - 1, ++turn_of) {
+    if (turn_of % (16 / kRows) != warp / kRows) continue;
     const int first = __ffs(m) - 1;
     const uint32_t after = m & (m - 1);
     const uint32_t mine = have & ~((1u << first) - 1) & (after ? (1u << (__ffs(after) - 1)) - 1 : ~0u);
@@ -527,29 +575,29 @@ constexpr int kMaxCtas = 256;                     // of a launch; the workspace 
 constexpr int kMaxBatch = 1024;                   // the cut is worked out in shared memory
 constexpr size_t kTicketBytes = kMaxCtas * 4;
 
-template <int D, int NG, bool kTwoPlanes>
+template <int D, int NG, bool kTwoPlanes, int R>
 cudaError_t launch_rows(const AttnParams& p, int dev, int ctas, cudaStream_t s) {
   // the kernel's shared memory limit, raised once a device
   static std::atomic<uint64_t> raised{0};
   const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
   if (!(raised.load(std::memory_order_relaxed) & bit) || !bit) {
-    const cudaError_t err = cudaFuncSetAttribute(k_attn_rows<D, NG, kTwoPlanes>,
+    const cudaError_t err = cudaFuncSetAttribute(k_attn_rows<D, NG, kTwoPlanes, R>,
                                                  cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 AttnSmem<D, NG>::bytes(kMaxBatch));
+                                                 AttnSmem<D, NG, R>::bytes(kMaxBatch));
     if (err != cudaSuccess) return err;
     raised.fetch_or(bit, std::memory_order_relaxed);
   }
-  k_attn_rows<D, NG, kTwoPlanes><<<ctas, (kAttnWarps + 1) * 32, AttnSmem<D, NG>::bytes(p.batch), s>>>(p);
+  k_attn_rows<D, NG, kTwoPlanes, R><<<ctas, (kAttnWarps + 1) * 32, AttnSmem<D, NG, R>::bytes(p.batch), s>>>(p);
   return cudaSuccess;
 }
 
-template <bool kTwoPlanes>
+template <bool kTwoPlanes, int R>
 cudaError_t dispatch_rows(const AttnParams& p, int d, int group, int dev, int ctas, cudaStream_t s) {
-  if (d == 128 && group == 32) return launch_rows<128, 4, kTwoPlanes>(p, dev, ctas, s);
-  if (d == 128 && group == 64) return launch_rows<128, 2, kTwoPlanes>(p, dev, ctas, s);
-  if (d == 128) return launch_rows<128, 1, kTwoPlanes>(p, dev, ctas, s);
-  if (group == 32) return launch_rows<64, 2, kTwoPlanes>(p, dev, ctas, s);
-  return launch_rows<64, 1, kTwoPlanes>(p, dev, ctas, s);
+  if (d == 128 && group == 32) return launch_rows<128, 4, kTwoPlanes, R>(p, dev, ctas, s);
+  if (d == 128 && group == 64) return launch_rows<128, 2, kTwoPlanes, R>(p, dev, ctas, s);
+  if (d == 128) return launch_rows<128, 1, kTwoPlanes, R>(p, dev, ctas, s);
+  if (group == 32) return launch_rows<64, 2, kTwoPlanes, R>(p, dev, ctas, s);
+  return launch_rows<64, 1, kTwoPlanes, R>(p, dev, ctas, s);
 }
 
 std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
@@ -568,6 +616,9 @@ std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a)
   if (kv->batch > kMaxBatch) return "at most 1024 sequences a call";
   if (a->n_tokens < 0 || double(a->n_tokens) * a->q.n_heads >= double(int64_t(1) << 31))
     return "n_tokens must not be negative, n_tokens * heads below 2^31";
+  // units: at most one more per sequence than full blocks of rows
+  if ((double(a->n_tokens) * (a->q.n_heads / kv->n_kv_heads) / 4 + kv->batch) * kv->n_kv_heads >= double(1 << kUnitBits))
+    return "n_tokens * heads / 4 + batch * n_kv_heads must be below 2^24";
   if (!a->q_begin && a->n_tokens % kv->batch) return "n_tokens must be a multiple of batch without q_begin";
   if (a->lse && !aligned_to(a->lse, 4)) return "lse must be 4-byte aligned";
   if (!a->workspace || !aligned_to(a->workspace, 256) || a->workspace_bytes < reskv_paged_attn_workspace(kv, a))
@@ -583,7 +634,7 @@ using namespace reskv;
 
 extern "C" size_t reskv_paged_attn_workspace(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
   if (!kv || !a || (kv->head_dim != 64 && kv->head_dim != 128)) return 0;
-  return kTicketBytes + size_t(kMaxCtas) * 2 * (record_floats(kv->head_dim) + kRows) * 4;
+  return kTicketBytes + size_t(kMaxCtas) * 2 * (record_floats(kv->head_dim, 8) + 8) * 4;
 }
 
 extern "C" reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a, void* stream) {
@@ -625,9 +676,13 @@ extern "C" reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_p
   if (ctas < 1) return launch_status("reading the SM count");
   if (ctas > kMaxCtas) ctas = kMaxCtas;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  // bf16 outputs: weights in one fp16 plane (2^-11) are finer than the output's 2^-8
-  const cudaError_t err = a->o.dtype == RESKV_BF16 ? dispatch_rows<false>(p, kv->head_dim, kv->quant_group, dev, ctas, s)
-                                                   : dispatch_rows<true>(p, kv->head_dim, kv->quant_group, dev, ctas, s);
+  // bf16 outputs: weights in one fp16 plane (2^-11) are finer than the output's 2^-8.
+  // Four rows a unit where a sequence has no more on average.
+  const bool one = a->o.dtype == RESKV_BF16, few = a->n_tokens * p.group <= 4 * int64_t(kv->batch);
+  const cudaError_t err = one ? (few ? dispatch_rows<false, 4>(p, kv->head_dim, kv->quant_group, dev, ctas, s)
+                                     : dispatch_rows<false, 8>(p, kv->head_dim, kv->quant_group, dev, ctas, s))
+                              : (few ? dispatch_rows<true, 4>(p, kv->head_dim, kv->quant_group, dev, ctas, s)
+                                     : dispatch_rows<true, 8>(p, kv->head_dim, kv->quant_group, dev, ctas, s));
   if (err != cudaSuccess)
     return paged_fail(RESKV_ERR_CUDA, std::string("paged attention: ") + cudaGetErrorString(err));
   return launch_status("paged attention");

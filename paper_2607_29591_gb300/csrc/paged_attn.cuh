@@ -145,8 +145,8 @@ __device__ __forceinline__ void load_meta(float (&s)[NG], float (&m)[NG], const 
 
 // --- the tile step -----------------------------------------------------------
 
-// Eight query rows (columns c of the transposed logits) of one warp against
-// tiles of 16 tokens.  In units of log2, with lane = 4 g + t:
+// R (8 or 4) query rows of one warp against tiles of 16 tokens.  In units of log2,
+// with lane = 4 g + t:
 //
 //   logits  S^T[16 tokens x 8] = sum over groups  scale * (codes Q^T) + minimum * sum Q
 //   output  O^T[dims x 8]     += codes^T (scale * P)^T,  and minima * P apart in fp32
@@ -163,21 +163,42 @@ __device__ __forceinline__ void load_meta(float (&s)[NG], float (&m)[NG], const 
 //
 // The reference moves only when it is passed by more than 8 (2^14 of fp16's
 // range, where 2^6 stands for a weight of one).
+//
+// Eight rows fill the eight columns of a product.  Four rows take the columns
+// twice: 0..3 for the first half of a row's groups, 4..7 for the second (zeros in
+// the query operand keep the halves apart; one shuffle adds their logits), and in
+// the output's product dims of the first half are its rows 0..7, of the second
+// rows 8..15.  A lane then scales and rounds the weights of half the groups:
+// 20 % fewer instructions a tile, and those bound the kernel.
 constexpr float kNoRef = -3.0e38f;
 
-template <int D, int NG, bool kTwoPlanes>
+template <int D, int NG, bool kTwoPlanes, int R>
 struct TileStep {
+  static constexpr int kRows = R;
+  static constexpr bool kHalves = R == 4;
   static constexpr int C = D / 32;               // 32-dim blocks
-  static constexpr int PG = C / NG;              // of one group
+  static constexpr int H = kHalves ? C / 2 : C;  // of them per lane
+  static constexpr int K = kHalves && NG > 1 ? NG / 2 : NG;         // groups per lane
+  static constexpr int PG = H / K;               // blocks of one group
 
-  // this lane's share of the query operand: column g
-  uint32_t qb[C][2][2];
+  // this lane's share of the query operand, column g: block c, code place 0..3
+  uint32_t qb[kHalves ? 2 * H : H][4];
   uint32_t qs[2];                                // sums over groups, three bf16 planes
-  float cq[2];                                   // logit scale of columns 2t, 2t + 1
-  // running state of columns 2t, 2t + 1
+  float cq[2];                                   // logit scale of this lane's rows
+  // running state of rows row(j)
   float ref[2], l[2];
-  float o[2 * C][4];                             // m-tile j: dims 4g + 2 (j % 2), + 1 of block j / 2
-  float om[NG][2];
+  float o[2 * C][4];
+  float om[K][2];
+  int t, g, half;
+
+  __device__ __forceinline__ void init(int lane) {
+    g = lane >> 2;
+    t = lane & 3;
+    half = kHalves ? t >> 1 : 0;
+  }
+  __device__ __forceinline__ int row(int j) const { return (kHalves ? 2 * (t & 1) : 2 * t) + j; }
+  // the 32-dim block that out(c, ., .) is of
+  __device__ __forceinline__ int block(int c) const { return c + half * H; }
 
   __device__ __forceinline__ void reset() {
 #pragma unroll
@@ -185,7 +206,7 @@ struct TileStep {
       ref[i] = kNoRef;
       l[i] = 0.f;
 #pragma unroll
-      for (int k = 0; k < NG; ++k) om[k][i] = 0.f;
+      for (int k = 0; k < K; ++k) om[k][i] = 0.f;
     }
 #pragma unroll
     for (int j = 0; j < 2 * C; ++j)
@@ -193,18 +214,19 @@ struct TileStep {
       for (int i = 0; i < 4; ++i) o[j][i] = 0.f;
   }
 
-  // Query row of column g (NULL: no such row).  Lane t takes dims 8 (4c + t) .. + 7.
-  __device__ __forceinline__ void load_q(const AttnParams& p, const void* row, int t, int lane) {
-    float x[C][8];
+  // Query row of column g (g & 3 of four; NULL: no such row).  Lane t takes dims 8 (4c + t) .. + 7 of blocks c.
+  __device__ __forceinline__ void load_q(const AttnParams& p, const void* qrow) {
+    const int second = kHalves ? g >> 2 : 0;
+    float x[H][8];
     float top = 0.f;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int at = 8 * (4 * c + t);
-      if (!row) {
+    for (int c = 0; c < H; ++c) {
+      const int at = 8 * (4 * (c + second * H) + t);
+      if (!qrow) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[c][i] = 0.f;
       } else if (p.q_wide) {
-        const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(row) + at);
+        const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(qrow) + at);
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -215,47 +237,55 @@ struct TileStep {
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          x[c][i] = p.q_f16 ? to_f32(static_cast<const __half*>(row)[at + i])
-                            : to_f32(static_cast<const __nv_bfloat16*>(row)[at + i]);
+          x[c][i] = p.q_f16 ? to_f32(static_cast<const __half*>(qrow)[at + i])
+                            : to_f32(static_cast<const __nv_bfloat16*>(qrow)[at + i]);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[c][i]));
     }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    if constexpr (kHalves) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
     // 2^e |x| < 2^15; two factors, as 2^e may pass fp32's range
     const int e = 141 - min(max(__float_as_int(top) >> 23, 1), 254), e1 = e >> 1, e2 = e - e1;
     const float f1 = __int_as_float((127 + e1) << 23), f2 = __int_as_float((127 + e2) << 23);
-    float sum[C];
+    float gs[NG];                                // group sums in units of the products, n 2^-24
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      sum[c] = 0.f;
+    for (int k = 0; k < NG; ++k) gs[k] = 0.f;
+#pragma unroll
+    for (int c = 0; c < H; ++c) {
+      float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         x[c][i] = x[c][i] * f1 * f2;
-        sum[c] += x[c][i];
+        sum += x[c][i];
       }
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        qb[c][j][0] = pack_f16(x[c][2 * j], x[c][4 + 2 * j]);
-        qb[c][j][1] = pack_f16(x[c][2 * j + 1] * 0.0625f, x[c][5 + 2 * j] * 0.0625f);
+      for (int j = 0; j < 4; ++j) {
+        const float f = j & 1 ? 0.0625f : 1.f;
+        const uint32_t w = pack_f16(x[c][j] * f, x[c][4 + j] * f);
+        if constexpr (kHalves) {
+          qb[c][j] = second ? 0u : w;
+          qb[H + c][j] = second ? w : 0u;
+        } else {
+          qb[c][j] = w;
+        }
       }
-      sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 1);
-      sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 2);
-    }
-    // group sums in units of the products, n 2^-24
-    float gs[NG];
-#pragma unroll
-    for (int k = 0; k < NG; ++k) {
-      gs[k] = 0.f;
-#pragma unroll
-      for (int c = 0; c < PG; ++c) gs[k] += sum[k * PG + c];
-      gs[k] *= 5.9604644775390625e-8f;
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      sum *= 5.9604644775390625e-8f;
+      if constexpr (kHalves) {
+        const float other = __shfl_xor_sync(0xffffffffu, sum, 16);
+        gs[c / PG] += second ? other : sum;
+        gs[NG == 1 ? 0 : K + c / PG] += second ? sum : other;
+      } else {
+        gs[c / PG] += sum;
+      }
     }
     float plane[NG][3];
 #pragma unroll
     for (int k = 0; k < NG; ++k) {
-      float r = gs[k];
+      float r = second ? 0.f : gs[k];            // counted once
 #pragma unroll
       for (int i = 0; i < 3; ++i) {
         plane[k][i] = __bfloat162float(__float2bfloat16_rn(r));
@@ -280,76 +310,116 @@ struct TileStep {
       qs[1] = 0u;
     }
     const float c = p.scale2 * 16777216.f * __int_as_float((127 - e1) << 23) * __int_as_float((127 - e2) << 23);
-    cq[0] = __shfl_sync(0xffffffffu, c, 8 * (lane & 3));
-    cq[1] = __shfl_sync(0xffffffffu, c, 8 * (lane & 3) + 4);
+    cq[0] = __shfl_sync(0xffffffffu, c, 4 * row(0));
+    cq[1] = __shfl_sync(0xffffffffu, c, 4 * row(1));
   }
 
-  // One tile in shared memory.  With kMask, row i (token g, g + 8) of column j
-  // takes part only where see[i][j].
+  // This lane's scales (first) or minima of one row, from the row's 4 NG bytes.
+  template <bool kMinima>
+  __device__ __forceinline__ void lane_meta(float (&s)[K], const uint8_t* meta) const {
+    if constexpr (NG == 4 && kHalves) {
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(meta + 4 * half + (kMinima ? 8 : 0));
+      s[0] = low_bf16(w);
+      s[1] = high_bf16(w);
+    } else if constexpr (NG == 4) {
+      const uint2 w = *reinterpret_cast<const uint2*>(meta + (kMinima ? 8 : 0));
+      s[0] = low_bf16(w.x);
+      s[1] = high_bf16(w.x);
+      s[2] = low_bf16(w.y);
+      s[3] = high_bf16(w.y);
+    } else if constexpr (NG == 2) {
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(meta + (kMinima ? 4 : 0));
+      if constexpr (kHalves) {
+        s[0] = half ? high_bf16(w) : low_bf16(w);
+      } else {
+        s[0] = low_bf16(w);
+        s[1] = high_bf16(w);
+      }
+    } else {
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(meta);
+      s[0] = kMinima ? high_bf16(w) : low_bf16(w);
+    }
+  }
+
+  // One tile in shared memory.  With kMask, token g + 8 i takes part in row(j) only where see[i][j].
   template <bool kMask>
-  __device__ __forceinline__ void step(const uint8_t* tile, int g, int t, const bool (&see)[2][2]) {
+  __device__ __forceinline__ void step(const uint8_t* tile, const bool (&see)[2][2]) {
     constexpr TileShape ts{D, NG};
     uint32_t kw[2][C];
     load_words<C>(kw[0], tile + g * (D / 2) + t * (D / 8));
     load_words<C>(kw[1], tile + (g + 8) * (D / 2) + t * (D / 8));
-    const uint8_t* kmeta = tile + ts.k_meta();
-    uint32_t r0[NG], r1[NG];
-    load_words<NG>(r0, kmeta + g * 4 * NG);
-    load_words<NG>(r1, kmeta + (g + 8) * 4 * NG);
+    const uint8_t* kmeta = tile + ts.k_meta() + g * 4 * NG;
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    if constexpr (NG == 4) {
-      const uint32_t m0 = (t & 1) ? r0[3] : r0[2], m1 = (t & 1) ? r1[3] : r1[2];
-      mma_bf16(acc, m0, m1, m0, m1, qs[0], qs[1]);
-    } else {
-      mma_bf16(acc, r0[NG - 1], r1[NG - 1], 0u, 0u, qs[0], 0u);
+    {
+      // minima against the sums of the query
+      const int at = NG == 4 ? 8 + 4 * (t & 1) : NG == 2 ? 4 : 0;
+      const uint32_t m0 = *reinterpret_cast<const uint32_t*>(kmeta + at);
+      const uint32_t m1 = *reinterpret_cast<const uint32_t*>(kmeta + 8 * 4 * NG + at);
+      if constexpr (NG == 4) mma_bf16(acc, m0, m1, m0, m1, qs[0], qs[1]);
+      else mma_bf16(acc, m0, m1, 0u, 0u, qs[0], 0u);
     }
+    float ks[2][K];
+    lane_meta<false>(ks[0], kmeta);
+    lane_meta<false>(ks[1], kmeta + 8 * 4 * NG);
 #pragma unroll
-    for (int k = 0; k < NG; ++k) {
+    for (int k = 0; k < K; ++k) {
       float a[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = k * PG; c < (k + 1) * PG; ++c) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const uint32_t w0 = j ? kw[0][c] >> 8 : kw[0][c], w1 = j ? kw[1][c] >> 8 : kw[1][c];
-          mma_f16(a, w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, qb[c][j][0], qb[c][j][1]);
+          if constexpr (kHalves) {
+            const uint32_t u0 = j ? kw[0][c + H] >> 8 : kw[0][c + H], u1 = j ? kw[1][c + H] >> 8 : kw[1][c + H];
+            mma_f16(a, w0 & 0x000f000fu, w1 & 0x000f000fu, u0 & 0x000f000fu, u1 & 0x000f000fu, qb[c][2 * j], qb[H + c][2 * j]);
+            mma_f16(a, w0 & 0x00f000f0u, w1 & 0x00f000f0u, u0 & 0x00f000f0u, u1 & 0x00f000f0u, qb[c][2 * j + 1],
+                    qb[H + c][2 * j + 1]);
+          } else {
+            mma_f16(a, w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, qb[c][2 * j], qb[c][2 * j + 1]);
+          }
         }
       }
-      const float s0 = (k & 1) ? high_bf16(r0[k / 2]) : low_bf16(r0[k / 2]);
-      const float s1 = (k & 1) ? high_bf16(r1[k / 2]) : low_bf16(r1[k / 2]);
-      acc[0] = fmaf(s0, a[0], acc[0]);
-      acc[1] = fmaf(s0, a[1], acc[1]);
-      acc[2] = fmaf(s1, a[2], acc[2]);
-      acc[3] = fmaf(s1, a[3], acc[3]);
+      acc[0] = fmaf(ks[0][k], a[0], acc[0]);
+      acc[1] = fmaf(ks[0][k], a[1], acc[1]);
+      acc[2] = fmaf(ks[1][k], a[2], acc[2]);
+      acc[3] = fmaf(ks[1][k], a[3], acc[3]);
     }
-    float vs[2][NG], vm[2][NG];
-    const uint8_t* vmeta = tile + ts.v_meta();
-    load_meta<NG>(vs[0], vm[0], vmeta + g * 4 * NG);
-    load_meta<NG>(vs[1], vm[1], vmeta + (g + 8) * 4 * NG);
-    // about log2 of each token's largest value scale (the bits of a float)
-    float sg[2];
+    if constexpr (kHalves) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 2);
+    }
+    float vs[2][K], vm[2][K], top_s[2];
+    const uint8_t* vmeta = tile + ts.v_meta() + g * 4 * NG;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      float top = vs[i][0];
+      lane_meta<false>(vs[i], vmeta + i * 8 * 4 * NG);
+      lane_meta<true>(vm[i], vmeta + i * 8 * 4 * NG);
+      top_s[i] = 1.2621774483536189e-29f;        // 2^-96; fmaxf passes over NaN, whose rows decide nothing
 #pragma unroll
-      for (int k = 1; k < NG; ++k) top = fmaxf(top, vs[i][k]);
-      sg[i] = fmaxf(fmaf(float(__float_as_int(top)), 1.1920928955078125e-7f, -127.f), -96.f);
+      for (int k = 0; k < K; ++k) top_s[i] = fmaxf(top_s[i], vs[i][k]);
     }
-    float y[4];
+    float w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      y[i] = fmaf(acc[i], cq[i & 1], -ref[i & 1]);
-      if (kMask && !see[i >> 1][i & 1]) y[i] = -INFINITY;
+      w[i] = exp2_fast(fmaf(acc[i], cq[i & 1], -ref[i & 1]));
+      if (kMask && !see[i >> 1][i & 1]) w[i] = 0.f;
     }
-    const float over = fmaxf(fmaxf(y[0], y[1]) + sg[0], fmaxf(y[2], y[3]) + sg[1]);
-    if (__any_sync(0xffffffffu, over > 14.f)) {
-      // a column's reference: 6 below its largest logit + log2 scale
+    const float over = fmaxf(fmaxf(w[0], w[1]) * top_s[0], fmaxf(w[2], w[3]) * top_s[1]);
+    if (__any_sync(0xffffffffu, over > 16384.f)) {
+      // a row's reference: 6 below its largest logit + log2 scale
+      float sg[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float s = top_s[i];
+        if constexpr (kHalves && NG > 1) s = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, 2));
+        sg[i] = fminf(log2f(s), 96.f);
+      }
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         float top = kNoRef;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float sc = sg[i] > 128.f ? -96.f : fminf(sg[i], 96.f);     // above 128: NaN, whose rows decide nothing
-          const float x = acc[2 * i + j] * cq[j] + sc;
+          const float x = acc[2 * i + j] * cq[j] + sg[i];
           if (!kMask || see[i][j]) top = fmaxf(top, x);
         }
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
@@ -360,7 +430,7 @@ struct TileStep {
         ref[j] = now;
         l[j] *= keep;
 #pragma unroll
-        for (int k = 0; k < NG; ++k) om[k][j] *= keep;
+        for (int k = 0; k < K; ++k) om[k][j] *= keep;
 #pragma unroll
         for (int m = 0; m < 2 * C; ++m) {
           o[m][j] *= keep;
@@ -369,29 +439,27 @@ struct TileStep {
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        y[i] = fmaf(acc[i], cq[i & 1], -ref[i & 1]);
-        if (kMask && !see[i >> 1][i & 1]) y[i] = -INFINITY;
+        w[i] = exp2_fast(fmaf(acc[i], cq[i & 1], -ref[i & 1]));
+        if (kMask && !see[i >> 1][i & 1]) w[i] = 0.f;
       }
     }
-    float w[4];
+    l[0] += w[0] + w[2];
+    l[1] += w[1] + w[3];
+    uint32_t b[K][2], b2[K][2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      w[i] = exp2_fast(y[i]);
-      l[i & 1] += w[i];
-    }
-    uint32_t b[NG][2], b2[NG][2];
-#pragma unroll
-    for (int k = 0; k < NG; ++k) {
+    for (int k = 0; k < K; ++k) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         float x0 = w[2 * i] * vs[i][k], x1 = w[2 * i + 1] * vs[i][k];
-        float m0 = w[2 * i] * vm[i][k], m1 = w[2 * i + 1] * vm[i][k];
         if constexpr (kMask) {                   // what is not seen may be NaN
-          if (!see[i][0]) x0 = m0 = 0.f;
-          if (!see[i][1]) x1 = m1 = 0.f;
+          if (!see[i][0]) x0 = 0.f;
+          if (!see[i][1]) x1 = 0.f;
+          if (see[i][0]) om[k][0] = fmaf(w[2 * i], vm[i][k], om[k][0]);
+          if (see[i][1]) om[k][1] = fmaf(w[2 * i + 1], vm[i][k], om[k][1]);
+        } else {
+          om[k][0] = fmaf(w[2 * i], vm[i][k], om[k][0]);
+          om[k][1] = fmaf(w[2 * i + 1], vm[i][k], om[k][1]);
         }
-        om[k][0] += m0;
-        om[k][1] += m1;
         const uint32_t h = pack_f16(x0, x1);
         b[k][i] = transpose8x8(h);
         if constexpr (kTwoPlanes) b2[k][i] = transpose8x8(rest_f16(x0, x1, h));
@@ -402,21 +470,31 @@ struct TileStep {
     load_words<C>(v0, codes + t * D + ts.v_place(t, g) * (D / 8));
     load_words<C>(v1, codes + (t + 4) * D + ts.v_place(t + 4, g) * (D / 8));
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
+    for (int c = 0; c < H; ++c) {
       const int k = c / PG;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const uint32_t w0 = j ? v0[c] >> 8 : v0[c], w1 = j ? v1[c] >> 8 : v1[c];
-        const uint32_t a0 = w0 & 0x000f000fu, a1 = w0 & 0x00f000f0u, a2 = w1 & 0x000f000fu, a3 = w1 & 0x00f000f0u;
-        mma_f16(o[2 * c + j], a0, a1, a2, a3, b[k][0], b[k][1]);
-        if constexpr (kTwoPlanes) mma_f16(o[2 * c + j], a0, a1, a2, a3, b2[k][0], b2[k][1]);
+        if constexpr (kHalves) {
+          const uint32_t u0 = j ? v0[c + H] >> 8 : v0[c + H], u1 = j ? v1[c + H] >> 8 : v1[c + H];
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const uint32_t mask = n ? 0x00f000f0u : 0x000f000fu;
+            float(&d)[4] = o[4 * c + 2 * j + n];
+            mma_f16(d, w0 & mask, u0 & mask, w1 & mask, u1 & mask, b[k][0], b[k][1]);
+            if constexpr (kTwoPlanes) mma_f16(d, w0 & mask, u0 & mask, w1 & mask, u1 & mask, b2[k][0], b2[k][1]);
+          }
+        } else {
+          const uint32_t a0 = w0 & 0x000f000fu, a1 = w0 & 0x00f000f0u, a2 = w1 & 0x000f000fu, a3 = w1 & 0x00f000f0u;
+          mma_f16(o[2 * c + j], a0, a1, a2, a3, b[k][0], b[k][1]);
+          if constexpr (kTwoPlanes) mma_f16(o[2 * c + j], a0, a1, a2, a3, b2[k][0], b2[k][1]);
+        }
       }
     }
   }
 
-  // Sums over the lanes of a column; then o, l hold whole columns, normalised:
-  // x(c, i, j) below is the softmax's output at dim 32c + 4g + i of column 2t + j,
-  // ref its log2 of the sum of 2^logit (-inf: nothing seen).
+  // Sums over the lanes of a row; then out(c, i, j) is the softmax's output at dim
+  // 32 block(c) + 4g + i of row(j), ref its log2 of the sum of 2^logit (-inf: nothing seen).
   __device__ __forceinline__ void finish() {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -424,7 +502,7 @@ struct TileStep {
       for (int s = 4; s < 32; s *= 2) {
         l[j] += __shfl_xor_sync(0xffffffffu, l[j], s);
 #pragma unroll
-        for (int k = 0; k < NG; ++k) om[k][j] += __shfl_xor_sync(0xffffffffu, om[k][j], s);
+        for (int k = 0; k < K; ++k) om[k][j] += __shfl_xor_sync(0xffffffffu, om[k][j], s);
       }
       const bool seen = ref[j] != kNoRef || l[j] != 0.f;
       const float inv = seen ? 1.f / l[j] : 0.f;
@@ -432,9 +510,12 @@ struct TileStep {
       l[j] = inv;
     }
   }
-  __device__ __forceinline__ float x(int c, int i, int j) const {
-    const float v = o[2 * c + i / 2][2 * (i & 1) + j] * ((i & 1) ? 1048576.f : 16777216.f);
-    return (v + om[c / PG][j]) * l[j];
+  __device__ __forceinline__ float out(int c, int i, int j) const {
+    const float f = (i & 1) ? 1048576.f : 16777216.f;
+    float v;
+    if constexpr (kHalves) v = half ? o[4 * c + i][2 + j] : o[4 * c + i][j];
+    else v = o[2 * c + i / 2][2 * (i & 1) + j];
+    return (v * f + om[c / PG][j]) * l[j];
   }
 };
 
