@@ -80,6 +80,7 @@ struct RowCursor {
   }
   __device__ void locate(const AttnParams& p, const int64_t* prefix, int64_t x) {
     int lo = 0, hi = p.batch;                     // tiles before lo <= x < tiles before hi
+#pragma unroll 1
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (tiles_of(prefix[mid]) <= x) lo = mid;
@@ -88,6 +89,7 @@ struct RowCursor {
     b = lo;
     s = sequence_of(p, b);
     int64_t left = x - tiles_of(prefix[b]);
+#pragma unroll 1
     for (r0 = 0;; r0 += R) {
       block(p);
       const int64_t n = int64_t(k.tiles) * p.kv_heads;
@@ -102,6 +104,7 @@ struct RowCursor {
   static __device__ int64_t unit_start(const AttnParams& p, const int64_t* prefix, int64_t i) {
     if (i >= units_of(prefix[p.batch])) return tiles_of(prefix[p.batch]);
     int lo = 0, hi = p.batch;
+#pragma unroll 1
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (units_of(prefix[mid]) <= i) lo = mid;
@@ -112,6 +115,7 @@ struct RowCursor {
     c.s = sequence_of(p, lo);
     int left = int(i - units_of(prefix[lo]));
     int64_t x = tiles_of(prefix[lo]);
+#pragma unroll 1
     for (c.r0 = 0;; c.r0 += R, left -= p.kv_heads) {
       c.block(p);
       if (left < p.kv_heads) return x + int64_t(left) * c.k.tiles;
@@ -125,6 +129,7 @@ struct RowCursor {
     h = 0;
     r0 += R;
     if (r0 >= s.count * p.group) {
+#pragma unroll 1
       do ++b; while (b < p.batch && prefix[b + 1] == prefix[b]);        // without queries
       if (b >= p.batch) return;
       s = sequence_of(p, b);
@@ -232,11 +237,13 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
   if (p.batch > 1) __syncthreads();
 
   // the tiles of every sequence, and what they sum up to
+#pragma unroll 1
   for (int b = threadIdx.x; b < p.batch; b += blockDim.x) {
     const Sequence s = sequence_of(p, b);
     const int rows = s.count * p.group;
     int64_t n = 0;
     int longest = 0;
+#pragma unroll 1
     for (int r0 = 0; r0 < rows; r0 += kRows) {
       const int k = row_block(p, s, r0, min(r0 + kRows, rows)).tiles;
       n += k;
@@ -256,6 +263,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
   if (warp == 0) {
     int64_t sum = 0;
     if (lane == 0) prefix[0] = 0;
+#pragma unroll 1
     for (int b = 0; b < p.batch; b += 32) {
       int64_t v = b + lane < p.batch ? prefix[b + lane + 1] : 0;
 #pragma unroll
@@ -335,6 +343,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     uint32_t round = 0;                           // times the ring has gone round
     int k = 0;                                    // tiles fed
     long long t0 = clock64();
+#pragma unroll 1
     while (__any_sync(0xffffffffu, x < end)) {
       bool fed = false;
       if (x < end) {
@@ -389,6 +398,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     st.init(lane);
     int k = 0;
     bool failed = false;
+#pragma unroll 1
     while (x < end && !failed) {
       const int n = int(min(int64_t(c.k.tiles - c.tile), end - x));
       const int rows = c.s.count * p.group;
@@ -411,6 +421,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
       const int last = c.s.len - c.s.count + min(c.r0 + kRows - 1, rows - 1) / p.group;
       const int all_lo = p.window > 0 ? max(0, last - p.window + 1) : 0;
       st.reset();
+#pragma unroll 1
       for (int i = 0; i < n; ++i, ++k) {
         const int stage = warp * kAttnStages + k % kAttnStages;
         if (!__all_sync(0xffffffffu, mbar_wait_bounded(&full[stage], (k / kAttnStages) & 1))) {
@@ -477,6 +488,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
   const int row = warp & (kRows - 1);
   const int u = lane;                             // dims 4u .. 4u + 3
   int turn_of = 0;
+#pragma unroll 1
   for (uint32_t m = begins; m; m &= m - 1, ++turn_of) {
     if (turn_of % (16 / kRows) != warp / kRows) continue;
     const int first = __ffs(m) - 1;
@@ -487,6 +499,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     const float ref = (mine >> lane) & 1 ? refs[lane * kRows + row] : -INFINITY;
     const Joined j = join_weights(ref);
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
     for (uint32_t e = mine; e; e &= e - 1) {
       const int i = __ffs(e) - 1;
       const float f = __shfl_sync(0xffffffffu, j.weight, i);
@@ -530,6 +543,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     auto record = [&](int i) { return p.partials + ((a0 + i) * 2 + (i == 0 ? 1 : 0)) * (RF + kRows); };
     Joined all{0.f, -INFINITY};
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
     for (int i0 = 0; i0 < n; i0 += 32) {
       const float ref = i0 + lane < n ? __ldcg(record(i0 + lane) + RF + row) : -INFINITY;
       const Joined j = join_weights(ref);

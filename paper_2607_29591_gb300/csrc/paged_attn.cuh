@@ -56,7 +56,9 @@ __device__ __forceinline__ Sequence sequence_of(const AttnParams& p, int b) {
 
 // Rows [r0, r1) of a sequence.
 __device__ __forceinline__ RowBlock row_block(const AttnParams& p, const Sequence& s, int r0, int r1) {
-  const int lo = s.len - s.count + r0 / p.group, hi = s.len - s.count + (r1 - 1) / p.group;
+  // (one block of a sequence's rows, the usual case, divides nothing)
+  const int lo = s.len - s.count + (r0 == 0 ? 0 : r0 / p.group);
+  const int hi = s.len - s.count + (r1 == s.count * p.group ? s.count - 1 : (r1 - 1) / p.group);
   RowBlock b;
   b.empty = hi < 0;
   const int from = p.window > 0 ? max(0, lo - p.window + 1) : 0;
