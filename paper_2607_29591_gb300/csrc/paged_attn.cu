@@ -22,7 +22,8 @@ namespace {
 // full, one bulk copy per tile, so that page lookups and copies cost the tile
 // step nothing.
 constexpr int kAttnWarps = 15;                      // computing; with the feeding warp 16, of 128 registers
-constexpr int kAttnStages = 4;
+constexpr int kAttnStages = 2;                    // of a warp's ring
+constexpr int kStageTiles = 2;                    // neighbours within a page, one copy
 constexpr int kMinTiles = 2;                      // of a piece, before more CTAs are used
 constexpr int kWholeTiles = 135;                  // 9 a warp
 
@@ -38,15 +39,15 @@ __host__ __device__ constexpr int record_floats(int d, int rows) { return rows *
 
 template <int D, int NG, int R>
 struct AttnSmem {
-  static constexpr int ring = kAttnWarps * kAttnStages * TileShape{D, NG}.bytes();
+  static constexpr int ring = kAttnWarps * kAttnStages * kStageTiles * TileShape{D, NG}.bytes();
   static constexpr int heads = kAttnWarps * record_floats(D, R) * 4;
   static constexpr int refs = 2 * kAttnWarps * R * 4;
   static constexpr int info = 2 * kAttnWarps * int(sizeof(RecordInfo));
   static constexpr int bars = 2 * kAttnWarps * kAttnStages * 8;
-  static constexpr int skips = kAttnWarps * kAttnStages * 4;
-  static constexpr int fixed = (ring + heads + refs + info + bars + skips + 16 + 15) / 16 * 16;
+  static constexpr int counts = kAttnWarps * kAttnStages * 4;
+  static constexpr int fixed = (ring + heads + refs + info + bars + counts + 16 + 15) / 16 * 16;
   static_assert((ring + heads + refs) % 8 == 0 && (ring + heads + refs + info) % 8 == 0 && ring % 16 == 0, "alignment");
-  static_assert(kAttnStages * TileShape{D, NG}.bytes() >= record_floats(D, R) * 4, "a drained ring holds a record");
+  static_assert(kAttnStages * kStageTiles * TileShape{D, NG}.bytes() >= record_floats(D, R) * 4, "a drained ring holds a record");
   static int bytes(int batch) { return fixed + (batch + 1) * 8; }
 };
 
@@ -221,7 +222,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
   using Cursor = RowCursor<R>;
   constexpr int kRows = R;
   constexpr TileShape ts{D, NG};
-  constexpr int TB = ts.bytes(), RS = record_stride(D), RF = record_floats(D, R);
+  constexpr int TB = ts.bytes(), SB = kStageTiles * TB, RS = record_stride(D), RF = record_floats(D, R);
   extern __shared__ __align__(128) uint8_t smem[];
   uint8_t* ring = smem;
   float* heads = reinterpret_cast<float*>(smem + S::ring);
@@ -229,8 +230,8 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
   RecordInfo* info = reinterpret_cast<RecordInfo*>(smem + S::ring + S::heads + S::refs);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::ring + S::heads + S::refs + S::info);
   uint64_t* vacant = full + kAttnWarps * kAttnStages;
-  int* skips = reinterpret_cast<int*>(vacant + kAttnWarps * kAttnStages);
-  int* shared_int = skips + kAttnWarps * kAttnStages;                 // [4]
+  int* counts = reinterpret_cast<int*>(vacant + kAttnWarps * kAttnStages);
+  int* shared_int = counts + kAttnWarps * kAttnStages;                 // [4]
   int64_t* prefix = reinterpret_cast<int64_t*>(smem + S::fixed);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) shared_int[2] = 0;
@@ -349,26 +350,29 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
       if (x < end) {
         const int at = w * kAttnStages + st;
         if (round == 0 || mbar_test(&vacant[at], (round - 1) & 1)) {
-          skips[at] = !ok;
+          const int n = min(min(kStageTiles, in_unit), min(in_page, int(min(end - x, int64_t(kStageTiles)))));
+          counts[at] = ok ? n : -n;
           if (ok) {
-            mbar_arrive_expect_tx(&full[at], TB);
-            copy_tile(ring + at * TB, src, TB, &full[at], policy);
+            mbar_arrive_expect_tx(&full[at], n * TB);
+            copy_tile(ring + at * SB, src, n * TB, &full[at], policy);
           } else {
             mbar_arrive(&full[at]);
           }
-          src += TB;
+          src += n * TB;
           ++k;
-          ++x;
+          x += n;
           if (++st == kAttnStages) {
             st = 0;
             ++round;
           }
-          if (--in_unit == 0) {
+          in_unit -= n;
+          in_page -= n;
+          if (in_unit == 0) {
             if (x < end) {
               c.next(p, prefix);
               begin_unit();
             }
-          } else if (--in_page == 0) {
+          } else if (in_page == 0) {
             turn_page(0);
           }
           fed = true;
@@ -422,15 +426,17 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
       const int all_lo = p.window > 0 ? max(0, last - p.window + 1) : 0;
       st.reset();
 #pragma unroll 1
-      for (int i = 0; i < n; ++i, ++k) {
+      for (int i = 0; i < n; ++k) {
         const int stage = warp * kAttnStages + k % kAttnStages;
         if (!__all_sync(0xffffffffu, mbar_wait_bounded(&full[stage], (k / kAttnStages) & 1))) {
           failed = true;
           break;
         }
-        if (!skips[stage]) {
-          const int pos = (c.k.first + c.tile + i) * kTile;
-          const uint8_t* tile = ring + stage * TB;
+        const int count = counts[stage];          // negative: a page that does not exist, or nothing to see
+        const uint8_t* tile = ring + stage * SB;
+        int pos = (c.k.first + c.tile + i) * kTile;
+#pragma unroll 1
+        for (int j = 0; j < count; ++j, pos += kTile, tile += TB) {
           bool see[2][2] = {{true, true}, {true, true}};
           if (pos >= all_lo && pos + kTile - 1 <= all_hi) {
             st.template step<false>(tile, see);
@@ -438,10 +444,11 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
-              for (int j = 0; j < 2; ++j) see[r][j] = pos + st.g + 8 * r >= lo[j] && pos + st.g + 8 * r <= hi[j];
+              for (int q = 0; q < 2; ++q) see[r][q] = pos + st.g + 8 * r >= lo[q] && pos + st.g + 8 * r <= hi[q];
             st.template step<true>(tile, see);
           }
         }
+        i += abs(count);
         __syncwarp();
         if (lane == 0) mbar_arrive(&vacant[stage]);
       }
@@ -453,7 +460,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
       const bool unit = c.tile == 0 && n == c.k.tiles;
       // else a record: begun before this piece, or cut off at its end
       const int slot = c.tile > 0 ? 0 : 1;
-      float* rec = slot == 0 ? heads + warp * RF : reinterpret_cast<float*>(ring + warp * kAttnStages * TB);
+      float* rec = slot == 0 ? heads + warp * RF : reinterpret_cast<float*>(ring + warp * kAttnStages * SB);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int r = st.row(j);
@@ -503,7 +510,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     for (uint32_t e = mine; e; e &= e - 1) {
       const int i = __ffs(e) - 1;
       const float f = __shfl_sync(0xffffffffu, j.weight, i);
-      const float* rec = (i & 1) ? reinterpret_cast<const float*>(ring + (i >> 1) * kAttnStages * TB) : heads + (i >> 1) * RF;
+      const float* rec = (i & 1) ? reinterpret_cast<const float*>(ring + (i >> 1) * kAttnStages * SB) : heads + (i >> 1) * RF;
       if (u < D / 4 && f != 0.f) add_scaled(a, f, *reinterpret_cast<const float4*>(rec + row * RS + 4 * u));
     }
     if (!cut(ri)) {
