@@ -302,30 +302,34 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
 
   if (warp == kAttnWarps) {
     // --- the feeding warp: lane w for warp w ---
+    // One turn of its loop serves every lane whose ring has a free stage; its length is
+    // what a stage waits for, so a turn does little: sizes come in bytes, pages are
+    // asked for one ahead.
     const int w = lane;
-    int64_t x = 0, end = 0;
+    int left = 0;                                 // tiles to feed
     Cursor c{};
     if (w < kAttnWarps) {
-      x = piece(w);
-      end = piece(w + 1);
-      if (x < end) c.locate(p, prefix, x);
+      const int64_t x = piece(w);
+      left = int(piece(w + 1) - x);
+      if (left > 0) c.locate(p, prefix, x);
     }
     uint64_t policy;
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
     const int tpp = p.page_tokens / kTile;        // tiles of a page
-    const int64_t head_bytes = int64_t(tpp) * TB;
-    const uint8_t* src = p.pages;                 // the next tile
+    const int64_t page_bytes = int64_t(p.kv_heads) * tpp * TB;
+    const uint8_t* head = p.pages;                // the unit's head in page 0
+    const uint8_t* src = head;                    // the next tile
     int in_unit = 0, in_page = 0;                 // tiles left of the unit and of the page, the next one included
     bool ok = false;                              // the page exists
     int page = 0;                                 // the page after this one, asked for a page ahead
     const int32_t* ask = p.page_table;
-    auto turn_page = [&](int first) {             // to `page`, from its tile `first`
-      ok = page >= 0 && page < p.n_pages;
+    auto turn_page = [&]() {                      // to `page`
+      ok = uint32_t(page) < uint32_t(p.n_pages);
       if (!ok) report_status(p.status, kStatusBadIndex);
-      src = p.pages + (int64_t(ok ? page : 0) * p.kv_heads + c.h) * head_bytes + first * TB;
-      in_page = tpp - first;
+      src = head + (ok ? page : 0) * page_bytes;
+      in_page = tpp;
       ++ask;
-      if (in_unit > in_page) page = *ask;
+      if (in_unit > tpp) page = *ask;
     };
     auto begin_unit = [&]() {
       in_unit = c.k.tiles - c.tile;
@@ -334,52 +338,57 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
         in_page = in_unit;
         return;
       }
-      const int tile = c.k.first + c.tile;
-      ask = p.page_table + int64_t(c.b) * p.table_pages + tile / tpp;
+      const int tile = c.k.first + c.tile, at = tile / tpp, first = tile - at * tpp;
+      head = p.pages + int64_t(c.h) * tpp * TB;
+      ask = p.page_table + int64_t(c.b) * p.table_pages + at;
       page = *ask;
-      turn_page(tile % tpp);
+      in_unit += first;                           // as from the page's first tile
+      turn_page();
+      in_unit -= first;
+      in_page -= first;
+      src += first * TB;
     };
-    if (x < end) begin_unit();
-    int st = 0;                                   // stage of the next tile
-    uint32_t round = 0;                           // times the ring has gone round
-    int k = 0;                                    // tiles fed
+    if (left > 0) begin_unit();
+    int st = 0;                                   // next stage
+    uint32_t parity = 1;                          // of the vacancy to wait for: a fresh barrier passes
+    int k = 0;                                    // stages fed
     long long t0 = clock64();
+    uint32_t busy = __ballot_sync(0xffffffffu, left > 0);
 #pragma unroll 1
-    while (__any_sync(0xffffffffu, x < end)) {
+    while (busy) {
       bool fed = false;
-      if (x < end) {
-        const int at = w * kAttnStages + st;
-        if (round == 0 || mbar_test(&vacant[at], (round - 1) & 1)) {
-          const int n = min(min(kStageTiles, in_unit), min(in_page, int(min(end - x, int64_t(kStageTiles)))));
-          counts[at] = ok ? n : -n;
-          if (ok) {
-            mbar_arrive_expect_tx(&full[at], n * TB);
-            copy_tile(ring + at * SB, src, n * TB, &full[at], policy);
-          } else {
-            mbar_arrive(&full[at]);
-          }
-          src += n * TB;
-          ++k;
-          x += n;
-          if (++st == kAttnStages) {
-            st = 0;
-            ++round;
-          }
-          in_unit -= n;
-          in_page -= n;
-          if (in_unit == 0) {
-            if (x < end) {
-              c.next(p, prefix);
-              begin_unit();
-            }
-          } else if (in_page == 0) {
-            turn_page(0);
-          }
-          fed = true;
+      const int at = w * kAttnStages + st;
+      if (left > 0 && mbar_test(&vacant[at], parity)) {
+        const int n = min(min(kStageTiles, left), min(in_page, in_unit));
+        counts[at] = ok ? n : -n;
+        if (ok) {
+          mbar_arrive_expect_tx(&full[at], n * TB);
+          copy_tile(ring + at * SB, src, n * TB, &full[at], policy);
+        } else {
+          mbar_arrive(&full[at]);
         }
+        src += n * TB;
+        ++k;
+        left -= n;
+        in_unit -= n;
+        in_page -= n;
+        if (++st == kAttnStages) {
+          st = 0;
+          parity ^= 1;
+        }
+        if (left > 0) {
+          if (in_unit == 0) {
+            c.next(p, prefix);
+            begin_unit();
+          } else if (in_page == 0) {
+            turn_page();
+          }
+        }
+        fed = true;
       }
       if (__any_sync(0xffffffffu, fed)) {
         t0 = clock64();
+        busy = __ballot_sync(0xffffffffu, left > 0);
         continue;
       }
       __nanosleep(32);
