@@ -65,6 +65,28 @@ __device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
   b = y;
 }
 
+// The kernels of a decode step follow one another within microseconds: each is
+// launched while the one before it on the stream still runs, and waits for its
+// end before it touches memory (wait_for_previous, the first thing they do).
+template <typename... P, typename... A>
+cudaError_t launch_early(void (*kernel)(P...), dim3 grid, dim3 block, size_t shared, cudaStream_t s, A... args) {
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = shared;
+  cfg.stream = s;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+__device__ __forceinline__ void wait_for_previous() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 inline int dtype_size(int32_t dtype) { return dtype == RESKV_F32 ? 4 : 2; }
 inline bool dtype_known(int32_t dtype) { return dtype >= RESKV_BF16 && dtype <= RESKV_F32; }
 inline bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }

@@ -117,9 +117,11 @@ struct RowCursor {
     int left = int(i - units_of(prefix[lo]));
     int64_t x = tiles_of(prefix[lo]);
 #pragma unroll 1
-    for (c.r0 = 0;; c.r0 += R, left -= p.kv_heads) {
+    for (c.r0 = 0;; c.r0 += R) {
       c.block(p);
+      if (c.k.tiles == 0) continue;               // no unit; the last block is one
       if (left < p.kv_heads) return x + int64_t(left) * c.k.tiles;
+      left -= p.kv_heads;
       x += int64_t(c.k.tiles) * p.kv_heads;
     }
   }
@@ -131,12 +133,17 @@ struct RowCursor {
     r0 += R;
     if (r0 >= s.count * p.group) {
 #pragma unroll 1
-      do ++b; while (b < p.batch && prefix[b + 1] == prefix[b]);        // without queries
+      do ++b; while (b < p.batch && prefix[b + 1] == prefix[b]);        // nothing to do
       if (b >= p.batch) return;
       s = sequence_of(p, b);
       r0 = 0;
     }
     block(p);
+#pragma unroll 1
+    while (k.tiles == 0 && r0 + R < s.count * p.group) {                  // rows before position 0
+      r0 += R;
+      block(p);
+    }
   }
 };
 
@@ -235,7 +242,14 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
   int64_t* prefix = reinterpret_cast<int64_t*>(smem + S::fixed);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) shared_int[2] = 0;
+  if (threadIdx.x < 2 * kAttnWarps) info[threadIdx.x].present = 0;
+  if (threadIdx.x < kAttnWarps * kAttnStages) {
+    mbar_init(&full[threadIdx.x], 1);
+    mbar_init(&vacant[threadIdx.x], 1);
+  }
+  fence_mbar_init();
   if (p.batch > 1) __syncthreads();
+  wait_for_previous();
 
   // the tiles of every sequence, and what they sum up to
 #pragma unroll 1
@@ -243,23 +257,18 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     const Sequence s = sequence_of(p, b);
     const int rows = s.count * p.group;
     int64_t n = 0;
-    int longest = 0;
+    int longest = 0, blocks = 0;
 #pragma unroll 1
     for (int r0 = 0; r0 < rows; r0 += kRows) {
       const int k = row_block(p, s, r0, min(r0 + kRows, rows)).tiles;
       n += k;
+      blocks += k > 0;
       longest = max(longest, k);
     }
-    prefix[b + 1] = (n * p.kv_heads << kUnitBits) + int64_t((rows + kRows - 1) / kRows) * p.kv_heads;
+    prefix[b + 1] = (n * p.kv_heads << kUnitBits) + int64_t(blocks) * p.kv_heads;
     if (p.batch == 1) shared_int[2] = longest;
     else atomicMax(&shared_int[2], longest);
   }
-  if (threadIdx.x < 2 * kAttnWarps) info[threadIdx.x].present = 0;
-  if (threadIdx.x < kAttnWarps * kAttnStages) {
-    mbar_init(&full[threadIdx.x], 1);
-    mbar_init(&vacant[threadIdx.x], 1);
-  }
-  fence_mbar_init();
   __syncthreads();
   if (warp == 0) {
     int64_t sum = 0;
@@ -274,6 +283,24 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
       }
       if (b + lane < p.batch) prefix[b + lane + 1] = sum + v;
       sum += __shfl_sync(0xffffffffu, v, 31);
+    }
+  }
+  if (warp == kAttnWarps) {
+    // meanwhile, zeros where rows see nothing: the blocks of rows that are no unit
+#pragma unroll 1
+    for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
+      const Sequence s = sequence_of(p, b);
+      if (s.len >= s.count) continue;
+      const int64_t rows = int64_t(s.count - s.len) * p.group;
+      const int r1 = s.len == 0 ? int(rows) : int(rows / kRows) * kRows;
+#pragma unroll 1
+      for (int64_t i = lane; i < int64_t(r1) * p.kv_heads * (D / 4); i += 32) {
+        const int u = int(i % (D / 4));
+        const int64_t hr = i / (D / 4);
+        const int h = int(hr / r1), r = int(hr - int64_t(h) * r1);
+        store_out(p, s, h, r, u, make_float4(0.f, 0.f, 0.f, 0.f));
+        if (u == 0) store_lse(p, s, h, r, -INFINITY);
+      }
     }
   }
   __syncthreads();
@@ -333,11 +360,6 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     };
     auto begin_unit = [&]() {
       in_unit = c.k.tiles - c.tile;
-      if (c.k.empty) {
-        ok = false;
-        in_page = in_unit;
-        return;
-      }
       const int tile = c.k.first + c.tile, at = tile / tpp, first = tile - at * tpp;
       head = p.pages + int64_t(c.h) * tpp * TB;
       ask = p.page_table + int64_t(c.b) * p.table_pages + at;
@@ -441,7 +463,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
           failed = true;
           break;
         }
-        const int count = counts[stage];          // negative: a page that does not exist, or nothing to see
+        const int count = counts[stage];          // negative: a page that does not exist
         const uint8_t* tile = ring + stage * SB;
         int pos = (c.k.first + c.tile + i) * kTile;
 #pragma unroll 1
@@ -617,8 +639,7 @@ cudaError_t launch_rows(const AttnParams& p, int dev, int ctas, cudaStream_t s) 
     if (err != cudaSuccess) return err;
     raised.fetch_or(bit, std::memory_order_relaxed);
   }
-  k_attn_rows<D, NG, kTwoPlanes, R><<<ctas, (kAttnWarps + 1) * 32, AttnSmem<D, NG, R>::bytes(p.batch), s>>>(p);
-  return cudaSuccess;
+  return launch_early(k_attn_rows<D, NG, kTwoPlanes, R>, ctas, (kAttnWarps + 1) * 32, AttnSmem<D, NG, R>::bytes(p.batch), s, p);
 }
 
 template <bool kTwoPlanes, int R>

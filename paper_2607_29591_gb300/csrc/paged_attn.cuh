@@ -26,10 +26,9 @@ struct AttnParams {
 
 // One block of query rows of one sequence: row r of the sequence is query token
 // r / group, head r % group of the KV head.  Its tiles are those any of its rows
-// sees; one that sees nothing still counts one (empty) tile.
+// sees (none: all of them stand before position 0).
 struct RowBlock {
   int first, tiles;               // first tile of the sequence's positions; count
-  bool empty;
 };
 
 struct Sequence {
@@ -60,10 +59,9 @@ __device__ __forceinline__ RowBlock row_block(const AttnParams& p, const Sequenc
   const int lo = s.len - s.count + (r0 == 0 ? 0 : r0 / p.group);
   const int hi = s.len - s.count + (r1 == s.count * p.group ? s.count - 1 : (r1 - 1) / p.group);
   RowBlock b;
-  b.empty = hi < 0;
   const int from = p.window > 0 ? max(0, lo - p.window + 1) : 0;
   b.first = from / kTile;
-  b.tiles = b.empty ? 1 : hi / kTile - b.first + 1;
+  b.tiles = hi < 0 ? 0 : hi / kTile - b.first + 1;
   return b;
 }
 
