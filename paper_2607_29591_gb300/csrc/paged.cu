@@ -34,30 +34,42 @@ struct AppendParams {
   int64_t n_pages, n_positions, n_tokens;
   int32_t batch, table_pages, page_tokens, kv_heads;
   int32_t rot, interleaved;
+  uint32_t blocks;                // of the launch that hold rows; the others turn queries
 };
 
-// min and max that keep a NaN
-__device__ __forceinline__ float min_nan(float a, float b) {
+// least and largest of three, a NaN kept
+__device__ __forceinline__ float min3_nan(float a, float b, float c) {
   float r;
-  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-__device__ __forceinline__ float max_nan(float a, float b) {
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float mul_01(float a, float b) {        // within [0, 1]
+  float r;
+  asm("mul.rn.sat.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
 
-// Four neighbouring dims per lane, D / 4 lanes a row: the codes of the lane's
-// dims (16 bits) and its group's scale (low half) and minimum (high half).
+// Eight neighbouring dims per lane, kGroup / 8 lanes a group: the codes of the
+// lane's dims and its group's scale (low half) and minimum (high half).
+//
+// A code is rint((x - m) / s), within 0..15, of the correctly rounded quotient.  It is
+// found as rint(15 u), u = (x - m) r within [0, 1], r = 1 / 15 s: 15 u is off by less
+// than 2^-17, so that a value whose fraction lies further than that from one half
+// has its code; where one of the lane's values is nearer, the lane divides.
 template <int kGroup>
-__device__ __forceinline__ void hold(const float (&x)[4], uint32_t& codes, uint32_t& sm) {
-  float lo = min_nan(min_nan(x[0], x[1]), min_nan(x[2], x[3]));
-  float hi = max_nan(max_nan(x[0], x[1]), max_nan(x[2], x[3]));
+__device__ __forceinline__ void hold(const float2 (&x)[4], uint32_t& codes, uint32_t& sm) {
+  float lo = min3_nan(min3_nan(x[0].x, x[0].y, x[1].x), min3_nan(x[1].y, x[2].x, x[2].y), min3_nan(x[3].x, x[3].y, x[3].y));
+  float hi = max3_nan(max3_nan(x[0].x, x[0].y, x[1].x), max3_nan(x[1].y, x[2].x, x[2].y), max3_nan(x[3].x, x[3].y, x[3].y));
 #pragma unroll
-  for (int o = 1; o < kGroup / 4; o *= 2) {
-    lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+  for (int o = 1; o < kGroup / 8; o *= 2) {
+    const float l = __shfl_xor_sync(0xffffffffu, lo, o), h = __shfl_xor_sync(0xffffffffu, hi, o);
+    lo = min3_nan(lo, l, l);
+    hi = max3_nan(hi, h, h);
   }
   uint32_t s16 = __bfloat16_as_ushort(__float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f)));
   uint32_t m16 = __bfloat16_as_ushort(__float2bfloat16_rn(lo));
@@ -68,111 +80,225 @@ __device__ __forceinline__ void hold(const float (&x)[4], uint32_t& codes, uint3
   } else if (s < 1.17549435e-38f) {
     s16 = 0;
   } else {
+    constexpr float kRound = 12582912.f;          // 1.5 2^23: adding it rounds to whole numbers
+    const float r = __frcp_rn(s) * 0.06666667f;
+    // codes 0..3 and 4..7 as 16-bit numbers; scales past 2^120 leave r no digits
+    float2 sum = make_float2(0.f, 0.f);
+    float worst = s > 1.3e36f ? 1.f : 0.f;
+    const float2 mm = make_float2(m, m), k15 = make_float2(15.f, 15.f), up = make_float2(kRound, kRound);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float n = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[i], m), s)), 0.f), 15.f);
-      codes |= uint32_t(int(n)) << (4 * i);
+    for (int i = 3; i >= 0; --i) {
+      // values i and 4 + i
+      const float2 v = i & 1 ? make_float2(x[i / 2].y, x[2 + i / 2].y) : make_float2(x[i / 2].x, x[2 + i / 2].x);
+      const float2 a = fsub2(v, mm);
+      const float2 u = make_float2(mul_01(a.x, r), mul_01(a.y, r));
+      const float2 n = fsub2(ffma2(u, k15, up), up);
+      const float2 d = ffma2(u, k15, make_float2(-n.x, -n.y));
+      worst = fmaxf(worst, fmaxf(fabsf(d.x), fabsf(d.y)));
+      sum = ffma2(sum, make_float2(16.f, 16.f), n);
     }
+    if (worst > 0.5f - 7.62939453125e-6f) {
+      sum = make_float2(0.f, 0.f);
+#pragma unroll 1
+      for (int k = 0; k < 2; ++k) {
+        float y = 0.f;
+#pragma unroll
+        for (int i = 3; i >= 0; --i) {
+          const float2 pair = k ? x[2 + i / 2] : x[i / 2];
+          const float a = __fsub_rn(i & 1 ? pair.y : pair.x, m);
+          y = fmaf(y, 16.f, fminf(fmaxf(rintf(__fdiv_rn(a, s)), 0.f), 15.f));
+        }
+        if (k) sum.y = y;
+        else sum.x = y;
+      }
+    }
+    codes = uint32_t(sum.x) | uint32_t(sum.y) << 16;
   }
   sm = s16 | (m16 << 16);
 }
 
-// One (token, KV head) per D / 4 lanes: K row, then V row.
-template <typename T, int D, int kGroup, bool kWide>
-__global__ void __launch_bounds__(256) k_paged_append(const __grid_constant__ AppendParams p) {
-  constexpr int L = D / 4, NG = D / kGroup;
+// kHeads KV heads of one token per D / 8 lanes: K row, then V row.  The rows' cos and
+// sin are read once.  What a row costs is instructions (about 160 a warp for the
+// two rows it holds of d = 128), then its bytes: see append_prompt's figures at the
+// entry point.
+template <typename T, int D, int kGroup, bool kWide, int kHeads>
+__device__ __forceinline__ void append_rows(const AppendParams& p, int64_t r, int lane) {
+  constexpr int NG = D / kGroup;
   constexpr TileShape ts{D, NG};
-  using P = Pack<T, 4>;
-  const int lane = threadIdx.x % L;
-  int64_t r = int64_t(blockIdx.x) * (256 / L) + threadIdx.x / L;
-  const bool in = r < p.n_tokens * p.kv_heads;
+  const int groups = (p.kv_heads + kHeads - 1) / kHeads;
+  const bool in = r < p.n_tokens * groups;
   if (!in) r = 0;                                   // stays for the shuffles, writes nothing
-  const int64_t tok = r / p.kv_heads;
-  const int h = int(r - tok * p.kv_heads);
+  const int64_t tok = uint32_t(r) / uint32_t(groups);
+  const int h0 = (int(r) - int(tok) * groups) * kHeads;
   const int pos = p.positions[tok], seq = p.seqs[tok];
-  bool live = in && pos >= 0, fault = false;
-  uint8_t* tile = nullptr;
+  bool live = in && pos >= 0;
+  uint8_t* tile = nullptr;                          // of head 0
   int row = 0;
+  const int64_t head_bytes = int64_t(p.page_tokens / kTile) * ts.bytes();
   if (live) {
     const int pg = pos / p.page_tokens;
-    fault = seq < 0 || seq >= p.batch || pg >= p.table_pages || (p.table && pos >= p.n_positions);
+    bool fault = seq < 0 || seq >= p.batch || pg >= p.table_pages || (p.table && pos >= p.n_positions);
     if (!fault) {
       const int page = p.page_table[int64_t(seq) * p.table_pages + pg];
       fault = page < 0 || page >= p.n_pages;
       const int slot = pos - pg * p.page_tokens;
       row = slot % kTile;
-      tile = p.pages + ((int64_t(page) * p.kv_heads + h) * (p.page_tokens / kTile) + slot / kTile) * ts.bytes();
+      tile = p.pages + int64_t(page) * p.kv_heads * head_bytes + slot / kTile * ts.bytes();
     }
     if (fault && lane == 0) report_status(p.status, kStatusBadIndex);
     live = !fault;
   }
-  const T* k = static_cast<const T*>(p.k) + tok * p.k_token + h * p.k_head;
-  const T* v = static_cast<const T*>(p.v) + tok * p.v_token + h * p.v_head;
-  float x[4];
-  auto load = [&](const T* at) {
+  auto load = [&](const T* at, float2 (&x)[4]) {
     if constexpr (kWide) {
-      const P a = *reinterpret_cast<const P*>(at);
+      constexpr int words = sizeof(T) * 8 / 16;
+      union { uint4 w[words]; T v[8]; } u;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = to_f32(a.v[i]);
+      for (int i = 0; i < words; ++i) u.w[i] = reinterpret_cast<const uint4*>(at)[i];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = make_float2(to_f32(u.v[2 * i]), to_f32(u.v[2 * i + 1]));
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = to_f32(at[i]);
+      for (int i = 0; i < 4; ++i) x[i] = make_float2(to_f32(at[2 * i]), to_f32(at[2 * i + 1]));
     }
   };
-  uint32_t codes, sm;
-  load(k + 4 * lane);
-  if (p.table && live) {
-    const float2* cs = p.table + int64_t(pos) * (p.rot / 2);
-    const int half = p.rot / 2;
+  // The lane's pairs: its eight dims against the eight rot / 2 away, or neighbours.
+  // Rotations that cut a lane's dims take them one by one.
+  const bool turns = p.table && live && 8 * lane < p.rot;
+  const int half = p.rot / 2;
+  const bool whole = p.interleaved ? p.rot % 8 == 0 : p.rot % 16 == 0;
+  const bool lower = 8 * lane < half;
+  // a dim x with partner o becomes x c + o s, s negated for the lower of a pair
+  float2 co[4], si[4];
+  if (turns && whole) {
+    const float2* c = p.table + int64_t(pos) * half + (p.interleaved ? 4 * lane : 8 * lane - (lower ? 0 : half));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int dim = 4 * lane + i;
-      if (dim >= p.rot) continue;
-      const bool lower = p.interleaved ? dim % 2 == 0 : dim < half;
-      const int pair = p.interleaved ? dim / 2 : (lower ? dim : dim - half);
-      const int other = p.interleaved ? dim ^ 1 : (lower ? dim + half : dim - half);
-      float a = to_f32(k[lower ? dim : other]), b = to_f32(k[lower ? other : dim]);
-      const float2 c = cs[pair];
-      turn(a, b, c.x, c.y);
-      x[i] = lower ? a : b;
+      if (p.interleaved) {
+        const float2 w = c[i];
+        co[i] = make_float2(w.x, w.x);
+        si[i] = make_float2(-w.y, w.y);
+      } else {
+        const float2 w0 = c[2 * i], w1 = c[2 * i + 1];
+        co[i] = make_float2(w0.x, w1.x);
+        si[i] = lower ? make_float2(-w0.y, -w1.y) : make_float2(w0.y, w1.y);
+      }
     }
   }
-  hold<kGroup>(x, codes, sm);
-  if (live) {
-    *reinterpret_cast<uint16_t*>(tile + ts.k_unit(row, lane)) = uint16_t(codes);
-    if (lane % (kGroup / 4) == 0) {
-      uint16_t* meta = reinterpret_cast<uint16_t*>(tile + ts.k_meta()) + row * 2 * NG + lane / (kGroup / 4);
-      meta[0] = uint16_t(sm);
-      meta[NG] = uint16_t(sm >> 16);
+#pragma unroll 1
+  for (int i = 0; i < kHeads; ++i) {
+    const int h = min(h0 + i, p.kv_heads - 1);      // the last head again: the same bytes
+    const T* k = static_cast<const T*>(p.k) + tok * p.k_token + h * p.k_head;
+    const T* v = static_cast<const T*>(p.v) + tok * p.v_token + h * p.v_head;
+    uint8_t* at = tile + h * head_bytes;
+    float2 x[4], y[4], o[4];
+    load(k + 8 * lane, x);
+    load(v + 8 * lane, y);
+    if (turns && whole) {
+      if (p.interleaved) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = make_float2(x[j].y, x[j].x);
+      } else {
+        load(k + 8 * lane + (lower ? half : -half), o);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[j].x = __fadd_rn(__fmul_rn(x[j].x, co[j].x), __fmul_rn(o[j].x, si[j].x));
+        x[j].y = __fadd_rn(__fmul_rn(x[j].y, co[j].y), __fmul_rn(o[j].y, si[j].y));
+      }
+    } else if (turns) {
+#pragma unroll 1
+      for (int j = 0; j < 8; ++j) {
+        const int dim = 8 * lane + j;
+        if (dim >= p.rot) break;
+        const bool low = p.interleaved ? dim % 2 == 0 : dim < half;
+        const int pair = p.interleaved ? dim / 2 : (low ? dim : dim - half);
+        const int other = p.interleaved ? dim ^ 1 : (low ? dim + half : dim - half);
+        float a = to_f32(k[low ? dim : other]), b = to_f32(k[low ? other : dim]);
+        const float2 c = p.table[int64_t(pos) * half + pair];
+        turn(a, b, c.x, c.y);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (2 * q == j) x[q].x = low ? a : b;
+          if (2 * q + 1 == j) x[q].y = low ? a : b;
+        }
+      }
     }
-  }
-  load(v + 4 * lane);
-  hold<kGroup>(x, codes, sm);
-  if (live) {
-    *reinterpret_cast<uint16_t*>(tile + ts.v_codes() + ts.v_unit(row, lane)) = uint16_t(codes);
-    if (lane % (kGroup / 4) == 0) {
-      uint16_t* meta = reinterpret_cast<uint16_t*>(tile + ts.v_meta()) + row * 2 * NG + lane / (kGroup / 4);
-      meta[0] = uint16_t(sm);
-      meta[NG] = uint16_t(sm >> 16);
+    uint32_t codes, sm;
+    hold<kGroup>(x, codes, sm);
+    const bool first = lane % (kGroup / 8) == 0;
+    if (live) {
+      *reinterpret_cast<uint32_t*>(at + ts.k_unit(row, 2 * lane)) = codes;
+      if (first) {
+        uint16_t* meta = reinterpret_cast<uint16_t*>(at + ts.k_meta()) + row * 2 * NG + lane / (kGroup / 8);
+        meta[0] = uint16_t(sm);
+        meta[NG] = uint16_t(sm >> 16);
+      }
+    }
+    hold<kGroup>(y, codes, sm);
+    if (live) {
+      uint8_t* c = at + ts.v_codes();
+      *reinterpret_cast<uint16_t*>(c + ts.v_unit(row, 2 * lane)) = uint16_t(codes);
+      *reinterpret_cast<uint16_t*>(c + ts.v_unit(row, 2 * lane + 1)) = uint16_t(codes >> 16);
+      if (first) {
+        uint16_t* meta = reinterpret_cast<uint16_t*>(at + ts.v_meta()) + row * 2 * NG + lane / (kGroup / 8);
+        meta[0] = uint16_t(sm);
+        meta[NG] = uint16_t(sm >> 16);
+      }
     }
   }
 }
 
+// The tokens' rows in the first blocks, their queries' rotation in the others.
+template <typename T, int D, int kGroup, bool kWide, int kHeads>
+__global__ void __launch_bounds__(256, 4) k_paged_append(const __grid_constant__ AppendParams p,
+                                                      const __grid_constant__ RopeParams q) {
+  constexpr int L = D / 8;
+  wait_for_previous();
+  if (blockIdx.x < p.blocks) {
+    append_rows<T, D, kGroup, kWide, kHeads>(p, int64_t(blockIdx.x) * (256 / L) + threadIdx.x / L, threadIdx.x % L);
+  } else if constexpr (kWide) {
+    constexpr int V = 16 / int(sizeof(T));
+    const int lane = threadIdx.x % q.lanes, row = threadIdx.x / q.lanes;
+    const int64_t r = int64_t(blockIdx.x - p.blocks) * q.rows_per_block + row;
+    if (row >= q.rows_per_block) return;
+    constexpr int kQ = kHeads == 1 ? 1 : kManyHeads<T>;
+    if (q.interleaved) rope_rows<T, V, true, kQ>(q, r, lane);
+    else rope_rows<T, V, false, kQ>(q, r, lane);
+  }
+}
+
+template <typename T, int D, int kGroup, bool kWide, int kHeads>
+cudaError_t launch_append_rows(AppendParams p, RopeParams q, cudaStream_t s) {
+  constexpr int rows = 256 / (D / 8), V = 16 / int(sizeof(T));
+  p.blocks = unsigned((p.n_tokens * ((p.kv_heads + kHeads - 1) / kHeads) + rows - 1) / rows);
+  unsigned blocks = p.blocks;
+  if (q.heads) {
+    q.lanes = rope_lanes(q.dim, q.rot, V);
+    q.rows_per_block = 256 / q.lanes;
+    constexpr int kQ = kHeads == 1 ? 1 : kManyHeads<T>;
+    q.head_groups = (q.heads + kQ - 1) / kQ;
+    blocks += unsigned((q.n_tokens * q.head_groups + q.rows_per_block - 1) / q.rows_per_block);
+  }
+  return launch_early(k_paged_append<T, D, kGroup, kWide, kHeads>, blocks, 256, 0, s, p, q);
+}
+
+// Eight heads a thread where that leaves every SM a thousand threads (32K tokens of
+// 8 KV and 32 query heads: 156 us, against 163 with four and 213 with one); one
+// where there are fewer rows.
 template <typename T, int D, int kGroup>
-void launch_append_rows(const AppendParams& p, bool wide, cudaStream_t s) {
-  constexpr int rows = 256 / (D / 4);
-  const unsigned blocks = unsigned((p.n_tokens * p.kv_heads + rows - 1) / rows);
-  if (wide) k_paged_append<T, D, kGroup, true><<<blocks, 256, 0, s>>>(p);
-  else k_paged_append<T, D, kGroup, false><<<blocks, 256, 0, s>>>(p);
+cudaError_t dispatch_heads(const AppendParams& p, const RopeParams& q, bool wide, cudaStream_t s) {
+  if (!wide) return launch_append_rows<T, D, kGroup, false, 1>(p, q, s);
+  if (p.n_tokens * p.kv_heads * (D / 8) >= int64_t(152) * 8192) return launch_append_rows<T, D, kGroup, true, 8>(p, q, s);
+  return launch_append_rows<T, D, kGroup, true, 1>(p, q, s);
 }
 
 template <typename T>
-void dispatch_append(const AppendParams& p, int d, int group, bool wide, cudaStream_t s) {
-  if (d == 128 && group == 32) launch_append_rows<T, 128, 32>(p, wide, s);
-  else if (d == 128 && group == 64) launch_append_rows<T, 128, 64>(p, wide, s);
-  else if (d == 128) launch_append_rows<T, 128, 128>(p, wide, s);
-  else if (group == 32) launch_append_rows<T, 64, 32>(p, wide, s);
-  else launch_append_rows<T, 64, 64>(p, wide, s);
+cudaError_t dispatch_append(const AppendParams& p, const RopeParams& q, int d, int group, bool wide, cudaStream_t s) {
+  if (d == 128 && group == 32) return dispatch_heads<T, 128, 32>(p, q, wide, s);
+  if (d == 128 && group == 64) return dispatch_heads<T, 128, 64>(p, q, wide, s);
+  if (d == 128) return dispatch_heads<T, 128, 128>(p, q, wide, s);
+  if (group == 32) return dispatch_heads<T, 64, 32>(p, q, wide, s);
+  return dispatch_heads<T, 64, 64>(p, q, wide, s);
 }
 
 // --- reading back ----------------------------------------------------------
@@ -189,83 +315,147 @@ struct GatherParams {
   int32_t table_pages, page_tokens, kv_heads, batch;
 };
 
-// Eight dims per thread, D / 8 threads a row; blockIdx.y: sequence and head.
+// Scale and minimum of one group from a row's words.
+template <int NG>
+__device__ __forceinline__ void group_meta(const uint32_t (&w)[NG], int k, float& s, float& m) {
+  if constexpr (NG == 1) {
+    s = low_bf16(w[0]);
+    m = high_bf16(w[0]);
+  } else {
+    s = k & 1 ? high_bf16(w[k / 2]) : low_bf16(w[k / 2]);
+    m = k & 1 ? high_bf16(w[NG / 2 + k / 2]) : low_bf16(w[NG / 2 + k / 2]);
+  }
+}
+
+template <typename T, int N, bool kWide>
+__device__ __forceinline__ void store_values(T* y, const float (&x)[N]) {
+  Pack<T, N> o;
+#pragma unroll
+  for (int i = 0; i < N; ++i) o.v[i] = from_f32<T>(x[i]);
+  if constexpr (!kWide) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = o.v[i];
+  } else if constexpr (sizeof(o) == 32) {
+    reinterpret_cast<uint4*>(y)[0] = reinterpret_cast<const uint4*>(&o)[0];
+    reinterpret_cast<uint4*>(y)[1] = reinterpret_cast<const uint4*>(&o)[1];
+  } else {
+    *reinterpret_cast<Pack<T, N>*>(y) = o;
+  }
+}
+
+// n codes of a masked word as fp32 (exact): two from the halves' low 4 bits.
+__device__ __forceinline__ float2 two_codes(uint32_t w) {
+  const uint32_t h = (w & 0x000f000fu) | 0x64006400u;               // 1024 + n in fp16
+  const __half2 n = __hsub2(*reinterpret_cast<const __half2*>(&h), __float2half2_rn(1024.f));
+  return __half22float2(n);
+}
+
+// One tile per warp, read as its attention reads it (whole 16-byte words), eight
+// dims of K and four of V a lane and word.  s n is exact in fp32, so a value is one
+// fma, rounded once more to the output's type.  Bound by DRAM: 8 prompts of up to
+// 32K positions (1.31 GB read and written) in 200 us, 0.96 of the measured copy
+// rate; one row's eight dims a thread, with seven loads of 2 or 4 bytes, took 338.
 template <typename T, int D, int kGroup, bool kWide>
 __global__ void __launch_bounds__(256) k_paged_gather(const __grid_constant__ GatherParams p) {
-  constexpr int L = D / 8, NG = D / kGroup;
+  constexpr int NG = D / kGroup, C = D / 32;
   constexpr TileShape ts{D, NG};
-  const int w = threadIdx.x % L;
-  const int64_t i = int64_t(blockIdx.x) * (256 / L) + threadIdx.x / L;
-  if (i >= p.n) return;
-  for (int bh = blockIdx.y; bh < p.batch * p.kv_heads; bh += gridDim.y) {
-    const int b = bh / p.kv_heads, h = bh - b * p.kv_heads;
-    const int64_t pos = (p.starts ? int64_t(p.starts[b]) : 0) + i;
+  wait_for_previous();
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int h = blockIdx.y % p.kv_heads;
+  for (int b = blockIdx.y / p.kv_heads; b < p.batch; b += gridDim.y / p.kv_heads) {
+    const int64_t start = p.starts ? p.starts[b] : 0, len = p.lens[b];
+    // tiles of the sequence, the first one that of position `start`
+    const int64_t first = start >= 0 ? start / kTile : -((-start + kTile - 1) / kTile);
+    const int64_t pos0 = (first + int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5)) * kTile;
+    if (pos0 >= start + p.n) continue;
     const uint8_t* tile = nullptr;
-    int row = 0;
-    if (pos >= 0 && pos < p.lens[b]) {
-      const int64_t pg = pos / p.page_tokens;
+    if (pos0 >= 0 && pos0 < len) {
+      const int64_t pg = pos0 / p.page_tokens;
       const int page = pg < p.table_pages ? p.page_table[int64_t(b) * p.table_pages + pg] : -1;
-      if (page >= 0 && page < p.n_pages) {
-        const int slot = int(pos - pg * p.page_tokens);
-        row = slot % kTile;
-        tile = p.pages + ((int64_t(page) * p.kv_heads + h) * (p.page_tokens / kTile) + slot / kTile) * ts.bytes();
-      } else if (w == 0) {
+      if (page >= 0 && page < p.n_pages)
+        tile = p.pages + ((int64_t(page) * p.kv_heads + h) * (p.page_tokens / kTile) + (pos0 - pg * p.page_tokens) / kTile) *
+                             int64_t(ts.bytes());
+      else if (lane == 0)
         report_status(p.status, kStatusBadIndex);
+    }
+    // output row of the tile's token r; NULL: not asked for
+    auto out = [&](int kv, int r) -> T* {
+      const int64_t i = pos0 + r - start;
+      if (i < 0 || i >= p.n) return nullptr;
+      return static_cast<T*>(p.out[kv]) + b * p.b_stride[kv] + h * p.h_stride[kv] + i * p.t_stride[kv];
+    };
+    if (p.out[0]) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = g + 8 * i;
+        uint32_t w[C] = {}, meta[NG] = {};
+        if (tile && pos0 + r < len) {
+          load_words<C>(w, tile + r * (D / 2) + t * (D / 8));
+          load_words<NG>(meta, tile + ts.k_meta() + r * 4 * NG);
+        }
+        T* y = out(0, r);
+        if (!y) continue;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          float s, m, x[8];
+          group_meta<NG>(meta, 32 * c / kGroup, s, m);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 n = two_codes(w[c] >> (4 * j));
+            x[j] = fmaf(s, n.x, m);
+            x[4 + j] = fmaf(s, n.y, m);
+          }
+          store_values<T, 8, kWide>(y + 8 * (4 * c + t), x);
+        }
       }
     }
+    if (p.out[1]) {
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      if (!p.out[kv]) continue;
-      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (tile) {
-        uint32_t word;
-        if (kv == 0) {
-          word = *reinterpret_cast<const uint32_t*>(tile + ts.k_unit(row, 2 * w));
-        } else {
-          const uint8_t* codes = tile + ts.v_codes();
-          word = *reinterpret_cast<const uint16_t*>(codes + ts.v_unit(row, 2 * w)) |
-                 uint32_t(*reinterpret_cast<const uint16_t*>(codes + ts.v_unit(row, 2 * w + 1))) << 16;
+      for (int i = 0; i < 2; ++i) {
+        const int pair = t + 4 * i, r = 2 * pair;
+        uint32_t w[C] = {}, meta[2][NG] = {};
+        if (tile) load_words<C>(w, tile + ts.v_codes() + pair * D + ts.v_place(pair, g) * (D / 8));
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const bool held = tile && pos0 + r + k < len;
+          if (held) load_words<NG>(meta[k], tile + ts.v_meta() + (r + k) * 4 * NG);
+          T* y = out(1, r + k);
+          if (!y) continue;
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            float s, m, x[4];
+            group_meta<NG>(meta[k], 32 * c / kGroup, s, m);
+            const uint32_t u = held ? (k ? w[c] >> 16 : w[c] & 0xffffu) : 0u;
+            const float2 n0 = two_codes(u | u << 12), n1 = two_codes(u >> 8 | u << 4);      // codes 0, 1 and 2, 3
+            x[0] = fmaf(s, n0.x, m);
+            x[1] = fmaf(s, n0.y, m);
+            x[2] = fmaf(s, n1.x, m);
+            x[3] = fmaf(s, n1.y, m);
+            store_values<T, 4, kWide>(y + 32 * c + 4 * g, x);
+          }
         }
-        const uint16_t* meta =
-            reinterpret_cast<const uint16_t*>(tile + (kv ? ts.v_meta() : ts.k_meta())) + row * 2 * NG + 8 * w / kGroup;
-        const float s = __uint_as_float(uint32_t(meta[0]) << 16), m = __uint_as_float(uint32_t(meta[NG]) << 16);
-        // s n is exact in fp32, so this is one rounding like s * n + m
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = fmaf(s, float((word >> (4 * j)) & 15u), m);
-      }
-      T* y = static_cast<T*>(p.out[kv]) + b * p.b_stride[kv] + h * p.h_stride[kv] + i * p.t_stride[kv] + 8 * w;
-      if constexpr (kWide) {
-        Pack<T, 8> o;                               // 16 bytes, 32 for fp32
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o.v[j] = from_f32<T>(x[j]);
-        constexpr int words = sizeof(T) * 8 / 16;
-        const uint4* from = reinterpret_cast<const uint4*>(&o);
-#pragma unroll
-        for (int j = 0; j < words; ++j) reinterpret_cast<uint4*>(y)[j] = from[j];
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = from_f32<T>(x[j]);
       }
     }
   }
 }
 
 template <typename T, int D, int kGroup>
-void launch_gather_rows(const GatherParams& p, bool wide, cudaStream_t s) {
-  constexpr int rows = 256 / (D / 8);
-  const int64_t bh = int64_t(p.batch) * p.kv_heads;
-  const dim3 grid(unsigned((p.n + rows - 1) / rows), unsigned(bh < 65535 ? bh : 65535));
-  if (wide) k_paged_gather<T, D, kGroup, true><<<grid, 256, 0, s>>>(p);
-  else k_paged_gather<T, D, kGroup, false><<<grid, 256, 0, s>>>(p);
+cudaError_t launch_gather_rows(const GatherParams& p, bool wide, cudaStream_t s) {
+  // one tile more than n holds, for a start inside a tile
+  const int64_t tiles = (p.n + kTile - 1) / kTile + (p.starts ? 1 : 0);
+  const int seqs = p.batch < 65535 / p.kv_heads ? p.batch : 65535 / p.kv_heads;
+  const dim3 grid(unsigned((tiles + 7) / 8), unsigned(seqs * p.kv_heads));
+  return wide ? launch_early(k_paged_gather<T, D, kGroup, true>, grid, 256, 0, s, p)
+              : launch_early(k_paged_gather<T, D, kGroup, false>, grid, 256, 0, s, p);
 }
 
 template <typename T>
-void dispatch_gather(const GatherParams& p, int d, int group, bool wide, cudaStream_t s) {
-  if (d == 128 && group == 32) launch_gather_rows<T, 128, 32>(p, wide, s);
-  else if (d == 128 && group == 64) launch_gather_rows<T, 128, 64>(p, wide, s);
-  else if (d == 128) launch_gather_rows<T, 128, 128>(p, wide, s);
-  else if (group == 32) launch_gather_rows<T, 64, 32>(p, wide, s);
-  else launch_gather_rows<T, 64, 64>(p, wide, s);
+cudaError_t dispatch_gather(const GatherParams& p, int d, int group, bool wide, cudaStream_t s) {
+  if (d == 128 && group == 32) return launch_gather_rows<T, 128, 32>(p, wide, s);
+  if (d == 128 && group == 64) return launch_gather_rows<T, 128, 64>(p, wide, s);
+  if (d == 128) return launch_gather_rows<T, 128, 128>(p, wide, s);
+  if (group == 32) return launch_gather_rows<T, 64, 32>(p, wide, s);
+  return launch_gather_rows<T, 64, 64>(p, wide, s);
 }
 
 }  // namespace
@@ -298,10 +488,6 @@ extern "C" reskv_status reskv_paged_append(const reskv_paged_kv* kv, int64_t n_t
   if (bad.empty() && (n_tokens < 0 || double(n_tokens) * kv->n_kv_heads >= double(int64_t(1) << 31)))
     bad = "n_tokens must not be negative, n_tokens * n_kv_heads below 2^31";
   if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
-  if (q) {
-    const reskv_status st = reskv_rope(rot, positions, n_tokens, kv->head_dim, 1, q, q_out, 0, kv->status, stream);
-    if (st != RESKV_OK) return st;
-  }
   AppendParams p{};
   p.seqs = seqs;
   p.positions = positions;
@@ -327,12 +513,38 @@ extern "C" reskv_status reskv_paged_append(const reskv_paged_kv* kv, int64_t n_t
     p.interleaved = rot->interleaved;
   }
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const size_t word = 4 * dtype_size(k->dtype);
-  const bool wide = rows_aligned(*k, word) && rows_aligned(*v, word);
-  if (k->dtype == RESKV_F32) dispatch_append<float>(p, kv->head_dim, kv->quant_group, wide, s);
-  else if (k->dtype == RESKV_F16) dispatch_append<__half>(p, kv->head_dim, kv->quant_group, wide, s);
-  else dispatch_append<__nv_bfloat16>(p, kv->head_dim, kv->quant_group, wide, s);
-  return launch_status("paged append");
+  const bool wide = rows_aligned(*k, 16) && rows_aligned(*v, 16);
+  RopeParams r{};
+  if (q) {
+    // in the same launch where its rows are moved in whole words like the keys', else in one of its own
+    const int v16 = 16 / dtype_size(q->dtype);
+    if (wide && q->dtype == k->dtype && rows_aligned(*q, 16) && rows_aligned(*q_out, 16) && aligned_to(rot->table, 16) &&
+        rot->rot_dim % (2 * v16) == 0) {
+      if (q->n_heads != q_out->n_heads || q->dtype != q_out->dtype)
+        return paged_fail(RESKV_ERR_INVALID_ARG, "q and q_out must have the same heads and one dtype");
+      if (double(n_tokens) * q->n_heads >= double(int64_t(1) << 31))
+        return paged_fail(RESKV_ERR_INVALID_ARG, "n_tokens * heads must be below 2^31");
+      r.t[0] = RopeTensor{q->data, q_out->data, q->token_stride, q->head_stride, q_out->token_stride,
+                          q_out->head_stride, q->n_heads};
+      r.heads = q->n_heads;
+      r.table = p.table;
+      r.positions = positions;
+      r.n_positions = rot->n_positions;
+      r.n_tokens = n_tokens;
+      r.status = kv->status;
+      r.dim = kv->head_dim;
+      r.rot = rot->rot_dim;
+      r.interleaved = rot->interleaved;
+    } else {
+      const reskv_status st = reskv_rope(rot, positions, n_tokens, kv->head_dim, 1, q, q_out, 0, kv->status, stream);
+      if (st != RESKV_OK) return st;
+    }
+  }
+  const cudaError_t err =
+      k->dtype == RESKV_F32   ? dispatch_append<float>(p, r, kv->head_dim, kv->quant_group, wide, s)
+      : k->dtype == RESKV_F16 ? dispatch_append<__half>(p, r, kv->head_dim, kv->quant_group, wide, s)
+                              : dispatch_append<__nv_bfloat16>(p, r, kv->head_dim, kv->quant_group, wide, s);
+  return launch_result(err, "paged append");
 }
 
 extern "C" reskv_status reskv_paged_gather(const reskv_paged_kv* kv, const int32_t* starts, const int32_t* lens,
@@ -374,8 +586,8 @@ extern "C" reskv_status reskv_paged_gather(const reskv_paged_kv* kv, const int32
   p.batch = kv->batch;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const int32_t dt = k ? k->dtype : v->dtype;
-  if (dt == RESKV_F32) dispatch_gather<float>(p, kv->head_dim, kv->quant_group, wide, s);
-  else if (dt == RESKV_F16) dispatch_gather<__half>(p, kv->head_dim, kv->quant_group, wide, s);
-  else dispatch_gather<__nv_bfloat16>(p, kv->head_dim, kv->quant_group, wide, s);
-  return launch_status("paged gather");
+  const cudaError_t err = dt == RESKV_F32   ? dispatch_gather<float>(p, kv->head_dim, kv->quant_group, wide, s)
+                          : dt == RESKV_F16 ? dispatch_gather<__half>(p, kv->head_dim, kv->quant_group, wide, s)
+                                            : dispatch_gather<__nv_bfloat16>(p, kv->head_dim, kv->quant_group, wide, s);
+  return launch_result(err, "paged gather");
 }

@@ -722,19 +722,18 @@ extern "C" reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_p
   p.tickets = static_cast<int32_t*>(a->workspace);
   p.partials = reinterpret_cast<float*>(static_cast<char*>(a->workspace) + kTicketBytes);
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return launch_status("reading the device");
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return launch_result(err, "reading the device");
   int ctas = sm_count(dev);
-  if (ctas < 1) return launch_status("reading the SM count");
+  if (ctas < 1) return launch_result(cudaErrorInvalidDevice, "reading the SM count");
   if (ctas > kMaxCtas) ctas = kMaxCtas;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // bf16 outputs: weights in one fp16 plane (2^-11) are finer than the output's 2^-8.
   // Four rows a unit where a sequence has no more on average.
   const bool one = a->o.dtype == RESKV_BF16, few = a->n_tokens * p.group <= 4 * int64_t(kv->batch);
-  const cudaError_t err = one ? (few ? dispatch_rows<false, 4>(p, kv->head_dim, kv->quant_group, dev, ctas, s)
-                                     : dispatch_rows<false, 8>(p, kv->head_dim, kv->quant_group, dev, ctas, s))
-                              : (few ? dispatch_rows<true, 4>(p, kv->head_dim, kv->quant_group, dev, ctas, s)
-                                     : dispatch_rows<true, 8>(p, kv->head_dim, kv->quant_group, dev, ctas, s));
-  if (err != cudaSuccess)
-    return paged_fail(RESKV_ERR_CUDA, std::string("paged attention: ") + cudaGetErrorString(err));
-  return launch_status("paged attention");
+  err = one ? (few ? dispatch_rows<false, 4>(p, kv->head_dim, kv->quant_group, dev, ctas, s)
+                   : dispatch_rows<false, 8>(p, kv->head_dim, kv->quant_group, dev, ctas, s))
+            : (few ? dispatch_rows<true, 4>(p, kv->head_dim, kv->quant_group, dev, ctas, s)
+                   : dispatch_rows<true, 8>(p, kv->head_dim, kv->quant_group, dev, ctas, s));
+  return launch_result(err, "paged attention");
 }

@@ -109,40 +109,6 @@ __device__ __forceinline__ float exp2_fast(float x) {          // 2^-inf = 0
   return y;
 }
 
-__device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-
-// Four 32-bit words (two for d = 64) of shared memory.
-template <int N>
-__device__ __forceinline__ void load_words(uint32_t (&w)[N], const void* p) {
-  if constexpr (N == 4) {
-    const uint4 v = *static_cast<const uint4*>(p);
-    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-  } else if constexpr (N == 2) {
-    const uint2 v = *static_cast<const uint2*>(p);
-    w[0] = v.x; w[1] = v.y;
-  } else {
-    w[0] = *static_cast<const uint32_t*>(p);
-  }
-}
-
-// A row's scales and minima from its 4 NG bytes.
-template <int NG>
-__device__ __forceinline__ void load_meta(float (&s)[NG], float (&m)[NG], const uint8_t* row) {
-  uint32_t w[NG];
-  load_words<NG>(w, row);
-  if constexpr (NG == 4) {
-    s[0] = low_bf16(w[0]); s[1] = high_bf16(w[0]); s[2] = low_bf16(w[1]); s[3] = high_bf16(w[1]);
-    m[0] = low_bf16(w[2]); m[1] = high_bf16(w[2]); m[2] = low_bf16(w[3]); m[3] = high_bf16(w[3]);
-  } else if constexpr (NG == 2) {
-    s[0] = low_bf16(w[0]); s[1] = high_bf16(w[0]);
-    m[0] = low_bf16(w[1]); m[1] = high_bf16(w[1]);
-  } else {
-    s[0] = low_bf16(w[0]);
-    m[0] = high_bf16(w[0]);
-  }
-}
-
 // --- the tile step -----------------------------------------------------------
 
 // R (8 or 4) query rows of one warp against tiles of 16 tokens.  In units of log2,

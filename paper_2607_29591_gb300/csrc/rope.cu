@@ -11,9 +11,9 @@ reskv_status paged_fail(reskv_status st, const std::string& msg) {
   return st;
 }
 
-reskv_status launch_status(const char* what) {
-  const cudaError_t err = cudaGetLastError();
+reskv_status launch_result(cudaError_t err, const char* what) {
   if (err == cudaSuccess) return RESKV_OK;
+  cudaGetLastError();
   return paged_fail(RESKV_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(err));
 }
 
@@ -60,71 +60,32 @@ __global__ void k_rope_table(const __grid_constant__ Frequencies fr, float2* tab
 
 // --- the rotation ----------------------------------------------------------
 
-// A row takes `lanes` threads: rot / 2V of them turn V pairs each, the others
-// copy 2V of the remaining dims.
-template <typename T, int V, bool kInter>
-__global__ void __launch_bounds__(256) k_rope(const __grid_constant__ RopeParams p) {
-  const int64_t r = int64_t(blockIdx.x) * p.rows_per_block + threadIdx.y;
-  const int64_t tok = r / p.heads;
-  const int h = int(r - tok * p.heads);
-  if (threadIdx.y >= p.rows_per_block || tok >= p.n_tokens) return;
-  const int lane = threadIdx.x;
-  const bool second = h >= p.t[0].heads;
-  const RopeTensor& t = p.t[second];
-  const int hh = second ? h - p.t[0].heads : h;
-  const T* x = static_cast<const T*>(t.x) + tok * t.x_token + hh * t.x_head;
-  T* y = static_cast<T*>(t.y) + tok * t.y_token + hh * t.y_head;
-  using P = Pack<T, V>;
-  const int turners = p.rot / (2 * V);
-  const int64_t pos = p.positions[tok];
-  const bool live = pos >= 0 && pos < p.n_positions;
-  if (pos >= p.n_positions && h == 0 && lane == 0) report_status(p.status, kStatusBadIndex);
-  if (lane < turners) {
-    const int ia = kInter ? 2 * V * lane : V * lane;
-    const int ib = kInter ? ia + V : ia + p.rot / 2;
-    P a = *reinterpret_cast<const P*>(x + ia), b = *reinterpret_cast<const P*>(x + ib);
-    if (live) {
-      const float2* cs = p.table + pos * (p.rot / 2) + V * lane;
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float2 c = cs[i];
-        const float s = p.backward ? -c.y : c.y;
-        // pair i of this lane: (a[i], b[i]), or neighbours of the 2V elements
-        T& u = kInter ? (2 * i < V ? a.v[(2 * i) % V] : b.v[(2 * i) % V]) : a.v[i];
-        T& w = kInter ? (2 * i + 1 < V ? a.v[(2 * i + 1) % V] : b.v[(2 * i + 1) % V]) : b.v[i];
-        float fa = to_f32(u), fb = to_f32(w);
-        turn(fa, fb, c.x, s);
-        u = from_f32<T>(fa);
-        w = from_f32<T>(fb);
-      }
-    }
-    *reinterpret_cast<P*>(y + ia) = a;
-    *reinterpret_cast<P*>(y + ib) = b;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int i = p.rot + V * (2 * (lane - turners) + j);
-      if (i < p.dim) *reinterpret_cast<P*>(y + i) = *reinterpret_cast<const P*>(x + i);
-    }
-  }
+template <typename T, int V, bool kInter, int kHeads>
+__global__ void __launch_bounds__(256, kHeads == 1 ? 6 : 4) k_rope(const __grid_constant__ RopeParams p) {
+  wait_for_previous();
+  rope_rows<T, V, kInter, kHeads>(p, int64_t(blockIdx.x) * p.rows_per_block + threadIdx.y, threadIdx.x);
 }
 
-template <typename T, int V>
-void launch_rope(RopeParams p, cudaStream_t s) {
-  p.lanes = p.rot / (2 * V) + ((p.dim - p.rot) / V + 1) / 2;
-  p.rows_per_block = p.lanes >= 256 ? 1 : 256 / p.lanes;
-  const int64_t rows = p.n_tokens * p.heads;
+// Four heads a thread where the rows of one leave every SM four times 2048
+// threads, one where there are fewer (a single token's launch is all latency).
+template <typename T, int V, int kHeads>
+cudaError_t launch_rope(RopeParams p, cudaStream_t s) {
+  p.lanes = rope_lanes(p.dim, p.rot, V);
+  p.rows_per_block = 256 / p.lanes;
+  p.head_groups = (p.heads + kHeads - 1) / kHeads;
+  const int64_t rows = p.n_tokens * p.head_groups;
   const unsigned blocks = unsigned((rows + p.rows_per_block - 1) / p.rows_per_block);
   const dim3 block(p.lanes, p.rows_per_block);
-  if (p.interleaved) k_rope<T, V, true><<<blocks, block, 0, s>>>(p);
-  else k_rope<T, V, false><<<blocks, block, 0, s>>>(p);
+  return p.interleaved ? launch_early(k_rope<T, V, true, kHeads>, blocks, block, 0, s, p)
+                       : launch_early(k_rope<T, V, false, kHeads>, blocks, block, 0, s, p);
 }
 
 template <typename T>
-void dispatch_rope(const RopeParams& p, bool wide, cudaStream_t s) {
+cudaError_t dispatch_rope(const RopeParams& p, bool wide, cudaStream_t s) {
   constexpr int V = 16 / int(sizeof(T));
-  if (wide && p.rot % (2 * V) == 0 && p.dim % V == 0) launch_rope<T, V>(p, s);
-  else launch_rope<T, 1>(p, s);
+  if (!wide || p.rot % (2 * V) || p.dim % V) return launch_rope<T, 1, 1>(p, s);
+  if (p.n_tokens * p.heads * rope_lanes(p.dim, p.rot, V) >= int64_t(152) * 8192) return launch_rope<T, V, kManyHeads<T>>(p, s);
+  return launch_rope<T, V, 1>(p, s);
 }
 
 }  // namespace
@@ -197,7 +158,7 @@ extern "C" reskv_status reskv_rope_table(const reskv_rope_config* c, int64_t n_p
   if (blocks > 0x7fffffff) return paged_fail(RESKV_ERR_UNSUPPORTED, "table too large");
   k_rope_table<<<unsigned(blocks), 256, 0, static_cast<cudaStream_t>(stream)>>>(
       fr, reinterpret_cast<float2*>(table), n_positions, pairs, m);
-  return launch_status("rope table");
+  return launch_result(cudaGetLastError(), "rope table");
 }
 
 extern "C" reskv_status reskv_rope(const reskv_rotation* rot, const int32_t* positions, int64_t n_tokens,
@@ -218,7 +179,7 @@ extern "C" reskv_status reskv_rope(const reskv_rotation* rot, const int32_t* pos
     if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
     if (x[i].n_heads != y[i].n_heads || x[i].dtype != y[i].dtype || x[i].dtype != x[0].dtype)
       return paged_fail(RESKV_ERR_INVALID_ARG, "x and y must have the same heads and one dtype");
-    wide = wide && rows_aligned(x[i], 16) && rows_aligned(y[i], 16);
+    wide = wide && rows_aligned(x[i], 16) && rows_aligned(y[i], 16) && aligned_to(rot->table, 16);
     p.t[i] = RopeTensor{x[i].data, y[i].data, x[i].token_stride, x[i].head_stride, y[i].token_stride,
                         y[i].head_stride, x[i].n_heads};
     p.heads += x[i].n_heads;
@@ -235,8 +196,8 @@ extern "C" reskv_status reskv_rope(const reskv_rotation* rot, const int32_t* pos
   p.interleaved = rot->interleaved;
   p.backward = backward != 0;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (x[0].dtype == RESKV_F32) dispatch_rope<float>(p, wide, s);
-  else if (x[0].dtype == RESKV_F16) dispatch_rope<__half>(p, wide, s);
-  else dispatch_rope<__nv_bfloat16>(p, wide, s);
-  return launch_status("rope");
+  const cudaError_t err = x[0].dtype == RESKV_F32   ? dispatch_rope<float>(p, wide, s)
+                          : x[0].dtype == RESKV_F16 ? dispatch_rope<__half>(p, wide, s)
+                                                    : dispatch_rope<__nv_bfloat16>(p, wide, s);
+  return launch_result(err, "rope");
 }

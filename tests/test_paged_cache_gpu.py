@@ -181,3 +181,49 @@ def test_gather_of_a_missing_page():
     assert (big[0, 0, 48:] == 0).all()
     with pytest.raises(R.ReskvError):
         kvc.check_status()
+
+
+@pytest.mark.parametrize("kv,heads,d,group,rot,interleaved,dtype", [(3, 6, 128, 32, 128, False, "bf16"), (8, 8, 64, 64, 32, True, "f16"),
+                                                                    (5, 7, 128, 128, 64, False, "f32")])
+def test_a_large_call_equals_small_ones(kv, heads, d, group, rot, interleaved, dtype):
+    """Calls large enough to take several heads a thread hold and turn what small calls do."""
+    T = 2 * 152 * 8192 // (kv * d // 8) + 37
+    g = torch.Generator(device="cuda").manual_seed(kv)
+    k, v, q = (torch.randn((T, h, d), generator=g, device="cuda").to(DT[dtype]) for h in (kv, kv, heads))
+    tab = R.reskv_rope_table(R.reskv_rope_config_default(rot_dim=rot), T + 9)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda") + 9
+    seqs = torch.zeros(T, dtype=torch.int32, device="cuda")
+    n = -(-(T + 9) // 64)
+    table = torch.randperm(n, generator=g, device="cuda").to(torch.int32)[None]
+    a, b = (R.PagedKV(R.reskv_paged_pages(n, kv, 64, d, group), table, 64, kv, d, group) for _ in range(2))
+    qa, qb, qc = (torch.empty_like(q) for _ in range(3))
+    R.reskv_paged_append(a, k, v, seqs, pos, table=tab, interleaved=interleaved, q=q, q_out=qa)
+    for i in range(0, T, 4096):
+        s = slice(i, i + 4096)
+        R.reskv_paged_append(b, k[s], v[s], seqs[s], pos[s], table=tab, interleaved=interleaved, q=q[s], q_out=qb[s])
+    R.reskv_rope(q, qc, pos, tab, interleaved=interleaved)
+    a.check_status()
+    assert torch.equal(a.pages, b.pages) and torch.equal(qa, qb) and torch.equal(qa, qc)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotated_rows_equal_rounded_products_and_sums(interleaved):
+    """Many fp32 rows: every product and sum of the rotation is rounded on its own, held keys included."""
+    T, kv, d = 4096, 2, 128
+    g = torch.Generator(device="cuda").manual_seed(11)
+    k = torch.randn((T, kv, d), generator=g, device="cuda")
+    tab = R.reskv_rope_table(R.reskv_rope_config_default(), T)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    c, s = tab[:, None, :, 0], tab[:, None, :, 1]
+    a, b = (k[..., 0::2], k[..., 1::2]) if interleaved else (k[..., :64], k[..., 64:])
+    x, y = a * c - b * s, b * c + a * s                                  # one operation a kernel: nothing fused
+    want = torch.stack([x, y], -1).flatten(-2) if interleaved else torch.cat([x, y], -1)
+    got = torch.empty_like(k)
+    R.reskv_rope(k, got, pos, tab, interleaved=interleaved)
+    assert torch.equal(got, want)
+    pages = [R.reskv_paged_pages(64, kv) for _ in range(2)]
+    table = torch.arange(64, dtype=torch.int32, device="cuda")[None]
+    seqs = torch.zeros(T, dtype=torch.int32, device="cuda")
+    R.reskv_paged_append(R.PagedKV(pages[0], table, 64, kv), k, k, seqs, pos, table=tab, interleaved=interleaved)
+    R.reskv_paged_append(R.PagedKV(pages[1], table, 64, kv), want, k, seqs, pos)
+    assert torch.equal(pages[0], pages[1])
