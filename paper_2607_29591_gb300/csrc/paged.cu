@@ -315,18 +315,6 @@ struct GatherParams {
   int32_t table_pages, page_tokens, kv_heads, batch;
 };
 
-// Scale and minimum of one group from a row's words.
-template <int NG>
-__device__ __forceinline__ void group_meta(const uint32_t (&w)[NG], int k, float& s, float& m) {
-  if constexpr (NG == 1) {
-    s = low_bf16(w[0]);
-    m = high_bf16(w[0]);
-  } else {
-    s = k & 1 ? high_bf16(w[k / 2]) : low_bf16(w[k / 2]);
-    m = k & 1 ? high_bf16(w[NG / 2 + k / 2]) : low_bf16(w[NG / 2 + k / 2]);
-  }
-}
-
 template <typename T, int N, bool kWide>
 __device__ __forceinline__ void store_values(T* y, const float (&x)[N]) {
   Pack<T, N> o;

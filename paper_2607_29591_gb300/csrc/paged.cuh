@@ -73,6 +73,18 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const void* p) {
   }
 }
 
+// Scale and minimum of one group from a row's words.
+template <int NG>
+__device__ __forceinline__ void group_meta(const uint32_t (&w)[NG], int k, float& s, float& m) {
+  if constexpr (NG == 1) {
+    s = low_bf16(w[0]);
+    m = high_bf16(w[0]);
+  } else {
+    s = k & 1 ? high_bf16(w[k / 2]) : low_bf16(w[k / 2]);
+    m = k & 1 ? high_bf16(w[NG / 2 + k / 2]) : low_bf16(w[NG / 2 + k / 2]);
+  }
+}
+
 // (a, b) turned by (cos, sin): products and sums rounded one by one, so that a
 // key is held with the same codes whatever path rotated it.  (Packed mul.rn and
 // add.rn pairs came out fused.)

@@ -147,37 +147,6 @@ struct RowCursor {
   }
 };
 
-// Output row r of a sequence, dims 4u .. 4u + 3.
-__device__ __forceinline__ void store_out(const AttnParams& p, const Sequence& s, int h, int r, int u, float4 v) {
-  const int64_t tok = s.q0 + r / p.group;
-  const int64_t at = tok * p.o_token + int64_t(h * p.group + r % p.group) * p.o_head + 4 * u;
-  const float f[4] = {v.x, v.y, v.z, v.w};
-  if (p.o_f32) {
-    float* y = static_cast<float*>(p.o) + at;
-    if (p.o_wide) {
-      *reinterpret_cast<float4*>(y) = v;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = f[i];
-    }
-    return;
-  }
-  uint16_t* y = static_cast<uint16_t*>(p.o) + at;
-  uint16_t e[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    e[i] = p.q_f16 ? __half_as_ushort(__float2half_rn(f[i])) : __bfloat16_as_ushort(__float2bfloat16_rn(f[i]));
-  if (p.o_wide) {
-    *reinterpret_cast<uint2*>(y) = make_uint2(e[0] | uint32_t(e[1]) << 16, e[2] | uint32_t(e[3]) << 16);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = e[i];
-  }
-}
-
-__device__ __forceinline__ void store_lse(const AttnParams& p, const Sequence& s, int h, int r, float ref) {
-  if (p.lse) p.lse[(s.q0 + r / p.group) * int64_t(p.heads) + h * p.group + r % p.group] = ref * 0.693147180559945f;
-}
 
 __device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
@@ -199,28 +168,6 @@ __device__ __forceinline__ void copy_tile(void* dst, const void* src, uint32_t b
       "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::
           "r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy)
       : "memory");
-}
-
-// The softmaxes of up to 32 records joined: each lane's weight for its record's
-// output, from their log2 sums (-inf: an empty or no record), and the joint sum.
-struct Joined {
-  float weight, ref;
-};
-__device__ __forceinline__ Joined join_weights(float ref) {
-  float top = ref;
-#pragma unroll
-  for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  const float f = ref == -INFINITY ? 0.f : exp2f(ref - top);
-  float sum = f;
-#pragma unroll
-  for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  return sum != 0.f ? Joined{f / sum, top + log2f(sum)} : Joined{0.f, -INFINITY};
-}
-__device__ __forceinline__ void add_scaled(float4& a, float f, float4 v) {
-  a.x = fmaf(f, v.x, a.x);
-  a.y = fmaf(f, v.y, a.y);
-  a.z = fmaf(f, v.z, a.z);
-  a.w = fmaf(f, v.w, a.w);
 }
 
 template <int D, int NG, bool kTwoPlanes, int R>
@@ -651,6 +598,19 @@ cudaError_t dispatch_rows(const AttnParams& p, int d, int group, int dev, int ct
   return launch_rows<64, 1, kTwoPlanes, R>(p, dev, ctas, s);
 }
 
+// Whole blocks of rows (paged_attn_blocks.cu) from kBlockRows rows a sequence on,
+// for bf16 outputs; sequences of different query counts keep to the other kernel,
+// whose cut is made on the device.
+constexpr int kBlockRows = 32;
+bool takes_blocks(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
+  if (a->q_begin || a->o.dtype != RESKV_BF16 || a->scale < 0.f || kv->batch < 1 || kv->n_kv_heads < 1) return false;
+  return a->n_tokens / kv->batch * (a->q.n_heads / kv->n_kv_heads) >= kBlockRows;
+}
+BlockPlan block_plan(const reskv_paged_kv* kv, const reskv_paged_attn_args* a, int sms) {
+  return plan_attn_blocks(a->n_tokens / kv->batch * (a->q.n_heads / kv->n_kv_heads), kv->batch, kv->n_kv_heads,
+                          int64_t(kv->table_pages) * kv->page_tokens, sms);
+}
+
 std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
   std::string bad = check_paged(kv);
   if (!bad.empty()) return bad;
@@ -685,7 +645,14 @@ using namespace reskv;
 
 extern "C" size_t reskv_paged_attn_workspace(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
   if (!kv || !a || (kv->head_dim != 64 && kv->head_dim != 128)) return 0;
-  return kTicketBytes + size_t(kMaxCtas) * 2 * (record_floats(kv->head_dim, 8) + 8) * 4;
+  size_t bytes = size_t(kMaxCtas) * 2 * (record_floats(kv->head_dim, 8) + 8) * 4;
+  int dev = 0, sms = 0;
+  if (takes_blocks(kv, a) && cudaGetDevice(&dev) == cudaSuccess && (sms = sm_count(dev)) > 0) {
+    const size_t more = attn_blocks_bytes(block_plan(kv, a, sms), kv->head_dim);
+    if (more > bytes) bytes = more;
+  }
+  cudaGetLastError();
+  return kTicketBytes + bytes;
 }
 
 extern "C" reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a, void* stream) {
@@ -726,8 +693,12 @@ extern "C" reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_p
   if (err != cudaSuccess) return launch_result(err, "reading the device");
   int ctas = sm_count(dev);
   if (ctas < 1) return launch_result(cudaErrorInvalidDevice, "reading the SM count");
-  if (ctas > kMaxCtas) ctas = kMaxCtas;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (takes_blocks(kv, a)) {
+    const BlockPlan plan = block_plan(kv, a, ctas);
+    return launch_result(launch_attn_blocks(p, plan, kv->head_dim, kv->quant_group, dev, p.partials, s), "paged attention");
+  }
+  if (ctas > kMaxCtas) ctas = kMaxCtas;
   // bf16 outputs: weights in one fp16 plane (2^-11) are finer than the output's 2^-8.
   // Four rows a unit where a sequence has no more on average.
   const bool one = a->o.dtype == RESKV_BF16, few = a->n_tokens * p.group <= 4 * int64_t(kv->batch);

@@ -109,6 +109,61 @@ __device__ __forceinline__ float exp2_fast(float x) {          // 2^-inf = 0
   return y;
 }
 
+// --- outputs -----------------------------------------------------------------
+
+// Output row r of a sequence, dims 4u .. 4u + 3.
+__device__ __forceinline__ void store_out(const AttnParams& p, const Sequence& s, int h, int r, int u, float4 v) {
+  const int64_t tok = s.q0 + r / p.group;
+  const int64_t at = tok * p.o_token + int64_t(h * p.group + r % p.group) * p.o_head + 4 * u;
+  const float f[4] = {v.x, v.y, v.z, v.w};
+  if (p.o_f32) {
+    float* y = static_cast<float*>(p.o) + at;
+    if (p.o_wide) {
+      *reinterpret_cast<float4*>(y) = v;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = f[i];
+    }
+    return;
+  }
+  uint16_t* y = static_cast<uint16_t*>(p.o) + at;
+  uint16_t e[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    e[i] = p.q_f16 ? __half_as_ushort(__float2half_rn(f[i])) : __bfloat16_as_ushort(__float2bfloat16_rn(f[i]));
+  if (p.o_wide) {
+    *reinterpret_cast<uint2*>(y) = make_uint2(e[0] | uint32_t(e[1]) << 16, e[2] | uint32_t(e[3]) << 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = e[i];
+  }
+}
+
+__device__ __forceinline__ void store_lse(const AttnParams& p, const Sequence& s, int h, int r, float ref) {
+  if (p.lse) p.lse[(s.q0 + r / p.group) * int64_t(p.heads) + h * p.group + r % p.group] = ref * 0.693147180559945f;
+}
+// The softmaxes of up to 32 records joined: each lane's weight for its record's
+// output, from their log2 sums (-inf: an empty or no record), and the joint sum.
+struct Joined {
+  float weight, ref;
+};
+__device__ __forceinline__ Joined join_weights(float ref) {
+  float top = ref;
+#pragma unroll
+  for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const float f = ref == -INFINITY ? 0.f : exp2f(ref - top);
+  float sum = f;
+#pragma unroll
+  for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return sum != 0.f ? Joined{f / sum, top + log2f(sum)} : Joined{0.f, -INFINITY};
+}
+__device__ __forceinline__ void add_scaled(float4& a, float f, float4 v) {
+  a.x = fmaf(f, v.x, a.x);
+  a.y = fmaf(f, v.y, a.y);
+  a.z = fmaf(f, v.z, a.z);
+  a.w = fmaf(f, v.w, a.w);
+}
+
 // --- the tile step -----------------------------------------------------------
 
 // R (8 or 4) query rows of one warp against tiles of 16 tokens.  In units of log2,
@@ -484,5 +539,16 @@ struct TileStep {
     return (v * f + om[c / PG][j]) * l[j];
   }
 };
+
+// --- many rows: paged_attn_blocks.cu ---
+// Blocks of 128 mt rows; each block's positions in `parts`.
+struct BlockPlan {
+  int mt, row_blocks, parts;
+  int64_t items;                  // CTAs
+};
+BlockPlan plan_attn_blocks(int64_t rows, int batch, int kv_heads, int64_t capacity, int sms);
+size_t attn_blocks_bytes(const BlockPlan& plan, int d);              // of records, where parts are joined
+cudaError_t launch_attn_blocks(const AttnParams& p, const BlockPlan& plan, int d, int quant_group, int dev, float* records,
+                               cudaStream_t s);
 
 }  // namespace reskv

@@ -1,0 +1,729 @@
+// Attention of many query rows (a chunk of a prompt) over the paged 4-bit cache,
+// on the fifth-generation tensor cores.
+//
+// A CTA takes one block of 128 or 256 query rows of one KV head and walks its
+// positions 64 at a time.  With few rows (paged_attn.cu) a code is unpacked for
+// every eight of them; here each tile is unpacked once for the block, into fp16
+// operands in shared memory:
+//
+//   S = Q K^T       [128 rows x 64 positions]   tcgen05.mma, per 128 rows, into TMEM
+//   P = 2^(S - ref) one row a thread, fp16 into shared memory
+//   O += P V        [128 rows x d]              tcgen05.mma, accumulated in TMEM
+//
+// Eight warps unpack and take the softmax, a ninth issues copies and products.
+// While the tensor cores form S of the next tile the warps take the softmax of
+// this one; while they add P V the warps unpack the tile after the next.
+//
+// Roundings.  Keys and values are divided by a power of two that only grows along
+// the block (the largest exponent met so far), queries by one per row, so that any
+// magnitude fits fp16.  Logits are formed from exact products: s (n - 8) has 11
+// bits, and m + 8 s, in two fp16 planes, meets the query's sums over the groups, in
+// two planes too, in one more step of the same product.  Values s n + m and weights
+// are rounded to fp16's 11 bits, finer than the bf16 the output is rounded to; other
+// output types take the kernel of few rows.  Sums, statistics and accumulators are
+// fp32.
+//
+// Bound by the warps' instructions (unpacking about 250 a tile and warp, the softmax
+// about 220) and the barriers between the phases.
+#include <atomic>
+
+#include "paged_attn.cuh"
+
+namespace reskv {
+namespace {
+
+constexpr int kPos = 64;                          // positions of a step
+constexpr int kSub = kPos / kTile;                // cache tiles of a step
+constexpr int kWarps = 8;                         // that compute
+constexpr int kThreads = (kWarps + 1) * 32;
+constexpr int kRaw = 3;                           // steps of packed tiles in flight
+
+// --- tensor core instructions ---
+
+// Descriptor of a K-major operand in shared memory: rows of 128 bytes (64 fp16)
+// with the 128-byte swizzle (16-byte word w of row r at w ^ (r & 7)), groups of
+// eight rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t operand(uint32_t saddr) {
+  return uint64_t((saddr & 0x3FFFFu) >> 4) | (uint64_t(1) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) |
+         (uint64_t(2) << 61);
+}
+// The same for rows of 32 bytes (one step) with the 32-byte swizzle (16-byte word
+// w at w ^ ((r >> 2) & 1)), groups of eight rows 256 bytes apart.
+__device__ __forceinline__ uint64_t operand32(uint32_t saddr) {
+  return uint64_t((saddr & 0x3FFFFu) >> 4) | (uint64_t(1) << 16) | (uint64_t(256 >> 4) << 32) | (uint64_t(1) << 46) |
+         (uint64_t(6) << 61);
+}
+// kind::f16, fp16 operands, fp32 accumulators, 128 rows, n columns
+__device__ __forceinline__ uint32_t shape_of(int n) {
+  return (1u << 4) | (uint32_t(n >> 3) << 17) | (uint32_t(128 >> 4) << 24);
+}
+__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(shape),
+      "r"(add ? 1 : 0));
+}
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// 16 columns of this thread's row; defined after landed()
+__device__ __forceinline__ void load16(uint32_t at, float* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
+        "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+      : "r"(at));
+}
+__device__ __forceinline__ void landed() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void defined16(float* r) {
+  asm volatile("" : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]), "+f"(r[8]),
+               "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]));
+}
+__device__ __forceinline__ void store16(uint32_t at, const float* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::
+          "r"(at), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]),
+      "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// 2^(14 - (e - 127)) and its inverse, of a biased exponent 15 <= e <= 254
+__device__ __forceinline__ float down(int e) { return __int_as_float((268 - e) << 23); }
+__device__ __forceinline__ float up(int e) { return __int_as_float((e - 14) << 23); }
+
+// --- shared memory ---
+
+template <int D, int NG, int MT>
+struct BlockSmem {
+  static constexpr int half = 128 * 128;          // 128 rows of 64 fp16
+  static constexpr int q = MT * (D / 64) * half;
+  static constexpr int kbuf = kPos * D * 2, vbuf = kPos * D * 2;
+  static constexpr int p = MT * half;
+  static constexpr int raw1 = kSub * TileShape{D, NG}.bytes();
+  static constexpr int q_more = 128 * 32, k_more = kPos * 32;         // the step of minima
+  static constexpr int at_k = q, at_v = at_k + 2 * kbuf, at_p = at_v + 3 * vbuf, at_qm = at_p + p, at_km = at_qm + MT * q_more,
+                       at_raw = at_km + 2 * k_more;
+  static constexpr int bytes = at_raw + kRaw * raw1 + 1024;           // operands on 1024 bytes
+};
+
+struct BlockShared {
+  uint64_t raw[kRaw], s[2], pv;
+  uint32_t tmem;
+  uint32_t valid[8];                              // which of a step's cache tiles exist (six steps are between copy and softmax)
+  int top[4][2];                                  // largest biased exponent of a step's K and V
+  uint32_t odd[4];                                // a step holds V groups that are NaN
+  uint8_t odd_groups[4][kPos];                    // which, per position
+};
+
+struct BlockParams {
+  AttnParams a;
+  int32_t row_blocks, parts;
+  float* records;                                 // parts > 1: [item][rows][D], then [item][rows] log2 sums
+};
+
+template <int D, int NG, int MT>
+__global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_constant__ BlockParams bp) {
+  using S = BlockSmem<D, NG, MT>;
+  constexpr int kRows = 128 * MT, C = D / 32, PG = C / NG, TB = TileShape{D, NG}.bytes();
+  constexpr TileShape ts{D, NG};
+  constexpr uint32_t kColumns = MT == 2 ? 512 : 256;
+  const AttnParams& p = bp.a;
+  extern __shared__ uint8_t dynamic[];
+  uint8_t* smem = dynamic + ((1024u - (smem_u32(dynamic) & 1023u)) & 1023u);
+  __shared__ __align__(16) BlockShared sh;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  if (tid == 0) {
+    for (int i = 0; i < kRaw; ++i) mbar_init(&sh.raw[i], 1);
+    mbar_init(&sh.s[0], 1);
+    mbar_init(&sh.s[1], 1);
+    mbar_init(&sh.pv, 1);
+    fence_mbar_init();
+  }
+  if (tid < 8) sh.top[tid >> 1][tid & 1] = 0;
+  if (tid < 4) sh.odd[tid] = 0;
+  wait_for_previous();
+
+  // the item: part of the positions of one block of rows
+  int item = blockIdx.x;
+  const int part = item % bp.parts;
+  const int unit = item / bp.parts;
+  const int blk = unit % bp.row_blocks, bh = unit / bp.row_blocks;
+  const int b = bh / p.kv_heads, h = bh - b * p.kv_heads;
+  const Sequence sq = sequence_of(p, b);
+  const int rows = sq.count * p.group, r0 = blk * kRows;
+  const RowBlock rb = row_block(p, sq, r0, min(r0 + kRows, rows));
+  const int steps_all = (rb.tiles + kSub - 1) / kSub;
+  const int step0 = int(int64_t(steps_all) * part / bp.parts);
+  const int n = int(int64_t(steps_all) * (part + 1) / bp.parts) - step0;
+  const int first = rb.first + step0 * kSub;      // first cache tile
+  const int tiles = min(rb.tiles - step0 * kSub, n * kSub);
+  // what the block's rows see
+  const int base = sq.len - sq.count;
+  const int hi_first = base + r0 / p.group, hi_last = base + (min(r0 + kRows, rows) - 1) / p.group;
+  const int from = p.window > 0 ? max(0, hi_first - p.window + 1) : 0;
+  const int lo_last = p.window > 0 ? max(0, hi_last - p.window + 1) : 0;
+
+  // this thread's row (of the first 256 threads; rows that do not exist see what the last one does)
+  const int mt = warp >> 2;
+  const bool has_row = warp < 4 * MT;
+  const int rt = (warp & 3) * 32 + lane;          // row within its 128
+  const int r = r0 + mt * 128 + rt;
+  const bool real = has_row && r < rows;
+  const int hi = base + min(r, rows - 1) / p.group;
+  const int lo = p.window > 0 ? max(0, hi - p.window + 1) : 0;
+  float ref = kNoRef, l = 0.f;
+  uint32_t nan_groups = 0;
+  float* const record = bp.records + int64_t(item) * kRows * D;
+  float* const record_ref = bp.records + int64_t(gridDim.x) * kRows * D + int64_t(item) * kRows;
+
+  auto finish_row = [&](int c, const float (&v)[32]) {       // dims 32c .. 32c + 31 of this thread's row
+    if (!real) return;
+    if (bp.parts > 1) {
+      float* y = record + int64_t(mt * 128 + rt) * D + 32 * c;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) reinterpret_cast<float4*>(y)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) store_out(p, sq, h, r, 8 * c + i, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+    }
+  };
+  if (n == 0) {                                   // nothing to see: the same for the whole CTA
+    const float zero[32] = {};
+#pragma unroll 1
+    for (int c = 0; c < C; ++c) finish_row(c, zero);
+    if (real) {
+      if (bp.parts > 1) record_ref[mt * 128 + rt] = -INFINITY;
+      else store_lse(p, sq, h, r, -INFINITY);
+    }
+    return;
+  }
+
+  if (warp == kWarps) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(kColumns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = sh.tmem;
+  const uint32_t smem_q = smem_u32(smem), smem_k = smem_q + S::at_k, smem_v = smem_q + S::at_v, smem_p = smem_q + S::at_p;
+  auto s_cols = [&](int buf, int m) { return tmem + uint32_t((buf * MT + m) * kPos); };
+  auto o_cols = [&](int m) { return tmem + uint32_t(2 * MT * kPos + m * 128); };
+
+  // --- the ninth warp: copies and products ---
+  const int tpp = p.page_tokens / kTile;
+  int copied = 0, s_issued = 0;
+  auto copy_step = [&](int i) {                   // lanes 0..3: one cache tile each
+    copied = i + 1;
+    const int stage = i % kRaw, t = i * kSub + lane;
+    int page = -1, at = 0;
+    const bool asked = lane < kSub && t < tiles;
+    if (asked) {
+      const int tile = first + t, pg = tile / tpp;
+      at = tile - pg * tpp;
+      page = p.page_table[int64_t(b) * p.table_pages + pg];
+    }
+    const bool ok = asked && page >= 0 && page < p.n_pages;
+    if (asked && !ok) report_status(p.status, kStatusBadIndex);
+    const uint32_t mask = __ballot_sync(0xffffffffu, ok);
+    if (lane == 0) {
+      sh.valid[i & 7] = mask;
+      if (mask) mbar_arrive_expect_tx(&sh.raw[stage], __popc(mask) * TB);
+      else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(&sh.raw[stage])) : "memory");
+    }
+    __syncwarp();
+    if (ok)
+      bulk_g2s(smem + S::at_raw + stage * S::raw1 + lane * TB,
+               p.pages + ((int64_t(page) * p.kv_heads + h) * tpp + at) * int64_t(TB), TB, &sh.raw[stage]);
+  };
+  auto issue_s = [&](int i) {                     // S of step i, one thread
+    s_issued = i + 1;
+    fence_after();
+#pragma unroll 1
+    for (int m = 0; m < MT; ++m) {
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
+        multiply(s_cols(i & 1, m), operand(smem_q + (m * (D / 64) + k / 4) * S::half + (k & 3) * 32),
+                 operand(smem_k + (i & 1) * S::kbuf + (k / 4) * (kPos * 128) + (k & 3) * 32), shape_of(kPos), k > 0);
+      multiply(s_cols(i & 1, m), operand32(smem_q + S::at_qm + m * S::q_more), operand32(smem_q + S::at_km + (i & 1) * S::k_more),
+               shape_of(kPos), true);
+    }
+    commit(&sh.s[i & 1]);
+  };
+  auto issue_o = [&](int i) {
+    fence_after();
+#pragma unroll 1
+    for (int m = 0; m < MT; ++m) {
+#pragma unroll
+      for (int k = 0; k < kPos / 16; ++k)
+        multiply(o_cols(m), operand(smem_p + m * S::half + k * 32), operand(smem_v + (i % 3) * S::vbuf + k * 32), shape_of(D),
+                 i > 0 || k > 0);
+    }
+    commit(&sh.pv);
+  };
+
+  // --- the computing warps' parts ---
+  bool failed = false;
+  auto in_block = [&](int pos) { return pos >= from && pos <= hi_last; };
+  // Step i's largest exponents, once its tiles have landed.
+  auto look = [&](int i) {
+    const int stage = i % kRaw, slot = i & 3;
+    if (!mbar_wait_bounded(&sh.raw[stage], (i / kRaw) & 1)) failed = true;
+    if (tid >= 2 * kPos) return;
+    const int tk = tid & (kPos - 1), which = tid / kPos;
+    const bool held = ((sh.valid[i & 7] >> (tk / kTile)) & 1) && in_block((first + i * kSub) * kTile + tk);
+    float top = 0.f;
+    uint32_t odd = 0;
+    if (held) {
+      const uint8_t* tile = smem + S::at_raw + stage * S::raw1 + (tk / kTile) * TB;
+      const uint16_t* meta = reinterpret_cast<const uint16_t*>(tile + (which ? ts.v_meta() : ts.k_meta())) + (tk % kTile) * 2 * NG;
+#pragma unroll
+      for (int k = 0; k < NG; ++k) {
+        const float s = __uint_as_float(uint32_t(meta[k]) << 16), m = __uint_as_float(uint32_t(meta[NG + k]) << 16);
+        const float big = fmaxf(fabsf(m), fabsf(fmaf(15.f, s, m)));
+        if (s != s || m != m) odd |= 1u << k;
+        else top = fmaxf(top, fminf(big, 3.0e38f));
+      }
+    }
+    if (which) {
+      sh.odd_groups[slot][tk] = uint8_t(odd);
+      if (odd) atomicOr(&sh.odd[slot], 1u);
+    }
+    const int e = __reduce_max_sync(0xffffffffu, __float_as_int(top) >> 23);
+    if (lane == 0) atomicMax(&sh.top[slot][which], e);
+  };
+  // Exponents that steps are held at: they only grow.
+  int ek = 15, ev = 15;
+  // Step i unpacked with them: warp w takes K (even) or V (odd) of cache tile w / 2.
+  auto unpack = [&](int i) {
+    const int stage = i % kRaw, sub = warp >> 1;
+    const int g = lane >> 2, t = lane & 3;
+    const uint8_t* tile = smem + S::at_raw + stage * S::raw1 + sub * TB;
+    const int pos = (first + i * kSub + sub) * kTile;
+    const bool exists = (sh.valid[i & 7] >> sub) & 1;
+    // codes n, less `less`, of the even and the odd places as fp16 numbers
+    auto whole = [](uint32_t v, float less) {
+      const uint32_t w = (v & 0x000f000fu) | 0x64006400u;              // 1024 + n
+      return __hsub2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(1024.f + less));
+    };
+    auto odd_place = [](uint32_t v, float less) {
+      const uint32_t w = (v & 0x00f000f0u) | 0x64006400u;              // 1024 + 16 n
+      return __hfma2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(0.0625f), __float2half2_rn(-64.f - less));
+    };
+    auto bits = [](__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); };
+    if ((warp & 1) == 0) {
+      const float f = down(ek);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int row = g + 8 * j, tk = sub * kTile + row;
+        const bool held = exists && in_block(pos + row);
+        uint32_t w[C] = {}, meta[NG] = {};
+        if (held) {
+          load_words<C>(w, tile + row * (D / 2) + t * (D / 8));
+          load_words<NG>(meta, tile + ts.k_meta() + row * 4 * NG);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          float s, m;
+          group_meta<NG>(meta, c / PG, s, m);
+          const __half2 s2 = __float2half2_rn(s * f);
+          // dims 0, 4, 1, 5, 2, 6, 3, 7 of the word's eight
+          const uint4 v = make_uint4(bits(__hmul2(whole(w[c], 8.f), s2)), bits(__hmul2(odd_place(w[c], 8.f), s2)),
+                                     bits(__hmul2(whole(w[c] >> 8, 8.f), s2)), bits(__hmul2(odd_place(w[c] >> 8, 8.f), s2)));
+          const int word = 4 * c + t;
+          *reinterpret_cast<uint4*>(smem + S::at_k + (i & 1) * S::kbuf + (word >> 3) * (kPos * 128) + tk * 128 +
+                                    (((word & 7) ^ (tk & 7)) << 4)) = v;
+        }
+        // the groups' m + 8 s: first planes (t = 0), second planes (1), first again (2), nothing (3)
+        float plane[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NG; ++k) {
+          float s, m;
+          group_meta<NG>(meta, k, s, m);
+          const float x = fmaf(8.f, s, m) * f, first_plane = __half2float(__float2half_rn(x));
+          plane[k] = t == 3 ? 0.f : t == 1 ? x - first_plane : first_plane;
+        }
+        *reinterpret_cast<uint2*>(smem + S::at_km + (i & 1) * S::k_more + tk * 32 + (((t >> 1) ^ ((tk >> 2) & 1)) << 4) + (t & 1) * 8) =
+            make_uint2(pack_f16(plane[0], plane[1]), pack_f16(plane[2], plane[3]));
+      }
+    } else {
+      const float f = down(ev);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int pair = t + 4 * j, tk = sub * kTile + 2 * pair;
+        const bool held0 = exists && in_block(pos + 2 * pair), held1 = exists && in_block(pos + 2 * pair + 1);
+        uint32_t w[C] = {}, meta0[NG] = {}, meta1[NG] = {};
+        if (held0 || held1) load_words<C>(w, tile + ts.v_codes() + pair * D + ts.v_place(pair, g) * (D / 8));
+        if (held0) load_words<NG>(meta0, tile + ts.v_meta() + 2 * pair * 4 * NG);
+        if (held1) load_words<NG>(meta1, tile + ts.v_meta() + (2 * pair + 1) * 4 * NG);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          float sa, ma, sb, mb;
+          group_meta<NG>(meta0, c / PG, sa, ma);
+          group_meta<NG>(meta1, c / PG, sb, mb);
+          if (sa != sa || ma != ma) sa = ma = 0.f;                       // NaN is put into the rows that see it at the end
+          if (sb != sb || mb != mb) sb = mb = 0.f;
+          const __half2 s2 = __floats2half2_rn(sa * f, sb * f), m2 = __floats2half2_rn(ma * f, mb * f);
+          const __half2 v[4] = {__hfma2(whole(w[c], 0.f), s2, m2), __hfma2(odd_place(w[c], 0.f), s2, m2),
+                                __hfma2(whole(w[c] >> 8, 0.f), s2, m2), __hfma2(odd_place(w[c] >> 8, 0.f), s2, m2)};
+          // dim 32c + 4g + e in row 32c + 8e + g: lanes of one store in eight rows, as many 16-byte words
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int row = 32 * c + 8 * e + g;
+            *reinterpret_cast<uint32_t*>(smem + S::at_v + (i % 3) * S::vbuf + row * 128 + (((tk >> 3) ^ (row & 7)) << 4) +
+                                         (tk & 7) * 2) = bits(v[e]);
+          }
+        }
+      }
+    }
+  };
+  auto grow = [&](int i, int& e, int which) { e = min(max(e, sh.top[i & 3][which]), 254); };
+
+  if (warp == kWarps) {
+    copy_step(0);
+    if (n > 1) copy_step(1);
+    if (n > 2) copy_step(2);
+  } else if (has_row) {
+    // the row's query, scaled below 2^8 (128 of them sum up within fp16), in the order of the keys' dims
+    const void* src = nullptr;
+    if (real)
+      src = static_cast<const uint16_t*>(p.q) + (sq.q0 + r / p.group) * p.q_token + int64_t(h * p.group + r % p.group) * p.q_head;
+    auto value = [&](int d) {
+      return p.q_f16 ? to_f32(static_cast<const __half*>(src)[d]) : to_f32(static_cast<const __nv_bfloat16*>(src)[d]);
+    };
+    float top = 0.f;
+    if (real) {
+#pragma unroll 8
+      for (int d = 0; d < D; ++d) top = fmaxf(top, fabsf(value(d)));
+    }
+    const int e = 134 - min(max(__float_as_int(top) >> 23, 1), 254), e1 = e >> 1, e2 = e - e1;
+    const float f1 = __int_as_float((127 + e1) << 23), f2 = __int_as_float((127 + e2) << 23);
+    float sums[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+#pragma unroll 1
+    for (int w = 0; w < D / 8; ++w) {
+      uint32_t x[4] = {0u, 0u, 0u, 0u};
+      if (real) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[j] = pack_f16(value(8 * w + j) * f1 * f2, value(8 * w + 4 + j) * f1 * f2);
+          const float2 held = __half22float2(*reinterpret_cast<const __half2*>(&x[j]));
+          sum += held.x + held.y;
+        }
+      }
+      if ((w + 1) % (D / 8 / NG) == 0) {          // the end of a group
+#pragma unroll
+        for (int k = 0; k < NG; ++k)
+          if ((w + 1) / (D / 8 / NG) == k + 1) sums[k] = sum;
+        sum = 0.f;
+      }
+      *reinterpret_cast<uint4*>(smem + (mt * (D / 64) + (w >> 3)) * S::half + rt * 128 + (((w & 7) ^ (rt & 7)) << 4)) =
+          make_uint4(x[0], x[1], x[2], x[3]);
+    }
+    // against the keys' planes: first planes twice, then what they left over
+    float left[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      left[k] = sums[k];
+      sums[k] = __half2float(__float2half_rn(sums[k]));
+      left[k] -= sums[k];
+    }
+    const uint2 top_planes = make_uint2(pack_f16(sums[0], sums[1]), pack_f16(sums[2], sums[3]));
+    const uint2 low_planes = make_uint2(pack_f16(left[0], left[1]), pack_f16(left[2], left[3]));
+    uint8_t* more = smem + S::at_qm + mt * S::q_more + rt * 32;
+    const int turn_word = ((rt >> 2) & 1) << 4;
+    *reinterpret_cast<uint4*>(more + turn_word) = make_uint4(top_planes.x, top_planes.y, top_planes.x, top_planes.y);
+    *reinterpret_cast<uint4*>(more + (16 ^ turn_word)) = make_uint4(low_planes.x, low_planes.y, 0u, 0u);
+    l = p.scale2 * __int_as_float((127 - e1) << 23) * __int_as_float((127 - e2) << 23);      // until the first step
+  }
+  const float cq = l;
+  l = 0.f;
+  if (warp < kWarps) {
+    look(0);
+    if (n > 1) look(1);
+    if (n > 2) look(2);
+  }
+  __syncthreads();
+  // exponents of the step at hand and of the two after it
+  int ek0 = 15, ev0 = 15, ek1 = 15, ev1 = 15;
+  if (warp < kWarps) {
+    grow(0, ek, 0);
+    grow(0, ev, 1);
+    ek0 = ek;
+    ev0 = ev;
+    unpack(0);
+    if (n > 1) {
+      grow(1, ek, 0);
+      grow(1, ev, 1);
+      unpack(1);
+    }
+    ek1 = ek;
+    ev1 = ev;
+    fence_proxy_async_smem();
+  }
+  failed = __syncthreads_or(failed);
+  if (!failed && warp == kWarps) {
+    if (n > 3) copy_step(3);
+    if (n > 4) copy_step(4);
+    if (lane == 0) issue_s(0);
+  }
+
+  int ev_was = ev0, done = 0;                     // done: products P V issued
+  const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
+#pragma unroll 1
+  for (int i = 0; i < n && !failed; ++i) {
+    if (warp == kWarps) {
+      if (i + 1 < n && lane == 0) issue_s(i + 1);
+      __syncwarp();
+    } else if (has_row) {
+      if (!mbar_wait_bounded(&sh.s[i & 1], (i >> 1) & 1)) failed = true;
+      fence_after();
+      float x[kPos];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) load16(s_cols(i & 1, mt) + lanes + 16 * k, x + 16 * k);
+      landed();
+#pragma unroll
+      for (int k = 0; k < 4; ++k) defined16(x + 16 * k);
+      const float f = fmaxf(cq * up(ek0), 1.17549435e-38f);      // positive: -inf stays -inf
+      const int pos = (first + i * kSub) * kTile;
+      const uint32_t valid = sh.valid[i & 7];
+      const bool all = pos >= lo_last && pos + kPos - 1 <= hi_first;
+      // the row sees positions pos + a .. pos + b - 1 of the step
+      const int a = min(max(lo - pos, 0), kPos), z = min(max(hi + 1 - pos, 0), kPos);
+      uint64_t see = ~0ull;
+      if (!all || valid != (1u << kSub) - 1u) {
+        see = z <= a ? 0ull : ((z == 64 ? ~0ull : (1ull << z) - 1ull) & ~((a == 64 ? 0ull : 1ull << a) - 1ull));
+#pragma unroll
+        for (int k = 0; k < kSub; ++k)
+          if (!((valid >> k) & 1)) see &= ~(0xffffull << (16 * k));
+      }
+      float sum = 0.f;
+      auto weights = [&]() {                      // x: logits -> weights, in place; their sum
+        float2 s2 = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < kPos; k += 2) {
+          const float2 y = ffma2(make_float2(x[k], x[k + 1]), make_float2(f, f), make_float2(-ref, -ref));
+          float2 w = make_float2(exp2_fast(y.x), exp2_fast(y.y));
+          s2 = fadd2(s2, w);
+          x[k] = w.x;
+          x[k + 1] = w.y;
+        }
+        sum = s2.x + s2.y;
+      };
+      const bool masked = __any_sync(0xffffffffu, see != ~0ull);
+      if (masked) {
+#pragma unroll
+        for (int k = 0; k < kPos; ++k)
+          if (!((see >> k) & 1)) x[k] = -INFINITY;
+      }
+      // Logits are needed again only where the reference moves: find that out from
+      // the largest (of three at a time) rather than from the weights.
+      float top = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < kPos; k += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(x[k]), "f"(x[k + 1]));
+      const float best = top * f;
+      float keep = 1.f;
+      bool moves = best - ref > 14.f;
+      if (moves) {
+        const float now = best - 6.f;
+        keep = exp2f(ref - now);
+        ref = now;
+      }
+      weights();
+      l = l * keep + sum;
+      if (sh.odd[i & 3]) {                        // NaN values: which groups this row sees
+#pragma unroll 1
+        for (int k = 0; k < kPos; ++k)
+          if ((see >> k) & 1) nan_groups |= sh.odd_groups[i & 3][k];
+      }
+      // P and O once the products before have been added
+      if (i > 0) {
+        if (!mbar_wait_bounded(&sh.pv, (i - 1) & 1)) failed = true;
+        fence_after();
+        if (ev0 != ev_was) keep *= __int_as_float((127 + max(ev_was - ev0, -126)) << 23);
+        if (__any_sync(0xffffffffu, keep != 1.f)) {
+#pragma unroll 1
+          for (int c = 0; c < D / 16; ++c) {
+            float v[16];
+            load16(o_cols(mt) + lanes + 16 * c, v);
+            landed();
+            defined16(v);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] *= keep;
+            store16(o_cols(mt) + lanes + 16 * c, v);
+          }
+          stored();
+        }
+      }
+      ev_was = ev0;
+#pragma unroll
+      for (int w = 0; w < 8; ++w)
+        *reinterpret_cast<uint4*>(smem + S::at_p + mt * S::half + rt * 128 + ((w ^ (rt & 7)) << 4)) =
+            make_uint4(pack_f16(x[8 * w], x[8 * w + 1]), pack_f16(x[8 * w + 2], x[8 * w + 3]),
+                       pack_f16(x[8 * w + 4], x[8 * w + 5]), pack_f16(x[8 * w + 6], x[8 * w + 7]));
+      fence_proxy_async_smem();
+      fence_before();
+    } else if (i > 0) {                           // a warp without rows also waits before it writes V
+      if (!mbar_wait_bounded(&sh.pv, (i - 1) & 1)) failed = true;
+    }
+    failed = __syncthreads_or(failed);
+    if (failed) break;
+    if (warp == kWarps) {
+      done = i + 1;
+      if (lane == 0) issue_o(i);
+      __syncwarp();
+    } else {
+      if (tid == 0) {
+        sh.top[i & 3][0] = sh.top[i & 3][1] = 0;
+        sh.odd[i & 3] = 0;
+      }
+      ek0 = ek1;
+      ev0 = ev1;
+      if (i + 2 < n) {
+        grow(i + 2, ek, 0);
+        grow(i + 2, ev, 1);
+        unpack(i + 2);
+        fence_proxy_async_smem();
+      }
+      ek1 = ek;
+      ev1 = ev;
+      if (i + 3 < n) look(i + 3);
+    }
+    failed = __syncthreads_or(failed);
+    if (!failed && warp == kWarps && i + 5 < n) copy_step(i + 5);
+  }
+
+  if (failed) {
+    // A wait gave up: let what is in flight land (waits with the same bound), then
+    // free the tensor memory; the output is incomplete.
+    if (tid == 0) report_status(p.status, kStatusWaitTimeout);
+    if (warp == kWarps && lane == 0) {
+      for (int i = copied > kRaw ? copied - kRaw : 0; i < copied; ++i) mbar_wait_bounded(&sh.raw[i % kRaw], (i / kRaw) & 1);
+      for (int i = s_issued > 2 ? s_issued - 2 : 0; i < s_issued; ++i) mbar_wait_bounded(&sh.s[i & 1], (i >> 1) & 1);
+      if (done > 0) mbar_wait_bounded(&sh.pv, (done - 1) & 1);
+    }
+  } else if (has_row) {
+    if (!mbar_wait_bounded(&sh.pv, (n - 1) & 1)) report_status(p.status, kStatusWaitTimeout);
+    fence_after();
+    const bool seen = ref != kNoRef || l != 0.f;
+    const float inv = seen ? up(ev_was) / l : 0.f;
+#pragma unroll 1
+    for (int c = 0; c < C; ++c) {
+      float o[32], v[32];
+      load16(o_cols(mt) + lanes + 32 * c, o);
+      load16(o_cols(mt) + lanes + 32 * c + 16, o + 16);
+      landed();
+      defined16(o);
+      defined16(o + 16);
+      const bool bad = (nan_groups >> (c / PG)) & 1;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) v[4 * (k & 7) + (k >> 3)] = bad ? __int_as_float(0x7fc00000) : o[k] * inv;
+      finish_row(c, v);
+    }
+    const float sum = seen ? ref + log2f(l) : -INFINITY;
+    if (real) {
+      if (bp.parts > 1) record_ref[mt * 128 + rt] = sum;
+      else store_lse(p, sq, h, r, sum);
+    }
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (warp == kWarps) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kColumns));
+}
+
+// The parts of a block's positions joined: one row per warp.
+template <int D, int MT>
+__global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ BlockParams bp, int items) {
+  constexpr int kRows = 128 * MT;
+  const AttnParams& p = bp.a;
+  wait_for_previous();
+  const int64_t w = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  const int unit = int(w / kRows), row = int(w - int64_t(unit) * kRows);
+  const int blk = unit % bp.row_blocks, bh = unit / bp.row_blocks;
+  const int b = bh / p.kv_heads, h = bh - b * p.kv_heads;
+  if (b >= p.batch) return;
+  const Sequence sq = sequence_of(p, b);
+  const int r = blk * kRows + row;
+  if (r >= sq.count * p.group) return;
+  const float* refs = bp.records + int64_t(items) * kRows * D;
+  const float ref = lane < bp.parts ? refs[(int64_t(unit) * bp.parts + lane) * kRows + row] : -INFINITY;
+  const Joined j = join_weights(ref);
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int k = 0; k < bp.parts; ++k) {
+    const float f = __shfl_sync(0xffffffffu, j.weight, k);
+    const float4 v = lane < D / 4 ? reinterpret_cast<const float4*>(bp.records + ((int64_t(unit) * bp.parts + k) * kRows + row) * D)[lane]
+                                  : make_float4(0.f, 0.f, 0.f, 0.f);
+    add_scaled(a, f, f != 0.f ? v : make_float4(0.f, 0.f, 0.f, 0.f));
+  }
+  if (lane < D / 4) store_out(p, sq, h, r, lane, a);
+  if (lane == 0) store_lse(p, sq, h, r, j.ref);
+}
+
+template <int D, int NG, int MT>
+cudaError_t launch(const BlockParams& bp, int dev, int items, cudaStream_t s) {
+  // the kernel's shared memory limit, raised once a device
+  static std::atomic<uint64_t> raised{0};
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+  if (!(raised.load(std::memory_order_relaxed) & bit) || !bit) {
+    const cudaError_t err = cudaFuncSetAttribute(k_attn_blocks<D, NG, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 BlockSmem<D, NG, MT>::bytes);
+    if (err != cudaSuccess) return err;
+    raised.fetch_or(bit, std::memory_order_relaxed);
+  }
+  cudaError_t err = launch_early(k_attn_blocks<D, NG, MT>, items, kThreads, BlockSmem<D, NG, MT>::bytes, s, bp);
+  if (err == cudaSuccess && bp.parts > 1) {
+    const int64_t rows = int64_t(items / bp.parts) * 128 * MT;
+    err = launch_early(k_attn_join<D, MT>, unsigned((rows + 7) / 8), 256, 0, s, bp, items);
+  }
+  return err;
+}
+
+template <int MT>
+cudaError_t dispatch(const BlockParams& bp, int d, int group, int dev, int items, cudaStream_t s) {
+  if (d == 128 && group == 32) return launch<128, 4, MT>(bp, dev, items, s);
+  if (d == 128 && group == 64) return launch<128, 2, MT>(bp, dev, items, s);
+  if (d == 128) return launch<128, 1, MT>(bp, dev, items, s);
+  if (group == 32) return launch<64, 2, MT>(bp, dev, items, s);
+  return launch<64, 1, MT>(bp, dev, items, s);
+}
+
+}  // namespace
+
+BlockPlan plan_attn_blocks(int64_t rows, int batch, int kv_heads, int64_t capacity, int sms) {
+  BlockPlan plan{};
+  plan.mt = rows > 128 ? 2 : 1;
+  const int64_t block = 128 * plan.mt;
+  plan.row_blocks = int((rows + block - 1) / block);
+  const int64_t units = int64_t(batch) * kv_heads * plan.row_blocks;
+  // the positions of fewer blocks than SMs in parts, of 512 positions at least
+  int64_t parts = units < sms ? sms / units : 1;
+  if (parts > capacity / 512) parts = capacity / 512;
+  if (parts > 32) parts = 32;
+  plan.parts = int(parts < 1 ? 1 : parts);
+  plan.items = units * plan.parts;
+  return plan;
+}
+
+size_t attn_blocks_bytes(const BlockPlan& plan, int d) {
+  return plan.parts > 1 ? size_t(plan.items) * 128 * plan.mt * (d + 1) * 4 : 0;
+}
+
+cudaError_t launch_attn_blocks(const AttnParams& p, const BlockPlan& plan, int d, int quant_group, int dev, float* records,
+                               cudaStream_t s) {
+  BlockParams bp{};
+  bp.a = p;
+  bp.row_blocks = plan.row_blocks;
+  bp.parts = plan.parts;
+  bp.records = records;
+  return plan.mt == 2 ? dispatch<2>(bp, d, quant_group, dev, int(plan.items), s)
+                      : dispatch<1>(bp, d, quant_group, dev, int(plan.items), s);
+}
+
+}  // namespace reskv

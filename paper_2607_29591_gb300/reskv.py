@@ -722,7 +722,7 @@ class PagedKV:
             head_dim=self.head_dim, quant_group=self.quant_group,
             status=_ints(self.status, "status", 1))
         self.address = ctypes.addressof(self.struct)
-        self.attn_workspace = load_library().reskv_paged_attn_workspace(self.struct, reskv_paged_attn_args())
+        self.attn_workspace = {}                 # bytes by (query tokens, heads, output type)
 
     def check_status(self) -> None:
         """Read and clear the status word (synchronises); raises if a fault was recorded."""
@@ -818,9 +818,12 @@ def reskv_paged_attn(kv: PagedKV, q, lens, o, q_begin=None, scale: Optional[floa
         raise ValueError(f"lse must hold {T * qh[3]} elements, got {lse.numel()}")
     s = _stream_of(stream, q)
     if workspace is None:
+        need = kv.attn_workspace.get((T, qh[3], oh[4]))
+        if need is None:
+            need = kv.attn_workspace[T, qh[3], oh[4]] = reskv_paged_attn_workspace(kv, T, qh[3], o.dtype)
         held = _workspaces.get((q.device.index, s))
-        if held is None or held[-1].numel() < kv.attn_workspace:
-            held = _workspace(q.device, s, kv.attn_workspace)
+        if held is None or held[-1].numel() < need:
+            held = _workspace(q.device, s, need)
         workspace = held[-1]
     st = lib.reskv_paged_attn(kv.address, _pack_attn(
         *qh, *oh, 0 if lse is None else _dptr(lse, "torch.float32", "lse").value,
@@ -830,8 +833,12 @@ def reskv_paged_attn(kv: PagedKV, q, lens, o, q_begin=None, scale: Optional[floa
         _check(st)
 
 
-def reskv_paged_attn_workspace(kv: PagedKV, n_tokens: int, heads: int) -> int:
-    """Workspace bytes of a reskv_paged_attn call over n_tokens query tokens."""
+def reskv_paged_attn_workspace(kv: PagedKV, n_tokens: int, heads: int, out_dtype=None) -> int:
+    """Workspace bytes of a reskv_paged_attn call over n_tokens query tokens
+    (outputs of out_dtype; None: the most any type needs)."""
+    import torch
+    _calls()
     a = reskv_paged_attn_args(n_tokens=n_tokens)
     a.q.n_heads = heads
+    a.o.dtype = _dtypes[torch.bfloat16 if out_dtype is None else out_dtype]
     return load_library().reskv_paged_attn_workspace(kv.struct, a)

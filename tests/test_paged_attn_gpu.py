@@ -252,3 +252,92 @@ def test_faults_are_reported():
     R.reskv_paged_attn(kvc, q, torch.tensor([64, 64], dtype=torch.int32, device="cuda"), o)
     kvc.check_status()
     check(o, None, attend_all(values, q64, [0, 1, 2], 4, 128 ** -0.5, 0), 128, "bf16")
+
+
+# --- blocks of many query rows (bf16 outputs) ---
+
+@pytest.mark.parametrize("d,group", [(128, 32), (128, 64), (128, 128), (64, 32), (64, 64)])
+@pytest.mark.parametrize("page,lens,new,per", [(16, [75, 64, 8], 8, 4), (64, [300, 129, 40, 0], 40, 4), (32, [257, 256], 65, 4), (48, [100], 100, 7)])
+def test_blocks_of_rows(d, group, page, lens, new, per):
+    case(d + page, lens, new, 2, per, d, group, page, "bf16")
+
+
+@pytest.mark.parametrize("d,group,window", [(128, 32, 0), (64, 64, 0), (128, 128, 700), (128, 32, 90)])
+def test_blocks_of_rows_with_their_positions_in_parts(d, group, window):
+    """One or two blocks and long contexts: every block's positions go to several CTAs, which may see nothing."""
+    case(window + d, [3100, 700], 12, 1, 4, d, group, 64, "bf16", window=window)
+    case(window + d + 1, [2100], 70, 1, 4, d, group, 16, "bf16", window=window)
+
+
+def test_blocks_peaked_and_of_any_size():
+    """The reference moves by hundreds; values' and keys' magnitudes grow from position to position."""
+    case(30, [500], 20, 1, 4, 128, 32, 64, "bf16", spread=30.0)
+    case(31, [300], 20, 1, 4, 128, 32, 64, "bf16", spread=1e-6)
+    rng = np.random.default_rng(32)
+    for kscale, vscale, growth in ((1.0, 1.0, 9.0), (1e-20, 1e-20, 3.0), (1e3, 1e18, -9.0), (1e-3, 1e-2, 0.0)):
+        n, new = 400, 24
+        kvc, _, _, _ = paged(rng, [0], 1, 128, 32, 16, extra_pages=25, table_pages=25)
+        kvc.page_table.copy_(torch.arange(25, dtype=torch.int32)[None])
+        size = np.exp(np.linspace(0, growth, n)).astype(np.float32)[:, None, None]
+        k, v = rows(rng, (n, 1), 128) * np.float32(kscale), rows(rng, (n, 1), 128) * np.float32(vscale) * size
+        R.reskv_paged_append(kvc, torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda(), torch.zeros(n, dtype=torch.int32, device="cuda"),
+                             torch.arange(n, dtype=torch.int32, device="cuda"))
+        ln = torch.tensor([n], dtype=torch.int32, device="cuda")
+        kk, vv = (torch.empty((1, 1, n, 128), device="cuda") for _ in range(2))
+        R.reskv_paged_gather(kvc, ln, kk, vv)
+        q, q64 = as_type(rng.standard_normal((new, 4, 128)) / kscale, "bf16")
+        o, lse = torch.empty((new, 4, 128), dtype=torch.bfloat16, device="cuda"), torch.empty((new, 4), device="cuda")
+        R.reskv_paged_attn(kvc, q, ln, o, lse=lse)
+        ref = po.attend(q64, kk[0].double().cpu().numpy(), vv[0].double().cpu().numpy(), 4, 128 ** -0.5)
+        unit = vscale
+        check(o.double() / unit, lse, [(ref[0] / unit, ref[1], ref[2], ref[3] / unit)], 128, "bf16")
+
+
+def test_blocks_see_nothing_of_other_slots_and_later_tokens():
+    """Garbage in unused slots, and NaN in tokens that only later queries see."""
+    rng = np.random.default_rng(33)
+    n, new, d, page = 150, 30, 128, 32
+    kvc, values, pages, table = paged(rng, [n], 2, d, 32, page)
+    q, q64 = as_type(rng.standard_normal((new, 8, d)), "bf16")
+    ln = torch.tensor([n], dtype=torch.int32, device="cuda")
+    o = torch.empty((new, 8, d), dtype=torch.bfloat16, device="cuda")
+    R.reskv_paged_attn(kvc, q, ln, o)
+    check(o, None, attend_all(values, q64, [0, new], 4, d ** -0.5, 0), d, "bf16")
+    # position 140: values of group 1 are NaN in head 0, keys in head 1
+    p = kvc.pages[int(table[0, 140 // page])].cpu().numpy()
+    held = po.hold(rows(rng, (2,), d), 32)
+    s16, m16 = held[1].copy(), held[2].copy()
+    s16[0, 1] = m16[0, 1] = 0x7FC0
+    s16[1, 2] = m16[1, 2] = 0x7FC0
+    po.put_row(p, 0, 140 % page, d, 32, 1, held[0][0], s16[0], m16[0])
+    po.put_row(p, 1, 140 % page, d, 32, 0, held[0][1], s16[1], m16[1])
+    kvc.pages[int(table[0, 140 // page])] = torch.from_numpy(p).cuda()
+    bad = torch.empty_like(o)
+    R.reskv_paged_attn(kvc, q, ln, bad)
+    first = new - (n - 140)                       # queries from here on see position 140
+    assert torch.equal(bad[:first], o[:first])
+    assert torch.isnan(bad[first:, :4, 32:64]).all() and torch.isfinite(bad[first:, :4, :32]).all() and torch.isfinite(bad[first:, :4, 64:]).all()
+    assert torch.isnan(bad[first:, 4:]).all()
+    kvc.check_status()
+
+
+def test_blocks_report_faults():
+    rng = np.random.default_rng(34)
+    kvc, values, _, table = paged(rng, [200, 90], 1, 128, 32, 16)
+    q, q64 = as_type(rng.standard_normal((40, 4, 128)), "bf16")
+    o = torch.empty_like(q)
+    ln = torch.tensor([200, 90], dtype=torch.int32, device="cuda")
+    R.reskv_paged_attn(kvc, q, ln, o)
+    kvc.check_status()
+    check(o, None, attend_all(values, q64, [0, 20, 40], 4, 128 ** -0.5, 0), 128, "bf16")
+    for page in (-1, len(kvc.pages)):
+        kvc.page_table[0, 3] = page
+        bad = torch.empty_like(q)
+        R.reskv_paged_attn(kvc, q, ln, bad)
+        with pytest.raises(R.ReskvError):
+            kvc.check_status()
+        # the missing page's positions are not seen, by this sequence alone
+        keep = np.r_[0:48, 64:200]
+        skip = [(values[0][0][:, keep], values[0][1][:, keep])]
+        check(bad[:20], None, attend_all(skip, q64[:20], [0, 20], 4, 128 ** -0.5, 0), 128, "bf16")
+        assert torch.equal(bad[20:], o[20:])
