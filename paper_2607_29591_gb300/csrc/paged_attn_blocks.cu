@@ -10,9 +10,20 @@
 //   P = 2^(S - ref) one row a thread, fp16 into shared memory
 //   O += P V        [128 rows x d]              tcgen05.mma, accumulated in TMEM
 //
-// Eight warps unpack and take the softmax, a ninth issues copies and products.
-// While the tensor cores form S of the next tile the warps take the softmax of
-// this one; while they add P V the warps unpack the tile after the next.
+// Four or eight warps take the softmax, a row a thread, eight others unpack up to
+// two steps ahead, and one issues copies and products.  Steps pass between them
+// through mbarriers:
+//
+//   q             the queries' operands are in shared memory (softmax -> products)
+//   raw[i % 3]    step i's packed tiles have landed        (copy -> unpack)
+//   looked        its largest exponents are known           (unpack's warps)
+//   ready[i & 3]  its operands are in shared memory         (unpack -> products, softmax)
+//   s[i & 1]      S is in TMEM, K's buffer is free          (products -> softmax, unpack)
+//   p             P is in shared memory, S's buffer is free  (softmax -> products)
+//   pv[i % 3]     O holds it, P's and V's buffers are free   (products -> softmax, unpack)
+//
+// No barrier completes a phase again before all that wait for the last one have
+// seen it: each next completion needs a step of the one that waits.
 //
 // Roundings.  Keys and values are divided by a power of two that only grows along
 // the block (the largest exponent met so far), queries by one per row, so that any
@@ -23,8 +34,9 @@
 // output types take the kernel of few rows.  Sums, statistics and accumulators are
 // fp32.
 //
-// Bound by the warps' instructions (unpacking about 250 a tile and warp, the softmax
-// about 220) and the barriers between the phases.
+// Bound by the warps' instructions.  With eight warps that did both in turn, between
+// two barriers of the whole block, 512 tokens behind 8K (2 sequences, 8 KV heads, 32
+// query heads, 133 GFLOP) took 357 us.
 #include <atomic>
 
 #include "paged_attn.cuh"
@@ -34,9 +46,12 @@ namespace {
 
 constexpr int kPos = 64;                          // positions of a step
 constexpr int kSub = kPos / kTile;                // cache tiles of a step
-constexpr int kWarps = 8;                         // that compute
-constexpr int kThreads = (kWarps + 1) * 32;
+constexpr int kThreads = 640;                     // warps 0-7 softmax, 8-15 unpack, 16 copies and products
+constexpr int kUnpackWarp = 8, kIssueWarp = 16;
 constexpr int kRaw = 3;                           // steps of packed tiles in flight
+// Registers a thread of each part: (2 x 136 + 2 x 80 + 40) x 128 of the launch's 96 x 640.
+constexpr int kRegsSoftmax = 136, kRegsUnpack = 80, kRegsIssue = 40;
+static_assert((2 * kRegsSoftmax + 2 * kRegsUnpack + kRegsIssue) * 128 <= 96 * kThreads, "registers");
 
 // --- tensor core instructions ---
 
@@ -111,13 +126,39 @@ struct BlockSmem {
 };
 
 struct BlockShared {
-  uint64_t raw[kRaw], s[2], pv;
-  uint32_t tmem;
-  uint32_t valid[8];                              // which of a step's cache tiles exist (six steps are between copy and softmax)
-  int top[4][2];                                  // largest biased exponent of a step's K and V
-  uint32_t odd[4];                                // a step holds V groups that are NaN
-  uint8_t odd_groups[4][kPos];                    // which, per position
+  uint64_t q, raw[kRaw], looked, ready[4], s[2], p, pv[3];
+  uint32_t tmem, abort;
+  // of step i at i & 7
+  uint32_t valid[8];                              // which of its cache tiles exist
+  int top[8][2];                                  // largest biased exponent of its K and V
+  int held[8][2];                                 // the exponents they are held at
+  uint32_t odd[8];                                // it has V groups that are NaN
+  uint8_t odd_groups[8][kPos];                    // which, per position
 };
+
+// Wait for phase `parity`; false once a wait of any warp has given up.
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, BlockShared& sh, uint32_t* status) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  volatile uint32_t* abort = &sh.abort;
+  while (!mbar_try_wait(bar, parity)) {
+    if (*abort) return false;
+    if (clock64() - t0 > kWaitLimitCycles) {
+      *abort = 1u;
+      report_status(status, kStatusWaitTimeout);
+      return false;
+    }
+  }
+  return true;
+}
+// The same for a whole warp.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, BlockShared& sh, uint32_t* status) {
+  return __all_sync(0xffffffffu, wait_for(bar, parity, sh, status));
+}
+__device__ __forceinline__ void warp_arrive(uint64_t* bar, int lane) {
+  __syncwarp();
+  if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 
 struct BlockParams {
   AttnParams a;
@@ -138,20 +179,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (tid == 0) {
+    mbar_init(&sh.q, 4 * MT);
     for (int i = 0; i < kRaw; ++i) mbar_init(&sh.raw[i], 1);
+    mbar_init(&sh.looked, 8);
+    for (int i = 0; i < 4; ++i) mbar_init(&sh.ready[i], 8);
     mbar_init(&sh.s[0], 1);
     mbar_init(&sh.s[1], 1);
-    mbar_init(&sh.pv, 1);
+    mbar_init(&sh.p, 4 * MT);
+    for (int i = 0; i < 3; ++i) mbar_init(&sh.pv[i], 1);
+    sh.abort = 0;
     fence_mbar_init();
   }
-  if (tid < 8) sh.top[tid >> 1][tid & 1] = 0;
-  if (tid < 4) sh.odd[tid] = 0;
+  if (tid < 16) sh.top[tid >> 1][tid & 1] = 0;
+  if (tid < 8) sh.odd[tid] = 0;
   wait_for_previous();
 
   // the item: part of the positions of one block of rows
-  int item = blockIdx.x;
-  const int part = item % bp.parts;
-  const int unit = item / bp.parts;
+  const int item = blockIdx.x;
+  const int part = item % bp.parts, unit = item / bp.parts;
   const int blk = unit % bp.row_blocks, bh = unit / bp.row_blocks;
   const int b = bh / p.kv_heads, h = bh - b * p.kv_heads;
   const Sequence sq = sequence_of(p, b);
@@ -168,19 +213,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
   const int from = p.window > 0 ? max(0, hi_first - p.window + 1) : 0;
   const int lo_last = p.window > 0 ? max(0, hi_last - p.window + 1) : 0;
 
-  // this thread's row (of the first 256 threads; rows that do not exist see what the last one does)
+  // a softmax thread's row (rows that do not exist see what the last one does)
   const int mt = warp >> 2;
-  const bool has_row = warp < 4 * MT;
   const int rt = (warp & 3) * 32 + lane;          // row within its 128
   const int r = r0 + mt * 128 + rt;
-  const bool real = has_row && r < rows;
-  const int hi = base + min(r, rows - 1) / p.group;
-  const int lo = p.window > 0 ? max(0, hi - p.window + 1) : 0;
-  float ref = kNoRef, l = 0.f;
-  uint32_t nan_groups = 0;
+  const bool real = warp < 4 * MT && r < rows;
   float* const record = bp.records + int64_t(item) * kRows * D;
   float* const record_ref = bp.records + int64_t(gridDim.x) * kRows * D + int64_t(item) * kRows;
-
   auto finish_row = [&](int c, const float (&v)[32]) {       // dims 32c .. 32c + 31 of this thread's row
     if (!real) return;
     if (bp.parts > 1) {
@@ -192,18 +231,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
       for (int i = 0; i < 8; ++i) store_out(p, sq, h, r, 8 * c + i, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
     }
   };
+  auto finish_sum = [&](float sum) {
+    if (!real) return;
+    if (bp.parts > 1) record_ref[mt * 128 + rt] = sum;
+    else store_lse(p, sq, h, r, sum);
+  };
   if (n == 0) {                                   // nothing to see: the same for the whole CTA
     const float zero[32] = {};
 #pragma unroll 1
     for (int c = 0; c < C; ++c) finish_row(c, zero);
-    if (real) {
-      if (bp.parts > 1) record_ref[mt * 128 + rt] = -INFINITY;
-      else store_lse(p, sq, h, r, -INFINITY);
-    }
+    finish_sum(-INFINITY);
     return;
   }
 
-  if (warp == kWarps) {
+  if (warp == kIssueWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(kColumns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
@@ -215,425 +256,420 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
   auto s_cols = [&](int buf, int m) { return tmem + uint32_t((buf * MT + m) * kPos); };
   auto o_cols = [&](int m) { return tmem + uint32_t(2 * MT * kPos + m * 128); };
 
-  // --- the ninth warp: copies and products ---
-  const int tpp = p.page_tokens / kTile;
-  int copied = 0, s_issued = 0;
-  auto copy_step = [&](int i) {                   // lanes 0..3: one cache tile each
-    copied = i + 1;
-    const int stage = i % kRaw, t = i * kSub + lane;
-    int page = -1, at = 0;
-    const bool asked = lane < kSub && t < tiles;
-    if (asked) {
-      const int tile = first + t, pg = tile / tpp;
-      at = tile - pg * tpp;
-      page = p.page_table[int64_t(b) * p.table_pages + pg];
-    }
-    const bool ok = asked && page >= 0 && page < p.n_pages;
-    if (asked && !ok) report_status(p.status, kStatusBadIndex);
-    const uint32_t mask = __ballot_sync(0xffffffffu, ok);
-    if (lane == 0) {
-      sh.valid[i & 7] = mask;
-      if (mask) mbar_arrive_expect_tx(&sh.raw[stage], __popc(mask) * TB);
-      else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(&sh.raw[stage])) : "memory");
-    }
-    __syncwarp();
-    if (ok)
-      bulk_g2s(smem + S::at_raw + stage * S::raw1 + lane * TB,
-               p.pages + ((int64_t(page) * p.kv_heads + h) * tpp + at) * int64_t(TB), TB, &sh.raw[stage]);
-  };
-  auto issue_s = [&](int i) {                     // S of step i, one thread
-    s_issued = i + 1;
-    fence_after();
+  if (warp >= kIssueWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+    if (warp == kIssueWarp) {
+      // --- copies and products ---
+      const int tpp = p.page_tokens / kTile;
+      int copied = 0, s_issued = 0, o_issued = 0;
+      auto copy_step = [&](int i) {               // lanes 0..3: one cache tile each
+        copied = i + 1;
+        const int stage = i % kRaw, t = i * kSub + lane;
+        int page = -1, at = 0;
+        const bool asked = lane < kSub && t < tiles;
+        if (asked) {
+          const int tile = first + t, pg = tile / tpp;
+          at = tile - pg * tpp;
+          page = p.page_table[int64_t(b) * p.table_pages + pg];
+        }
+        const bool ok = asked && page >= 0 && page < p.n_pages;
+        if (asked && !ok) report_status(p.status, kStatusBadIndex);
+        const uint32_t mask = __ballot_sync(0xffffffffu, ok);
+        if (lane == 0) {
+          sh.valid[i & 7] = mask;
+          if (mask) mbar_arrive_expect_tx(&sh.raw[stage], __popc(mask) * TB);
+          else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(&sh.raw[stage])) : "memory");
+        }
+        __syncwarp();
+        if (ok)
+          bulk_g2s(smem + S::at_raw + stage * S::raw1 + lane * TB,
+                   p.pages + ((int64_t(page) * p.kv_heads + h) * tpp + at) * int64_t(TB), TB, &sh.raw[stage]);
+      };
+      auto issue_s = [&](int i) {                 // S of step i
+        s_issued = i + 1;
+        fence_after();
+        if (lane == 0) {
 #pragma unroll 1
-    for (int m = 0; m < MT; ++m) {
+          for (int m = 0; m < MT; ++m) {
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k)
-        multiply(s_cols(i & 1, m), operand(smem_q + (m * (D / 64) + k / 4) * S::half + (k & 3) * 32),
-                 operand(smem_k + (i & 1) * S::kbuf + (k / 4) * (kPos * 128) + (k & 3) * 32), shape_of(kPos), k > 0);
-      multiply(s_cols(i & 1, m), operand32(smem_q + S::at_qm + m * S::q_more), operand32(smem_q + S::at_km + (i & 1) * S::k_more),
-               shape_of(kPos), true);
-    }
-    commit(&sh.s[i & 1]);
-  };
-  auto issue_o = [&](int i) {
-    fence_after();
+            for (int k = 0; k < D / 16; ++k)
+              multiply(s_cols(i & 1, m), operand(smem_q + (m * (D / 64) + k / 4) * S::half + (k & 3) * 32),
+                       operand(smem_k + (i & 1) * S::kbuf + (k / 4) * (kPos * 128) + (k & 3) * 32), shape_of(kPos), k > 0);
+            multiply(s_cols(i & 1, m), operand32(smem_q + S::at_qm + m * S::q_more), operand32(smem_q + S::at_km + (i & 1) * S::k_more),
+                     shape_of(kPos), true);
+          }
+          commit(&sh.s[i & 1]);
+        }
+        __syncwarp();
+      };
+      auto issue_o = [&](int i) {
+        o_issued = i + 1;
+        fence_after();
+        if (lane == 0) {
 #pragma unroll 1
-    for (int m = 0; m < MT; ++m) {
+          for (int m = 0; m < MT; ++m) {
 #pragma unroll
-      for (int k = 0; k < kPos / 16; ++k)
-        multiply(o_cols(m), operand(smem_p + m * S::half + k * 32), operand(smem_v + (i % 3) * S::vbuf + k * 32), shape_of(D),
-                 i > 0 || k > 0);
-    }
-    commit(&sh.pv);
-  };
-
-  // --- the computing warps' parts ---
-  bool failed = false;
-  auto in_block = [&](int pos) { return pos >= from && pos <= hi_last; };
-  // Step i's largest exponents, once its tiles have landed.
-  auto look = [&](int i) {
-    const int stage = i % kRaw, slot = i & 3;
-    if (!mbar_wait_bounded(&sh.raw[stage], (i / kRaw) & 1)) failed = true;
-    if (tid >= 2 * kPos) return;
-    const int tk = tid & (kPos - 1), which = tid / kPos;
-    const bool held = ((sh.valid[i & 7] >> (tk / kTile)) & 1) && in_block((first + i * kSub) * kTile + tk);
-    float top = 0.f;
-    uint32_t odd = 0;
-    if (held) {
-      const uint8_t* tile = smem + S::at_raw + stage * S::raw1 + (tk / kTile) * TB;
-      const uint16_t* meta = reinterpret_cast<const uint16_t*>(tile + (which ? ts.v_meta() : ts.k_meta())) + (tk % kTile) * 2 * NG;
-#pragma unroll
-      for (int k = 0; k < NG; ++k) {
-        const float s = __uint_as_float(uint32_t(meta[k]) << 16), m = __uint_as_float(uint32_t(meta[NG + k]) << 16);
-        const float big = fmaxf(fabsf(m), fabsf(fmaf(15.f, s, m)));
-        if (s != s || m != m) odd |= 1u << k;
-        else top = fmaxf(top, fminf(big, 3.0e38f));
+            for (int k = 0; k < kPos / 16; ++k)
+              multiply(o_cols(m), operand(smem_p + m * S::half + k * 32), operand(smem_v + (i % 3) * S::vbuf + k * 32), shape_of(D),
+                       i > 0 || k > 0);
+          }
+          commit(&sh.pv[i % 3]);
+        }
+        __syncwarp();
+      };
+#pragma unroll 1
+      for (int i = 0; i < kRaw && i < n; ++i) copy_step(i);
+      bool ok = warp_wait(&sh.q, 0, sh, p.status);
+      // S of step i + 1 goes out before O of step i, whose weights take longer
+#pragma unroll 1
+      for (int i = -1; i < n && ok; ++i) {
+        if (i + 1 < n) {
+          ok = warp_wait(&sh.ready[(i + 1) & 3], ((i + 1) >> 2) & 1, sh, p.status);
+          if (!ok) break;
+          issue_s(i + 1);
+          if (i + 1 + kRaw < n) copy_step(i + 1 + kRaw);
+        }
+        if (i >= 0) {
+          ok = warp_wait(&sh.p, i & 1, sh, p.status);
+          if (!ok) break;
+          issue_o(i);
+        }
       }
+      if (!ok && lane == 0) {
+        // a wait gave up: let what is in flight land (each wait with the same bound); the output is incomplete
+        for (int i = copied > kRaw ? copied - kRaw : 0; i < copied; ++i) mbar_wait_bounded(&sh.raw[i % kRaw], (i / kRaw) & 1);
+        for (int i = s_issued > 2 ? s_issued - 2 : 0; i < s_issued; ++i) mbar_wait_bounded(&sh.s[i & 1], (i >> 1) & 1);
+        for (int i = o_issued > 3 ? o_issued - 3 : 0; i < o_issued; ++i) mbar_wait_bounded(&sh.pv[i % 3], (i / 3) & 1);
+      }
+      __syncwarp();
     }
-    if (which) {
-      sh.odd_groups[slot][tk] = uint8_t(odd);
-      if (odd) atomicOr(&sh.odd[slot], 1u);
-    }
-    const int e = __reduce_max_sync(0xffffffffu, __float_as_int(top) >> 23);
-    if (lane == 0) atomicMax(&sh.top[slot][which], e);
-  };
-  // Exponents that steps are held at: they only grow.
-  int ek = 15, ev = 15;
-  // Step i unpacked with them: warp w takes K (even) or V (odd) of cache tile w / 2.
-  auto unpack = [&](int i) {
-    const int stage = i % kRaw, sub = warp >> 1;
-    const int g = lane >> 2, t = lane & 3;
-    const uint8_t* tile = smem + S::at_raw + stage * S::raw1 + sub * TB;
-    const int pos = (first + i * kSub + sub) * kTile;
-    const bool exists = (sh.valid[i & 7] >> sub) & 1;
-    // codes n, less `less`, of the even and the odd places as fp16 numbers
-    auto whole = [](uint32_t v, float less) {
-      const uint32_t w = (v & 0x000f000fu) | 0x64006400u;              // 1024 + n
-      return __hsub2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(1024.f + less));
-    };
-    auto odd_place = [](uint32_t v, float less) {
-      const uint32_t w = (v & 0x00f000f0u) | 0x64006400u;              // 1024 + 16 n
-      return __hfma2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(0.0625f), __float2half2_rn(-64.f - less));
-    };
-    auto bits = [](__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); };
-    if ((warp & 1) == 0) {
-      const float f = down(ek);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int row = g + 8 * j, tk = sub * kTile + row;
-        const bool held = exists && in_block(pos + row);
-        uint32_t w[C] = {}, meta[NG] = {};
-        if (held) {
-          load_words<C>(w, tile + row * (D / 2) + t * (D / 8));
-          load_words<NG>(meta, tile + ts.k_meta() + row * 4 * NG);
-        }
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          float s, m;
-          group_meta<NG>(meta, c / PG, s, m);
-          const __half2 s2 = __float2half2_rn(s * f);
-          // dims 0, 4, 1, 5, 2, 6, 3, 7 of the word's eight
-          const uint4 v = make_uint4(bits(__hmul2(whole(w[c], 8.f), s2)), bits(__hmul2(odd_place(w[c], 8.f), s2)),
-                                     bits(__hmul2(whole(w[c] >> 8, 8.f), s2)), bits(__hmul2(odd_place(w[c] >> 8, 8.f), s2)));
-          const int word = 4 * c + t;
-          *reinterpret_cast<uint4*>(smem + S::at_k + (i & 1) * S::kbuf + (word >> 3) * (kPos * 128) + tk * 128 +
-                                    (((word & 7) ^ (tk & 7)) << 4)) = v;
-        }
-        // the groups' m + 8 s: first planes (t = 0), second planes (1), first again (2), nothing (3)
-        float plane[4] = {0.f, 0.f, 0.f, 0.f};
+  } else if (warp >= kUnpackWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsUnpack));
+    // --- unpacking: warp w takes K (even) or V (odd) of cache tile w / 2 of a step ---
+    const int uw = warp - kUnpackWarp, ut = tid - kUnpackWarp * 32;
+    auto in_block = [&](int pos) { return pos >= from && pos <= hi_last; };
+    // The largest exponents of a step that has landed.
+    auto look = [&](int i) {
+      const int stage = i % kRaw, slot = i & 7;
+      if (ut >= 2 * kPos) return;
+      const int tk = ut & (kPos - 1), which = ut / kPos;
+      const bool held = ((sh.valid[i & 7] >> (tk / kTile)) & 1) && in_block((first + i * kSub) * kTile + tk);
+      float top = 0.f;
+      uint32_t odd = 0;
+      if (held) {
+        const uint8_t* tile = smem + S::at_raw + stage * S::raw1 + (tk / kTile) * TB;
+        const uint16_t* meta = reinterpret_cast<const uint16_t*>(tile + (which ? ts.v_meta() : ts.k_meta())) + (tk % kTile) * 2 * NG;
 #pragma unroll
         for (int k = 0; k < NG; ++k) {
-          float s, m;
-          group_meta<NG>(meta, k, s, m);
-          const float x = fmaf(8.f, s, m) * f, first_plane = __half2float(__float2half_rn(x));
-          plane[k] = t == 3 ? 0.f : t == 1 ? x - first_plane : first_plane;
-        }
-        *reinterpret_cast<uint2*>(smem + S::at_km + (i & 1) * S::k_more + tk * 32 + (((t >> 1) ^ ((tk >> 2) & 1)) << 4) + (t & 1) * 8) =
-            make_uint2(pack_f16(plane[0], plane[1]), pack_f16(plane[2], plane[3]));
-      }
-    } else {
-      const float f = down(ev);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int pair = t + 4 * j, tk = sub * kTile + 2 * pair;
-        const bool held0 = exists && in_block(pos + 2 * pair), held1 = exists && in_block(pos + 2 * pair + 1);
-        uint32_t w[C] = {}, meta0[NG] = {}, meta1[NG] = {};
-        if (held0 || held1) load_words<C>(w, tile + ts.v_codes() + pair * D + ts.v_place(pair, g) * (D / 8));
-        if (held0) load_words<NG>(meta0, tile + ts.v_meta() + 2 * pair * 4 * NG);
-        if (held1) load_words<NG>(meta1, tile + ts.v_meta() + (2 * pair + 1) * 4 * NG);
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          float sa, ma, sb, mb;
-          group_meta<NG>(meta0, c / PG, sa, ma);
-          group_meta<NG>(meta1, c / PG, sb, mb);
-          if (sa != sa || ma != ma) sa = ma = 0.f;                       // NaN is put into the rows that see it at the end
-          if (sb != sb || mb != mb) sb = mb = 0.f;
-          const __half2 s2 = __floats2half2_rn(sa * f, sb * f), m2 = __floats2half2_rn(ma * f, mb * f);
-          const __half2 v[4] = {__hfma2(whole(w[c], 0.f), s2, m2), __hfma2(odd_place(w[c], 0.f), s2, m2),
-                                __hfma2(whole(w[c] >> 8, 0.f), s2, m2), __hfma2(odd_place(w[c] >> 8, 0.f), s2, m2)};
-          // dim 32c + 4g + e in row 32c + 8e + g: lanes of one store in eight rows, as many 16-byte words
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int row = 32 * c + 8 * e + g;
-            *reinterpret_cast<uint32_t*>(smem + S::at_v + (i % 3) * S::vbuf + row * 128 + (((tk >> 3) ^ (row & 7)) << 4) +
-                                         (tk & 7) * 2) = bits(v[e]);
-          }
+          const float s = __uint_as_float(uint32_t(meta[k]) << 16), m = __uint_as_float(uint32_t(meta[NG + k]) << 16);
+          const float big = fmaxf(fabsf(m), fabsf(fmaf(15.f, s, m)));
+          if (s != s || m != m) odd |= 1u << k;
+          else top = fmaxf(top, fminf(big, 3.0e38f));
         }
       }
-    }
-  };
-  auto grow = [&](int i, int& e, int which) { e = min(max(e, sh.top[i & 3][which]), 254); };
-
-  if (warp == kWarps) {
-    copy_step(0);
-    if (n > 1) copy_step(1);
-    if (n > 2) copy_step(2);
-  } else if (has_row) {
-    // the row's query, scaled below 2^8 (128 of them sum up within fp16), in the order of the keys' dims
-    const void* src = nullptr;
-    if (real)
-      src = static_cast<const uint16_t*>(p.q) + (sq.q0 + r / p.group) * p.q_token + int64_t(h * p.group + r % p.group) * p.q_head;
-    auto value = [&](int d) {
-      return p.q_f16 ? to_f32(static_cast<const __half*>(src)[d]) : to_f32(static_cast<const __nv_bfloat16*>(src)[d]);
+      if (which) {
+        sh.odd_groups[slot][tk] = uint8_t(odd);
+        if (odd) atomicOr(&sh.odd[slot], 1u);
+      }
+      const int e = __reduce_max_sync(0xffffffffu, __float_as_int(top) >> 23);
+      if (lane == 0) atomicMax(&sh.top[slot][which], e);
     };
-    float top = 0.f;
-    if (real) {
-#pragma unroll 8
-      for (int d = 0; d < D; ++d) top = fmaxf(top, fabsf(value(d)));
-    }
-    const int e = 134 - min(max(__float_as_int(top) >> 23, 1), 254), e1 = e >> 1, e2 = e - e1;
-    const float f1 = __int_as_float((127 + e1) << 23), f2 = __int_as_float((127 + e2) << 23);
-    float sums[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
-#pragma unroll 1
-    for (int w = 0; w < D / 8; ++w) {
-      uint32_t x[4] = {0u, 0u, 0u, 0u};
-      if (real) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          x[j] = pack_f16(value(8 * w + j) * f1 * f2, value(8 * w + 4 + j) * f1 * f2);
-          const float2 held = __half22float2(*reinterpret_cast<const __half2*>(&x[j]));
-          sum += held.x + held.y;
-        }
-      }
-      if ((w + 1) % (D / 8 / NG) == 0) {          // the end of a group
-#pragma unroll
-        for (int k = 0; k < NG; ++k)
-          if ((w + 1) / (D / 8 / NG) == k + 1) sums[k] = sum;
-        sum = 0.f;
-      }
-      *reinterpret_cast<uint4*>(smem + (mt * (D / 64) + (w >> 3)) * S::half + rt * 128 + (((w & 7) ^ (rt & 7)) << 4)) =
-          make_uint4(x[0], x[1], x[2], x[3]);
-    }
-    // against the keys' planes: first planes twice, then what they left over
-    float left[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      left[k] = sums[k];
-      sums[k] = __half2float(__float2half_rn(sums[k]));
-      left[k] -= sums[k];
-    }
-    const uint2 top_planes = make_uint2(pack_f16(sums[0], sums[1]), pack_f16(sums[2], sums[3]));
-    const uint2 low_planes = make_uint2(pack_f16(left[0], left[1]), pack_f16(left[2], left[3]));
-    uint8_t* more = smem + S::at_qm + mt * S::q_more + rt * 32;
-    const int turn_word = ((rt >> 2) & 1) << 4;
-    *reinterpret_cast<uint4*>(more + turn_word) = make_uint4(top_planes.x, top_planes.y, top_planes.x, top_planes.y);
-    *reinterpret_cast<uint4*>(more + (16 ^ turn_word)) = make_uint4(low_planes.x, low_planes.y, 0u, 0u);
-    l = p.scale2 * __int_as_float((127 - e1) << 23) * __int_as_float((127 - e2) << 23);      // until the first step
-  }
-  const float cq = l;
-  l = 0.f;
-  if (warp < kWarps) {
-    look(0);
-    if (n > 1) look(1);
-    if (n > 2) look(2);
-  }
-  __syncthreads();
-  // exponents of the step at hand and of the two after it
-  int ek0 = 15, ev0 = 15, ek1 = 15, ev1 = 15;
-  if (warp < kWarps) {
-    grow(0, ek, 0);
-    grow(0, ev, 1);
-    ek0 = ek;
-    ev0 = ev;
-    unpack(0);
-    if (n > 1) {
-      grow(1, ek, 0);
-      grow(1, ev, 1);
-      unpack(1);
-    }
-    ek1 = ek;
-    ev1 = ev;
-    fence_proxy_async_smem();
-  }
-  failed = __syncthreads_or(failed);
-  if (!failed && warp == kWarps) {
-    if (n > 3) copy_step(3);
-    if (n > 4) copy_step(4);
-    if (lane == 0) issue_s(0);
-  }
-
-  int ev_was = ev0, done = 0;                     // done: products P V issued
-  const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
-#pragma unroll 1
-  for (int i = 0; i < n && !failed; ++i) {
-    if (warp == kWarps) {
-      if (i + 1 < n && lane == 0) issue_s(i + 1);
-      __syncwarp();
-    } else if (has_row) {
-      if (!mbar_wait_bounded(&sh.s[i & 1], (i >> 1) & 1)) failed = true;
-      fence_after();
-      float x[kPos];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) load16(s_cols(i & 1, mt) + lanes + 16 * k, x + 16 * k);
-      landed();
-#pragma unroll
-      for (int k = 0; k < 4; ++k) defined16(x + 16 * k);
-      const float f = fmaxf(cq * up(ek0), 1.17549435e-38f);      // positive: -inf stays -inf
-      const int pos = (first + i * kSub) * kTile;
-      const uint32_t valid = sh.valid[i & 7];
-      const bool all = pos >= lo_last && pos + kPos - 1 <= hi_first;
-      // the row sees positions pos + a .. pos + b - 1 of the step
-      const int a = min(max(lo - pos, 0), kPos), z = min(max(hi + 1 - pos, 0), kPos);
-      uint64_t see = ~0ull;
-      if (!all || valid != (1u << kSub) - 1u) {
-        see = z <= a ? 0ull : ((z == 64 ? ~0ull : (1ull << z) - 1ull) & ~((a == 64 ? 0ull : 1ull << a) - 1ull));
-#pragma unroll
-        for (int k = 0; k < kSub; ++k)
-          if (!((valid >> k) & 1)) see &= ~(0xffffull << (16 * k));
-      }
-      float sum = 0.f;
-      auto weights = [&]() {                      // x: logits -> weights, in place; their sum
-        float2 s2 = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < kPos; k += 2) {
-          const float2 y = ffma2(make_float2(x[k], x[k + 1]), make_float2(f, f), make_float2(-ref, -ref));
-          float2 w = make_float2(exp2_fast(y.x), exp2_fast(y.y));
-          s2 = fadd2(s2, w);
-          x[k] = w.x;
-          x[k + 1] = w.y;
-        }
-        sum = s2.x + s2.y;
+    // Exponents that steps are held at: they only grow.
+    int ek = 15, ev = 15;
+    auto unpack = [&](int i) {
+      const int stage = i % kRaw, sub = uw >> 1;
+      const int g = lane >> 2, t = lane & 3;
+      const uint8_t* tile = smem + S::at_raw + stage * S::raw1 + sub * TB;
+      const int pos = (first + i * kSub + sub) * kTile;
+      const bool exists = (sh.valid[i & 7] >> sub) & 1;
+      // codes n, less `less`, of the even and the odd places as fp16 numbers
+      auto whole = [](uint32_t v, float less) {
+        const uint32_t w = (v & 0x000f000fu) | 0x64006400u;              // 1024 + n
+        return __hsub2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(1024.f + less));
       };
-      const bool masked = __any_sync(0xffffffffu, see != ~0ull);
-      if (masked) {
+      auto odd_place = [](uint32_t v, float less) {
+        const uint32_t w = (v & 0x00f000f0u) | 0x64006400u;              // 1024 + 16 n
+        return __hfma2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(0.0625f), __float2half2_rn(-64.f - less));
+      };
+      auto bits = [](__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); };
+      if ((uw & 1) == 0) {
+        const float f = down(ek);
 #pragma unroll
-        for (int k = 0; k < kPos; ++k)
-          if (!((see >> k) & 1)) x[k] = -INFINITY;
-      }
-      // Logits are needed again only where the reference moves: find that out from
-      // the largest (of three at a time) rather than from the weights.
-      float top = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < kPos; k += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(x[k]), "f"(x[k + 1]));
-      const float best = top * f;
-      float keep = 1.f;
-      bool moves = best - ref > 14.f;
-      if (moves) {
-        const float now = best - 6.f;
-        keep = exp2f(ref - now);
-        ref = now;
-      }
-      weights();
-      l = l * keep + sum;
-      if (sh.odd[i & 3]) {                        // NaN values: which groups this row sees
-#pragma unroll 1
-        for (int k = 0; k < kPos; ++k)
-          if ((see >> k) & 1) nan_groups |= sh.odd_groups[i & 3][k];
-      }
-      // P and O once the products before have been added
-      if (i > 0) {
-        if (!mbar_wait_bounded(&sh.pv, (i - 1) & 1)) failed = true;
-        fence_after();
-        if (ev0 != ev_was) keep *= __int_as_float((127 + max(ev_was - ev0, -126)) << 23);
-        if (__any_sync(0xffffffffu, keep != 1.f)) {
-#pragma unroll 1
-          for (int c = 0; c < D / 16; ++c) {
-            float v[16];
-            load16(o_cols(mt) + lanes + 16 * c, v);
-            landed();
-            defined16(v);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) v[k] *= keep;
-            store16(o_cols(mt) + lanes + 16 * c, v);
+        for (int j = 0; j < 2; ++j) {
+          const int row = g + 8 * j, tk = sub * kTile + row;
+          const bool held = exists && in_block(pos + row);
+          uint32_t w[C] = {}, meta[NG] = {};
+          if (held) {
+            load_words<C>(w, tile + row * (D / 2) + t * (D / 8));
+            load_words<NG>(meta, tile + ts.k_meta() + row * 4 * NG);
           }
-          stored();
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            float s, m;
+            group_meta<NG>(meta, c / PG, s, m);
+            const __half2 s2 = __float2half2_rn(s * f);
+            // dims 0, 4, 1, 5, 2, 6, 3, 7 of the word's eight
+            const uint4 v = make_uint4(bits(__hmul2(whole(w[c], 8.f), s2)), bits(__hmul2(odd_place(w[c], 8.f), s2)),
+                                       bits(__hmul2(whole(w[c] >> 8, 8.f), s2)), bits(__hmul2(odd_place(w[c] >> 8, 8.f), s2)));
+            const int word = 4 * c + t;
+            *reinterpret_cast<uint4*>(smem + S::at_k + (i & 1) * S::kbuf + (word >> 3) * (kPos * 128) + tk * 128 +
+                                      (((word & 7) ^ (tk & 7)) << 4)) = v;
+          }
+          // the groups' m + 8 s: first planes (t = 0), second planes (1), first again (2), nothing (3)
+          float plane[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < NG; ++k) {
+            float s, m;
+            group_meta<NG>(meta, k, s, m);
+            const float x = fmaf(8.f, s, m) * f, first_plane = __half2float(__float2half_rn(x));
+            plane[k] = t == 3 ? 0.f : t == 1 ? x - first_plane : first_plane;
+          }
+          *reinterpret_cast<uint2*>(smem + S::at_km + (i & 1) * S::k_more + tk * 32 + (((t >> 1) ^ ((tk >> 2) & 1)) << 4) + (t & 1) * 8) =
+              make_uint2(pack_f16(plane[0], plane[1]), pack_f16(plane[2], plane[3]));
+        }
+      } else {
+        const float f = down(ev);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int pair = t + 4 * j, tk = sub * kTile + 2 * pair;
+          const bool held0 = exists && in_block(pos + 2 * pair), held1 = exists && in_block(pos + 2 * pair + 1);
+          uint32_t w[C] = {}, meta0[NG] = {}, meta1[NG] = {};
+          if (held0 || held1) load_words<C>(w, tile + ts.v_codes() + pair * D + ts.v_place(pair, g) * (D / 8));
+          if (held0) load_words<NG>(meta0, tile + ts.v_meta() + 2 * pair * 4 * NG);
+          if (held1) load_words<NG>(meta1, tile + ts.v_meta() + (2 * pair + 1) * 4 * NG);
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            float sa, ma, sb, mb;
+            group_meta<NG>(meta0, c / PG, sa, ma);
+            group_meta<NG>(meta1, c / PG, sb, mb);
+            if (sa != sa || ma != ma) sa = ma = 0.f;                       // NaN is put into the rows that see it at the end
+            if (sb != sb || mb != mb) sb = mb = 0.f;
+            const __half2 s2 = __floats2half2_rn(sa * f, sb * f), m2 = __floats2half2_rn(ma * f, mb * f);
+            const __half2 v[4] = {__hfma2(whole(w[c], 0.f), s2, m2), __hfma2(odd_place(w[c], 0.f), s2, m2),
+                                  __hfma2(whole(w[c] >> 8, 0.f), s2, m2), __hfma2(odd_place(w[c] >> 8, 0.f), s2, m2)};
+            // dim 32c + 4g + e in row 32c + 8e + g: lanes of one store in eight rows, as many 16-byte words
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int row = 32 * c + 8 * e + g;
+              *reinterpret_cast<uint32_t*>(smem + S::at_v + (i % 3) * S::vbuf + row * 128 + (((tk >> 3) ^ (row & 7)) << 4) +
+                                           (tk & 7) * 2) = bits(v[e]);
+            }
+          }
         }
       }
-      ev_was = ev0;
-#pragma unroll
-      for (int w = 0; w < 8; ++w)
-        *reinterpret_cast<uint4*>(smem + S::at_p + mt * S::half + rt * 128 + ((w ^ (rt & 7)) << 4)) =
-            make_uint4(pack_f16(x[8 * w], x[8 * w + 1]), pack_f16(x[8 * w + 2], x[8 * w + 3]),
-                       pack_f16(x[8 * w + 4], x[8 * w + 5]), pack_f16(x[8 * w + 6], x[8 * w + 7]));
-      fence_proxy_async_smem();
-      fence_before();
-    } else if (i > 0) {                           // a warp without rows also waits before it writes V
-      if (!mbar_wait_bounded(&sh.pv, (i - 1) & 1)) failed = true;
-    }
-    failed = __syncthreads_or(failed);
-    if (failed) break;
-    if (warp == kWarps) {
-      done = i + 1;
-      if (lane == 0) issue_o(i);
-      __syncwarp();
-    } else {
-      if (tid == 0) {
-        sh.top[i & 3][0] = sh.top[i & 3][1] = 0;
-        sh.odd[i & 3] = 0;
-      }
-      ek0 = ek1;
-      ev0 = ev1;
-      if (i + 2 < n) {
-        grow(i + 2, ek, 0);
-        grow(i + 2, ev, 1);
-        unpack(i + 2);
-        fence_proxy_async_smem();
-      }
-      ek1 = ek;
-      ev1 = ev;
-      if (i + 3 < n) look(i + 3);
-    }
-    failed = __syncthreads_or(failed);
-    if (!failed && warp == kWarps && i + 5 < n) copy_step(i + 5);
-  }
-
-  if (failed) {
-    // A wait gave up: let what is in flight land (waits with the same bound), then
-    // free the tensor memory; the output is incomplete.
-    if (tid == 0) report_status(p.status, kStatusWaitTimeout);
-    if (warp == kWarps && lane == 0) {
-      for (int i = copied > kRaw ? copied - kRaw : 0; i < copied; ++i) mbar_wait_bounded(&sh.raw[i % kRaw], (i / kRaw) & 1);
-      for (int i = s_issued > 2 ? s_issued - 2 : 0; i < s_issued; ++i) mbar_wait_bounded(&sh.s[i & 1], (i >> 1) & 1);
-      if (done > 0) mbar_wait_bounded(&sh.pv, (done - 1) & 1);
-    }
-  } else if (has_row) {
-    if (!mbar_wait_bounded(&sh.pv, (n - 1) & 1)) report_status(p.status, kStatusWaitTimeout);
-    fence_after();
-    const bool seen = ref != kNoRef || l != 0.f;
-    const float inv = seen ? up(ev_was) / l : 0.f;
+    };
+    bool ok = warp_wait(&sh.raw[0], 0, sh, p.status);
+    if (ok) look(0);
+    warp_arrive(&sh.looked, lane);
 #pragma unroll 1
-    for (int c = 0; c < C; ++c) {
-      float o[32], v[32];
-      load16(o_cols(mt) + lanes + 32 * c, o);
-      load16(o_cols(mt) + lanes + 32 * c + 16, o + 16);
-      landed();
-      defined16(o);
-      defined16(o + 16);
-      const bool bad = (nan_groups >> (c / PG)) & 1;
-#pragma unroll
-      for (int k = 0; k < 32; ++k) v[4 * (k & 7) + (k >> 3)] = bad ? __int_as_float(0x7fc00000) : o[k] * inv;
-      finish_row(c, v);
+    for (int i = 0; i < n && ok; ++i) {
+      ok = warp_wait(&sh.looked, i & 1, sh, p.status);
+      if (ok && i >= 2) ok = warp_wait(&sh.s[i & 1], ((i - 2) >> 1) & 1, sh, p.status);
+      if (ok && i >= 3) ok = warp_wait(&sh.pv[i % 3], ((i - 3) / 3) & 1, sh, p.status);
+      if (!ok) break;
+      ek = min(max(ek, sh.top[i & 7][0]), 254);
+      ev = min(max(ev, sh.top[i & 7][1]), 254);
+      if (ut == 0) {
+        sh.held[i & 7][0] = ek;
+        sh.held[i & 7][1] = ev;
+        // of step i - 4, which every warp is done with
+        sh.top[(i + 4) & 7][0] = sh.top[(i + 4) & 7][1] = 0;
+        sh.odd[(i + 4) & 7] = 0;
+      }
+      unpack(i);
+      fence_proxy_async_smem();
+      warp_arrive(&sh.ready[i & 3], lane);
+      if (i + 1 < n) {
+        ok = warp_wait(&sh.raw[(i + 1) % kRaw], ((i + 1) / kRaw) & 1, sh, p.status);
+        if (ok) look(i + 1);
+        warp_arrive(&sh.looked, lane);
+      }
     }
-    const float sum = seen ? ref + log2f(l) : -INFINITY;
-    if (real) {
-      if (bp.parts > 1) record_ref[mt * 128 + rt] = sum;
-      else store_lse(p, sq, h, r, sum);
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    if (warp < 4 * MT) {
+      // --- the softmax, a row a thread ---
+      const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
+      const int hi = base + min(r, rows - 1) / p.group;
+      const int lo = p.window > 0 ? max(0, hi - p.window + 1) : 0;
+      float ref = kNoRef, l = 0.f;
+      uint32_t nan_groups = 0;
+      // the row's query, scaled below 2^8 (128 of them sum up within fp16), in the order of the keys' dims
+      const void* src = nullptr;
+      if (real)
+        src = static_cast<const uint16_t*>(p.q) + (sq.q0 + r / p.group) * p.q_token + int64_t(h * p.group + r % p.group) * p.q_head;
+      auto value = [&](int d) {
+        return p.q_f16 ? to_f32(static_cast<const __half*>(src)[d]) : to_f32(static_cast<const __nv_bfloat16*>(src)[d]);
+      };
+      float top = 0.f;
+      if (real) {
+#pragma unroll 8
+        for (int d = 0; d < D; ++d) top = fmaxf(top, fabsf(value(d)));
+      }
+      const int e = 134 - min(max(__float_as_int(top) >> 23, 1), 254), e1 = e >> 1, e2 = e - e1;
+      const float f1 = __int_as_float((127 + e1) << 23), f2 = __int_as_float((127 + e2) << 23);
+      float sums[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+#pragma unroll 1
+      for (int w = 0; w < D / 8; ++w) {
+        uint32_t x[4] = {0u, 0u, 0u, 0u};
+        if (real) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            x[j] = pack_f16(value(8 * w + j) * f1 * f2, value(8 * w + 4 + j) * f1 * f2);
+            const float2 held = __half22float2(*reinterpret_cast<const __half2*>(&x[j]));
+            sum += held.x + held.y;
+          }
+        }
+        if ((w + 1) % (D / 8 / NG) == 0) {          // the end of a group
+#pragma unroll
+          for (int k = 0; k < NG; ++k)
+            if ((w + 1) / (D / 8 / NG) == k + 1) sums[k] = sum;
+          sum = 0.f;
+        }
+        *reinterpret_cast<uint4*>(smem + (mt * (D / 64) + (w >> 3)) * S::half + rt * 128 + (((w & 7) ^ (rt & 7)) << 4)) =
+            make_uint4(x[0], x[1], x[2], x[3]);
+      }
+      // against the keys' planes: first planes twice, then what they left over
+      float left[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        left[k] = sums[k];
+        sums[k] = __half2float(__float2half_rn(sums[k]));
+        left[k] -= sums[k];
+      }
+      const uint2 top_planes = make_uint2(pack_f16(sums[0], sums[1]), pack_f16(sums[2], sums[3]));
+      const uint2 low_planes = make_uint2(pack_f16(left[0], left[1]), pack_f16(left[2], left[3]));
+      uint8_t* more = smem + S::at_qm + mt * S::q_more + rt * 32;
+      const int turn_word = ((rt >> 2) & 1) << 4;
+      *reinterpret_cast<uint4*>(more + turn_word) = make_uint4(top_planes.x, top_planes.y, top_planes.x, top_planes.y);
+      *reinterpret_cast<uint4*>(more + (16 ^ turn_word)) = make_uint4(low_planes.x, low_planes.y, 0u, 0u);
+      l = p.scale2 * __int_as_float((127 - e1) << 23) * __int_as_float((127 - e2) << 23);      // until the first step
+      const float cq = l;
+      l = 0.f;
+      fence_proxy_async_smem();
+      warp_arrive(&sh.q, lane);
+      int ev_was = 15;
+      bool ok = true;
+#pragma unroll 1
+      for (int i = 0; i < n; ++i) {
+        ok = warp_wait(&sh.ready[i & 3], (i >> 2) & 1, sh, p.status) && warp_wait(&sh.s[i & 1], (i >> 1) & 1, sh, p.status);
+        if (!ok) break;
+        fence_after();
+        const int ek0 = sh.held[i & 7][0], ev0 = sh.held[i & 7][1];
+        float x[kPos];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) load16(s_cols(i & 1, mt) + lanes + 16 * k, x + 16 * k);
+        landed();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) defined16(x + 16 * k);
+        const float f = fmaxf(cq * up(ek0), 1.17549435e-38f);      // positive: -inf stays -inf
+        const int pos = (first + i * kSub) * kTile;
+        const uint32_t valid = sh.valid[i & 7];
+        const bool all = pos >= lo_last && pos + kPos - 1 <= hi_first;
+        // the row sees positions pos + a .. pos + z - 1 of the step
+        const int a = min(max(lo - pos, 0), kPos), z = min(max(hi + 1 - pos, 0), kPos);
+        uint64_t see = ~0ull;
+        if (!all || valid != (1u << kSub) - 1u) {
+          see = z <= a ? 0ull : ((z == 64 ? ~0ull : (1ull << z) - 1ull) & ~((a == 64 ? 0ull : 1ull << a) - 1ull));
+#pragma unroll
+          for (int k = 0; k < kSub; ++k)
+            if (!((valid >> k) & 1)) see &= ~(0xffffull << (16 * k));
+        }
+        float sum = 0.f;
+        auto weights = [&]() {                      // x: logits -> weights, in place; their sum
+          float2 s2 = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int k = 0; k < kPos; k += 2) {
+            const float2 y = ffma2(make_float2(x[k], x[k + 1]), make_float2(f, f), make_float2(-ref, -ref));
+            float2 w = make_float2(exp2_fast(y.x), exp2_fast(y.y));
+            s2 = fadd2(s2, w);
+            x[k] = w.x;
+            x[k + 1] = w.y;
+          }
+          sum = s2.x + s2.y;
+        };
+        const bool masked = __any_sync(0xffffffffu, see != ~0ull);
+        if (masked) {
+#pragma unroll
+          for (int k = 0; k < kPos; ++k)
+            if (!((see >> k) & 1)) x[k] = -INFINITY;
+        }
+        // Logits are needed again only where the reference moves: find that out from
+        // the largest (of three at a time) rather than from the weights.
+        float top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kPos; k += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(x[k]), "f"(x[k + 1]));
+        const float best = top * f;
+        float keep = 1.f;
+        bool moves = best - ref > 14.f;
+        if (moves) {
+          const float now = best - 6.f;
+          keep = exp2f(ref - now);
+          ref = now;
+        }
+        weights();
+        l = l * keep + sum;
+        if (sh.odd[i & 7]) {                        // NaN values: which groups this row sees
+#pragma unroll 1
+          for (int k = 0; k < kPos; ++k)
+            if ((see >> k) & 1) nan_groups |= sh.odd_groups[i & 7][k];
+        }
+        // P and O once the products before have been added
+        if (i > 0) {
+          ok = warp_wait(&sh.pv[(i - 1) % 3], ((i - 1) / 3) & 1, sh, p.status);
+          if (!ok) break;
+          fence_after();
+          if (ev0 != ev_was) keep *= __int_as_float((127 + max(ev_was - ev0, -126)) << 23);
+          if (__any_sync(0xffffffffu, keep != 1.f)) {
+#pragma unroll 1
+            for (int c = 0; c < D / 16; ++c) {
+              float v[16];
+              load16(o_cols(mt) + lanes + 16 * c, v);
+              landed();
+              defined16(v);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) v[k] *= keep;
+              store16(o_cols(mt) + lanes + 16 * c, v);
+            }
+            stored();
+          }
+        }
+        ev_was = ev0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w)
+          *reinterpret_cast<uint4*>(smem + S::at_p + mt * S::half + rt * 128 + ((w ^ (rt & 7)) << 4)) =
+              make_uint4(pack_f16(x[8 * w], x[8 * w + 1]), pack_f16(x[8 * w + 2], x[8 * w + 3]),
+                         pack_f16(x[8 * w + 4], x[8 * w + 5]), pack_f16(x[8 * w + 6], x[8 * w + 7]));
+        fence_proxy_async_smem();
+        fence_before();
+        warp_arrive(&sh.p, lane);
+      }
+      if (ok) ok = warp_wait(&sh.pv[(n - 1) % 3], ((n - 1) / 3) & 1, sh, p.status);
+      if (ok) {
+        fence_after();
+        const bool seen = ref != kNoRef || l != 0.f;
+        const float inv = seen ? up(ev_was) / l : 0.f;
+#pragma unroll 1
+        for (int c = 0; c < C; ++c) {
+          float o[32], v[32];
+          load16(o_cols(mt) + lanes + 32 * c, o);
+          load16(o_cols(mt) + lanes + 32 * c + 16, o + 16);
+          landed();
+          defined16(o);
+          defined16(o + 16);
+          const bool bad = (nan_groups >> (c / PG)) & 1;
+#pragma unroll
+          for (int k = 0; k < 32; ++k) v[4 * (k & 7) + (k >> 3)] = bad ? __int_as_float(0x7fc00000) : o[k] * inv;
+          finish_row(c, v);
+        }
+        finish_sum(seen ? ref + log2f(l) : -INFINITY);
+      }
     }
   }
   fence_before();
   __syncthreads();
   fence_after();
-  if (warp == kWarps) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kColumns));
+  if (warp == kIssueWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kColumns));
 }
 
 // The parts of a block's positions joined: one row per warp.
