@@ -11,7 +11,7 @@
 //   O += P V        [128 rows x d]              tcgen05.mma, accumulated in TMEM
 //
 // Four or eight warps take the softmax, a row a thread, eight others unpack up to
-// two steps ahead, and one issues copies and products.  Steps pass between them
+// two steps ahead, one issues the products and one the copies.  Steps pass between them
 // through mbarriers:
 //
 //   q             the queries' operands are in shared memory (softmax -> products)
@@ -46,8 +46,8 @@ namespace {
 
 constexpr int kPos = 64;                          // positions of a step
 constexpr int kSub = kPos / kTile;                // cache tiles of a step
-constexpr int kThreads = 640;                     // warps 0-7 softmax, 8-15 unpack, 16 copies and products
-constexpr int kUnpackWarp = 8, kIssueWarp = 16;
+constexpr int kThreads = 640;                     // warps 0-7 softmax, 8-15 unpack, 16 products, 17 copies
+constexpr int kUnpackWarp = 8, kIssueWarp = 16, kCopyWarp = 17;
 constexpr int kRaw = 3;                           // steps of packed tiles in flight
 // Registers a thread of each part: (2 x 136 + 2 x 80 + 40) x 128 of the launch's 96 x 640.
 constexpr int kRegsSoftmax = 136, kRegsUnpack = 80, kRegsIssue = 40;
@@ -55,27 +55,22 @@ static_assert((2 * kRegsSoftmax + 2 * kRegsUnpack + kRegsIssue) * 128 <= 96 * kT
 
 // --- tensor core instructions ---
 
-// Descriptor of a K-major operand in shared memory: rows of 128 bytes (64 fp16)
-// with the 128-byte swizzle (16-byte word w of row r at w ^ (r & 7)), groups of
-// eight rows 1024 bytes apart.
-__device__ __forceinline__ uint64_t operand(uint32_t saddr) {
-  return uint64_t((saddr & 0x3FFFFu) >> 4) | (uint64_t(1) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) |
-         (uint64_t(2) << 61);
-}
-// The same for rows of 32 bytes (one step) with the 32-byte swizzle (16-byte word
-// w at w ^ ((r >> 2) & 1)), groups of eight rows 256 bytes apart.
-__device__ __forceinline__ uint64_t operand32(uint32_t saddr) {
-  return uint64_t((saddr & 0x3FFFFu) >> 4) | (uint64_t(1) << 16) | (uint64_t(256 >> 4) << 32) | (uint64_t(1) << 46) |
-         (uint64_t(6) << 61);
-}
+// Descriptors of K-major operands in shared memory: the address / 16 in the low
+// word, beside a constant; in the high word the distance of groups of eight rows
+// / 16, version 1 and the swizzle.  Rows of 128 bytes (64 fp16) have the 128-byte
+// swizzle (16-byte word w of row r at w ^ (r & 7)); rows of 32 bytes (one step) the
+// 32-byte swizzle (w at w ^ ((r >> 2) & 1)).
+__device__ __forceinline__ uint32_t operand(uint32_t saddr) { return (saddr >> 4) | (1u << 16); }
+constexpr uint32_t kRows128 = (1024 >> 4) | (1u << 14) | (2u << 29);
+constexpr uint32_t kRows32 = (256 >> 4) | (1u << 14) | (6u << 29);
+
 // kind::f16, fp16 operands, fp32 accumulators, 128 rows, n columns
-__device__ __forceinline__ uint32_t shape_of(int n) {
-  return (1u << 4) | (uint32_t(n >> 3) << 17) | (uint32_t(128 >> 4) << 24);
-}
-__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add) {
+__host__ __device__ constexpr uint32_t shape_of(int n) { return (1u << 4) | (uint32_t(n >> 3) << 17) | (uint32_t(128 >> 4) << 24); }
+template <uint32_t kHigh, uint32_t kShape>
+__device__ __forceinline__ void multiply(uint32_t d, uint32_t a, uint32_t b, bool add) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(shape),
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(kHigh), "r"(kShape),
       "r"(add ? 1 : 0));
 }
 __device__ __forceinline__ void commit(uint64_t* bar) {
@@ -259,9 +254,68 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
   if (warp >= kIssueWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
     if (warp == kIssueWarp) {
-      // --- copies and products ---
+      // --- products ---
+      int s_issued = 0, o_issued = 0;
+      // Every product is one instruction of one thread, so the operands' words are
+      // worked out here and the loops below have only additions.
+      const uint32_t q0 = operand(smem_q), qm0 = operand(smem_q + S::at_qm), p0 = operand(smem_p);
+      auto issue_s = [&](int i) {                 // S of step i
+        s_issued = i + 1;
+        fence_after();
+        if (lane == 0) {
+          const uint32_t k0 = operand(smem_k + (i & 1) * S::kbuf), km0 = operand(smem_q + S::at_km + (i & 1) * S::k_more);
+          const uint32_t d0 = s_cols(i & 1, 0);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+              multiply<kRows128, shape_of(kPos)>(d0 + m * kPos, q0 + (((m * (D / 64) + k / 4) * S::half + (k & 3) * 32) >> 4),
+                                                 k0 + (((k / 4) * (kPos * 128) + (k & 3) * 32) >> 4), k > 0);
+            multiply<kRows32, shape_of(kPos)>(d0 + m * kPos, qm0 + ((m * S::q_more) >> 4), km0, true);
+          }
+          commit(&sh.s[i & 1]);
+        }
+        __syncwarp();
+      };
+      auto issue_o = [&](int i) {
+        o_issued = i + 1;
+        fence_after();
+        if (lane == 0) {
+          const uint32_t v0 = operand(smem_v + (i % 3) * S::vbuf), d0 = o_cols(0);
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int k = 0; k < kPos / 16; ++k)
+              multiply<kRows128, shape_of(D)>(d0 + m * 128, p0 + ((m * S::half + k * 32) >> 4), v0 + ((k * 32) >> 4), i > 0 || k > 0);
+          commit(&sh.pv[i % 3]);
+        }
+        __syncwarp();
+      };
+      bool ok = warp_wait(&sh.q, 0, sh, p.status);
+      // S of step i + 1 goes out before O of step i, whose weights take longer
+#pragma unroll 1
+      for (int i = -1; i < n && ok; ++i) {
+        if (i + 1 < n) {
+          ok = warp_wait(&sh.ready[(i + 1) & 3], ((i + 1) >> 2) & 1, sh, p.status);
+          if (!ok) break;
+          issue_s(i + 1);
+        }
+        if (i >= 0) {
+          ok = warp_wait(&sh.p, i & 1, sh, p.status);
+          if (!ok) break;
+          issue_o(i);
+        }
+      }
+      if (!ok && lane == 0) {
+        // a wait gave up: let what is in flight land (each wait with the same bound); the output is incomplete
+        for (int i = s_issued > 2 ? s_issued - 2 : 0; i < s_issued; ++i) mbar_wait_bounded(&sh.s[i & 1], (i >> 1) & 1);
+        for (int i = o_issued > 3 ? o_issued - 3 : 0; i < o_issued; ++i) mbar_wait_bounded(&sh.pv[i % 3], (i / 3) & 1);
+      }
+      __syncwarp();
+    } else if (warp == kCopyWarp) {
+      // --- copies ---
       const int tpp = p.page_tokens / kTile;
-      int copied = 0, s_issued = 0, o_issued = 0;
+      int copied = 0;
       auto copy_step = [&](int i) {               // lanes 0..3: one cache tile each
         copied = i + 1;
         const int stage = i % kRaw, t = i * kSub + lane;
@@ -285,62 +339,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
           bulk_g2s(smem + S::at_raw + stage * S::raw1 + lane * TB,
                    p.pages + ((int64_t(page) * p.kv_heads + h) * tpp + at) * int64_t(TB), TB, &sh.raw[stage]);
       };
-      auto issue_s = [&](int i) {                 // S of step i
-        s_issued = i + 1;
-        fence_after();
-        if (lane == 0) {
+      bool ok = true;
 #pragma unroll 1
-          for (int m = 0; m < MT; ++m) {
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-              multiply(s_cols(i & 1, m), operand(smem_q + (m * (D / 64) + k / 4) * S::half + (k & 3) * 32),
-                       operand(smem_k + (i & 1) * S::kbuf + (k / 4) * (kPos * 128) + (k & 3) * 32), shape_of(kPos), k > 0);
-            multiply(s_cols(i & 1, m), operand32(smem_q + S::at_qm + m * S::q_more), operand32(smem_q + S::at_km + (i & 1) * S::k_more),
-                     shape_of(kPos), true);
-          }
-          commit(&sh.s[i & 1]);
-        }
-        __syncwarp();
-      };
-      auto issue_o = [&](int i) {
-        o_issued = i + 1;
-        fence_after();
-        if (lane == 0) {
-#pragma unroll 1
-          for (int m = 0; m < MT; ++m) {
-#pragma unroll
-            for (int k = 0; k < kPos / 16; ++k)
-              multiply(o_cols(m), operand(smem_p + m * S::half + k * 32), operand(smem_v + (i % 3) * S::vbuf + k * 32), shape_of(D),
-                       i > 0 || k > 0);
-          }
-          commit(&sh.pv[i % 3]);
-        }
-        __syncwarp();
-      };
-#pragma unroll 1
-      for (int i = 0; i < kRaw && i < n; ++i) copy_step(i);
-      bool ok = warp_wait(&sh.q, 0, sh, p.status);
-      // S of step i + 1 goes out before O of step i, whose weights take longer
-#pragma unroll 1
-      for (int i = -1; i < n && ok; ++i) {
-        if (i + 1 < n) {
-          ok = warp_wait(&sh.ready[(i + 1) & 3], ((i + 1) >> 2) & 1, sh, p.status);
-          if (!ok) break;
-          issue_s(i + 1);
-          if (i + 1 + kRaw < n) copy_step(i + 1 + kRaw);
-        }
-        if (i >= 0) {
-          ok = warp_wait(&sh.p, i & 1, sh, p.status);
-          if (!ok) break;
-          issue_o(i);
-        }
+      for (int i = 0; i < n && ok; ++i) {
+        if (i >= kRaw) ok = warp_wait(&sh.ready[(i - kRaw) & 3], ((i - kRaw) >> 2) & 1, sh, p.status);
+        if (ok) copy_step(i);
       }
-      if (!ok && lane == 0) {
-        // a wait gave up: let what is in flight land (each wait with the same bound); the output is incomplete
+      if (!ok && lane == 0)
         for (int i = copied > kRaw ? copied - kRaw : 0; i < copied; ++i) mbar_wait_bounded(&sh.raw[i % kRaw], (i / kRaw) & 1);
-        for (int i = s_issued > 2 ? s_issued - 2 : 0; i < s_issued; ++i) mbar_wait_bounded(&sh.s[i & 1], (i >> 1) & 1);
-        for (int i = o_issued > 3 ? o_issued - 3 : 0; i < o_issued; ++i) mbar_wait_bounded(&sh.pv[i % 3], (i / 3) & 1);
-      }
       __syncwarp();
     }
   } else if (warp >= kUnpackWarp) {
@@ -381,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
       const int g = lane >> 2, t = lane & 3;
       const uint8_t* tile = smem + S::at_raw + stage * S::raw1 + sub * TB;
       const int pos = (first + i * kSub + sub) * kTile;
-      const bool exists = (sh.valid[i & 7] >> sub) & 1;
+      const bool exists = (sh.valid[i & 7] >> sub) & 1, odd = sh.odd[i & 7] != 0;
       // codes n, less `less`, of the even and the odd places as fp16 numbers
       auto whole = [](uint32_t v, float less) {
         const uint32_t w = (v & 0x000f000fu) | 0x64006400u;              // 1024 + n
@@ -442,8 +448,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
             float sa, ma, sb, mb;
             group_meta<NG>(meta0, c / PG, sa, ma);
             group_meta<NG>(meta1, c / PG, sb, mb);
-            if (sa != sa || ma != ma) sa = ma = 0.f;                       // NaN is put into the rows that see it at the end
-            if (sb != sb || mb != mb) sb = mb = 0.f;
+              if (odd) {                            // NaN is put into the rows that see it at the end
+              if (sa != sa || ma != ma) sa = ma = 0.f;
+              if (sb != sb || mb != mb) sb = mb = 0.f;
+            }
             const __half2 s2 = __floats2half2_rn(sa * f, sb * f), m2 = __floats2half2_rn(ma * f, mb * f);
             const __half2 v[4] = {__hfma2(whole(w[c], 0.f), s2, m2), __hfma2(odd_place(w[c], 0.f), s2, m2),
                                   __hfma2(whole(w[c] >> 8, 0.f), s2, m2), __hfma2(odd_place(w[c] >> 8, 0.f), s2, m2)};
@@ -495,39 +503,46 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
       float ref = kNoRef, l = 0.f;
       uint32_t nan_groups = 0;
       // the row's query, scaled below 2^8 (128 of them sum up within fp16), in the order of the keys' dims
-      const void* src = nullptr;
-      if (real)
-        src = static_cast<const uint16_t*>(p.q) + (sq.q0 + r / p.group) * p.q_token + int64_t(h * p.group + r % p.group) * p.q_head;
-      auto value = [&](int d) {
-        return p.q_f16 ? to_f32(static_cast<const __half*>(src)[d]) : to_f32(static_cast<const __nv_bfloat16*>(src)[d]);
-      };
-      float top = 0.f;
+      uint32_t w[D / 2];                          // two neighbouring dims a word
+#pragma unroll
+      for (int k = 0; k < D / 2; ++k) w[k] = 0u;
       if (real) {
-#pragma unroll 8
-        for (int d = 0; d < D; ++d) top = fmaxf(top, fabsf(value(d)));
+        const uint16_t* src = static_cast<const uint16_t*>(p.q) + (sq.q0 + r / p.group) * p.q_token +
+                              int64_t(h * p.group + r % p.group) * p.q_head;
+        if (p.q_wide) {
+#pragma unroll
+          for (int k = 0; k < D / 8; ++k) {
+            const uint4 v = reinterpret_cast<const uint4*>(src)[k];
+            w[4 * k] = v.x;
+            w[4 * k + 1] = v.y;
+            w[4 * k + 2] = v.z;
+            w[4 * k + 3] = v.w;
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < D / 2; ++k) w[k] = src[2 * k] | uint32_t(src[2 * k + 1]) << 16;
+        }
       }
+      auto two = [&](int k) { return p.q_f16 ? __half22float2(*reinterpret_cast<const __half2*>(&w[k])) : bf16x2_to_float2(w[k]); };
+      float top = 0.f;
+#pragma unroll
+      for (int k = 0; k < D / 2; ++k) top = fmaxf(top, fmaxf(fabsf(two(k).x), fabsf(two(k).y)));
       const int e = 134 - min(max(__float_as_int(top) >> 23, 1), 254), e1 = e >> 1, e2 = e - e1;
       const float f1 = __int_as_float((127 + e1) << 23), f2 = __int_as_float((127 + e2) << 23);
-      float sums[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
-#pragma unroll 1
-      for (int w = 0; w < D / 8; ++w) {
-        uint32_t x[4] = {0u, 0u, 0u, 0u};
-        if (real) {
+      float sums[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            x[j] = pack_f16(value(8 * w + j) * f1 * f2, value(8 * w + 4 + j) * f1 * f2);
-            const float2 held = __half22float2(*reinterpret_cast<const __half2*>(&x[j]));
-            sum += held.x + held.y;
-          }
-        }
-        if ((w + 1) % (D / 8 / NG) == 0) {          // the end of a group
+      for (int k = 0; k < D / 8; ++k) {
+        const float2 v0 = two(4 * k), v1 = two(4 * k + 1), v2 = two(4 * k + 2), v3 = two(4 * k + 3);
+        // dims 0, 4, 1, 5, 2, 6, 3, 7 of eight
+        const uint4 v = make_uint4(pack_f16(v0.x * f1 * f2, v2.x * f1 * f2), pack_f16(v0.y * f1 * f2, v2.y * f1 * f2),
+                                   pack_f16(v1.x * f1 * f2, v3.x * f1 * f2), pack_f16(v1.y * f1 * f2, v3.y * f1 * f2));
+        const uint32_t held[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-          for (int k = 0; k < NG; ++k)
-            if ((w + 1) / (D / 8 / NG) == k + 1) sums[k] = sum;
-          sum = 0.f;
+        for (int j = 0; j < 4; ++j) {
+          const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&held[j]));
+          sums[k / (D / 8 / NG)] += x.x + x.y;
         }
-        *reinterpret_cast<uint4*>(smem + (mt * (D / 64) + (w >> 3)) * S::half + rt * 128 + (((w & 7) ^ (rt & 7)) << 4)) =
-            make_uint4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<uint4*>(smem + (mt * (D / 64) + (k >> 3)) * S::half + rt * 128 + (((k & 7) ^ (rt & 7)) << 4)) = v;
       }
       // against the keys' planes: first planes twice, then what they left over
       float left[4];
@@ -543,9 +558,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
       const int turn_word = ((rt >> 2) & 1) << 4;
       *reinterpret_cast<uint4*>(more + turn_word) = make_uint4(top_planes.x, top_planes.y, top_planes.x, top_planes.y);
       *reinterpret_cast<uint4*>(more + (16 ^ turn_word)) = make_uint4(low_planes.x, low_planes.y, 0u, 0u);
-      l = p.scale2 * __int_as_float((127 - e1) << 23) * __int_as_float((127 - e2) << 23);      // until the first step
-      const float cq = l;
-      l = 0.f;
+      const float cq = p.scale2 * __int_as_float((127 - e1) << 23) * __int_as_float((127 - e2) << 23);
       fence_proxy_async_smem();
       warp_arrive(&sh.q, lane);
       int ev_was = 15;
