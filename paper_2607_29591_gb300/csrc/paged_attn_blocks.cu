@@ -73,6 +73,12 @@ __device__ __forceinline__ void multiply(uint32_t d, uint32_t a, uint32_t b, boo
       "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(kHigh), "r"(kShape),
       "r"(add ? 1 : 0));
 }
+// True in one thread of a converged warp.
+__device__ __forceinline__ bool elected() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e != 0;
+}
 __device__ __forceinline__ void commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
@@ -262,7 +268,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
       auto issue_s = [&](int i) {                 // S of step i
         s_issued = i + 1;
         fence_after();
-        if (lane == 0) {
+        if (elected()) {
           const uint32_t k0 = operand(smem_k + (i & 1) * S::kbuf), km0 = operand(smem_q + S::at_km + (i & 1) * S::k_more);
           const uint32_t d0 = s_cols(i & 1, 0);
 #pragma unroll
@@ -280,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
       auto issue_o = [&](int i) {
         o_issued = i + 1;
         fence_after();
-        if (lane == 0) {
+        if (elected()) {
           const uint32_t v0 = operand(smem_v + (i % 3) * S::vbuf), d0 = o_cols(0);
 #pragma unroll
           for (int m = 0; m < MT; ++m)
