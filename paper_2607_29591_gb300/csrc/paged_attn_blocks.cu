@@ -16,7 +16,7 @@
 //
 //   q             the queries' operands are in shared memory (softmax -> products)
 //   raw[i % 3]    step i's packed tiles have landed        (copy -> unpack)
-//   looked        its largest exponents are known           (unpack's warps)
+//   looked[i & 3] its largest exponents are known           (two warps of their own -> unpack)
 //   ready[i & 3]  its operands are in shared memory         (unpack -> products, softmax)
 //   s[i & 1]      S is in TMEM, K's buffer is free          (products -> softmax, unpack)
 //   p             P is in shared memory, S's buffer is free  (softmax -> products)
@@ -46,8 +46,8 @@ namespace {
 
 constexpr int kPos = 64;                          // positions of a step
 constexpr int kSub = kPos / kTile;                // cache tiles of a step
-constexpr int kThreads = 640;                     // warps 0-7 softmax, 8-15 unpack, 16 products, 17 copies
-constexpr int kUnpackWarp = 8, kIssueWarp = 16, kCopyWarp = 17;
+constexpr int kThreads = 640;                     // warps 0-7 softmax, 8-15 unpack, 16 products, 17 copies, 18-19 exponents
+constexpr int kUnpackWarp = 8, kIssueWarp = 16, kCopyWarp = 17, kLookWarp = 18;
 constexpr int kRaw = 3;                           // steps of packed tiles in flight
 // Registers a thread of each part: (2 x 136 + 2 x 80 + 40) x 128 of the launch's 96 x 640.
 constexpr int kRegsSoftmax = 136, kRegsUnpack = 80, kRegsIssue = 40;
@@ -127,7 +127,7 @@ struct BlockSmem {
 };
 
 struct BlockShared {
-  uint64_t q, raw[kRaw], looked, ready[4], s[2], p, pv[3];
+  uint64_t q, raw[kRaw], looked[4], ready[4], s[2], p, pv[3];
   uint32_t tmem, abort;
   // of step i at i & 7
   uint32_t valid[8];                              // which of its cache tiles exist
@@ -182,8 +182,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
   if (tid == 0) {
     mbar_init(&sh.q, 4 * MT);
     for (int i = 0; i < kRaw; ++i) mbar_init(&sh.raw[i], 1);
-    mbar_init(&sh.looked, 8);
-    for (int i = 0; i < 4; ++i) mbar_init(&sh.ready[i], 8);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&sh.ready[i], 8);
+      mbar_init(&sh.looked[i], 2);
+    }
     mbar_init(&sh.s[0], 1);
     mbar_init(&sh.s[1], 1);
     mbar_init(&sh.p, 4 * MT);
@@ -191,8 +193,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
     sh.abort = 0;
     fence_mbar_init();
   }
-  if (tid < 16) sh.top[tid >> 1][tid & 1] = 0;
-  if (tid < 8) sh.odd[tid] = 0;
   wait_for_previous();
 
   // the item: part of the positions of one block of rows
@@ -257,6 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
   auto s_cols = [&](int buf, int m) { return tmem + uint32_t((buf * MT + m) * kPos); };
   auto o_cols = [&](int m) { return tmem + uint32_t(2 * MT * kPos + m * 128); };
 
+  auto in_block = [&](int pos) { return pos >= from && pos <= hi_last; };
   if (warp >= kIssueWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
     if (warp == kIssueWarp) {
@@ -354,38 +355,49 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
       if (!ok && lane == 0)
         for (int i = copied > kRaw ? copied - kRaw : 0; i < copied; ++i) mbar_wait_bounded(&sh.raw[i % kRaw], (i / kRaw) & 1);
       __syncwarp();
+    } else {
+      // --- a step's largest exponents: two positions' keys (warp 18) or values (19) a lane ---
+      const int which = warp - kLookWarp;
+      bool ok = true;
+#pragma unroll 1
+      for (int i = 0; i < n && ok; ++i) {
+        ok = warp_wait(&sh.raw[i % kRaw], (i / kRaw) & 1, sh, p.status);
+        // its slots were step i - 8's, whose weights are long in P
+        float top = 0.f;
+        uint32_t any_odd = 0;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int tk = lane + 32 * j;
+          uint32_t odd = 0;
+          if (((sh.valid[i & 7] >> (tk / kTile)) & 1) && in_block((first + i * kSub) * kTile + tk)) {
+            const uint8_t* tile = smem + S::at_raw + (i % kRaw) * S::raw1 + (tk / kTile) * TB;
+            uint32_t meta[NG];
+            load_words<NG>(meta, tile + (which ? ts.v_meta() : ts.k_meta()) + (tk % kTile) * 4 * NG);
+#pragma unroll
+            for (int k = 0; k < NG; ++k) {
+              float s, m;
+              group_meta<NG>(meta, k, s, m);
+              if (s != s || m != m) odd |= 1u << k;
+              else top = fmaxf(top, fminf(fmaxf(fabsf(m), fabsf(fmaf(15.f, s, m))), 3.0e38f));
+            }
+          }
+          if (which) sh.odd_groups[i & 7][tk] = uint8_t(odd);
+          any_odd |= odd;
+        }
+        const int e = __reduce_max_sync(0xffffffffu, __float_as_int(top) >> 23);
+        const bool some = __any_sync(0xffffffffu, any_odd != 0);
+        if (lane == 0) {
+          sh.top[i & 7][which] = e;
+          if (which) sh.odd[i & 7] = some;
+        }
+        warp_arrive(&sh.looked[i & 3], lane);
+        // three steps ahead of the unpacking at most, as the copies are
+      }
     }
   } else if (warp >= kUnpackWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsUnpack));
     // --- unpacking: warp w takes K (even) or V (odd) of cache tile w / 2 of a step ---
     const int uw = warp - kUnpackWarp, ut = tid - kUnpackWarp * 32;
-    auto in_block = [&](int pos) { return pos >= from && pos <= hi_last; };
-    // The largest exponents of a step that has landed.
-    auto look = [&](int i) {
-      const int stage = i % kRaw, slot = i & 7;
-      if (ut >= 2 * kPos) return;
-      const int tk = ut & (kPos - 1), which = ut / kPos;
-      const bool held = ((sh.valid[i & 7] >> (tk / kTile)) & 1) && in_block((first + i * kSub) * kTile + tk);
-      float top = 0.f;
-      uint32_t odd = 0;
-      if (held) {
-        const uint8_t* tile = smem + S::at_raw + stage * S::raw1 + (tk / kTile) * TB;
-        const uint16_t* meta = reinterpret_cast<const uint16_t*>(tile + (which ? ts.v_meta() : ts.k_meta())) + (tk % kTile) * 2 * NG;
-#pragma unroll
-        for (int k = 0; k < NG; ++k) {
-          const float s = __uint_as_float(uint32_t(meta[k]) << 16), m = __uint_as_float(uint32_t(meta[NG + k]) << 16);
-          const float big = fmaxf(fabsf(m), fabsf(fmaf(15.f, s, m)));
-          if (s != s || m != m) odd |= 1u << k;
-          else top = fmaxf(top, fminf(big, 3.0e38f));
-        }
-      }
-      if (which) {
-        sh.odd_groups[slot][tk] = uint8_t(odd);
-        if (odd) atomicOr(&sh.odd[slot], 1u);
-      }
-      const int e = __reduce_max_sync(0xffffffffu, __float_as_int(top) >> 23);
-      if (lane == 0) atomicMax(&sh.top[slot][which], e);
-    };
     // Exponents that steps are held at: they only grow.
     int ek = 15, ev = 15;
     auto unpack = [&](int i) {
@@ -406,15 +418,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
       auto bits = [](__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); };
       if ((uw & 1) == 0) {
         const float f = down(ek);
+        uint32_t words[2][C] = {}, metas[2][NG] = {};
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const int row = g + 8 * j, tk = sub * kTile + row;
-          const bool held = exists && in_block(pos + row);
-          uint32_t w[C] = {}, meta[NG] = {};
-          if (held) {
-            load_words<C>(w, tile + row * (D / 2) + t * (D / 8));
-            load_words<NG>(meta, tile + ts.k_meta() + row * 4 * NG);
+          const int row = g + 8 * j;
+          if (exists && in_block(pos + row)) {
+            load_words<C>(words[j], tile + row * (D / 2) + t * (D / 8));
+            load_words<NG>(metas[j], tile + ts.k_meta() + row * 4 * NG);
           }
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int tk = sub * kTile + g + 8 * j;
+          const uint32_t(&w)[C] = words[j];
+          const uint32_t(&meta)[NG] = metas[j];
 #pragma unroll
           for (int c = 0; c < C; ++c) {
             float s, m;
@@ -441,14 +458,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
         }
       } else {
         const float f = down(ev);
+        uint32_t words[2][C] = {}, metas[4][NG] = {};
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const int pair = t + 4 * j, tk = sub * kTile + 2 * pair;
+          const int pair = t + 4 * j;
           const bool held0 = exists && in_block(pos + 2 * pair), held1 = exists && in_block(pos + 2 * pair + 1);
-          uint32_t w[C] = {}, meta0[NG] = {}, meta1[NG] = {};
-          if (held0 || held1) load_words<C>(w, tile + ts.v_codes() + pair * D + ts.v_place(pair, g) * (D / 8));
-          if (held0) load_words<NG>(meta0, tile + ts.v_meta() + 2 * pair * 4 * NG);
-          if (held1) load_words<NG>(meta1, tile + ts.v_meta() + (2 * pair + 1) * 4 * NG);
+          if (held0 || held1) load_words<C>(words[j], tile + ts.v_codes() + pair * D + ts.v_place(pair, g) * (D / 8));
+          if (held0) load_words<NG>(metas[2 * j], tile + ts.v_meta() + 2 * pair * 4 * NG);
+          if (held1) load_words<NG>(metas[2 * j + 1], tile + ts.v_meta() + (2 * pair + 1) * 4 * NG);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int tk = sub * kTile + 2 * (t + 4 * j);
+          const uint32_t(&w)[C] = words[j];
+          const uint32_t(&meta0)[NG] = metas[2 * j];
+          const uint32_t(&meta1)[NG] = metas[2 * j + 1];
 #pragma unroll
           for (int c = 0; c < C; ++c) {
             float sa, ma, sb, mb;
@@ -472,12 +496,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
         }
       }
     };
-    bool ok = warp_wait(&sh.raw[0], 0, sh, p.status);
-    if (ok) look(0);
-    warp_arrive(&sh.looked, lane);
+    bool ok = true;
 #pragma unroll 1
     for (int i = 0; i < n && ok; ++i) {
-      ok = warp_wait(&sh.looked, i & 1, sh, p.status);
+      ok = warp_wait(&sh.raw[i % kRaw], (i / kRaw) & 1, sh, p.status) && warp_wait(&sh.looked[i & 3], (i >> 2) & 1, sh, p.status);
       if (ok && i >= 2) ok = warp_wait(&sh.s[i & 1], ((i - 2) >> 1) & 1, sh, p.status);
       if (ok && i >= 3) ok = warp_wait(&sh.pv[i % 3], ((i - 3) / 3) & 1, sh, p.status);
       if (!ok) break;
@@ -486,18 +508,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
       if (ut == 0) {
         sh.held[i & 7][0] = ek;
         sh.held[i & 7][1] = ev;
-        // of step i - 4, which every warp is done with
-        sh.top[(i + 4) & 7][0] = sh.top[(i + 4) & 7][1] = 0;
-        sh.odd[(i + 4) & 7] = 0;
       }
       unpack(i);
       fence_proxy_async_smem();
       warp_arrive(&sh.ready[i & 3], lane);
-      if (i + 1 < n) {
-        ok = warp_wait(&sh.raw[(i + 1) % kRaw], ((i + 1) / kRaw) & 1, sh, p.status);
-        if (ok) look(i + 1);
-        warp_arrive(&sh.looked, lane);
-      }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
@@ -594,39 +608,45 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
           for (int k = 0; k < kSub; ++k)
             if (!((valid >> k) & 1)) see &= ~(0xffffull << (16 * k));
         }
-        float sum = 0.f;
-        auto weights = [&]() {                      // x: logits -> weights, in place; their sum
-          float2 s2 = make_float2(0.f, 0.f);
-#pragma unroll
-          for (int k = 0; k < kPos; k += 2) {
-            const float2 y = ffma2(make_float2(x[k], x[k + 1]), make_float2(f, f), make_float2(-ref, -ref));
-            float2 w = make_float2(exp2_fast(y.x), exp2_fast(y.y));
-            s2 = fadd2(s2, w);
-            x[k] = w.x;
-            x[k + 1] = w.y;
-          }
-          sum = s2.x + s2.y;
-        };
         const bool masked = __any_sync(0xffffffffu, see != ~0ull);
-        if (masked) {
+        auto mask = [&]() {
+          if (!masked) return;
 #pragma unroll
           for (int k = 0; k < kPos; ++k)
             if (!((see >> k) & 1)) x[k] = -INFINITY;
-        }
-        // Logits are needed again only where the reference moves: find that out from
-        // the largest (of three at a time) rather than from the weights.
-        float top = -INFINITY;
+        };
+        auto weights = [&]() {                    // x: logits -> weights, in place; returns their sum
+          float2 s2[4] = {};
 #pragma unroll
-        for (int k = 0; k < kPos; k += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(x[k]), "f"(x[k + 1]));
-        const float best = top * f;
-        float keep = 1.f;
-        bool moves = best - ref > 14.f;
-        if (moves) {
-          const float now = best - 6.f;
+          for (int k = 0; k < kPos; k += 2) {
+            const float2 y = ffma2(make_float2(x[k], x[k + 1]), make_float2(f, f), make_float2(-ref, -ref));
+            const float2 v = make_float2(exp2_fast(y.x), exp2_fast(y.y));
+            s2[(k / 2) & 3] = fadd2(s2[(k / 2) & 3], v);
+            x[k] = v.x;
+            x[k + 1] = v.y;
+          }
+          const float2 t = fadd2(fadd2(s2[0], s2[1]), fadd2(s2[2], s2[3]));
+          return t.x + t.y;
+        };
+        mask();
+        float sum = weights(), keep = 1.f;
+        // A sum within 2^14 has every weight within fp16.  Otherwise the logits, still in
+        // TMEM, are taken again and the reference goes 6 below the largest.
+        if (__any_sync(0xffffffffu, !(sum <= 16384.f))) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) load16(s_cols(i & 1, mt) + lanes + 16 * k, x + 16 * k);
+          landed();
+#pragma unroll
+          for (int k = 0; k < 4; ++k) defined16(x + 16 * k);
+          mask();
+          float top = -INFINITY;
+#pragma unroll
+          for (int k = 0; k < kPos; k += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(x[k]), "f"(x[k + 1]));
+          const float now = sum <= 16384.f ? ref : fmaxf(ref, top * f - 6.f);
           keep = exp2f(ref - now);
           ref = now;
+          sum = weights();
         }
-        weights();
         l = l * keep + sum;
         if (sh.odd[i & 7]) {                        // NaN values: which groups this row sees
 #pragma unroll 1
