@@ -101,9 +101,8 @@ struct RowCursor {
     tile = int(left - int64_t(h) * k.tiles);
     start = x - tile;
   }
-  // first tile of unit i
-  static __device__ int64_t unit_start(const AttnParams& p, const int64_t* prefix, int64_t i) {
-    if (i >= units_of(prefix[p.batch])) return tiles_of(prefix[p.batch]);
+  // To the beginning of unit i, which exists.
+  __device__ void locate_unit(const AttnParams& p, const int64_t* prefix, int64_t i) {
     int lo = 0, hi = p.batch;
 #pragma unroll 1
     while (hi - lo > 1) {
@@ -111,19 +110,21 @@ struct RowCursor {
       if (units_of(prefix[mid]) <= i) lo = mid;
       else hi = mid;
     }
-    RowCursor c;
-    c.b = lo;
-    c.s = sequence_of(p, lo);
+    b = lo;
+    s = sequence_of(p, lo);
+    tile = 0;
     int left = int(i - units_of(prefix[lo]));
-    int64_t x = tiles_of(prefix[lo]);
+    start = tiles_of(prefix[lo]);
 #pragma unroll 1
-    for (c.r0 = 0;; c.r0 += R) {
-      c.block(p);
-      if (c.k.tiles == 0) continue;               // no unit; the last block is one
-      if (left < p.kv_heads) return x + int64_t(left) * c.k.tiles;
+    for (r0 = 0;; r0 += R) {
+      block(p);
+      if (k.tiles == 0) continue;                 // no unit; the last block is one
+      if (left < p.kv_heads) break;
       left -= p.kv_heads;
-      x += int64_t(c.k.tiles) * p.kv_heads;
+      start += int64_t(k.tiles) * p.kv_heads;
     }
+    h = left;
+    start += int64_t(h) * k.tiles;
   }
   __device__ void next(const AttnParams& p, const int64_t* prefix) {
     start += k.tiles;
@@ -265,13 +266,30 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
   if (whole) ctas = whole_ctas;
   if (cta >= ctas) return;
   int64_t c0, c1;                                 // this CTA's tiles
+  Cursor unit{};                                  // its first unit, or (no tiles) not known
   if (whole) {
-    c0 = Cursor::unit_start(p, prefix, part_begin(cta, units, ctas));
-    c1 = Cursor::unit_start(p, prefix, part_begin(cta + 1, units, ctas));
+    const int u0 = int(part_begin(cta, units, ctas)), u1 = int(part_begin(cta + 1, units, ctas));
+    if (u1 > u0 + 1 && u1 < units) {
+      unit.locate_unit(p, prefix, u1);
+      c1 = unit.start;
+    } else {
+      c1 = N;
+    }
+    unit.locate_unit(p, prefix, u0);
+    c0 = unit.start;
+    if (u1 == u0 + 1) c1 = c0 + unit.k.tiles;
   } else {
     c0 = part_begin(cta, N, ctas);
     c1 = part_begin(cta + 1, N, ctas);
   }
+  auto to_tile = [&](Cursor& c, int64_t x) {      // within the first unit without another search
+    if (x - unit.start < unit.k.tiles && unit.k.tiles > 0) {
+      c = unit;
+      c.tile = int(x - unit.start);
+    } else {
+      c.locate(p, prefix, x);
+    }
+  };
   auto piece = [&](int w) { return c0 + part_begin(w, c1 - c0, kAttnWarps); };
 
   if (warp == kAttnWarps) {
@@ -285,7 +303,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     if (w < kAttnWarps) {
       const int64_t x = piece(w);
       left = int(piece(w + 1) - x);
-      if (left > 0) c.locate(p, prefix, x);
+      if (left > 0) to_tile(c, x);
     }
     uint64_t policy;
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
@@ -375,7 +393,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     int64_t x = piece(warp);
     const int64_t end = piece(warp + 1);
     Cursor c{};
-    if (x < end) c.locate(p, prefix, x);
+    if (x < end) to_tile(c, x);
     TileStep<D, NG, kTwoPlanes, R> st;
     st.init(lane);
     int k = 0;

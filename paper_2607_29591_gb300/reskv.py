@@ -560,6 +560,7 @@ _pack_rotation = struct.Struct("Pqii").pack          # reskv_rotation
 _pack_rows = struct.Struct("Pqqqi4x").pack           # reskv_rows
 _pack_attn = struct.Struct("PqqiiPqqiiPPPqfiPQ").pack  # reskv_paged_attn_args
 _dtypes = {}
+_kinds = []                 # torch.int32, torch.float32, the current stream's address of a device
 _direct = None
 
 
@@ -570,6 +571,7 @@ def _calls():
         import torch
         load_library()
         _dtypes.update({torch.bfloat16: RESKV_BF16, torch.float16: RESKV_F16, torch.float32: RESKV_F32})
+        _kinds.extend((torch.int32, torch.float32, getattr(torch._C, "_cuda_getCurrentRawStream", None)))
         lib = ctypes.CDLL(LIB_PATH)
         vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
         lib.reskv_rope.argtypes = [vp, vp, i64, i32, i32, vp, vp, i32, vp, vp]
@@ -585,9 +587,10 @@ def _calls():
 def _stream_of(stream, t) -> int:
     """Address of the stream, by default torch's current one on the tensor's device."""
     if stream is None:
+        if _kinds[2] is not None:
+            return _kinds[2](t.get_device())
         import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        return raw(t.device.index) if raw else torch.cuda.current_stream(t.device).cuda_stream
+        return torch.cuda.current_stream(t.device).cuda_stream
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -615,8 +618,7 @@ def _ints(t, what: str, n: int) -> int:
     """Address of a contiguous int32 CUDA tensor of n elements."""
     if t.numel() != n:
         raise ValueError(f"{what} must hold {n} elements, got {t.numel()}")
-    import torch
-    if t.dtype is not torch.int32 or not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not _kinds[0] or not t.is_cuda or not t.is_contiguous():
         return _dptr(t, "torch.int32", what).value
     return t.data_ptr()
 
@@ -625,8 +627,7 @@ def _rotation(table, interleaved: bool) -> bytes:
     shape = table.shape
     if len(shape) != 3 or shape[2] != 2:
         raise ValueError(f"table must be [positions, rot_dim / 2, 2], got {tuple(shape)}")
-    import torch
-    if table.dtype is not torch.float32 or not table.is_cuda or not table.is_contiguous():
+    if table.dtype is not _kinds[1] or not table.is_cuda or not table.is_contiguous():
         _dptr(table, "torch.float32", "table")
     return _pack_rotation(table.data_ptr(), shape[0], 2 * shape[1], 1 if interleaved else 0)
 
@@ -705,6 +706,7 @@ class PagedKV:
     def __init__(self, pages, page_table, page_tokens: int, n_kv_heads: int, head_dim: int = 128,
                  quant_group: int = 32, status=None):
         import torch
+        _calls()
         per = n_kv_heads * reskv_paged_head_bytes(page_tokens, head_dim, quant_group)
         if pages.numel() % per or pages.numel() == 0:
             raise ValueError(f"pages must hold a multiple of {per} bytes, got {pages.numel()}")
@@ -821,7 +823,7 @@ def reskv_paged_attn(kv: PagedKV, q, lens, o, q_begin=None, scale: Optional[floa
         need = kv.attn_workspace.get((T, qh[3], oh[4]))
         if need is None:
             need = kv.attn_workspace[T, qh[3], oh[4]] = reskv_paged_attn_workspace(kv, T, qh[3], o.dtype)
-        held = _workspaces.get((q.device.index, s))
+        held = _workspaces.get((q.get_device(), s))
         if held is None or held[-1].numel() < need:
             held = _workspace(q.device, s, need)
         workspace = held[-1]
