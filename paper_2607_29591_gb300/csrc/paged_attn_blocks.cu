@@ -7,7 +7,7 @@
 // operands in shared memory:
 //
 //   S = Q K^T       [128 rows x 64 positions]   tcgen05.mma, per 128 rows, into TMEM
-//   P = 2^(S - ref) one row a thread, fp16 into shared memory
+//   P = 2^(S - ref) one row a thread, fp16 into TMEM (256 rows: shared memory)
 //   O += P V        [128 rows x d]              tcgen05.mma, accumulated in TMEM
 //
 // Four or eight warps take the softmax, a row a thread, eight others unpack up to
@@ -19,7 +19,7 @@
 //   looked[i & 3] its largest exponents are known           (two warps of their own -> unpack)
 //   ready[i & 3]  its operands are in shared memory         (unpack -> products, softmax)
 //   s[i & 1]      S is in TMEM, K's buffer is free          (products -> softmax, unpack)
-//   p             P is in shared memory, S's buffer is free  (softmax -> products)
+//   p             P is in place, S's buffer is free         (softmax -> products)
 //   pv[i % 3]     O holds it, P's and V's buffers are free   (products -> softmax, unpack)
 //
 // No barrier completes a phase again before all that wait for the last one have
@@ -73,6 +73,14 @@ __device__ __forceinline__ void multiply(uint32_t d, uint32_t a, uint32_t b, boo
       "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(kHigh), "r"(kShape),
       "r"(add ? 1 : 0));
 }
+// The same with the first operand in tensor memory: a row a lane, two fp16 a column.
+template <uint32_t kHigh, uint32_t kShape>
+__device__ __forceinline__ void multiply_from(uint32_t d, uint32_t a, uint32_t b, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 db, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(kHigh), "r"(kShape),
+      "r"(add ? 1 : 0));
+}
 // True in one thread of a converged warp.
 __device__ __forceinline__ bool elected() {
   uint32_t e;
@@ -118,9 +126,9 @@ struct BlockSmem {
   static constexpr int half = 128 * 128;          // 128 rows of 64 fp16
   static constexpr int q = MT * (D / 64) * half;
   static constexpr int kbuf = kPos * D * 2, vbuf = kPos * D * 2;
-  static constexpr int p = MT * half;
   static constexpr int raw1 = kSub * TileShape{D, NG}.bytes();
   static constexpr int q_more = 128 * 32, k_more = kPos * 32;         // the step of minima
+  static constexpr int p = MT == 2 ? MT * half : 0;
   static constexpr int at_k = q, at_v = at_k + 2 * kbuf, at_p = at_v + 3 * vbuf, at_qm = at_p + p, at_km = at_qm + MT * q_more,
                        at_raw = at_km + 2 * k_more;
   static constexpr int bytes = at_raw + kRaw * raw1 + 1024;           // operands on 1024 bytes
@@ -172,7 +180,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
   using S = BlockSmem<D, NG, MT>;
   constexpr int kRows = 128 * MT, C = D / 32, PG = C / NG, TB = TileShape{D, NG}.bytes();
   constexpr TileShape ts{D, NG};
-  constexpr uint32_t kColumns = MT == 2 ? 512 : 256;
+  constexpr uint32_t kColumns = 512;
+  constexpr bool kPTensor = MT == 1;              // P in tensor memory, where two blocks leave it no room
   const AttnParams& p = bp.a;
   extern __shared__ uint8_t dynamic[];
   uint8_t* smem = dynamic + ((1024u - (smem_u32(dynamic) & 1023u)) & 1023u);
@@ -253,9 +262,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
   __syncthreads();
   fence_after();
   const uint32_t tmem = sh.tmem;
-  const uint32_t smem_q = smem_u32(smem), smem_k = smem_q + S::at_k, smem_v = smem_q + S::at_v, smem_p = smem_q + S::at_p;
+  const uint32_t smem_q = smem_u32(smem), smem_k = smem_q + S::at_k, smem_v = smem_q + S::at_v;
   auto s_cols = [&](int buf, int m) { return tmem + uint32_t((buf * MT + m) * kPos); };
   auto o_cols = [&](int m) { return tmem + uint32_t(2 * MT * kPos + m * 128); };
+  const uint32_t p_cols = tmem + uint32_t(2 * MT * kPos + MT * 128);
 
   auto in_block = [&](int pos) { return pos >= from && pos <= hi_last; };
   if (warp >= kIssueWarp) {
@@ -265,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
       int s_issued = 0, o_issued = 0;
       // Every product is one instruction of one thread, so the operands' words are
       // worked out here and the loops below have only additions.
-      const uint32_t q0 = operand(smem_q), qm0 = operand(smem_q + S::at_qm), p0 = operand(smem_p);
+      const uint32_t q0 = operand(smem_q), qm0 = operand(smem_q + S::at_qm), p0 = operand(smem_q + S::at_p);
       auto issue_s = [&](int i) {                 // S of step i
         s_issued = i + 1;
         fence_after();
@@ -293,7 +303,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
           for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int k = 0; k < kPos / 16; ++k)
-              multiply<kRows128, shape_of(D)>(d0 + m * 128, p0 + ((m * S::half + k * 32) >> 4), v0 + ((k * 32) >> 4), i > 0 || k > 0);
+              if constexpr (kPTensor)
+                multiply_from<kRows128, shape_of(D)>(d0, p_cols + k * 8, v0 + ((k * 32) >> 4), i > 0 || k > 0);
+              else
+                multiply<kRows128, shape_of(D)>(d0 + m * 128, p0 + ((m * S::half + k * 32) >> 4), v0 + ((k * 32) >> 4), i > 0 || k > 0);
           commit(&sh.pv[i % 3]);
         }
         __syncwarp();
@@ -674,12 +687,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
           }
         }
         ev_was = ev0;
+        if constexpr (kPTensor) {
 #pragma unroll
-        for (int w = 0; w < 8; ++w)
-          *reinterpret_cast<uint4*>(smem + S::at_p + mt * S::half + rt * 128 + ((w ^ (rt & 7)) << 4)) =
-              make_uint4(pack_f16(x[8 * w], x[8 * w + 1]), pack_f16(x[8 * w + 2], x[8 * w + 3]),
-                         pack_f16(x[8 * w + 4], x[8 * w + 5]), pack_f16(x[8 * w + 6], x[8 * w + 7]));
-        fence_proxy_async_smem();
+          for (int k = 0; k < 2; ++k) {
+            float pair[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) pair[j] = __uint_as_float(pack_f16(x[32 * k + 2 * j], x[32 * k + 2 * j + 1]));
+            store16(p_cols + lanes + 16 * k, pair);
+          }
+          stored();
+        } else {
+#pragma unroll
+          for (int w = 0; w < 8; ++w)
+            *reinterpret_cast<uint4*>(smem + S::at_p + mt * S::half + rt * 128 + ((w ^ (rt & 7)) << 4)) =
+                make_uint4(pack_f16(x[8 * w], x[8 * w + 1]), pack_f16(x[8 * w + 2], x[8 * w + 3]),
+                           pack_f16(x[8 * w + 4], x[8 * w + 5]), pack_f16(x[8 * w + 6], x[8 * w + 7]));
+          fence_proxy_async_smem();
+        }
         fence_before();
         warp_arrive(&sh.p, lane);
       }
