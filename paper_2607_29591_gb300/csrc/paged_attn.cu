@@ -616,10 +616,13 @@ cudaError_t dispatch_rows(const AttnParams& p, int d, int group, int dev, int ct
   return launch_rows<64, 1, kTwoPlanes, R>(p, dev, ctas, s);
 }
 
-// Whole blocks of rows (paged_attn_blocks.cu) from kBlockRows rows a sequence on,
+// Whole blocks of rows (paged_attn_blocks.cu) from kBlockRows rows a sequence on: a
+// block costs the same up to 128, eight rows after eight cost more and more.  At 32,
+// 48 and 64 rows, us: one sequence of 32K 42, 57, 69 against 53, 54, 55; 8 of 8K 70, 94,
+// 120 against 100 at all three; one of 1000 15, 16, 17 against 19, 20, 20.  So it is
 // for bf16 outputs; sequences of different query counts keep to the other kernel,
 // whose cut is made on the device.
-constexpr int kBlockRows = 32;
+constexpr int kBlockRows = 48;
 bool takes_blocks(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
   if (a->q_begin || a->o.dtype != RESKV_BF16 || a->scale < 0.f || kv->batch < 1 || kv->n_kv_heads < 1) return false;
   return a->n_tokens / kv->batch * (a->q.n_heads / kv->n_kv_heads) >= kBlockRows;
