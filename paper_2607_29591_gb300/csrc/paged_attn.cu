@@ -233,41 +233,25 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
       sum += __shfl_sync(0xffffffffu, v, 31);
     }
   }
-  if (warp == kAttnWarps) {
-    // meanwhile, zeros where rows see nothing: the blocks of rows that are no unit
-#pragma unroll 1
-    for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
-      const Sequence s = sequence_of(p, b);
-      if (s.len >= s.count) continue;
-      const int64_t rows = int64_t(s.count - s.len) * p.group;
-      const int r1 = s.len == 0 ? int(rows) : int(rows / kRows) * kRows;
-#pragma unroll 1
-      for (int64_t i = lane; i < int64_t(r1) * p.kv_heads * (D / 4); i += 32) {
-        const int u = int(i % (D / 4));
-        const int64_t hr = i / (D / 4);
-        const int h = int(hr / r1), r = int(hr - int64_t(h) * r1);
-        store_out(p, s, h, r, u, make_float4(0.f, 0.f, 0.f, 0.f));
-        if (u == 0) store_lse(p, s, h, r, -INFINITY);
-      }
-    }
-  }
   __syncthreads();
   const int64_t N = tiles_of(prefix[p.batch]);
-  if (N == 0) return;
   int ctas = gridDim.x;
-  if (N < int64_t(ctas) * kAttnWarps * kMinTiles) ctas = (int(N) + kAttnWarps * kMinTiles - 1) / (kAttnWarps * kMinTiles);
+  if (N < int64_t(ctas) * kAttnWarps * kMinTiles) ctas = max(1, (int(N) + kAttnWarps * kMinTiles - 1) / (kAttnWarps * kMinTiles));
   const int cta = blockIdx.x;
   // Whole units to every CTA where that costs it few tiles more than equal pieces:
   // joining records across CTAs takes about the time of kWholeTiles tiles.
   const int units = int(units_of(prefix[p.batch]));
   const int whole_ctas = min(units, int(gridDim.x));
-  const int64_t most = int64_t((units + whole_ctas - 1) / whole_ctas) * shared_int[2];
+  const int64_t most = units ? int64_t((units + whole_ctas - 1) / whole_ctas) * shared_int[2] : 0;
   const bool whole = most <= part_begin(1, N, ctas) + kWholeTiles;
   if (whole) ctas = whole_ctas;
-  if (cta >= ctas) return;
+  const bool active = cta < ctas;
+  if (!active && warp != kAttnWarps) return;      // a CTA without tiles only has rows without any to write
   int64_t c0, c1;                                 // this CTA's tiles
   Cursor unit{};                                  // its first unit, or (no tiles) not known
-  if (whole) {
+  if (!active) {
+    c0 = c1 = 0;
+  } else if (whole) {
     const int u0 = int(part_begin(cta, units, ctas)), u1 = int(part_begin(cta + 1, units, ctas));
     if (u1 > u0 + 1 && u1 < units) {
       unit.locate_unit(p, prefix, u1);
@@ -300,7 +284,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     const int w = lane;
     int left = 0;                                 // tiles to feed
     Cursor c{};
-    if (w < kAttnWarps) {
+    if (active && w < kAttnWarps) {
       const int64_t x = piece(w);
       left = int(piece(w + 1) - x);
       if (left > 0) to_tile(c, x);
@@ -388,6 +372,23 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
         break;
       }
     }
+    // The feeding done, zeros where rows see nothing: the blocks of rows that are no unit.
+#pragma unroll 1
+    for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
+      const Sequence s = sequence_of(p, b);
+      if (s.len >= s.count) continue;
+      const int64_t rows = int64_t(s.count - s.len) * p.group;
+      const int r1 = s.len == 0 ? int(rows) : int(rows / kRows) * kRows;
+#pragma unroll 1
+      for (int64_t i = lane; i < int64_t(r1) * p.kv_heads * (D / 4); i += 32) {
+        const int u = int(i % (D / 4));
+        const int64_t hr = i / (D / 4);
+        const int h = int(hr / r1), r = int(hr - int64_t(h) * r1);
+        store_out(p, s, h, r, u, make_float4(0.f, 0.f, 0.f, 0.f));
+        if (u == 0) store_lse(p, s, h, r, -INFINITY);
+      }
+    }
+    if (!active) return;
   } else {
     // --- a computing warp ---
     int64_t x = piece(warp);
@@ -488,34 +489,51 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
   const uint32_t begins = __ballot_sync(0xffffffffu, present && (!below || before != start));
   if (!begins) return;                            // the same in every warp
   auto cut = [&](const RecordInfo& r) { return r.start < c0 || r.start + r.tiles > c1; };
-  const int row = warp & (kRows - 1);
-  const int u = lane;                             // dims 4u .. 4u + 3
+  // One run: each of its rows to `across` warps, which share its dims.  More: each row
+  // to one warp, runs in turn.  Lane = lanes e + i takes dims 4i .. 4i + 3 of a
+  // warp's share, of every `apart`-th record from e on.
+  constexpr int kAcross = 16 / kRows;
+  const int across = (begins & (begins - 1)) == 0 ? kAcross : 1;
+  const int lanes = D / 4 / across, apart = 32 / lanes, every = lane / lanes;
+  const int row = across == 1 ? warp % kRows : warp / kAcross;
+  const int u = (across == 1 ? 0 : warp % kAcross * lanes) + lane % lanes;               // dims 4u .. 4u + 3
+  auto all_lanes = [&](float4 a, int from) {
+#pragma unroll 1
+    for (int o = from; o < 32; o *= 2) {
+      a.x += __shfl_xor_sync(0xffffffffu, a.x, o);
+      a.y += __shfl_xor_sync(0xffffffffu, a.y, o);
+      a.z += __shfl_xor_sync(0xffffffffu, a.z, o);
+      a.w += __shfl_xor_sync(0xffffffffu, a.w, o);
+    }
+    return a;
+  };
   int turn_of = 0;
 #pragma unroll 1
   for (uint32_t m = begins; m; m &= m - 1, ++turn_of) {
-    if (turn_of % (16 / kRows) != warp / kRows) continue;
+    if (across == 1 && turn_of % kAcross != warp / kRows) continue;
     const int first = __ffs(m) - 1;
     const uint32_t after = m & (m - 1);
-    const uint32_t mine = have & ~((1u << first) - 1) & (after ? (1u << (__ffs(after) - 1)) - 1 : ~0u);
+    const int stop = after ? __ffs(after) - 1 : 32;
     const RecordInfo& ri = info[first];
     if (ri.r0 + row >= ri.s.count * p.group) continue;
-    const float ref = (mine >> lane) & 1 ? refs[lane * kRows + row] : -INFINITY;
-    const Joined j = join_weights(ref);
+    const bool mine = lane >= first && lane < stop && ((have >> lane) & 1);
+    const Joined j = join_weights(mine ? refs[lane * kRows + row] : -INFINITY);
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-    for (uint32_t e = mine; e; e &= e - 1) {
-      const int i = __ffs(e) - 1;
-      const float f = __shfl_sync(0xffffffffu, j.weight, i);
+    for (int e0 = first; e0 < stop; e0 += apart) {
+      const int i = e0 + every;
+      const float f = __shfl_sync(0xffffffffu, j.weight, i & 31);
       const float* rec = (i & 1) ? reinterpret_cast<const float*>(ring + (i >> 1) * kAttnStages * SB) : heads + (i >> 1) * RF;
-      if (u < D / 4 && f != 0.f) add_scaled(a, f, *reinterpret_cast<const float4*>(rec + row * RS + 4 * u));
+      if (i < stop && f != 0.f) add_scaled(a, f, *reinterpret_cast<const float4*>(rec + row * RS + 4 * u));
     }
+    a = all_lanes(a, lanes);
     if (!cut(ri)) {
-      if (u < D / 4) store_out(p, ri.s, ri.h, ri.r0 + row, u, a);
-      if (lane == 0) store_lse(p, ri.s, ri.h, ri.r0 + row, j.ref);
+      if (every == 0) store_out(p, ri.s, ri.h, ri.r0 + row, u, a);
+      if (lane == 0 && u == 0) store_lse(p, ri.s, ri.h, ri.r0 + row, j.ref);
     } else {
       float* rec = p.partials + (cta * 2 + (ri.start >= c0 ? 1 : 0)) * (RF + kRows);
-      if (u < D / 4) *reinterpret_cast<float4*>(rec + row * RS + 4 * u) = a;
-      if (lane == 0) rec[RF + row] = j.ref;
+      if (every == 0) *reinterpret_cast<float4*>(rec + row * RS + 4 * u) = a;
+      if (lane == 0 && u == 0) rec[RF + row] = j.ref;
     }
   }
   // units cut between CTAs: at most the first and the last run
@@ -536,11 +554,13 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     shared_int[threadIdx.x] = last;
   }
   __syncthreads();
+  constexpr int kLanes = D / 4 / kAcross, kEvery = 32 / kLanes;         // a row to kAcross warps
+  const int row2 = warp / kAcross, every2 = lane / kLanes, u2 = warp % kAcross * kLanes + lane % kLanes;
 #pragma unroll 1
   for (int which = 0; which < 2; ++which) {
     if (!shared_int[which]) continue;
     const RecordInfo& ri = info[which ? run_b : run_a];
-    if (warp >= kRows || ri.r0 + row >= ri.s.count * p.group) continue;
+    if (ri.r0 + row2 >= ri.s.count * p.group) continue;
     const int a0 = part_of(ri.start, N, ctas), n = part_of(ri.start + ri.tiles - 1, N, ctas) - a0 + 1;
     // record i of the unit: the CTA it begins in keeps it second, the others first
     auto record = [&](int i) { return p.partials + ((a0 + i) * 2 + (i == 0 ? 1 : 0)) * (RF + kRows); };
@@ -548,17 +568,19 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
     for (int i0 = 0; i0 < n; i0 += 32) {
-      const float ref = i0 + lane < n ? __ldcg(record(i0 + lane) + RF + row) : -INFINITY;
+      const float ref = i0 + lane < n ? __ldcg(record(i0 + lane) + RF + row2) : -INFINITY;
       const Joined j = join_weights(ref);
       float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
       const int stop = min(32, n - i0);
-#pragma unroll 4
-      for (int i = 0; i < stop; ++i) {
-        const float f = __shfl_sync(0xffffffffu, j.weight, i);
-        const float4 v = u < D / 4 ? __ldcg(reinterpret_cast<const float4*>(record(i0 + i) + row * RS + 4 * u))
-                                   : make_float4(0.f, 0.f, 0.f, 0.f);
-        add_scaled(b, f, f != 0.f ? v : make_float4(0.f, 0.f, 0.f, 0.f));
+#pragma unroll 2
+      for (int e0 = 0; e0 < stop; e0 += kEvery) {
+        const int i = e0 + every2;
+        const float f = __shfl_sync(0xffffffffu, j.weight, i & 31);
+        const float4 v = i < stop ? __ldcg(reinterpret_cast<const float4*>(record(i0 + i) + row2 * RS + 4 * u2))
+                                  : make_float4(0.f, 0.f, 0.f, 0.f);
+        add_scaled(b, f, i < stop && f != 0.f ? v : make_float4(0.f, 0.f, 0.f, 0.f));
       }
+      b = all_lanes(b, kLanes);
       if (n <= 32) {
         a = b;
         all = j;
@@ -571,8 +593,8 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
         all = k;
       }
     }
-    if (u < D / 4) store_out(p, ri.s, ri.h, ri.r0 + row, u, a);
-    if (lane == 0) store_lse(p, ri.s, ri.h, ri.r0 + row, all.ref);
+    if (every2 == 0) store_out(p, ri.s, ri.h, ri.r0 + row2, u2, a);
+    if (lane == 0 && u2 == 0) store_lse(p, ri.s, ri.h, ri.r0 + row2, all.ref);
   }
 }
 
