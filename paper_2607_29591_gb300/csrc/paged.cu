@@ -462,120 +462,124 @@ extern "C" reskv_status reskv_paged_append(const reskv_paged_kv* kv, int64_t n_t
                                            const int32_t* positions, const reskv_rotation* rot,
                                            const reskv_heads* k, const reskv_heads* v, const reskv_heads* q,
                                            const reskv_heads* q_out, void* stream) {
-  if (n_tokens == 0) return RESKV_OK;
-  std::string bad = check_paged(kv);
-  if (bad.empty()) bad = check_heads(k, "k");
-  if (bad.empty()) bad = check_heads(v, "v");
-  if (bad.empty() && rot) bad = check_rotation(rot, kv->head_dim);
-  if (bad.empty() && (!seqs || !positions)) bad = "seqs or positions is NULL";
-  if (bad.empty() && (k->n_heads != kv->n_kv_heads || v->n_heads != kv->n_kv_heads))
-    bad = "k and v must have the cache's n_kv_heads";
-  if (bad.empty() && k->dtype != v->dtype) bad = "k and v must have one dtype";
-  if (bad.empty() && (q != nullptr) != (q_out != nullptr)) bad = "q and q_out go together";
-  if (bad.empty() && q && !rot) bad = "q needs a rotation";
-  if (bad.empty() && (n_tokens < 0 || double(n_tokens) * kv->n_kv_heads >= double(int64_t(1) << 31)))
-    bad = "n_tokens must not be negative, n_tokens * n_kv_heads below 2^31";
-  if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
-  AppendParams p{};
-  p.seqs = seqs;
-  p.positions = positions;
-  p.page_table = kv->page_table;
-  p.pages = static_cast<uint8_t*>(kv->pages);
-  p.status = kv->status;
-  p.k = k->data;
-  p.v = v->data;
-  p.k_token = k->token_stride;
-  p.k_head = k->head_stride;
-  p.v_token = v->token_stride;
-  p.v_head = v->head_stride;
-  p.n_pages = kv->n_pages;
-  p.n_tokens = n_tokens;
-  p.batch = kv->batch;
-  p.table_pages = kv->table_pages;
-  p.page_tokens = kv->page_tokens;
-  p.kv_heads = kv->n_kv_heads;
-  if (rot) {
-    p.table = reinterpret_cast<const float2*>(rot->table);
-    p.n_positions = rot->n_positions;
-    p.rot = rot->rot_dim;
-    p.interleaved = rot->interleaved;
-  }
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const bool wide = rows_aligned(*k, 16) && rows_aligned(*v, 16);
-  RopeParams r{};
-  if (q) {
-    // in the same launch where its rows are moved in whole words like the keys', else in one of its own
-    const int v16 = 16 / dtype_size(q->dtype);
-    if (wide && q->dtype == k->dtype && rows_aligned(*q, 16) && rows_aligned(*q_out, 16) && aligned_to(rot->table, 16) &&
-        rot->rot_dim % (2 * v16) == 0) {
-      if (q->n_heads != q_out->n_heads || q->dtype != q_out->dtype)
-        return paged_fail(RESKV_ERR_INVALID_ARG, "q and q_out must have the same heads and one dtype");
-      if (double(n_tokens) * q->n_heads >= double(int64_t(1) << 31))
-        return paged_fail(RESKV_ERR_INVALID_ARG, "n_tokens * heads must be below 2^31");
-      r.t[0] = RopeTensor{q->data, q_out->data, q->token_stride, q->head_stride, q_out->token_stride,
-                          q_out->head_stride, q->n_heads};
-      r.heads = q->n_heads;
-      r.table = p.table;
-      r.positions = positions;
-      r.n_positions = rot->n_positions;
-      r.n_tokens = n_tokens;
-      r.status = kv->status;
-      r.dim = kv->head_dim;
-      r.rot = rot->rot_dim;
-      r.interleaved = rot->interleaved;
-    } else {
-      const reskv_status st = reskv_rope(rot, positions, n_tokens, kv->head_dim, 1, q, q_out, 0, kv->status, stream);
-      if (st != RESKV_OK) return st;
+  return no_throw([&]() -> reskv_status {
+    if (n_tokens == 0) return RESKV_OK;
+    std::string bad = check_paged(kv);
+    if (bad.empty()) bad = check_heads(k, "k");
+    if (bad.empty()) bad = check_heads(v, "v");
+    if (bad.empty() && rot) bad = check_rotation(rot, kv->head_dim);
+    if (bad.empty() && (!seqs || !positions)) bad = "seqs or positions is NULL";
+    if (bad.empty() && (k->n_heads != kv->n_kv_heads || v->n_heads != kv->n_kv_heads))
+      bad = "k and v must have the cache's n_kv_heads";
+    if (bad.empty() && k->dtype != v->dtype) bad = "k and v must have one dtype";
+    if (bad.empty() && (q != nullptr) != (q_out != nullptr)) bad = "q and q_out go together";
+    if (bad.empty() && q && !rot) bad = "q needs a rotation";
+    if (bad.empty() && (n_tokens < 0 || double(n_tokens) * kv->n_kv_heads >= double(int64_t(1) << 31)))
+      bad = "n_tokens must not be negative, n_tokens * n_kv_heads below 2^31";
+    if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
+    AppendParams p{};
+    p.seqs = seqs;
+    p.positions = positions;
+    p.page_table = kv->page_table;
+    p.pages = static_cast<uint8_t*>(kv->pages);
+    p.status = kv->status;
+    p.k = k->data;
+    p.v = v->data;
+    p.k_token = k->token_stride;
+    p.k_head = k->head_stride;
+    p.v_token = v->token_stride;
+    p.v_head = v->head_stride;
+    p.n_pages = kv->n_pages;
+    p.n_tokens = n_tokens;
+    p.batch = kv->batch;
+    p.table_pages = kv->table_pages;
+    p.page_tokens = kv->page_tokens;
+    p.kv_heads = kv->n_kv_heads;
+    if (rot) {
+      p.table = reinterpret_cast<const float2*>(rot->table);
+      p.n_positions = rot->n_positions;
+      p.rot = rot->rot_dim;
+      p.interleaved = rot->interleaved;
     }
-  }
-  const cudaError_t err =
-      k->dtype == RESKV_F32   ? dispatch_append<float>(p, r, kv->head_dim, kv->quant_group, wide, s)
-      : k->dtype == RESKV_F16 ? dispatch_append<__half>(p, r, kv->head_dim, kv->quant_group, wide, s)
-                              : dispatch_append<__nv_bfloat16>(p, r, kv->head_dim, kv->quant_group, wide, s);
-  return launch_result(err, "paged append");
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const bool wide = rows_aligned(*k, 16) && rows_aligned(*v, 16);
+    RopeParams r{};
+    if (q) {
+      // in the same launch where its rows are moved in whole words like the keys', else in one of its own
+      const int v16 = 16 / dtype_size(q->dtype);
+      if (wide && q->dtype == k->dtype && rows_aligned(*q, 16) && rows_aligned(*q_out, 16) && aligned_to(rot->table, 16) &&
+          rot->rot_dim % (2 * v16) == 0) {
+        if (q->n_heads != q_out->n_heads || q->dtype != q_out->dtype)
+          return paged_fail(RESKV_ERR_INVALID_ARG, "q and q_out must have the same heads and one dtype");
+        if (double(n_tokens) * q->n_heads >= double(int64_t(1) << 31))
+          return paged_fail(RESKV_ERR_INVALID_ARG, "n_tokens * heads must be below 2^31");
+        r.t[0] = RopeTensor{q->data, q_out->data, q->token_stride, q->head_stride, q_out->token_stride,
+                            q_out->head_stride, q->n_heads};
+        r.heads = q->n_heads;
+        r.table = p.table;
+        r.positions = positions;
+        r.n_positions = rot->n_positions;
+        r.n_tokens = n_tokens;
+        r.status = kv->status;
+        r.dim = kv->head_dim;
+        r.rot = rot->rot_dim;
+        r.interleaved = rot->interleaved;
+      } else {
+        const reskv_status st = reskv_rope(rot, positions, n_tokens, kv->head_dim, 1, q, q_out, 0, kv->status, stream);
+        if (st != RESKV_OK) return st;
+      }
+    }
+    const cudaError_t err =
+        k->dtype == RESKV_F32   ? dispatch_append<float>(p, r, kv->head_dim, kv->quant_group, wide, s)
+        : k->dtype == RESKV_F16 ? dispatch_append<__half>(p, r, kv->head_dim, kv->quant_group, wide, s)
+                                : dispatch_append<__nv_bfloat16>(p, r, kv->head_dim, kv->quant_group, wide, s);
+    return launch_result(err, "paged append");
+  });
 }
 
 extern "C" reskv_status reskv_paged_gather(const reskv_paged_kv* kv, const int32_t* starts, const int32_t* lens,
                                            int64_t n, const reskv_rows* k, const reskv_rows* v, void* stream) {
-  if (n == 0) return RESKV_OK;
-  std::string bad = check_paged(kv);
-  if (bad.empty() && !lens) bad = "lens is NULL";
-  if (bad.empty() && !k && !v) bad = "k and v are both NULL";
-  if (bad.empty() && k && v && k->dtype != v->dtype) bad = "k and v must have one dtype";
-  GatherParams p{};
-  bool wide = true;
-  const reskv_rows* rows[2] = {k, v};
-  for (int i = 0; i < 2 && bad.empty(); ++i) {
-    const reskv_rows* r = rows[i];
-    if (!r) continue;
-    if (!r->data || !dtype_known(r->dtype)) { bad = "an output is NULL or of an unknown dtype"; break; }
-    const int64_t size = dtype_size(r->dtype);
-    if (!aligned_to(r->data, size)) bad = "outputs must be aligned to their element size";
-    if (r->batch_stride < 0 || r->head_stride < 0 || r->token_stride < 0) bad = "strides must not be negative";
-    wide = wide && aligned_to(r->data, 16) && r->batch_stride * size % 16 == 0 && r->head_stride * size % 16 == 0 &&
-           r->token_stride * size % 16 == 0;
-    p.out[i] = r->data;
-    p.b_stride[i] = r->batch_stride;
-    p.h_stride[i] = r->head_stride;
-    p.t_stride[i] = r->token_stride;
-  }
-  if (bad.empty() && (n < 0 || n >= (int64_t(1) << 31))) bad = "n must be in [0, 2^31)";
-  if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
-  p.starts = starts;
-  p.lens = lens;
-  p.page_table = kv->page_table;
-  p.pages = static_cast<const uint8_t*>(kv->pages);
-  p.status = kv->status;
-  p.n = n;
-  p.n_pages = kv->n_pages;
-  p.table_pages = kv->table_pages;
-  p.page_tokens = kv->page_tokens;
-  p.kv_heads = kv->n_kv_heads;
-  p.batch = kv->batch;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const int32_t dt = k ? k->dtype : v->dtype;
-  const cudaError_t err = dt == RESKV_F32   ? dispatch_gather<float>(p, kv->head_dim, kv->quant_group, wide, s)
-                          : dt == RESKV_F16 ? dispatch_gather<__half>(p, kv->head_dim, kv->quant_group, wide, s)
-                                            : dispatch_gather<__nv_bfloat16>(p, kv->head_dim, kv->quant_group, wide, s);
-  return launch_result(err, "paged gather");
+  return no_throw([&]() -> reskv_status {
+    if (n == 0) return RESKV_OK;
+    std::string bad = check_paged(kv);
+    if (bad.empty() && !lens) bad = "lens is NULL";
+    if (bad.empty() && !k && !v) bad = "k and v are both NULL";
+    if (bad.empty() && k && v && k->dtype != v->dtype) bad = "k and v must have one dtype";
+    GatherParams p{};
+    bool wide = true;
+    const reskv_rows* rows[2] = {k, v};
+    for (int i = 0; i < 2 && bad.empty(); ++i) {
+      const reskv_rows* r = rows[i];
+      if (!r) continue;
+      if (!r->data || !dtype_known(r->dtype)) { bad = "an output is NULL or of an unknown dtype"; break; }
+      const int64_t size = dtype_size(r->dtype);
+      if (!aligned_to(r->data, size)) bad = "outputs must be aligned to their element size";
+      if (r->batch_stride < 0 || r->head_stride < 0 || r->token_stride < 0) bad = "strides must not be negative";
+      wide = wide && aligned_to(r->data, 16) && r->batch_stride * size % 16 == 0 && r->head_stride * size % 16 == 0 &&
+             r->token_stride * size % 16 == 0;
+      p.out[i] = r->data;
+      p.b_stride[i] = r->batch_stride;
+      p.h_stride[i] = r->head_stride;
+      p.t_stride[i] = r->token_stride;
+    }
+    if (bad.empty() && (n < 0 || n >= (int64_t(1) << 31))) bad = "n must be in [0, 2^31)";
+    if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
+    p.starts = starts;
+    p.lens = lens;
+    p.page_table = kv->page_table;
+    p.pages = static_cast<const uint8_t*>(kv->pages);
+    p.status = kv->status;
+    p.n = n;
+    p.n_pages = kv->n_pages;
+    p.table_pages = kv->table_pages;
+    p.page_tokens = kv->page_tokens;
+    p.kv_heads = kv->n_kv_heads;
+    p.batch = kv->batch;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int32_t dt = k ? k->dtype : v->dtype;
+    const cudaError_t err = dt == RESKV_F32   ? dispatch_gather<float>(p, kv->head_dim, kv->quant_group, wide, s)
+                            : dt == RESKV_F16 ? dispatch_gather<__half>(p, kv->head_dim, kv->quant_group, wide, s)
+                                              : dispatch_gather<__nv_bfloat16>(p, kv->head_dim, kv->quant_group, wide, s);
+    return launch_result(err, "paged gather");
+  });
 }

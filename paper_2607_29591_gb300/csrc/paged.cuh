@@ -128,6 +128,17 @@ inline bool rows_aligned(const reskv_heads& t, size_t bytes) {
          t.head_stride * size % int64_t(bytes) == 0;
 }
 
+// An entry point's body: nothing is thrown across the C boundary (what can throw
+// is the text of an error).
+template <typename F>
+reskv_status no_throw(F body) noexcept {
+  try {
+    return body();
+  } catch (...) {
+    return RESKV_ERR_OOM;
+  }
+}
+
 // Host checks shared by the entry points; "" when fine.
 std::string check_heads(const reskv_heads* t, const char* name);
 std::string check_rotation(const reskv_rotation* r, int32_t head_dim);

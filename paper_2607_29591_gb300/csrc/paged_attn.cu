@@ -611,7 +611,7 @@ int sm_count(int dev) {
 }
 
 constexpr int kMaxCtas = 256;                     // of a launch; the workspace holds as many records
-constexpr int kMaxBatch = 1024;                   // the cut is worked out in shared memory
+constexpr int kMaxBatch = 1024;                   // of a launch: the cut is worked out in shared memory
 constexpr size_t kTicketBytes = kMaxCtas * 4;
 
 template <int D, int NG, bool kTwoPlanes, int R>
@@ -667,7 +667,6 @@ std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a)
   if (a->q.n_heads % kv->n_kv_heads || a->q.n_heads / kv->n_kv_heads > 64)
     return "q's heads must be a multiple of n_kv_heads, at most 64 per KV head";
   if (!a->lens) return "lens is NULL";
-  if (kv->batch > kMaxBatch) return "at most 1024 sequences a call";
   if (a->n_tokens < 0 || double(a->n_tokens) * a->q.n_heads >= double(int64_t(1) << 31))
     return "n_tokens must not be negative, n_tokens * heads below 2^31";
   // units: at most one more per sequence than full blocks of rows
@@ -699,55 +698,73 @@ extern "C" size_t reskv_paged_attn_workspace(const reskv_paged_kv* kv, const res
 }
 
 extern "C" reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a, void* stream) {
-  if (a && a->n_tokens == 0) return RESKV_OK;
-  const std::string bad = check_attn(kv, a);
-  if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
-  AttnParams p{};
-  p.q = a->q.data;
-  p.o = a->o.data;
-  p.lse = a->lse;
-  p.q_token = a->q.token_stride;
-  p.q_head = a->q.head_stride;
-  p.o_token = a->o.token_stride;
-  p.o_head = a->o.head_stride;
-  p.q_begin = a->q_begin;
-  p.lens = a->lens;
-  p.page_table = kv->page_table;
-  p.pages = static_cast<const uint8_t*>(kv->pages);
-  p.status = kv->status;
-  p.n_pages = kv->n_pages;
-  p.n_tokens = a->n_tokens;
-  p.batch = kv->batch;
-  p.table_pages = kv->table_pages;
-  p.page_tokens = kv->page_tokens;
-  p.kv_heads = kv->n_kv_heads;
-  p.heads = a->q.n_heads;
-  p.window = a->window;
-  p.o_f32 = a->o.dtype == RESKV_F32;
-  p.scale2 = (a->scale != 0.f ? a->scale : 1.f / std::sqrt(float(kv->head_dim))) * kLog2e;
-  p.group = p.heads / p.kv_heads;
-  p.q_f16 = a->q.dtype == RESKV_F16;
-  p.q_wide = rows_aligned(a->q, 16);
-  p.o_wide = rows_aligned(a->o, size_t(4 * dtype_size(a->o.dtype)));
-  p.tickets = static_cast<int32_t*>(a->workspace);
-  p.partials = reinterpret_cast<float*>(static_cast<char*>(a->workspace) + kTicketBytes);
-  int dev = 0;
-  cudaError_t err = cudaGetDevice(&dev);
-  if (err != cudaSuccess) return launch_result(err, "reading the device");
-  int ctas = sm_count(dev);
-  if (ctas < 1) return launch_result(cudaErrorInvalidDevice, "reading the SM count");
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (takes_blocks(kv, a)) {
-    const BlockPlan plan = block_plan(kv, a, ctas);
-    return launch_result(launch_attn_blocks(p, plan, kv->head_dim, kv->quant_group, dev, p.partials, s), "paged attention");
-  }
-  if (ctas > kMaxCtas) ctas = kMaxCtas;
-  // bf16 outputs: weights in one fp16 plane (2^-11) are finer than the output's 2^-8.
-  // Four rows a unit where a sequence has no more on average.
-  const bool one = a->o.dtype == RESKV_BF16, few = a->n_tokens * p.group <= 4 * int64_t(kv->batch);
-  err = one ? (few ? dispatch_rows<false, 4>(p, kv->head_dim, kv->quant_group, dev, ctas, s)
-                   : dispatch_rows<false, 8>(p, kv->head_dim, kv->quant_group, dev, ctas, s))
-            : (few ? dispatch_rows<true, 4>(p, kv->head_dim, kv->quant_group, dev, ctas, s)
-                   : dispatch_rows<true, 8>(p, kv->head_dim, kv->quant_group, dev, ctas, s));
-  return launch_result(err, "paged attention");
+  return no_throw([&]() -> reskv_status {
+    if (a && a->n_tokens == 0) return RESKV_OK;
+    const std::string bad = check_attn(kv, a);
+    if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
+    AttnParams p{};
+    p.q = a->q.data;
+    p.o = a->o.data;
+    p.lse = a->lse;
+    p.q_token = a->q.token_stride;
+    p.q_head = a->q.head_stride;
+    p.o_token = a->o.token_stride;
+    p.o_head = a->o.head_stride;
+    p.q_begin = a->q_begin;
+    p.lens = a->lens;
+    p.page_table = kv->page_table;
+    p.pages = static_cast<const uint8_t*>(kv->pages);
+    p.status = kv->status;
+    p.n_pages = kv->n_pages;
+    p.n_tokens = a->n_tokens;
+    p.batch = kv->batch;
+    p.table_pages = kv->table_pages;
+    p.page_tokens = kv->page_tokens;
+    p.kv_heads = kv->n_kv_heads;
+    p.heads = a->q.n_heads;
+    p.window = a->window;
+    p.o_f32 = a->o.dtype == RESKV_F32;
+    p.scale2 = (a->scale != 0.f ? a->scale : 1.f / std::sqrt(float(kv->head_dim))) * kLog2e;
+    p.group = p.heads / p.kv_heads;
+    p.q_f16 = a->q.dtype == RESKV_F16;
+    p.q_wide = rows_aligned(a->q, 16);
+    p.o_wide = rows_aligned(a->o, size_t(4 * dtype_size(a->o.dtype)));
+    p.tickets = static_cast<int32_t*>(a->workspace);
+    p.partials = reinterpret_cast<float*>(static_cast<char*>(a->workspace) + kTicketBytes);
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess) return launch_result(err, "reading the device");
+    int ctas = sm_count(dev);
+    if (ctas < 1) return launch_result(cudaErrorInvalidDevice, "reading the SM count");
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (takes_blocks(kv, a)) {
+      const BlockPlan plan = block_plan(kv, a, ctas);
+      return launch_result(launch_attn_blocks(p, plan, kv->head_dim, kv->quant_group, dev, p.partials, s), "paged attention");
+    }
+    if (ctas > kMaxCtas) ctas = kMaxCtas;
+    // bf16 outputs: weights in one fp16 plane (2^-11) are finer than the output's 2^-8.
+    // Four rows a unit where a sequence has no more on average.
+    const bool one = a->o.dtype == RESKV_BF16, few = a->n_tokens * p.group <= 4 * int64_t(kv->batch);
+    const int64_t each = a->n_tokens / kv->batch;    // query tokens a sequence without q_begin
+    for (int b0 = 0; b0 < kv->batch && err == cudaSuccess; b0 += kMaxBatch) {
+      AttnParams l = p;
+      l.batch = kv->batch - b0 < kMaxBatch ? kv->batch - b0 : kMaxBatch;
+      l.lens += b0;
+      l.page_table += int64_t(b0) * p.table_pages;
+      if (p.q_begin) {
+        l.q_begin += b0;
+      } else {
+        const int64_t t0 = b0 * each;
+        l.n_tokens = l.batch * each;
+        l.q = static_cast<const char*>(p.q) + t0 * p.q_token * 2;
+        l.o = static_cast<char*>(p.o) + t0 * p.o_token * dtype_size(a->o.dtype);
+        if (p.lse) l.lse = p.lse + t0 * p.heads;
+      }
+      err = one ? (few ? dispatch_rows<false, 4>(l, kv->head_dim, kv->quant_group, dev, ctas, s)
+                       : dispatch_rows<false, 8>(l, kv->head_dim, kv->quant_group, dev, ctas, s))
+                : (few ? dispatch_rows<true, 4>(l, kv->head_dim, kv->quant_group, dev, ctas, s)
+                       : dispatch_rows<true, 8>(l, kv->head_dim, kv->quant_group, dev, ctas, s));
+    }
+    return launch_result(err, "paged attention");
+  });
 }

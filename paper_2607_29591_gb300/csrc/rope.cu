@@ -110,94 +110,98 @@ extern "C" void reskv_rope_config_default(reskv_rope_config* cfg) {
 
 extern "C" reskv_status reskv_rope_table(const reskv_rope_config* c, int64_t n_positions, float* table,
                                          void* stream) {
-  if (!c || !table) return paged_fail(RESKV_ERR_INVALID_ARG, "NULL argument");
-  if (!aligned_to(table, 8)) return paged_fail(RESKV_ERR_INVALID_ARG, "table must be 8-byte aligned");
-  const int R = c->rot_dim, pairs = R / 2;
-  if (R < 2 || R % 2 || pairs > kMaxPairs)
-    return paged_fail(RESKV_ERR_INVALID_ARG, "rot_dim must be even and in [2, 512]");
-  if (n_positions < 1 || n_positions > (int64_t(1) << 31))
-    return paged_fail(RESKV_ERR_INVALID_ARG, "n_positions must be in [1, 2^31]");
-  if (!(c->base > 1.0) || !std::isfinite(c->base) || !(c->factor >= 1.0) || !std::isfinite(c->factor))
-    return paged_fail(RESKV_ERR_INVALID_ARG, "need base > 1 and factor >= 1");
-  if (!(c->magnitude >= 0.0) || !std::isfinite(c->magnitude))
-    return paged_fail(RESKV_ERR_INVALID_ARG, "magnitude must not be negative");
-  const double two_pi = 6.283185307179586476925;
-  const bool by_turns = c->scaling == RESKV_ROPE_WAVELENGTH, yarn = c->scaling == RESKV_ROPE_YARN;
-  if ((by_turns || yarn) && (!(c->original_positions >= 1.0) || !std::isfinite(c->original_positions)))
-    return paged_fail(RESKV_ERR_INVALID_ARG, "original_positions must be >= 1");
-  if (by_turns && !(c->low_freq > 0.0 && c->high_freq > c->low_freq && std::isfinite(c->high_freq)))
-    return paged_fail(RESKV_ERR_INVALID_ARG, "need 0 < low_freq < high_freq");
-  if (yarn && !(c->beta_slow > 0.0 && c->beta_fast > c->beta_slow && std::isfinite(c->beta_fast)))
-    return paged_fail(RESKV_ERR_INVALID_ARG, "need 0 < beta_slow < beta_fast");
-  if (c->scaling < RESKV_ROPE_NONE || c->scaling > RESKV_ROPE_YARN)
-    return paged_fail(RESKV_ERR_INVALID_ARG, "unknown scaling");
-  if (c->scaling == RESKV_ROPE_BASE && R < 4)
-    return paged_fail(RESKV_ERR_INVALID_ARG, "RESKV_ROPE_BASE needs rot_dim >= 4");
+  return no_throw([&]() -> reskv_status {
+    if (!c || !table) return paged_fail(RESKV_ERR_INVALID_ARG, "NULL argument");
+    if (!aligned_to(table, 8)) return paged_fail(RESKV_ERR_INVALID_ARG, "table must be 8-byte aligned");
+    const int R = c->rot_dim, pairs = R / 2;
+    if (R < 2 || R % 2 || pairs > kMaxPairs)
+      return paged_fail(RESKV_ERR_INVALID_ARG, "rot_dim must be even and in [2, 512]");
+    if (n_positions < 1 || n_positions > (int64_t(1) << 31))
+      return paged_fail(RESKV_ERR_INVALID_ARG, "n_positions must be in [1, 2^31]");
+    if (!(c->base > 1.0) || !std::isfinite(c->base) || !(c->factor >= 1.0) || !std::isfinite(c->factor))
+      return paged_fail(RESKV_ERR_INVALID_ARG, "need base > 1 and factor >= 1");
+    if (!(c->magnitude >= 0.0) || !std::isfinite(c->magnitude))
+      return paged_fail(RESKV_ERR_INVALID_ARG, "magnitude must not be negative");
+    const double two_pi = 6.283185307179586476925;
+    const bool by_turns = c->scaling == RESKV_ROPE_WAVELENGTH, yarn = c->scaling == RESKV_ROPE_YARN;
+    if ((by_turns || yarn) && (!(c->original_positions >= 1.0) || !std::isfinite(c->original_positions)))
+      return paged_fail(RESKV_ERR_INVALID_ARG, "original_positions must be >= 1");
+    if (by_turns && !(c->low_freq > 0.0 && c->high_freq > c->low_freq && std::isfinite(c->high_freq)))
+      return paged_fail(RESKV_ERR_INVALID_ARG, "need 0 < low_freq < high_freq");
+    if (yarn && !(c->beta_slow > 0.0 && c->beta_fast > c->beta_slow && std::isfinite(c->beta_fast)))
+      return paged_fail(RESKV_ERR_INVALID_ARG, "need 0 < beta_slow < beta_fast");
+    if (c->scaling < RESKV_ROPE_NONE || c->scaling > RESKV_ROPE_YARN)
+      return paged_fail(RESKV_ERR_INVALID_ARG, "unknown scaling");
+    if (c->scaling == RESKV_ROPE_BASE && R < 4)
+      return paged_fail(RESKV_ERR_INVALID_ARG, "RESKV_ROPE_BASE needs rot_dim >= 4");
 
-  Frequencies fr{};
-  const double base = c->scaling == RESKV_ROPE_BASE ? c->base * std::pow(c->factor, double(R) / (R - 2)) : c->base;
-  // YARN: the (fractional) pair that makes b turns within the original positions
-  auto pair_of = [&](double b) {
-    return R * std::log(c->original_positions / (b * two_pi)) / (2.0 * std::log(base));
-  };
-  const double first = std::fmax(0.0, std::floor(pair_of(c->beta_fast)));
-  const double last = std::fmax(first + 1e-3, std::fmin(R - 1.0, std::ceil(pair_of(c->beta_slow))));
-  for (int i = 0; i < pairs; ++i) {
-    const double f = std::pow(base, -2.0 * i / R);
-    double w = 0.0;                       // share of the interpolated frequency
-    if (c->scaling == RESKV_ROPE_LINEAR) w = 1.0;
-    if (by_turns)
-      w = (c->high_freq - c->original_positions * f / two_pi) / (c->high_freq - c->low_freq);
-    if (yarn) w = (i - first) / (last - first);
-    w = std::fmin(1.0, std::fmax(0.0, w));
-    fr.f[i] = f * (1.0 - w) + f / c->factor * w;
-  }
-  double m = c->magnitude;
-  if (m == 0.0) m = yarn ? 0.1 * std::log(c->factor) + 1.0 : 1.0;
-  const int64_t n = n_positions * pairs, blocks = (n + 255) / 256;
-  if (blocks > 0x7fffffff) return paged_fail(RESKV_ERR_UNSUPPORTED, "table too large");
-  k_rope_table<<<unsigned(blocks), 256, 0, static_cast<cudaStream_t>(stream)>>>(
-      fr, reinterpret_cast<float2*>(table), n_positions, pairs, m);
-  return launch_result(cudaGetLastError(), "rope table");
+    Frequencies fr{};
+    const double base = c->scaling == RESKV_ROPE_BASE ? c->base * std::pow(c->factor, double(R) / (R - 2)) : c->base;
+    // YARN: the (fractional) pair that makes b turns within the original positions
+    auto pair_of = [&](double b) {
+      return R * std::log(c->original_positions / (b * two_pi)) / (2.0 * std::log(base));
+    };
+    const double first = std::fmax(0.0, std::floor(pair_of(c->beta_fast)));
+    const double last = std::fmax(first + 1e-3, std::fmin(R - 1.0, std::ceil(pair_of(c->beta_slow))));
+    for (int i = 0; i < pairs; ++i) {
+      const double f = std::pow(base, -2.0 * i / R);
+      double w = 0.0;                       // share of the interpolated frequency
+      if (c->scaling == RESKV_ROPE_LINEAR) w = 1.0;
+      if (by_turns)
+        w = (c->high_freq - c->original_positions * f / two_pi) / (c->high_freq - c->low_freq);
+      if (yarn) w = (i - first) / (last - first);
+      w = std::fmin(1.0, std::fmax(0.0, w));
+      fr.f[i] = f * (1.0 - w) + f / c->factor * w;
+    }
+    double m = c->magnitude;
+    if (m == 0.0) m = yarn ? 0.1 * std::log(c->factor) + 1.0 : 1.0;
+    const int64_t n = n_positions * pairs, blocks = (n + 255) / 256;
+    if (blocks > 0x7fffffff) return paged_fail(RESKV_ERR_UNSUPPORTED, "table too large");
+    k_rope_table<<<unsigned(blocks), 256, 0, static_cast<cudaStream_t>(stream)>>>(
+        fr, reinterpret_cast<float2*>(table), n_positions, pairs, m);
+    return launch_result(cudaGetLastError(), "rope table");
+  });
 }
 
 extern "C" reskv_status reskv_rope(const reskv_rotation* rot, const int32_t* positions, int64_t n_tokens,
                                    int32_t head_dim, int32_t n_tensors, const reskv_heads* x,
                                    const reskv_heads* y, int32_t backward, uint32_t* status, void* stream) {
-  if (n_tokens == 0) return RESKV_OK;
-  if (!x || !y || !positions) return paged_fail(RESKV_ERR_INVALID_ARG, "NULL argument");
-  if (n_tensors != 1 && n_tensors != 2) return paged_fail(RESKV_ERR_INVALID_ARG, "n_tensors must be 1 or 2");
-  if (head_dim < 2 || head_dim % 2 || head_dim > 512)
-    return paged_fail(RESKV_ERR_INVALID_ARG, "head_dim must be even and in [2, 512]");
-  std::string bad = check_rotation(rot, head_dim);
-  if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
-  RopeParams p{};
-  bool wide = true;
-  for (int i = 0; i < n_tensors; ++i) {
-    bad = check_heads(&x[i], "x");
-    if (bad.empty()) bad = check_heads(&y[i], "y");
+  return no_throw([&]() -> reskv_status {
+    if (n_tokens == 0) return RESKV_OK;
+    if (!x || !y || !positions) return paged_fail(RESKV_ERR_INVALID_ARG, "NULL argument");
+    if (n_tensors != 1 && n_tensors != 2) return paged_fail(RESKV_ERR_INVALID_ARG, "n_tensors must be 1 or 2");
+    if (head_dim < 2 || head_dim % 2 || head_dim > 512)
+      return paged_fail(RESKV_ERR_INVALID_ARG, "head_dim must be even and in [2, 512]");
+    std::string bad = check_rotation(rot, head_dim);
     if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
-    if (x[i].n_heads != y[i].n_heads || x[i].dtype != y[i].dtype || x[i].dtype != x[0].dtype)
-      return paged_fail(RESKV_ERR_INVALID_ARG, "x and y must have the same heads and one dtype");
-    wide = wide && rows_aligned(x[i], 16) && rows_aligned(y[i], 16) && aligned_to(rot->table, 16);
-    p.t[i] = RopeTensor{x[i].data, y[i].data, x[i].token_stride, x[i].head_stride, y[i].token_stride,
-                        y[i].head_stride, x[i].n_heads};
-    p.heads += x[i].n_heads;
-  }
-  if (n_tokens < 0 || double(n_tokens) * p.heads >= double(int64_t(1) << 31))
-    return paged_fail(RESKV_ERR_INVALID_ARG, "n_tokens must not be negative, n_tokens * heads below 2^31");
-  p.table = reinterpret_cast<const float2*>(rot->table);
-  p.positions = positions;
-  p.n_positions = rot->n_positions;
-  p.n_tokens = n_tokens;
-  p.status = status;
-  p.dim = head_dim;
-  p.rot = rot->rot_dim;
-  p.interleaved = rot->interleaved;
-  p.backward = backward != 0;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t err = x[0].dtype == RESKV_F32   ? dispatch_rope<float>(p, wide, s)
-                          : x[0].dtype == RESKV_F16 ? dispatch_rope<__half>(p, wide, s)
-                                                    : dispatch_rope<__nv_bfloat16>(p, wide, s);
-  return launch_result(err, "rope");
+    RopeParams p{};
+    bool wide = true;
+    for (int i = 0; i < n_tensors; ++i) {
+      bad = check_heads(&x[i], "x");
+      if (bad.empty()) bad = check_heads(&y[i], "y");
+      if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
+      if (x[i].n_heads != y[i].n_heads || x[i].dtype != y[i].dtype || x[i].dtype != x[0].dtype)
+        return paged_fail(RESKV_ERR_INVALID_ARG, "x and y must have the same heads and one dtype");
+      wide = wide && rows_aligned(x[i], 16) && rows_aligned(y[i], 16) && aligned_to(rot->table, 16);
+      p.t[i] = RopeTensor{x[i].data, y[i].data, x[i].token_stride, x[i].head_stride, y[i].token_stride,
+                          y[i].head_stride, x[i].n_heads};
+      p.heads += x[i].n_heads;
+    }
+    if (n_tokens < 0 || double(n_tokens) * p.heads >= double(int64_t(1) << 31))
+      return paged_fail(RESKV_ERR_INVALID_ARG, "n_tokens must not be negative, n_tokens * heads below 2^31");
+    p.table = reinterpret_cast<const float2*>(rot->table);
+    p.positions = positions;
+    p.n_positions = rot->n_positions;
+    p.n_tokens = n_tokens;
+    p.status = status;
+    p.dim = head_dim;
+    p.rot = rot->rot_dim;
+    p.interleaved = rot->interleaved;
+    p.backward = backward != 0;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const cudaError_t err = x[0].dtype == RESKV_F32   ? dispatch_rope<float>(p, wide, s)
+                            : x[0].dtype == RESKV_F16 ? dispatch_rope<__half>(p, wide, s)
+                                                      : dispatch_rope<__nv_bfloat16>(p, wide, s);
+    return launch_result(err, "rope");
+  });
 }

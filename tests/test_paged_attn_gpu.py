@@ -341,3 +341,35 @@ def test_blocks_report_faults():
         skip = [(values[0][0][:, keep], values[0][1][:, keep])]
         check(bad[:20], None, attend_all(skip, q64[:20], [0, 20], 4, 128 ** -0.5, 0), 128, "bf16")
         assert torch.equal(bad[20:], o[20:])
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+def test_more_sequences_than_a_launch_takes(ragged):
+    """2100 sequences: three launches of the few-row kernel, whose outputs equal those of the sequences apart."""
+    B, kv, per, d = 2100, 1, 2, 64
+    rng = np.random.default_rng(40)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    lens = torch.from_numpy(rng.integers(0, 33, B).astype(np.int32)).cuda()
+    pages = R.reskv_paged_pages(2 * B, kv, 16, d, 64)
+    table = torch.randperm(2 * B, generator=g, device="cuda").to(torch.int32).view(B, 2)
+    kvc = R.PagedKV(pages, table, 16, kv, d, 64)
+    k, v = (torch.randn((B * 32, kv, d), generator=g, device="cuda") for _ in range(2))
+    R.reskv_paged_append(kvc, k, v, torch.arange(B, dtype=torch.int32, device="cuda").repeat_interleave(32),
+                         torch.arange(32, dtype=torch.int32, device="cuda").repeat(B))
+    counts = rng.integers(0, 3, B) if ragged else np.ones(B, np.int64)
+    begins = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    q = torch.randn((int(begins[-1]), kv * per, d), generator=g, device="cuda").bfloat16()
+    o, lse = torch.full_like(q, float("nan")), torch.full(q.shape[:2], float("nan"), device="cuda")
+    R.reskv_paged_attn(kvc, q, lens, o, q_begin=torch.from_numpy(begins).cuda() if ragged else None, lse=lse)
+    kvc.check_status()
+    for b in (0, 1, 1023, 1024, 1500, 2047, 2048, 2099):
+        one = R.PagedKV(pages, table[b:b + 1].contiguous(), 16, kv, d, 64)
+        s = slice(int(begins[b]), int(begins[b + 1]))
+        if s.start == s.stop:
+            continue
+        want, ref = torch.empty_like(q[s]), torch.empty_like(lse[s])
+        R.reskv_paged_attn(one, q[s], lens[b:b + 1].contiguous(), want, lse=ref)
+        # the same tiles in the same order or in other pieces: a rounding of the output apart
+        assert ((o[s].float() - want.float()).abs() <= 2.0 ** -7 * want.float().abs() + 1e-3).all()
+        assert torch.allclose(lse[s], ref, atol=1e-3) or (lse[s] == ref).all()
+    assert torch.isfinite(o).all()

@@ -100,6 +100,20 @@ def test_strides_in_place_and_unaligned_rows():
     assert torch.equal(odd_in, qo)
 
 
+def test_table_on_an_eight_byte_boundary():
+    rng = np.random.default_rng(9)
+    tab = po.table(30, po.frequencies(64)).astype(np.float32)
+    held = torch.zeros(tab.size + 2, device="cuda")
+    held[2:] = torch.from_numpy(tab).cuda().flatten()
+    x = torch.from_numpy(rows(rng, (20, 3), 64)).bfloat16().cuda()
+    pos = torch.arange(20, dtype=torch.int32, device="cuda") + 10
+    for inter in (False, True):
+        a, b = torch.empty_like(x), torch.empty_like(x)
+        R.reskv_rope(x, a, pos, held[2:].view(30, 32, 2), interleaved=inter)
+        R.reskv_rope(x, b, pos, torch.from_numpy(tab).cuda(), interleaved=inter)
+        assert torch.equal(a, b)
+
+
 def test_padding_and_positions_outside_the_table():
     rng = np.random.default_rng(2)
     table = torch.from_numpy(po.table(8, po.frequencies(64)).astype(np.float32)).cuda()
