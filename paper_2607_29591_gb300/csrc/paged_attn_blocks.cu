@@ -49,8 +49,8 @@ constexpr int kSub = kPos / kTile;                // cache tiles of a step
 constexpr int kThreads = 640;                     // warps 0-7 softmax, 8-15 unpack, 16 products, 17 copies, 18-19 exponents
 constexpr int kUnpackWarp = 8, kIssueWarp = 16, kCopyWarp = 17, kLookWarp = 18;
 constexpr int kRaw = 3;                           // steps of packed tiles in flight
-// Registers a thread of each part: (2 x 136 + 2 x 80 + 40) x 128 of the launch's 96 x 640.
-constexpr int kRegsSoftmax = 136, kRegsUnpack = 80, kRegsIssue = 40;
+// Registers a thread of each part: (2 x 128 + 2 x 88 + 40) x 128 of the launch's 96 x 640.
+constexpr int kRegsSoftmax = 128, kRegsUnpack = 88, kRegsIssue = 40;
 static_assert((2 * kRegsSoftmax + 2 * kRegsUnpack + kRegsIssue) * 128 <= 96 * kThreads, "registers");
 
 // --- tensor core instructions ---
