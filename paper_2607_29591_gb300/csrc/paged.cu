@@ -60,7 +60,11 @@ __device__ __forceinline__ float mul_01(float a, float b) {        // within [0,
 // A code is rint((x - m) / s), within 0..15, of the correctly rounded quotient.  It is
 // found as rint(15 u), u = (x - m) r within [0, 1], r = 1 / 15 s: 15 u is off by less
 // than 2^-17, so that a value whose fraction lies further than that from one half
-// has its code; where one of the lane's values is nearer, the lane divides.
+// has its code.  Where one of the lane's values is nearer (of 16-bit inputs many are
+// halfway), the lane compares them with t s, t the half next to 15 u: one fma has the
+// sign of x - m - t s.  The quotient itself would say the same: t s has 13 bits, so
+// that x - m, unless it is t s, is further from it than the quotient's rounding
+// reaches.
 template <int kGroup>
 __device__ __forceinline__ void hold(const float2 (&x)[4], uint32_t& codes, uint32_t& sm) {
   float lo = min3_nan(min3_nan(x[0].x, x[0].y, x[1].x), min3_nan(x[1].y, x[2].x, x[2].y), min3_nan(x[3].x, x[3].y, x[3].y));
@@ -82,45 +86,50 @@ __device__ __forceinline__ void hold(const float2 (&x)[4], uint32_t& codes, uint
   } else {
     constexpr float kRound = 12582912.f;          // 1.5 2^23: adding it rounds to whole numbers
     const float r = __frcp_rn(s) * 0.06666667f;
-    // codes 0..3 and 4..7 as 16-bit numbers; scales past 2^120 leave r no digits
+    // codes 0..3 and 4..7 as 16-bit numbers, negated; scales past 2^120 leave r few digits
     float2 sum = make_float2(0.f, 0.f);
     float worst = s > 1.3e36f ? 1.f : 0.f;
     const float2 mm = make_float2(m, m), k15 = make_float2(15.f, 15.f), up = make_float2(kRound, kRound);
+    const float2 k16 = make_float2(16.f, 16.f);
+    auto pair = [&](int i) {                      // values i and 4 + i
+      return i & 1 ? make_float2(x[i / 2].y, x[2 + i / 2].y) : make_float2(x[i / 2].x, x[2 + i / 2].x);
+    };
 #pragma unroll
     for (int i = 3; i >= 0; --i) {
-      // values i and 4 + i
-      const float2 v = i & 1 ? make_float2(x[i / 2].y, x[2 + i / 2].y) : make_float2(x[i / 2].x, x[2 + i / 2].x);
-      const float2 a = fsub2(v, mm);
+      const float2 a = fsub2(pair(i), mm);
       const float2 u = make_float2(mul_01(a.x, r), mul_01(a.y, r));
-      const float2 n = fsub2(ffma2(u, k15, up), up);
-      const float2 d = ffma2(u, k15, make_float2(-n.x, -n.y));
+      const float2 n = fsub2(up, ffma2(u, k15, up));               // -n
+      const float2 d = ffma2(u, k15, n);
       worst = fmaxf(worst, fmaxf(fabsf(d.x), fabsf(d.y)));
-      sum = ffma2(sum, make_float2(16.f, 16.f), n);
+      sum = ffma2(sum, k16, n);
     }
     if (worst > 0.5f - 7.62939453125e-6f) {
       sum = make_float2(0.f, 0.f);
-#pragma unroll 1
-      for (int k = 0; k < 2; ++k) {
-        float y = 0.f;
 #pragma unroll
-        for (int i = 3; i >= 0; --i) {
-          const float2 pair = k ? x[2 + i / 2] : x[i / 2];
-          const float a = __fsub_rn(i & 1 ? pair.y : pair.x, m);
-          y = fmaf(y, 16.f, fminf(fmaxf(rintf(__fdiv_rn(a, s)), 0.f), 15.f));
+      for (int i = 3; i >= 0; --i) {
+        const float2 a = fsub2(pair(i), mm);
+        const float u[2] = {mul_01(a.x, r), mul_01(a.y, r)};
+        float n[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float near = __fsub_rn(fmaf(u[k], 15.f, kRound), kRound);
+          const float t = near + copysignf(0.5f, fmaf(u[k], 15.f, -near));
+          const float over = fmaf(-t, s, k ? a.y : a.x);
+          n[k] = over == 0.f ? rintf(t) : t + copysignf(0.5f, over);
         }
-        if (k) sum.y = y;
-        else sum.x = y;
+        sum = ffma2(sum, k16, make_float2(-n[0], -n[1]));
       }
     }
-    codes = uint32_t(sum.x) | uint32_t(sum.y) << 16;
+    codes = uint32_t(-sum.x) | uint32_t(-sum.y) << 16;
   }
   sm = s16 | (m16 << 16);
 }
 
 // kHeads KV heads of one token per D / 8 lanes: K row, then V row.  The rows' cos and
-// sin are read once.  What a row costs is instructions (about 160 a warp for the
-// two rows it holds of d = 128), then its bytes: see append_prompt's figures at the
-// entry point.
+// sin are read once.  What a row costs is instructions: the rows of 32768 tokens of 8 KV heads
+// of 128 by themselves take 66 us (176 MB, 2.7 TB/s; schedulers 72 % busy).  With their
+// 32 query heads turned beside them (713 MB) it is 151 us, 4.7 TB/s; turns and rows
+// mixed block by block were slower (168 us), as fewer loads were in flight.
 template <typename T, int D, int kGroup, bool kWide, int kHeads>
 __device__ __forceinline__ void append_rows(const AppendParams& p, int64_t r, int lane) {
   constexpr int NG = D / kGroup;
@@ -148,18 +157,23 @@ __device__ __forceinline__ void append_rows(const AppendParams& p, int64_t r, in
     if (fault && lane == 0) report_status(p.status, kStatusBadIndex);
     live = !fault;
   }
-  auto load = [&](const T* at, float2 (&x)[4]) {
+  union Eight {
+    uint4 w[sizeof(T) * 8 / 16];
+    T v[8];
+    __device__ Eight() {}
+  };
+  auto load = [&](const T* at, Eight& u) {
     if constexpr (kWide) {
-      constexpr int words = sizeof(T) * 8 / 16;
-      union { uint4 w[words]; T v[8]; } u;
 #pragma unroll
-      for (int i = 0; i < words; ++i) u.w[i] = reinterpret_cast<const uint4*>(at)[i];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = make_float2(to_f32(u.v[2 * i]), to_f32(u.v[2 * i + 1]));
+      for (int i = 0; i < int(sizeof(u) / 16); ++i) u.w[i] = reinterpret_cast<const uint4*>(at)[i];
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = make_float2(to_f32(at[2 * i]), to_f32(at[2 * i + 1]));
+      for (int i = 0; i < 8; ++i) u.v[i] = at[i];
     }
+  };
+  auto floats = [](const Eight& u, float2 (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = make_float2(to_f32(u.v[2 * i]), to_f32(u.v[2 * i + 1]));
   };
   // The lane's pairs: its eight dims against the eight rot / 2 away, or neighbours.
   // Rotations that cut a lane's dims take them one by one.
@@ -184,21 +198,29 @@ __device__ __forceinline__ void append_rows(const AppendParams& p, int64_t r, in
       }
     }
   }
+  // A head's words are asked for before those of the one before are held.
+  Eight kw, vw, ow;
+  auto ask = [&](int h) {
+    const T* k = static_cast<const T*>(p.k) + tok * p.k_token + h * p.k_head + 8 * lane;
+    load(k, kw);
+    load(static_cast<const T*>(p.v) + tok * p.v_token + h * p.v_head + 8 * lane, vw);
+    if (turns && whole && !p.interleaved) load(k + (lower ? half : -half), ow);
+  };
+  ask(h0);
 #pragma unroll 1
   for (int i = 0; i < kHeads; ++i) {
     const int h = min(h0 + i, p.kv_heads - 1);      // the last head again: the same bytes
     const T* k = static_cast<const T*>(p.k) + tok * p.k_token + h * p.k_head;
-    const T* v = static_cast<const T*>(p.v) + tok * p.v_token + h * p.v_head;
     uint8_t* at = tile + h * head_bytes;
     float2 x[4], y[4], o[4];
-    load(k + 8 * lane, x);
-    load(v + 8 * lane, y);
+    floats(kw, x);
+    floats(vw, y);
     if (turns && whole) {
       if (p.interleaved) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = make_float2(x[j].y, x[j].x);
       } else {
-        load(k + 8 * lane + (lower ? half : -half), o);
+        floats(ow, o);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -223,6 +245,7 @@ __device__ __forceinline__ void append_rows(const AppendParams& p, int64_t r, in
         }
       }
     }
+    if (kHeads > 1 && i + 1 < kHeads) ask(min(h + 1, p.kv_heads - 1));
     uint32_t codes, sm;
     hold<kGroup>(x, codes, sm);
     const bool first = lane % (kGroup / 8) == 0;
@@ -283,8 +306,8 @@ cudaError_t launch_append_rows(AppendParams p, RopeParams q, cudaStream_t s) {
 }
 
 // Eight heads a thread where that leaves every SM a thousand threads (32K tokens of
-// 8 KV and 32 query heads: 156 us, against 163 with four and 213 with one); one
-// where there are fewer rows.
+// 8 KV and 32 query heads: 151 us, against 158 with four); one where there are fewer
+// rows.
 template <typename T, int D, int kGroup>
 cudaError_t dispatch_heads(const AppendParams& p, const RopeParams& q, bool wide, cudaStream_t s) {
   if (!wide) return launch_append_rows<T, D, kGroup, false, 1>(p, q, s);
@@ -341,7 +364,7 @@ __device__ __forceinline__ float2 two_codes(uint32_t w) {
 // One tile per warp, read as its attention reads it (whole 16-byte words), eight
 // dims of K and four of V a lane and word.  s n is exact in fp32, so a value is one
 // fma, rounded once more to the output's type.  Bound by DRAM: 8 prompts of up to
-// 32K positions (1.31 GB read and written) in 200 us, 0.96 of the measured copy
+// 32K positions (1.31 GB read and written) in 194 us, 0.99 of the measured copy
 // rate; one row's eight dims a thread, with seven loads of 2 or 4 bytes, took 338.
 template <typename T, int D, int kGroup, bool kWide>
 __global__ void __launch_bounds__(256) k_paged_gather(const __grid_constant__ GatherParams p) {
