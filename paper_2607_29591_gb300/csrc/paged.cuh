@@ -172,7 +172,8 @@ struct RopeParams {
 // others copy 2V of the remaining dims.
 inline int rope_lanes(int dim, int rot, int v) { return rot / (2 * v) + ((dim - rot) / v + 1) / 2; }
 
-// Heads a thread takes where a call has rows enough.
+// Heads a thread takes where a call has rows enough: 16-bit words come out of more
+// registers, so that four heads would leave fewer threads to an SM.
 template <typename T> constexpr int kManyHeads = sizeof(T) == 2 ? 2 : 4;
 
 // Thread `lane` of row group r: the lane's pairs of kHeads neighbouring heads of one

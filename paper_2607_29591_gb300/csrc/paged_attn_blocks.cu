@@ -34,9 +34,12 @@
 // output types take the kernel of few rows.  Sums, statistics and accumulators are
 // fp32.
 //
-// Bound by the warps' instructions.  With eight warps that did both in turn, between
-// two barriers of the whole block, 512 tokens behind 8K (2 sequences, 8 KV heads, 32
-// query heads, 133 GFLOP) took 357 us.
+// Bound by the warps' instructions (the schedulers issue in 56 % of the cycles, the
+// tensor cores work in 29 %): 512 tokens behind 8K (2 sequences, 8 KV heads, 32 query
+// heads, 133 GFLOP) take 220 us, 605 TFLOP/s.  With eight warps that unpacked and took
+// the softmax in turn, between two barriers of the whole block, it was 357 us; with
+// the roles apart 280; with exponents in warps of their own, and weights formed
+// before a largest logit is looked for, 218.
 #include <atomic>
 
 #include "paged_attn.cuh"
