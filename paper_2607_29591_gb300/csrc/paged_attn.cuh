@@ -541,10 +541,16 @@ struct TileStep {
 };
 
 // --- many rows: paged_attn_blocks.cu ---
-// Blocks of 128 mt rows; each block's positions in `parts`.
+// Units are blocks of 128 mt rows of a KV head and sequence.  The first `whole` are
+// one CTA's work each.  The positions of the others are cut into `even` parts of
+// share / 2^16 of a unit's steps and, where `tail`, a shorter last one.
 struct BlockPlan {
-  int mt, row_blocks, parts;
-  int64_t items;                  // CTAs
+  int mt, row_blocks;
+  int units, whole;
+  int even, tail, share;
+  int items;                      // CTAs: whole units, even parts, last parts
+  __host__ __device__ int parts() const { return even + tail; }
+  __host__ __device__ int64_t slots() const { return parts() > 1 ? int64_t(units - whole) * parts() : 0; }      // records
 };
 BlockPlan plan_attn_blocks(int64_t rows, int batch, int kv_heads, int64_t capacity, int sms);
 size_t attn_blocks_bytes(const BlockPlan& plan, int d);              // of records, where parts are joined

@@ -174,8 +174,8 @@ __device__ __forceinline__ void warp_arrive(uint64_t* bar, int lane) {
 
 struct BlockParams {
   AttnParams a;
-  int32_t row_blocks, parts;
-  float* records;                                 // parts > 1: [item][rows][D], then [item][rows] log2 sums
+  BlockPlan plan;
+  float* records;                                 // [slot][rows][D], then [slot][rows] log2 sums
 };
 
 template <int D, int NG, int MT>
@@ -208,16 +208,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
   wait_for_previous();
 
   // the item: part of the positions of one block of rows
-  const int item = blockIdx.x;
-  const int part = item % bp.parts, unit = item / bp.parts;
-  const int blk = unit % bp.row_blocks, bh = unit / bp.row_blocks;
+  const BlockPlan& plan = bp.plan;
+  const int cut = plan.units - plan.whole, item = int(blockIdx.x) - plan.whole;
+  const bool apart = item >= 0 && plan.parts() > 1;
+  int part = 0, unit = blockIdx.x;
+  if (apart) {
+    const bool last = item >= cut * plan.even;
+    unit = last ? item - cut * plan.even : item / plan.even;
+    part = last ? plan.even : item - unit * plan.even;
+    unit += plan.whole;
+  }
+  const int blk = unit % plan.row_blocks, bh = unit / plan.row_blocks;
   const int b = bh / p.kv_heads, h = bh - b * p.kv_heads;
   const Sequence sq = sequence_of(p, b);
   const int rows = sq.count * p.group, r0 = blk * kRows;
   const RowBlock rb = row_block(p, sq, r0, min(r0 + kRows, rows));
   const int steps_all = (rb.tiles + kSub - 1) / kSub;
-  const int step0 = int(int64_t(steps_all) * part / bp.parts);
-  const int n = int(int64_t(steps_all) * (part + 1) / bp.parts) - step0;
+  const int step0 = apart ? int((int64_t(steps_all) * part * plan.share) >> 16) : 0;
+  const int n = (apart && part + 1 < plan.parts() ? int((int64_t(steps_all) * (part + 1) * plan.share) >> 16) : steps_all) - step0;
   const int first = rb.first + step0 * kSub;      // first cache tile
   const int tiles = min(rb.tiles - step0 * kSub, n * kSub);
   // what the block's rows see
@@ -231,11 +239,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
   const int rt = (warp & 3) * 32 + lane;          // row within its 128
   const int r = r0 + mt * 128 + rt;
   const bool real = warp < 4 * MT && r < rows;
-  float* const record = bp.records + int64_t(item) * kRows * D;
-  float* const record_ref = bp.records + int64_t(gridDim.x) * kRows * D + int64_t(item) * kRows;
+  const int64_t slot = apart ? int64_t(unit - plan.whole) * plan.parts() + part : 0;
+  float* const record = bp.records + slot * kRows * D;
+  float* const record_ref = bp.records + plan.slots() * kRows * D + slot * kRows;
   auto finish_row = [&](int c, const float (&v)[32]) {       // dims 32c .. 32c + 31 of this thread's row
     if (!real) return;
-    if (bp.parts > 1) {
+    if (apart) {
       float* y = record + int64_t(mt * 128 + rt) * D + 32 * c;
 #pragma unroll
       for (int i = 0; i < 8; ++i) reinterpret_cast<float4*>(y)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
@@ -246,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
   };
   auto finish_sum = [&](float sum) {
     if (!real) return;
-    if (bp.parts > 1) record_ref[mt * 128 + rt] = sum;
+    if (apart) record_ref[mt * 128 + rt] = sum;
     else store_lse(p, sq, h, r, sum);
   };
   if (n == 0) {                                   // nothing to see: the same for the whole CTA
@@ -740,27 +749,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
 
 // The parts of a block's positions joined: one row per warp.
 template <int D, int MT>
-__global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ BlockParams bp, int items) {
+__global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ BlockParams bp) {
   constexpr int kRows = 128 * MT;
   const AttnParams& p = bp.a;
   wait_for_previous();
   const int64_t w = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
-  const int unit = int(w / kRows), row = int(w - int64_t(unit) * kRows);
-  const int blk = unit % bp.row_blocks, bh = unit / bp.row_blocks;
+  const int cut = int(w / kRows), row = int(w - int64_t(cut) * kRows);
+  const int parts = bp.plan.parts(), unit = bp.plan.whole + cut;
+  const int blk = unit % bp.plan.row_blocks, bh = unit / bp.plan.row_blocks;
   const int b = bh / p.kv_heads, h = bh - b * p.kv_heads;
   if (b >= p.batch) return;
   const Sequence sq = sequence_of(p, b);
   const int r = blk * kRows + row;
   if (r >= sq.count * p.group) return;
-  const float* refs = bp.records + int64_t(items) * kRows * D;
-  const float ref = lane < bp.parts ? refs[(int64_t(unit) * bp.parts + lane) * kRows + row] : -INFINITY;
+  const int64_t slot = int64_t(cut) * parts;
+  const float* refs = bp.records + bp.plan.slots() * kRows * D;
+  const float ref = lane < parts ? refs[(slot + lane) * kRows + row] : -INFINITY;
   const Joined j = join_weights(ref);
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int k = 0; k < bp.parts; ++k) {
+  for (int k = 0; k < parts; ++k) {
     const float f = __shfl_sync(0xffffffffu, j.weight, k);
-    const float4 v = lane < D / 4 ? reinterpret_cast<const float4*>(bp.records + ((int64_t(unit) * bp.parts + k) * kRows + row) * D)[lane]
+    const float4 v = lane < D / 4 ? reinterpret_cast<const float4*>(bp.records + ((slot + k) * kRows + row) * D)[lane]
                                   : make_float4(0.f, 0.f, 0.f, 0.f);
     add_scaled(a, f, f != 0.f ? v : make_float4(0.f, 0.f, 0.f, 0.f));
   }
@@ -769,7 +780,7 @@ __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ Block
 }
 
 template <int D, int NG, int MT>
-cudaError_t launch(const BlockParams& bp, int dev, int items, cudaStream_t s) {
+cudaError_t launch(const BlockParams& bp, int dev, cudaStream_t s) {
   // the kernel's shared memory limit, raised once a device
   static std::atomic<uint64_t> raised{0};
   const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
@@ -779,21 +790,21 @@ cudaError_t launch(const BlockParams& bp, int dev, int items, cudaStream_t s) {
     if (err != cudaSuccess) return err;
     raised.fetch_or(bit, std::memory_order_relaxed);
   }
-  cudaError_t err = launch_early(k_attn_blocks<D, NG, MT>, items, kThreads, BlockSmem<D, NG, MT>::bytes, s, bp);
-  if (err == cudaSuccess && bp.parts > 1) {
-    const int64_t rows = int64_t(items / bp.parts) * 128 * MT;
-    err = launch_early(k_attn_join<D, MT>, unsigned((rows + 7) / 8), 256, 0, s, bp, items);
+  cudaError_t err = launch_early(k_attn_blocks<D, NG, MT>, bp.plan.items, kThreads, BlockSmem<D, NG, MT>::bytes, s, bp);
+  if (err == cudaSuccess && bp.plan.slots() > 0) {
+    const int64_t rows = int64_t(bp.plan.units - bp.plan.whole) * 128 * MT;
+    err = launch_early(k_attn_join<D, MT>, unsigned((rows + 7) / 8), 256, 0, s, bp);
   }
   return err;
 }
 
 template <int MT>
-cudaError_t dispatch(const BlockParams& bp, int d, int group, int dev, int items, cudaStream_t s) {
-  if (d == 128 && group == 32) return launch<128, 4, MT>(bp, dev, items, s);
-  if (d == 128 && group == 64) return launch<128, 2, MT>(bp, dev, items, s);
-  if (d == 128) return launch<128, 1, MT>(bp, dev, items, s);
-  if (group == 32) return launch<64, 2, MT>(bp, dev, items, s);
-  return launch<64, 1, MT>(bp, dev, items, s);
+cudaError_t dispatch(const BlockParams& bp, int d, int group, int dev, cudaStream_t s) {
+  if (d == 128 && group == 32) return launch<128, 4, MT>(bp, dev, s);
+  if (d == 128 && group == 64) return launch<128, 2, MT>(bp, dev, s);
+  if (d == 128) return launch<128, 1, MT>(bp, dev, s);
+  if (group == 32) return launch<64, 2, MT>(bp, dev, s);
+  return launch<64, 1, MT>(bp, dev, s);
 }
 
 }  // namespace
@@ -803,29 +814,49 @@ BlockPlan plan_attn_blocks(int64_t rows, int batch, int kv_heads, int64_t capaci
   plan.mt = rows > 128 ? 2 : 1;
   const int64_t block = 128 * plan.mt;
   plan.row_blocks = int((rows + block - 1) / block);
-  const int64_t units = int64_t(batch) * kv_heads * plan.row_blocks;
-  // the positions of fewer blocks than SMs in parts, of 512 positions at least
-  int64_t parts = units < sms ? sms / units : 1;
-  if (parts > capacity / 512) parts = capacity / 512;
-  if (parts > 32) parts = 32;
-  plan.parts = int(parts < 1 ? 1 : parts);
-  plan.items = units * plan.parts;
+  plan.units = batch * kv_heads * plan.row_blocks;             // below 2^24
+  // An SM takes one CTA at a time, in the order of their numbers.  Units that do not
+  // fill the SMs once more are cut into parts that do, of 512 positions at least.
+  // SMs still left over then take one short part of each, `turns` of those in the time
+  // of a longer one; what a CTA does before its first step and after its last takes as
+  // long as twelve (18 us).  Against cutting only what leaves SMs idle from the start,
+  // into equal parts: 16 tokens behind 8K of 20 sequences (160 units) 312 -> 196 us,
+  // 512 behind 128K of one (64 units) 1614 -> 1410.
+  const int cut = plan.units % sms;
+  plan.whole = plan.units - cut;
+  const int64_t most = capacity / 512 < 32 ? capacity / 512 : 32;
+  int64_t even = cut ? sms / cut : 1;
+  if (even > most) even = most;
+  plan.even = int(even < 1 ? 1 : even);
+  plan.share = 65536 / plan.even;
+  const int left = cut ? sms - cut * plan.even : 0;
+  if (left > 0 && plan.even < 32) {
+    const int turns = (cut + left - 1) / left;
+    const double fixed = 12.0 * kPos / double(capacity);
+    const double tail = (1.0 - plan.even * (turns - 1) * fixed) / (1.0 + turns * plan.even);
+    // below 1024 positions records and their joining cost what is gained (512 tokens
+    // behind 8K of two sequences, 128 units: 226 us cut, 216 whole)
+    if (tail * double(capacity) >= 1024.0) {
+      plan.tail = 1;
+      plan.share = int(65536.0 * (1.0 - tail) / plan.even);
+    }
+  }
+  if (plan.parts() == 1) plan.whole = plan.units;
+  plan.items = plan.whole + (plan.units - plan.whole) * plan.parts();
   return plan;
 }
 
 size_t attn_blocks_bytes(const BlockPlan& plan, int d) {
-  return plan.parts > 1 ? size_t(plan.items) * 128 * plan.mt * (d + 1) * 4 : 0;
+  return size_t(plan.slots()) * 128 * plan.mt * (d + 1) * 4;
 }
 
 cudaError_t launch_attn_blocks(const AttnParams& p, const BlockPlan& plan, int d, int quant_group, int dev, float* records,
                                cudaStream_t s) {
   BlockParams bp{};
   bp.a = p;
-  bp.row_blocks = plan.row_blocks;
-  bp.parts = plan.parts;
+  bp.plan = plan;
   bp.records = records;
-  return plan.mt == 2 ? dispatch<2>(bp, d, quant_group, dev, int(plan.items), s)
-                      : dispatch<1>(bp, d, quant_group, dev, int(plan.items), s);
+  return plan.mt == 2 ? dispatch<2>(bp, d, quant_group, dev, s) : dispatch<1>(bp, d, quant_group, dev, s);
 }
 
 }  // namespace reskv

@@ -373,3 +373,42 @@ def test_more_sequences_than_a_launch_takes(ragged):
         assert ((o[s].float() - want.float()).abs() <= 2.0 ** -7 * want.float().abs() + 1e-3).all()
         assert torch.allclose(lse[s], ref, atol=1e-3) or (lse[s] == ref).all()
     assert torch.isfinite(o).all()
+
+
+@pytest.mark.parametrize("B,kv,new,length,window", [
+    (12, 8, 16, 5000, 0),          # a part and a shorter one
+    (2, 8, 260, 5000, 0),          # the same of 256 rows
+    (31, 8, 16, 5000, 0),          # units of one CTA, and some in two parts
+    (20, 8, 16, 2100, 0),          # units of one CTA, and some in four equal parts
+    (31, 8, 16, 5000, 300),        # parts that see nothing
+])
+def test_blocks_in_parts_of_two_lengths(B, kv, new, length, window):
+    """More units than the oracle takes: against the few-row kernel's fp32 output (query counts given), whose own
+    share of the tolerance is added."""
+    d, per, page = 128, 4, 64
+    g = torch.Generator(device="cuda").manual_seed(B + new)
+    n_pages = (length + page - 1) // page
+    pages = R.reskv_paged_pages(B * n_pages, kv, page, d, 32)
+    table = torch.randperm(B * n_pages, generator=g, device="cuda").to(torch.int32).view(B, n_pages)
+    kvc = R.PagedKV(pages, table, page, kv, d, 32)
+    for b in range(B):
+        k, v = (torch.randn((length, kv, d), generator=g, device="cuda") for _ in range(2))
+        R.reskv_paged_append(kvc, k, v, torch.full((length,), b, dtype=torch.int32, device="cuda"),
+                             torch.arange(length, dtype=torch.int32, device="cuda"))
+    lens = torch.tensor([max(new, length - 97 * b) for b in range(B)], dtype=torch.int32, device="cuda")
+    q = torch.randn((B * new, kv * per, d), generator=g, device="cuda").bfloat16()
+    o, lse = torch.full_like(q, float("nan")), torch.full(q.shape[:2], float("nan"), device="cuda")
+    R.reskv_paged_attn(kvc, q, lens, o, lse=lse, window=window)
+    ref, ref_lse = torch.empty(q.shape, device="cuda"), torch.empty_like(lse)
+    begins = (torch.arange(B + 1, device="cuda") * new).to(torch.int32)
+    R.reskv_paged_attn(kvc, q, lens, ref, q_begin=begins, lse=ref_lse, window=window)
+    kvc.check_status()
+    kk, vv = (torch.empty((B, kv, length, d), device="cuda") for _ in range(2))
+    R.reskv_paged_gather(kvc, lens, kk, vv)
+    x = d ** -0.5 * (q.float().view(B, new, kv, per, d).abs().amax((1, 3, 4)) * kk.abs().sum(-1).amax(-1)).max().item()
+    tol = 2 * (2 * d * 2.0 ** -23 * x + 2.0 ** -11 + 2.0 ** -16) * vv.abs().max().item() + HALF_ULP["bf16"] * ref.abs() * 1.01 + 1e-7
+    assert ((o.float() - ref).abs() <= tol).all()
+    assert ((lse - ref_lse).abs() <= 2 * (d * 2.0 ** -23 * x + 2.0 ** -12 + 2.0 ** -22 * ref_lse.abs())).all()
+    again = torch.empty_like(o)
+    R.reskv_paged_attn(kvc, q, lens, again, window=window)
+    assert torch.equal(o, again)
