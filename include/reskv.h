@@ -646,6 +646,19 @@ reskv_status reskv_paged_gather(const reskv_paged_kv* kv, const int32_t* starts,
  *   o = sum_t softmax_t(scale <q, k_t>) v_t
  * over the held values k_t, v_t.  A query that sees nothing (p < 0) gets o = 0.
  * Sums and softmax statistics in fp32.
+ *
+ * A fault is a lens[b] outside [0, table_pages * page_tokens], taken as the nearest,
+ * or a page outside the pages, whose tokens nobody sees; q_begin outside
+ * [0, n_tokens] is taken as the nearest.  NaN held at a position reaches the queries
+ * that see it and no others.  Limits: n_tokens * heads below 2^31, n_tokens *
+ * heads / 4 + batch * n_kv_heads below 2^24; scales s of held values at most 2^96.
+ *
+ * Roundings: logits are sums of exact products.  The softmax weights are rounded to
+ * 11 bits where o is bf16 (22 otherwise), and the held values also to 11 bits where
+ * o is bf16, q_begin NULL and a sequence has 48 query rows (its query tokens times
+ * heads / n_kv_heads) or more, which the tensor cores then take 128 at a time.
+ * The result depends on the split of the work, which depends on batch, n_tokens,
+ * lens and the device, but not on the order in which blocks run.
  */
 typedef struct reskv_paged_attn_args {
   reskv_heads q;                       /* [n_tokens, heads, d] bf16 or fp16; heads a
@@ -668,8 +681,9 @@ typedef struct reskv_paged_attn_args {
   size_t workspace_bytes;              /* at least reskv_paged_attn_workspace() */
 } reskv_paged_attn_args;
 
-/* Workspace bytes of a call; depends on the head shape, batch and n_tokens (an
- * upper bound over fewer), not on the lengths. */
+/* Workspace bytes of a call; depends on the head shape, batch, n_tokens, o's type,
+ * q_begin being NULL and the page table's width, not on the lengths.  After a wait
+ * that gave up (code 1 in the status word) zero the workspace again. */
 size_t reskv_paged_attn_workspace(const reskv_paged_kv* kv, const reskv_paged_attn_args* args);
 
 reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* args,

@@ -731,6 +731,8 @@ class PagedKV:
         word = int(self.status.item())
         if word:
             self.status.zero_()
+            if word & 1:
+                _workspaces.clear()              # what such a call leaves is not ready for the next
             raise ReskvError(RESKV_ERR_DEVICE_STATUS, f"paged cache status word {word} (1 = bounded wait "
                                                       "timed out, 2 = index out of range)")
 

@@ -412,3 +412,32 @@ def test_blocks_in_parts_of_two_lengths(B, kv, new, length, window):
     again = torch.empty_like(o)
     R.reskv_paged_attn(kvc, q, lens, again, window=window)
     assert torch.equal(o, again)
+
+
+def test_offsets_beyond_32_bits():
+    """A cache of 5 GB whose last pages are used, against the same tokens in one of a few pages."""
+    d, kv, per, page, n = 128, 8, 4, 64, 200
+    g = torch.Generator(device="cuda").manual_seed(2)
+    used = (n + page - 1) // page
+    page_bytes = R.reskv_paged_pages(1, kv, page, d, 32).numel()
+    n_pages = (5 << 30) // page_bytes
+    far = torch.empty((n_pages, page_bytes), dtype=torch.uint8, device="cuda")
+    table = (n_pages - 1 - torch.arange(used, device="cuda", dtype=torch.int32))[None].contiguous()
+    big = R.PagedKV(far, table, page, kv, d, 32)
+    small = R.PagedKV(R.reskv_paged_pages(used, kv, page, d, 32), torch.arange(used, device="cuda", dtype=torch.int32)[None],
+                      page, kv, d, 32)
+    k, v = (torch.randn((n, kv, d), generator=g, device="cuda").bfloat16() for _ in range(2))
+    seqs, pos = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.arange(n, dtype=torch.int32, device="cuda")
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    outs = []
+    for kvc in (big, small):
+        R.reskv_paged_append(kvc, k, v, seqs, pos)
+        kk, vv = (torch.empty((1, kv, n, d), device="cuda") for _ in range(2))
+        R.reskv_paged_gather(kvc, lens, kk, vv)
+        outs.append([kk, vv])
+        for new in (1, 20):                             # the kernel of few rows, that of many
+            q = torch.randn((new, kv * per, d), generator=torch.Generator(device="cuda").manual_seed(new), device="cuda").bfloat16()
+            outs[-1].append(torch.empty_like(q))
+            R.reskv_paged_attn(kvc, q, lens, outs[-1][-1])
+        kvc.check_status()
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
