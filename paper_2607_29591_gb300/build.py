@@ -1,15 +1,18 @@
 """Compile the CUDA library in-tree for sm_103a (nvcc, no cmake).
 
 ``build()`` compiles every translation unit of ``csrc/`` in parallel and links
-``libreskv.so`` beside this file.  Objects go to ``_build/``.  Both are
-git-ignored build products.
+``libreskv.so`` beside this file, and ``_bind.so``, the small calls' way to it from
+torch tensors (host C++).  Objects go to ``_build/``.  All are git-ignored build
+products.
 """
 from __future__ import annotations
 
 import concurrent.futures
+import importlib.util
 import os
 import shutil
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -19,6 +22,7 @@ LIB = os.path.join(HERE, "libreskv.so")
 SOURCES = ["reskv_api.cu", "decode_kernel.cu", "decode_mma.cu", "decode_cluster.cu",
            "construct.cu", "decode_noalloc.cu", "append.cu", "rope.cu", "paged.cu", "paged_attn.cu",
            "paged_attn_blocks.cu"]
+BIND = os.path.join(HERE, "_bind.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I" + INCLUDE,
                 "-I" + CSRC]
@@ -56,14 +60,32 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
+def _bind(force: bool) -> None:
+    src = os.path.join(CSRC, "bind.cpp")
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    if not force and not _stale(BIND, [src, os.path.join(INCLUDE, "reskv.h"), os.path.join(torch, "version.py")]):
+        return
+    lib = os.path.join(torch, "lib")
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I" + INCLUDE, "-I" + os.path.join(torch, "include"),
+           "-I" + os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+           "-I" + sysconfig.get_paths()["include"], src, "-o", BIND + ".new", "-L" + lib, "-ltorch_python",
+           "-ltorch_cpu", "-lc10", "-Wl,-rpath," + lib]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"g++ failed on bind.cpp:\n{res.stderr}")
+    os.replace(BIND + ".new", BIND)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     """Build libreskv.so if any source changed; return its path."""
     os.makedirs(BUILD_DIR, exist_ok=True)
     if force:
         for f in os.listdir(BUILD_DIR):
             os.remove(os.path.join(BUILD_DIR, f))
-    with concurrent.futures.ThreadPoolExecutor(len(SOURCES)) as ex:
+    with concurrent.futures.ThreadPoolExecutor(len(SOURCES) + 1) as ex:
+        bind = ex.submit(_bind, force)
         objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
+        bind.result()
     if force or _stale(LIB, objs):
         cmd = [nvcc()] + ARCH + ["-shared", "-o", LIB] + objs
         res = subprocess.run(cmd, capture_output=True, text=True)

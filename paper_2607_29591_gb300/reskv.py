@@ -562,11 +562,12 @@ _pack_attn = struct.Struct("PqqiiPqqiiPPPqfiPQ").pack  # reskv_paged_attn_args
 _dtypes = {}
 _kinds = []                 # torch.int32, torch.float32, the current stream's address of a device
 _direct = None
+_bind = None                # the same calls from plain CUDA tensors, without Python in between
 
 
 def _calls():
     """The paged calls with every struct passed as an address or packed bytes."""
-    global _direct
+    global _direct, _bind
     if _direct is None:
         import torch
         load_library()
@@ -580,6 +581,14 @@ def _calls():
         lib.reskv_paged_attn.argtypes = [vp, vp, vp]
         for f in (lib.reskv_rope, lib.reskv_paged_append, lib.reskv_paged_gather, lib.reskv_paged_attn):
             f.restype = i32
+        if not os.path.exists(os.path.join(os.path.dirname(LIB_PATH), "_bind.so")):
+            raise RuntimeError("_bind.so is missing: build it with `python -m paper_2607_29591_gb300.build` "
+                               "(there is no fallback)")
+        from . import _bind as bind
+        if _kinds[2] is not None:
+            bind.setup(*(ctypes.cast(f, ctypes.c_void_p).value for f in
+                         (lib.reskv_rope, lib.reskv_paged_append, lib.reskv_paged_gather)), _kinds[2])
+            _bind = bind
         _direct = lib
     return _direct
 
@@ -662,6 +671,10 @@ def reskv_rope(q, q_out, positions, table, k=None, k_out=None, interleaved: bool
     (reskv_rope_table); rot_dim < d rotates a part of every head.  status: int32
     [1] that a position outside the table sets to 2.
     """
+    if _bind is not None:
+        st = _bind.rope(q, q_out, positions, table, k, k_out, interleaved, backward, status, stream)
+        if st >= 0:
+            return _check(st) if st else None
     if (k is None) != (k_out is None):
         raise ValueError("k and k_out go together")
     if q.dim() != 3:
@@ -746,6 +759,10 @@ def reskv_paged_append(kv: PagedKV, k, v, seqs, positions, table=None, interleav
     k, v: [T, n_kv_heads, d], one of bf16, f16, f32; seqs, positions: int32 [T],
     negative positions mark padding; q, q_out: [T, heads, d].
     """
+    if _bind is not None:
+        st = _bind.append(kv.address, k, v, seqs, positions, table, interleaved, q, q_out, stream)
+        if st >= 0:
+            return _check(st) if st else None
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
     lib = _calls()
@@ -777,6 +794,10 @@ def reskv_paged_gather(kv: PagedKV, lens, k_out=None, v_out=None, starts=None, s
     """The values held at positions starts[b] .. starts[b] + n - 1 (starts None:
     from 0) into k_out, v_out [batch, n_kv_heads, n, d] bf16, f16 or f32; rows at
     positions >= lens[b] are zero.  starts, lens: int32 [batch]."""
+    if _bind is not None:
+        st = _bind.gather(kv.address, lens, k_out, v_out, starts, stream, kv.pages)
+        if st >= 0:
+            return _check(st) if st else None
     if k_out is None and v_out is None:
         raise ValueError("k_out or v_out is needed")
     lib = _calls()
