@@ -642,11 +642,12 @@ cudaError_t dispatch_rows(const AttnParams& p, int d, int group, int dev, int ct
 // block costs the same up to 128, eight rows after eight cost more and more.  At 32,
 // 48 and 64 rows, us: one sequence of 32K 42, 57, 69 against 53, 54, 55; 8 of 8K 70, 94,
 // 120 against 100 at all three; one of 1000 15, 16, 17 against 19, 20, 20.  So it is
-// for bf16 outputs; sequences of different query counts keep to the other kernel,
+// for bf16 outputs; fp16 ones take the other kernel's two planes, 64 to 50 and 17 to 19
+// at 48 rows of the first and last.  fp32 outputs and sequences of different query counts keep to the other kernel,
 // whose cut is made on the device.
 constexpr int kBlockRows = 48;
 bool takes_blocks(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
-  if (a->q_begin || a->o.dtype != RESKV_BF16 || a->scale < 0.f || kv->batch < 1 || kv->n_kv_heads < 1) return false;
+  if (a->q_begin || a->o.dtype == RESKV_F32 || a->scale < 0.f || kv->batch < 1 || kv->n_kv_heads < 1) return false;
   return a->n_tokens / kv->batch * (a->q.n_heads / kv->n_kv_heads) >= kBlockRows;
 }
 BlockPlan block_plan(const reskv_paged_kv* kv, const reskv_paged_attn_args* a, int sms) {

@@ -30,8 +30,8 @@
 // magnitude fits fp16.  Logits are formed from exact products: s (n - 8) has 11
 // bits, and m + 8 s, in two fp16 planes, meets the query's sums over the groups, in
 // two planes too, in one more step of the same product.  Values s n + m and weights
-// are rounded to fp16's 11 bits, finer than the bf16 the output is rounded to; other
-// output types take the kernel of few rows.  Sums, statistics and accumulators are
+// are rounded to fp16's 11 bits, no coarser than the 16-bit types the output is rounded
+// to; fp32 outputs take the kernel of few rows.  Sums, statistics and accumulators are
 // fp32.
 //
 // Bound by the warps' instructions (the schedulers issue in 56 % of the cycles, the

@@ -269,6 +269,14 @@ def test_blocks_of_rows_with_their_positions_in_parts(d, group, window):
     case(window + d + 1, [2100], 70, 1, 4, d, group, 16, "bf16", window=window)
 
 
+@pytest.mark.parametrize("d,group", [(128, 32), (64, 64)])
+def test_blocks_with_fp16_outputs(d, group):
+    case(d + 50, [300, 129, 40, 0], 40, 2, 4, d, group, 64, "f16")
+    case(d + 51, [3100, 700], 12, 1, 4, d, group, 16, "f16")
+    case(d + 52, [257], 65, 2, 4, d, group, 32, "f16", window=100)
+    case(d + 53, [500], 20, 1, 4, d, group, 64, "f16", spread=30.0)
+
+
 def test_blocks_peaked_and_of_any_size():
     """The reference moves by hundreds; values' and keys' magnitudes grow from position to position."""
     case(30, [500], 20, 1, 4, 128, 32, 64, "bf16", spread=30.0)
