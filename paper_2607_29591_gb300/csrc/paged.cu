@@ -127,8 +127,8 @@ __device__ __forceinline__ void hold(const float2 (&x)[4], uint32_t& codes, uint
 
 // kHeads KV heads of one token per D / 8 lanes: K row, then V row.  The rows' cos and
 // sin are read once.  What a row costs is instructions: the rows of 32768 tokens of 8 KV heads
-// of 128 by themselves take 66 us (176 MB, 2.7 TB/s; schedulers 72 % busy).  With their
-// 32 query heads turned beside them (713 MB) it is 151 us, 4.7 TB/s; turns and rows
+// of 128 by themselves take 65 us (176 MB, 2.7 TB/s; schedulers 72 % busy).  With their
+// 32 query heads turned beside them (713 MB) it is 146 us, 4.9 TB/s; turns and rows
 // mixed block by block were slower (168 us), as fewer loads were in flight.
 template <typename T, int D, int kGroup, bool kWide, int kHeads>
 __device__ __forceinline__ void append_rows(const AppendParams& p, int64_t r, int lane) {
@@ -271,14 +271,16 @@ __device__ __forceinline__ void append_rows(const AppendParams& p, int64_t r, in
   }
 }
 
-// The tokens' rows in the first blocks, their queries' rotation in the others.
+// The tokens' rows in the first blocks, their queries' rotation in the others (blocks of
+// 128 threads, against 256: 4 x 1024 tokens 24.3 and 26.6 us, 8 x 4096 146 and 150).
+constexpr int kAppendThreads = 128;
 template <typename T, int D, int kGroup, bool kWide, int kHeads>
-__global__ void __launch_bounds__(256, 4) k_paged_append(const __grid_constant__ AppendParams p,
+__global__ void __launch_bounds__(kAppendThreads, 1024 / kAppendThreads) k_paged_append(const __grid_constant__ AppendParams p,
                                                       const __grid_constant__ RopeParams q) {
   constexpr int L = D / 8;
   wait_for_previous();
   if (blockIdx.x < p.blocks) {
-    append_rows<T, D, kGroup, kWide, kHeads>(p, int64_t(blockIdx.x) * (256 / L) + threadIdx.x / L, threadIdx.x % L);
+    append_rows<T, D, kGroup, kWide, kHeads>(p, int64_t(blockIdx.x) * (kAppendThreads / L) + threadIdx.x / L, threadIdx.x % L);
   } else if constexpr (kWide) {
     constexpr int V = 16 / int(sizeof(T));
     const int lane = threadIdx.x % q.lanes, row = threadIdx.x / q.lanes;
@@ -292,21 +294,21 @@ __global__ void __launch_bounds__(256, 4) k_paged_append(const __grid_constant__
 
 template <typename T, int D, int kGroup, bool kWide, int kHeads>
 cudaError_t launch_append_rows(AppendParams p, RopeParams q, cudaStream_t s) {
-  constexpr int rows = 256 / (D / 8), V = 16 / int(sizeof(T));
+  constexpr int rows = kAppendThreads / (D / 8), V = 16 / int(sizeof(T));
   p.blocks = unsigned((p.n_tokens * ((p.kv_heads + kHeads - 1) / kHeads) + rows - 1) / rows);
   unsigned blocks = p.blocks;
   if (q.heads) {
     q.lanes = rope_lanes(q.dim, q.rot, V);
-    q.rows_per_block = 256 / q.lanes;
+    q.rows_per_block = kAppendThreads / q.lanes;
     constexpr int kQ = kHeads == 1 ? 1 : kManyHeads<T>;
     q.head_groups = (q.heads + kQ - 1) / kQ;
     blocks += unsigned((q.n_tokens * q.head_groups + q.rows_per_block - 1) / q.rows_per_block);
   }
-  return launch_early(k_paged_append<T, D, kGroup, kWide, kHeads>, blocks, 256, 0, s, p, q);
+  return launch_early(k_paged_append<T, D, kGroup, kWide, kHeads>, blocks, kAppendThreads, 0, s, p, q);
 }
 
 // Eight heads a thread where that leaves every SM a thousand threads (32K tokens of
-// 8 KV and 32 query heads: 151 us, against 158 with four); one where there are fewer
+// 8 KV and 32 query heads: 146 us; four heads took 5 % more); one where there are fewer
 // rows.
 template <typename T, int D, int kGroup>
 cudaError_t dispatch_heads(const AppendParams& p, const RopeParams& q, bool wide, cudaStream_t s) {
