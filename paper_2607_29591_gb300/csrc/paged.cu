@@ -64,7 +64,8 @@ __device__ __forceinline__ float mul_01(float a, float b) {        // within [0,
 // halfway), the lane compares them with t s, t the half next to 15 u: one fma has the
 // sign of x - m - t s.  The quotient itself would say the same: t s has 13 bits, so
 // that x - m, unless it is t s, is further from it than the quotient's rounding
-// reaches.
+// reaches.  Both passes end in 0..15: a minimum that bf16 rounds down leaves the largest
+// values of a group far from zero more than 15.5 scales above it.
 template <int kGroup>
 __device__ __forceinline__ void hold(const float2 (&x)[4], uint32_t& codes, uint32_t& sm) {
   float lo = min3_nan(min3_nan(x[0].x, x[0].y, x[1].x), min3_nan(x[1].y, x[2].x, x[2].y), min3_nan(x[3].x, x[3].y, x[3].y));
@@ -115,7 +116,8 @@ __device__ __forceinline__ void hold(const float2 (&x)[4], uint32_t& codes, uint
           const float near = __fsub_rn(fmaf(u[k], 15.f, kRound), kRound);
           const float t = near + copysignf(0.5f, fmaf(u[k], 15.f, -near));
           const float over = fmaf(-t, s, k ? a.y : a.x);
-          n[k] = over == 0.f ? rintf(t) : t + copysignf(0.5f, over);
+          // (u ends at one: what lies past the top code comes out as 16 here, from t = 15.5)
+          n[k] = fminf(over == 0.f ? rintf(t) : t + copysignf(0.5f, over), 15.f);
         }
         sum = ffma2(sum, k16, make_float2(-n[0], -n[1]));
       }
