@@ -416,11 +416,11 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         hi[j] = c.s.len - c.s.count + min(c.r0 + st.row(j), rows - 1) / p.group;
-        lo[j] = p.window > 0 ? max(0, hi[j] - p.window + 1) : 0;
+        lo[j] = first_seen(p, hi[j]);
       }
       const int all_hi = c.s.len - c.s.count + c.r0 / p.group;
       const int last = c.s.len - c.s.count + min(c.r0 + kRows - 1, rows - 1) / p.group;
-      const int all_lo = p.window > 0 ? max(0, last - p.window + 1) : 0;
+      const int all_lo = first_seen(p, last);
       st.reset();
 #pragma unroll 1
       for (int i = 0; i < n; ++k) {

@@ -53,14 +53,18 @@ __device__ __forceinline__ Sequence sequence_of(const AttnParams& p, int b) {
   return s;
 }
 
+// First position that a query at `pos` sees (pos may lie far below 0, a window be any).
+__device__ __forceinline__ int first_seen(const AttnParams& p, int pos) {
+  return p.window > 0 && pos >= p.window ? pos - p.window + 1 : 0;
+}
+
 // Rows [r0, r1) of a sequence.
 __device__ __forceinline__ RowBlock row_block(const AttnParams& p, const Sequence& s, int r0, int r1) {
   // (one block of a sequence's rows, the usual case, divides nothing)
   const int lo = s.len - s.count + (r0 == 0 ? 0 : r0 / p.group);
   const int hi = s.len - s.count + (r1 == s.count * p.group ? s.count - 1 : (r1 - 1) / p.group);
   RowBlock b;
-  const int from = p.window > 0 ? max(0, lo - p.window + 1) : 0;
-  b.first = from / kTile;
+  b.first = first_seen(p, lo) / kTile;
   b.tiles = hi < 0 ? 0 : hi / kTile - b.first + 1;
   return b;
 }

@@ -231,8 +231,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
   // what the block's rows see
   const int base = sq.len - sq.count;
   const int hi_first = base + r0 / p.group, hi_last = base + (min(r0 + kRows, rows) - 1) / p.group;
-  const int from = p.window > 0 ? max(0, hi_first - p.window + 1) : 0;
-  const int lo_last = p.window > 0 ? max(0, hi_last - p.window + 1) : 0;
+  const int from = first_seen(p, hi_first);
+  const int lo_last = first_seen(p, hi_last);
 
   // a softmax thread's row (rows that do not exist see what the last one does)
   const int mt = warp >> 2;
@@ -544,7 +544,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
       // --- the softmax, a row a thread ---
       const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
       const int hi = base + min(r, rows - 1) / p.group;
-      const int lo = p.window > 0 ? max(0, hi - p.window + 1) : 0;
+      const int lo = first_seen(p, hi);
       float ref = kNoRef, l = 0.f;
       uint32_t nan_groups = 0;
       // the row's query, scaled below 2^8 (128 of them sum up within fp16), in the order of the keys' dims
