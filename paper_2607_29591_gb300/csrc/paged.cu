@@ -501,8 +501,13 @@ extern "C" reskv_status reskv_paged_append(const reskv_paged_kv* kv, int64_t n_t
     if (bad.empty() && k->dtype != v->dtype) bad = "k and v must have one dtype";
     if (bad.empty() && (q != nullptr) != (q_out != nullptr)) bad = "q and q_out go together";
     if (bad.empty() && q && !rot) bad = "q needs a rotation";
+    if (bad.empty() && q) bad = check_heads(q, "q");
+    if (bad.empty() && q) bad = check_heads(q_out, "q_out");
+    if (bad.empty() && q && (q->n_heads != q_out->n_heads || q->dtype != q_out->dtype))
+      bad = "q and q_out must have the same heads and one dtype";
     if (bad.empty() && (n_tokens < 0 || double(n_tokens) * kv->n_kv_heads >= double(int64_t(1) << 31)))
       bad = "n_tokens must not be negative, n_tokens * n_kv_heads below 2^31";
+    if (bad.empty() && q && double(n_tokens) * q->n_heads >= double(int64_t(1) << 31)) bad = "n_tokens * heads must be below 2^31";
     if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
     AppendParams p{};
     p.seqs = seqs;
@@ -536,10 +541,6 @@ extern "C" reskv_status reskv_paged_append(const reskv_paged_kv* kv, int64_t n_t
       const int v16 = 16 / dtype_size(q->dtype);
       if (wide && q->dtype == k->dtype && rows_aligned(*q, 16) && rows_aligned(*q_out, 16) && aligned_to(rot->table, 16) &&
           rot->rot_dim % (2 * v16) == 0) {
-        if (q->n_heads != q_out->n_heads || q->dtype != q_out->dtype)
-          return paged_fail(RESKV_ERR_INVALID_ARG, "q and q_out must have the same heads and one dtype");
-        if (double(n_tokens) * q->n_heads >= double(int64_t(1) << 31))
-          return paged_fail(RESKV_ERR_INVALID_ARG, "n_tokens * heads must be below 2^31");
         r.t[0] = RopeTensor{q->data, q_out->data, q->token_stride, q->head_stride, q_out->token_stride,
                             q_out->head_stride, q->n_heads};
         r.heads = q->n_heads;
