@@ -479,7 +479,8 @@ reskv_status reskv_noalloc_check_status(void* stream, int32_t* last_kernel);
  * counterpart in the paper, which starts from a prefilled cache).
  *
  * These calls own no memory: tensors, pages and workspace are the caller's.
- * They allocate nothing and may be captured into CUDA graphs.  Device-side
+ * They allocate nothing and may be captured into CUDA graphs (reskv_paged_attn with a
+ * workspace that its graph shares with no call that may run beside it).  Device-side
  * faults (a position, sequence or page outside its range) touch no memory out
  * of range: the row is skipped or left as stated, and RESKV codes are ORed into
  * the caller's status word (2 = index out of range, 1 = a bounded wait gave up).
@@ -688,6 +689,13 @@ size_t reskv_paged_attn_workspace(const reskv_paged_kv* kv, const reskv_paged_at
 
 reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* args,
                               void* stream);
+
+/* 1 while `stream` is being captured into a graph, else 0.  For callers that would
+ * make a workspace on demand: what is zeroed during a capture is not zeroed until the
+ * graph runs, and graphs that share a workspace must be ordered like calls, so a
+ * captured call brings a workspace of its own (the Python binding asks this before it
+ * uses the one that it keeps per stream). */
+int32_t reskv_stream_capturing(void* stream);
 
 #ifdef __cplusplus
 }

@@ -579,7 +579,9 @@ def _calls():
         lib.reskv_paged_append.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
         lib.reskv_paged_gather.argtypes = [vp, vp, vp, i64, vp, vp, vp]
         lib.reskv_paged_attn.argtypes = [vp, vp, vp]
-        for f in (lib.reskv_rope, lib.reskv_paged_append, lib.reskv_paged_gather, lib.reskv_paged_attn):
+        lib.reskv_stream_capturing.argtypes = [vp]
+        for f in (lib.reskv_rope, lib.reskv_paged_append, lib.reskv_paged_gather, lib.reskv_paged_attn,
+                  lib.reskv_stream_capturing):
             f.restype = i32
         if not os.path.exists(os.path.join(os.path.dirname(LIB_PATH), "_bind.so")):
             raise RuntimeError("_bind.so is missing: build it with `python -m paper_2607_29591_gb300.build` "
@@ -816,11 +818,12 @@ _workspaces = {}
 
 def _workspace(device, stream: int, nbytes: int):
     """Zeroed workspaces of a device and stream, the last the largest; what one
-    grew from is kept (a captured graph may hold its address)."""
+    grew from is kept (calls on the stream may still be using it)."""
     import torch
+    new = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+    torch.cuda.current_stream(device).synchronize()      # zeroed before it is any call's
     held = _workspaces.setdefault((device.index, stream), [])
-    held.append(torch.zeros(nbytes, dtype=torch.uint8, device=device))
-    torch.cuda.current_stream(device).synchronize()
+    held.append(new)
     return held
 
 
@@ -833,7 +836,8 @@ def reskv_paged_attn(kv: PagedKV, q, lens, o, q_begin=None, scale: Optional[floa
     lens[b] tokens it holds; o: [T, heads, d] of q's dtype or float32.  window:
     positions a query sees, itself included (0: all).  lse: float32 [T, heads]
     for ln sum exp, or None.  workspace: zeroed uint8 tensor of at least
-    reskv_paged_attn_workspace() bytes (None: one kept per stream).
+    reskv_paged_attn_workspace() bytes (None: one kept per stream); a call that is
+    captured into a graph brings its own.
     """
     lib = _calls()
     T, d, B = q.shape[0], kv.head_dim, kv.batch
@@ -843,6 +847,9 @@ def reskv_paged_attn(kv: PagedKV, q, lens, o, q_begin=None, scale: Optional[floa
         raise ValueError(f"lse must hold {T * qh[3]} elements, got {lse.numel()}")
     s = _stream_of(stream, q)
     if workspace is None:
+        if lib.reskv_stream_capturing(s):
+            raise ValueError("a call that is captured into a graph needs workspace=: a zeroed uint8 tensor of "
+                             "reskv_paged_attn_workspace() bytes, made before the capture")
         need = kv.attn_workspace.get((T, qh[3], oh[4]))
         if need is None:
             need = kv.attn_workspace[T, qh[3], oh[4]] = reskv_paged_attn_workspace(kv, T, qh[3], o.dtype)
