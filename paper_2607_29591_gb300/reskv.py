@@ -747,7 +747,7 @@ class PagedKV:
         if word:
             self.status.zero_()
             if word & 1:
-                _workspaces.clear()              # what such a call leaves is not ready for the next
+                _zero_workspaces(self.status.device)     # what such a call leaves is not ready for the next
             raise ReskvError(RESKV_ERR_DEVICE_STATUS, f"paged cache status word {word} (1 = bounded wait "
                                                       "timed out, 2 = index out of range)")
 
@@ -825,6 +825,17 @@ def _workspace(device, stream: int, nbytes: int):
     held = _workspaces.setdefault((device.index, stream), [])
     held.append(new)
     return held
+
+
+def _zero_workspaces(device) -> None:
+    """Make the kept workspaces of a device ready again, in place: what runs there may hold their addresses."""
+    import torch
+    torch.cuda.synchronize(device)
+    for (index, _), held in list(_workspaces.items()):
+        if index == device.index:
+            for w in held:
+                w.zero_()
+    torch.cuda.synchronize(device)
 
 
 def reskv_paged_attn(kv: PagedKV, q, lens, o, q_begin=None, scale: Optional[float] = None, window: int = 0,

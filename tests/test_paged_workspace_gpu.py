@@ -78,3 +78,36 @@ def test_a_workspace_that_could_not_be_zeroed_is_not_kept(monkeypatch):
     R.reskv_paged_attn(kv, q, lt, out, stream=side)
     side.synchronize()
     assert torch.equal(out, want)
+
+
+def test_kept_workspaces_are_zeroed_in_place_after_a_wait_that_gave_up(monkeypatch):
+    """Every stream's, none dropped: work in flight may be using it."""
+    monkeypatch.setattr(R, "_workspaces", {})
+    kv, q, lt, want = state()
+    side, out = torch.cuda.Stream(), torch.zeros_like(q)
+    R.reskv_paged_attn(kv, q, lt, out, stream=side)
+    torch.cuda.synchronize()
+    kept = [w for held in R._workspaces.values() for w in held]
+    assert len(kept) == 2
+    at = [w.data_ptr() for w in kept]
+    for w in kept:
+        w.fill_(0x11)
+    kv.status.fill_(1)                                 # what a kernel whose wait gave up reports
+    with pytest.raises(R.ReskvError, match="word 1"):
+        kv.check_status()
+    now = [w for held in R._workspaces.values() for w in held]
+    assert [w.data_ptr() for w in now] == at and all((w == 0).all() for w in now)
+    for stream in (None, side):
+        out.zero_()
+        torch.cuda.synchronize()
+        R.reskv_paged_attn(kv, q, lt, out, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    for w in kept:
+        w.fill_(0x11)
+    kv.status.fill_(2)                                 # an index out of range leaves them ready
+    with pytest.raises(R.ReskvError, match="word 2"):
+        kv.check_status()
+    assert all((w == 0x11).all() for w in kept)
+    for w in kept:
+        w.zero_()
