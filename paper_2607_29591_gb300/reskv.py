@@ -868,10 +868,13 @@ def reskv_paged_attn(kv: PagedKV, q, lens, o, q_begin=None, scale: Optional[floa
         if held is None or held[-1].numel() < need:
             held = _workspace(q.device, s, need)
         workspace = held[-1]
+    elif not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor")
     st = lib.reskv_paged_attn(kv.address, _pack_attn(
         *qh, *oh, 0 if lse is None else _dptr(lse, "torch.float32", "lse").value,
         0 if q_begin is None else _ints(q_begin, "q_begin", B + 1), _ints(lens, "lens", B), T,
-        0.0 if scale is None else scale, window, workspace.data_ptr(), workspace.numel()), s)
+        0.0 if scale is None else scale, window, workspace.data_ptr(),
+        workspace.numel() * workspace.element_size()), s)
     if st:
         _check(st)
 

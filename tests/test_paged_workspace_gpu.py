@@ -111,3 +111,21 @@ def test_kept_workspaces_are_zeroed_in_place_after_a_wait_that_gave_up(monkeypat
     assert all((w == 0x11).all() for w in kept)
     for w in kept:
         w.zero_()
+
+
+def test_workspaces_that_are_refused():
+    """Host memory, rows that do not lie together, too few bytes; any type of enough bytes will do."""
+    kv, q, lt, want = state()
+    n = own(kv, q).numel()
+    out = torch.zeros_like(q)
+    for bad in (torch.zeros(n, dtype=torch.uint8), torch.zeros(n, dtype=torch.uint8).pin_memory(),
+                torch.zeros((n, 2), dtype=torch.uint8, device="cuda")[:, 0], torch.zeros((2, n), dtype=torch.uint8, device="cuda").t()):
+        with pytest.raises(ValueError, match="workspace must be"):
+            R.reskv_paged_attn(kv, q, lt, out, workspace=bad)
+    for few in (own(kv, q)[:-1], own(kv, q)[16:], torch.zeros(n // 4 - 1, dtype=torch.int32, device="cuda")):
+        with pytest.raises(R.ReskvError, match="workspace must be"):
+            R.reskv_paged_attn(kv, q, lt, out, workspace=few)
+    for good in (own(kv, q), torch.zeros(-(-n // 4), dtype=torch.int32, device="cuda")):
+        out.zero_()
+        R.reskv_paged_attn(kv, q, lt, out, workspace=good)
+        assert torch.equal(out, want)
