@@ -610,7 +610,9 @@ int64_t reskv_paged_head_bytes(int32_t page_tokens, int32_t head_dim, int32_t qu
  *                     nothing is held, q's row is copied.  Each (sequence,
  *                     position) at most once a call.  A sequence or position
  *                     outside the table, a page outside the pages, or a position
- *                     >= n_positions is a fault: nothing is held, q is copied.
+ *                     >= n_positions is a fault: nothing is held.  What q_out gets
+ *                     goes by the position alone, as in reskv_rope: copied at one
+ *                     >= n_positions, turned otherwise.
  *   k, v            : device [n_tokens, n_kv_heads, head_dim], one dtype
  *   q, q_out        : device [n_tokens, any heads, head_dim] of any dtype, or NULL
  */
