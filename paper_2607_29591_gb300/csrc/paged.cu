@@ -34,6 +34,7 @@ struct AppendParams {
   int64_t n_pages, n_positions, n_tokens;
   int32_t batch, table_pages, page_tokens, kv_heads;
   int32_t rot, interleaved;
+  int32_t head_groups, heads_each;  // of a token; KV heads a thread takes, at most kHeads
   uint32_t blocks;                // of the launch that hold rows; the others turn queries
 };
 
@@ -127,7 +128,7 @@ __device__ __forceinline__ void hold(const float2 (&x)[4], uint32_t& codes, uint
   sm = s16 | (m16 << 16);
 }
 
-// kHeads KV heads of one token per D / 8 lanes: K row, then V row.  The rows' cos and
+// Up to kHeads KV heads of one token per D / 8 lanes: K row, then V row.  The rows' cos and
 // sin are read once.  What a row costs is instructions: the rows of 32768 tokens of 8 KV heads
 // of 128 by themselves take 65 us (176 MB, 2.7 TB/s; schedulers 72 % busy).  With their
 // 32 query heads turned beside them (713 MB) it is 146 us, 4.9 TB/s; turns and rows
@@ -136,11 +137,11 @@ template <typename T, int D, int kGroup, bool kWide, int kHeads>
 __device__ __forceinline__ void append_rows(const AppendParams& p, int64_t r, int lane) {
   constexpr int NG = D / kGroup;
   constexpr TileShape ts{D, NG};
-  const int groups = (p.kv_heads + kHeads - 1) / kHeads;
+  const int groups = p.head_groups, each = kHeads == 1 ? 1 : p.heads_each;
   const bool in = r < p.n_tokens * groups;
   if (!in) r = 0;                                   // stays for the shuffles, writes nothing
   const int64_t tok = uint32_t(r) / uint32_t(groups);
-  const int h0 = (int(r) - int(tok) * groups) * kHeads;
+  const int h0 = (int(r) - int(tok) * groups) * each;
   const int pos = p.positions[tok], seq = p.seqs[tok];
   bool live = in && pos >= 0;
   uint8_t* tile = nullptr;                          // of head 0
@@ -210,7 +211,7 @@ __device__ __forceinline__ void append_rows(const AppendParams& p, int64_t r, in
   };
   ask(h0);
 #pragma unroll 1
-  for (int i = 0; i < kHeads; ++i) {
+  for (int i = 0; i < each; ++i) {
     const int h = min(h0 + i, p.kv_heads - 1);      // the last head again: the same bytes
     const T* k = static_cast<const T*>(p.k) + tok * p.k_token + h * p.k_head;
     uint8_t* at = tile + h * head_bytes;
@@ -247,7 +248,7 @@ __device__ __forceinline__ void append_rows(const AppendParams& p, int64_t r, in
         }
       }
     }
-    if (kHeads > 1 && i + 1 < kHeads) ask(min(h + 1, p.kv_heads - 1));
+    if (kHeads > 1 && i + 1 < each) ask(min(h + 1, p.kv_heads - 1));
     uint32_t codes, sm;
     hold<kGroup>(x, codes, sm);
     const bool first = lane % (kGroup / 8) == 0;
@@ -297,7 +298,10 @@ __global__ void __launch_bounds__(kAppendThreads, 1024 / kAppendThreads) k_paged
 template <typename T, int D, int kGroup, bool kWide, int kHeads>
 cudaError_t launch_append_rows(AppendParams p, RopeParams q, cudaStream_t s) {
   constexpr int rows = kAppendThreads / (D / 8), V = 16 / int(sizeof(T));
-  p.blocks = unsigned((p.n_tokens * ((p.kv_heads + kHeads - 1) / kHeads) + rows - 1) / rows);
+  // all threads take the same number of heads (9 as 5 and 4, so that one of ten is the last again)
+  p.head_groups = (p.kv_heads + kHeads - 1) / kHeads;
+  p.heads_each = (p.kv_heads + p.head_groups - 1) / p.head_groups;
+  p.blocks = unsigned((p.n_tokens * p.head_groups + rows - 1) / rows);
   unsigned blocks = p.blocks;
   if (q.heads) {
     q.lanes = rope_lanes(q.dim, q.rot, V);
@@ -309,9 +313,10 @@ cudaError_t launch_append_rows(AppendParams p, RopeParams q, cudaStream_t s) {
   return launch_early(k_paged_append<T, D, kGroup, kWide, kHeads>, blocks, kAppendThreads, 0, s, p, q);
 }
 
-// Eight heads a thread where that leaves every SM a thousand threads (32K tokens of
+// Up to eight heads a thread where that leaves every SM a thousand threads (32K tokens of
 // 8 KV and 32 query heads: 146 us; four heads took 5 % more); one where there are fewer
-// rows.
+// rows.  2^18 rows of 1, 2, 4, 8 and 9 KV heads: 101, 76, 67, 64 and 72 us (one head a
+// thread: 88 to 90).
 template <typename T, int D, int kGroup>
 cudaError_t dispatch_heads(const AppendParams& p, const RopeParams& q, bool wide, cudaStream_t s) {
   if (!wide) return launch_append_rows<T, D, kGroup, false, 1>(p, q, s);
