@@ -524,7 +524,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
       const int i = e0 + every;
       const float f = __shfl_sync(0xffffffffu, j.weight, i & 31);
       const float* rec = (i & 1) ? reinterpret_cast<const float*>(ring + (i >> 1) * kAttnStages * SB) : heads + (i >> 1) * RF;
-      if (i < stop && f != 0.f) add_scaled(a, f, *reinterpret_cast<const float4*>(rec + row * RS + 4 * u));
+      if (i < stop && ((j.present >> i) & 1)) add_scaled(a, f, *reinterpret_cast<const float4*>(rec + row * RS + 4 * u));
     }
     a = all_lanes(a, lanes);
     if (!cut(ri)) {
@@ -564,7 +564,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     const int a0 = part_of(ri.start, N, ctas), n = part_of(ri.start + ri.tiles - 1, N, ctas) - a0 + 1;
     // record i of the unit: the CTA it begins in keeps it second, the others first
     auto record = [&](int i) { return p.partials + ((a0 + i) * 2 + (i == 0 ? 1 : 0)) * (RF + kRows); };
-    Joined all{0.f, -INFINITY};
+    Joined all{0.f, -INFINITY, 0u};
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
     for (int i0 = 0; i0 < n; i0 += 32) {
@@ -578,7 +578,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
         const float f = __shfl_sync(0xffffffffu, j.weight, i & 31);
         const float4 v = i < stop ? __ldcg(reinterpret_cast<const float4*>(record(i0 + i) + row2 * RS + 4 * u2))
                                   : make_float4(0.f, 0.f, 0.f, 0.f);
-        add_scaled(b, f, i < stop && f != 0.f ? v : make_float4(0.f, 0.f, 0.f, 0.f));
+        add_scaled(b, f, i < stop && ((j.present >> i) & 1) ? v : make_float4(0.f, 0.f, 0.f, 0.f));
       }
       b = all_lanes(b, kLanes);
       if (n <= 32) {

@@ -147,9 +147,11 @@ __device__ __forceinline__ void store_lse(const AttnParams& p, const Sequence& s
   if (p.lse) p.lse[(s.q0 + r / p.group) * int64_t(p.heads) + h * p.group + r % p.group] = ref * 0.693147180559945f;
 }
 // The softmaxes of up to 32 records joined: each lane's weight for its record's
-// output, from their log2 sums (-inf: an empty or no record), and the joint sum.
+// output, from their log2 sums (-inf: an empty or no record), the records that are none
+// of these, and the joint sum.  A record of weight 0 still counts: a NaN in it is seen.
 struct Joined {
   float weight, ref;
+  uint32_t present;
 };
 __device__ __forceinline__ Joined join_weights(float ref) {
   float top = ref;
@@ -159,7 +161,8 @@ __device__ __forceinline__ Joined join_weights(float ref) {
   float sum = f;
 #pragma unroll
   for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  return sum != 0.f ? Joined{f / sum, top + log2f(sum)} : Joined{0.f, -INFINITY};
+  const uint32_t present = __ballot_sync(0xffffffffu, ref != -INFINITY);
+  return sum != 0.f ? Joined{f / sum, top + log2f(sum), present} : Joined{0.f, -INFINITY, 0u};
 }
 __device__ __forceinline__ void add_scaled(float4& a, float f, float4 v) {
   a.x = fmaf(f, v.x, a.x);

@@ -773,7 +773,7 @@ __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ Block
     const float f = __shfl_sync(0xffffffffu, j.weight, k);
     const float4 v = lane < D / 4 ? reinterpret_cast<const float4*>(bp.records + ((slot + k) * kRows + row) * D)[lane]
                                   : make_float4(0.f, 0.f, 0.f, 0.f);
-    add_scaled(a, f, f != 0.f ? v : make_float4(0.f, 0.f, 0.f, 0.f));
+    add_scaled(a, f, (j.present >> k) & 1 ? v : make_float4(0.f, 0.f, 0.f, 0.f));
   }
   if (lane < D / 4) store_out(p, sq, h, r, lane, a);
   if (lane == 0) store_lse(p, sq, h, r, j.ref);
