@@ -654,7 +654,8 @@ reskv_status reskv_paged_gather(const reskv_paged_kv* kv, const int32_t* starts,
  * or a page outside the pages, whose tokens nobody sees; q_begin outside
  * [0, n_tokens] is taken as the nearest.  NaN held at a position reaches the queries
  * that see it and no others.  Limits: n_tokens * heads below 2^31, n_tokens *
- * heads / 4 + batch * n_kv_heads below 2^24; scales s of held values at most 2^96.
+ * heads / 4 + batch * n_kv_heads below 2^24; scales s of held values at most 2^96, and
+ * where all groups of a value's row are constant (s = 0) their minima at most 2^48.
  *
  * Roundings: logits are sums of exact products.  The softmax weights are rounded to
  * 11 bits where o is bf16 (22 otherwise).  Where o has 16 bits, q_begin is NULL and

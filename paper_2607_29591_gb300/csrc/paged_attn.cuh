@@ -187,7 +187,9 @@ __device__ __forceinline__ void add_scaled(float4& a, float f, float4 v) {
 // fp16 (two planes, 22 bits, unless the output is bf16).  Queries are scaled by a
 // power of two to fp16's top, weights by the running reference: it follows the
 // largest logit + log2 of the token's largest value scale, so that P * scale
-// stays in fp16's range for value scales between 2^-96 and 2^96.
+// stays in fp16's range for value scales between 2^-96 and 2^96.  A token whose values
+// are constant within every group has no scale and counts as one of 2^-48: its weight
+// stays below 2^62, and times a minimum of up to 2^48 a sum within fp32.
 //
 // The reference moves only when it is passed by more than 8 (2^14 of fp16's
 // range, where 2^6 stands for a weight of one).
@@ -199,6 +201,7 @@ __device__ __forceinline__ void add_scaled(float4& a, float f, float4 v) {
 // rows 8..15.  A lane then scales and rounds the weights of half the groups:
 // 20 % fewer instructions a tile, and those bound the kernel.
 constexpr float kNoRef = -3.0e38f;
+constexpr float kLeastScale = 1.2621774483536189e-29f, kNoScale = 3.552713678800501e-15f;      // 2^-96, 2^-48
 
 template <int D, int NG, bool kTwoPlanes, int R>
 struct TileStep {
@@ -422,7 +425,7 @@ struct TileStep {
     for (int i = 0; i < 2; ++i) {
       lane_meta<false>(vs[i], vmeta + i * 8 * 4 * NG);
       lane_meta<true>(vm[i], vmeta + i * 8 * 4 * NG);
-      top_s[i] = 1.2621774483536189e-29f;        // 2^-96; fmaxf passes over NaN, whose rows decide nothing
+      top_s[i] = kNoScale;                       // at least; fmaxf passes over NaN, whose rows decide nothing
 #pragma unroll
       for (int k = 0; k < K; ++k) top_s[i] = fmaxf(top_s[i], vs[i][k]);
     }
@@ -438,9 +441,11 @@ struct TileStep {
       float sg[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        float s = top_s[i];
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) s = fmaxf(s, vs[i][k]);
         if constexpr (kHalves && NG > 1) s = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, 2));
-        sg[i] = fminf(log2f(s), 96.f);
+        sg[i] = fminf(log2f(s == 0.f ? kNoScale : fmaxf(s, kLeastScale)), 96.f);
       }
 #pragma unroll
       for (int j = 0; j < 2; ++j) {

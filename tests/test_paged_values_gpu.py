@@ -1,19 +1,23 @@
-"""Unusual held values in attention over the paged cache: NaN whose weight vanishes."""
+"""Unusual held values in attention over the paged cache: NaN whose weight vanishes, rows
+of constants of any size."""
+import numpy as np
 import pytest
 import torch
 
-from paged_cases import DT
+from oracle import paged_oracle as po
+from paged_cases import DT, as_type
 from paper_2607_29591_gb300 import reskv as R
+from test_paged_attn_gpu import check
 
 pytestmark = pytest.mark.gpu
 
 
-def filled(k, v, page=64):
+def filled(k, v, page=64, group=32):
     """A cache of one sequence with the fp32 rows k, v [n, kv, 128], in pages in reverse order."""
     n, kv, d = k.shape
     pages = -(-n // page)
     table = torch.arange(pages - 1, -1, -1, dtype=torch.int32, device="cuda")[None].contiguous()
-    cache = R.PagedKV(R.reskv_paged_pages(pages, kv, page, d, 32), table, page, kv, d, 32)
+    cache = R.PagedKV(R.reskv_paged_pages(pages, kv, page, d, group), table, page, kv, d, group)
     R.reskv_paged_append(cache, k, v, torch.zeros(n, dtype=torch.int32, device="cuda"), torch.arange(n, dtype=torch.int32, device="cuda"))
     cache.check_status()
     return cache
@@ -37,3 +41,32 @@ def test_nan_of_vanishing_weight_reaches_the_output(n, new, dtype, out):
     assert torch.isnan(o[:, :4, 32:64]).all()
     assert torch.isfinite(o[:, :4, :32]).all() and torch.isfinite(o[:, :4, 64:]).all() and torch.isfinite(o[:, 4:]).all()
     assert torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("new,dtype,out", [(1, "bf16", "bf16"), (1, "f16", "f32"), (3, "bf16", "f32"), (20, "bf16", "bf16")])
+@pytest.mark.parametrize("c,mix", [(0.0, False), (1.0, False), (-65504.0, False), (1e9, False), (-1e12, False), (1e9, True)])
+def test_rows_of_constants(c, mix, new, dtype, out, group):
+    """Values without a scale, under logits that rise along the positions; with `mix` beside rows of their size that
+    have one, and zeros.  Tolerance as in test_paged_attn_gpu.py, in units of the values."""
+    rng = np.random.default_rng(90)
+    n = 700
+    # logits from about -20 to 20: the reference follows in steps and within them
+    q = 0.5 * rng.standard_normal((new, 4, 128)) + 1.0
+    k = np.linspace(-1.8, 1.8, n)[:, None, None] + 0.2 * rng.standard_normal((n, 1, 128))
+    v = np.full((n, 1, 128), c)
+    if mix:
+        v[1::3] = c * rng.standard_normal((len(v[1::3]), 1, 128))
+        v[2::3] = 0
+    k, v = (torch.from_numpy(x.astype(np.float32)).cuda() for x in (k, v))
+    cache = filled(k, v, group=group)
+    ln = torch.tensor([n], dtype=torch.int32, device="cuda")
+    kk, vv = (torch.empty((1, 1, n, 128), device="cuda") for _ in range(2))
+    R.reskv_paged_gather(cache, ln, kk, vv)
+    qt, q64 = as_type(q, dtype)
+    o, lse = torch.full((new, 4, 128), float("nan"), dtype=DT[out], device="cuda"), torch.empty((new, 4), device="cuda")
+    R.reskv_paged_attn(cache, qt, ln, o, lse=lse)
+    cache.check_status()
+    unit = abs(c) or 1.0
+    ro, rl, xm, vm = po.attend(q64, kk[0].double().cpu().numpy(), vv[0].double().cpu().numpy(), 4, 128 ** -0.5)
+    check(o.double() / unit, lse, [(ro / unit, rl, xm, vm / unit)], 128, out)
