@@ -113,6 +113,12 @@ __device__ __forceinline__ float exp2_fast(float x) {          // 2^-inf = 0
   return y;
 }
 
+__device__ __forceinline__ float min_nan(float a, float b) {     // a NaN kept
+  float y;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
 // --- outputs -----------------------------------------------------------------
 
 // Output row r of a sequence, dims 4u .. 4u + 3.
@@ -438,7 +444,7 @@ struct TileStep {
     const float over = fmaxf(fmaxf(w[0], w[1]) * top_s[0], fmaxf(w[2], w[3]) * top_s[1]);
     if (__any_sync(0xffffffffu, over > 16384.f)) {
       // a row's reference: 6 below its largest logit + log2 scale
-      float sg[2];
+      float sg[2], x[4];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         float s = 0.f;
@@ -452,8 +458,8 @@ struct TileStep {
         float top = kNoRef;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float x = acc[2 * i + j] * cq[j] + sg[i];
-          if (!kMask || see[i][j]) top = fmaxf(top, x);
+          x[2 * i + j] = __fmul_rn(acc[2 * i + j], cq[j]);
+          if (!kMask || see[i][j]) top = fmaxf(top, x[2 * i + j] + sg[i]);
         }
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
@@ -470,9 +476,11 @@ struct TileStep {
           o[m][2 + j] *= keep;
         }
       }
+      // From the rounded logits that the reference was taken from: past 2^26 it may lie many
+      // units off the unrounded ones, and 6 and sg may be lost in it.
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        w[i] = exp2_fast(fmaf(acc[i], cq[i & 1], -ref[i & 1]));
+        w[i] = exp2_fast(min_nan(x[i] - ref[i & 1], 6.5f - sg[i >> 1]));
         if (kMask && !see[i >> 1][i & 1]) w[i] = 0.f;
       }
     }

@@ -1,11 +1,11 @@
 """Unusual held values in attention over the paged cache: NaN whose weight vanishes, rows
-of constants of any size."""
+of constants of any size, logits of any size."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import paged_oracle as po
-from paged_cases import DT, as_type
+from paged_cases import DT, HALF_ULP, as_type
 from paper_2607_29591_gb300 import reskv as R
 from test_paged_attn_gpu import check
 
@@ -70,3 +70,27 @@ def test_rows_of_constants(c, mix, new, dtype, out, group):
     unit = abs(c) or 1.0
     ro, rl, xm, vm = po.attend(q64, kk[0].double().cpu().numpy(), vv[0].double().cpu().numpy(), 4, 128 ** -0.5)
     check(o.double() / unit, lse, [(ro / unit, rl, xm, vm / unit)], 128, out)
+
+
+@pytest.mark.parametrize("size", [1e5, 1e7, 1e8, 3e8, 1e9, 1e10, 1e12, 1e15, 1e20])
+@pytest.mark.parametrize("n,new,dtype,out", [(300, 1, "bf16", "bf16"), (300, 1, "f16", "f32"), (300, 3, "bf16", "f32"), (4000, 1, "bf16", "f32")])
+def test_logits_of_any_size(size, n, new, dtype, out):
+    """One key's logit is past what fp32 counts in ones, another's as far below: the output is the one's value.  Its
+    weight times the group's scale is rounded to 11 bits, times a code at most the row's range, then the output; the log-sum-exp is the logit, 128 products and
+    a scaling of fp32 (129 2^-23 of it)."""
+    g = torch.Generator(device="cuda").manual_seed(n + new)
+    k, v = 0.1 * torch.randn((n, 1, 128), generator=g, device="cuda"), torch.randn((n, 1, 128), generator=g, device="cuda")
+    k[n // 3], k[n // 2] = size, -size
+    cache = filled(k, v)
+    ln = torch.tensor([n], dtype=torch.int32, device="cuda")
+    kk, vv = (torch.empty((1, 1, n, 128), device="cuda") for _ in range(2))
+    R.reskv_paged_gather(cache, ln, kk, vv)
+    q = (1 + 0.1 * torch.rand((new, 4, 128), generator=g, device="cuda")).to(DT[dtype])
+    o, lse = torch.full((new, 4, 128), float("nan"), dtype=DT[out], device="cuda"), torch.empty((new, 4), device="cuda")
+    R.reskv_paged_attn(cache, q, ln, o, lse=lse)
+    cache.check_status()
+    win = vv[0, 0, n // 3]
+    tol = 2.0 ** -11 * (win.max() - win.min()) + HALF_ULP[out] * win.abs() * 1.01
+    assert ((o.float() - win).abs() <= tol).all()
+    logit = (q.double() * kk[0, 0, n // 3].double()).sum(-1) * 128 ** -0.5
+    assert ((lse.double() - logit).abs() <= 129 * 2.0 ** -23 * logit.abs()).all()
