@@ -32,7 +32,9 @@
 // two planes too, in one more step of the same product.  Values s n + m and weights
 // are rounded to fp16's 11 bits, no coarser than the 16-bit types the output is rounded
 // to; fp32 outputs take the kernel of few rows.  Sums, statistics and accumulators are
-// fp32.
+// fp32.  A row whose logits or output come out small beside what the block's largest key
+// or value leaves of fp16's digits (a token that other rows see, far larger than all it
+// sees) is computed again in fp32, by plain_rows().
 //
 // Bound by the warps' instructions (the schedulers issue in 56 % of the cycles, the
 // tensor cores work in 29 %): 512 tokens behind 8K (2 sequences, 8 KV heads, 32 query
@@ -52,6 +54,12 @@ constexpr int kSub = kPos / kTile;                // cache tiles of a step
 constexpr int kThreads = 640;                     // warps 0-7 softmax, 8-15 unpack, 16 products, 17 copies, 18-19 exponents
 constexpr int kUnpackWarp = 8, kIssueWarp = 16, kCopyWarp = 17, kLookWarp = 18;
 constexpr int kRaw = 3;                           // steps of packed tiles in flight
+// What a row makes of operands that were held for the whole block is checked at its end.
+// The block's keys leave logits off by 2^-10 of their unit at most, which is below 2^-14 up
+// to kFarLogits (rows whose query times the largest key is some 2^17); past that logits
+// may also be too large for weights formed from unrounded ones.  Values are off by 2^-25,
+// 2^-12 of an output of kFarValues.
+constexpr float kFarLogits = 0.03125f, kFarValues = 1.220703125e-4f;          // 2^-5, 2^-13
 // Registers a thread of each part: (2 x 128 + 2 x 88 + 40) x 128 of the launch's 96 x 640.
 constexpr int kRegsSoftmax = 128, kRegsUnpack = 88, kRegsIssue = 40;
 static_assert((2 * kRegsSoftmax + 2 * kRegsUnpack + kRegsIssue) * 128 <= 96 * kThreads, "registers");
@@ -177,6 +185,98 @@ struct BlockParams {
   BlockPlan plan;
   float* records;                                 // [slot][rows][D], then [slot][rows] log2 sums
 };
+
+// A softmax warp's rows without tensor cores, one after the other, in fp32, whatever the
+// magnitudes: a lane has four dims, four positions are taken at a time.  Far slower (a
+// chunk all of whose rows go this way, 512 tokens behind 8K of two sequences: 54 ms) and
+// for inputs past what a model makes; out of line, so that the loops of the roles do not
+// move in the instruction caches for it.
+template <int D, int NG>
+__device__ __noinline__ void plain_rows(const BlockParams& bp, const Sequence& sq, int b, int h, int r0, int first, int tiles,
+                                        float* record, float* record_ref) {
+  const AttnParams& p = bp.a;
+  constexpr TileShape ts{D, NG};
+  constexpr int TB = ts.bytes();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rows = sq.count * p.group, base = sq.len - sq.count;
+  __syncwarp();
+  const int tpp = p.page_tokens / kTile, u = lane < D / 4 ? lane : 0, group = 4 * u * NG / D;
+#pragma unroll 1
+  for (int i = 0; i < 32; ++i) {
+    const int local = warp * 32 + i, row = r0 + local;
+    if (row >= rows) break;
+    const uint16_t* src = static_cast<const uint16_t*>(p.q) + (sq.q0 + row / p.group) * p.q_token +
+                          int64_t(h * p.group + row % p.group) * p.q_head + 4 * u;
+    float qv[4], o[4] = {0.f, 0.f, 0.f, 0.f}, top = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float x = p.q_f16 ? __half2float(__ushort_as_half(src[j])) : __bfloat162float(__ushort_as_bfloat16(src[j]));
+      qv[j] = lane < D / 4 ? x : 0.f;
+    }
+    const int hi = base + row / p.group, lo = first_seen(p, hi);
+    const int stop = hi < 0 ? 0 : min(hi / kTile + 1, first + tiles);
+#pragma unroll 1
+    for (int t = max(lo / kTile, first); t < stop; ++t) {
+      const int page = p.page_table[int64_t(b) * p.table_pages + t / tpp];
+      if (page < 0 || page >= p.n_pages) continue;
+      const uint8_t* tile = p.pages + ((int64_t(page) * p.kv_heads + h) * tpp + t % tpp) * int64_t(TB);
+#pragma unroll 1
+      for (int k0 = 0; k0 < kTile; k0 += 4) {
+        auto value = [&](int k, int codes, int meta, int j) {
+          const uint16_t* sm = reinterpret_cast<const uint16_t*>(tile + meta) + 2 * NG * k + group;
+          const float s = __bfloat162float(__ushort_as_bfloat16(sm[0])), m = __bfloat162float(__ushort_as_bfloat16(sm[NG]));
+          return fmaf(s, float(*reinterpret_cast<const uint16_t*>(tile + codes) >> (4 * j) & 15), m);
+        };
+        float x[4], v[4][4], now = top;
+        bool any = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          x[k] = 0.f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            x[k] = fmaf(qv[j], value(k0 + k, ts.k_unit(k0 + k, u), ts.k_meta(), j), x[k]);
+            v[k][j] = value(k0 + k, ts.v_codes() + ts.v_unit(k0 + k, u), ts.v_meta(), j);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+#pragma unroll
+          for (int d = 16; d; d /= 2) x[k] += __shfl_xor_sync(0xffffffffu, x[k], d);
+          const int pos = t * kTile + k0 + k;
+          x[k] = pos >= lo && pos <= hi ? x[k] * p.scale2 : -INFINITY;
+          now = fmaxf(now, x[k]);
+          any |= x[k] != -INFINITY;
+        }
+        if (!any) continue;
+        const float keep = exp2f(top - now);
+        top = now;
+        l *= keep;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] *= keep;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (x[k] == -INFINITY) continue;
+          const float w = exp2f(x[k] - now);
+          l += w;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[j] = fmaf(w, v[k][j], o[j]);
+        }
+      }
+    }
+    const bool seen = l != 0.f;
+    const float inv = seen ? 1.f / l : 0.f;
+    const float4 v = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    if (lane < D / 4) {
+      if (record) reinterpret_cast<float4*>(record + int64_t(local) * D)[lane] = v;
+      else store_out(p, sq, h, row, lane, v);
+    }
+    if (lane == 0) {
+      const float sum = seen ? top + log2f(l) : -INFINITY;
+      if (record) record_ref[local] = sum;
+      else store_lse(p, sq, h, row, sum);
+    }
+  }
+}
 
 template <int D, int NG, int MT>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_constant__ BlockParams bp) {
@@ -724,6 +824,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
         fence_after();
         const bool seen = ref != kNoRef || l != 0.f;
         const float inv = seen ? up(ev_was) / l : 0.f;
+        float top_o = 0.f;
 #pragma unroll 1
         for (int c = 0; c < C; ++c) {
           float o[32], v[32];
@@ -734,10 +835,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
           defined16(o + 16);
           const bool bad = (nan_groups >> (c / PG)) & 1;
 #pragma unroll
+          for (int k = 0; k < 32; ++k) top_o = fmaxf(top_o, fabsf(o[k]));
+#pragma unroll
           for (int k = 0; k < 32; ++k) v[4 * (k & 7) + (k >> 3)] = bad ? __int_as_float(0x7fc00000) : o[k] * inv;
           finish_row(c, v);
         }
         finish_sum(seen ? ref + log2f(l) : -INFINITY);
+        // a row that lost digits to keys or values far larger than its own: the warp's rows again
+        const bool lost = cq * up(sh.held[(n - 1) & 7][0]) > kFarLogits || (ev_was > 15 && top_o < l * kFarValues);
+        if (__any_sync(0xffffffffu, real && seen && lost))
+          plain_rows<D, NG>(bp, sq, b, h, r0, first, tiles, apart ? record : nullptr, record_ref);
       }
     }
   }

@@ -73,7 +73,8 @@ def test_rows_of_constants(c, mix, new, dtype, out, group):
 
 
 @pytest.mark.parametrize("size", [1e5, 1e7, 1e8, 3e8, 1e9, 1e10, 1e12, 1e15, 1e20])
-@pytest.mark.parametrize("n,new,dtype,out", [(300, 1, "bf16", "bf16"), (300, 1, "f16", "f32"), (300, 3, "bf16", "f32"), (4000, 1, "bf16", "f32")])
+@pytest.mark.parametrize("n,new,dtype,out", [(300, 1, "bf16", "bf16"), (300, 1, "f16", "f32"), (300, 3, "bf16", "f32"), (4000, 1, "bf16", "f32"),
+                                             (300, 20, "bf16", "bf16"), (3100, 12, "f16", "f16"), (300, 70, "bf16", "bf16")])
 def test_logits_of_any_size(size, n, new, dtype, out):
     """One key's logit is past what fp32 counts in ones, another's as far below: the output is the one's value.  Its
     weight times the group's scale is rounded to 11 bits, times a code at most the row's range, then the output; the log-sum-exp is the logit, 128 products and
@@ -94,3 +95,33 @@ def test_logits_of_any_size(size, n, new, dtype, out):
     assert ((o.float() - win).abs() <= tol).all()
     logit = (q.double() * kk[0, 0, n // 3].double()).sum(-1) * 128 ** -0.5
     assert ((lse.double() - logit).abs() <= 129 * 2.0 ** -23 * logit.abs()).all()
+
+
+@pytest.mark.parametrize("k_size,v_size", [(1.0, 1e12), (1e12, 1.0), (3e8, 1e30), (1e-14, 1e-14)])
+@pytest.mark.parametrize("n,new,window,at", [
+    (150, 30, 0, 140),             # a later token of the chunk: the queries before it do not see it
+    (150, 30, 10, 125),            # one that leaves the window: the queries after it do not
+    (3100, 12, 0, 3095),           # the same with the positions in parts
+    (300, 70, 40, 233),            # blocks of 256 rows
+])
+def test_blocks_beside_a_token_of_another_size(n, new, window, at, k_size, v_size):
+    """One token's key and value are far larger (or smaller) than the others': queries that do not see it, in the same
+    block of rows, are as exact as ever.  Tolerance as in test_paged_attn_gpu.py, by what each query sees."""
+    rng = np.random.default_rng(91)
+    k, v = rng.standard_normal((n, 1, 128)), rng.standard_normal((n, 1, 128))
+    k[at] *= k_size
+    v[at] *= v_size
+    k, v = (torch.from_numpy(x.astype(np.float32)).cuda() for x in (k, v))
+    cache = filled(k, v)
+    ln = torch.tensor([n], dtype=torch.int32, device="cuda")
+    kk, vv = (torch.empty((1, 1, n, 128), device="cuda") for _ in range(2))
+    R.reskv_paged_gather(cache, ln, kk, vv)
+    q, q64 = as_type(rng.standard_normal((new, 4, 128)), "bf16")
+    o, lse = torch.full_like(q, float("nan")), torch.empty((new, 4), device="cuda")
+    R.reskv_paged_attn(cache, q, ln, o, lse=lse, window=window)
+    cache.check_status()
+    ref = po.attend(q64, kk[0].double().cpu().numpy(), vv[0].double().cpu().numpy(), 4, 128 ** -0.5, window)
+    check(o, lse, [ref], 128, "bf16")
+    again = torch.empty_like(o)
+    R.reskv_paged_attn(cache, q, ln, again, window=window)
+    assert torch.equal(o, again)
