@@ -1,9 +1,9 @@
 """Compile the CUDA library in-tree for sm_103a (nvcc, no cmake).
 
 ``build()`` compiles every translation unit of ``csrc/`` in parallel and links
-``libreskv.so`` beside this file, and ``_bind.so``, the small calls' way to it from
-torch tensors (host C++).  Objects go to ``_build/``.  All are git-ignored build
-products.
+``libreskv.so`` beside this file, and, where torch is installed, ``_bind.so``, the
+small calls' way to it from torch tensors (host C++).  Objects go to ``_build/``.
+All are git-ignored build products.
 """
 from __future__ import annotations
 
@@ -62,7 +62,10 @@ def _compile(src: str, verbose: bool) -> str:
 
 def _bind(force: bool) -> None:
     src = os.path.join(CSRC, "bind.cpp")
-    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    spec = importlib.util.find_spec("torch")
+    if spec is None:            # the C library by itself needs none
+        return
+    torch = spec.submodule_search_locations[0]
     if not force and not _stale(BIND, [src, os.path.join(INCLUDE, "reskv.h"), os.path.join(torch, "version.py")]):
         return
     lib = os.path.join(torch, "lib")
