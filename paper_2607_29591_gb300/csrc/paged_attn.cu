@@ -24,6 +24,7 @@ namespace {
 constexpr int kAttnWarps = 15;                      // computing; with the feeding warp 16, of 128 registers
 constexpr int kAttnStages = 2;                    // of a warp's ring
 constexpr int kStageTiles = 2;                    // neighbours within a page, one copy
+constexpr int kSettleStages = 8;                  // taken between two settle()s
 constexpr int kMinTiles = 2;                      // of a piece, before more CTAs are used
 constexpr int kWholeTiles = 135;                  // 9 a warp
 
@@ -446,6 +447,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
           }
         }
         i += abs(count);
+        if (k % kSettleStages == kSettleStages - 1) st.settle();
         __syncwarp();
         if (lane == 0) mbar_arrive(&vacant[stage]);
       }
