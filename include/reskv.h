@@ -660,7 +660,9 @@ reskv_status reskv_paged_gather(const reskv_paged_kv* kv, const int32_t* starts,
  * Roundings: logits are sums of exact products.  The softmax weights are rounded to
  * 11 bits where o is bf16 (22 otherwise).  Where o has 16 bits, q_begin is NULL and
  * a sequence has 48 query rows (its query tokens times heads / n_kv_heads) or more,
- * the tensor cores take 128 at a time, with weights and held values of 11 bits.
+ * the tensor cores take 128 at a time, with weights and held values of 11 bits; rows
+ * whose logits pass 2^17 or so, or that lie beside tokens far larger than all they see,
+ * are formed in fp32, some hundred times slower.
  * The result depends on the split of the work, which depends on batch, n_tokens,
  * lens and the device, but not on the order in which blocks run.
  */

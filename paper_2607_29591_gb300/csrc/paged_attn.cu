@@ -642,11 +642,11 @@ cudaError_t dispatch_rows(const AttnParams& p, int d, int group, int dev, int ct
 
 // Whole blocks of rows (paged_attn_blocks.cu) from kBlockRows rows a sequence on: a
 // block costs the same up to 128, eight rows after eight cost more and more.  At 32,
-// 48 and 64 rows, us: one sequence of 32K 42, 57, 69 against 53, 54, 55; 8 of 8K 70, 94,
-// 120 against 100 at all three; one of 1000 15, 16, 17 against 19, 20, 20.  So it is
-// for bf16 outputs; fp16 ones take the other kernel's two planes, 64 to 50 and 17 to 19
-// at 48 rows of the first and last.  fp32 outputs and sequences of different query counts keep to the other kernel,
-// whose cut is made on the device.
+// 48 and 64 rows, us: one sequence of 32K 46, 61, 73 against 53, 53, 55; 8 of 8K 73, 99,
+// 125 against 97 at all three; one of 1000 17, 19, 20 against 22.  So it is for bf16
+// outputs; fp16 ones take the other kernel's two planes: 69, 114 and 20 at 48 rows against
+// 53, 96 and 22.  fp32 outputs and sequences of different query counts keep to the other
+// kernel, whose cut is made on the device.
 constexpr int kBlockRows = 48;
 bool takes_blocks(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
   if (a->q_begin || a->o.dtype == RESKV_F32 || a->scale < 0.f || kv->batch < 1 || kv->n_kv_heads < 1) return false;

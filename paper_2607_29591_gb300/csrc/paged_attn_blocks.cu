@@ -36,9 +36,9 @@
 // or value leaves of fp16's digits (a token that other rows see, far larger than all it
 // sees) is computed again in fp32, by plain_rows().
 //
-// Bound by the warps' instructions (the schedulers issue in 56 % of the cycles, the
+// Bound by the warps' instructions (the schedulers issue in 57 % of the cycles, the
 // tensor cores work in 29 %): 512 tokens behind 8K (2 sequences, 8 KV heads, 32 query
-// heads, 133 GFLOP) take 220 us, 605 TFLOP/s.  With eight warps that unpacked and took
+// heads, 133 GFLOP) take 219 us, 608 TFLOP/s.  With eight warps that unpacked and took
 // the softmax in turn, between two barriers of the whole block, it was 357 us; with
 // the roles apart 280; with exponents in warps of their own, and weights formed
 // before a largest logit is looked for, 218.

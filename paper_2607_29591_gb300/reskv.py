@@ -845,7 +845,8 @@ def reskv_paged_attn(kv: PagedKV, q, lens, o, q_begin=None, scale: Optional[floa
     q: bf16 or f16 [T, heads, d], sequence b's query tokens rows q_begin[b] ..
     q_begin[b + 1] - 1 (int32 [batch + 1]; None: T / batch each), the last of the
     lens[b] tokens it holds; o: [T, heads, d] of q's dtype or float32.  window:
-    positions a query sees, itself included (0: all).  lse: float32 [T, heads]
+    positions a query sees, itself included (0: all).  scale: of the logits (None
+    or 0: 1 / sqrt(d)).  lse: float32 [T, heads]
     for ln sum exp, or None.  workspace: zeroed uint8 tensor of at least
     reskv_paged_attn_workspace() bytes (None: one kept per stream); a call that is
     captured into a graph brings its own.
