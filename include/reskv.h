@@ -695,6 +695,98 @@ size_t reskv_paged_attn_workspace(const reskv_paged_kv* kv, const reskv_paged_at
 reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* args,
                               void* stream);
 
+/*
+ * Sequences that begin with the same tokens attend to one copy of them: reskv_paged_attn
+ * with every position of a prefix seen first.  The sequences of `kv` (batch of them, their
+ * own tokens behind the prefix, as reskv_paged_attn has them) form prefix->batch groups;
+ * group g is sequences seq_begin[g] .. seq_begin[g+1] - 1 and all their query tokens see
+ * positions 0 .. prefix_lens[g] - 1 of row g of prefix->page_table, then, as always, the own
+ * positions up to their own.  Query i of n_b stands at own position p = lens[b] - n_b + i; one
+ * with p < 0 sees the prefix alone; one that sees nothing gets o = 0.  A prefix's pages are read
+ * and unpacked once for 128 or 256 rows (query tokens times heads / n_kv_heads) of a group,
+ * not once for every sequence.
+ *
+ * kv and prefix have the same head shape, page_tokens and quant_group, and may share their
+ * pages.  Positions are the caller's matter (keys are held rotated).  args is
+ * reskv_paged_attn's with window 0.  A prefix_lens[g] outside the table is a fault and taken
+ * as the nearest; a seq_begin that is out of order or outside [0, batch] likewise; the
+ * queries of a sequence of no group see their own tokens alone.  Faults go to kv's and
+ * prefix's status words.  Limits and roundings are reskv_paged_attn's; both parts are
+ * joined in fp32.
+ *   seq_begin   : device int32 [prefix->batch + 1], ascending; NULL: batch / prefix->batch each
+ *   prefix_lens : device int32 [prefix->batch]
+ * Workspace as in reskv_paged_attn (the same one may serve both), of at least
+ * reskv_paged_attn_shared_workspace() bytes, which depends on what the other depends on and
+ * on prefix's table.
+ */
+size_t reskv_paged_attn_shared_workspace(const reskv_paged_kv* kv, const reskv_paged_kv* prefix,
+                                         const reskv_paged_attn_args* args);
+
+reskv_status reskv_paged_attn_shared(const reskv_paged_kv* kv, const reskv_paged_kv* prefix,
+                                     const int32_t* seq_begin, const int32_t* prefix_lens,
+                                     const reskv_paged_attn_args* args, void* stream);
+
+/*
+ * Attention to states of another length, such as an encoder's (cross attention): every
+ * query token of sequence b sees the first kv_lens[b] of the sequence's rows of k and v,
+ * whatever its place.  Query head h attends with KV head h / (heads / n_kv_heads):
+ *   x_j = scale <q, k_j>,  o = sum_j softmax_j(x) v_j,  lse = ln sum_j exp(x_j)
+ * A query that sees nothing gets o = 0 and lse = -inf.  Tokens of several beams that read
+ * the same states are query tokens of one sequence; their states are read once.
+ *
+ * Rows that nobody sees (behind kv_lens[b], between sequences) may hold anything, NaN too.
+ * Query tokens of no sequence are neither read nor written.  Logits are sums of exact
+ * products in fp32; statistics and sums are fp32.  The softmax weights are rounded to
+ * q's type before they meet the values (16 bits or more with up to 16 query rows a
+ * sequence and KV head): half a step of a weight, beside the half step of the output.
+ * A fault (q_begin or kv_begin out of order or outside the rows, kv_lens outside the
+ * sequence's rows) is reported and the value taken as the nearest.  Rows on 16-byte
+ * boundaries (data and strides) take the fast kernels; others a general one, some
+ * hundred times slower.
+ * The result depends on shapes and lengths, not on the order in which blocks run.
+ */
+typedef struct reskv_cross_attn_args {
+  reskv_heads q;                       /* [n_tokens, heads, d] bf16 or fp16; heads a multiple
+                                          of k's, at most 64 per KV head       */
+  reskv_heads k, v;                    /* [n_rows, n_kv_heads, d], q's dtype   */
+  reskv_heads o;                       /* q's shape and dtype, not overlapping q, k or v */
+  float* lse;                          /* device fp32 [n_tokens, heads] or NULL */
+  const int32_t* q_begin;              /* device int32 [batch + 1], ascending: tokens
+                                          q_begin[b] .. q_begin[b+1] - 1 are sequence b's;
+                                          NULL: n_tokens / batch each          */
+  const int32_t* kv_begin;             /* the same of the rows of k and v; NULL: n_rows / batch */
+  const int32_t* kv_lens;              /* device int32 [batch]; NULL: all rows of a sequence */
+  int64_t n_tokens, n_rows;            /* n_tokens * heads and n_rows * n_kv_heads below 2^31 */
+  int32_t batch;
+  int32_t head_dim;                    /* 64 or 128                            */
+  float scale;                         /* 0: 1 / sqrt(head_dim)                */
+  uint32_t* status;                    /* device word for faults, or NULL      */
+  void* workspace;                     /* reskv_cross_attn_backward: device, 256-byte aligned, any
+                                          contents; its first 1024 bytes are left as they are, so
+                                          that one of reskv_paged_attn's may serve, too.  Calls that
+                                          share one must be ordered.  Else unused */
+  size_t workspace_bytes;              /* at least reskv_cross_attn_workspace() */
+} reskv_cross_attn_args;
+
+reskv_status reskv_cross_attn(const reskv_cross_attn_args* args, void* stream);
+
+/* Workspace bytes of reskv_cross_attn_backward; depends on n_tokens and q's heads. */
+size_t reskv_cross_attn_workspace(const reskv_cross_attn_args* args);
+
+/*
+ * The gradient of reskv_cross_attn: args with the o and lse that it wrote (both read), d_o the
+ * gradient of o.  With p_j = exp(x_j - lse), D = <d_o, o> and t_j = p_j (<d_o, v_j> - D):
+ *   d_v_j = sum p_j d_o,  d_q = scale sum_j t_j k_j,  d_k_j = scale sum t_j q
+ * the sums of d_k and d_v over the sequence's queries and the heads of the KV head.  Rows of a
+ * sequence behind kv_lens[b], or that no query sees, get d_k = d_v = 0; rows of no sequence are
+ * left as they were.  Sums are fp32 in a fixed order (no atomics); p and t are rounded to q's type before
+ * the products that sum them.
+ *   d_o, d_q : q's shape and dtype;  d_k, d_v : k's shape and dtype
+ */
+reskv_status reskv_cross_attn_backward(const reskv_cross_attn_args* args, const reskv_heads* d_o,
+                                       const reskv_heads* d_q, const reskv_heads* d_k,
+                                       const reskv_heads* d_v, void* stream);
+
 /* 1 while `stream` is being captured into a graph, else 0.  For callers that would
  * make a workspace on demand: what is zeroed during a capture is not zeroed until the
  * graph runs, and graphs that share a workspace must be ordered like calls, so a

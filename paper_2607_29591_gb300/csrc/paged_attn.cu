@@ -377,8 +377,8 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
 #pragma unroll 1
     for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
       const Sequence s = sequence_of(p, b);
-      if (s.len >= s.count) continue;
-      const int64_t rows = int64_t(s.count - s.len) * p.group;
+      if (position_of(p, s, 0) >= 0) continue;
+      const int64_t rows = int64_t(s.count - s.len) * p.group;       // (of a group: it has no positions)
       const int r1 = s.len == 0 ? int(rows) : int(rows / kRows) * kRows;
 #pragma unroll 1
       for (int64_t i = lane; i < int64_t(r1) * p.kv_heads * (D / 4); i += 32) {
@@ -416,11 +416,11 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
       int lo[2], hi[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        hi[j] = c.s.len - c.s.count + min(c.r0 + st.row(j), rows - 1) / p.group;
+        hi[j] = position_of(p, c.s, min(c.r0 + st.row(j), rows - 1) / p.group);
         lo[j] = first_seen(p, hi[j]);
       }
-      const int all_hi = c.s.len - c.s.count + c.r0 / p.group;
-      const int last = c.s.len - c.s.count + min(c.r0 + kRows - 1, rows - 1) / p.group;
+      const int all_hi = position_of(p, c.s, c.r0 / p.group);
+      const int last = position_of(p, c.s, min(c.r0 + kRows - 1, rows - 1) / p.group);
       const int all_lo = first_seen(p, last);
       st.reset();
 #pragma unroll 1
@@ -657,7 +657,14 @@ BlockPlan block_plan(const reskv_paged_kv* kv, const reskv_paged_attn_args* a, i
                           int64_t(kv->table_pages) * kv->page_tokens, sms);
 }
 
-std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
+cudaError_t device_sms(int* dev, int* sms) {
+  const cudaError_t err = cudaGetDevice(dev);
+  if (err != cudaSuccess) return err;
+  *sms = sm_count(*dev);
+  return *sms < 1 ? cudaErrorInvalidDevice : cudaSuccess;
+}
+
+std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a, size_t workspace) {
   std::string bad = check_paged(kv);
   if (!bad.empty()) return bad;
   if (!a) return "args is NULL";
@@ -677,10 +684,75 @@ std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a)
     return "n_tokens * heads / 4 + batch * n_kv_heads must be below 2^24";
   if (!a->q_begin && a->n_tokens % kv->batch) return "n_tokens must be a multiple of batch without q_begin";
   if (a->lse && !aligned_to(a->lse, 4)) return "lse must be 4-byte aligned";
-  if (!a->workspace || !aligned_to(a->workspace, 256) || a->workspace_bytes < reskv_paged_attn_workspace(kv, a))
-    return "workspace must be 256-byte aligned and hold reskv_paged_attn_workspace() bytes";
+  if (!a->workspace || !aligned_to(a->workspace, 256) || a->workspace_bytes < workspace)
+    return "workspace must be 256-byte aligned and hold the bytes that the call's _workspace() asks for";
   if (!std::isfinite(a->scale) || a->window < 0) return "scale must be finite and window not negative";
   return "";
+}
+
+AttnParams attn_params(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
+  AttnParams p{};
+  p.q = a->q.data;
+  p.o = a->o.data;
+  p.lse = a->lse;
+  p.q_token = a->q.token_stride;
+  p.q_head = a->q.head_stride;
+  p.o_token = a->o.token_stride;
+  p.o_head = a->o.head_stride;
+  p.q_begin = a->q_begin;
+  p.lens = a->lens;
+  p.page_table = kv->page_table;
+  p.pages = static_cast<const uint8_t*>(kv->pages);
+  p.status = kv->status;
+  p.n_pages = kv->n_pages;
+  p.n_tokens = a->n_tokens;
+  p.batch = kv->batch;
+  p.table_pages = kv->table_pages;
+  p.page_tokens = kv->page_tokens;
+  p.kv_heads = kv->n_kv_heads;
+  p.heads = a->q.n_heads;
+  p.window = a->window;
+  p.o_f32 = a->o.dtype == RESKV_F32;
+  p.scale2 = (a->scale != 0.f ? a->scale : 1.f / std::sqrt(float(kv->head_dim))) * kLog2e;
+  p.group = p.heads / p.kv_heads;
+  p.q_f16 = a->q.dtype == RESKV_F16;
+  p.q_wide = rows_aligned(a->q, 16);
+  p.o_wide = rows_aligned(a->o, size_t(4 * dtype_size(a->o.dtype)));
+  p.lse_unit = 0.693147180559945f;
+  p.tickets = static_cast<int32_t*>(a->workspace);
+  p.partials = reinterpret_cast<float*>(static_cast<char*>(a->workspace) + kTicketBytes);
+  return p;
+}
+
+// The kernel of few rows, in launches of kMaxBatch sequences (or groups).  `one`: weights in
+// one fp16 plane (2^-11), finer than bf16's 2^-8.  Four rows a unit where a sequence has no more on average.
+cudaError_t attn_rows(const AttnParams& p, const reskv_paged_kv* kv, bool one, int dev, int ctas, cudaStream_t s) {
+  if (ctas > kMaxCtas) ctas = kMaxCtas;
+  const bool few = p.n_tokens * p.group <= 4 * int64_t(p.batch);
+  const int64_t each = p.n_tokens / p.batch;       // query tokens a sequence without q_begin
+  cudaError_t err = cudaSuccess;
+  for (int b0 = 0; b0 < p.batch && err == cudaSuccess; b0 += kMaxBatch) {
+    AttnParams l = p;
+    l.batch = p.batch - b0 < kMaxBatch ? p.batch - b0 : kMaxBatch;
+    l.lens += b0;
+    l.page_table += int64_t(b0) * p.table_pages;
+    if (p.members) {
+      // one launch holds all groups
+    } else if (p.q_begin) {
+      l.q_begin += b0;
+    } else {
+      const int64_t t0 = b0 * each;
+      l.n_tokens = l.batch * each;
+      l.q = static_cast<const char*>(p.q) + t0 * p.q_token * 2;
+      l.o = static_cast<char*>(p.o) + t0 * p.o_token * (p.o_f32 ? 4 : 2);
+      if (p.lse) l.lse = p.lse + t0 * p.heads;
+    }
+    err = one ? (few ? dispatch_rows<false, 4>(l, kv->head_dim, kv->quant_group, dev, ctas, s)
+                     : dispatch_rows<false, 8>(l, kv->head_dim, kv->quant_group, dev, ctas, s))
+              : (few ? dispatch_rows<true, 4>(l, kv->head_dim, kv->quant_group, dev, ctas, s)
+                     : dispatch_rows<true, 8>(l, kv->head_dim, kv->quant_group, dev, ctas, s));
+  }
+  return err;
 }
 
 }  // namespace
@@ -703,72 +775,153 @@ extern "C" size_t reskv_paged_attn_workspace(const reskv_paged_kv* kv, const res
 extern "C" reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a, void* stream) {
   return no_throw([&]() -> reskv_status {
     if (a && a->n_tokens == 0) return RESKV_OK;
-    const std::string bad = check_attn(kv, a);
+    const std::string bad = check_attn(kv, a, reskv_paged_attn_workspace(kv, a));
     if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
-    AttnParams p{};
-    p.q = a->q.data;
-    p.o = a->o.data;
-    p.lse = a->lse;
-    p.q_token = a->q.token_stride;
-    p.q_head = a->q.head_stride;
-    p.o_token = a->o.token_stride;
-    p.o_head = a->o.head_stride;
-    p.q_begin = a->q_begin;
-    p.lens = a->lens;
-    p.page_table = kv->page_table;
-    p.pages = static_cast<const uint8_t*>(kv->pages);
-    p.status = kv->status;
-    p.n_pages = kv->n_pages;
-    p.n_tokens = a->n_tokens;
-    p.batch = kv->batch;
-    p.table_pages = kv->table_pages;
-    p.page_tokens = kv->page_tokens;
-    p.kv_heads = kv->n_kv_heads;
-    p.heads = a->q.n_heads;
-    p.window = a->window;
-    p.o_f32 = a->o.dtype == RESKV_F32;
-    p.scale2 = (a->scale != 0.f ? a->scale : 1.f / std::sqrt(float(kv->head_dim))) * kLog2e;
-    p.group = p.heads / p.kv_heads;
-    p.q_f16 = a->q.dtype == RESKV_F16;
-    p.q_wide = rows_aligned(a->q, 16);
-    p.o_wide = rows_aligned(a->o, size_t(4 * dtype_size(a->o.dtype)));
-    p.tickets = static_cast<int32_t*>(a->workspace);
-    p.partials = reinterpret_cast<float*>(static_cast<char*>(a->workspace) + kTicketBytes);
-    int dev = 0;
-    cudaError_t err = cudaGetDevice(&dev);
+    const AttnParams p = attn_params(kv, a);
+    int dev = 0, sms = 0;
+    const cudaError_t err = device_sms(&dev, &sms);
     if (err != cudaSuccess) return launch_result(err, "reading the device");
-    int ctas = sm_count(dev);
-    if (ctas < 1) return launch_result(cudaErrorInvalidDevice, "reading the SM count");
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (takes_blocks(kv, a)) {
-      const BlockPlan plan = block_plan(kv, a, ctas);
-      return launch_result(launch_attn_blocks(p, plan, kv->head_dim, kv->quant_group, dev, p.partials, s), "paged attention");
-    }
-    if (ctas > kMaxCtas) ctas = kMaxCtas;
-    // bf16 outputs: weights in one fp16 plane (2^-11) are finer than the output's 2^-8.
-    // Four rows a unit where a sequence has no more on average.
-    const bool one = a->o.dtype == RESKV_BF16, few = a->n_tokens * p.group <= 4 * int64_t(kv->batch);
-    const int64_t each = a->n_tokens / kv->batch;    // query tokens a sequence without q_begin
-    for (int b0 = 0; b0 < kv->batch && err == cudaSuccess; b0 += kMaxBatch) {
-      AttnParams l = p;
-      l.batch = kv->batch - b0 < kMaxBatch ? kv->batch - b0 : kMaxBatch;
-      l.lens += b0;
-      l.page_table += int64_t(b0) * p.table_pages;
-      if (p.q_begin) {
-        l.q_begin += b0;
-      } else {
-        const int64_t t0 = b0 * each;
-        l.n_tokens = l.batch * each;
-        l.q = static_cast<const char*>(p.q) + t0 * p.q_token * 2;
-        l.o = static_cast<char*>(p.o) + t0 * p.o_token * dtype_size(a->o.dtype);
-        if (p.lse) l.lse = p.lse + t0 * p.heads;
-      }
-      err = one ? (few ? dispatch_rows<false, 4>(l, kv->head_dim, kv->quant_group, dev, ctas, s)
-                       : dispatch_rows<false, 8>(l, kv->head_dim, kv->quant_group, dev, ctas, s))
-                : (few ? dispatch_rows<true, 4>(l, kv->head_dim, kv->quant_group, dev, ctas, s)
-                       : dispatch_rows<true, 8>(l, kv->head_dim, kv->quant_group, dev, ctas, s));
-    }
-    return launch_result(err, "paged attention");
+    if (takes_blocks(kv, a))
+      return launch_result(launch_attn_blocks(p, block_plan(kv, a, sms), kv->head_dim, kv->quant_group, dev, p.partials, s),
+                           "paged attention");
+    return launch_result(attn_rows(p, kv, a->o.dtype == RESKV_BF16, dev, sms, s), "paged attention");
+  });
+}
+
+// --- a shared prefix ---
+// Two passes, each with the kernel that its rows are for, into fp32 rows and sums, and a join.
+namespace reskv {
+namespace {
+
+// The prefix in blocks of rows: as in takes_blocks, by the mean rows of a group.
+bool prefix_in_blocks(const reskv_paged_kv* prefix, const reskv_paged_attn_args* a) {
+  return a->o.dtype != RESKV_F32 && a->scale >= 0.f && double(a->n_tokens) * a->q.n_heads / prefix->n_kv_heads >= double(kBlockRows) * prefix->batch;
+}
+// Blocks of 128 rows a CTA takes.
+int prefix_mt(const reskv_paged_kv* prefix, const reskv_paged_attn_args* a) {
+  return a->n_tokens * (a->q.n_heads / prefix->n_kv_heads) > 128 * int64_t(prefix->batch) ? 2 : 1;
+}
+
+struct SharedLayout {             // of the workspace, in bytes from its start
+  size_t own, own_ref, prefix, prefix_ref, bytes;
+};
+size_t padded(size_t n) { return (n + 255) / 256 * 256; }
+SharedLayout shared_layout(const reskv_paged_kv* kv, const reskv_paged_kv* prefix, const reskv_paged_attn_args* a, int sms) {
+  const size_t rows = size_t(a->n_tokens) * a->q.n_heads;
+  size_t records = size_t(kMaxCtas) * 2 * (record_floats(kv->head_dim, 8) + 8) * 4;
+  if (takes_blocks(kv, a)) {
+    const size_t more = attn_blocks_bytes(block_plan(kv, a, sms), kv->head_dim);
+    if (more > records) records = more;
+  }
+  SharedLayout l{};
+  l.own = padded(kTicketBytes + records);
+  l.own_ref = l.own + padded(rows * kv->head_dim * 4);
+  l.prefix = l.own_ref + padded(rows * 4);
+  if (prefix_in_blocks(prefix, a)) {
+    const int block = 128 * prefix_mt(prefix, a);
+    const size_t items = size_t(group_items(a->n_tokens * (a->q.n_heads / kv->n_kv_heads), prefix->batch, kv->n_kv_heads, block, sms));
+    l.prefix_ref = l.prefix + padded(items * block * kv->head_dim * 4);
+    l.bytes = l.prefix_ref + padded(items * block * 4);
+  } else {
+    l.prefix_ref = l.prefix + padded(rows * kv->head_dim * 4);
+    l.bytes = l.prefix_ref + padded(rows * 4);
+  }
+  return l;
+}
+
+std::string check_shared(const reskv_paged_kv* kv, const reskv_paged_kv* prefix, const int32_t* seq_begin,
+                         const int32_t* prefix_lens, const reskv_paged_attn_args* a) {
+  std::string bad = check_paged(prefix);
+  if (!bad.empty()) return "the prefix: " + bad;
+  bad = check_attn(kv, a, reskv_paged_attn_shared_workspace(kv, prefix, a));
+  if (!bad.empty()) return bad;
+  if (prefix->head_dim != kv->head_dim || prefix->n_kv_heads != kv->n_kv_heads || prefix->quant_group != kv->quant_group ||
+      prefix->page_tokens != kv->page_tokens)
+    return "the prefix must have the cache's head_dim, n_kv_heads, quant_group and page_tokens";
+  if (!prefix_lens) return "prefix_lens is NULL";
+  if (!seq_begin && kv->batch % prefix->batch) return "batch must be a multiple of the prefixes without seq_begin";
+  if (a->window != 0) return "window must be 0";
+  if (prefix->batch > kMaxBatch) return "at most 1024 prefixes a call";
+  if ((double(a->n_tokens) * (a->q.n_heads / kv->n_kv_heads) / 4 + prefix->batch) * kv->n_kv_heads >= double(1 << kUnitBits))
+    return "n_tokens * heads / 4 + prefixes * n_kv_heads must be below 2^24";
+  return "";
+}
+
+}  // namespace
+}  // namespace reskv
+
+extern "C" size_t reskv_paged_attn_shared_workspace(const reskv_paged_kv* kv, const reskv_paged_kv* prefix,
+                                                    const reskv_paged_attn_args* a) {
+  if (!kv || !prefix || !a || (kv->head_dim != 64 && kv->head_dim != 128) || kv->batch < 1 || kv->n_kv_heads < 1 ||
+      prefix->batch < 1 || prefix->n_kv_heads != kv->n_kv_heads || a->n_tokens < 0 || a->q.n_heads < 1)
+    return 0;
+  int dev = 0, sms = 0;
+  if (device_sms(&dev, &sms) != cudaSuccess) cudaGetLastError();
+  return shared_layout(kv, prefix, a, sms).bytes;
+}
+
+extern "C" reskv_status reskv_paged_attn_shared(const reskv_paged_kv* kv, const reskv_paged_kv* prefix, const int32_t* seq_begin,
+                                                const int32_t* prefix_lens, const reskv_paged_attn_args* a, void* stream) {
+  return no_throw([&]() -> reskv_status {
+    if (a && a->n_tokens == 0) return RESKV_OK;
+    const std::string bad = check_shared(kv, prefix, seq_begin, prefix_lens, a);
+    if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
+    int dev = 0, sms = 0;
+    cudaError_t err = device_sms(&dev, &sms);
+    if (err != cudaSuccess) return launch_result(err, "reading the device");
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const SharedLayout l = shared_layout(kv, prefix, a, sms);
+    char* ws = static_cast<char*>(a->workspace);
+    const bool one = a->o.dtype == RESKV_BF16;
+    // the own tokens into fp32 rows [token][head][dim]
+    const AttnParams call = attn_params(kv, a);
+    AttnParams p = call;
+    p.o = ws + l.own;
+    p.lse = reinterpret_cast<float*>(ws + l.own_ref);
+    p.o_f32 = p.o_wide = 1;
+    p.o_head = kv->head_dim;
+    p.o_token = int64_t(p.heads) * kv->head_dim;
+    p.lse_unit = 1.f;
+    err = takes_blocks(kv, a) ? launch_attn_blocks(p, block_plan(kv, a, sms), kv->head_dim, kv->quant_group, dev, p.partials, s)
+                              : attn_rows(p, kv, one, dev, sms, s);
+    // the prefix: a group's query tokens are one sequence's that all see all
+    p.lens = prefix_lens;
+    p.page_table = prefix->page_table;
+    p.pages = static_cast<const uint8_t*>(prefix->pages);
+    p.status = prefix->status;
+    p.n_pages = prefix->n_pages;
+    p.batch = prefix->batch;
+    p.table_pages = prefix->table_pages;
+    p.seq_begin = seq_begin;
+    p.members = kv->batch;
+    const bool blocks = prefix_in_blocks(prefix, a);
+    const int mt = prefix_mt(prefix, a);
+    p.o = ws + l.prefix;
+    p.lse = reinterpret_cast<float*>(ws + l.prefix_ref);
+    const int items = int(group_items(p.n_tokens * p.group, p.batch, p.kv_heads, 128 * mt, sms));
+    if (err == cudaSuccess)
+      err = blocks ? launch_attn_groups(p, mt, items, sms, kv->head_dim, kv->quant_group, dev, static_cast<float*>(p.o), s)
+                   : attn_rows(p, prefix, one, dev, sms, s);
+    SharedJoin j{};
+    j.a = p;
+    j.a.o = call.o;
+    j.a.lse = call.lse;
+    j.a.o_token = call.o_token;
+    j.a.o_head = call.o_head;
+    j.a.o_f32 = call.o_f32;
+    j.a.o_wide = call.o_wide;
+    j.a.lse_unit = call.lse_unit;
+    j.own = reinterpret_cast<const float*>(ws + l.own);
+    j.own_ref = reinterpret_cast<const float*>(ws + l.own_ref);
+    j.prefix = reinterpret_cast<const float*>(ws + l.prefix);
+    j.prefix_ref = reinterpret_cast<const float*>(ws + l.prefix_ref);
+    j.block_rows = blocks ? 128 * mt : 0;
+    j.items = items;
+    j.ctas = sms;
+    j.dim = kv->head_dim;
+    if (err == cudaSuccess) err = launch_shared_join(j, s);
+    return launch_result(err, "attention with a shared prefix");
   });
 }
 

@@ -22,6 +22,11 @@ struct AttnParams {
   int32_t batch, table_pages, page_tokens, kv_heads, heads, group;
   int32_t window, q_f16, o_f32, q_wide, o_wide;
   float scale2;                   // scale * log2 e
+  float lse_unit;                 // what lse holds of a log2 of a sum: ln 2 of it, or all
+  // A prefix that groups of sequences share: `batch` groups of `members` sequences, whose
+  // query tokens all see all of the group's positions (members 0: neither).
+  const int32_t* seq_begin;
+  int32_t members;
 };
 
 // One block of query rows of one sequence: row r of the sequence is query token
@@ -37,7 +42,27 @@ struct Sequence {
 
 __device__ __forceinline__ Sequence sequence_of(const AttnParams& p, int b) {
   Sequence s;
-  if (p.q_begin) {
+  if (p.members) {
+    int s0, s1;
+    if (p.seq_begin) {
+      s0 = p.seq_begin[b];
+      s1 = p.seq_begin[b + 1];
+      if (s0 < 0 || s0 > p.members || s1 < s0 || s1 > p.members) report_status(p.status, kStatusBadIndex);
+      s0 = min(max(s0, 0), p.members);
+      s1 = min(max(s1, s0), p.members);
+    } else {
+      const int each = p.members / p.batch;
+      s0 = b * each;
+      s1 = s0 + each;
+    }
+    int64_t t0 = s0 * (p.n_tokens / p.members), t1 = s1 * (p.n_tokens / p.members);
+    if (p.q_begin) {
+      t0 = min(max(int64_t(p.q_begin[s0]), int64_t(0)), p.n_tokens);
+      t1 = min(max(int64_t(p.q_begin[s1]), t0), p.n_tokens);
+    }
+    s.q0 = int(t0);
+    s.count = int(t1 - t0);
+  } else if (p.q_begin) {
     const int64_t lo = min(max(int64_t(p.q_begin[b]), int64_t(0)), p.n_tokens);
     const int64_t hi = min(max(int64_t(p.q_begin[b + 1]), lo), p.n_tokens);
     s.q0 = int(lo);
@@ -53,6 +78,11 @@ __device__ __forceinline__ Sequence sequence_of(const AttnParams& p, int b) {
   return s;
 }
 
+// Position of a sequence's query token i, the last that it sees.
+__device__ __forceinline__ int position_of(const AttnParams& p, const Sequence& s, int i) {
+  return p.members ? s.len - 1 : s.len - s.count + i;
+}
+
 // First position that a query at `pos` sees (pos may lie far below 0, a window be any).
 __device__ __forceinline__ int first_seen(const AttnParams& p, int pos) {
   return p.window > 0 && pos >= p.window ? pos - p.window + 1 : 0;
@@ -61,8 +91,8 @@ __device__ __forceinline__ int first_seen(const AttnParams& p, int pos) {
 // Rows [r0, r1) of a sequence.
 __device__ __forceinline__ RowBlock row_block(const AttnParams& p, const Sequence& s, int r0, int r1) {
   // (one block of a sequence's rows, the usual case, divides nothing)
-  const int lo = s.len - s.count + (r0 == 0 ? 0 : r0 / p.group);
-  const int hi = s.len - s.count + (r1 == s.count * p.group ? s.count - 1 : (r1 - 1) / p.group);
+  const int lo = position_of(p, s, r0 == 0 ? 0 : r0 / p.group);
+  const int hi = position_of(p, s, r1 == s.count * p.group ? s.count - 1 : (r1 - 1) / p.group);
   RowBlock b;
   b.first = first_seen(p, lo) / kTile;
   b.tiles = hi < 0 ? 0 : hi / kTile - b.first + 1;
@@ -150,7 +180,7 @@ __device__ __forceinline__ void store_out(const AttnParams& p, const Sequence& s
 }
 
 __device__ __forceinline__ void store_lse(const AttnParams& p, const Sequence& s, int h, int r, float ref) {
-  if (p.lse) p.lse[(s.q0 + r / p.group) * int64_t(p.heads) + h * p.group + r % p.group] = ref * 0.693147180559945f;
+  if (p.lse) p.lse[(s.q0 + r / p.group) * int64_t(p.heads) + h * p.group + r % p.group] = ref * p.lse_unit;
 }
 // The softmaxes of up to 32 records joined: each lane's weight for its record's
 // output, from their log2 sums (-inf: an empty or no record), the records that are none
@@ -610,6 +640,110 @@ struct BlockPlan {
 };
 BlockPlan plan_attn_blocks(int64_t rows, int batch, int kv_heads, int64_t capacity, int sms);
 size_t attn_blocks_bytes(const BlockPlan& plan, int d);              // of records, where parts are joined
+
+// --- a prefix shared by groups of sequences: paged_attn_blocks.cu, paged_shared.cu ---
+// Units are blocks of 128 mt rows of a KV head and group.  How many rows and positions a
+// group has only the device knows, so it makes the plan: where units do not fill the SMs
+// their positions are cut into parts of about equal steps.  Part k of unit (group, head,
+// block) is item first + (head * parts + k) * row_blocks + block, CTA and record alike.
+struct GroupPlan {
+  int group;                      // the group, or -1
+  Sequence s;
+  int first, row_blocks, parts;   // of its items; parts 0: nothing to see
+};
+constexpr int kBlockPos = 64;     // positions of a step
+constexpr int kLeastSteps = 8;    // of a part
+
+// One warp; the same in all its lanes.  For the group of item `item`, or (item < 0) group `group`.
+__device__ __forceinline__ GroupPlan group_plan(const AttnParams& p, int block_rows, int ctas, int item, int group, int lane) {
+  auto units_steps = [&](int g, int& units, int& steps) {
+    units = steps = 0;
+    if (g >= p.batch) return;
+    const Sequence s = sequence_of(p, g);
+    steps = (s.len + kBlockPos - 1) / kBlockPos;
+    if (steps > 0) units = int((int64_t(s.count) * p.group + block_rows - 1) / block_rows) * p.kv_heads;
+  };
+  auto total = [&](int x) { return __reduce_add_sync(0xffffffffu, uint32_t(x)); };
+  // a part's steps: the fewest with which the parts fit the SMs (units that do not: whole)
+  uint32_t units = 0, longest = 0;
+  float work = 0.f;
+#pragma unroll 1
+  for (int g0 = 0; g0 < p.batch; g0 += 32) {
+    int u, n;
+    units_steps(g0 + lane, u, n);
+    units += total(u);
+    longest = max(longest, __reduce_max_sync(0xffffffffu, uint32_t(n)));
+    float w = float(u) * float(n);
+#pragma unroll
+    for (int o = 16; o; o /= 2) w += __shfl_xor_sync(0xffffffffu, w, o);
+    work += w;
+  }
+  uint32_t size = longest;
+  if (units <= uint32_t(ctas)) {
+    size = max(uint32_t(kLeastSteps), uint32_t(ceilf(work / float(ctas))));
+#pragma unroll 1
+    while (size < longest) {
+      uint32_t items = 0;
+#pragma unroll 1
+      for (int g0 = 0; g0 < p.batch; g0 += 32) {
+        int u, n;
+        units_steps(g0 + lane, u, n);
+        items += total(u * int((n + size - 1) / size));
+      }
+      if (items <= uint32_t(ctas)) break;
+      size += max(1u, size / 32);
+    }
+  }
+  size = max(size, 1u);
+  GroupPlan out{-1, {}, 0, 0, 0};
+  int first = 0;
+#pragma unroll 1
+  for (int g0 = 0; g0 < p.batch; g0 += 32) {
+    int u, n;
+    units_steps(g0 + lane, u, n);
+    const int parts = u ? int((n + size - 1) / size) : 0, mine = u * parts;
+    int before = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int x = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += x;
+    }
+    const int all = __shfl_sync(0xffffffffu, before, 31);
+    before = first + before - mine;
+    const bool here = item >= 0 ? item >= before && item < before + mine : g0 + lane == group;
+    const uint32_t who = __ballot_sync(0xffffffffu, here);
+    if (who) {
+      const int l = __ffs(who) - 1;
+      out.group = g0 + l;
+      out.first = __shfl_sync(0xffffffffu, before, l);
+      out.parts = __shfl_sync(0xffffffffu, parts, l);
+      out.row_blocks = __shfl_sync(0xffffffffu, u, l) / p.kv_heads;
+      out.s = sequence_of(p, out.group);
+      return out;
+    }
+    first += all;
+  }
+  return out;
+}
+
+// Items and records that a call may have.
+inline int64_t group_items(int64_t rows, int groups, int kv_heads, int block_rows, int ctas) {
+  const int64_t units = (rows / block_rows + groups) * kv_heads;
+  return units > ctas ? units : ctas;
+}
+cudaError_t launch_attn_groups(const AttnParams& p, int mt, int items, int ctas, int d, int quant_group, int dev, float* records,
+                               cudaStream_t s);
+// The softmaxes over the own tokens (fp32 rows in the order of o, log2 sums) and over
+// the prefix (the same, or records: block_rows > 0) joined into o.
+struct SharedJoin {
+  AttnParams a;                   // the prefix's pass, with the call's o and lse
+  const float* own;
+  const float* own_ref;
+  const float* prefix;
+  const float* prefix_ref;
+  int32_t block_rows, items, ctas, dim;
+};
+cudaError_t launch_shared_join(const SharedJoin& j, cudaStream_t s);
 cudaError_t launch_attn_blocks(const AttnParams& p, const BlockPlan& plan, int d, int quant_group, int dev, float* records,
                                cudaStream_t s);
 

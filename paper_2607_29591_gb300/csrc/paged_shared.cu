@@ -1,0 +1,101 @@
+// Attention with a shared prefix (reskv_paged_attn_shared): the join of its two passes.
+//
+// The passes leave, for every query row, the softmax's output over what they saw and the
+// log2 sum of its weights: the own tokens' in one row, the prefix's in one row or, where
+// it was taken in blocks of rows, in one record for each part of its positions.
+// With sums s_k and outputs o_k the output is sum 2^(s_k - S) o_k, S = log2 sum 2^s_k.
+// A warp a row; bound by its reads (fp32 rows that the passes left in L2).
+#include "paged_attn.cuh"
+
+namespace reskv {
+namespace {
+
+constexpr int kWarps = 8;
+
+// Index i with begin[i] <= x < begin[i + 1], or -1.
+__device__ __forceinline__ int range_of(const int32_t* begin, int n, int64_t x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (begin[mid] <= x) lo = mid;
+    else hi = mid;
+  }
+  return begin[lo] <= x && x < begin[lo + 1] ? lo : -1;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kWarps * 32) k_shared_join(const __grid_constant__ SharedJoin j) {
+  const AttnParams& p = j.a;
+  const int lane = threadIdx.x & 31;
+  const int64_t row = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int64_t tok = row / p.heads;
+  const int head = int(row - tok * p.heads);
+  wait_for_previous();
+  if (tok >= p.n_tokens) return;
+  // the sequence, then the group
+  const int seq = p.q_begin ? range_of(p.q_begin, p.members, tok) : int(tok / (p.n_tokens / p.members));
+  if (seq < 0) return;                            // a query of no sequence
+  const int group = p.seq_begin ? range_of(p.seq_begin, p.batch, seq) : seq / (p.members / p.batch);
+  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+  const float own = j.own_ref[row];
+  const bool with_own = own != -INFINITY;
+  float4 a = zero;
+  if (lane < D / 4 && with_own) a = reinterpret_cast<const float4*>(j.own + row * D)[lane];
+  int parts = 0;
+  int64_t first = 0, stride = 0;                  // rows of the prefix's records
+  if (group >= 0 && j.block_rows) {
+    const GroupPlan g = group_plan(p, j.block_rows, j.ctas, -1, group, lane);
+    const int64_t r = (tok - g.s.q0) * p.group + head % p.group;
+    // (of a seq_begin out of order there may be more items than CTAs and records)
+    if (tok >= g.s.q0 && tok < g.s.q0 + g.s.count && g.first + int64_t(g.parts) * g.row_blocks * p.kv_heads <= j.items) {
+      parts = g.parts;
+      stride = int64_t(g.row_blocks) * j.block_rows;
+      first = (g.first + int64_t(head / p.group) * parts * g.row_blocks) * j.block_rows + r;
+    }
+  } else if (group >= 0) {
+    const Sequence s = sequence_of(p, group);
+    if (tok >= s.q0 && tok < s.q0 + s.count) {
+      parts = 1;
+      first = row;
+    }
+  }
+  float top = own;
+#pragma unroll 1
+  for (int k = lane; k < parts; k += 32) top = fmaxf(top, j.prefix_ref[first + k * stride]);
+#pragma unroll
+  for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  // a part of weight 0 still counts: a NaN in it is seen
+  float sum = 0.f;
+  if (with_own) {
+    const float f = exp2f(own - top);
+    sum = f;
+    a = make_float4(a.x * f, a.y * f, a.z * f, a.w * f);
+  }
+#pragma unroll 2
+  for (int k = 0; k < parts; ++k) {
+    const float ref = j.prefix_ref[first + k * stride];
+    if (ref == -INFINITY) continue;
+    const float f = exp2f(ref - top);
+    sum += f;
+    if (lane < D / 4) add_scaled(a, f, reinterpret_cast<const float4*>(j.prefix + (first + k * stride) * D)[lane]);
+  }
+  const bool seen = sum != 0.f;
+  const float inv = seen ? 1.f / sum : 0.f;
+  Sequence at{};
+  at.q0 = int(tok);
+  at.count = 1;
+  const int h = head / p.group, r = head % p.group;
+  if (lane < D / 4) store_out(p, at, h, r, lane, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+  if (lane == 0) store_lse(p, at, h, r, seen ? top + log2f(sum) : -INFINITY);
+}
+
+}  // namespace
+
+cudaError_t launch_shared_join(const SharedJoin& j, cudaStream_t s) {
+  const int64_t rows = j.a.n_tokens * j.a.heads;
+  const unsigned blocks = unsigned((rows + kWarps - 1) / kWarps);
+  return j.dim == 128 ? launch_early(k_shared_join<128>, blocks, kWarps * 32, 0, s, j)
+                      : launch_early(k_shared_join<64>, blocks, kWarps * 32, 0, s, j);
+}
+
+}  // namespace reskv

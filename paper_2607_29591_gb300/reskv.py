@@ -132,6 +132,15 @@ class reskv_paged_attn_args(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t)]
 
 
+class reskv_cross_attn_args(ctypes.Structure):
+    _fields_ = [("q", reskv_heads), ("k", reskv_heads), ("v", reskv_heads), ("o", reskv_heads),
+                ("lse", ctypes.c_void_p), ("q_begin", ctypes.c_void_p), ("kv_begin", ctypes.c_void_p),
+                ("kv_lens", ctypes.c_void_p), ("n_tokens", ctypes.c_int64), ("n_rows", ctypes.c_int64),
+                ("batch", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("status", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
 _lib = None
 
 
@@ -202,6 +211,17 @@ def load_library():
     lib.reskv_paged_attn_workspace.restype = sz
     lib.reskv_paged_attn.argtypes = [kvp, attnp, vp]
     lib.reskv_paged_attn.restype = i32
+    lib.reskv_paged_attn_shared_workspace.argtypes = [kvp, kvp, attnp]
+    lib.reskv_paged_attn_shared_workspace.restype = sz
+    lib.reskv_paged_attn_shared.argtypes = [kvp, kvp, vp, vp, attnp, vp]
+    lib.reskv_paged_attn_shared.restype = i32
+    crossp = ctypes.POINTER(reskv_cross_attn_args)
+    lib.reskv_cross_attn.argtypes = [crossp, vp]
+    lib.reskv_cross_attn.restype = i32
+    lib.reskv_cross_attn_workspace.argtypes = [crossp]
+    lib.reskv_cross_attn_workspace.restype = sz
+    lib.reskv_cross_attn_backward.argtypes = [crossp, headsp, headsp, headsp, headsp, vp]
+    lib.reskv_cross_attn_backward.restype = i32
     _lib = lib
     return lib
 
@@ -559,6 +579,7 @@ _pack_heads = struct.Struct("Pqqii").pack            # reskv_heads
 _pack_rotation = struct.Struct("Pqii").pack          # reskv_rotation
 _pack_rows = struct.Struct("Pqqqi4x").pack           # reskv_rows
 _pack_attn = struct.Struct("PqqiiPqqiiPPPqfiPQ").pack  # reskv_paged_attn_args
+_pack_cross = struct.Struct("PqqiiPqqiiPqqiiPqqiiPPPPqqiif4xPPQ").pack  # reskv_cross_attn_args
 _dtypes = {}
 _kinds = []                 # torch.int32, torch.float32, the current stream's address of a device
 _direct = None
@@ -579,9 +600,12 @@ def _calls():
         lib.reskv_paged_append.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
         lib.reskv_paged_gather.argtypes = [vp, vp, vp, i64, vp, vp, vp]
         lib.reskv_paged_attn.argtypes = [vp, vp, vp]
+        lib.reskv_paged_attn_shared.argtypes = [vp, vp, vp, vp, vp, vp]
+        lib.reskv_cross_attn.argtypes = [vp, vp]
+        lib.reskv_cross_attn_backward.argtypes = [vp, vp, vp, vp, vp, vp]
         lib.reskv_stream_capturing.argtypes = [vp]
         for f in (lib.reskv_rope, lib.reskv_paged_append, lib.reskv_paged_gather, lib.reskv_paged_attn,
-                  lib.reskv_stream_capturing):
+                  lib.reskv_paged_attn_shared, lib.reskv_cross_attn, lib.reskv_cross_attn_backward, lib.reskv_stream_capturing):
             f.restype = i32
         if not os.path.exists(os.path.join(os.path.dirname(LIB_PATH), "_bind.so")):
             raise RuntimeError("_bind.so is missing: build it with `python -m paper_2607_29591_gb300.build` "
@@ -827,6 +851,17 @@ def _workspace(device, stream: int, nbytes: int):
     return held
 
 
+def _kept_workspace(lib, t, stream: int, need: int, size: str):
+    """The workspace kept for the tensor's device and the stream, of `need` bytes at least."""
+    if lib.reskv_stream_capturing(stream):
+        raise ValueError("a call that is captured into a graph needs workspace=: a zeroed uint8 tensor of "
+                         f"{size} bytes, made before the capture")
+    held = _workspaces.get((t.get_device(), stream))
+    if held is None or held[-1].numel() < need:
+        held = _workspace(t.device, stream, need)
+    return held[-1]
+
+
 def _zero_workspaces(device) -> None:
     """Make the kept workspaces of a device ready again, in place: what runs there may hold their addresses."""
     import torch
@@ -852,32 +887,32 @@ def reskv_paged_attn(kv: PagedKV, q, lens, o, q_begin=None, scale: Optional[floa
     captured into a graph brings its own.
     """
     lib = _calls()
+    heads, out = q.shape[1] if q.dim() == 3 else 0, o.dtype
+    s = _stream_of(stream, q)
+    if workspace is None:
+        need = kv.attn_workspace.get((q.shape[0], heads, out))
+        if need is None and out in _dtypes:
+            need = kv.attn_workspace[q.shape[0], heads, out] = reskv_paged_attn_workspace(kv, q.shape[0], heads, out)
+        workspace = _kept_workspace(lib, q, s, need or 0, "reskv_paged_attn_workspace()")
+    st = lib.reskv_paged_attn(kv.address, _attn(kv, q, lens, o, q_begin, scale, window, lse, workspace), s)
+    if st:
+        _check(st)
+
+
+def _attn(kv: PagedKV, q, lens, o, q_begin, scale, window, lse, workspace) -> bytes:
+    """A reskv_paged_attn_args' bytes."""
     T, d, B = q.shape[0], kv.head_dim, kv.batch
     qh = _heads(q, "q", T, None, d)
     oh = _heads(o, "o", T, qh[3], d)
     if lse is not None and lse.numel() != T * qh[3]:
         raise ValueError(f"lse must hold {T * qh[3]} elements, got {lse.numel()}")
-    s = _stream_of(stream, q)
-    if workspace is None:
-        if lib.reskv_stream_capturing(s):
-            raise ValueError("a call that is captured into a graph needs workspace=: a zeroed uint8 tensor of "
-                             "reskv_paged_attn_workspace() bytes, made before the capture")
-        need = kv.attn_workspace.get((T, qh[3], oh[4]))
-        if need is None:
-            need = kv.attn_workspace[T, qh[3], oh[4]] = reskv_paged_attn_workspace(kv, T, qh[3], o.dtype)
-        held = _workspaces.get((q.get_device(), s))
-        if held is None or held[-1].numel() < need:
-            held = _workspace(q.device, s, need)
-        workspace = held[-1]
-    elif not workspace.is_cuda or not workspace.is_contiguous():
+    if not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous CUDA tensor")
-    st = lib.reskv_paged_attn(kv.address, _pack_attn(
+    return _pack_attn(
         *qh, *oh, 0 if lse is None else _dptr(lse, "torch.float32", "lse").value,
         0 if q_begin is None else _ints(q_begin, "q_begin", B + 1), _ints(lens, "lens", B), T,
         0.0 if scale is None else scale, window, workspace.data_ptr(),
-        workspace.numel() * workspace.element_size()), s)
-    if st:
-        _check(st)
+        workspace.numel() * workspace.element_size())
 
 
 def reskv_paged_attn_workspace(kv: PagedKV, n_tokens: int, heads: int, out_dtype=None) -> int:
@@ -889,3 +924,122 @@ def reskv_paged_attn_workspace(kv: PagedKV, n_tokens: int, heads: int, out_dtype
     a.q.n_heads = heads
     a.o.dtype = _dtypes[torch.bfloat16 if out_dtype is None else out_dtype]
     return load_library().reskv_paged_attn_workspace(kv.struct, a)
+
+
+def reskv_paged_attn_shared(kv: PagedKV, prefix: PagedKV, q, lens, prefix_lens, o, seq_begin=None, q_begin=None,
+                            scale: Optional[float] = None, lse=None, workspace=None, stream=None) -> None:
+    """Attention of every sequence's newest tokens over a prefix that its group shares and over
+    its own tokens behind it.
+
+    kv: the sequences' own tokens, of which lens[b] are held; prefix: the prefixes, one a row of
+    its page table, of which prefix_lens[g] positions are held (int32 [prefixes]).  Sequences
+    seq_begin[g] .. seq_begin[g + 1] - 1 share prefix g (int32 [prefixes + 1]; None: equal
+    numbers); one that is in no group sees its own tokens alone.  kv and prefix have one shape and may
+    share their pages.  The other arguments are reskv_paged_attn's; workspace: zeroed, of at
+    least reskv_paged_attn_shared_workspace() bytes (None: one kept per stream).
+    """
+    lib = _calls()
+    s = _stream_of(stream, q)
+    if workspace is None:
+        key = (q.shape[0], q.shape[1] if q.dim() == 3 else 0, o.dtype, prefix.batch, prefix.table_pages)
+        need = kv.attn_workspace.get(key)
+        if need is None and o.dtype in _dtypes:
+            need = kv.attn_workspace[key] = reskv_paged_attn_shared_workspace(kv, prefix, key[0], key[1], o.dtype)
+        workspace = _kept_workspace(lib, q, s, need or 0, "reskv_paged_attn_shared_workspace()")
+    st = lib.reskv_paged_attn_shared(
+        kv.address, prefix.address, None if seq_begin is None else _ints(seq_begin, "seq_begin", prefix.batch + 1),
+        _ints(prefix_lens, "prefix_lens", prefix.batch), _attn(kv, q, lens, o, q_begin, scale, 0, lse, workspace), s)
+    if st:
+        _check(st)
+
+
+def reskv_paged_attn_shared_workspace(kv: PagedKV, prefix: PagedKV, n_tokens: int, heads: int, out_dtype=None) -> int:
+    """Workspace bytes of a reskv_paged_attn_shared call over n_tokens query tokens (outputs of out_dtype;
+    None: 16 bits)."""
+    import torch
+    _calls()
+    a = reskv_paged_attn_args(n_tokens=n_tokens)
+    a.q.n_heads = heads
+    a.o.dtype = _dtypes[torch.bfloat16 if out_dtype is None else out_dtype]
+    return load_library().reskv_paged_attn_shared_workspace(kv.struct, prefix.struct, a)
+
+
+# ---------------------------------------------------------------------------
+# attention to states of another length, and its gradient
+# ---------------------------------------------------------------------------
+
+def _cross(q, k, v, o, batch, q_begin, kv_begin, kv_lens, scale, lse, status, workspace=None) -> bytes:
+    """A reskv_cross_attn_args' bytes."""
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError(f"q and k must be [tokens, heads, dim], got {tuple(q.shape)} and {tuple(k.shape)}")
+    _calls()
+    T, d = q.shape[0], q.shape[2]
+    rows = k.shape[0]
+    qh = _heads(q, "q", T, None, d)
+    kh = _heads(k, "k", rows, None, d)
+    if lse is not None and lse.numel() != T * qh[3]:
+        raise ValueError(f"lse must hold {T * qh[3]} elements, got {lse.numel()}")
+    return _pack_cross(
+        *qh, *kh, *_heads(v, "v", rows, kh[3], d), *_heads(o, "o", T, qh[3], d),
+        0 if lse is None else _dptr(lse, "torch.float32", "lse").value,
+        0 if q_begin is None else _ints(q_begin, "q_begin", batch + 1),
+        0 if kv_begin is None else _ints(kv_begin, "kv_begin", batch + 1),
+        0 if kv_lens is None else _ints(kv_lens, "kv_lens", batch), T, rows, batch, d,
+        0.0 if scale is None else scale, 0 if status is None else _ints(status, "status", 1),
+        0 if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.numel() * workspace.element_size())
+
+
+def reskv_cross_attn(q, k, v, o, batch: int = 1, q_begin=None, kv_begin=None, kv_lens=None,
+                     scale: Optional[float] = None, lse=None, status=None, stream=None) -> None:
+    """Attention of every sequence's query tokens to all of the sequence's states.
+
+    q, o: bf16 or f16 [T, heads, d]; k, v: [rows, n_kv_heads, d] of q's dtype; any token and
+    head strides.  Sequence b's query tokens are rows q_begin[b] .. q_begin[b + 1] - 1 of q
+    (int32 [batch + 1]; None: T / batch each), its states rows kv_begin[b] .. of k and v (likewise),
+    of which the first kv_lens[b] count (int32 [batch]; None: all).  Several beams that read
+    the same states are one sequence.  scale: of the logits (None or 0: 1 / sqrt(d)).  lse:
+    float32 [T, heads] for ln sum exp, which the gradient needs, or None.  status: int32 [1]
+    that begins or lengths outside their range set to 2.
+    """
+    a = _cross(q, k, v, o, batch, q_begin, kv_begin, kv_lens, scale, lse, status)
+    st = _calls().reskv_cross_attn(a, _stream_of(stream, q))
+    if st:
+        _check(st)
+
+
+def reskv_cross_attn_workspace(n_tokens: int, heads: int) -> int:
+    """Workspace bytes of a reskv_cross_attn_backward call."""
+    a = reskv_cross_attn_args(n_tokens=n_tokens)
+    a.q.n_heads = heads
+    return load_library().reskv_cross_attn_workspace(a)
+
+
+def reskv_cross_attn_backward(q, k, v, o, lse, d_o, d_q, d_k, d_v, batch: int = 1, q_begin=None, kv_begin=None,
+                              kv_lens=None, scale: Optional[float] = None, status=None, workspace=None,
+                              stream=None) -> None:
+    """The gradient of reskv_cross_attn: d_q, d_k, d_v from d_o and the o and lse that it wrote.
+
+    d_o, d_q: like q; d_k, d_v: like k (any strides).  Rows of a sequence that nobody sees get
+    zeros, rows of no sequence are left.  The other arguments are those of the call before.
+    workspace: uint8 tensor of at least reskv_cross_attn_workspace() bytes (None: one kept per
+    stream); a call that is captured into a graph brings its own.
+    """
+    lib = _calls()
+    s = _stream_of(stream, q)
+    T = q.shape[0]
+    if workspace is None:
+        workspace = _kept_workspace(lib, q, s, reskv_cross_attn_workspace(T, q.shape[1]) if q.dim() == 3 else 0,
+                                    "reskv_cross_attn_workspace()")
+    elif not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor")
+    if lse is None:
+        raise ValueError("the gradient needs the lse of reskv_cross_attn")
+    a = _cross(q, k, v, o, batch, q_begin, kv_begin, kv_lens, scale, lse, status, workspace)
+    H, d, rows, kv = q.shape[1], q.shape[2], k.shape[0], k.shape[1]
+    st = lib.reskv_cross_attn_backward(a, _pack_heads(*_heads(d_o, "d_o", T, H, d)),
+                                       _pack_heads(*_heads(d_q, "d_q", T, H, d)),
+                                       _pack_heads(*_heads(d_k, "d_k", rows, kv, d)),
+                                       _pack_heads(*_heads(d_v, "d_v", rows, kv, d)), s)
+    if st:
+        _check(st)

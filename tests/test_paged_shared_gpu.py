@@ -1,0 +1,180 @@
+"""Attention with a shared prefix against fp64: tolerance as for reskv_paged_attn (logits summed in fp32,
+weights of 11 bits at least, half a unit of the output's type), the weights of the joined
+parts within 2^-18 beside."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cross_oracle as co
+from paged_cases import DT, HALF_ULP, as_type, paged
+from paper_2607_29591_gb300 import reskv as R
+
+pytestmark = pytest.mark.gpu
+
+
+def check(o, lse, refs, d, dtype):
+    ro, rl, xm, vm = (np.concatenate([r[i] for r in refs]) for i in range(4))
+    got = o.double().cpu().numpy()
+    share = 2 * d * 2.0 ** -23 * xm + 2.0 ** -11 + 2.0 ** -16 + (2.0 ** -11 if dtype != "f32" else 0)      # weights and held values
+    tol = (share * vm)[..., None] + HALF_ULP[dtype] * np.abs(ro) * 1.01 + 1e-7
+    assert np.isfinite(got).all()
+    assert (np.abs(got - ro) <= tol).all(), (np.abs(got - ro) - tol).max()
+    gl = lse.double().cpu().numpy()
+    assert ((gl == -np.inf) == (rl == -np.inf)).all()
+    seen = rl != -np.inf
+    bound = d * 2.0 ** -23 * xm + 2.0 ** -12 + 2.0 ** -22 * np.abs(np.where(seen, rl, 0))
+    assert (np.abs(gl[seen] - rl[seen]) <= bound[seen]).all()
+
+
+def case(seed, prefix_lens, lens, members, new, kv=2, per=4, d=128, group=32, page=32, dtype="bf16", out=None, counts=None,
+         scale=None, uniform=False):
+    """members: sequences of every group; counts: query tokens of every sequence (None: new each)."""
+    rng = np.random.default_rng(seed)
+    prefix, pv, _, _ = paged(rng, prefix_lens, kv, d, group, page)
+    own, ov, _, _ = paged(rng, lens, kv, d, group, page)
+    B, H = len(lens), kv * per
+    n = counts if counts is not None else [new] * B
+    begins = np.concatenate([[0], np.cumsum(n)]).astype(np.int32)
+    at = np.concatenate([[0], np.cumsum(members)]).astype(np.int32)
+    q, q64 = as_type(rng.standard_normal((begins[-1], H, d)), dtype)
+    ints = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    a = dict(seq_begin=None if uniform else ints(at), q_begin=None if counts is None else ints(begins), scale=scale)
+
+    def run():
+        o = torch.full((begins[-1], H, d), float("nan"), dtype=DT[out or dtype], device="cuda")
+        lse = torch.full((begins[-1], H), float("nan"), device="cuda")
+        R.reskv_paged_attn_shared(own, prefix, q, ints(lens), ints(prefix_lens), o, lse=lse, **a)
+        own.check_status()
+        prefix.check_status()
+        return o, lse
+
+    o, lse = run()
+    refs = []
+    for b in range(B):
+        g = int(np.searchsorted(at, b, "right")) - 1
+        pk, pvv = pv[g] if g < len(prefix_lens) else (np.zeros((kv, 0, d)),) * 2
+        k, v = np.concatenate([pk, ov[b][0]], 1), np.concatenate([pvv, ov[b][1]], 1)
+        t = np.arange(k.shape[1])
+        upto = pk.shape[1] + lens[b] - n[b] + np.arange(n[b])
+        see = (t <= upto[:, None]) | (t < pk.shape[1])
+        see &= (t < pk.shape[1]) | (t <= upto[:, None])
+        refs.append(co.attend(q64[begins[b]:begins[b + 1]], k, v, d ** -0.5 if scale is None else scale, see))
+    check(o, lse, refs, d, out or dtype)
+    o2, lse2 = run()
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("d,group", [(128, 32), (128, 64), (128, 128), (64, 32), (64, 64)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("batch", [3, 20])
+def test_single_tokens(d, group, dtype, batch):
+    lens = [1 + (37 * i) % 90 for i in range(batch)]
+    case(1, [150], lens, [batch], 1, d=d, group=group, dtype=dtype)
+
+
+@pytest.mark.parametrize("prefix", [0, 1, 15, 16, 17, 64, 65, 700])
+@pytest.mark.parametrize("batch", [2, 40])
+def test_prefix_lengths(prefix, batch):
+    case(prefix, [prefix], [5 + i for i in range(batch)], [batch], 1, per=2)
+
+
+@pytest.mark.parametrize("per", [1, 3, 7, 16])
+@pytest.mark.parametrize("batch", [4, 33])
+def test_head_groups(per, batch):
+    case(per, [90], [3 + 2 * i for i in range(batch)], [batch], 1, kv=3, per=per, d=64, group=32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_several_groups(dtype):
+    case(2, [100, 0, 333, 17], [9, 30, 1, 64, 65, 2, 70, 40, 8, 3], [1, 4, 3, 2], 1, dtype=dtype)
+    case(3, [100, 0, 333, 17], [9 + i for i in range(70)], [20, 0, 30, 20], 1, dtype=dtype)
+    case(4, [64, 200], [20] * 40, [20, 20], 1, uniform=True, dtype=dtype)
+    case(5, [50], [9, 30, 12], [2], 1, dtype=dtype)                    # the last sequence is in no group
+
+
+@pytest.mark.parametrize("new", [2, 5, 16])
+@pytest.mark.parametrize("batch", [1, 9])
+def test_several_tokens(new, batch):
+    case(new, [140], [new + 7 * i for i in range(batch)], [batch], new)
+    case(new + 1, [140, 30], [new + 7 * i for i in range(batch + 1)], [batch, 1], new, dtype="f16", d=64, group=64)
+
+
+def test_ragged_queries_and_tokens_before_the_own_ones():
+    case(6, [120, 60], [20, 9, 64, 3, 30], [3, 2], None, counts=[2, 0, 7, 3, 1])
+    case(7, [120, 60], [1, 0, 2], [2, 1], 3)                            # some stand before their own tokens
+    case(8, [0, 60], [1, 0, 2], [2, 1], 3)                              # and see nothing
+    case(9, [120], [40] * 4, [4], None, counts=[30, 1, 60, 0])
+
+
+def test_chunks_of_own_tokens():
+    """So many new tokens that both passes go by blocks of rows."""
+    case(10, [300], [80, 64], [2], 64)
+    case(11, [300, 70], [64, 64, 64, 64], [1, 3], 40, dtype="f16", uniform=False)
+
+
+def test_outputs_in_fp32_and_scale():
+    case(12, [200], [50, 60, 1], [3], 1, out="f32")
+    case(13, [200], [50 + i for i in range(30)], [30], 1, out="f32", dtype="f16", d=64, scale=0.05)
+
+
+def test_agrees_with_one_long_sequence():
+    """A prefix and own tokens in one sequence's pages, through reskv_paged_attn."""
+    rng = np.random.default_rng(14)
+    kv, per, d, page = 2, 4, 128, 16
+    whole, _, _, table = paged(rng, [96 + 21, 96 + 40], kv, d, 32, page)
+    # sequence 0's first six pages are the prefix of both
+    t = torch.from_numpy(table).cuda()
+    whole.page_table[1, :6] = t[0, :6]
+    lens = torch.tensor([21, 40], dtype=torch.int32, device="cuda")
+    prefix = R.PagedKV(whole.pages, t[:1, :6].contiguous(), page, kv, d, 32)
+    own = R.PagedKV(whole.pages, t[:, 6:].contiguous(), page, kv, d, 32)
+    q, _ = as_type(rng.standard_normal((2, kv * per, d)), "f16")
+    a, b = (torch.empty(q.shape, device="cuda") for _ in range(2))
+    R.reskv_paged_attn(whole, q, lens + 96, a)
+    R.reskv_paged_attn_shared(own, prefix, q, lens, torch.tensor([96], dtype=torch.int32, device="cuda"), b)
+    for kvc in (whole, own, prefix):
+        kvc.check_status()
+    assert float((a - b).abs().max()) <= 2.0 ** -16 * 40              # two fp32 results, values within 40
+
+
+def test_faults_are_reported_and_bounded():
+    rng = np.random.default_rng(15)
+    prefix, _, _, _ = paged(rng, [60, 60], 2, 128, 32, 32)
+    own, _, _, _ = paged(rng, [20] * 30, 2, 128, 32, 32)
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    q, _ = as_type(rng.standard_normal((30, 8, 128)), "bf16")
+    o = torch.empty_like(q)
+    for seqs, lens in (([0, 15, 30], [60, 1000]), ([0, 15, 30], [-1, 60]), ([0, 15, 300], [60, 60]), ([-4, 15, 30], [60, 60]),
+                       ([0, 30, 0], [60, 60]), ([30, 0, 30], [60, 60])):
+        R.reskv_paged_attn_shared(own, prefix, q, ints([20] * 30), ints(lens), o, seq_begin=ints(seqs))
+        with pytest.raises(R.ReskvError, match="index"):
+            prefix.check_status()
+        own.check_status()
+
+
+@pytest.mark.parametrize("batch", [3, 24])
+def test_captured_call_replayed(batch):
+    rng = np.random.default_rng(16)
+    prefix, _, _, _ = paged(rng, [200], 2, 128, 32, 32)
+    own, _, _, _ = paged(rng, [50] * batch, 2, 128, 32, 32)
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    q, _ = as_type(rng.standard_normal((batch, 8, 128)), "bf16")
+    o, lens, plens = torch.empty_like(q), ints([50] * batch), ints([200])
+    ws = torch.zeros(R.reskv_paged_attn_shared_workspace(own, prefix, batch, 8), dtype=torch.uint8, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        R.reskv_paged_attn_shared(own, prefix, q, lens, plens, o, workspace=ws)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=s):
+        R.reskv_paged_attn_shared(own, prefix, q, lens, plens, o, workspace=ws)
+    q.mul_(0.5)
+    lens.copy_(ints([7 + i for i in range(batch)]))
+    plens.fill_(99)
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    got = o.clone()
+    R.reskv_paged_attn_shared(own, prefix, q, lens, plens, o)
+    assert torch.equal(got, o)
