@@ -58,6 +58,14 @@ __device__ __forceinline__ CrossSequence cross_sequence(const CrossParams& p, in
   return s;
 }
 
+// Many query rows, on the fifth-generation tensor cores; cross_blocks.cu.  Copies take whole tokens:
+// a tile of 128 rows has cross_tile_tokens of them.
+struct CrossMaps {
+  CUtensorMap q, k, v;
+};
+inline int cross_tile_tokens(int group) { return 128 / group; }
+cudaError_t launch_cross_blocks(const CrossParams& p, const CrossMaps& maps, int d, int dev, int sms, cudaStream_t s);
+
 // Rows of any alignment; cross_general.cu.
 cudaError_t launch_cross_general(const CrossParams& p, int d, cudaStream_t s);
 cudaError_t launch_cross_grad_general(const CrossParams& p, int d, cudaStream_t s);

@@ -75,7 +75,18 @@ extern "C" reskv_status reskv_cross_attn(const reskv_cross_attn_args* a, void* s
     if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
     if (a->n_tokens == 0) return RESKV_OK;
     const CrossParams p = params_of(a);
-    return launch_result(launch_cross_general(p, a->head_dim, static_cast<cudaStream_t>(stream)), "cross attention");
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int dev = 0, sms = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (err != cudaSuccess) return launch_result(err, "reading the device");
+    CrossMaps maps;
+    const bool fast = rows_aligned(a->o, 16) && a->n_rows > 0 &&
+                      encode_heads(&maps.q, a->q, a->n_tokens, a->head_dim, p.group, cross_tile_tokens(p.group)) &&
+                      encode_heads(&maps.k, a->k, a->n_rows, a->head_dim, 1, 128) &&
+                      encode_heads(&maps.v, a->v, a->n_rows, a->head_dim, 1, 128);
+    return launch_result(fast ? launch_cross_blocks(p, maps, a->head_dim, dev, sms, s) : launch_cross_general(p, a->head_dim, s),
+                         "cross attention");
   });
 }
 

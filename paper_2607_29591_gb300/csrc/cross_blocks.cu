@@ -1,0 +1,543 @@
+// Cross attention of many query rows (a prompt against an encoder's states) on the
+// fifth-generation tensor cores.
+//
+// A row is a query token and head of a KV head; a tile is 128 rows (as many whole tokens as
+// fit).  A CTA takes two tiles and walks the states 128 at a time:
+//
+//   S = Q K^T       [128 rows x 128 states]  both operands in shared memory, into TMEM
+//   P = 2^(S - ref) one row a thread, in the type of q, over S in TMEM
+//   O += P V        [128 rows x d]           P from TMEM, V as it lies (across), into TMEM
+//
+// Copies, products and the softmax (four warps a tile) are roles of their own; while one tile's
+// softmax runs, the tensor cores work for the other.  Where a sequence has one tile's rows
+// only, the CTA's two streams take the even and the odd tiles of states (kSplit).  Where
+// there are too few blocks for the SMs, a cluster of CTAs shares a block's states.  Streams and
+// CTAs leave their rows in shared memory and are joined over the cluster, in order.
+//
+//   q             queries have landed
+//   full[op]      a tile of K or V has landed                (copies -> products)
+//   empty[op]     its products are done                      (products -> copies)
+//   s[m]          S of stream m is there, and the O before   (products -> softmax)
+//   p[m]          P is in place                              (softmax -> products)
+//   tail          the last V has landed, behind its last state anything: a warp puts zeros there
+//                 and passes it on as full[op]
+//
+// The reference of a row moves only when weights pass 2^14; it then lies 6 below the largest
+// logit.  No largest logit is looked for otherwise.
+#include <atomic>
+
+#include "cross.cuh"
+#include "tensor_core.cuh"
+#include "warp_mma.cuh"
+
+namespace reskv {
+namespace {
+
+using namespace tc;
+
+constexpr int kStates = 128;                      // of a tile
+constexpr int kThreads = 384;                     // warps 0-3, 4-7 softmax, 8 copies, 9 products, 10 the tail
+constexpr int kCopyWarp = 8, kIssueWarp = 9, kTailWarp = 10;
+constexpr int kRegsSoftmax = 232, kRegsIssue = 40;
+static_assert((2 * kRegsSoftmax + kRegsIssue) * 128 <= 168 * kThreads, "registers");
+constexpr float kNoReference = -3.0e38f;
+
+struct BlocksParams {
+  CrossParams a;
+  CUtensorMap q, k, v;
+  int32_t tile_tokens;            // whole tokens of a tile
+  int32_t cluster;
+};
+
+template <int D, bool kSplit>
+struct BlocksSmem {
+  static constexpr int half = 128 * 128;          // 128 rows of 64 elements
+  static constexpr int tile = D / 64 * half;
+  static constexpr int q = (kSplit ? 1 : 2) * tile;
+  static constexpr int slots = (224 * 1024 - q) / tile > 8 ? 8 : (224 * 1024 - q) / tile;
+  static constexpr int bytes = q + slots * tile + 1024;               // on a boundary of 1024
+  static constexpr int at_ref = 2 * 128 * D * 4;  // of rows to be joined: outputs, then references and sums
+  static_assert(at_ref + 2 * 256 * 4 <= q + slots * tile, "rows to be joined");
+};
+
+struct BlocksShared {
+  uint64_t q, full[8], empty[8], s[2], p[2], done, tail;
+  uint32_t tmem, abort;
+};
+
+__device__ __forceinline__ uint32_t rank_in_cluster() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void sync_cluster() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t of_rank(uint32_t local, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float read_cluster(uint32_t at) {
+  float x;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
+  return x;
+}
+__device__ __forceinline__ float4 read_cluster4(uint32_t at) {
+  float4 x;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at) : "memory");
+  return x;
+}
+
+template <bool kF16>
+__device__ __forceinline__ uint32_t pack_two(float lo, float hi) {
+  return kF16 ? pack_f16(lo, hi) : pack_bf16(lo, hi);
+}
+
+template <int D, bool kF16, bool kSplit>
+__global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_constant__ BlocksParams bp) {
+  using S = BlocksSmem<D, kSplit>;
+  constexpr uint32_t kType = kF16 ? 0u : kBf16;
+  constexpr uint32_t kLogits = shape_of(kStates) | kType, kOutputs = shape_of(D) | kType | kAcross;
+  const CrossParams& p = bp.a;
+  extern __shared__ uint8_t dynamic[];
+  uint8_t* smem = dynamic + ((1024u - (smem_u32(dynamic) & 1023u)) & 1023u);
+  __shared__ __align__(16) BlocksShared sh;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int cs = bp.cluster, rank = cs > 1 ? int(rank_in_cluster()) : 0;
+
+  if (tid == 0) {
+    mbar_init(&sh.q, 1);
+    for (int i = 0; i < S::slots; ++i) {
+      mbar_init(&sh.full[i], 1);
+      mbar_init(&sh.empty[i], 1);
+    }
+    for (int m = 0; m < 2; ++m) {
+      mbar_init(&sh.s[m], 1);
+      mbar_init(&sh.p[m], 4);
+    }
+    mbar_init(&sh.done, 1);
+    mbar_init(&sh.tail, 1);
+    sh.abort = 0;
+    fence_mbar_init();
+  }
+  wait_for_previous();
+
+  // the block: tokens t0 .. of sequence b, KV head h
+  const int tt = bp.tile_tokens, block_tokens = (kSplit ? 1 : 2) * tt;
+  int item = int(blockIdx.x) / cs, b = 0, blocks = 0;
+  if (p.q_begin) {
+    bool found = false;
+#pragma unroll 1
+    for (int b0 = 0; b0 < p.batch; b0 += 32) {
+      int mine = 0, first, count;
+      if (b0 + lane < p.batch) {
+        cross_range(p.q_begin, b0 + lane, p.batch, p.n_tokens, p.status, first, count);
+        mine = (count + block_tokens - 1) / block_tokens;
+      }
+      int upto = mine * p.kv_heads;
+#pragma unroll
+      for (int o = 1; o < 32; o *= 2) {
+        const int x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, upto > item);
+      if (past) {
+        const int l = __ffs(past) - 1;
+        b = b0 + l;
+        blocks = __shfl_sync(0xffffffffu, mine, l);
+        item -= __shfl_sync(0xffffffffu, upto, l) - blocks * p.kv_heads;
+        found = true;
+        break;
+      }
+      item -= __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (!found) return;                           // the same for the whole cluster
+  } else {
+    blocks = (int(p.n_tokens / p.batch) + block_tokens - 1) / block_tokens;
+    b = item / (blocks * p.kv_heads);
+    item -= b * blocks * p.kv_heads;
+  }
+  const int h = item / blocks, t0 = (item - h * blocks) * block_tokens;
+  const CrossSequence sq = cross_sequence(p, b);
+  const bool two = !kSplit && t0 + tt < sq.count;
+  const int all = (sq.seen + kStates - 1) / kStates;
+  const int first = int(int64_t(all) * rank / cs), n = int(int64_t(all) * (rank + 1) / cs) - first;      // tiles of states
+  const int steps[2] = {kSplit ? (n + 1) / 2 : n, kSplit ? n / 2 : two ? n : 0};
+  const int left = sq.seen - (first + n - 1) * kStates;               // states of the last tile
+  const bool cut = n > 0 && left < kStates;
+
+  // a softmax thread's row
+  const int m = (warp >> 2) & 1, rt = (warp & 3) * 32 + lane;
+  const int row_token = rt / p.group, token = t0 + (kSplit ? 0 : m * tt) + row_token;
+  const bool real = warp < 8 && row_token < tt && token < sq.count;
+  const int head = h * p.group + rt - row_token * p.group;
+  if (sq.seen == 0) {                             // the same for the whole cluster
+    if (real && rank == 0 && (m == 0 || !kSplit)) {
+      uint16_t* y = static_cast<uint16_t*>(p.o.data) + (sq.q0 + token) * p.o.token + head * p.o.head;
+#pragma unroll 1
+      for (int i = 0; i < D / 8; ++i) reinterpret_cast<uint4*>(y)[i] = make_uint4(0, 0, 0, 0);
+      if (p.lse) p.lse[int64_t(sq.q0 + token) * p.heads + head] = -INFINITY;
+    }
+    return;
+  }
+  if (warp == kIssueWarp) take_columns(smem_u32(&sh.tmem));
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = sh.tmem, smem_q = smem_u32(smem), ring = smem_q + S::q;
+  auto s_cols = [&](int s) { return tmem + uint32_t(s * kStates); };
+  auto o_cols = [&](int s) { return tmem + uint32_t(2 * kStates + s * D); };
+  // Tiles come in the order of their first use: K0 V0 K1 V1 .., or split K0 K1 V0 K2 V1 ..
+  auto k_op = [&](int t) { return kSplit ? (t == 0 ? 0 : 2 * t - 1) : 2 * t; };
+  auto v_op = [&](int t) { return kSplit ? (t + 1 < n ? 2 * t + 2 : 2 * t + 1) : 2 * t + 1; };
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+    if (warp == kCopyWarp) {
+      // --- copies ---
+      int copied = 0;
+      bool ok = true;
+      if (elected() && n > 0) {
+        const int halves = D / 64, tiles = kSplit || !two ? 1 : 2;
+        mbar_arrive_expect_tx(&sh.q, uint32_t(tiles * halves * tt * p.group * 128));
+        for (int i = 0; i < tiles; ++i)
+          for (int x = 0; x < halves; ++x)
+            copy_box(smem_q + i * S::tile + x * S::half, &bp.q, 64 * x, h * p.group, sq.q0 + t0 + i * tt, &sh.q);
+      }
+      __syncwarp();
+#pragma unroll 1
+      for (int op = 0; op < 2 * n && ok; ++op) {
+        const int slot = op % S::slots, turn = op / S::slots;
+        if (turn > 0) ok = role_wait(&sh.empty[slot], (turn - 1) & 1, &sh.abort, p.status);
+        if (!ok) break;
+        const bool values = kSplit ? (op > 0 && (op == 2 * n - 1 || (op & 1) == 0)) : (op & 1);
+        const int t = !kSplit ? op / 2 : op == 0 ? 0 : op == 2 * n - 1 ? n - 1 : values ? op / 2 - 1 : (op + 1) / 2;
+        if (elected()) {
+          uint64_t* bar = cut && values && t == n - 1 ? &sh.tail : &sh.full[slot];
+          mbar_arrive_expect_tx(bar, S::tile);
+#pragma unroll
+          for (int x = 0; x < D / 64; ++x)
+            copy_box(ring + slot * S::tile + x * S::half, values ? &bp.v : &bp.k, 64 * x, h, sq.k0 + (first + t) * kStates, bar);
+        }
+        __syncwarp();
+        copied = op + 1;
+      }
+      if (!ok && lane == 0) {                     // a wait gave up: let what is in flight land
+        mbar_wait_bounded(&sh.q, 0);
+        for (int op = copied > S::slots ? copied - S::slots : 0; op < copied; ++op)
+          mbar_wait_bounded(cut && op == v_op(n - 1) ? &sh.tail : &sh.full[op % S::slots],
+                            cut && op == v_op(n - 1) ? 0 : (op / S::slots) & 1);
+      }
+      __syncwarp();
+    } else if (warp == kIssueWarp) {
+      // --- products ---
+      auto wait_tile = [&](int op) { return role_wait(&sh.full[op % S::slots], (op / S::slots) & 1, &sh.abort, p.status); };
+      auto release = [&](int op) {
+        if (elected()) commit(&sh.empty[op % S::slots]);
+        __syncwarp();
+      };
+      auto issue_s = [&](int s, int op) {
+        fence_after();
+        if (elected()) {
+          const uint32_t q0 = operand(smem_q + (kSplit ? 0 : s) * S::tile), k0 = operand(ring + op % S::slots * S::tile);
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k)
+            multiply<kRows128, kLogits>(s_cols(s), q0 + (((k / 4) * S::half + (k & 3) * 32) >> 4),
+                                        k0 + (((k / 4) * S::half + (k & 3) * 32) >> 4), k > 0);
+          commit(&sh.s[s]);
+        }
+        __syncwarp();
+      };
+      auto issue_o = [&](int s, int op, bool add) {
+        fence_after();
+        if (elected()) {
+          const uint32_t v0 = operand_across(ring + op % S::slots * S::tile, S::half);
+#pragma unroll
+          for (int k = 0; k < kStates / 16; ++k)
+            multiply_from<kRows128, kOutputs>(o_cols(s), s_cols(s) + k * 8, v0 + ((k * 16 * 128) >> 4), add || k > 0);
+        }
+        __syncwarp();
+      };
+      bool ok = n == 0 || role_wait(&sh.q, 0, &sh.abort, p.status);
+      // the first logits of both streams
+      for (int s = 0; s < 2 && ok; ++s) {
+        if (steps[s] == 0) continue;
+        const int op = k_op(kSplit ? s : 0);
+        if (kSplit || s == 0) ok = wait_tile(op);
+        if (!ok) break;
+        issue_s(s, op);
+        if (kSplit || s == 1 || !two) release(op);
+      }
+#pragma unroll 1
+      for (int i = 0; i < steps[0] && ok; ++i) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          if (i >= steps[s] || !ok) continue;
+          const int t = kSplit ? 2 * i + s : i, next = kSplit ? t + 2 : t + 1;
+          const bool last_use = kSplit || s == 1 || !two;
+          if (kSplit || s == 0) ok = wait_tile(v_op(t));
+          if (ok) ok = role_wait(&sh.p[s], i & 1, &sh.abort, p.status);
+          if (!ok) break;
+          issue_o(s, v_op(t), i > 0);
+          if (last_use) release(v_op(t));
+          if (next < n) {
+            if (kSplit || s == 0) ok = wait_tile(k_op(next));
+            if (!ok) break;
+            issue_s(s, k_op(next));
+            if (last_use) release(k_op(next));
+          }
+        }
+      }
+      // all products: also where a wait gave up, which the softmax does not see then
+      if (elected()) commit(&sh.done);
+      __syncwarp();
+      if (!ok) mbar_wait_bounded(&sh.done, 0);
+    } else if (warp == kTailWarp && cut) {
+      // --- what lies behind the last state: weights are zero there, values may be anything ---
+      const int slot = v_op(n - 1) % S::slots;
+      if (role_wait(&sh.tail, 0, &sh.abort, p.status)) {
+        for (int i = lane; i < (kStates - left) * 8 * (D / 64); i += 32) {
+          const int x = i / ((kStates - left) * 8), r = i - x * (kStates - left) * 8;
+          *reinterpret_cast<uint4*>(smem + S::q + slot * S::tile + x * S::half + left * 128 + r * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async_smem();
+        role_arrive(&sh.full[slot]);
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    // --- the softmax, a row a thread ---
+    const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
+    const int mine = steps[m];
+    const float f = p.scale2;
+    float ref = kNoReference, l = 0.f;
+    bool ok = true;
+#pragma unroll 1
+    for (int i = 0; i < mine; ++i) {
+      ok = role_wait(&sh.s[m], i & 1, &sh.abort, p.status);
+      if (!ok) break;
+      fence_after();
+      const int t = kSplit ? 2 * i + m : i;
+      const int upto = t == n - 1 ? left : kStates;
+      float x[kStates];
+      auto logits = [&]() {
+#pragma unroll
+        for (int k = 0; k < kStates / 16; ++k) load16(s_cols(m) + lanes + 16 * k, x + 16 * k);
+        landed();
+#pragma unroll
+        for (int k = 0; k < kStates / 16; ++k) defined16(x + 16 * k);
+      };
+      auto weights = [&]() {                      // x: logits -> weights, in place; returns their sum
+        float2 s2[4] = {};
+#pragma unroll
+        for (int k = 0; k < kStates; k += 2) {
+          const float2 y = ffma2(make_float2(x[k], x[k + 1]), make_float2(f, f), make_float2(-ref, -ref));
+          x[k] = exp2_fast(y.x);
+          x[k + 1] = exp2_fast(y.y);
+        }
+        if (upto < kStates) {
+#pragma unroll
+          for (int k = 0; k < kStates; ++k)
+            if (k >= upto) x[k] = 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < kStates; k += 2) s2[(k / 2) & 3] = fadd2(s2[(k / 2) & 3], make_float2(x[k], x[k + 1]));
+        const float2 s = fadd2(fadd2(s2[0], s2[1]), fadd2(s2[2], s2[3]));
+        return s.x + s.y;
+      };
+      logits();
+      float sum = weights(), keep = 1.f;
+      if (__any_sync(0xffffffffu, !(sum <= 16384.f))) {
+        logits();
+        float top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kStates; ++k) top = fmaxf(top, k < upto ? __fmul_rn(x[k], f) : -INFINITY);
+        const float now = sum <= 16384.f ? ref : fmaxf(ref, top - 6.f);
+        keep = exp2f(ref - now);
+        ref = now;
+        sum = weights();
+      }
+      l = l * keep + sum;
+      if (i > 0 && __any_sync(0xffffffffu, keep != 1.f)) {       // (S's barrier has the products before it behind it)
+#pragma unroll 1
+        for (int c = 0; c < D / 16; ++c) {
+          float v[16];
+          load16(o_cols(m) + lanes + 16 * c, v);
+          landed();
+          defined16(v);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] *= keep;
+          store16(o_cols(m) + lanes + 16 * c, v);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t w[32];
+#pragma unroll
+        for (int k = 0; k < 32; ++k) w[k] = pack_two<kF16>(x[64 * c + 2 * k], x[64 * c + 2 * k + 1]);
+        store32(s_cols(m) + lanes + 32 * c, w);
+      }
+      stored();
+      fence_before();
+      role_arrive(&sh.p[m]);
+    }
+    if (ok && mine > 0) ok = role_wait(&sh.done, 0, &sh.abort, p.status);
+    fence_after();
+    const bool seen = mine > 0 && ok;
+    if (cs == 1 && !kSplit) {
+      const float inv = 1.f / l;
+      if (seen) {
+        uint16_t* y = static_cast<uint16_t*>(p.o.data) + (sq.q0 + token) * p.o.token + head * p.o.head;
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          float o[32];
+          load16(o_cols(m) + lanes + 32 * c, o);
+          load16(o_cols(m) + lanes + 32 * c + 16, o + 16);
+          landed();
+          defined16(o);
+          defined16(o + 16);
+          if (real) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint32_t w[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) w[e] = pack_two<kF16>(o[8 * k + 2 * e] * inv, o[8 * k + 2 * e + 1] * inv);
+              reinterpret_cast<uint4*>(y)[4 * c + k] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+        }
+        if (real && p.lse) p.lse[int64_t(sq.q0 + token) * p.heads + head] = (ref + log2f(l)) * 0.693147180559945f;
+      }
+    } else {
+      // for the join: all products are done, operands' memory is free (word u of row r at u ^ r)
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      float4* rows = reinterpret_cast<float4*>(smem) + (m * 128 + rt) * (D / 4);
+      if (seen) {
+#pragma unroll 1
+        for (int c = 0; c < D / 16; ++c) {
+          float o[16];
+          load16(o_cols(m) + lanes + 16 * c, o);
+          landed();
+          defined16(o);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) rows[(4 * c + k) ^ (rt & (D / 4 - 1))] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+        }
+      }
+      float* refs = reinterpret_cast<float*>(smem + S::at_ref);
+      refs[m * 128 + rt] = seen ? ref : -INFINITY;
+      refs[256 + m * 128 + rt] = seen ? l : 0.f;
+    }
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (warp == kIssueWarp) give_columns(tmem);
+  if (cs == 1 && !kSplit) return;
+  if (cs > 1) sync_cluster();
+
+  // --- the join: a row a warp, rows dealt to the cluster's softmax warps (the others have few registers) ---
+  const int rows = kSplit ? 128 : two ? 256 : 128;
+  const uint32_t at_rows = smem_q, at_ref = smem_q + S::at_ref, at_sum = at_ref + 256 * 4;
+  constexpr int kSources = kSplit ? 2 : 1;
+#pragma unroll 1
+  for (int r = rank * 8 + warp; warp < 8 && r < rows; r += cs * 8) {
+    const int rm = r >> 7, rr = r & 127;          // (split: tile 0's row, of both streams)
+    const int tk = rr / p.group, tok = t0 + rm * tt + tk;
+    if (tk >= tt || tok >= sq.count) continue;
+    // source i: stream i % kSources of rank i / kSources; at most 32 of them
+    const int sources = cs * kSources;
+    float ref = -INFINITY, sum = 0.f;
+    if (lane < sources) {
+      const uint32_t at = uint32_t((kSplit ? lane & 1 : rm) * 128 + rr) * 4, from = uint32_t(lane / kSources);
+      ref = read_cluster(of_rank(at_ref + at, from));
+      sum = read_cluster(of_rank(at_sum + at, from));
+    }
+    float top = ref;
+#pragma unroll
+    for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float w = ref == -INFINITY ? 0.f : exp2f(ref - top);
+    float total = w == 0.f && sum == sum ? 0.f : w * sum;
+#pragma unroll
+    for (int o = 16; o; o /= 2) total += __shfl_xor_sync(0xffffffffu, total, o);
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int u = lane < D / 4 ? lane : 0;
+#pragma unroll 1
+    for (int i = 0; i < sources; ++i) {
+      const float wi = __shfl_sync(0xffffffffu, w, i);
+      if (__shfl_sync(0xffffffffu, ref, i) == -INFINITY) continue;    // a source without states
+      const uint32_t at = at_rows + uint32_t(((kSplit ? i & 1 : rm) * 128 + rr) * (D / 4) + (u ^ (rr & (D / 4 - 1)))) * 16;
+      const float4 v = read_cluster4(of_rank(at, uint32_t(i / kSources)));
+      a.x = fmaf(wi, v.x, a.x);
+      a.y = fmaf(wi, v.y, a.y);
+      a.z = fmaf(wi, v.z, a.z);
+      a.w = fmaf(wi, v.w, a.w);
+    }
+    const float inv = 1.f / total;
+    const int hd = h * p.group + rr - tk * p.group;
+    if (lane < D / 4) {
+      uint16_t* y = static_cast<uint16_t*>(p.o.data) + (sq.q0 + tok) * p.o.token + hd * p.o.head;
+      reinterpret_cast<uint2*>(y)[u] = make_uint2(pack_two<kF16>(a.x * inv, a.y * inv), pack_two<kF16>(a.z * inv, a.w * inv));
+    }
+    const float lse = (top + log2f(total)) * 0.693147180559945f;
+    if (lane == 0 && p.lse) p.lse[int64_t(sq.q0 + tok) * p.heads + hd] = lse;
+    __syncwarp();
+  }
+  __syncthreads();
+  if (cs > 1) sync_cluster();                     // nobody leaves while its rows are read
+}
+
+template <int D, bool kF16, bool kSplit>
+cudaError_t launch(const BlocksParams& bp, int64_t items, int dev, cudaStream_t s) {
+  // the kernel's shared memory limit, raised once a device
+  static std::atomic<uint64_t> raised{0};
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+  if (!(raised.load(std::memory_order_relaxed) & bit) || !bit) {
+    const cudaError_t err = cudaFuncSetAttribute(k_cross_blocks<D, kF16, kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 BlocksSmem<D, kSplit>::bytes);
+    if (err != cudaSuccess) return err;
+    raised.fetch_or(bit, std::memory_order_relaxed);
+  }
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = unsigned(bp.cluster);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(unsigned(items * bp.cluster));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = BlocksSmem<D, kSplit>::bytes;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = bp.cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, k_cross_blocks<D, kF16, kSplit>, bp);
+}
+
+}  // namespace
+
+cudaError_t launch_cross_blocks(const CrossParams& p, const CrossMaps& maps, int d, int dev, int sms, cudaStream_t s) {
+  BlocksParams bp{};
+  bp.a = p;
+  bp.q = maps.q;
+  bp.k = maps.k;
+  bp.v = maps.v;
+  bp.tile_tokens = cross_tile_tokens(p.group);
+  // one tile a CTA where sequences have no more on average
+  const bool split = p.n_tokens <= int64_t(bp.tile_tokens) * p.batch;
+  const int64_t block_tokens = int64_t(split ? 1 : 2) * bp.tile_tokens;
+  const int64_t blocks = (p.n_tokens / p.batch + block_tokens - 1) / block_tokens;
+  const int64_t sure = (blocks > 0 ? blocks : 1) * p.batch * p.kv_heads;           // about as many blocks as there are
+  const int64_t items = p.q_begin ? (p.n_tokens / block_tokens + p.batch) * p.kv_heads : blocks * p.batch * p.kv_heads;
+  // a cluster for each block where that fills the SMs, of two tiles of states a CTA at least
+  const int64_t tiles = (p.n_rows / p.batch + kStates - 1) / kStates;
+  bp.cluster = 1;
+  while (bp.cluster < 8 && sure * bp.cluster * 2 <= sms && bp.cluster * 4 <= tiles) bp.cluster *= 2;
+  if (d == 128)
+    return p.f16 ? (split ? launch<128, true, true>(bp, items, dev, s) : launch<128, true, false>(bp, items, dev, s))
+                 : (split ? launch<128, false, true>(bp, items, dev, s) : launch<128, false, false>(bp, items, dev, s));
+  return p.f16 ? (split ? launch<64, true, true>(bp, items, dev, s) : launch<64, true, false>(bp, items, dev, s))
+               : (split ? launch<64, false, true>(bp, items, dev, s) : launch<64, false, false>(bp, items, dev, s));
+}
+
+}  // namespace reskv

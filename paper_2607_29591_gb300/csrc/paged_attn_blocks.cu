@@ -45,9 +45,12 @@
 #include <atomic>
 
 #include "paged_attn.cuh"
+#include "tensor_core.cuh"
 
 namespace reskv {
 namespace {
+
+using namespace tc;
 
 constexpr int kPos = kBlockPos;                   // positions of a step
 constexpr int kSub = kPos / kTile;                // cache tiles of a step
@@ -63,68 +66,6 @@ constexpr float kFarLogits = 0.03125f, kFarValues = 1.220703125e-4f;          //
 // Registers a thread of each part: (2 x 128 + 2 x 88 + 40) x 128 of the launch's 96 x 640.
 constexpr int kRegsSoftmax = 128, kRegsUnpack = 88, kRegsIssue = 40;
 static_assert((2 * kRegsSoftmax + 2 * kRegsUnpack + kRegsIssue) * 128 <= 96 * kThreads, "registers");
-
-// --- tensor core instructions ---
-
-// Descriptors of K-major operands in shared memory: the address / 16 in the low
-// word, beside a constant; in the high word the distance of groups of eight rows
-// / 16, version 1 and the swizzle.  Rows of 128 bytes (64 fp16) have the 128-byte
-// swizzle (16-byte word w of row r at w ^ (r & 7)); rows of 32 bytes (one step) the
-// 32-byte swizzle (w at w ^ ((r >> 2) & 1)).
-__device__ __forceinline__ uint32_t operand(uint32_t saddr) { return (saddr >> 4) | (1u << 16); }
-constexpr uint32_t kRows128 = (1024 >> 4) | (1u << 14) | (2u << 29);
-constexpr uint32_t kRows32 = (256 >> 4) | (1u << 14) | (6u << 29);
-
-// kind::f16, fp16 operands, fp32 accumulators, 128 rows, n columns
-__host__ __device__ constexpr uint32_t shape_of(int n) { return (1u << 4) | (uint32_t(n >> 3) << 17) | (uint32_t(128 >> 4) << 24); }
-template <uint32_t kHigh, uint32_t kShape>
-__device__ __forceinline__ void multiply(uint32_t d, uint32_t a, uint32_t b, bool add) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(kHigh), "r"(kShape),
-      "r"(add ? 1 : 0));
-}
-// The same with the first operand in tensor memory: a row a lane, two fp16 a column.
-template <uint32_t kHigh, uint32_t kShape>
-__device__ __forceinline__ void multiply_from(uint32_t d, uint32_t a, uint32_t b, bool add) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 db, {%2, %3};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(kHigh), "r"(kShape),
-      "r"(add ? 1 : 0));
-}
-// True in one thread of a converged warp.
-__device__ __forceinline__ bool elected() {
-  uint32_t e;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
-  return e != 0;
-}
-__device__ __forceinline__ void commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-// 16 columns of this thread's row; defined after landed()
-__device__ __forceinline__ void load16(uint32_t at, float* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
-        "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
-      : "r"(at));
-}
-__device__ __forceinline__ void landed() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void defined16(float* r) {
-  asm volatile("" : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]), "+f"(r[8]),
-               "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]));
-}
-__device__ __forceinline__ void store16(uint32_t at, const float* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::
-          "r"(at), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]),
-      "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15])
-      : "memory");
-}
-__device__ __forceinline__ void stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // 2^(14 - (e - 127)) and its inverse, of a biased exponent 15 <= e <= 254
 __device__ __forceinline__ float down(int e) { return __int_as_float((268 - e) << 23); }

@@ -296,6 +296,23 @@ reskv_status finalize_ragged_layout(reskv_cache* c) {
   return st;
 }
 
+bool encode_heads(CUtensorMap* map, const reskv_heads& t, int64_t tokens, int dim, int box_heads, int box_tokens) {
+  PFN_cuTensorMapEncodeTiled_v12000 enc = tensor_map_encoder();
+  if (!enc) return false;
+  // (the stride of a single head or token is anyone's)
+  const int64_t head = t.n_heads == 1 ? dim : t.head_stride, token = tokens == 1 ? int64_t(dim) * t.n_heads : t.token_stride;
+  if (head <= 0 || token <= 0 || head % 8 || token % 8 || head >= (int64_t(1) << 38) || token >= (int64_t(1) << 38) ||
+      reinterpret_cast<uintptr_t>(t.data) % 16)
+    return false;
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const cuuint64_t dims[3] = {cuuint64_t(dim), cuuint64_t(t.n_heads), cuuint64_t(tokens)};
+  const cuuint64_t strides[2] = {cuuint64_t(head) * 2, cuuint64_t(token) * 2};
+  const cuuint32_t box[3] = {64, cuuint32_t(box_heads), cuuint32_t(box_tokens)};
+  return enc(map, t.dtype == RESKV_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, t.data, dims,
+             strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool encode_rows(CUtensorMap* map, const void* base, uint64_t rows, int rank) {
   PFN_cuTensorMapEncodeTiled_v12000 enc = tensor_map_encoder();
   if (!enc) return false;
