@@ -58,12 +58,62 @@ __device__ __forceinline__ CrossSequence cross_sequence(const CrossParams& p, in
   return s;
 }
 
+// The block that a CTA takes: of the `count` tokens (or rows) of every sequence, `per` a block, for
+// each KV head; blocks of a KV head lie side by side.  One warp; false: no such block.
+struct CrossBlock {
+  int b, h, first;                // sequence, KV head, first token within the sequence
+};
+__device__ __forceinline__ bool cross_block(const CrossParams& p, const int32_t* begin, int64_t total, int per, int item, int lane,
+                                            CrossBlock& out) {
+  int blocks;
+  if (begin) {
+    bool found = false;
+#pragma unroll 1
+    for (int b0 = 0; b0 < p.batch; b0 += 32) {
+      int mine = 0, first, count;
+      if (b0 + lane < p.batch) {
+        cross_range(begin, b0 + lane, p.batch, total, p.status, first, count);
+        mine = (count + per - 1) / per;
+      }
+      int upto = mine * p.kv_heads;
+#pragma unroll
+      for (int o = 1; o < 32; o *= 2) {
+        const int x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, upto > item);
+      if (past) {
+        const int l = __ffs(past) - 1;
+        out.b = b0 + l;
+        blocks = __shfl_sync(0xffffffffu, mine, l);
+        item -= __shfl_sync(0xffffffffu, upto, l) - blocks * p.kv_heads;
+        found = true;
+        break;
+      }
+      item -= __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (!found) return false;
+  } else {
+    blocks = (int(total / p.batch) + per - 1) / per;
+    out.b = item / (blocks * p.kv_heads);
+    item -= out.b * blocks * p.kv_heads;
+  }
+  out.h = item / blocks;
+  out.first = (item - out.h * blocks) * per;
+  return true;
+}
+// Blocks that a call may have.
+inline int64_t cross_blocks(const CrossParams& p, const int32_t* begin, int64_t total, int per) {
+  return begin ? (total / per + p.batch) * p.kv_heads : (total / p.batch + per - 1) / per * p.batch * p.kv_heads;
+}
+
 // Many query rows, on the fifth-generation tensor cores; cross_blocks.cu.  Copies take whole tokens:
 // a tile of 128 rows has cross_tile_tokens of them.
 struct CrossMaps {
-  CUtensorMap q, k, v;
+  CUtensorMap q, k, v, d_o;
 };
 inline int cross_tile_tokens(int group) { return 128 / group; }
+cudaError_t launch_cross_grad(const CrossParams& p, const CrossMaps& maps, int d, int dev, cudaStream_t s);      // cross_grad.cu
 cudaError_t launch_cross_blocks(const CrossParams& p, const CrossMaps& maps, int d, int dev, int sms, cudaStream_t s);
 
 // Rows of any alignment; cross_general.cu.

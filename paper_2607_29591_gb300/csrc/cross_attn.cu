@@ -64,6 +64,19 @@ CrossParams params_of(const reskv_cross_attn_args* a) {
   return p;
 }
 
+cudaError_t device_sms(int* dev, int* sms) {
+  const cudaError_t err = cudaGetDevice(dev);
+  return err != cudaSuccess ? err : cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *dev);
+}
+
+// false: rows that copies cannot address
+bool encode_maps(CrossMaps* maps, const reskv_cross_attn_args* a, const CrossParams& p) {
+  return a->n_rows > 0 && a->n_tokens > 0 &&
+         encode_heads(&maps->q, a->q, a->n_tokens, a->head_dim, p.group, cross_tile_tokens(p.group)) &&
+         encode_heads(&maps->k, a->k, a->n_rows, a->head_dim, 1, 128) &&
+         encode_heads(&maps->v, a->v, a->n_rows, a->head_dim, 1, 128);
+}
+
 }  // namespace
 }  // namespace reskv
 
@@ -77,14 +90,10 @@ extern "C" reskv_status reskv_cross_attn(const reskv_cross_attn_args* a, void* s
     const CrossParams p = params_of(a);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     int dev = 0, sms = 0;
-    cudaError_t err = cudaGetDevice(&dev);
-    if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    const cudaError_t err = device_sms(&dev, &sms);
     if (err != cudaSuccess) return launch_result(err, "reading the device");
     CrossMaps maps;
-    const bool fast = rows_aligned(a->o, 16) && a->n_rows > 0 &&
-                      encode_heads(&maps.q, a->q, a->n_tokens, a->head_dim, p.group, cross_tile_tokens(p.group)) &&
-                      encode_heads(&maps.k, a->k, a->n_rows, a->head_dim, 1, 128) &&
-                      encode_heads(&maps.v, a->v, a->n_rows, a->head_dim, 1, 128);
+    const bool fast = rows_aligned(a->o, 16) && encode_maps(&maps, a, p);
     return launch_result(fast ? launch_cross_blocks(p, maps, a->head_dim, dev, sms, s) : launch_cross_general(p, a->head_dim, s),
                          "cross attention");
   });
@@ -126,7 +135,15 @@ extern "C" reskv_status reskv_cross_attn_backward(const reskv_cross_attn_args* a
       p.d_k = rows_of(*d_k);
       p.d_v = rows_of(*d_v);
     }
-    return launch_result(launch_cross_grad_general(p, a->head_dim, static_cast<cudaStream_t>(stream)),
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int dev = 0, sms = 0;
+    const cudaError_t err = device_sms(&dev, &sms);
+    if (err != cudaSuccess) return launch_result(err, "reading the device");
+    CrossMaps maps;
+    const bool fast = tokens && rows && rows_aligned(a->o, 16) && rows_aligned(*d_o, 16) && rows_aligned(*d_q, 16) &&
+                      rows_aligned(*d_k, 16) && rows_aligned(*d_v, 16) && encode_maps(&maps, a, p) &&
+                      encode_heads(&maps.d_o, *d_o, a->n_tokens, a->head_dim, p.group, cross_tile_tokens(p.group));
+    return launch_result(fast ? launch_cross_grad(p, maps, a->head_dim, dev, s) : launch_cross_grad_general(p, a->head_dim, s),
                          "the gradient of cross attention");
   });
 }

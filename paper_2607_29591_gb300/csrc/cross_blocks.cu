@@ -89,11 +89,6 @@ __device__ __forceinline__ float4 read_cluster4(uint32_t at) {
   return x;
 }
 
-template <bool kF16>
-__device__ __forceinline__ uint32_t pack_two(float lo, float hi) {
-  return kF16 ? pack_f16(lo, hi) : pack_bf16(lo, hi);
-}
-
 template <int D, bool kF16, bool kSplit>
 __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_constant__ BlocksParams bp) {
   using S = BlocksSmem<D, kSplit>;
@@ -125,40 +120,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
 
   // the block: tokens t0 .. of sequence b, KV head h
   const int tt = bp.tile_tokens, block_tokens = (kSplit ? 1 : 2) * tt;
-  int item = int(blockIdx.x) / cs, b = 0, blocks = 0;
-  if (p.q_begin) {
-    bool found = false;
-#pragma unroll 1
-    for (int b0 = 0; b0 < p.batch; b0 += 32) {
-      int mine = 0, first, count;
-      if (b0 + lane < p.batch) {
-        cross_range(p.q_begin, b0 + lane, p.batch, p.n_tokens, p.status, first, count);
-        mine = (count + block_tokens - 1) / block_tokens;
-      }
-      int upto = mine * p.kv_heads;
-#pragma unroll
-      for (int o = 1; o < 32; o *= 2) {
-        const int x = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += x;
-      }
-      const uint32_t past = __ballot_sync(0xffffffffu, upto > item);
-      if (past) {
-        const int l = __ffs(past) - 1;
-        b = b0 + l;
-        blocks = __shfl_sync(0xffffffffu, mine, l);
-        item -= __shfl_sync(0xffffffffu, upto, l) - blocks * p.kv_heads;
-        found = true;
-        break;
-      }
-      item -= __shfl_sync(0xffffffffu, upto, 31);
-    }
-    if (!found) return;                           // the same for the whole cluster
-  } else {
-    blocks = (int(p.n_tokens / p.batch) + block_tokens - 1) / block_tokens;
-    b = item / (blocks * p.kv_heads);
-    item -= b * blocks * p.kv_heads;
-  }
-  const int h = item / blocks, t0 = (item - h * blocks) * block_tokens;
+  CrossBlock block;
+  if (!cross_block(p, p.q_begin, p.n_tokens, block_tokens, int(blockIdx.x) / cs, lane, block)) return;      // the whole cluster
+  const int b = block.b, h = block.h, t0 = block.first;
   const CrossSequence sq = cross_sequence(p, b);
   const bool two = !kSplit && t0 + tt < sq.count;
   const int all = (sq.seen + kStates - 1) / kStates;
@@ -528,7 +492,7 @@ cudaError_t launch_cross_blocks(const CrossParams& p, const CrossMaps& maps, int
   const int64_t block_tokens = int64_t(split ? 1 : 2) * bp.tile_tokens;
   const int64_t blocks = (p.n_tokens / p.batch + block_tokens - 1) / block_tokens;
   const int64_t sure = (blocks > 0 ? blocks : 1) * p.batch * p.kv_heads;           // about as many blocks as there are
-  const int64_t items = p.q_begin ? (p.n_tokens / block_tokens + p.batch) * p.kv_heads : blocks * p.batch * p.kv_heads;
+  const int64_t items = cross_blocks(p, p.q_begin, p.n_tokens, int(block_tokens));
   // a cluster for each block where that fills the SMs, of two tiles of states a CTA at least
   const int64_t tiles = (p.n_rows / p.batch + kStates - 1) / kStates;
   bp.cluster = 1;

@@ -1,0 +1,664 @@
+// The gradient of cross attention on the fifth-generation tensor cores, in two kernels
+// that each form the weights again; every sum has one owner and one order, so there are no
+// atomics:
+//
+//   queries   a CTA has 128 rows (query tokens x heads of a KV head) and walks the states 128 at a time:
+//             S = Q K^T, G = dO V^T (TMEM);  T = P (G - D), P = 2^(S - lse), in q's type over S;  dQ += T K
+//   states    a CTA has 128 states and walks the rows 128 at a time:
+//             S^T = K Q^T, G^T = V dO^T;  P^T over S^T, T^T over G^T;  dV += P^T dO, dK += T^T Q
+//
+// D = <dO, O> of each row is formed by the first and kept for the second.  Seven products of a
+// tile where five would do if dQ were summed with atomics.  Heads of a KV head are rows of one
+// sum.  P and T are rounded to q's type (half a step of themselves; P times 2^12 in fp16, whose
+// range ends at 2^-24), sums are fp32.
+//
+// Roles: warps 0-7 turn S and G into P and T, a row of TMEM a thread, half of its columns each; 8
+// copies; 9 issues products; 10 puts zeros where a last tile's rows are no one's (a product sums
+// over them, times 0, and they may be NaN); 11 (states) the rows' lse and D.
+#include <atomic>
+
+#include "cross.cuh"
+#include "tensor_core.cuh"
+#include "warp_mma.cuh"
+
+namespace reskv {
+namespace {
+
+using namespace tc;
+
+constexpr int kTile = 128;                        // rows and states of a tile
+constexpr int kThreads = 384;
+constexpr int kCopyWarp = 8, kIssueWarp = 9, kTailWarp = 10, kStatsWarp = 11;
+constexpr int kRegsSoftmax = 232, kRegsIssue = 40;
+static_assert((2 * kRegsSoftmax + kRegsIssue) * 128 <= 168 * kThreads, "registers");
+constexpr int kHalf = kTile * 128;                // bytes of 128 rows of 64 elements
+
+struct GradParams {
+  CrossParams a;
+  CUtensorMap q, k, v, g;
+  int32_t tile_tokens;
+};
+
+// Half of a row in TMEM: columns at .. at + 63.
+__device__ __forceinline__ void load64(uint32_t at, float (&x)[64]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) load16(at + 16 * k, x + 16 * k);
+}
+__device__ __forceinline__ void landed64(float (&x)[64]) {
+  landed();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) defined16(x + 16 * k);
+}
+// 64 values in q's type over the first 32 of the 64 columns that they came from
+template <bool kF16>
+__device__ __forceinline__ void store64(uint32_t at, const float (&x)[64]) {
+  uint32_t w[32];
+#pragma unroll
+  for (int k = 0; k < 32; ++k) w[k] = pack_two<kF16>(x[2 * k], x[2 * k + 1]);
+  store32(at, w);
+  stored();
+}
+// and where step k of a product finds its 16 of them
+__device__ __forceinline__ uint32_t step_of(uint32_t at, int k) { return at + uint32_t((k >> 2) * 64 + (k & 3) * 8); }
+
+// Columns [c0, c0 + n) of a thread's TMEM row, times f, to y in 16 bits.
+template <bool kF16, int N>
+__device__ __forceinline__ void store_columns(uint32_t at, float f, uint16_t* y, bool real) {
+#pragma unroll 1
+  for (int c = 0; c < N / 16; ++c) {
+    float o[16];
+    load16(at + 16 * c, o);
+    landed();
+    defined16(o);
+    if (real) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = pack_two<kF16>(o[8 * k + 2 * e] * f, o[8 * k + 2 * e + 1] * f);
+        reinterpret_cast<uint4*>(y)[2 * c + k] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+}
+template <int N>
+__device__ __forceinline__ void store_zeros(uint16_t* y) {
+#pragma unroll 1
+  for (int k = 0; k < N / 8; ++k) reinterpret_cast<uint4*>(y)[k] = make_uint4(0, 0, 0, 0);
+}
+
+// Zeros into rows [r0, r1) of a tile in shared memory (one warp).
+template <int D>
+__device__ __forceinline__ void clear_rows(uint8_t* tile, int r0, int r1, int lane) {
+  const int words = (r1 - r0) * 8;
+  for (int i = lane; i < words * (D / 64); i += 32) {
+    const int x = i / words;
+    *reinterpret_cast<uint4*>(tile + x * kHalf + r0 * 128 + (i - x * words) * 16) = make_uint4(0, 0, 0, 0);
+  }
+}
+
+template <bool kF16>
+__device__ __forceinline__ float dot8(uint4 a, uint4 b) {
+  const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float2 u, v;
+    if constexpr (kF16) {
+      u = __half22float2(*reinterpret_cast<const __half2*>(&x[i]));
+      v = __half22float2(*reinterpret_cast<const __half2*>(&y[i]));
+    } else {
+      u = bf16x2_to_float2(x[i]);
+      v = bf16x2_to_float2(y[i]);
+    }
+    s = fmaf(u.x, v.x, fmaf(u.y, v.y, s));
+  }
+  return s;
+}
+
+// --- queries -------------------------------------------------------------------
+
+template <int D>
+struct QuerySmem {
+  static constexpr int tile = D / 64 * kHalf;
+  static constexpr int slots = (224 * 1024 - 2 * tile) / tile > 8 ? 8 : (224 * 1024 - 2 * tile) / tile;
+  static constexpr int at_g = tile, at_ring = 2 * tile;
+  static constexpr int bytes = at_ring + slots * tile + 1024;
+};
+struct QueryShared {
+  uint64_t q, full[8], empty[8], s[2], g, g_taken, t, done, tail;
+  uint32_t tmem, abort;
+  float delta[2][kTile];
+};
+
+template <int D, bool kF16>
+__global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_constant__ GradParams gp) {
+  using S = QuerySmem<D>;
+  constexpr uint32_t kType = kF16 ? 0u : kBf16;
+  constexpr uint32_t kLogits = shape_of(kTile) | kType, kSums = shape_of(D) | kType | kAcross;
+  const CrossParams& p = gp.a;
+  extern __shared__ uint8_t dynamic[];
+  uint8_t* smem = dynamic + ((1024u - (smem_u32(dynamic) & 1023u)) & 1023u);
+  __shared__ __align__(16) QueryShared sh;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    mbar_init(&sh.q, 1);
+    for (int i = 0; i < S::slots; ++i) {
+      mbar_init(&sh.full[i], 1);
+      mbar_init(&sh.empty[i], 1);
+    }
+    mbar_init(&sh.s[0], 1);
+    mbar_init(&sh.s[1], 1);
+    mbar_init(&sh.g, 1);
+    mbar_init(&sh.g_taken, 8);
+    mbar_init(&sh.t, 8);
+    mbar_init(&sh.done, 1);
+    mbar_init(&sh.tail, 1);
+    sh.abort = 0;
+    fence_mbar_init();
+  }
+  wait_for_previous();
+
+  const int tt = gp.tile_tokens;
+  CrossBlock block;
+  if (!cross_block(p, p.q_begin, p.n_tokens, tt, int(blockIdx.x), lane, block)) return;      // the whole CTA
+  const int h = block.h, t0 = block.first;
+  const CrossSequence sq = cross_sequence(p, block.b);
+  const int n = (sq.seen + kTile - 1) / kTile, left = sq.seen - (n - 1) * kTile;
+  const bool cut = left < kTile;
+  // a softmax thread's row, and its half of the columns
+  const int c = warp >> 2, rt = (warp & 3) * 32 + lane, row_token = rt / p.group, token = t0 + row_token;
+  const bool real = warp < 8 && row_token < tt && token < sq.count;
+  const int head = h * p.group + rt - row_token * p.group;
+  const int64_t at_token = sq.q0 + token;
+  uint16_t* const dq = static_cast<uint16_t*>(p.d_q.data) + (real ? at_token * p.d_q.token + head * p.d_q.head + c * (D / 2) : 0);
+  if (n == 0) {                                   // the same for the whole CTA
+    if (real) store_zeros<D / 2>(dq);
+    return;
+  }
+  if (warp == kIssueWarp) take_columns(smem_u32(&sh.tmem));
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = sh.tmem, smem_q = smem_u32(smem), smem_g = smem_q + S::at_g, ring = smem_q + S::at_ring;
+  auto s_cols = [&](int i) { return tmem + uint32_t((i & 1) * kTile); };
+  const uint32_t g_cols = tmem + 2 * kTile, o_cols = tmem + 3 * kTile;
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+    if (warp == kCopyWarp) {
+      // --- copies: K0 V0 K1 V1 .. ---
+      if (elected()) {
+        mbar_arrive_expect_tx(&sh.q, uint32_t(2 * (D / 64) * tt * p.group * 128));
+        for (int x = 0; x < D / 64; ++x) {
+          copy_box(smem_q + x * kHalf, &gp.q, 64 * x, h * p.group, sq.q0 + t0, &sh.q);
+          copy_box(smem_g + x * kHalf, &gp.g, 64 * x, h * p.group, sq.q0 + t0, &sh.q);
+        }
+      }
+      __syncwarp();
+      int copied = 0;
+      bool ok = true;
+#pragma unroll 1
+      for (int op = 0; op < 2 * n && ok; ++op) {
+        const int slot = op % S::slots, turn = op / S::slots;
+        if (turn > 0) ok = role_wait(&sh.empty[slot], (turn - 1) & 1, &sh.abort, p.status);
+        if (!ok) break;
+        if (elected()) {
+          uint64_t* bar = cut && op == 2 * n - 2 ? &sh.tail : &sh.full[slot];
+          mbar_arrive_expect_tx(bar, S::tile);
+#pragma unroll
+          for (int x = 0; x < D / 64; ++x)
+            copy_box(ring + slot * S::tile + x * kHalf, op & 1 ? &gp.v : &gp.k, 64 * x, h, sq.k0 + op / 2 * kTile, bar);
+        }
+        __syncwarp();
+        copied = op + 1;
+      }
+      if (!ok && lane == 0) {                     // a wait gave up: let what is in flight land
+        mbar_wait_bounded(&sh.q, 0);
+        for (int op = copied > S::slots ? copied - S::slots : 0; op < copied; ++op) {
+          const bool last = cut && op == 2 * n - 2;
+          mbar_wait_bounded(last ? &sh.tail : &sh.full[op % S::slots], last ? 0 : (op / S::slots) & 1);
+        }
+      }
+      __syncwarp();
+    } else if (warp == kIssueWarp) {
+      // --- products ---
+      auto wait_tile = [&](int op) { return role_wait(&sh.full[op % S::slots], (op / S::slots) & 1, &sh.abort, p.status); };
+      auto tile_of = [&](int op) { return ring + op % S::slots * S::tile; };
+      auto outer = [&](uint32_t d, uint32_t a, uint32_t b, uint64_t* bar) {      // [128 x 128] = A B^T over D dims
+        fence_after();
+        if (elected()) {
+          const uint32_t a0 = operand(a), b0 = operand(b);
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k)
+            multiply<kRows128, kLogits>(d, a0 + (((k / 4) * kHalf + (k & 3) * 32) >> 4), b0 + (((k / 4) * kHalf + (k & 3) * 32) >> 4),
+                                        k > 0);
+          commit(bar);
+        }
+        __syncwarp();
+      };
+      auto release = [&](int op) {
+        if (elected()) commit(&sh.empty[op % S::slots]);
+        __syncwarp();
+      };
+      bool ok = role_wait(&sh.q, 0, &sh.abort, p.status) && wait_tile(0);
+      if (ok) {
+        outer(s_cols(0), smem_q, tile_of(0), &sh.s[0]);
+        ok = wait_tile(1);
+      }
+      if (ok) {
+        outer(g_cols, smem_g, tile_of(1), &sh.g);
+        release(1);
+      }
+#pragma unroll 1
+      for (int i = 0; i < n && ok; ++i) {
+        if (i + 1 < n) {
+          ok = wait_tile(2 * i + 2);
+          if (!ok) break;
+          outer(s_cols(i + 1), smem_q, tile_of(2 * i + 2), &sh.s[(i + 1) & 1]);
+          ok = wait_tile(2 * i + 3) && role_wait(&sh.g_taken, i & 1, &sh.abort, p.status);
+          if (!ok) break;
+          outer(g_cols, smem_g, tile_of(2 * i + 3), &sh.g);
+          release(2 * i + 3);
+        }
+        ok = role_wait(&sh.t, i & 1, &sh.abort, p.status);
+        if (!ok) break;
+        fence_after();
+        if (elected()) {
+          const uint32_t k0 = operand_across(tile_of(2 * i), kHalf);
+#pragma unroll
+          for (int k = 0; k < kTile / 16; ++k)
+            multiply_from<kRows128, kSums>(o_cols, step_of(s_cols(i), k), k0 + ((k * 16 * 128) >> 4), i > 0 || k > 0);
+        }
+        __syncwarp();
+        release(2 * i);
+      }
+      if (elected()) commit(&sh.done);
+      __syncwarp();
+      if (!ok) mbar_wait_bounded(&sh.done, 0);
+    } else if (warp == kTailWarp && cut) {
+      // --- behind the last state: T is zero there, keys may be anything ---
+      const int slot = (2 * n - 2) % S::slots;
+      if (role_wait(&sh.tail, 0, &sh.abort, p.status)) {
+        clear_rows<D>(smem + S::at_ring + slot * S::tile, left, kTile, lane);
+        fence_proxy_async_smem();
+        role_arrive(&sh.full[slot]);
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    // --- weights ---
+    const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
+    // D: half of the row's dims each
+    float delta = 0.f;
+    if (real) {
+      const uint4* g = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.d_o.data) + at_token * p.d_o.token +
+                                                      head * p.d_o.head + c * (D / 2));
+      const uint4* o = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.o.data) + at_token * p.o.token +
+                                                      head * p.o.head + c * (D / 2));
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) delta += dot8<kF16>(g[k], o[k]);
+    }
+    sh.delta[c][rt] = delta;
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    delta = sh.delta[0][rt] + sh.delta[1][rt];
+    const int64_t stat = at_token * p.heads + head;
+    if (real && c == 0) p.delta[stat] = delta;
+    const float f = p.scale2, lse2 = real ? p.lse[stat] * kLog2e : 0.f;
+    bool ok = true;
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+      ok = role_wait(&sh.s[i & 1], (i >> 1) & 1, &sh.abort, p.status) && role_wait(&sh.g, i & 1, &sh.abort, p.status);
+      if (!ok) break;
+      fence_after();
+      float x[64], y[64];
+      load64(s_cols(i) + lanes + 64 * c, x);
+      load64(g_cols + lanes + 64 * c, y);
+      landed64(x);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) defined16(y + 16 * k);
+      fence_before();
+      role_arrive(&sh.g_taken);
+#pragma unroll
+      for (int k = 0; k < 64; k += 2) {
+        const float2 e = ffma2(make_float2(x[k], x[k + 1]), make_float2(f, f), make_float2(-lse2, -lse2));
+        const float2 w = make_float2(exp2_fast(e.x), exp2_fast(e.y));
+        const float2 t = fmul2(w, fadd2(make_float2(y[k], y[k + 1]), make_float2(-delta, -delta)));
+        x[k] = t.x;
+        x[k + 1] = t.y;
+      }
+      const int upto = (i == n - 1 ? left : kTile) - 64 * c;
+      if (upto < 64) {
+#pragma unroll
+        for (int k = 0; k < 64; ++k)
+          if (k >= upto) x[k] = 0.f;
+      }
+      store64<kF16>(s_cols(i) + lanes + 64 * c, x);
+      fence_before();
+      role_arrive(&sh.t);
+    }
+    if (ok) ok = role_wait(&sh.done, 0, &sh.abort, p.status);
+    if (ok) {
+      fence_after();
+      store_columns<kF16, D / 2>(o_cols + lanes + c * (D / 2), p.scale, dq, real);
+    }
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (warp == kIssueWarp) give_columns(tmem);
+}
+
+// --- states --------------------------------------------------------------------
+
+constexpr int kStages = 2;
+template <int D>
+struct StateSmem {
+  static constexpr int tile = D / 64 * kHalf;
+  static constexpr int at_v = tile, at_ring = 2 * tile;               // a stage: Q, then dO
+  static constexpr int bytes = at_ring + kStages * 2 * tile + 1024;
+};
+struct StateShared {
+  uint64_t kv, full[kStages], empty[kStages], s, g, p, t, done, tail;
+  uint32_t tmem, abort;
+  float lse2[kStages][kTile], delta[kStages][kTile];
+};
+
+template <int D, bool kF16>
+__global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_constant__ GradParams gp) {
+  using S = StateSmem<D>;
+  constexpr uint32_t kType = kF16 ? 0u : kBf16;
+  constexpr uint32_t kLogits = shape_of(kTile) | kType, kSums = shape_of(D) | kType | kAcross;
+  constexpr float kUp = kF16 ? 12.f : 0.f, kDown = kF16 ? 0x1p-12f : 1.f;          // of P
+  const CrossParams& p = gp.a;
+  extern __shared__ uint8_t dynamic[];
+  uint8_t* smem = dynamic + ((1024u - (smem_u32(dynamic) & 1023u)) & 1023u);
+  __shared__ __align__(16) StateShared sh;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    mbar_init(&sh.kv, 1);
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&sh.full[i], 2);
+      mbar_init(&sh.empty[i], 1);
+    }
+    mbar_init(&sh.s, 1);
+    mbar_init(&sh.g, 1);
+    mbar_init(&sh.p, 8);
+    mbar_init(&sh.t, 8);
+    mbar_init(&sh.done, 1);
+    mbar_init(&sh.tail, 1);
+    sh.abort = 0;
+    fence_mbar_init();
+  }
+  wait_for_previous();
+
+  CrossBlock block;
+  if (!cross_block(p, p.kv_begin, p.n_rows, kTile, int(blockIdx.x), lane, block)) return;    // the whole CTA
+  const int h = block.h, j0 = block.first;
+  const CrossSequence sq = cross_sequence(p, block.b);
+  const int tt = gp.tile_tokens, used = tt * p.group;                 // rows of a full tile
+  const int n = j0 < sq.seen ? (sq.count + tt - 1) / tt : 0;
+  const int left = (sq.count - (n - 1) * tt) * p.group;               // rows of the last tile
+  const bool cut = left < used;
+  // a softmax thread's state; warps 0-3 write dV, 4-7 dK
+  const int c = warp >> 2, rt = (warp & 3) * 32 + lane, j = j0 + rt;
+  const bool owned = warp < 8 && j < sq.rows;
+  const CrossRows& to = c ? p.d_k : p.d_v;
+  uint16_t* const out = static_cast<uint16_t*>(to.data) + (owned ? (sq.k0 + j) * to.token + h * to.head : 0);
+  if (n == 0) {                                   // nobody sees them: the same for the whole CTA
+    if (owned) store_zeros<D>(out);
+    return;
+  }
+  if (warp == kIssueWarp) take_columns(smem_u32(&sh.tmem));
+  if (used < kTile && warp < 2 * kStages) {       // rows that no copy writes
+    clear_rows<D>(smem + S::at_ring + warp * S::tile, used, kTile, lane);
+    fence_proxy_async_smem();
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = sh.tmem, smem_k = smem_u32(smem), smem_v = smem_k + S::at_v, ring = smem_k + S::at_ring;
+  const uint32_t s_cols = tmem, g_cols = tmem + kTile, v_cols = tmem + 2 * kTile, k_cols = tmem + 3 * kTile;
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+    if (warp == kCopyWarp) {
+      // --- copies ---
+      if (elected()) {
+        mbar_arrive_expect_tx(&sh.kv, 2 * S::tile);
+        for (int x = 0; x < D / 64; ++x) {
+          copy_box(smem_k + x * kHalf, &gp.k, 64 * x, h, sq.k0 + j0, &sh.kv);
+          copy_box(smem_v + x * kHalf, &gp.v, 64 * x, h, sq.k0 + j0, &sh.kv);
+        }
+      }
+      __syncwarp();
+      int copied = 0;
+      bool ok = true;
+#pragma unroll 1
+      for (int i = 0; i < n && ok; ++i) {
+        const int stage = i % kStages;
+        if (i >= kStages) ok = role_wait(&sh.empty[stage], (i / kStages - 1) & 1, &sh.abort, p.status);
+        if (!ok) break;
+        if (elected()) {
+          uint64_t* bar = cut && i == n - 1 ? &sh.tail : &sh.full[stage];
+          mbar_arrive_expect_tx(bar, uint32_t(2 * (D / 64) * used * 128));
+          const uint32_t dst = ring + stage * 2 * S::tile;
+#pragma unroll
+          for (int x = 0; x < D / 64; ++x) {
+            copy_box(dst + x * kHalf, &gp.q, 64 * x, h * p.group, sq.q0 + i * tt, bar);
+            copy_box(dst + S::tile + x * kHalf, &gp.g, 64 * x, h * p.group, sq.q0 + i * tt, bar);
+          }
+        }
+        __syncwarp();
+        copied = i + 1;
+      }
+      if (!ok && lane == 0) {                     // a wait gave up: let what is in flight land
+        mbar_wait_bounded(&sh.kv, 0);
+        for (int i = copied > kStages ? copied - kStages : 0; i < copied; ++i) {
+          const bool last = cut && i == n - 1;
+          mbar_wait_bounded(last ? &sh.tail : &sh.full[i % kStages], last ? 0 : (i / kStages) & 1);
+        }
+      }
+      __syncwarp();
+    } else if (warp == kIssueWarp) {
+      // --- products ---
+      auto wait_tile = [&](int i) { return role_wait(&sh.full[i % kStages], (i / kStages) & 1, &sh.abort, p.status); };
+      auto outer = [&](uint32_t d, uint32_t a, uint32_t b, uint64_t* bar) {      // [128 x 128] = A B^T over D dims
+        fence_after();
+        if (elected()) {
+          const uint32_t a0 = operand(a), b0 = operand(b);
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k)
+            multiply<kRows128, kLogits>(d, a0 + (((k / 4) * kHalf + (k & 3) * 32) >> 4), b0 + (((k / 4) * kHalf + (k & 3) * 32) >> 4),
+                                        k > 0);
+          commit(bar);
+        }
+        __syncwarp();
+      };
+      auto add_to = [&](uint32_t d, uint32_t a, uint32_t b, bool add) {          // [128 x D] += A B over 128 rows
+        fence_after();
+        if (elected()) {
+          const uint32_t b0 = operand_across(b, kHalf);
+#pragma unroll
+          for (int k = 0; k < kTile / 16; ++k)
+            multiply_from<kRows128, kSums>(d, step_of(a, k), b0 + ((k * 16 * 128) >> 4), add || k > 0);
+        }
+        __syncwarp();
+      };
+      auto q_tile = [&](int i) { return ring + i % kStages * 2 * S::tile; };
+      bool ok = role_wait(&sh.kv, 0, &sh.abort, p.status) && wait_tile(0);
+      if (ok) {
+        outer(s_cols, smem_k, q_tile(0), &sh.s);
+        outer(g_cols, smem_v, q_tile(0) + S::tile, &sh.g);
+      }
+#pragma unroll 1
+      for (int i = 0; i < n && ok; ++i) {
+        ok = role_wait(&sh.p, i & 1, &sh.abort, p.status);
+        if (!ok) break;
+        add_to(v_cols, s_cols, q_tile(i) + S::tile, i > 0);
+        if (i + 1 < n) {
+          ok = wait_tile(i + 1);
+          if (!ok) break;
+          outer(s_cols, smem_k, q_tile(i + 1), &sh.s);
+        }
+        ok = role_wait(&sh.t, i & 1, &sh.abort, p.status);
+        if (!ok) break;
+        add_to(k_cols, g_cols, q_tile(i), i > 0);
+        if (elected()) commit(&sh.empty[i % kStages]);
+        __syncwarp();
+        if (i + 1 < n) outer(g_cols, smem_v, q_tile(i + 1) + S::tile, &sh.g);
+      }
+      if (elected()) commit(&sh.done);
+      __syncwarp();
+      if (!ok) mbar_wait_bounded(&sh.done, 0);
+    } else if (warp == kTailWarp) {
+      // --- the last tile's rows that are another sequence's ---
+      if (cut && role_wait(&sh.tail, 0, &sh.abort, p.status)) {
+        const int stage = (n - 1) % kStages;
+        uint8_t* tile = smem + S::at_ring + stage * 2 * S::tile;
+        clear_rows<D>(tile, left, used, lane);
+        clear_rows<D>(tile + S::tile, left, used, lane);
+        fence_proxy_async_smem();
+        role_arrive(&sh.full[stage]);
+      }
+    } else {
+      // --- the rows' sums and D ---
+      bool ok = true;
+#pragma unroll 1
+      for (int i = 0; i < n && ok; ++i) {
+        const int stage = i % kStages;
+        float l[4], e[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = lane + 32 * k, tk = i * tt + r / p.group;
+          const bool here = r < used && tk < sq.count;
+          const int64_t at = int64_t(sq.q0 + tk) * p.heads + h * p.group + r % p.group;
+          l[k] = here ? p.lse[at] : 0.f;
+          e[k] = here ? p.delta[at] : 0.f;
+        }
+        if (i >= kStages) ok = role_wait(&sh.empty[stage], (i / kStages - 1) & 1, &sh.abort, p.status);
+        if (!ok) break;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          sh.lse2[stage][lane + 32 * k] = fmaf(l[k], kLog2e, -kUp);
+          sh.delta[stage][lane + 32 * k] = e[k] * kDown;
+        }
+        role_arrive(&sh.full[stage]);
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    // --- weights: rows 64 c .. 64 c + 63 of a tile ---
+    const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
+    const float f = p.scale2;
+    bool ok = true;
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+      const int stage = i % kStages, upto = (i == n - 1 ? left : used) - 64 * c;
+      // (the tile's barrier also has its sums behind it)
+      ok = role_wait(&sh.full[stage], (i / kStages) & 1, &sh.abort, p.status) && role_wait(&sh.s, i & 1, &sh.abort, p.status);
+      if (!ok) break;
+      fence_after();
+      float x[64];
+      load64(s_cols + lanes + 64 * c, x);
+      landed64(x);
+      const float4* l4 = reinterpret_cast<const float4*>(&sh.lse2[stage][64 * c]);
+      const float4* e4 = reinterpret_cast<const float4*>(&sh.delta[stage][64 * c]);
+#pragma unroll
+      for (int k = 0; k < 64; k += 4) {
+        const float4 l = l4[k / 4];
+        const float2 u = ffma2(make_float2(x[k], x[k + 1]), make_float2(f, f), make_float2(-l.x, -l.y));
+        const float2 v = ffma2(make_float2(x[k + 2], x[k + 3]), make_float2(f, f), make_float2(-l.z, -l.w));
+        x[k] = exp2_fast(u.x);
+        x[k + 1] = exp2_fast(u.y);
+        x[k + 2] = exp2_fast(v.x);
+        x[k + 3] = exp2_fast(v.y);
+      }
+      if (upto < 64) {
+#pragma unroll
+        for (int k = 0; k < 64; ++k)
+          if (k >= upto) x[k] = 0.f;
+      }
+      store64<kF16>(s_cols + lanes + 64 * c, x);
+      fence_before();
+      role_arrive(&sh.p);
+      ok = role_wait(&sh.g, i & 1, &sh.abort, p.status);
+      if (!ok) break;
+      fence_after();
+      float y[64];
+      load64(g_cols + lanes + 64 * c, y);
+      landed64(y);
+#pragma unroll
+      for (int k = 0; k < 64; k += 4) {
+        const float4 e = e4[k / 4];
+        const float2 u = fmul2(make_float2(x[k], x[k + 1]),
+                               ffma2(make_float2(y[k], y[k + 1]), make_float2(kDown, kDown), make_float2(-e.x, -e.y)));
+        const float2 v = fmul2(make_float2(x[k + 2], x[k + 3]),
+                               ffma2(make_float2(y[k + 2], y[k + 3]), make_float2(kDown, kDown), make_float2(-e.z, -e.w)));
+        y[k] = u.x;
+        y[k + 1] = u.y;
+        y[k + 2] = v.x;
+        y[k + 3] = v.y;
+      }
+      if (upto < 64) {
+#pragma unroll
+        for (int k = 0; k < 64; ++k)
+          if (k >= upto) y[k] = 0.f;
+      }
+      store64<kF16>(g_cols + lanes + 64 * c, y);
+      fence_before();
+      role_arrive(&sh.t);
+    }
+    if (ok) ok = role_wait(&sh.done, 0, &sh.abort, p.status);
+    if (ok) {
+      fence_after();
+      const bool seen = owned && j < sq.seen;
+      store_columns<kF16, D>((c ? k_cols : v_cols) + lanes, c ? p.scale : kDown, out, seen);
+      if (owned && !seen) store_zeros<D>(out);
+    }
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (warp == kIssueWarp) give_columns(tmem);
+}
+
+// One kernel; its shared memory limit is raised once a device.
+template <int kBytes, typename F>
+cudaError_t launch(F kernel, std::atomic<uint64_t>& raised, const GradParams& gp, int64_t blocks, int dev, cudaStream_t s) {
+  if (blocks == 0) return cudaSuccess;
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+  if (!(raised.load(std::memory_order_relaxed) & bit) || !bit) {
+    const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (err != cudaSuccess) return err;
+    raised.fetch_or(bit, std::memory_order_relaxed);
+  }
+  return launch_early(kernel, unsigned(blocks), kThreads, kBytes, s, gp);
+}
+
+template <int D, bool kF16>
+cudaError_t both(const GradParams& gp, int dev, cudaStream_t s) {
+  static std::atomic<uint64_t> raised_q{0}, raised_kv{0};
+  const CrossParams& p = gp.a;
+  const cudaError_t err = launch<QuerySmem<D>::bytes>(k_cross_grad_q<D, kF16>, raised_q, gp,
+                                                      cross_blocks(p, p.q_begin, p.n_tokens, gp.tile_tokens), dev, s);
+  return err != cudaSuccess ? err
+                            : launch<StateSmem<D>::bytes>(k_cross_grad_kv<D, kF16>, raised_kv, gp,
+                                                          cross_blocks(p, p.kv_begin, p.n_rows, kTile), dev, s);
+}
+
+}  // namespace
+
+cudaError_t launch_cross_grad(const CrossParams& p, const CrossMaps& maps, int d, int dev, cudaStream_t s) {
+  GradParams gp{};
+  gp.a = p;
+  gp.q = maps.q;
+  gp.k = maps.k;
+  gp.v = maps.v;
+  gp.g = maps.d_o;
+  gp.tile_tokens = cross_tile_tokens(p.group);
+  if (d == 128) return p.f16 ? both<128, true>(gp, dev, s) : both<128, false>(gp, dev, s);
+  return p.f16 ? both<64, true>(gp, dev, s) : both<64, false>(gp, dev, s);
+}
+
+}  // namespace reskv

@@ -43,6 +43,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return d;
 }
 
+template <bool kF16>
+__device__ __forceinline__ uint32_t pack_two(float lo, float hi) {
+  return kF16 ? pack_f16(lo, hi) : pack_bf16(lo, hi);
+}
+
 // what pack_f16 left over
 __device__ __forceinline__ uint32_t rest_f16(float lo, float hi, uint32_t packed) {
   const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&packed));
