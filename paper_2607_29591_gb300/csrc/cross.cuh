@@ -3,6 +3,8 @@
 #pragma once
 #include <cuda.h>
 
+#include <atomic>
+
 #include "paged.cuh"
 
 namespace reskv {
@@ -58,13 +60,14 @@ __device__ __forceinline__ CrossSequence cross_sequence(const CrossParams& p, in
   return s;
 }
 
-// The block that a CTA takes: of the `count` tokens (or rows) of every sequence, `per` a block, for
-// each KV head; blocks of a KV head lie side by side.  One warp; false: no such block.
+// The block that a CTA takes: of the `count` tokens (or rows) of every sequence, `times` things each,
+// `per` of those a block, for each KV head; blocks of a KV head lie side by side.  One warp; false: no
+// such block.
 struct CrossBlock {
-  int b, h, first;                // sequence, KV head, first token within the sequence
+  int b, h, first;                // sequence, KV head, first of its things
 };
 __device__ __forceinline__ bool cross_block(const CrossParams& p, const int32_t* begin, int64_t total, int per, int item, int lane,
-                                            CrossBlock& out) {
+                                            CrossBlock& out, int times = 1) {
   int blocks;
   if (begin) {
     bool found = false;
@@ -73,7 +76,7 @@ __device__ __forceinline__ bool cross_block(const CrossParams& p, const int32_t*
       int mine = 0, first, count;
       if (b0 + lane < p.batch) {
         cross_range(begin, b0 + lane, p.batch, total, p.status, first, count);
-        mine = (count + per - 1) / per;
+        mine = (count * times + per - 1) / per;
       }
       int upto = mine * p.kv_heads;
 #pragma unroll
@@ -94,7 +97,7 @@ __device__ __forceinline__ bool cross_block(const CrossParams& p, const int32_t*
     }
     if (!found) return false;
   } else {
-    blocks = (int(total / p.batch) + per - 1) / per;
+    blocks = (int(total / p.batch) * times + per - 1) / per;
     out.b = item / (blocks * p.kv_heads);
     item -= out.b * blocks * p.kv_heads;
   }
@@ -103,8 +106,60 @@ __device__ __forceinline__ bool cross_block(const CrossParams& p, const int32_t*
   return true;
 }
 // Blocks that a call may have.
-inline int64_t cross_blocks(const CrossParams& p, const int32_t* begin, int64_t total, int per) {
-  return begin ? (total / per + p.batch) * p.kv_heads : (total / p.batch + per - 1) / per * p.batch * p.kv_heads;
+inline int64_t cross_blocks(const CrossParams& p, const int32_t* begin, int64_t total, int per, int times = 1) {
+  return begin ? (total * times / per + p.batch) * p.kv_heads : (total / p.batch * times + per - 1) / per * p.batch * p.kv_heads;
+}
+
+// --- clusters ---
+__device__ __forceinline__ uint32_t rank_in_cluster() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void sync_cluster() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t of_rank(uint32_t local, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float read_cluster(uint32_t at) {
+  float x;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
+  return x;
+}
+__device__ __forceinline__ float4 read_cluster4(uint32_t at) {
+  float4 x;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at) : "memory");
+  return x;
+}
+// One launch with programmatic dependence, in clusters where `cluster` > 1.
+template <typename K, typename P>
+cudaError_t launch_clusters(K kernel, int64_t blocks, int cluster, int threads, size_t shared, cudaStream_t s, const P& params) {
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = unsigned(cluster);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(unsigned(blocks * cluster));
+  cfg.blockDim = dim3(unsigned(threads));
+  cfg.dynamicSmemBytes = shared;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, params);
+}
+// A kernel's shared memory limit, raised once a device.
+template <typename K>
+cudaError_t raise_shared(K kernel, std::atomic<uint64_t>& raised, int bytes, int dev) {
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+  if (bit && (raised.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (err == cudaSuccess) raised.fetch_or(bit, std::memory_order_relaxed);
+  return err;
 }
 
 // Many query rows, on the fifth-generation tensor cores; cross_blocks.cu.  Copies take whole tokens:
@@ -113,6 +168,9 @@ struct CrossMaps {
   CUtensorMap q, k, v, d_o;
 };
 inline int cross_tile_tokens(int group) { return 128 / group; }
+// Few query rows: cross_rows.cu.  Copies of kRowStates states.
+constexpr int kRowStates = 64;
+cudaError_t launch_cross_rows(const CrossParams& p, const CrossMaps& maps, int d, int dev, int sms, cudaStream_t s);
 cudaError_t launch_cross_grad(const CrossParams& p, const CrossMaps& maps, int d, int dev, cudaStream_t s);      // cross_grad.cu
 cudaError_t launch_cross_blocks(const CrossParams& p, const CrossMaps& maps, int d, int dev, int sms, cudaStream_t s);
 

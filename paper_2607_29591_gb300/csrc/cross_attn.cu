@@ -70,12 +70,15 @@ cudaError_t device_sms(int* dev, int* sms) {
 }
 
 // false: rows that copies cannot address
-bool encode_maps(CrossMaps* maps, const reskv_cross_attn_args* a, const CrossParams& p) {
+bool encode_maps(CrossMaps* maps, const reskv_cross_attn_args* a, const CrossParams& p, int box_states) {
   return a->n_rows > 0 && a->n_tokens > 0 &&
          encode_heads(&maps->q, a->q, a->n_tokens, a->head_dim, p.group, cross_tile_tokens(p.group)) &&
-         encode_heads(&maps->k, a->k, a->n_rows, a->head_dim, 1, 128) &&
-         encode_heads(&maps->v, a->v, a->n_rows, a->head_dim, 1, 128);
+         encode_heads(&maps->k, a->k, a->n_rows, a->head_dim, 1, box_states) &&
+         encode_heads(&maps->v, a->v, a->n_rows, a->head_dim, 1, box_states);
 }
+
+// The kernel of few rows where a sequence and KV head have kFewRows of them on average.
+constexpr int kFewRows = 16;
 
 }  // namespace
 }  // namespace reskv
@@ -93,8 +96,11 @@ extern "C" reskv_status reskv_cross_attn(const reskv_cross_attn_args* a, void* s
     const cudaError_t err = device_sms(&dev, &sms);
     if (err != cudaSuccess) return launch_result(err, "reading the device");
     CrossMaps maps;
-    const bool fast = rows_aligned(a->o, 16) && encode_maps(&maps, a, p);
-    return launch_result(fast ? launch_cross_blocks(p, maps, a->head_dim, dev, sms, s) : launch_cross_general(p, a->head_dim, s),
+    const bool few = a->n_tokens * p.group <= kFewRows * int64_t(a->batch);
+    const bool fast = rows_aligned(a->q, 16) && rows_aligned(a->o, 16) && encode_maps(&maps, a, p, few ? kRowStates : 128);
+    return launch_result(!fast ? launch_cross_general(p, a->head_dim, s)
+                         : few ? launch_cross_rows(p, maps, a->head_dim, dev, sms, s)
+                               : launch_cross_blocks(p, maps, a->head_dim, dev, sms, s),
                          "cross attention");
   });
 }
@@ -141,7 +147,7 @@ extern "C" reskv_status reskv_cross_attn_backward(const reskv_cross_attn_args* a
     if (err != cudaSuccess) return launch_result(err, "reading the device");
     CrossMaps maps;
     const bool fast = tokens && rows && rows_aligned(a->o, 16) && rows_aligned(*d_o, 16) && rows_aligned(*d_q, 16) &&
-                      rows_aligned(*d_k, 16) && rows_aligned(*d_v, 16) && encode_maps(&maps, a, p) &&
+                      rows_aligned(*d_k, 16) && rows_aligned(*d_v, 16) && encode_maps(&maps, a, p, 128) &&
                       encode_heads(&maps.d_o, *d_o, a->n_tokens, a->head_dim, p.group, cross_tile_tokens(p.group));
     return launch_result(fast ? launch_cross_grad(p, maps, a->head_dim, dev, s) : launch_cross_grad_general(p, a->head_dim, s),
                          "the gradient of cross attention");

@@ -24,8 +24,6 @@
 //
 // The reference of a row moves only when weights pass 2^14; it then lies 6 below the largest
 // logit.  No largest logit is looked for otherwise.
-#include <atomic>
-
 #include "cross.cuh"
 #include "tensor_core.cuh"
 #include "warp_mma.cuh"
@@ -64,30 +62,6 @@ struct BlocksShared {
   uint64_t q, full[8], empty[8], s[2], p[2], done, tail;
   uint32_t tmem, abort;
 };
-
-__device__ __forceinline__ uint32_t rank_in_cluster() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void sync_cluster() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t of_rank(uint32_t local, uint32_t rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
-  return r;
-}
-__device__ __forceinline__ float read_cluster(uint32_t at) {
-  float x;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
-  return x;
-}
-__device__ __forceinline__ float4 read_cluster4(uint32_t at) {
-  float4 x;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at) : "memory");
-  return x;
-}
 
 template <int D, bool kF16, bool kSplit>
 __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_constant__ BlocksParams bp) {
@@ -453,29 +427,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
 
 template <int D, bool kF16, bool kSplit>
 cudaError_t launch(const BlocksParams& bp, int64_t items, int dev, cudaStream_t s) {
-  // the kernel's shared memory limit, raised once a device
   static std::atomic<uint64_t> raised{0};
-  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
-  if (!(raised.load(std::memory_order_relaxed) & bit) || !bit) {
-    const cudaError_t err = cudaFuncSetAttribute(k_cross_blocks<D, kF16, kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 BlocksSmem<D, kSplit>::bytes);
-    if (err != cudaSuccess) return err;
-    raised.fetch_or(bit, std::memory_order_relaxed);
-  }
-  cudaLaunchAttribute attr[2]{};
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = unsigned(bp.cluster);
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(unsigned(items * bp.cluster));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = BlocksSmem<D, kSplit>::bytes;
-  cfg.stream = s;
-  cfg.attrs = attr;
-  cfg.numAttrs = bp.cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, k_cross_blocks<D, kF16, kSplit>, bp);
+  const cudaError_t err = raise_shared(k_cross_blocks<D, kF16, kSplit>, raised, BlocksSmem<D, kSplit>::bytes, dev);
+  return err != cudaSuccess ? err
+                            : launch_clusters(k_cross_blocks<D, kF16, kSplit>, items, bp.cluster, kThreads, BlocksSmem<D, kSplit>::bytes, s, bp);
 }
 
 }  // namespace

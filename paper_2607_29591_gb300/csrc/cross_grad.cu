@@ -15,8 +15,6 @@
 // Roles: warps 0-7 turn S and G into P and T, a row of TMEM a thread, half of its columns each; 8
 // copies; 9 issues products; 10 puts zeros where a last tile's rows are no one's (a product sums
 // over them, times 0, and they may be NaN); 11 (states) the rows' lse and D.
-#include <atomic>
-
 #include "cross.cuh"
 #include "tensor_core.cuh"
 #include "warp_mma.cuh"
@@ -623,28 +621,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
   if (warp == kIssueWarp) give_columns(tmem);
 }
 
-// One kernel; its shared memory limit is raised once a device.
-template <int kBytes, typename F>
-cudaError_t launch(F kernel, std::atomic<uint64_t>& raised, const GradParams& gp, int64_t blocks, int dev, cudaStream_t s) {
-  if (blocks == 0) return cudaSuccess;
-  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
-  if (!(raised.load(std::memory_order_relaxed) & bit) || !bit) {
-    const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
-    if (err != cudaSuccess) return err;
-    raised.fetch_or(bit, std::memory_order_relaxed);
-  }
-  return launch_early(kernel, unsigned(blocks), kThreads, kBytes, s, gp);
-}
-
 template <int D, bool kF16>
 cudaError_t both(const GradParams& gp, int dev, cudaStream_t s) {
   static std::atomic<uint64_t> raised_q{0}, raised_kv{0};
   const CrossParams& p = gp.a;
-  const cudaError_t err = launch<QuerySmem<D>::bytes>(k_cross_grad_q<D, kF16>, raised_q, gp,
-                                                      cross_blocks(p, p.q_begin, p.n_tokens, gp.tile_tokens), dev, s);
-  return err != cudaSuccess ? err
-                            : launch<StateSmem<D>::bytes>(k_cross_grad_kv<D, kF16>, raised_kv, gp,
-                                                          cross_blocks(p, p.kv_begin, p.n_rows, kTile), dev, s);
+  cudaError_t err = raise_shared(k_cross_grad_q<D, kF16>, raised_q, QuerySmem<D>::bytes, dev);
+  if (err == cudaSuccess) err = raise_shared(k_cross_grad_kv<D, kF16>, raised_kv, StateSmem<D>::bytes, dev);
+  if (err == cudaSuccess)
+    err = launch_clusters(k_cross_grad_q<D, kF16>, cross_blocks(p, p.q_begin, p.n_tokens, gp.tile_tokens), 1, kThreads,
+                          QuerySmem<D>::bytes, s, gp);
+  if (err == cudaSuccess)
+    err = launch_clusters(k_cross_grad_kv<D, kF16>, cross_blocks(p, p.kv_begin, p.n_rows, kTile), 1, kThreads, StateSmem<D>::bytes,
+                          s, gp);
+  return err;
 }
 
 }  // namespace
