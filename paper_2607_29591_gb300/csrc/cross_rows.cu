@@ -322,9 +322,12 @@ cudaError_t launch(const RowsParams& rp, int dev, int sms, cudaStream_t s) {
   // about as many as there are: with q_begin there may be one more a sequence
   const int64_t rows = p.n_tokens / p.batch * p.group, sure = ((rows + 8 * NB - 1) / (8 * NB) + (rows == 0)) * p.batch * p.kv_heads;
   const int64_t tiles = (p.n_rows / p.batch + kRowStates - 1) / kRowStates;
+  // As many CTAs as SMs at least; what a CTA takes beside its states (some 6 us) makes more of them
+  // slower: 16 x 16 heads of 64, 5 beams over 1500 states 19 us by one CTA a head, 25 by 4, 42 by 8; 64 heads
+  // over 3000 states, 16 rows each, 26 by 2, 24 by 4, 33 by 8; 32 heads over 8192 28 by 8.
   RowsParams l = rp;
   l.cluster = 1;
-  while (l.cluster < 8 && sure * l.cluster < 8 * sms && l.cluster * 2 <= tiles) l.cluster *= 2;
+  while (l.cluster < 8 && sure * l.cluster < sms && l.cluster * 2 <= tiles) l.cluster *= 2;
   return launch_clusters(k_cross_rows<D, kF16, NB>, items, l.cluster, kThreads, RowsSmem<D, NB>::bytes, s, l);
 }
 
