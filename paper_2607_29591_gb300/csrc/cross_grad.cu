@@ -3,14 +3,20 @@
 // atomics:
 //
 //   queries   a CTA has 128 rows (query tokens x heads of a KV head) and walks the states 128 at a time:
-//             S = Q K^T, G = dO V^T (TMEM);  T = P (G - D), P = 2^(S - lse), in q's type over S;  dQ += T K
+//             S = Q K^T, G = dO V^T (TMEM);  P = 2^(S - lse) over S, T = P (G - D) over G, in q's type;
+//             B += P K, dQ += T K
 //   states    a CTA has 128 states and walks the rows 128 at a time:
 //             S^T = K Q^T, G^T = V dO^T;  P^T over S^T, T^T over G^T;  dV += P^T dO, dK += T^T Q
 //
-// D = <dO, O> of each row is formed by the first and kept for the second.  Seven products of a
-// tile where five would do if dQ were summed with atomics.  Heads of a KV head are rows of one
-// sum.  P and T are rounded to q's type (half a step of themselves; P times 2^12 in fp16, whose
-// range ends at 2^-24), sums are fp32.
+// D = <dO, O> with the O that was rounded to 16 bits is off by up to half a step of it, which
+// in rows whose attention has a peak is much of G - D (a batch of 512 tokens over 577 states:
+// dQ off by 8e-3 of itself, of which 2.3e-3 are the roundings of T and dQ).  As the P of a row sum up to
+// 1, the row's sum of T is what D lacks: D + sum T goes to the second kernel, and dQ is corrected
+// to T K - e P K.  There e sums T as rounded, so that the weights of the K sum up to 0 as those of the
+// formula do: what all keys of a row have in common (they are akin to its query) stays out of
+// dQ, and with it T's roundings (dQ 3.3e-3 off otherwise).  So a tile costs eight products; seven without that, five if dQ
+// were summed with atomics.  Heads of a KV head are rows of one sum.  P and T are rounded to q's
+// type (half a step of themselves; P times 2^12 in fp16, whose range ends at 2^-24), sums are fp32.
 //
 // Roles: warps 0-7 turn S and G into P and T, a row of TMEM a thread, half of its columns each; 8
 // copies; 9 issues products; 10 puts zeros where a last tile's rows are no one's (a product sums
@@ -47,13 +53,18 @@ __device__ __forceinline__ void landed64(float (&x)[64]) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) defined16(x + 16 * k);
 }
-// 64 values in q's type over the first 32 of the 64 columns that they came from
+// 64 values in q's type over the first 32 of the 64 columns that they came from; `sum`: and their sum, as rounded
 template <bool kF16>
-__device__ __forceinline__ void store64(uint32_t at, const float (&x)[64]) {
+__device__ __forceinline__ void store64(uint32_t at, const float (&x)[64], float2* sum = nullptr) {
   uint32_t w[32];
 #pragma unroll
   for (int k = 0; k < 32; ++k) w[k] = pack_two<kF16>(x[2 * k], x[2 * k + 1]);
   store32(at, w);
+  if (sum) {
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+      *sum = fadd2(*sum, kF16 ? __half22float2(*reinterpret_cast<const __half2*>(&w[k])) : bf16x2_to_float2(w[k]));
+  }
   stored();
 }
 // and where step k of a product finds its 16 of them
@@ -124,9 +135,9 @@ struct QuerySmem {
   static constexpr int bytes = at_ring + slots * tile + 1024;
 };
 struct QueryShared {
-  uint64_t q, full[8], empty[8], s[2], g, g_taken, t, done, tail;
+  uint64_t q, full[8], empty[8], s, g, p, t, done, tail;
   uint32_t tmem, abort;
-  float delta[2][kTile];
+  float sums[2][kTile];           // D at the beginning, sums of T at the end
 };
 
 template <int D, bool kF16>
@@ -134,6 +145,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
   using S = QuerySmem<D>;
   constexpr uint32_t kType = kF16 ? 0u : kBf16;
   constexpr uint32_t kLogits = shape_of(kTile) | kType, kSums = shape_of(D) | kType | kAcross;
+  constexpr float kUp = kF16 ? 12.f : 0.f, kDown = kF16 ? 0x1p-12f : 1.f;          // of P
   const CrossParams& p = gp.a;
   extern __shared__ uint8_t dynamic[];
   uint8_t* smem = dynamic + ((1024u - (smem_u32(dynamic) & 1023u)) & 1023u);
@@ -145,10 +157,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
       mbar_init(&sh.full[i], 1);
       mbar_init(&sh.empty[i], 1);
     }
-    mbar_init(&sh.s[0], 1);
-    mbar_init(&sh.s[1], 1);
+    mbar_init(&sh.s, 1);
     mbar_init(&sh.g, 1);
-    mbar_init(&sh.g_taken, 8);
+    mbar_init(&sh.p, 8);
     mbar_init(&sh.t, 8);
     mbar_init(&sh.done, 1);
     mbar_init(&sh.tail, 1);
@@ -179,8 +190,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
   __syncthreads();
   fence_after();
   const uint32_t tmem = sh.tmem, smem_q = smem_u32(smem), smem_g = smem_q + S::at_g, ring = smem_q + S::at_ring;
-  auto s_cols = [&](int i) { return tmem + uint32_t((i & 1) * kTile); };
-  const uint32_t g_cols = tmem + 2 * kTile, o_cols = tmem + 3 * kTile;
+  const uint32_t s_cols = tmem, g_cols = tmem + kTile, b_cols = tmem + 2 * kTile, o_cols = tmem + 3 * kTile;
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
@@ -239,9 +249,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
         if (elected()) commit(&sh.empty[op % S::slots]);
         __syncwarp();
       };
+      auto add_to = [&](uint32_t d, uint32_t a, uint32_t b, bool add) {          // [128 x D] += A B over 128 states
+        fence_after();
+        if (elected()) {
+          const uint32_t b0 = operand_across(b, kHalf);
+#pragma unroll
+          for (int k = 0; k < kTile / 16; ++k)
+            multiply_from<kRows128, kSums>(d, step_of(a, k), b0 + ((k * 16 * 128) >> 4), add || k > 0);
+        }
+        __syncwarp();
+      };
       bool ok = role_wait(&sh.q, 0, &sh.abort, p.status) && wait_tile(0);
       if (ok) {
-        outer(s_cols(0), smem_q, tile_of(0), &sh.s[0]);
+        outer(s_cols, smem_q, tile_of(0), &sh.s);
         ok = wait_tile(1);
       }
       if (ok) {
@@ -250,32 +270,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
       }
 #pragma unroll 1
       for (int i = 0; i < n && ok; ++i) {
+        ok = role_wait(&sh.p, i & 1, &sh.abort, p.status);
+        if (!ok) break;
+        add_to(b_cols, s_cols, tile_of(2 * i), i > 0);
         if (i + 1 < n) {
           ok = wait_tile(2 * i + 2);
           if (!ok) break;
-          outer(s_cols(i + 1), smem_q, tile_of(2 * i + 2), &sh.s[(i + 1) & 1]);
-          ok = wait_tile(2 * i + 3) && role_wait(&sh.g_taken, i & 1, &sh.abort, p.status);
+          outer(s_cols, smem_q, tile_of(2 * i + 2), &sh.s);
+        }
+        ok = role_wait(&sh.t, i & 1, &sh.abort, p.status);
+        if (!ok) break;
+        add_to(o_cols, g_cols, tile_of(2 * i), i > 0);
+        release(2 * i);
+        if (i + 1 < n) {
+          ok = wait_tile(2 * i + 3);
           if (!ok) break;
           outer(g_cols, smem_g, tile_of(2 * i + 3), &sh.g);
           release(2 * i + 3);
         }
-        ok = role_wait(&sh.t, i & 1, &sh.abort, p.status);
-        if (!ok) break;
-        fence_after();
-        if (elected()) {
-          const uint32_t k0 = operand_across(tile_of(2 * i), kHalf);
-#pragma unroll
-          for (int k = 0; k < kTile / 16; ++k)
-            multiply_from<kRows128, kSums>(o_cols, step_of(s_cols(i), k), k0 + ((k * 16 * 128) >> 4), i > 0 || k > 0);
-        }
-        __syncwarp();
-        release(2 * i);
       }
       if (elected()) commit(&sh.done);
       __syncwarp();
       if (!ok) mbar_wait_bounded(&sh.done, 0);
     } else if (warp == kTailWarp && cut) {
-      // --- behind the last state: T is zero there, keys may be anything ---
+      // --- behind the last state: P and T are zero there, keys may be anything ---
       const int slot = (2 * n - 2) % S::slots;
       if (role_wait(&sh.tail, 0, &sh.abort, p.status)) {
         clear_rows<D>(smem + S::at_ring + slot * S::tile, left, kTile, lane);
@@ -297,48 +315,91 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) delta += dot8<kF16>(g[k], o[k]);
     }
-    sh.delta[c][rt] = delta;
+    sh.sums[c][rt] = delta;
     asm volatile("bar.sync 1, 256;" ::: "memory");
-    delta = sh.delta[0][rt] + sh.delta[1][rt];
+    delta = sh.sums[0][rt] + sh.sums[1][rt];
     const int64_t stat = at_token * p.heads + head;
-    if (real && c == 0) p.delta[stat] = delta;
-    const float f = p.scale2, lse2 = real ? p.lse[stat] * kLog2e : 0.f;
+    const float f = p.scale2, lse2 = real ? fmaf(p.lse[stat], kLog2e, -kUp) : 0.f, down = -delta * kDown;
+    float2 more = make_float2(0.f, 0.f), rounded = more;      // sums of T
     bool ok = true;
 #pragma unroll 1
     for (int i = 0; i < n; ++i) {
-      ok = role_wait(&sh.s[i & 1], (i >> 1) & 1, &sh.abort, p.status) && role_wait(&sh.g, i & 1, &sh.abort, p.status);
+      const int upto = (i == n - 1 ? left : kTile) - 64 * c;
+      ok = role_wait(&sh.s, i & 1, &sh.abort, p.status);
       if (!ok) break;
       fence_after();
-      float x[64], y[64];
-      load64(s_cols(i) + lanes + 64 * c, x);
-      load64(g_cols + lanes + 64 * c, y);
+      float x[64];
+      load64(s_cols + lanes + 64 * c, x);
       landed64(x);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) defined16(y + 16 * k);
-      fence_before();
-      role_arrive(&sh.g_taken);
 #pragma unroll
       for (int k = 0; k < 64; k += 2) {
         const float2 e = ffma2(make_float2(x[k], x[k + 1]), make_float2(f, f), make_float2(-lse2, -lse2));
-        const float2 w = make_float2(exp2_fast(e.x), exp2_fast(e.y));
-        const float2 t = fmul2(w, fadd2(make_float2(y[k], y[k + 1]), make_float2(-delta, -delta)));
-        x[k] = t.x;
-        x[k + 1] = t.y;
+        x[k] = exp2_fast(e.x);
+        x[k + 1] = exp2_fast(e.y);
       }
-      const int upto = (i == n - 1 ? left : kTile) - 64 * c;
       if (upto < 64) {
 #pragma unroll
         for (int k = 0; k < 64; ++k)
           if (k >= upto) x[k] = 0.f;
       }
-      store64<kF16>(s_cols(i) + lanes + 64 * c, x);
+      store64<kF16>(s_cols + lanes + 64 * c, x);
+      fence_before();
+      role_arrive(&sh.p);
+      ok = role_wait(&sh.g, i & 1, &sh.abort, p.status);
+      if (!ok) break;
+      fence_after();
+      float y[64];
+      load64(g_cols + lanes + 64 * c, y);
+      landed64(y);
+#pragma unroll
+      for (int k = 0; k < 64; k += 2) {
+        const float2 t = fmul2(make_float2(x[k], x[k + 1]),
+                               ffma2(make_float2(y[k], y[k + 1]), make_float2(kDown, kDown), make_float2(down, down)));
+        y[k] = t.x;
+        y[k + 1] = t.y;
+      }
+      if (upto < 64) {
+#pragma unroll
+        for (int k = 0; k < 64; ++k)
+          if (k >= upto) y[k] = 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 64; k += 2) more = fadd2(more, make_float2(y[k], y[k + 1]));
+      store64<kF16>(g_cols + lanes + 64 * c, y, &rounded);
       fence_before();
       role_arrive(&sh.t);
     }
     if (ok) ok = role_wait(&sh.done, 0, &sh.abort, p.status);
+    auto both_halves = [&](float x) {
+      sh.sums[c][rt] = x;
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      x = sh.sums[0][rt] + sh.sums[1][rt];
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      return x;
+    };
+    const float lacks = both_halves(more.x + more.y), e = both_halves(rounded.x + rounded.y);
+    if (real && c == 0) p.delta[stat] = delta + lacks;
     if (ok) {
       fence_after();
-      store_columns<kF16, D / 2>(o_cols + lanes + c * (D / 2), p.scale, dq, real);
+      const float back = -e * kDown;
+#pragma unroll 1
+      for (int m = 0; m < D / 32; ++m) {
+        float a[16], b[16];
+        load16(o_cols + lanes + c * (D / 2) + 16 * m, a);
+        load16(b_cols + lanes + c * (D / 2) + 16 * m, b);
+        landed();
+        defined16(a);
+        defined16(b);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) a[k] = fmaf(back, b[k], a[k]) * p.scale;
+        if (real) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            reinterpret_cast<uint4*>(dq)[2 * m + k] =
+                make_uint4(pack_two<kF16>(a[8 * k], a[8 * k + 1]), pack_two<kF16>(a[8 * k + 2], a[8 * k + 3]),
+                           pack_two<kF16>(a[8 * k + 4], a[8 * k + 5]), pack_two<kF16>(a[8 * k + 6], a[8 * k + 7]));
+        }
+      }
     }
   }
   fence_before();
