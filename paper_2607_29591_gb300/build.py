@@ -21,7 +21,7 @@ BUILD_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libreskv.so")
 SOURCES = ["reskv_api.cu", "decode_kernel.cu", "decode_mma.cu", "decode_cluster.cu",
            "construct.cu", "decode_noalloc.cu", "append.cu", "rope.cu", "paged.cu", "paged_attn.cu",
-           "paged_attn_blocks.cu", "paged_shared.cu", "cross_attn.cu", "cross_general.cu", "cross_blocks.cu", "cross_rows.cu",
+           "paged_attn_blocks.cu", "paged_prefix.cu", "paged_shared.cu", "cross_attn.cu", "cross_general.cu", "cross_blocks.cu", "cross_rows.cu",
            "cross_grad.cu"]
 BIND = os.path.join(HERE, "_bind.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

@@ -420,7 +420,7 @@ struct StateSmem {
 struct StateShared {
   uint64_t kv, full[kStages], empty[kStages], s, g, p, t, done, tail;
   uint32_t tmem, abort;
-  float lse2[kStages][kTile], delta[kStages][kTile];
+  alignas(16) float lse2[kStages][kTile], delta[kStages][kTile];
 };
 
 template <int D, bool kF16>

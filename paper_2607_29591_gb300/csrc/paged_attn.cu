@@ -69,7 +69,7 @@ constexpr int kUnitBits = 24;
 __device__ __forceinline__ int64_t tiles_of(int64_t x) { return x >> kUnitBits; }
 __device__ __forceinline__ int64_t units_of(int64_t x) { return x & ((int64_t(1) << kUnitBits) - 1); }
 
-template <int R>
+template <int R, bool kShared>
 struct RowCursor {
   int b, r0, h, tile;                             // tile: within the unit
   Sequence s;
@@ -89,7 +89,7 @@ struct RowCursor {
       else hi = mid;
     }
     b = lo;
-    s = sequence_of(p, b);
+    s = sequence_of<kShared>(p, b);
     int64_t left = x - tiles_of(prefix[b]);
 #pragma unroll 1
     for (r0 = 0;; r0 += R) {
@@ -112,7 +112,7 @@ struct RowCursor {
       else hi = mid;
     }
     b = lo;
-    s = sequence_of(p, lo);
+    s = sequence_of<kShared>(p, lo);
     tile = 0;
     int left = int(i - units_of(prefix[lo]));
     start = tiles_of(prefix[lo]);
@@ -137,7 +137,7 @@ struct RowCursor {
 #pragma unroll 1
       do ++b; while (b < p.batch && prefix[b + 1] == prefix[b]);        // nothing to do
       if (b >= p.batch) return;
-      s = sequence_of(p, b);
+      s = sequence_of<kShared>(p, b);
       r0 = 0;
     }
     block(p);
@@ -172,10 +172,10 @@ __device__ __forceinline__ void copy_tile(void* dst, const void* src, uint32_t b
       : "memory");
 }
 
-template <int D, int NG, bool kTwoPlanes, int R>
+template <int D, int NG, bool kTwoPlanes, int R, bool kShared>
 __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __grid_constant__ AttnParams p) {
   using S = AttnSmem<D, NG, R>;
-  using Cursor = RowCursor<R>;
+  using Cursor = RowCursor<R, kShared>;
   constexpr int kRows = R;
   constexpr TileShape ts{D, NG};
   constexpr int TB = ts.bytes(), SB = kStageTiles * TB, RS = record_stride(D), RF = record_floats(D, R);
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
   // the tiles of every sequence, and what they sum up to
 #pragma unroll 1
   for (int b = threadIdx.x; b < p.batch; b += blockDim.x) {
-    const Sequence s = sequence_of(p, b);
+    const Sequence s = sequence_of<kShared>(p, b);
     const int rows = s.count * p.group;
     int64_t n = 0;
     int longest = 0, blocks = 0;
@@ -295,14 +295,15 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     const int tpp = p.page_tokens / kTile;        // tiles of a page
     const int64_t page_bytes = int64_t(p.kv_heads) * tpp * TB;
     const uint8_t* head = p.pages;                // the unit's head in page 0
+    int64_t n_pages = p.n_pages;
     const uint8_t* src = head;                    // the next tile
     int in_unit = 0, in_page = 0;                 // tiles left of the unit and of the page, the next one included
     bool ok = false;                              // the page exists
     int page = 0;                                 // the page after this one, asked for a page ahead
     const int32_t* ask = p.page_table;
     auto turn_page = [&]() {                      // to `page`
-      ok = uint32_t(page) < uint32_t(p.n_pages);
-      if (!ok) report_status(p.status, kStatusBadIndex);
+      ok = uint32_t(page) < uint32_t(n_pages);
+      if (!ok) report_status(kShared && c.s.all ? p.prefix_status : p.status, kStatusBadIndex);
       src = head + (ok ? page : 0) * page_bytes;
       in_page = tpp;
       ++ask;
@@ -311,8 +312,15 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     auto begin_unit = [&]() {
       in_unit = c.k.tiles - c.tile;
       const int tile = c.k.first + c.tile, at = tile / tpp, first = tile - at * tpp;
-      head = p.pages + int64_t(c.h) * tpp * TB;
-      ask = p.page_table + int64_t(c.b) * p.table_pages + at;
+      if (kShared && c.s.all) {
+        head = p.prefix_data + int64_t(c.h) * tpp * TB;
+        ask = p.prefix_table + int64_t(c.b - p.own) * p.prefix_pages + at;
+        n_pages = p.prefix_n_pages;
+      } else {
+        head = p.pages + int64_t(c.h) * tpp * TB;
+        ask = p.page_table + int64_t(c.b) * p.table_pages + at;
+        if (kShared) n_pages = p.n_pages;
+      }
       page = *ask;
       in_unit += first;                           // as from the page's first tile
       turn_page();
@@ -376,8 +384,8 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     // The feeding done, zeros where rows see nothing: the blocks of rows that are no unit.
 #pragma unroll 1
     for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
-      const Sequence s = sequence_of(p, b);
-      if (position_of(p, s, 0) >= 0) continue;
+      const Sequence s = sequence_of<kShared>(p, b);
+      if (position_of(s, 0) >= 0) continue;
       const int64_t rows = int64_t(s.count - s.len) * p.group;       // (of a group: it has no positions)
       const int r1 = s.len == 0 ? int(rows) : int(rows / kRows) * kRows;
 #pragma unroll 1
@@ -416,11 +424,11 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
       int lo[2], hi[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        hi[j] = position_of(p, c.s, min(c.r0 + st.row(j), rows - 1) / p.group);
+        hi[j] = position_of(c.s, min(c.r0 + st.row(j), rows - 1) / p.group);
         lo[j] = first_seen(p, hi[j]);
       }
-      const int all_hi = position_of(p, c.s, c.r0 / p.group);
-      const int last = position_of(p, c.s, min(c.r0 + kRows - 1, rows - 1) / p.group);
+      const int all_hi = position_of(c.s, c.r0 / p.group);
+      const int last = position_of(c.s, min(c.r0 + kRows - 1, rows - 1) / p.group);
       const int all_lo = first_seen(p, last);
       st.reset();
 #pragma unroll 1
@@ -616,28 +624,28 @@ constexpr int kMaxCtas = 256;                     // of a launch; the workspace 
 constexpr int kMaxBatch = 1024;                   // of a launch: the cut is worked out in shared memory
 constexpr size_t kTicketBytes = kMaxCtas * 4;
 
-template <int D, int NG, bool kTwoPlanes, int R>
+template <int D, int NG, bool kTwoPlanes, int R, bool kShared>
 cudaError_t launch_rows(const AttnParams& p, int dev, int ctas, cudaStream_t s) {
   // the kernel's shared memory limit, raised once a device
   static std::atomic<uint64_t> raised{0};
   const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
   if (!(raised.load(std::memory_order_relaxed) & bit) || !bit) {
-    const cudaError_t err = cudaFuncSetAttribute(k_attn_rows<D, NG, kTwoPlanes, R>,
+    const cudaError_t err = cudaFuncSetAttribute(k_attn_rows<D, NG, kTwoPlanes, R, kShared>,
                                                  cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                  AttnSmem<D, NG, R>::bytes(kMaxBatch));
     if (err != cudaSuccess) return err;
     raised.fetch_or(bit, std::memory_order_relaxed);
   }
-  return launch_early(k_attn_rows<D, NG, kTwoPlanes, R>, ctas, (kAttnWarps + 1) * 32, AttnSmem<D, NG, R>::bytes(p.batch), s, p);
+  return launch_early(k_attn_rows<D, NG, kTwoPlanes, R, kShared>, ctas, (kAttnWarps + 1) * 32, AttnSmem<D, NG, R>::bytes(p.batch), s, p);
 }
 
-template <bool kTwoPlanes, int R>
+template <bool kTwoPlanes, int R, bool kShared>
 cudaError_t dispatch_rows(const AttnParams& p, int d, int group, int dev, int ctas, cudaStream_t s) {
-  if (d == 128 && group == 32) return launch_rows<128, 4, kTwoPlanes, R>(p, dev, ctas, s);
-  if (d == 128 && group == 64) return launch_rows<128, 2, kTwoPlanes, R>(p, dev, ctas, s);
-  if (d == 128) return launch_rows<128, 1, kTwoPlanes, R>(p, dev, ctas, s);
-  if (group == 32) return launch_rows<64, 2, kTwoPlanes, R>(p, dev, ctas, s);
-  return launch_rows<64, 1, kTwoPlanes, R>(p, dev, ctas, s);
+  if (d == 128 && group == 32) return launch_rows<128, 4, kTwoPlanes, R, kShared>(p, dev, ctas, s);
+  if (d == 128 && group == 64) return launch_rows<128, 2, kTwoPlanes, R, kShared>(p, dev, ctas, s);
+  if (d == 128) return launch_rows<128, 1, kTwoPlanes, R, kShared>(p, dev, ctas, s);
+  if (group == 32) return launch_rows<64, 2, kTwoPlanes, R, kShared>(p, dev, ctas, s);
+  return launch_rows<64, 1, kTwoPlanes, R, kShared>(p, dev, ctas, s);
 }
 
 // Whole blocks of rows (paged_attn_blocks.cu) from kBlockRows rows a sequence on: a
@@ -736,9 +744,7 @@ cudaError_t attn_rows(const AttnParams& p, const reskv_paged_kv* kv, bool one, i
     l.batch = p.batch - b0 < kMaxBatch ? p.batch - b0 : kMaxBatch;
     l.lens += b0;
     l.page_table += int64_t(b0) * p.table_pages;
-    if (p.members) {
-      // one launch holds all groups
-    } else if (p.q_begin) {
+    if (p.q_begin) {
       l.q_begin += b0;
     } else {
       const int64_t t0 = b0 * each;
@@ -747,10 +753,10 @@ cudaError_t attn_rows(const AttnParams& p, const reskv_paged_kv* kv, bool one, i
       l.o = static_cast<char*>(p.o) + t0 * p.o_token * (p.o_f32 ? 4 : 2);
       if (p.lse) l.lse = p.lse + t0 * p.heads;
     }
-    err = one ? (few ? dispatch_rows<false, 4>(l, kv->head_dim, kv->quant_group, dev, ctas, s)
-                     : dispatch_rows<false, 8>(l, kv->head_dim, kv->quant_group, dev, ctas, s))
-              : (few ? dispatch_rows<true, 4>(l, kv->head_dim, kv->quant_group, dev, ctas, s)
-                     : dispatch_rows<true, 8>(l, kv->head_dim, kv->quant_group, dev, ctas, s));
+    err = one ? (few ? dispatch_rows<false, 4, false>(l, kv->head_dim, kv->quant_group, dev, ctas, s)
+                     : dispatch_rows<false, 8, false>(l, kv->head_dim, kv->quant_group, dev, ctas, s))
+              : (few ? dispatch_rows<true, 4, false>(l, kv->head_dim, kv->quant_group, dev, ctas, s)
+                     : dispatch_rows<true, 8, false>(l, kv->head_dim, kv->quant_group, dev, ctas, s));
   }
   return err;
 }
@@ -790,13 +796,20 @@ extern "C" reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_p
 }
 
 // --- a shared prefix ---
-// Two passes, each with the kernel that its rows are for, into fp32 rows and sums, and a join.
+// Over the own tokens and over the prefix into fp32 rows and sums, and a join.  Where groups have
+// few rows both are units of one launch of the kernel of few rows (units of eight rows: a group has
+// more).  Otherwise the prefix goes by blocks of rows, in a launch that begins while the own tokens' runs.
 namespace reskv {
 namespace {
 
 // The prefix in blocks of rows: as in takes_blocks, by the mean rows of a group.
 bool prefix_in_blocks(const reskv_paged_kv* prefix, const reskv_paged_attn_args* a) {
-  return a->o.dtype != RESKV_F32 && a->scale >= 0.f && double(a->n_tokens) * a->q.n_heads / prefix->n_kv_heads >= double(kBlockRows) * prefix->batch;
+  return a->o.dtype != RESKV_F32 && a->scale >= 0.f &&
+         double(a->n_tokens) * a->q.n_heads / prefix->n_kv_heads >= double(kBlockRows) * prefix->batch;
+}
+// Sequences and groups that one launch of the kernel of few rows holds.
+bool one_launch(const reskv_paged_kv* kv, const reskv_paged_kv* prefix, const reskv_paged_attn_args* a) {
+  return int64_t(kv->batch) + prefix->batch <= kMaxBatch && !takes_blocks(kv, a);
 }
 // Blocks of 128 rows a CTA takes.
 int prefix_mt(const reskv_paged_kv* prefix, const reskv_paged_attn_args* a) {
@@ -804,7 +817,7 @@ int prefix_mt(const reskv_paged_kv* prefix, const reskv_paged_attn_args* a) {
 }
 
 struct SharedLayout {             // of the workspace, in bytes from its start
-  size_t own, own_ref, prefix, prefix_ref, bytes;
+  size_t own, own_ref, prefix, prefix_ref, plans, bytes;
 };
 size_t padded(size_t n) { return (n + 255) / 256 * 256; }
 SharedLayout shared_layout(const reskv_paged_kv* kv, const reskv_paged_kv* prefix, const reskv_paged_attn_args* a, int sms) {
@@ -818,15 +831,14 @@ SharedLayout shared_layout(const reskv_paged_kv* kv, const reskv_paged_kv* prefi
   l.own = padded(kTicketBytes + records);
   l.own_ref = l.own + padded(rows * kv->head_dim * 4);
   l.prefix = l.own_ref + padded(rows * 4);
+  size_t held = rows;
   if (prefix_in_blocks(prefix, a)) {
     const int block = 128 * prefix_mt(prefix, a);
-    const size_t items = size_t(group_items(a->n_tokens * (a->q.n_heads / kv->n_kv_heads), prefix->batch, kv->n_kv_heads, block, sms));
-    l.prefix_ref = l.prefix + padded(items * block * kv->head_dim * 4);
-    l.bytes = l.prefix_ref + padded(items * block * 4);
-  } else {
-    l.prefix_ref = l.prefix + padded(rows * kv->head_dim * 4);
-    l.bytes = l.prefix_ref + padded(rows * 4);
+    held = size_t(group_items(a->n_tokens * (a->q.n_heads / kv->n_kv_heads), prefix->batch, kv->n_kv_heads, block, sms)) * block;
   }
+  l.prefix_ref = l.prefix + padded(held * kv->head_dim * 4);
+  l.plans = l.prefix_ref + padded(held * 4);
+  l.bytes = l.plans + padded(size_t(prefix->batch) * sizeof(GroupPlan));
   return l;
 }
 
@@ -842,9 +854,9 @@ std::string check_shared(const reskv_paged_kv* kv, const reskv_paged_kv* prefix,
   if (!prefix_lens) return "prefix_lens is NULL";
   if (!seq_begin && kv->batch % prefix->batch) return "batch must be a multiple of the prefixes without seq_begin";
   if (a->window != 0) return "window must be 0";
-  if (prefix->batch > kMaxBatch) return "at most 1024 prefixes a call";
-  if ((double(a->n_tokens) * (a->q.n_heads / kv->n_kv_heads) / 4 + prefix->batch) * kv->n_kv_heads >= double(1 << kUnitBits))
-    return "n_tokens * heads / 4 + prefixes * n_kv_heads must be below 2^24";
+  if (prefix->batch >= kMaxBatch) return "fewer than 1024 prefixes a call";
+  if ((double(a->n_tokens) * (a->q.n_heads / kv->n_kv_heads) / 2 + kv->batch + prefix->batch) * kv->n_kv_heads >= double(1 << kUnitBits))
+    return "n_tokens * heads / 2 + (batch + prefixes) * n_kv_heads must be below 2^24";
   return "";
 }
 
@@ -883,28 +895,43 @@ extern "C" reskv_status reskv_paged_attn_shared(const reskv_paged_kv* kv, const 
     p.o_head = kv->head_dim;
     p.o_token = int64_t(p.heads) * kv->head_dim;
     p.lse_unit = 1.f;
-    err = takes_blocks(kv, a) ? launch_attn_blocks(p, block_plan(kv, a, sms), kv->head_dim, kv->quant_group, dev, p.partials, s)
-                              : attn_rows(p, kv, one, dev, sms, s);
     // the prefix: a group's query tokens are one sequence's that all see all
-    p.lens = prefix_lens;
-    p.page_table = prefix->page_table;
-    p.pages = static_cast<const uint8_t*>(prefix->pages);
-    p.status = prefix->status;
-    p.n_pages = prefix->n_pages;
-    p.batch = prefix->batch;
-    p.table_pages = prefix->table_pages;
-    p.seq_begin = seq_begin;
-    p.members = kv->batch;
-    const bool blocks = prefix_in_blocks(prefix, a);
+    AttnParams g = p;
+    g.sequences = kv->batch;
+    g.seq_begin = seq_begin;
+    g.prefix_lens = prefix_lens;
+    g.prefix_table = prefix->page_table;
+    g.prefix_data = static_cast<const uint8_t*>(prefix->pages);
+    g.prefix_status = prefix->status;
+    g.prefix_n_pages = prefix->n_pages;
+    g.prefix_pages = prefix->table_pages;
+    g.prefix_o = reinterpret_cast<float*>(ws + l.prefix);
+    g.prefix_ref = reinterpret_cast<float*>(ws + l.prefix_ref);
+    const bool blocks = prefix_in_blocks(prefix, a), fused = !blocks && one_launch(kv, prefix, a);
     const int mt = prefix_mt(prefix, a);
-    p.o = ws + l.prefix;
-    p.lse = reinterpret_cast<float*>(ws + l.prefix_ref);
-    const int items = int(group_items(p.n_tokens * p.group, p.batch, p.kv_heads, 128 * mt, sms));
-    if (err == cudaSuccess)
-      err = blocks ? launch_attn_groups(p, mt, items, sms, kv->head_dim, kv->quant_group, dev, static_cast<float*>(p.o), s)
-                   : attn_rows(p, prefix, one, dev, sms, s);
+    const int items = blocks ? int(group_items(p.n_tokens * p.group, prefix->batch, p.kv_heads, 128 * mt, sms)) : 0;
+    GroupPlan* plans = reinterpret_cast<GroupPlan*>(ws + l.plans);
+    if (fused) {
+      g.batch = kv->batch + prefix->batch;
+      g.own = kv->batch;
+      const int ctas = sms < kMaxCtas ? sms : kMaxCtas;
+      err = one ? dispatch_rows<false, 8, true>(g, kv->head_dim, kv->quant_group, dev, ctas, s)
+                : dispatch_rows<true, 8, true>(g, kv->head_dim, kv->quant_group, dev, ctas, s);
+    } else {
+      err = takes_blocks(kv, a) ? launch_attn_blocks(p, block_plan(kv, a, sms), kv->head_dim, kv->quant_group, dev, p.partials, s)
+                                : attn_rows(p, kv, one, dev, sms, s);
+    }
+    g.batch = prefix->batch;
+    g.own = 0;
+    if (err == cudaSuccess && blocks)
+      err = launch_attn_groups(g, mt, items, sms, kv->head_dim, kv->quant_group, dev, g.prefix_o, plans, s);
+    if (err == cudaSuccess && !blocks && !fused) {
+      const int ctas = sms < kMaxCtas ? sms : kMaxCtas;
+      err = one ? dispatch_rows<false, 8, true>(g, kv->head_dim, kv->quant_group, dev, ctas, s)
+                : dispatch_rows<true, 8, true>(g, kv->head_dim, kv->quant_group, dev, ctas, s);
+    }
     SharedJoin j{};
-    j.a = p;
+    j.a = g;
     j.a.o = call.o;
     j.a.lse = call.lse;
     j.a.o_token = call.o_token;
@@ -912,13 +939,14 @@ extern "C" reskv_status reskv_paged_attn_shared(const reskv_paged_kv* kv, const 
     j.a.o_f32 = call.o_f32;
     j.a.o_wide = call.o_wide;
     j.a.lse_unit = call.lse_unit;
-    j.own = reinterpret_cast<const float*>(ws + l.own);
-    j.own_ref = reinterpret_cast<const float*>(ws + l.own_ref);
-    j.prefix = reinterpret_cast<const float*>(ws + l.prefix);
-    j.prefix_ref = reinterpret_cast<const float*>(ws + l.prefix_ref);
-    j.block_rows = blocks ? 128 * mt : 0;
+    j.own = static_cast<const float*>(p.o);
+    j.own_ref = p.lse;
+    j.prefix = g.prefix_o;
+    j.prefix_ref = g.prefix_ref;
+    j.plans = blocks ? plans : nullptr;
+    j.block_rows = 128 * mt;
     j.items = items;
-    j.ctas = sms;
+    j.groups = prefix->batch;
     j.dim = kv->head_dim;
     if (err == cudaSuccess) err = launch_shared_join(j, s);
     return launch_result(err, "attention with a shared prefix");

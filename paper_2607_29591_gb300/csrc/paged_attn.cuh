@@ -24,10 +24,18 @@ struct AttnParams {
   int32_t window, q_f16, o_f32, q_wide, o_wide;
   float scale2;                   // scale * log2 e
   float lse_unit;                 // what lse holds of a log2 of a sum: ln 2 of it, or all
-  // A prefix that groups of sequences share: `batch` groups of `members` sequences, whose
-  // query tokens all see all of the group's positions (members 0: neither).
+  // Prefixes that groups of the call's `sequences` share: behind `own` sequences `batch` holds groups,
+  // whose query tokens all see all of the group's positions.  What is the groups':
+  int32_t sequences, own;
   const int32_t* seq_begin;
-  int32_t members;
+  int32_t prefix_pages;           // of a row of their page table
+  const int32_t* prefix_lens;
+  const int32_t* prefix_table;
+  const uint8_t* prefix_data;
+  uint32_t* prefix_status;
+  int64_t prefix_n_pages;
+  float* prefix_o;                // fp32 rows [token][head][dim], o_head elements each
+  float* prefix_ref;              // log2 sums
 };
 
 // One block of query rows of one sequence: row r of the sequence is query token
@@ -39,50 +47,59 @@ struct RowBlock {
 
 struct Sequence {
   int len, count, q0;             // held tokens, query tokens, first query token
+  bool all;                       // a group: everything is seen
 };
 
-__device__ __forceinline__ Sequence sequence_of(const AttnParams& p, int b) {
+__device__ __forceinline__ int clamp_len(int len, int room, uint32_t* status) {
+  if (len < 0 || len > room) report_status(status, kStatusBadIndex);
+  return min(max(len, 0), room);
+}
+// Group g's query tokens, those of its sequences.
+__device__ __forceinline__ Sequence group_of(const AttnParams& p, int g, int groups) {
+  const int members = p.sequences;
   Sequence s;
-  if (p.members) {
-    int s0, s1;
-    if (p.seq_begin) {
-      s0 = p.seq_begin[b];
-      s1 = p.seq_begin[b + 1];
-      if (s0 < 0 || s0 > p.members || s1 < s0 || s1 > p.members) report_status(p.status, kStatusBadIndex);
-      s0 = min(max(s0, 0), p.members);
-      s1 = min(max(s1, s0), p.members);
-    } else {
-      const int each = p.members / p.batch;
-      s0 = b * each;
-      s1 = s0 + each;
-    }
-    int64_t t0 = s0 * (p.n_tokens / p.members), t1 = s1 * (p.n_tokens / p.members);
-    if (p.q_begin) {
-      t0 = min(max(int64_t(p.q_begin[s0]), int64_t(0)), p.n_tokens);
-      t1 = min(max(int64_t(p.q_begin[s1]), t0), p.n_tokens);
-    }
-    s.q0 = int(t0);
-    s.count = int(t1 - t0);
-  } else if (p.q_begin) {
+  int s0, s1;
+  if (p.seq_begin) {
+    s0 = p.seq_begin[g];
+    s1 = p.seq_begin[g + 1];
+    if (s0 < 0 || s0 > members || s1 < s0 || s1 > members) report_status(p.prefix_status, kStatusBadIndex);
+    s0 = min(max(s0, 0), members);
+    s1 = min(max(s1, s0), members);
+  } else {
+    s0 = g * (members / groups);
+    s1 = s0 + members / groups;
+  }
+  int64_t t0 = s0 * (p.n_tokens / members), t1 = s1 * (p.n_tokens / members);
+  if (p.q_begin) {
+    t0 = min(max(int64_t(p.q_begin[s0]), int64_t(0)), p.n_tokens);
+    t1 = min(max(int64_t(p.q_begin[s1]), t0), p.n_tokens);
+  }
+  s.q0 = int(t0);
+  s.count = int(t1 - t0);
+  s.len = clamp_len(p.prefix_lens[g], p.prefix_pages * p.page_tokens, p.prefix_status);        // below 2^31
+  s.all = true;
+  return s;
+}
+template <bool kShared = false>
+__device__ __forceinline__ Sequence sequence_of(const AttnParams& p, int b) {
+  if (kShared && b >= p.own) return group_of(p, b - p.own, p.batch - p.own);
+  Sequence s;
+  if (p.q_begin) {
     const int64_t lo = min(max(int64_t(p.q_begin[b]), int64_t(0)), p.n_tokens);
     const int64_t hi = min(max(int64_t(p.q_begin[b + 1]), lo), p.n_tokens);
     s.q0 = int(lo);
     s.count = int(hi - lo);
   } else {
-    s.count = int(p.n_tokens / p.batch);
+    s.count = int(p.n_tokens / (kShared ? p.own : p.batch));
     s.q0 = b * s.count;
   }
-  const int room = p.table_pages * p.page_tokens;      // below 2^31
-  const int len = p.lens[b];
-  if (len < 0 || len > room) report_status(p.status, kStatusBadIndex);
-  s.len = min(max(len, 0), room);
+  s.len = clamp_len(p.lens[b], p.table_pages * p.page_tokens, p.status);           // below 2^31
+  s.all = false;
   return s;
 }
 
 // Position of a sequence's query token i, the last that it sees.
-__device__ __forceinline__ int position_of(const AttnParams& p, const Sequence& s, int i) {
-  return p.members ? s.len - 1 : s.len - s.count + i;
-}
+__device__ __forceinline__ int position_of(const Sequence& s, int i) { return s.all ? s.len - 1 : s.len - s.count + i; }
 
 // First position that a query at `pos` sees (pos may lie far below 0, a window be any).
 __device__ __forceinline__ int first_seen(const AttnParams& p, int pos) {
@@ -92,8 +109,8 @@ __device__ __forceinline__ int first_seen(const AttnParams& p, int pos) {
 // Rows [r0, r1) of a sequence.
 __device__ __forceinline__ RowBlock row_block(const AttnParams& p, const Sequence& s, int r0, int r1) {
   // (one block of a sequence's rows, the usual case, divides nothing)
-  const int lo = position_of(p, s, r0 == 0 ? 0 : r0 / p.group);
-  const int hi = position_of(p, s, r1 == s.count * p.group ? s.count - 1 : (r1 - 1) / p.group);
+  const int lo = position_of(s, r0 == 0 ? 0 : r0 / p.group);
+  const int hi = position_of(s, r1 == s.count * p.group ? s.count - 1 : (r1 - 1) / p.group);
   RowBlock b;
   b.first = first_seen(p, lo) / kTile;
   b.tiles = hi < 0 ? 0 : hi / kTile - b.first + 1;
@@ -107,6 +124,10 @@ __device__ __forceinline__ void store_out(const AttnParams& p, const Sequence& s
   const int64_t tok = s.q0 + r / p.group;
   const int64_t at = tok * p.o_token + int64_t(h * p.group + r % p.group) * p.o_head + 4 * u;
   const float f[4] = {v.x, v.y, v.z, v.w};
+  if (s.all) {                                    // fp32 rows [token][head][dim]
+    *reinterpret_cast<float4*>(p.prefix_o + (tok * p.heads + h * p.group + r % p.group) * p.o_head + 4 * u) = v;
+    return;
+  }
   if (p.o_f32) {
     float* y = static_cast<float*>(p.o) + at;
     if (p.o_wide) {
@@ -131,6 +152,10 @@ __device__ __forceinline__ void store_out(const AttnParams& p, const Sequence& s
 }
 
 __device__ __forceinline__ void store_lse(const AttnParams& p, const Sequence& s, int h, int r, float ref) {
+  if (s.all) {                                    // fp32 rows [token][head][dim]
+    p.prefix_ref[(s.q0 + r / p.group) * int64_t(p.heads) + h * p.group + r % p.group] = ref;
+    return;
+  }
   if (p.lse) p.lse[(s.q0 + r / p.group) * int64_t(p.heads) + h * p.group + r % p.group] = ref * p.lse_unit;
 }
 // The softmaxes of up to 32 records joined: each lane's weight for its record's
@@ -591,37 +616,52 @@ struct BlockPlan {
 };
 BlockPlan plan_attn_blocks(int64_t rows, int batch, int kv_heads, int64_t capacity, int sms);
 size_t attn_blocks_bytes(const BlockPlan& plan, int d);              // of records, where parts are joined
+cudaError_t launch_attn_blocks(const AttnParams& p, const BlockPlan& plan, int d, int quant_group, int dev, float* records,
+                               cudaStream_t s);
 
-// --- a prefix shared by groups of sequences: paged_attn_blocks.cu, paged_shared.cu ---
-// Units are blocks of 128 mt rows of a KV head and group.  How many rows and positions a
-// group has only the device knows, so it makes the plan: where units do not fill the SMs
+// --- a prefix shared by groups of sequences: paged_prefix.cu, paged_shared.cu ---
+// Units are blocks of 128 mt rows (mt 1 or 2) of a KV head and group.  How many rows and positions
+// a group has only the device knows, so it makes the plan: where units do not fill the SMs
 // their positions are cut into parts of about equal steps.  Part k of unit (group, head,
 // block) is item first + (head * parts + k) * row_blocks + block, CTA and record alike.
 struct GroupPlan {
   int group;                      // the group, or -1
-  Sequence s;
   int first, row_blocks, parts;   // of its items; parts 0: nothing to see
+  int q0, count, len;             // its query tokens and positions
+  int pad;
 };
 constexpr int kBlockPos = 64;     // positions of a step
-constexpr int kLeastSteps = 8;    // of a part
+constexpr int kLeastSteps = 4;    // of a part
 
-// One warp; the same in all its lanes.  For the group of item `item`, or (item < 0) group `group`.
-__device__ __forceinline__ GroupPlan group_plan(const AttnParams& p, int block_rows, int ctas, int item, int group, int lane) {
+// One warp; the same in all its lanes: the plan of item `item`'s group.  With `plans`, those of all
+// groups are written there instead.
+__device__ __forceinline__ GroupPlan group_plan(const AttnParams& p, int block_rows, int ctas, int item, int lane,
+                                                GroupPlan* plans = nullptr) {
   auto units_steps = [&](int g, int& units, int& steps) {
+    Sequence s{};
     units = steps = 0;
-    if (g >= p.batch) return;
-    const Sequence s = sequence_of(p, g);
+    if (g >= p.batch) return s;
+    s = group_of(p, g, p.batch);
     steps = (s.len + kBlockPos - 1) / kBlockPos;
     if (steps > 0) units = int((int64_t(s.count) * p.group + block_rows - 1) / block_rows) * p.kv_heads;
+    return s;
   };
   auto total = [&](int x) { return __reduce_add_sync(0xffffffffu, uint32_t(x)); };
+  // up to 32 groups are looked up once
+  int u0, n0;
+  const Sequence mine0 = units_steps(lane, u0, n0);
+  auto at = [&](int g0, int& u, int& n) {
+    u = u0;
+    n = n0;
+    return g0 == 0 ? mine0 : units_steps(g0 + lane, u, n);
+  };
   // a part's steps: the fewest with which the parts fit the SMs (units that do not: whole)
   uint32_t units = 0, longest = 0;
   float work = 0.f;
 #pragma unroll 1
   for (int g0 = 0; g0 < p.batch; g0 += 32) {
     int u, n;
-    units_steps(g0 + lane, u, n);
+    at(g0, u, n);
     units += total(u);
     longest = max(longest, __reduce_max_sync(0xffffffffu, uint32_t(n)));
     float w = float(u) * float(n);
@@ -638,7 +678,7 @@ __device__ __forceinline__ GroupPlan group_plan(const AttnParams& p, int block_r
 #pragma unroll 1
       for (int g0 = 0; g0 < p.batch; g0 += 32) {
         int u, n;
-        units_steps(g0 + lane, u, n);
+        at(g0, u, n);
         items += total(u * int((n + size - 1) / size));
       }
       if (items <= uint32_t(ctas)) break;
@@ -646,12 +686,12 @@ __device__ __forceinline__ GroupPlan group_plan(const AttnParams& p, int block_r
     }
   }
   size = max(size, 1u);
-  GroupPlan out{-1, {}, 0, 0, 0};
+  GroupPlan out{-1, 0, 0, 0, 0, 0, 0, 0};
   int first = 0;
 #pragma unroll 1
   for (int g0 = 0; g0 < p.batch; g0 += 32) {
     int u, n;
-    units_steps(g0 + lane, u, n);
+    const Sequence s = at(g0, u, n);
     const int parts = u ? int((n + size - 1) / size) : 0, mine = u * parts;
     int before = mine;
 #pragma unroll
@@ -661,16 +701,22 @@ __device__ __forceinline__ GroupPlan group_plan(const AttnParams& p, int block_r
     }
     const int all = __shfl_sync(0xffffffffu, before, 31);
     before = first + before - mine;
-    const bool here = item >= 0 ? item >= before && item < before + mine : g0 + lane == group;
-    const uint32_t who = __ballot_sync(0xffffffffu, here);
-    if (who) {
-      const int l = __ffs(who) - 1;
-      out.group = g0 + l;
-      out.first = __shfl_sync(0xffffffffu, before, l);
-      out.parts = __shfl_sync(0xffffffffu, parts, l);
-      out.row_blocks = __shfl_sync(0xffffffffu, u, l) / p.kv_heads;
-      out.s = sequence_of(p, out.group);
-      return out;
+    const GroupPlan g{g0 + lane, before, u / p.kv_heads, parts, s.q0, s.count, s.len, 0};
+    if (plans) {
+      if (g.group < p.batch) plans[g.group] = g;
+    } else {
+      const uint32_t who = __ballot_sync(0xffffffffu, item >= before && item < before + mine);
+      if (who) {
+        const int l = __ffs(who) - 1;
+        out.group = g0 + l;
+        out.first = __shfl_sync(0xffffffffu, before, l);
+        out.row_blocks = __shfl_sync(0xffffffffu, g.row_blocks, l);
+        out.parts = __shfl_sync(0xffffffffu, parts, l);
+        out.q0 = __shfl_sync(0xffffffffu, s.q0, l);
+        out.count = __shfl_sync(0xffffffffu, s.count, l);
+        out.len = __shfl_sync(0xffffffffu, s.len, l);
+        return out;
+      }
     }
     first += all;
   }
@@ -683,19 +729,18 @@ inline int64_t group_items(int64_t rows, int groups, int kv_heads, int block_row
   return units > ctas ? units : ctas;
 }
 cudaError_t launch_attn_groups(const AttnParams& p, int mt, int items, int ctas, int d, int quant_group, int dev, float* records,
-                               cudaStream_t s);
+                               GroupPlan* plans, cudaStream_t s);
 // The softmaxes over the own tokens (fp32 rows in the order of o, log2 sums) and over
-// the prefix (the same, or records: block_rows > 0) joined into o.
+// the prefix (the same, or the records of `plans`) joined into o.
 struct SharedJoin {
-  AttnParams a;                   // the prefix's pass, with the call's o and lse
+  AttnParams a;                   // the call's, with the groups as in the prefix's pass
   const float* own;
   const float* own_ref;
   const float* prefix;
   const float* prefix_ref;
-  int32_t block_rows, items, ctas, dim;
+  const GroupPlan* plans;         // NULL: the prefix has rows in the order of o, too
+  int32_t block_rows, items, groups, dim;
 };
 cudaError_t launch_shared_join(const SharedJoin& j, cudaStream_t s);
-cudaError_t launch_attn_blocks(const AttnParams& p, const BlockPlan& plan, int d, int quant_group, int dev, float* records,
-                               cudaStream_t s);
 
 }  // namespace reskv

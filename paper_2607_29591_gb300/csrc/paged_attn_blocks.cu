@@ -52,7 +52,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kPos = kBlockPos;                   // positions of a step
+constexpr int kPos = 64;                          // positions of a step
 constexpr int kSub = kPos / kTile;                // cache tiles of a step
 constexpr int kThreads = 640;                     // warps 0-7 softmax, 8-15 unpack, 16 products, 17 copies, 18-19 exponents
 constexpr int kUnpackWarp = 8, kIssueWarp = 16, kCopyWarp = 17, kLookWarp = 18;
@@ -125,8 +125,6 @@ struct BlockParams {
   AttnParams a;
   BlockPlan plan;
   float* records;                                 // [slot][rows][D], then [slot][rows] log2 sums
-  float* sums;
-  int32_t ctas;                                   // a prefix's groups: of the device; else 0
 };
 
 // A softmax warp's rows without tensor cores, one after the other, in fp32, whatever the
@@ -141,7 +139,7 @@ __device__ __noinline__ void plain_rows(const BlockParams& bp, const Sequence& s
   constexpr TileShape ts{D, NG};
   constexpr int TB = ts.bytes();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rows = sq.count * p.group;
+  const int rows = sq.count * p.group, base = sq.len - sq.count;
   __syncwarp();
   const int tpp = p.page_tokens / kTile, u = lane < D / 4 ? lane : 0, group = 4 * u * NG / D;
 #pragma unroll 1
@@ -156,7 +154,7 @@ __device__ __noinline__ void plain_rows(const BlockParams& bp, const Sequence& s
       const float x = p.q_f16 ? __half2float(__ushort_as_half(src[j])) : __bfloat162float(__ushort_as_bfloat16(src[j]));
       qv[j] = lane < D / 4 ? x : 0.f;
     }
-    const int hi = position_of(p, sq, row / p.group), lo = first_seen(p, hi);
+    const int hi = base + row / p.group, lo = first_seen(p, hi);
     const int stop = hi < 0 ? 0 : min(hi / kTile + 1, first + tiles);
 #pragma unroll 1
     for (int t = max(lo / kTile, first); t < stop; ++t) {
@@ -252,52 +250,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
 
   // the item: part of the positions of one block of rows
   const BlockPlan& plan = bp.plan;
-  bool apart;
-  int64_t slot = 0;
-  int b, h, r0, rows, step0, n;
-  Sequence sq;
-  RowBlock rb;
-  if (bp.ctas) {                                  // of a prefix: always a record
-    const GroupPlan g = group_plan(p, kRows, bp.ctas, int(blockIdx.x), 0, lane);
-    if (g.group < 0) return;                      // the same for the whole CTA
-    apart = true;
-    slot = blockIdx.x;
-    const int local = int(blockIdx.x) - g.first, hp = local / g.row_blocks, part = hp % g.parts;
-    b = g.group;
-    h = hp / g.parts;
-    r0 = (local - hp * g.row_blocks) * kRows;
-    sq = g.s;
-    rows = sq.count * p.group;
-    rb = row_block(p, sq, r0, min(r0 + kRows, rows));
-    const int steps_all = (rb.tiles + kSub - 1) / kSub;
-    step0 = int(int64_t(steps_all) * part / g.parts);
-    n = int(int64_t(steps_all) * (part + 1) / g.parts) - step0;
-  } else {
-    const int cut = plan.units - plan.whole, item = int(blockIdx.x) - plan.whole;
-    apart = item >= 0 && plan.parts() > 1;
-    int part = 0, unit = blockIdx.x;
-    if (apart) {
-      const bool last = item >= cut * plan.even;
-      unit = last ? item - cut * plan.even : item / plan.even;
-      part = last ? plan.even : item - unit * plan.even;
-      slot = int64_t(unit) * plan.parts() + part;
-      unit += plan.whole;
-    }
-    const int blk = unit % plan.row_blocks, bh = unit / plan.row_blocks;
-    b = bh / p.kv_heads;
-    h = bh - b * p.kv_heads;
-    sq = sequence_of(p, b);
-    rows = sq.count * p.group;
-    r0 = blk * kRows;
-    rb = row_block(p, sq, r0, min(r0 + kRows, rows));
-    const int steps_all = (rb.tiles + kSub - 1) / kSub;
-    step0 = apart ? int((int64_t(steps_all) * part * plan.share) >> 16) : 0;
-    n = (apart && part + 1 < plan.parts() ? int((int64_t(steps_all) * (part + 1) * plan.share) >> 16) : steps_all) - step0;
+  const int cut = plan.units - plan.whole, item = int(blockIdx.x) - plan.whole;
+  const bool apart = item >= 0 && plan.parts() > 1;
+  int part = 0, unit = blockIdx.x;
+  if (apart) {
+    const bool last = item >= cut * plan.even;
+    unit = last ? item - cut * plan.even : item / plan.even;
+    part = last ? plan.even : item - unit * plan.even;
+    unit += plan.whole;
   }
+  const int blk = unit % plan.row_blocks, bh = unit / plan.row_blocks;
+  const int b = bh / p.kv_heads, h = bh - b * p.kv_heads;
+  const Sequence sq = sequence_of(p, b);
+  const int rows = sq.count * p.group, r0 = blk * kRows;
+  const RowBlock rb = row_block(p, sq, r0, min(r0 + kRows, rows));
+  const int steps_all = (rb.tiles + kSub - 1) / kSub;
+  const int step0 = apart ? int((int64_t(steps_all) * part * plan.share) >> 16) : 0;
+  const int n = (apart && part + 1 < plan.parts() ? int((int64_t(steps_all) * (part + 1) * plan.share) >> 16) : steps_all) - step0;
   const int first = rb.first + step0 * kSub;      // first cache tile
   const int tiles = min(rb.tiles - step0 * kSub, n * kSub);
   // what the block's rows see
-  const int hi_first = position_of(p, sq, r0 / p.group), hi_last = position_of(p, sq, (min(r0 + kRows, rows) - 1) / p.group);
+  const int base = sq.len - sq.count;
+  const int hi_first = base + r0 / p.group, hi_last = base + (min(r0 + kRows, rows) - 1) / p.group;
   const int from = first_seen(p, hi_first);
   const int lo_last = first_seen(p, hi_last);
 
@@ -306,8 +280,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
   const int rt = (warp & 3) * 32 + lane;          // row within its 128
   const int r = r0 + mt * 128 + rt;
   const bool real = warp < 4 * MT && r < rows;
+  const int64_t slot = apart ? int64_t(unit - plan.whole) * plan.parts() + part : 0;
   float* const record = bp.records + slot * kRows * D;
-  float* const record_ref = bp.sums + slot * kRows;
+  float* const record_ref = bp.records + plan.slots() * kRows * D + slot * kRows;
   auto finish_row = [&](int c, const float (&v)[32]) {       // dims 32c .. 32c + 31 of this thread's row
     if (!real) return;
     if (apart) {
@@ -609,7 +584,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_blocks(const __grid_consta
     if (warp < 4 * MT) {
       // --- the softmax, a row a thread ---
       const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
-      const int hi = position_of(p, sq, min(r, rows - 1) / p.group);
+      const int hi = base + min(r, rows - 1) / p.group;
       const int lo = first_seen(p, hi);
       float ref = kNoRef, l = 0.f;
       uint32_t nan_groups = 0;
@@ -837,7 +812,7 @@ __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ Block
   const int r = blk * kRows + row;
   if (r >= sq.count * p.group) return;
   const int64_t slot = int64_t(cut) * parts;
-  const float* refs = bp.sums;
+  const float* refs = bp.records + bp.plan.slots() * kRows * D;
   const float ref = lane < parts ? refs[(slot + lane) * kRows + row] : -INFINITY;
   const Joined j = join_weights(ref);
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -864,7 +839,7 @@ cudaError_t launch(const BlockParams& bp, int dev, cudaStream_t s) {
     raised.fetch_or(bit, std::memory_order_relaxed);
   }
   cudaError_t err = launch_early(k_attn_blocks<D, NG, MT>, bp.plan.items, kThreads, BlockSmem<D, NG, MT>::bytes, s, bp);
-  if (err == cudaSuccess && !bp.ctas && bp.plan.slots() > 0) {
+  if (err == cudaSuccess && bp.plan.slots() > 0) {
     const int64_t rows = int64_t(bp.plan.units - bp.plan.whole) * 128 * MT;
     err = launch_early(k_attn_join<D, MT>, unsigned((rows + 7) / 8), 256, 0, s, bp);
   }
@@ -929,20 +904,7 @@ cudaError_t launch_attn_blocks(const AttnParams& p, const BlockPlan& plan, int d
   bp.a = p;
   bp.plan = plan;
   bp.records = records;
-  bp.sums = records + plan.slots() * 128 * plan.mt * d;
   return plan.mt == 2 ? dispatch<2>(bp, d, quant_group, dev, s) : dispatch<1>(bp, d, quant_group, dev, s);
-}
-
-cudaError_t launch_attn_groups(const AttnParams& p, int mt, int items, int ctas, int d, int quant_group, int dev, float* records,
-                               cudaStream_t s) {
-  BlockParams bp{};
-  bp.a = p;
-  bp.plan.mt = mt;
-  bp.plan.items = items;
-  bp.records = records;
-  bp.sums = p.lse;
-  bp.ctas = ctas;
-  return mt == 2 ? dispatch<2>(bp, d, quant_group, dev, s) : dispatch<1>(bp, d, quant_group, dev, s);
 }
 
 }  // namespace reskv

@@ -1,0 +1,613 @@
+// Attention of a group's query rows over the prefix that its sequences share (the
+// first pass of reskv_paged_attn_shared where groups have many rows), on the
+// fifth-generation tensor cores.
+//
+// Every row sees every position, so a tile needs no masks: it is 64 positions, unpacked once for two
+// blocks of 128 rows, or, where a group has no more than 128 rows (kSplit), for one while the CTA's other
+// stream has the next tile:
+//
+//   S = Q K^T       [128 rows x 64 positions]  fp16 operands in shared memory, into TMEM, two deep
+//   P = 2^(S f + c - ref)                      a row a thread, fp16 over S
+//   O += P V        [128 rows x d]             P from TMEM, V^T [dims x positions] in shared memory
+//
+// Eight warps unpack, each from packed rows that it copies itself, four tiles ahead; eight take the
+// softmax, one issues the products.
+//
+//   ready[t % n]  tile t's operands are in shared memory, in one of n slots      (unpack -> products)
+//   free[t % n]   its products are done                        (products -> unpack)
+//   s[m][i & 1]   S of stream m's tile i is in TMEM            (products -> softmax)
+//   p[m][i & 1]   P is in place (a warp may be a tile ahead)   (softmax -> products)
+//   pv[m]         O holds it                                   (products -> softmax)
+//
+// Any magnitude fits fp16, whatever stands beside it: each position's key and each position's value is divided
+// by a power of two of its own, each query row by one.  Keys enter as s (n - 8), exact in 11
+// bits, and m + 8 s in two planes against the sums of the query over its groups, so that logits are
+// sums of exact products; f is the power of two that the logit of a row and position takes.  Values
+// s n + m are rounded to 11 bits, no coarser than the 16-bit types of the output.  Their
+// power of two goes into the weight's exponent (c), and the reference follows the largest
+// logit + c; the sum of the weights takes 2^-c back.  Positions that do not exist have c = -inf.
+#include <atomic>
+
+#include "paged_attn.cuh"
+#include "tensor_core.cuh"
+
+namespace reskv {
+namespace {
+
+using namespace tc;
+
+constexpr int kPos = kBlockPos;                   // positions of a tile
+constexpr int kSub = kPos / kTile;                // cache tiles of it
+constexpr int kAhead = 4;                          // tiles whose packed rows a warp has under way
+constexpr int kThreads = 640;                     // warps 0-7 softmax, 8-15 unpack, 16 products, 17 the plans
+constexpr int kUnpackWarp = 8, kIssueWarp = 16, kPlanWarp = 17;
+constexpr int kRegsSoftmax = 128, kRegsUnpack = 88, kRegsIssue = 40;
+static_assert((2 * kRegsSoftmax + 2 * kRegsUnpack + kRegsIssue) * 128 <= 96 * kThreads, "registers");
+constexpr int kHalf = 128 * 128;                  // bytes of 128 rows of 64 fp16
+// The power of two that a value is held at: no lower than 2^-60 of the largest that its warp has met, or 2^-100.
+constexpr int kLeastBelow = 60, kLeastExponent = 41;
+
+struct PrefixParams {
+  AttnParams a;
+  GroupPlan* plans;
+  float* records;                                 // [item][rows][D]
+  float* sums;                                    // [item][rows]: log2 sums
+  int32_t ctas;
+};
+
+constexpr int kMostPacked = TileShape{128, 4}.bytes() / 2;            // of K or V of a cache tile
+template <int D, bool kSplit>
+struct PrefixSmem {
+  static constexpr int tiles = kSplit ? 1 : 2, slots = kSplit ? 4 : 3;
+  static constexpr int q = D / 64 * kHalf, q_more = 128 * 32;         // of 128 rows
+  static constexpr int k = D / 64 * kPos * 128, k_more = kPos * 32, v = D * 128;
+  static constexpr int at_q_more = tiles * q, at_slots = at_q_more + tiles * q_more;
+  static constexpr int slot = k + v + k_more;                         // K, V^T, the keys' minima
+  static constexpr int raw = 8 * kMostPacked;                         // packed rows of a tile
+  static constexpr int at_raw = at_slots + slots * slot, all = at_raw + kAhead * raw;
+  static constexpr int at_ref = 2 * 128 * D * 4;                      // of rows to be joined: outputs, references, sums
+  static constexpr int bytes = all + 1024;
+  static_assert(at_ref + 2 * 256 * 4 <= all && slot % 1024 == 0 && at_slots % 1024 == 0, "shared memory");
+};
+struct PrefixShared {
+  uint64_t q, ready[4], free[4], s[2][2], p[2][2], pv[2], done;
+  uint32_t tmem, abort;
+  GroupPlan plan;
+  // per position of a slot: 2^e of its key; log2 of its value's scale (-inf: no such position), and 2^- of that
+  alignas(16) float up[4][kPos], c[4][kPos], inv[4][kPos];
+};
+
+// 2^(14 - (e - 127)) and its inverse, of a biased exponent 15 <= e <= 254
+__device__ __forceinline__ float down(int e) { return __int_as_float((268 - e) << 23); }
+__device__ __forceinline__ float up(int e) { return __int_as_float((e - 14) << 23); }
+__device__ __forceinline__ uint32_t bits(__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); }
+// codes n, less `less`, of the even and the odd places as fp16 numbers
+__device__ __forceinline__ __half2 even_codes(uint32_t v, float less) {
+  const uint32_t w = (v & 0x000f000fu) | 0x64006400u;                // 1024 + n
+  return __hsub2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(1024.f + less));
+}
+__device__ __forceinline__ __half2 odd_codes(uint32_t v, float less) {
+  const uint32_t w = (v & 0x00f000f0u) | 0x64006400u;                // 1024 + 16 n
+  return __hfma2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(0.0625f), __float2half2_rn(-64.f - less));
+}
+// The biased exponent of a row's largest value or minimum, NaN passed over.
+template <int NG>
+__device__ __forceinline__ int top_exponent(const uint32_t (&meta)[NG]) {
+  float top = 0.f;
+#pragma unroll
+  for (int k = 0; k < NG; ++k) {
+    float s, m;
+    group_meta<NG>(meta, k, s, m);
+    top = fmaxf(top, fminf(fmaxf(fabsf(m), fabsf(fmaf(15.f, s, m))), 3.0e38f));
+  }
+  return min(max(__float_as_int(top) >> 23, 15), 254);
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+template <int D, int NG, bool kSplit>
+__global__ void __launch_bounds__(kThreads, 1) k_attn_prefix(const __grid_constant__ PrefixParams pp) {
+  using S = PrefixSmem<D, kSplit>;
+  constexpr int kRows = 128 * S::tiles, C = D / 32, PG = C / NG, TB = TileShape{D, NG}.bytes();
+  constexpr TileShape ts{D, NG};
+  const AttnParams& p = pp.a;
+  extern __shared__ uint8_t dynamic[];
+  uint8_t* smem = dynamic + ((1024u - (smem_u32(dynamic) & 1023u)) & 1023u);
+  __shared__ __align__(16) PrefixShared sh;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    mbar_init(&sh.q, 8);
+    for (int i = 0; i < S::slots; ++i) {
+      mbar_init(&sh.ready[i], 8);
+      mbar_init(&sh.free[i], 1);
+    }
+    for (int m = 0; m < 2; ++m) {
+      mbar_init(&sh.s[m][0], 1);
+      mbar_init(&sh.s[m][1], 1);
+      mbar_init(&sh.p[m][0], 4);
+      mbar_init(&sh.p[m][1], 4);
+      mbar_init(&sh.pv[m], 1);
+    }
+    mbar_init(&sh.done, 1);
+    sh.abort = 0;
+    fence_mbar_init();
+  }
+  // This launch reads nothing that the one before it, over the own tokens, writes, and that one lets it
+  // begin only once all before are done; it ends after it, for the join behind both.
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (warp == kPlanWarp) {
+    const GroupPlan g = group_plan(p, kRows, pp.ctas, int(blockIdx.x), lane);
+    if (lane == 0) sh.plan = g;
+  }
+  if (warp == kIssueWarp) take_columns(smem_u32(&sh.tmem));
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = sh.tmem;
+  const GroupPlan plan = sh.plan;
+  if (plan.group < 0) {                           // no item: the same for the whole CTA
+    if (blockIdx.x == 0 && warp == kPlanWarp) group_plan(p, kRows, pp.ctas, 0, lane, pp.plans);
+    if (warp == kIssueWarp) give_columns(tmem);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    return;
+  }
+  const int local = int(blockIdx.x) - plan.first, hp = local / plan.row_blocks, part = hp % plan.parts, h = hp / plan.parts;
+  const int r0 = (local - hp * plan.row_blocks) * kRows, rows = min(plan.count * p.group - r0, kRows);
+  const int all = (plan.len + kPos - 1) / kPos;
+  const int first = int(int64_t(all) * part / plan.parts), n = int(int64_t(all) * (part + 1) / plan.parts) - first;      // tiles, > 0
+  const int steps[2] = {kSplit ? (n + 1) / 2 : n, kSplit ? n / 2 : rows > 128 ? n : 0};
+  const uint32_t smem_q = smem_u32(smem);
+  auto s_cols = [&](int m, int i) { return tmem + uint32_t((2 * m + (i & 1)) * kPos); };
+  auto o_cols = [&](int m) { return tmem + uint32_t(4 * kPos + m * 128); };
+
+  if (warp >= kIssueWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+    if (warp == kIssueWarp) {
+      // --- products ---
+      const uint32_t q0 = operand(smem_q), qm0 = operand(smem_q + S::at_q_more);
+      auto slot_of = [&](int t) { return smem_q + S::at_slots + t % S::slots * S::slot; };
+      auto wait_tile = [&](int t) { return role_wait(&sh.ready[t % S::slots], (t / S::slots) & 1, &sh.abort, p.status); };
+      auto issue_s = [&](int m, int i, int t) {
+        fence_after();
+        if (elected()) {
+          const uint32_t k0 = operand(slot_of(t)), km0 = operand(slot_of(t) + S::k + S::v), d = s_cols(m, i);
+          const uint32_t a0 = q0 + (kSplit ? 0 : m * (S::q >> 4)), am0 = qm0 + (kSplit ? 0 : m * (S::q_more >> 4));
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k)
+            multiply<kRows128, shape_of(kPos)>(d, a0 + (((k / 4) * kHalf + (k & 3) * 32) >> 4),
+                                               k0 + (((k / 4) * (kPos * 128) + (k & 3) * 32) >> 4), k > 0);
+          multiply<kRows32, shape_of(kPos)>(d, am0, km0, true);
+          commit(&sh.s[m][i & 1]);
+        }
+        __syncwarp();
+      };
+      auto issue_o = [&](int m, int i, int t) {
+        fence_after();
+        if (elected()) {
+          const uint32_t v0 = operand(slot_of(t) + S::k);
+#pragma unroll
+          for (int k = 0; k < kPos / 16; ++k)
+            multiply_from<kRows128, shape_of(D)>(o_cols(m), s_cols(m, i) + k * 8, v0 + ((k * 32) >> 4), i > 0 || k > 0);
+          commit(&sh.pv[m]);
+        }
+        __syncwarp();
+      };
+      auto tile_of = [&](int m, int i) { return kSplit ? 2 * i + m : i; };
+      bool ok = role_wait(&sh.q, 0, &sh.abort, p.status);
+      for (int m = 0; m < 2 && ok; ++m) {
+        if (steps[m] == 0) continue;
+        ok = wait_tile(tile_of(m, 0));
+        if (ok) issue_s(m, 0, tile_of(m, 0));
+      }
+      // S of a stream's next tile goes out before O of the last, whose weights take longer
+#pragma unroll 1
+      for (int i = 0; i < steps[0] && ok; ++i) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          if (i >= steps[m] || !ok) continue;
+          const int t = tile_of(m, i);
+          if (i + 1 < steps[m]) {
+            ok = wait_tile(tile_of(m, i + 1));
+            if (!ok) break;
+            issue_s(m, i + 1, tile_of(m, i + 1));
+          }
+          ok = role_wait(&sh.p[m][i & 1], (i >> 1) & 1, &sh.abort, p.status);
+          if (!ok) break;
+          issue_o(m, i, t);
+          if (kSplit || m == 1 || steps[1] == 0) {
+            if (elected()) commit(&sh.free[t % S::slots]);
+            __syncwarp();
+          }
+        }
+      }
+      if (elected()) commit(&sh.done);
+      __syncwarp();
+      if (!ok) mbar_wait_bounded(&sh.done, 0);
+    } else if (warp == kPlanWarp && blockIdx.x == 0) {
+      group_plan(p, kRows, pp.ctas, 0, lane, pp.plans);
+    }
+  } else if (warp >= kUnpackWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsUnpack));
+    // --- unpacking: warp w takes K (even) or V (odd) of cache tile w / 2 ---
+    const int uw = warp - kUnpackWarp, sub = uw >> 1, g = lane >> 2, t4 = lane & 3;
+    const bool values = uw & 1;
+    const int tpp = p.page_tokens / kTile;
+    const int32_t* table = p.page_table + int64_t(plan.group) * p.table_pages;
+    const int tiles = (plan.len + kTile - 1) / kTile;               // cache tiles held
+    auto page_of = [&](int i) {                   // of this warp's cache tile of tile i
+      const int tile = (first + i) * kSub + sub;
+      return i < n && tile < tiles ? __ldg(table + tile / tpp) : -1;
+    };
+    uint32_t there = 0;                           // bit i & 7: the cache tile of tile i exists
+    // The warp's packed rows of tile i, 16 bytes a lane and copy; a group of copies whether there are any or not
+    auto fetch = [&](int i, int page) {
+      const int tile = (first + i) * kSub + sub;
+      bool ok = i < n && tile < tiles;
+      if (ok && (page < 0 || page >= p.n_pages)) {
+        if (lane == 0) report_status(p.status, kStatusBadIndex);
+        ok = false;
+      }
+      there = (there & ~(1u << (i & 7))) | uint32_t(ok) << (i & 7);
+      if (ok) {
+        const uint8_t* src = p.pages + ((int64_t(page) * p.kv_heads + h) * tpp + tile % tpp) * int64_t(TB) + (values ? TB / 2 : 0);
+        const uint32_t dst = smem_q + S::at_raw + (i % kAhead) * S::raw + uw * kMostPacked;
+#pragma unroll
+        for (int k = 0; k < (TB / 32 + 31) / 32; ++k)
+          if (32 * k + lane < TB / 32) copy16(dst + (32 * k + lane) * 16, src + (32 * k + lane) * 16);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int most = 0;                                 // the largest exponent of a value that the warp has met
+    auto unpack = [&](int i, int slot) {
+      const uint8_t* src = smem + S::at_raw + (i % kAhead) * S::raw + uw * kMostPacked;
+      const int left = (there >> (i & 7)) & 1 ? plan.len - ((first + i) * kSub + sub) * kTile : 0;       // rows that exist
+      uint8_t* at = smem + S::at_slots + slot * S::slot;
+      if (!values) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int row = g + 8 * j, tk = sub * kTile + row;
+          uint32_t words[C] = {}, meta[NG] = {};
+          if (row < left) {
+            load_words<C>(words, src + row * (D / 2) + t4 * (D / 8));
+            load_words<NG>(meta, src + ts.k_meta() + row * 4 * NG);
+          }
+          const int e = top_exponent<NG>(meta);
+          const float f = down(e);
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            float s, m;
+            group_meta<NG>(meta, c / PG, s, m);
+            const __half2 s2 = __float2half2_rn(s * f);
+            const uint32_t w = words[c];
+            // dims 0, 4, 1, 5, 2, 6, 3, 7 of the word's eight
+            const uint4 v = make_uint4(bits(__hmul2(even_codes(w, 8.f), s2)), bits(__hmul2(odd_codes(w, 8.f), s2)),
+                                       bits(__hmul2(even_codes(w >> 8, 8.f), s2)), bits(__hmul2(odd_codes(w >> 8, 8.f), s2)));
+            const int word = 4 * c + t4;
+            *reinterpret_cast<uint4*>(at + (word >> 3) * (kPos * 128) + tk * 128 + (((word & 7) ^ (tk & 7)) << 4)) = v;
+          }
+          // the groups' m + 8 s: first planes (t4 = 0), second planes (1), first again (2), nothing (3)
+          float plane[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < NG; ++k) {
+            float s, m;
+            group_meta<NG>(meta, k, s, m);
+            const float x = fmaf(8.f, s, m) * f, top = __half2float(__float2half_rn(x));
+            plane[k] = t4 == 3 ? 0.f : t4 == 1 ? x - top : top;
+          }
+          *reinterpret_cast<uint2*>(at + S::k + S::v + tk * 32 + (((t4 >> 1) ^ ((tk >> 2) & 1)) << 4) + (t4 & 1) * 8) =
+              make_uint2(pack_f16(plane[0], plane[1]), pack_f16(plane[2], plane[3]));
+          if (t4 == 0) sh.up[slot][tk] = up(e);
+        }
+      } else {
+        constexpr int kCodes = 0, kMeta = ts.codes();        // of V alone
+        uint32_t words[2][C] = {}, metas[4][NG] = {};
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int pair = t4 + 4 * j;
+          if (2 * pair < left) load_words<C>(words[j], src + kCodes + pair * D + ts.v_place(pair, g) * (D / 8));
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (2 * pair + e < left) load_words<NG>(metas[2 * j + e], src + kMeta + (2 * pair + e) * 4 * NG);
+        }
+        int e[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) e[j] = top_exponent<NG>(metas[j]);
+        most = max(most, int(__reduce_max_sync(0xffffffffu, uint32_t(max(max(e[0], e[1]), max(e[2], e[3]))))));
+        const int least = max(most - kLeastBelow, kLeastExponent);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int tk = sub * kTile + 2 * (t4 + 4 * j);
+          const int ea = max(e[2 * j], least), eb = max(e[2 * j + 1], least);
+          const float fa = down(ea), fb = down(eb);
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            float sa, ma, sb, mb;
+            group_meta<NG>(metas[2 * j], c / PG, sa, ma);
+            group_meta<NG>(metas[2 * j + 1], c / PG, sb, mb);
+            const __half2 s2 = __floats2half2_rn(sa * fa, sb * fb), m2 = __floats2half2_rn(ma * fa, mb * fb);
+            const uint32_t w = words[j][c];
+            const __half2 v[4] = {__hfma2(even_codes(w, 0.f), s2, m2), __hfma2(odd_codes(w, 0.f), s2, m2),
+                                  __hfma2(even_codes(w >> 8, 0.f), s2, m2), __hfma2(odd_codes(w >> 8, 0.f), s2, m2)};
+            // dim 32c + 4g + i in row 32c + 8i + g: lanes of one store in eight rows, as many 16-byte words
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int row = 32 * c + 8 * i + g;
+              *reinterpret_cast<uint32_t*>(at + S::k + row * 128 + (((tk >> 3) ^ (row & 7)) << 4) + (tk & 7) * 2) = bits(v[i]);
+            }
+          }
+          if (g == 0) {
+            sh.c[slot][tk] = 2 * (t4 + 4 * j) < left ? float(ea - 141) : -INFINITY;
+            sh.c[slot][tk + 1] = 2 * (t4 + 4 * j) + 1 < left ? float(eb - 141) : -INFINITY;
+            sh.inv[slot][tk] = fa;
+            sh.inv[slot][tk + 1] = fb;
+          }
+        }
+      }
+    };
+    bool ok = true;
+#pragma unroll 1
+    for (int i = 0; i < kAhead - 1; ++i) fetch(i, page_of(i));
+    int page = page_of(kAhead - 1);               // of the next to fetch, asked for a tile ahead
+#pragma unroll 1
+    for (int i = 0; i < n && ok; ++i) {
+      const int slot = i % S::slots;
+      __syncwarp();                               // (all lanes have read what lay there)
+      fetch(i + kAhead - 1, page);
+      page = page_of(i + kAhead);
+      if (i >= S::slots) ok = role_wait(&sh.free[slot], (i / S::slots - 1) & 1, &sh.abort, p.status);
+      if (!ok) break;
+      asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+      __syncwarp();
+      unpack(i, slot);
+      fence_proxy_async_smem();
+      role_arrive(&sh.ready[slot]);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");        // (a wait that gave up leaves some)
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    // --- the softmax, a row a thread ---
+    const int m = warp >> 2, rt = (warp & 3) * 32 + lane, r = r0 + (kSplit ? 0 : m * 128) + rt;
+    const bool real = (kSplit ? 0 : m * 128) + rt < rows;
+    const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
+    float cq;
+    {
+      // the row's query, scaled below 2^8 (128 of them sum up within fp16), in the order of the keys' dims
+      uint32_t w[D / 2];                          // two neighbouring dims a word
+#pragma unroll
+      for (int k = 0; k < D / 2; ++k) w[k] = 0u;
+      if (real) {
+        const uint16_t* src = static_cast<const uint16_t*>(p.q) + (plan.q0 + r / p.group) * p.q_token +
+                              int64_t(h * p.group + r % p.group) * p.q_head;
+        if (p.q_wide) {
+#pragma unroll
+          for (int k = 0; k < D / 8; ++k) {
+            const uint4 v = reinterpret_cast<const uint4*>(src)[k];
+            w[4 * k] = v.x;
+            w[4 * k + 1] = v.y;
+            w[4 * k + 2] = v.z;
+            w[4 * k + 3] = v.w;
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < D / 2; ++k) w[k] = src[2 * k] | uint32_t(src[2 * k + 1]) << 16;
+        }
+      }
+      auto two = [&](int k) { return p.q_f16 ? __half22float2(*reinterpret_cast<const __half2*>(&w[k])) : bf16x2_to_float2(w[k]); };
+      float top = 0.f;
+#pragma unroll
+      for (int k = 0; k < D / 2; ++k) top = fmaxf(top, fmaxf(fabsf(two(k).x), fabsf(two(k).y)));
+      const int e = 134 - min(max(__float_as_int(top) >> 23, 1), 254), e1 = e >> 1, e2 = e - e1;
+      const float f1 = __int_as_float((127 + e1) << 23), f2 = __int_as_float((127 + e2) << 23);
+      float sums[4] = {0.f, 0.f, 0.f, 0.f}, left[4];
+#pragma unroll
+      for (int k = 0; k < D / 8; ++k) {
+        const float2 v0 = two(4 * k), v1 = two(4 * k + 1), v2 = two(4 * k + 2), v3 = two(4 * k + 3);
+        // dims 0, 4, 1, 5, 2, 6, 3, 7 of eight
+        const uint32_t held[4] = {pack_f16(v0.x * f1 * f2, v2.x * f1 * f2), pack_f16(v0.y * f1 * f2, v2.y * f1 * f2),
+                                  pack_f16(v1.x * f1 * f2, v3.x * f1 * f2), pack_f16(v1.y * f1 * f2, v3.y * f1 * f2)};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&held[j]));
+          sums[k / (D / 8 / NG)] += x.x + x.y;
+        }
+        if (!kSplit || m == 0)                    // (two streams have one block of rows)
+          *reinterpret_cast<uint4*>(smem + m * S::q + (k >> 3) * kHalf + rt * 128 + (((k & 7) ^ (rt & 7)) << 4)) =
+              make_uint4(held[0], held[1], held[2], held[3]);
+      }
+      // against the keys' planes: first planes twice, then what they left over
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        left[k] = sums[k];
+        sums[k] = __half2float(__float2half_rn(sums[k]));
+        left[k] -= sums[k];
+      }
+      const uint2 top_planes = make_uint2(pack_f16(sums[0], sums[1]), pack_f16(sums[2], sums[3]));
+      const uint2 low_planes = make_uint2(pack_f16(left[0], left[1]), pack_f16(left[2], left[3]));
+      if (!kSplit || m == 0) {
+        uint8_t* more = smem + S::at_q_more + m * S::q_more + rt * 32;
+        const int turn_word = ((rt >> 2) & 1) << 4;
+        *reinterpret_cast<uint4*>(more + turn_word) = make_uint4(top_planes.x, top_planes.y, top_planes.x, top_planes.y);
+        *reinterpret_cast<uint4*>(more + (16 ^ turn_word)) = make_uint4(low_planes.x, low_planes.y, 0u, 0u);
+      }
+      cq = p.scale2 * __int_as_float((127 - e1) << 23) * __int_as_float((127 - e2) << 23);
+      fence_proxy_async_smem();
+    }
+    role_arrive(&sh.q);
+    const int mine = steps[m];
+    float ref = kNoRef, l = 0.f;
+    bool ok = true;
+#pragma unroll 1
+    for (int i = 0; i < mine; ++i) {
+      ok = role_wait(&sh.s[m][i & 1], (i >> 1) & 1, &sh.abort, p.status);
+      if (!ok) break;
+      fence_after();
+      const int slot = (kSplit ? 2 * i + m : i) % S::slots;
+      float x[kPos];
+      auto logits = [&]() {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) load16(s_cols(m, i) + lanes + 16 * k, x + 16 * k);
+        landed();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) defined16(x + 16 * k);
+      };
+      const float4* up4 = reinterpret_cast<const float4*>(sh.up[slot]);
+      const float4* c4 = reinterpret_cast<const float4*>(sh.c[slot]);
+      const float4* inv4 = reinterpret_cast<const float4*>(sh.inv[slot]);
+      logits();
+      // weights (times the values' scale) in place, their sum and that of the weights alone
+      float2 w2 = make_float2(0.f, 0.f), l2 = w2;
+#pragma unroll
+      for (int k = 0; k < kPos; k += 4) {
+        const float4 u = up4[k / 4], c = c4[k / 4], v = inv4[k / 4];
+        const float2 a = ffma2(make_float2(x[k], x[k + 1]), fmul2(make_float2(u.x, u.y), make_float2(cq, cq)),
+                               fadd2(make_float2(c.x, c.y), make_float2(-ref, -ref)));
+        const float2 b = ffma2(make_float2(x[k + 2], x[k + 3]), fmul2(make_float2(u.z, u.w), make_float2(cq, cq)),
+                               fadd2(make_float2(c.z, c.w), make_float2(-ref, -ref)));
+        x[k] = exp2_fast(a.x);
+        x[k + 1] = exp2_fast(a.y);
+        x[k + 2] = exp2_fast(b.x);
+        x[k + 3] = exp2_fast(b.y);
+        w2 = fadd2(w2, fadd2(make_float2(x[k], x[k + 1]), make_float2(x[k + 2], x[k + 3])));
+        l2 = ffma2(make_float2(x[k], x[k + 1]), make_float2(v.x, v.y), l2);
+        l2 = ffma2(make_float2(x[k + 2], x[k + 3]), make_float2(v.z, v.w), l2);
+      }
+      float keep = 1.f;
+      const float sum = w2.x + w2.y;
+      if (__any_sync(0xffffffffu, !(sum <= 16384.f))) {
+        // The logits again, and the reference 6 below the largest; from rounded logits, as the
+        // reference is: past 2^26 it may lie many units off the unrounded ones.
+        logits();
+        float top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kPos; ++k) {
+          x[k] = __fadd_rn(__fmul_rn(x[k], sh.up[slot][k] * cq), sh.c[slot][k]);
+          top = fmaxf(top, x[k]);
+        }
+        const float now = sum <= 16384.f ? ref : fmaxf(ref, top - 6.f);
+        keep = exp2f(ref - now);
+        ref = now;
+        l2 = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < kPos; ++k) {
+          x[k] = exp2_fast(min_nan(x[k] - ref, 15.5f));
+          l2.x = fmaf(x[k], sh.inv[slot][k], l2.x);
+        }
+      }
+      l = l * keep + (l2.x + l2.y);
+      if (i > 0 && __any_sync(0xffffffffu, keep != 1.f)) {
+        ok = role_wait(&sh.pv[m], (i - 1) & 1, &sh.abort, p.status);
+        if (!ok) break;
+        fence_after();
+#pragma unroll 1
+        for (int c = 0; c < D / 16; ++c) {
+          float v[16];
+          load16(o_cols(m) + lanes + 16 * c, v);
+          landed();
+          defined16(v);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] *= keep;
+          store16(o_cols(m) + lanes + 16 * c, v);
+        }
+      }
+      uint32_t w[32];
+#pragma unroll
+      for (int k = 0; k < 32; ++k) w[k] = pack_f16(x[2 * k], x[2 * k + 1]);
+      store32(s_cols(m, i) + lanes, w);
+      stored();
+      fence_before();
+      role_arrive(&sh.p[m][i & 1]);
+    }
+    if (ok) ok = role_wait(&sh.done, 0, &sh.abort, p.status);
+    fence_after();
+    asm volatile("bar.sync 1, 256;" ::: "memory");        // all products are done: their operands' memory is free
+    const bool seen = mine > 0 && ok && (ref != kNoRef || l != 0.f);
+    float4* out = reinterpret_cast<float4*>(smem) + (m * 128 + rt) * (D / 4);
+    float* refs = reinterpret_cast<float*>(smem + S::at_ref);
+    if (mine > 0 && ok) {
+#pragma unroll 1
+      for (int c = 0; c < C; ++c) {
+        float o[32];
+        load16(o_cols(m) + lanes + 32 * c, o);
+        load16(o_cols(m) + lanes + 32 * c + 16, o + 16);
+        landed();
+        defined16(o);
+        defined16(o + 16);
+        // dims 4k .. 4k + 3 of the 32 came as columns k, 8 + k, ..; word u of row r at u ^ r, on banks of their own
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          out[(8 * c + k) ^ (rt & (D / 4 - 1))] = make_float4(o[k], o[8 + k], o[16 + k], o[24 + k]);
+      }
+    }
+    refs[m * 128 + rt] = seen ? ref : -INFINITY;
+    refs[256 + m * 128 + rt] = seen ? l : 0.f;
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    // --- the record: a row a warp, of one stream or of two joined ---
+    const int64_t slot = int64_t(blockIdx.x) * kRows;
+    const float4* held = reinterpret_cast<const float4*>(smem);
+#pragma unroll 2
+    for (int i = warp; i < rows; i += 8) {
+      const float a = refs[i], b = kSplit ? refs[128 + i] : -INFINITY, top = fmaxf(a, b);
+      const float wa = a == -INFINITY ? 0.f : exp2f(a - top), wb = b == -INFINITY ? 0.f : exp2f(b - top);
+      const float total = (a == -INFINITY ? 0.f : wa * refs[256 + i]) + (b == -INFINITY ? 0.f : wb * refs[256 + 128 + i]);
+      const bool any = a != -INFINITY || b != -INFINITY;
+      const float inv = any ? 1.f / total : 0.f;
+      if (lane < D / 4) {
+        const int u = lane ^ (i & (D / 4 - 1));
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (a != -INFINITY) add_scaled(v, wa * inv, held[i * (D / 4) + u]);
+        if (kSplit && b != -INFINITY) add_scaled(v, wb * inv, held[(128 + i) * (D / 4) + u]);
+        reinterpret_cast<float4*>(pp.records + (slot + i) * D)[lane] = v;
+      }
+      if (lane == 0) pp.sums[slot + i] = any ? top + log2f(total) : -INFINITY;
+    }
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (warp == kIssueWarp) give_columns(tmem);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+template <int D, int NG, bool kSplit>
+cudaError_t launch(const PrefixParams& pp, int items, int dev, cudaStream_t s) {
+  // the kernel's shared memory limit, raised once a device
+  static std::atomic<uint64_t> raised{0};
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+  if (!(raised.load(std::memory_order_relaxed) & bit) || !bit) {
+    const cudaError_t err = cudaFuncSetAttribute(k_attn_prefix<D, NG, kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 PrefixSmem<D, kSplit>::bytes);
+    if (err != cudaSuccess) return err;
+    raised.fetch_or(bit, std::memory_order_relaxed);
+  }
+  return launch_early(k_attn_prefix<D, NG, kSplit>, unsigned(items), kThreads, PrefixSmem<D, kSplit>::bytes, s, pp);
+}
+
+template <bool kSplit>
+cudaError_t dispatch(const PrefixParams& pp, int items, int d, int group, int dev, cudaStream_t s) {
+  if (d == 128 && group == 32) return launch<128, 4, kSplit>(pp, items, dev, s);
+  if (d == 128 && group == 64) return launch<128, 2, kSplit>(pp, items, dev, s);
+  if (d == 128) return launch<128, 1, kSplit>(pp, items, dev, s);
+  if (group == 32) return launch<64, 2, kSplit>(pp, items, dev, s);
+  return launch<64, 1, kSplit>(pp, items, dev, s);
+}
+
+}  // namespace
+
+cudaError_t launch_attn_groups(const AttnParams& p, int mt, int items, int ctas, int d, int quant_group, int dev, float* records,
+                               GroupPlan* plans, cudaStream_t s) {
+  PrefixParams pp{};
+  pp.a = p;
+  pp.a.page_table = p.prefix_table;               // the kernel has groups for sequences
+  pp.a.pages = p.prefix_data;
+  pp.a.status = p.prefix_status;
+  pp.a.n_pages = p.prefix_n_pages;
+  pp.a.table_pages = p.prefix_pages;
+  pp.plans = plans;
+  pp.records = records;
+  pp.sums = p.prefix_ref;
+  pp.ctas = ctas;
+  return mt == 1 ? dispatch<true>(pp, items, d, quant_group, dev, s) : dispatch<false>(pp, items, d, quant_group, dev, s);
+}
+
+}  // namespace reskv

@@ -33,51 +33,58 @@ __global__ void __launch_bounds__(kWarps * 32) k_shared_join(const __grid_consta
   wait_for_previous();
   if (tok >= p.n_tokens) return;
   // the sequence, then the group
-  const int seq = p.q_begin ? range_of(p.q_begin, p.members, tok) : int(tok / (p.n_tokens / p.members));
+  const int seq = p.q_begin ? range_of(p.q_begin, p.sequences, tok) : int(tok / (p.n_tokens / p.sequences));
   if (seq < 0) return;                            // a query of no sequence
-  const int group = p.seq_begin ? range_of(p.seq_begin, p.batch, seq) : seq / (p.members / p.batch);
+  const int group = p.seq_begin ? range_of(p.seq_begin, j.groups, seq) : seq / (p.sequences / j.groups);
+  const int u = lane < D / 4 ? lane : 0;
   const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
   const float own = j.own_ref[row];
   const bool with_own = own != -INFINITY;
-  float4 a = zero;
-  if (lane < D / 4 && with_own) a = reinterpret_cast<const float4*>(j.own + row * D)[lane];
+  float4 a = with_own ? reinterpret_cast<const float4*>(j.own + row * D)[u] : zero;
   int parts = 0;
   int64_t first = 0, stride = 0;                  // rows of the prefix's records
-  if (group >= 0 && j.block_rows) {
-    const GroupPlan g = group_plan(p, j.block_rows, j.ctas, -1, group, lane);
-    const int64_t r = (tok - g.s.q0) * p.group + head % p.group;
+  if (group >= 0 && j.plans) {
+    const GroupPlan g = j.plans[group];
+    const int64_t r = (tok - g.q0) * p.group + head % p.group;
     // (of a seq_begin out of order there may be more items than CTAs and records)
-    if (tok >= g.s.q0 && tok < g.s.q0 + g.s.count && g.first + int64_t(g.parts) * g.row_blocks * p.kv_heads <= j.items) {
+    if (tok >= g.q0 && tok < g.q0 + g.count && g.first + int64_t(g.parts) * g.row_blocks * p.kv_heads <= j.items) {
       parts = g.parts;
       stride = int64_t(g.row_blocks) * j.block_rows;
       first = (g.first + int64_t(head / p.group) * parts * g.row_blocks) * j.block_rows + r;
     }
   } else if (group >= 0) {
-    const Sequence s = sequence_of(p, group);
+    const Sequence s = group_of(p, group, j.groups);
     if (tok >= s.q0 && tok < s.q0 + s.count) {
       parts = 1;
       first = row;
     }
   }
-  float top = own;
+  // 32 parts at a time, their sums in the lanes; a part of weight 0 still counts: a NaN in it is seen
+  float top = own, sum = with_own ? 1.f : 0.f;
 #pragma unroll 1
-  for (int k = lane; k < parts; k += 32) top = fmaxf(top, j.prefix_ref[first + k * stride]);
+  for (int k0 = 0; k0 < parts; k0 += 32) {
+    const int n = min(32, parts - k0);
+    const float ref = lane < n ? j.prefix_ref[first + (k0 + lane) * stride] : -INFINITY;
+    const float* rows = j.prefix + (first + k0 * stride) * D;
+    float now = ref;
 #pragma unroll
-  for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  // a part of weight 0 still counts: a NaN in it is seen
-  float sum = 0.f;
-  if (with_own) {
-    const float f = exp2f(own - top);
-    sum = f;
-    a = make_float4(a.x * f, a.y * f, a.z * f, a.w * f);
-  }
-#pragma unroll 2
-  for (int k = 0; k < parts; ++k) {
-    const float ref = j.prefix_ref[first + k * stride];
-    if (ref == -INFINITY) continue;
-    const float f = exp2f(ref - top);
-    sum += f;
-    if (lane < D / 4) add_scaled(a, f, reinterpret_cast<const float4*>(j.prefix + (first + k * stride) * D)[lane]);
+    for (int o = 16; o; o /= 2) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, o));
+    now = fmaxf(now, top);
+    const uint32_t present = __ballot_sync(0xffffffffu, ref != -INFINITY);
+    if (!present) continue;
+    const float keep = top == -INFINITY ? 0.f : exp2f(top - now), f = ref == -INFINITY ? 0.f : exp2f(ref - now);
+    float more = f;
+#pragma unroll
+    for (int o = 16; o; o /= 2) more += __shfl_xor_sync(0xffffffffu, more, o);
+    sum = top == -INFINITY ? more : fmaf(sum, keep, more);
+    a = top == -INFINITY ? zero : make_float4(a.x * keep, a.y * keep, a.z * keep, a.w * keep);
+    top = now;
+#pragma unroll 8
+    for (int k = 0; k < n; ++k) {
+      const float w = __shfl_sync(0xffffffffu, f, k);
+      const float4 v = (present >> k) & 1 ? reinterpret_cast<const float4*>(rows + k * stride * D)[u] : zero;
+      add_scaled(a, w, v);
+    }
   }
   const bool seen = sum != 0.f;
   const float inv = seen ? 1.f / sum : 0.f;
