@@ -5,11 +5,11 @@
 // fit).  A CTA takes two tiles and walks the states 128 at a time:
 //
 //   S = Q K^T       [128 rows x 128 states]  both operands in shared memory, into TMEM
-//   P = 2^(S - ref) one row a thread, in the type of q, over S in TMEM
+//   P = 2^(S - ref) half a row a thread, in the type of q, over S in TMEM
 //   O += P V        [128 rows x d]           P from TMEM, V as it lies (across), into TMEM
 //
-// Copies, products and the softmax (four warps a tile) are roles of their own; while one tile's
-// softmax runs, the tensor cores work for the other.  Where a sequence has one tile's rows
+// Copies, products and the softmax (eight warps a tile, two threads a row) are roles of their own; while one
+// tile's softmax runs, the tensor cores work for the other.  Where a sequence has one tile's rows
 // only, the CTA's two streams take the even and the odd tiles of states (kSplit).  Where
 // there are too few blocks for the SMs, a cluster of CTAs shares a block's states.  Streams and
 // CTAs leave their rows in shared memory and are joined over the cluster, in order.
@@ -34,10 +34,10 @@ namespace {
 using namespace tc;
 
 constexpr int kStates = 128;                      // of a tile
-constexpr int kThreads = 384;                     // warps 0-3, 4-7 softmax, 8 copies, 9 products, 10 the tail
-constexpr int kCopyWarp = 8, kIssueWarp = 9, kTailWarp = 10;
-constexpr int kRegsSoftmax = 232, kRegsIssue = 40;
-static_assert((2 * kRegsSoftmax + kRegsIssue) * 128 <= 168 * kThreads, "registers");
+constexpr int kThreads = 640;                     // warps 0-7, 8-15 softmax, 16 copies, 17 products, 18 the tail
+constexpr int kSoftmaxWarps = 16, kCopyWarp = 16, kIssueWarp = 17, kTailWarp = 18;
+constexpr int kRegsSoftmax = 104, kRegsIssue = 56;
+static_assert((4 * kRegsSoftmax + kRegsIssue) * 128 <= 96 * kThreads, "registers");
 constexpr float kNoReference = -3.0e38f;
 
 struct BlocksParams {
@@ -56,12 +56,23 @@ struct BlocksSmem {
   static constexpr int bytes = q + slots * tile + 1024;               // on a boundary of 1024
   static constexpr int at_ref = 2 * 128 * D * 4;  // of rows to be joined: outputs, then references and sums
   static_assert(at_ref + 2 * 256 * 4 <= q + slots * tile, "rows to be joined");
+  static_assert(bytes + 1024 + 256 <= 227 * 1024, "shared memory");
 };
 
 struct BlocksShared {
   uint64_t q, full[8], empty[8], s[2], p[2], done, tail;
   uint32_t tmem, abort;
+  float half[2][128];             // of a row's second half, for the first and back
 };
+// A barrier of two warps; true in all where `x` is in one.
+__device__ __forceinline__ bool pair_any(int id, bool x) {
+  uint32_t y;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbarrier.cta.red.or.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(y) : "r"(id), "r"(uint32_t(x)) : "memory");
+  return y != 0;
+}
+__device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
+
 
 template <int D, bool kF16, bool kSplit>
 __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_constant__ BlocksParams bp) {
@@ -83,7 +94,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
     }
     for (int m = 0; m < 2; ++m) {
       mbar_init(&sh.s[m], 1);
-      mbar_init(&sh.p[m], 4);
+      mbar_init(&sh.p[m], 8);
     }
     mbar_init(&sh.done, 1);
     mbar_init(&sh.tail, 1);
@@ -105,17 +116,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
   const int left = sq.seen - (first + n - 1) * kStates;               // states of the last tile
   const bool cut = n > 0 && left < kStates;
 
-  // a softmax thread's row
-  const int m = (warp >> 2) & 1, rt = (warp & 3) * 32 + lane;
+  // a softmax thread's row and half
+  const int m = (warp >> 3) & 1, c = (warp >> 2) & 1, rt = (warp & 3) * 32 + lane;
   const int row_token = rt / p.group, token = t0 + (kSplit ? 0 : m * tt) + row_token;
-  const bool real = warp < 8 && row_token < tt && token < sq.count;
+  const bool real = warp < kSoftmaxWarps && row_token < tt && token < sq.count;
   const int head = h * p.group + rt - row_token * p.group;
   if (sq.seen == 0) {                             // the same for the whole cluster
     if (real && rank == 0 && (m == 0 || !kSplit)) {
-      uint16_t* y = static_cast<uint16_t*>(p.o.data) + (sq.q0 + token) * p.o.token + head * p.o.head;
+      uint16_t* y = static_cast<uint16_t*>(p.o.data) + (sq.q0 + token) * p.o.token + head * p.o.head + c * (D / 2);
 #pragma unroll 1
-      for (int i = 0; i < D / 8; ++i) reinterpret_cast<uint4*>(y)[i] = make_uint4(0, 0, 0, 0);
-      if (p.lse) p.lse[int64_t(sq.q0 + token) * p.heads + head] = -INFINITY;
+      for (int i = 0; i < D / 16; ++i) reinterpret_cast<uint4*>(y)[i] = make_uint4(0, 0, 0, 0);
+      if (p.lse && c == 0) p.lse[int64_t(sq.q0 + token) * p.heads + head] = -INFINITY;
     }
     return;
   }
@@ -130,7 +141,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
   auto k_op = [&](int t) { return kSplit ? (t == 0 ? 0 : 2 * t - 1) : 2 * t; };
   auto v_op = [&](int t) { return kSplit ? (t + 1 < n ? 2 * t + 2 : 2 * t + 1) : 2 * t + 1; };
 
-  if (warp >= 8) {
+  if (warp >= kSoftmaxWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
     if (warp == kCopyWarp) {
       // --- copies ---
@@ -193,7 +204,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
           const uint32_t v0 = operand_across(ring + op % S::slots * S::tile, S::half);
 #pragma unroll
           for (int k = 0; k < kStates / 16; ++k)
-            multiply_from<kRows128, kOutputs>(o_cols(s), s_cols(s) + k * 8, v0 + ((k * 16 * 128) >> 4), add || k > 0);
+            multiply_from<kRows128, kOutputs>(o_cols(s), step_of(s_cols(s), k), v0 + ((k * 16 * 128) >> 4), add || k > 0);
         }
         __syncwarp();
       };
@@ -245,77 +256,90 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-    // --- the softmax, a row a thread ---
+    // --- the softmax, half a row a thread: states 64 c .. 64 c + 63 of a tile.  With one thread a row (four
+    // warps a tile) a tile waited for 128 exponentials a thread one after the other: 8 x 1024 tokens over
+    // 4096 states 523 us, 365 without any exponential ---
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
-    const int mine = steps[m];
+    const int mine = steps[m], pair = 1 + 4 * m + (warp & 3);
     const float f = p.scale2;
     float ref = kNoReference, l = 0.f;
     bool ok = true;
 #pragma unroll 1
     for (int i = 0; i < mine; ++i) {
       ok = role_wait(&sh.s[m], i & 1, &sh.abort, p.status);
-      if (!ok) break;
       fence_after();
       const int t = kSplit ? 2 * i + m : i;
-      const int upto = t == n - 1 ? left : kStates;
-      float x[kStates];
-      auto logits = [&]() {
+      const int upto = (t == n - 1 ? left : kStates) - 64 * c;
+      float x[64];
+      load64(s_cols(m) + lanes + 64 * c, x);
+      landed64(x);
+      float2 s2[4] = {};
 #pragma unroll
-        for (int k = 0; k < kStates / 16; ++k) load16(s_cols(m) + lanes + 16 * k, x + 16 * k);
-        landed();
+      for (int k = 0; k < 64; k += 2) {
+        const float2 y = ffma2(make_float2(x[k], x[k + 1]), make_float2(f, f), make_float2(-ref, -ref));
+        x[k] = exp2_fast(y.x);
+        x[k + 1] = exp2_fast(y.y);
+      }
+      if (upto < 64) {
 #pragma unroll
-        for (int k = 0; k < kStates / 16; ++k) defined16(x + 16 * k);
-      };
-      auto weights = [&]() {                      // x: logits -> weights, in place; returns their sum
-        float2 s2[4] = {};
+        for (int k = 0; k < 64; ++k)
+          if (k >= upto) x[k] = 0.f;
+      }
 #pragma unroll
-        for (int k = 0; k < kStates; k += 2) {
-          const float2 y = ffma2(make_float2(x[k], x[k + 1]), make_float2(f, f), make_float2(-ref, -ref));
-          x[k] = exp2_fast(y.x);
-          x[k + 1] = exp2_fast(y.y);
+      for (int k = 0; k < 64; k += 2) s2[(k / 2) & 3] = fadd2(s2[(k / 2) & 3], make_float2(x[k], x[k + 1]));
+      s2[0] = fadd2(fadd2(s2[0], s2[1]), fadd2(s2[2], s2[3]));
+      float sum = s2[0].x + s2[0].y, keep = 1.f;
+      if (pair_any(pair, !ok || !(sum <= 8192.f))) {
+        if (pair_any(pair, !ok)) {                // a wait gave up: both leave
+          ok = false;
+          break;
         }
-        if (upto < kStates) {
-#pragma unroll
-          for (int k = 0; k < kStates; ++k)
-            if (k >= upto) x[k] = 0.f;
-        }
-#pragma unroll
-        for (int k = 0; k < kStates; k += 2) s2[(k / 2) & 3] = fadd2(s2[(k / 2) & 3], make_float2(x[k], x[k + 1]));
-        const float2 s = fadd2(fadd2(s2[0], s2[1]), fadd2(s2[2], s2[3]));
-        return s.x + s.y;
-      };
-      logits();
-      float sum = weights(), keep = 1.f;
-      if (__any_sync(0xffffffffu, !(sum <= 16384.f))) {
-        logits();
+        // The logits again, and the reference 6 below the row's largest; weights from rounded logits, as
+        // the reference is: past 2^26 it may lie many units off the unrounded ones.
+        load64(s_cols(m) + lanes + 64 * c, x);
+        landed64(x);
         float top = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < kStates; ++k) top = fmaxf(top, k < upto ? __fmul_rn(x[k], f) : -INFINITY);
-        const float now = sum <= 16384.f ? ref : fmaxf(ref, top - 6.f);
+        for (int k = 0; k < 64; ++k) {
+          x[k] = k < upto ? __fmul_rn(x[k], f) : -INFINITY;
+          top = fmaxf(top, x[k]);
+        }
+        // (one half at a time: the other's word is read before its own is written)
+        if (c == 1) sh.half[m][rt] = top;
+        pair_sync(pair);
+        if (c == 0) {
+          top = fmaxf(top, sh.half[m][rt]);
+          sh.half[m][rt] = top;
+        }
+        pair_sync(pair);
+        top = sh.half[m][rt];
+        const float now = fmaxf(ref, top - 6.f);
         keep = exp2f(ref - now);
         ref = now;
-        sum = weights();
+        sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < 64; ++k) {
+          x[k] = exp2_fast(x[k] - ref);
+          sum += x[k];
+        }
       }
       l = l * keep + sum;
       if (i > 0 && __any_sync(0xffffffffu, keep != 1.f)) {       // (S's barrier has the products before it behind it)
 #pragma unroll 1
-        for (int c = 0; c < D / 16; ++c) {
+        for (int k0 = 0; k0 < D / 32; ++k0) {
           float v[16];
-          load16(o_cols(m) + lanes + 16 * c, v);
+          load16(o_cols(m) + lanes + c * (D / 2) + 16 * k0, v);
           landed();
           defined16(v);
 #pragma unroll
           for (int k = 0; k < 16; ++k) v[k] *= keep;
-          store16(o_cols(m) + lanes + 16 * c, v);
+          store16(o_cols(m) + lanes + c * (D / 2) + 16 * k0, v);
         }
       }
+      uint32_t w[32];
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        uint32_t w[32];
-#pragma unroll
-        for (int k = 0; k < 32; ++k) w[k] = pack_two<kF16>(x[64 * c + 2 * k], x[64 * c + 2 * k + 1]);
-        store32(s_cols(m) + lanes + 32 * c, w);
-      }
+      for (int k = 0; k < 32; ++k) w[k] = pack_two<kF16>(x[2 * k], x[2 * k + 1]);
+      store32(s_cols(m) + lanes + 64 * c, w);
       stored();
       fence_before();
       role_arrive(&sh.p[m]);
@@ -323,48 +347,58 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
     if (ok && mine > 0) ok = role_wait(&sh.done, 0, &sh.abort, p.status);
     fence_after();
     const bool seen = mine > 0 && ok;
+    // the row's sum, of both halves
+    if (c == 1) sh.half[m][rt] = l;
+    pair_sync(pair);
+    if (c == 0) {
+      l += sh.half[m][rt];
+      sh.half[m][rt] = l;
+    }
+    pair_sync(pair);
+    l = sh.half[m][rt];
     if (cs == 1 && !kSplit) {
       const float inv = 1.f / l;
       if (seen) {
-        uint16_t* y = static_cast<uint16_t*>(p.o.data) + (sq.q0 + token) * p.o.token + head * p.o.head;
+        uint16_t* y = static_cast<uint16_t*>(p.o.data) + (sq.q0 + token) * p.o.token + head * p.o.head + c * (D / 2);
 #pragma unroll 1
-        for (int c = 0; c < D / 32; ++c) {
-          float o[32];
-          load16(o_cols(m) + lanes + 32 * c, o);
-          load16(o_cols(m) + lanes + 32 * c + 16, o + 16);
+        for (int k0 = 0; k0 < D / 32; ++k0) {
+          float o[16];
+          load16(o_cols(m) + lanes + c * (D / 2) + 16 * k0, o);
           landed();
           defined16(o);
-          defined16(o + 16);
           if (real) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 2; ++k) {
               uint32_t w[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) w[e] = pack_two<kF16>(o[8 * k + 2 * e] * inv, o[8 * k + 2 * e + 1] * inv);
-              reinterpret_cast<uint4*>(y)[4 * c + k] = make_uint4(w[0], w[1], w[2], w[3]);
+              reinterpret_cast<uint4*>(y)[2 * k0 + k] = make_uint4(w[0], w[1], w[2], w[3]);
             }
           }
         }
-        if (real && p.lse) p.lse[int64_t(sq.q0 + token) * p.heads + head] = (ref + log2f(l)) * 0.693147180559945f;
+        if (real && p.lse && c == 0) p.lse[int64_t(sq.q0 + token) * p.heads + head] = (ref + log2f(l)) * 0.693147180559945f;
       }
     } else {
       // for the join: all products are done, operands' memory is free (word u of row r at u ^ r)
-      asm volatile("bar.sync 1, 256;" ::: "memory");
+      asm volatile("bar.sync 9, 512;" ::: "memory");
       float4* rows = reinterpret_cast<float4*>(smem) + (m * 128 + rt) * (D / 4);
       if (seen) {
 #pragma unroll 1
-        for (int c = 0; c < D / 16; ++c) {
+        for (int k0 = 0; k0 < D / 32; ++k0) {
           float o[16];
-          load16(o_cols(m) + lanes + 16 * c, o);
+          load16(o_cols(m) + lanes + c * (D / 2) + 16 * k0, o);
           landed();
           defined16(o);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) rows[(4 * c + k) ^ (rt & (D / 4 - 1))] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+          for (int k = 0; k < 4; ++k)
+            rows[(c * (D / 8) + 4 * k0 + k) ^ (rt & (D / 4 - 1))] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
         }
       }
       float* refs = reinterpret_cast<float*>(smem + S::at_ref);
-      refs[m * 128 + rt] = seen ? ref : -INFINITY;
-      refs[256 + m * 128 + rt] = seen ? l : 0.f;
+      if (c == 0) {
+        refs[m * 128 + rt] = seen ? ref : -INFINITY;
+        refs[256 + m * 128 + rt] = seen ? l : 0.f;
+      }
     }
   }
   fence_before();
@@ -379,7 +413,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
   const uint32_t at_rows = smem_q, at_ref = smem_q + S::at_ref, at_sum = at_ref + 256 * 4;
   constexpr int kSources = kSplit ? 2 : 1;
 #pragma unroll 1
-  for (int r = rank * 8 + warp; warp < 8 && r < rows; r += cs * 8) {
+  for (int r = rank * kSoftmaxWarps + warp; warp < kSoftmaxWarps && r < rows; r += cs * kSoftmaxWarps) {
     const int rm = r >> 7, rr = r & 127;          // (split: tile 0's row, of both streams)
     const int tk = rr / p.group, tok = t0 + rm * tt + tk;
     if (tk >= tt || tok >= sq.count) continue;

@@ -43,16 +43,6 @@ struct GradParams {
   int32_t tile_tokens;
 };
 
-// Half of a row in TMEM: columns at .. at + 63.
-__device__ __forceinline__ void load64(uint32_t at, float (&x)[64]) {
-#pragma unroll
-  for (int k = 0; k < 4; ++k) load16(at + 16 * k, x + 16 * k);
-}
-__device__ __forceinline__ void landed64(float (&x)[64]) {
-  landed();
-#pragma unroll
-  for (int k = 0; k < 4; ++k) defined16(x + 16 * k);
-}
 // 64 values in q's type over the first 32 of the 64 columns that they came from; `sum`: and their sum, as rounded
 template <bool kF16>
 __device__ __forceinline__ void store64(uint32_t at, const float (&x)[64], float2* sum = nullptr) {
@@ -67,9 +57,6 @@ __device__ __forceinline__ void store64(uint32_t at, const float (&x)[64], float
   }
   stored();
 }
-// and where step k of a product finds its 16 of them
-__device__ __forceinline__ uint32_t step_of(uint32_t at, int k) { return at + uint32_t((k >> 2) * 64 + (k & 3) * 8); }
-
 // Columns [c0, c0 + n) of a thread's TMEM row, times f, to y in 16 bits.
 template <bool kF16, int N>
 __device__ __forceinline__ void store_columns(uint32_t at, float f, uint16_t* y, bool real) {

@@ -105,6 +105,20 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, i
       : "memory");
 }
 
+// Half of a 128-column row in TMEM: columns at .. at + 63.
+__device__ __forceinline__ void load64(uint32_t at, float (&x)[64]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) load16(at + 16 * k, x + 16 * k);
+}
+__device__ __forceinline__ void landed64(float (&x)[64]) {
+  landed();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) defined16(x + 16 * k);
+}
+// Two halves of a row, 64 values of 16 bits in the first 32 of 64 columns each: where step k (16 values) of a
+// product over them finds its own.
+__device__ __forceinline__ uint32_t step_of(uint32_t at, int k) { return at + uint32_t((k >> 2) * 64 + (k & 3) * 8); }
+
 // Waits of kernels whose warps have roles: bounded, and over for all once one gave up.
 __device__ __forceinline__ bool role_wait(uint64_t* bar, uint32_t parity, uint32_t* abort, uint32_t* status) {
   bool ok = mbar_try_wait(bar, parity);
