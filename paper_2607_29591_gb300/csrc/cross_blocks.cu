@@ -22,8 +22,7 @@
 //   tail          the last V has landed, behind its last state anything: a warp puts zeros there
 //                 and passes it on as full[op]
 //
-// The reference of a row moves only when weights pass 2^14; it then lies 6 below the largest
-// logit.  No largest logit is looked for otherwise.
+// The reference of a row moves only when a weight passes 2^13; it then lies 6 below the largest logit.
 #include "cross.cuh"
 #include "tensor_core.cuh"
 #include "warp_mma.cuh"
@@ -64,13 +63,7 @@ struct BlocksShared {
   uint32_t tmem, abort;
   float half[2][128];             // of a row's second half, for the first and back
 };
-// A barrier of two warps; true in all where `x` is in one.
-__device__ __forceinline__ bool pair_any(int id, bool x) {
-  uint32_t y;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbarrier.cta.red.or.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-               : "=r"(y) : "r"(id), "r"(uint32_t(x)) : "memory");
-  return y != 0;
-}
+// A barrier of two warps.
 __device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
 
 
@@ -186,14 +179,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
         if (elected()) commit(&sh.empty[op % S::slots]);
         __syncwarp();
       };
+      const uint32_t logits = kLogits | (p.scale2 < 0.f ? kNegative : 0u);
       auto issue_s = [&](int s, int op) {
         fence_after();
         if (elected()) {
           const uint32_t q0 = operand(smem_q + (kSplit ? 0 : s) * S::tile), k0 = operand(ring + op % S::slots * S::tile);
 #pragma unroll
           for (int k = 0; k < D / 16; ++k)
-            multiply<kRows128, kLogits>(s_cols(s), q0 + (((k / 4) * S::half + (k & 3) * 32) >> 4),
-                                        k0 + (((k / 4) * S::half + (k & 3) * 32) >> 4), k > 0);
+            multiply<kRows128>(s_cols(s), q0 + (((k / 4) * S::half + (k & 3) * 32) >> 4),
+                               k0 + (((k / 4) * S::half + (k & 3) * 32) >> 4), logits, k > 0);
           commit(&sh.s[s]);
         }
         __syncwarp();
@@ -256,73 +250,72 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-    // --- the softmax, half a row a thread: states 64 c .. 64 c + 63 of a tile.  With one thread a row (four
-    // warps a tile) a tile waited for 128 exponentials a thread one after the other: 8 x 1024 tokens over
-    // 4096 states 523 us, 365 without any exponential ---
+    // --- the softmax, half a row a thread: states 64 c .. 64 c + 63 of a tile.  Both threads of a row look
+    // for its largest logit in all of it, so that they agree without a word.  8 x 1024 tokens over 4096
+    // states, us: with one thread a row, whose 128 exponentials a tile waits for, 523 (without any exponential
+    // 365); with half a row each and a barrier of the two, 478 ---
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
     const int mine = steps[m], pair = 1 + 4 * m + (warp & 3);
-    const float f = p.scale2;
+    const float f = fabsf(p.scale2);              // (a negative scale is the product's: S = -Q K^T)
     float ref = kNoReference, l = 0.f;
     bool ok = true;
 #pragma unroll 1
     for (int i = 0; i < mine; ++i) {
       ok = role_wait(&sh.s[m], i & 1, &sh.abort, p.status);
+      if (!ok) break;
       fence_after();
       const int t = kSplit ? 2 * i + m : i;
-      const int upto = (t == n - 1 ? left : kStates) - 64 * c;
-      float x[64];
+      const int states = t == n - 1 ? left : kStates, upto = states - 64 * c;
+      float x[64], top = -INFINITY;
+      {
+        // the other half, for its largest logit alone
+        const uint32_t at = s_cols(m) + lanes + 64 * (1 - c);
+        const int other = states - 64 * (1 - c);
+        load64(at, x);
+        landed64(x);
+        if (other < 64) {
+#pragma unroll
+          for (int k = 0; k < 64; ++k)
+            if (k >= other) x[k] = -INFINITY;
+        }
+#pragma unroll
+        for (int k = 0; k < 64; k += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(x[k]), "f"(x[k + 1]));
+      }
       load64(s_cols(m) + lanes + 64 * c, x);
       landed64(x);
-      float2 s2[4] = {};
-#pragma unroll
-      for (int k = 0; k < 64; k += 2) {
-        const float2 y = ffma2(make_float2(x[k], x[k + 1]), make_float2(f, f), make_float2(-ref, -ref));
-        x[k] = exp2_fast(y.x);
-        x[k + 1] = exp2_fast(y.y);
-      }
       if (upto < 64) {
 #pragma unroll
         for (int k = 0; k < 64; ++k)
-          if (k >= upto) x[k] = 0.f;
+          if (k >= upto) x[k] = -INFINITY;
       }
 #pragma unroll
-      for (int k = 0; k < 64; k += 2) s2[(k / 2) & 3] = fadd2(s2[(k / 2) & 3], make_float2(x[k], x[k + 1]));
-      s2[0] = fadd2(fadd2(s2[0], s2[1]), fadd2(s2[2], s2[3]));
-      float sum = s2[0].x + s2[0].y, keep = 1.f;
-      if (pair_any(pair, !ok || !(sum <= 8192.f))) {
-        if (pair_any(pair, !ok)) {                // a wait gave up: both leave
-          ok = false;
-          break;
-        }
-        // The logits again, and the reference 6 below the row's largest; weights from rounded logits, as
-        // the reference is: past 2^26 it may lie many units off the unrounded ones.
-        load64(s_cols(m) + lanes + 64 * c, x);
-        landed64(x);
-        float top = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < 64; ++k) {
-          x[k] = k < upto ? __fmul_rn(x[k], f) : -INFINITY;
-          top = fmaxf(top, x[k]);
-        }
-        // (one half at a time: the other's word is read before its own is written)
-        if (c == 1) sh.half[m][rt] = top;
-        pair_sync(pair);
-        if (c == 0) {
-          top = fmaxf(top, sh.half[m][rt]);
-          sh.half[m][rt] = top;
-        }
-        pair_sync(pair);
-        top = sh.half[m][rt];
-        const float now = fmaxf(ref, top - 6.f);
+      for (int k = 0; k < 64; k += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(x[k]), "f"(x[k + 1]));
+      float keep = 1.f;
+      float2 s2[4] = {};
+      if (__any_sync(0xffffffffu, fmaf(top, f, -ref) > 13.f)) {
+        // The reference 6 below the row's largest, weights from rounded logits as the reference is: past
+        // 2^26 it may lie many units off the unrounded ones.
+        const float now = fmaxf(ref, __fmul_rn(top, f) - 6.f);
         keep = exp2f(ref - now);
         ref = now;
-        sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < 64; ++k) {
-          x[k] = exp2_fast(x[k] - ref);
-          sum += x[k];
+        for (int k = 0; k < 64; ++k) x[k] = __fsub_rn(__fmul_rn(x[k], f), ref);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 64; k += 2) {
+          const float2 y = ffma2(make_float2(x[k], x[k + 1]), make_float2(f, f), make_float2(-ref, -ref));
+          x[k] = y.x;
+          x[k + 1] = y.y;
         }
       }
+#pragma unroll
+      for (int k = 0; k < 64; k += 2) {
+        x[k] = exp2_fast(x[k]);
+        x[k + 1] = exp2_fast(x[k + 1]);
+        s2[(k / 2) & 3] = fadd2(s2[(k / 2) & 3], make_float2(x[k], x[k + 1]));
+      }
+      s2[0] = fadd2(fadd2(s2[0], s2[1]), fadd2(s2[2], s2[3]));
+      const float sum = s2[0].x + s2[0].y;
       l = l * keep + sum;
       if (i > 0 && __any_sync(0xffffffffu, keep != 1.f)) {       // (S's barrier has the products before it behind it)
 #pragma unroll 1

@@ -26,8 +26,16 @@ constexpr uint32_t kRows32 = (256 >> 4) | (1u << 14) | (6u << 29);
 
 // kind::f16, fp16 operands, fp32 accumulators, 128 rows, n columns
 __host__ __device__ constexpr uint32_t shape_of(int n) { return (1u << 4) | (uint32_t(n >> 3) << 17) | (uint32_t(128 >> 4) << 24); }
-// of a shape: bf16 operands; the second operand lies across
+// Of a shape: bf16 operands; the second operand lies across
 constexpr uint32_t kBf16 = 1u << 7 | 1u << 10, kAcross = 1u << 16;
+constexpr uint32_t kNegative = 1u << 13;          // the first operand's sign turned
+template <uint32_t kHigh>
+__device__ __forceinline__ void multiply(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(kHigh), "r"(shape),
+      "r"(add ? 1 : 0));
+}
 template <uint32_t kHigh, uint32_t kShape>
 __device__ __forceinline__ void multiply(uint32_t d, uint32_t a, uint32_t b, bool add) {
   asm volatile(
