@@ -816,6 +816,29 @@ int prefix_mt(const reskv_paged_kv* prefix, const reskv_paged_attn_args* a) {
   return a->n_tokens * (a->q.n_heads / prefix->n_kv_heads) > 128 * int64_t(prefix->batch) ? 2 : 1;
 }
 
+// SMs of the pass over the own tokens while the prefix has the others; 0: one after the other, with all.  By
+// the times of both (us) with n SMs, as measured, for the tables' room; what is fixed of them is most of it
+// where a prefix has some thousand positions: 64 sequences of 512 behind 8192 67 -> 54 us.
+int own_sms(const reskv_paged_kv* kv, const reskv_paged_kv* prefix, const reskv_paged_attn_args* a, int sms) {
+  const double rows = double(a->n_tokens) * (a->q.n_heads / kv->n_kv_heads);
+  const double tiles = double(kv->table_pages) * kv->page_tokens / kTile * kv->n_kv_heads * kv->batch * std::ceil(rows / kv->batch / 8.0);
+  const double block = 128.0 * prefix_mt(prefix, a);
+  const double steps = double(prefix->table_pages) * prefix->page_tokens / kBlockPos * kv->n_kv_heads * prefix->batch *
+                       std::ceil(rows / prefix->batch / block);
+  auto own = [&](int n) { return 9.0 + 0.07 * tiles / n; };
+  auto other = [&](int n) { return 18.0 + 1.5 * steps / n; };
+  double best = own(sms) + other(sms) - 3.0;
+  int best_n = 0;
+  for (int n = 8; n + 8 <= sms; n += 8) {
+    const double t = own(n) > other(sms - n) ? own(n) : other(sms - n);
+    if (t < best) {
+      best = t;
+      best_n = n;
+    }
+  }
+  return best_n;
+}
+
 struct SharedLayout {             // of the workspace, in bytes from its start
   size_t own, own_ref, prefix, prefix_ref, plans, bytes;
 };
@@ -834,10 +857,11 @@ SharedLayout shared_layout(const reskv_paged_kv* kv, const reskv_paged_kv* prefi
   size_t held = rows;
   if (prefix_in_blocks(prefix, a)) {
     const int block = 128 * prefix_mt(prefix, a);
-    held = size_t(group_items(a->n_tokens * (a->q.n_heads / kv->n_kv_heads), prefix->batch, kv->n_kv_heads, block, sms)) * block;
+    // rows of records: 128 or 256 of two streams or blocks an item
+    held = size_t(group_items(a->n_tokens * (a->q.n_heads / kv->n_kv_heads), prefix->batch, kv->n_kv_heads, block, sms)) * 256;
   }
   l.prefix_ref = l.prefix + padded(held * kv->head_dim * 4);
-  l.plans = l.prefix_ref + padded(held * 4);
+  l.plans = l.prefix_ref + padded(held * 8);
   l.bytes = l.plans + padded(size_t(prefix->batch) * sizeof(GroupPlan));
   return l;
 }
@@ -909,7 +933,8 @@ extern "C" reskv_status reskv_paged_attn_shared(const reskv_paged_kv* kv, const 
     g.prefix_ref = reinterpret_cast<float*>(ws + l.prefix_ref);
     const bool blocks = prefix_in_blocks(prefix, a), fused = !blocks && one_launch(kv, prefix, a);
     const int mt = prefix_mt(prefix, a);
-    const int items = blocks ? int(group_items(p.n_tokens * p.group, prefix->batch, p.kv_heads, 128 * mt, sms)) : 0;
+    const int apart = blocks && !takes_blocks(kv, a) ? own_sms(kv, prefix, a, sms) : 0;
+    const int items = blocks ? int(group_items(p.n_tokens * p.group, prefix->batch, p.kv_heads, 128 * mt, sms - apart)) : 0;
     GroupPlan* plans = reinterpret_cast<GroupPlan*>(ws + l.plans);
     if (fused) {
       g.batch = kv->batch + prefix->batch;
@@ -919,12 +944,12 @@ extern "C" reskv_status reskv_paged_attn_shared(const reskv_paged_kv* kv, const 
                 : dispatch_rows<true, 8, true>(g, kv->head_dim, kv->quant_group, dev, ctas, s);
     } else {
       err = takes_blocks(kv, a) ? launch_attn_blocks(p, block_plan(kv, a, sms), kv->head_dim, kv->quant_group, dev, p.partials, s)
-                                : attn_rows(p, kv, one, dev, sms, s);
+                                : attn_rows(p, kv, one, dev, apart ? apart : sms, s);
     }
     g.batch = prefix->batch;
     g.own = 0;
     if (err == cudaSuccess && blocks)
-      err = launch_attn_groups(g, mt, items, sms, kv->head_dim, kv->quant_group, dev, g.prefix_o, plans, s);
+      err = launch_attn_groups(g, mt, items, sms - apart, kv->head_dim, kv->quant_group, dev, g.prefix_o, plans, s);
     if (err == cudaSuccess && !blocks && !fused) {
       const int ctas = sms < kMaxCtas ? sms : kMaxCtas;
       err = one ? dispatch_rows<false, 8, true>(g, kv->head_dim, kv->quant_group, dev, ctas, s)

@@ -50,8 +50,8 @@ constexpr int kLeastBelow = 60, kLeastExponent = 41;
 struct PrefixParams {
   AttnParams a;
   GroupPlan* plans;
-  float* records;                                 // [item][rows][D]
-  float* sums;                                    // [item][rows]: log2 sums
+  float* records;                                 // [record][rows][D]: outputs times their sum; kSplit: two an item
+  float2* sums;                                   // [record][rows]: reference (log2) and sum; -inf: nothing seen
   int32_t ctas;
 };
 
@@ -65,9 +65,8 @@ struct PrefixSmem {
   static constexpr int slot = k + v + k_more;                         // K, V^T, the keys' minima
   static constexpr int raw = 8 * kMostPacked;                         // packed rows of a tile
   static constexpr int at_raw = at_slots + slots * slot, all = at_raw + kAhead * raw;
-  static constexpr int at_ref = 2 * 128 * D * 4;                      // of rows to be joined: outputs, references, sums
   static constexpr int bytes = all + 1024;
-  static_assert(at_ref + 2 * 256 * 4 <= all && slot % 1024 == 0 && at_slots % 1024 == 0, "shared memory");
+  static_assert(2 * 128 * D * 4 <= all && slot % 1024 == 0 && at_slots % 1024 == 0, "shared memory");
 };
 struct PrefixShared {
   uint64_t q, ready[4], free[4], s[2][2], p[2][2], pv[2], done;
@@ -263,28 +262,38 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_prefix(const __grid_consta
       const uint8_t* src = smem + S::at_raw + (i % kAhead) * S::raw + uw * kMostPacked;
       const int left = (there >> (i & 7)) & 1 ? plan.len - ((first + i) * kSub + sub) * kTile : 0;       // rows that exist
       uint8_t* at = smem + S::at_slots + slot * S::slot;
+      // the row's exponent, found by lane row, and what the softmax takes of it
+      int mine = 15;
+      if (lane < kTile && lane < left) {
+        uint32_t meta[NG];
+        load_words<NG>(meta, src + ts.codes() + lane * 4 * NG);
+        mine = top_exponent<NG>(meta);
+      }
       if (!values) {
+        if (lane < kTile) sh.up[slot][sub * kTile + lane] = up(mine);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int row = g + 8 * j, tk = sub * kTile + row;
           uint32_t words[C] = {}, meta[NG] = {};
           if (row < left) {
             load_words<C>(words, src + row * (D / 2) + t4 * (D / 8));
-            load_words<NG>(meta, src + ts.k_meta() + row * 4 * NG);
+            load_words<NG>(meta, src + ts.codes() + row * 4 * NG);
           }
-          const int e = top_exponent<NG>(meta);
-          const float f = down(e);
+          const float f = down(__shfl_sync(0xffffffffu, mine, row));
 #pragma unroll
-          for (int c = 0; c < C; ++c) {
+          for (int k = 0; k < NG; ++k) {
             float s, m;
-            group_meta<NG>(meta, c / PG, s, m);
+            group_meta<NG>(meta, k, s, m);
             const __half2 s2 = __float2half2_rn(s * f);
-            const uint32_t w = words[c];
-            // dims 0, 4, 1, 5, 2, 6, 3, 7 of the word's eight
-            const uint4 v = make_uint4(bits(__hmul2(even_codes(w, 8.f), s2)), bits(__hmul2(odd_codes(w, 8.f), s2)),
-                                       bits(__hmul2(even_codes(w >> 8, 8.f), s2)), bits(__hmul2(odd_codes(w >> 8, 8.f), s2)));
-            const int word = 4 * c + t4;
-            *reinterpret_cast<uint4*>(at + (word >> 3) * (kPos * 128) + tk * 128 + (((word & 7) ^ (tk & 7)) << 4)) = v;
+#pragma unroll
+            for (int c = k * PG; c < (k + 1) * PG; ++c) {
+              const uint32_t w = words[c];
+              // dims 0, 4, 1, 5, 2, 6, 3, 7 of the word's eight
+              const uint4 v = make_uint4(bits(__hmul2(even_codes(w, 8.f), s2)), bits(__hmul2(odd_codes(w, 8.f), s2)),
+                                         bits(__hmul2(even_codes(w >> 8, 8.f), s2)), bits(__hmul2(odd_codes(w >> 8, 8.f), s2)));
+              const int word = 4 * c + t4;
+              *reinterpret_cast<uint4*>(at + (word >> 3) * (kPos * 128) + tk * 128 + (((word & 7) ^ (tk & 7)) << 4)) = v;
+            }
           }
           // the groups' m + 8 s: first planes (t4 = 0), second planes (1), first again (2), nothing (3)
           float plane[4] = {0.f, 0.f, 0.f, 0.f};
@@ -297,50 +306,42 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_prefix(const __grid_consta
           }
           *reinterpret_cast<uint2*>(at + S::k + S::v + tk * 32 + (((t4 >> 1) ^ ((tk >> 2) & 1)) << 4) + (t4 & 1) * 8) =
               make_uint2(pack_f16(plane[0], plane[1]), pack_f16(plane[2], plane[3]));
-          if (t4 == 0) sh.up[slot][tk] = up(e);
         }
       } else {
-        constexpr int kCodes = 0, kMeta = ts.codes();        // of V alone
-        uint32_t words[2][C] = {}, metas[4][NG] = {};
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int pair = t4 + 4 * j;
-          if (2 * pair < left) load_words<C>(words[j], src + kCodes + pair * D + ts.v_place(pair, g) * (D / 8));
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            if (2 * pair + e < left) load_words<NG>(metas[2 * j + e], src + kMeta + (2 * pair + e) * 4 * NG);
+        most = max(most, int(__reduce_max_sync(0xffffffffu, uint32_t(mine))));
+        mine = max(mine, max(most - kLeastBelow, kLeastExponent));
+        if (lane < kTile) {
+          sh.c[slot][sub * kTile + lane] = lane < left ? float(mine - 141) : -INFINITY;
+          sh.inv[slot][sub * kTile + lane] = down(mine);
         }
-        int e[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) e[j] = top_exponent<NG>(metas[j]);
-        most = max(most, int(__reduce_max_sync(0xffffffffu, uint32_t(max(max(e[0], e[1]), max(e[2], e[3]))))));
-        const int least = max(most - kLeastBelow, kLeastExponent);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const int tk = sub * kTile + 2 * (t4 + 4 * j);
-          const int ea = max(e[2 * j], least), eb = max(e[2 * j + 1], least);
-          const float fa = down(ea), fb = down(eb);
-#pragma unroll
-          for (int c = 0; c < C; ++c) {
-            float sa, ma, sb, mb;
-            group_meta<NG>(metas[2 * j], c / PG, sa, ma);
-            group_meta<NG>(metas[2 * j + 1], c / PG, sb, mb);
-            const __half2 s2 = __floats2half2_rn(sa * fa, sb * fb), m2 = __floats2half2_rn(ma * fa, mb * fb);
-            const uint32_t w = words[j][c];
-            const __half2 v[4] = {__hfma2(even_codes(w, 0.f), s2, m2), __hfma2(odd_codes(w, 0.f), s2, m2),
-                                  __hfma2(even_codes(w >> 8, 0.f), s2, m2), __hfma2(odd_codes(w >> 8, 0.f), s2, m2)};
-            // dim 32c + 4g + i in row 32c + 8i + g: lanes of one store in eight rows, as many 16-byte words
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int row = 32 * c + 8 * i + g;
-              *reinterpret_cast<uint32_t*>(at + S::k + row * 128 + (((tk >> 3) ^ (row & 7)) << 4) + (tk & 7) * 2) = bits(v[i]);
-            }
+          const int pair = t4 + 4 * j, tk = sub * kTile + 2 * pair;
+          uint32_t words[C] = {}, meta0[NG] = {}, meta1[NG] = {};
+          if (2 * pair < left) {
+            load_words<C>(words, src + pair * D + ts.v_place(pair, g) * (D / 8));
+            load_words<NG>(meta0, src + ts.codes() + 2 * pair * 4 * NG);
           }
-          if (g == 0) {
-            sh.c[slot][tk] = 2 * (t4 + 4 * j) < left ? float(ea - 141) : -INFINITY;
-            sh.c[slot][tk + 1] = 2 * (t4 + 4 * j) + 1 < left ? float(eb - 141) : -INFINITY;
-            sh.inv[slot][tk] = fa;
-            sh.inv[slot][tk + 1] = fb;
+          if (2 * pair + 1 < left) load_words<NG>(meta1, src + ts.codes() + (2 * pair + 1) * 4 * NG);
+          const float fa = down(__shfl_sync(0xffffffffu, mine, 2 * pair)), fb = down(__shfl_sync(0xffffffffu, mine, 2 * pair + 1));
+#pragma unroll
+          for (int k = 0; k < NG; ++k) {
+            float sa, ma, sb, mb;
+            group_meta<NG>(meta0, k, sa, ma);
+            group_meta<NG>(meta1, k, sb, mb);
+            const __half2 s2 = __floats2half2_rn(sa * fa, sb * fb), m2 = __floats2half2_rn(ma * fa, mb * fb);
+#pragma unroll
+            for (int c = k * PG; c < (k + 1) * PG; ++c) {
+              const uint32_t w = words[c];
+              const __half2 v[4] = {__hfma2(even_codes(w, 0.f), s2, m2), __hfma2(odd_codes(w, 0.f), s2, m2),
+                                    __hfma2(even_codes(w >> 8, 0.f), s2, m2), __hfma2(odd_codes(w >> 8, 0.f), s2, m2)};
+              // dim 32c + 4g + i in row 32c + 8i + g: lanes of one store in eight rows, as many 16-byte words
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int row = 32 * c + 8 * i + g;
+                *reinterpret_cast<uint32_t*>(at + S::k + row * 128 + (((tk >> 3) ^ (row & 7)) << 4) + (tk & 7) * 2) = bits(v[i]);
+              }
+            }
           }
         }
       }
@@ -372,63 +373,68 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_prefix(const __grid_consta
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
     float cq;
     {
-      // the row's query, scaled below 2^8 (128 of them sum up within fp16), in the order of the keys' dims
-      uint32_t w[D / 2];                          // two neighbouring dims a word
-#pragma unroll
-      for (int k = 0; k < D / 2; ++k) w[k] = 0u;
-      if (real) {
-        const uint16_t* src = static_cast<const uint16_t*>(p.q) + (plan.q0 + r / p.group) * p.q_token +
-                              int64_t(h * p.group + r % p.group) * p.q_head;
-        if (p.q_wide) {
-#pragma unroll
-          for (int k = 0; k < D / 8; ++k) {
-            const uint4 v = reinterpret_cast<const uint4*>(src)[k];
-            w[4 * k] = v.x;
-            w[4 * k + 1] = v.y;
-            w[4 * k + 2] = v.z;
-            w[4 * k + 3] = v.w;
-          }
-        } else {
-#pragma unroll
-          for (int k = 0; k < D / 2; ++k) w[k] = src[2 * k] | uint32_t(src[2 * k + 1]) << 16;
+      // The row's query, scaled below 2^8 (128 of them sum up within fp16), in the order of the keys' dims.
+      // In short loops, as all code that runs once here is: straight on, every 128 bytes of it are waited for.
+      const uint16_t* src = static_cast<const uint16_t*>(p.q) +
+                            (real ? (plan.q0 + r / p.group) * p.q_token + int64_t(h * p.group + r % p.group) * p.q_head : 0);
+      auto eight = [&](int k, float (&x)[8]) {    // dims 8k .. 8k + 7
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (real && p.q_wide) {
+          v = reinterpret_cast<const uint4*>(src)[k];
+        } else if (real) {
+          const uint16_t* e = src + 8 * k;
+          v = make_uint4(e[0] | uint32_t(e[1]) << 16, e[2] | uint32_t(e[3]) << 16, e[4] | uint32_t(e[5]) << 16, e[6] | uint32_t(e[7]) << 16);
         }
-      }
-      auto two = [&](int k) { return p.q_f16 ? __half22float2(*reinterpret_cast<const __half2*>(&w[k])) : bf16x2_to_float2(w[k]); };
-      float top = 0.f;
-#pragma unroll
-      for (int k = 0; k < D / 2; ++k) top = fmaxf(top, fmaxf(fabsf(two(k).x), fabsf(two(k).y)));
-      const int e = 134 - min(max(__float_as_int(top) >> 23, 1), 254), e1 = e >> 1, e2 = e - e1;
-      const float f1 = __int_as_float((127 + e1) << 23), f2 = __int_as_float((127 + e2) << 23);
-      float sums[4] = {0.f, 0.f, 0.f, 0.f}, left[4];
-#pragma unroll
-      for (int k = 0; k < D / 8; ++k) {
-        const float2 v0 = two(4 * k), v1 = two(4 * k + 1), v2 = two(4 * k + 2), v3 = two(4 * k + 3);
-        // dims 0, 4, 1, 5, 2, 6, 3, 7 of eight
-        const uint32_t held[4] = {pack_f16(v0.x * f1 * f2, v2.x * f1 * f2), pack_f16(v0.y * f1 * f2, v2.y * f1 * f2),
-                                  pack_f16(v1.x * f1 * f2, v3.x * f1 * f2), pack_f16(v1.y * f1 * f2, v3.y * f1 * f2)};
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&held[j]));
-          sums[k / (D / 8 / NG)] += x.x + x.y;
+          const float2 f = p.q_f16 ? __half22float2(*reinterpret_cast<const __half2*>(&w[j])) : bf16x2_to_float2(w[j]);
+          x[2 * j] = f.x;
+          x[2 * j + 1] = f.y;
         }
-        if (!kSplit || m == 0)                    // (two streams have one block of rows)
-          *reinterpret_cast<uint4*>(smem + m * S::q + (k >> 3) * kHalf + rt * 128 + (((k & 7) ^ (rt & 7)) << 4)) =
-              make_uint4(held[0], held[1], held[2], held[3]);
-      }
-      // against the keys' planes: first planes twice, then what they left over
+      };
+      float top = 0.f;
+#pragma unroll 2
+      for (int k = 0; k < D / 8; ++k) {
+        float x[8];
+        eight(k, x);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        left[k] = sums[k];
-        sums[k] = __half2float(__float2half_rn(sums[k]));
-        left[k] -= sums[k];
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[j]));
       }
-      const uint2 top_planes = make_uint2(pack_f16(sums[0], sums[1]), pack_f16(sums[2], sums[3]));
-      const uint2 low_planes = make_uint2(pack_f16(left[0], left[1]), pack_f16(left[2], left[3]));
-      if (!kSplit || m == 0) {
-        uint8_t* more = smem + S::at_q_more + m * S::q_more + rt * 32;
-        const int turn_word = ((rt >> 2) & 1) << 4;
-        *reinterpret_cast<uint4*>(more + turn_word) = make_uint4(top_planes.x, top_planes.y, top_planes.x, top_planes.y);
-        *reinterpret_cast<uint4*>(more + (16 ^ turn_word)) = make_uint4(low_planes.x, low_planes.y, 0u, 0u);
+      const int e = 134 - min(max(__float_as_int(top) >> 23, 1), 254), e1 = e >> 1, e2 = e - e1;
+      const float f1 = __int_as_float((127 + e1) << 23), f2 = __int_as_float((127 + e2) << 23);
+      uint8_t* const row = smem + m * S::q + rt * 128;
+      uint8_t* const more = smem + S::at_q_more + m * S::q_more + rt * 32;
+      const bool mine = !kSplit || m == 0;        // (two streams have one block of rows)
+      const int turn_word = ((rt >> 2) & 1) << 4;
+      if (mine) {
+        *reinterpret_cast<uint4*>(more) = make_uint4(0u, 0u, 0u, 0u);
+        *reinterpret_cast<uint4*>(more + 16) = make_uint4(0u, 0u, 0u, 0u);
+      }
+#pragma unroll 1
+      for (int n0 = 0; n0 < NG; ++n0) {
+        float sum = 0.f;
+#pragma unroll 2
+        for (int k = n0 * (D / 8 / NG); k < (n0 + 1) * (D / 8 / NG); ++k) {
+          float x[8];
+          eight(k, x);
+          uint32_t held[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {           // dims 0, 4, 1, 5, 2, 6, 3, 7 of eight
+            held[j] = pack_f16(x[j] * f1 * f2, x[4 + j] * f1 * f2);
+            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&held[j]));
+            sum += y.x + y.y;
+          }
+          if (mine) *reinterpret_cast<uint4*>(row + (k >> 3) * kHalf + (((k & 7) ^ (rt & 7)) << 4)) = make_uint4(held[0], held[1], held[2], held[3]);
+        }
+        // against the keys' planes: first planes twice, then what they left over
+        const __half first_plane = __float2half_rn(sum), rest = __float2half_rn(sum - __half2float(first_plane));
+        if (mine) {
+          __half* at = reinterpret_cast<__half*>(more);
+          at[turn_word / 2 + n0] = first_plane;
+          at[turn_word / 2 + 4 + n0] = first_plane;
+          at[(16 ^ turn_word) / 2 + n0] = rest;
+        }
       }
       cq = p.scale2 * __int_as_float((127 - e1) << 23) * __int_as_float((127 - e2) << 23);
       fence_proxy_async_smem();
@@ -444,55 +450,43 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_prefix(const __grid_consta
       fence_after();
       const int slot = (kSplit ? 2 * i + m : i) % S::slots;
       float x[kPos];
-      auto logits = [&]() {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) load16(s_cols(m, i) + lanes + 16 * k, x + 16 * k);
-        landed();
-#pragma unroll
-        for (int k = 0; k < 4; ++k) defined16(x + 16 * k);
-      };
+      load64(s_cols(m, i) + lanes, x);
+      landed64(x);
       const float4* up4 = reinterpret_cast<const float4*>(sh.up[slot]);
       const float4* c4 = reinterpret_cast<const float4*>(sh.c[slot]);
       const float4* inv4 = reinterpret_cast<const float4*>(sh.inv[slot]);
-      logits();
-      // weights (times the values' scale) in place, their sum and that of the weights alone
-      float2 w2 = make_float2(0.f, 0.f), l2 = w2;
+      // logits with the values' scale, the largest, then weights in place and the sum of the weights alone
+      float top = -INFINITY;
 #pragma unroll
       for (int k = 0; k < kPos; k += 4) {
-        const float4 u = up4[k / 4], c = c4[k / 4], v = inv4[k / 4];
-        const float2 a = ffma2(make_float2(x[k], x[k + 1]), fmul2(make_float2(u.x, u.y), make_float2(cq, cq)),
-                               fadd2(make_float2(c.x, c.y), make_float2(-ref, -ref)));
-        const float2 b = ffma2(make_float2(x[k + 2], x[k + 3]), fmul2(make_float2(u.z, u.w), make_float2(cq, cq)),
-                               fadd2(make_float2(c.z, c.w), make_float2(-ref, -ref)));
+        const float4 u = up4[k / 4], c = c4[k / 4];
+        const float2 a = ffma2(make_float2(x[k], x[k + 1]), fmul2(make_float2(u.x, u.y), make_float2(cq, cq)), make_float2(c.x, c.y));
+        const float2 b = ffma2(make_float2(x[k + 2], x[k + 3]), fmul2(make_float2(u.z, u.w), make_float2(cq, cq)), make_float2(c.z, c.w));
+        x[k] = a.x;
+        x[k + 1] = a.y;
+        x[k + 2] = b.x;
+        x[k + 3] = b.y;
+        asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(a.x), "f"(a.y));
+        asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(b.x), "f"(b.y));
+      }
+      float keep = 1.f;
+      if (__any_sync(0xffffffffu, top - ref > 13.f)) {
+        const float now = fmaxf(ref, top - 6.f);
+        keep = exp2f(ref - now);
+        ref = now;
+      }
+      float2 l2 = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kPos; k += 4) {
+        const float4 v = inv4[k / 4];
+        const float2 a = fadd2(make_float2(x[k], x[k + 1]), make_float2(-ref, -ref));
+        const float2 b = fadd2(make_float2(x[k + 2], x[k + 3]), make_float2(-ref, -ref));
         x[k] = exp2_fast(a.x);
         x[k + 1] = exp2_fast(a.y);
         x[k + 2] = exp2_fast(b.x);
         x[k + 3] = exp2_fast(b.y);
-        w2 = fadd2(w2, fadd2(make_float2(x[k], x[k + 1]), make_float2(x[k + 2], x[k + 3])));
         l2 = ffma2(make_float2(x[k], x[k + 1]), make_float2(v.x, v.y), l2);
         l2 = ffma2(make_float2(x[k + 2], x[k + 3]), make_float2(v.z, v.w), l2);
-      }
-      float keep = 1.f;
-      const float sum = w2.x + w2.y;
-      if (__any_sync(0xffffffffu, !(sum <= 16384.f))) {
-        // The logits again, and the reference 6 below the largest; from rounded logits, as the
-        // reference is: past 2^26 it may lie many units off the unrounded ones.
-        logits();
-        float top = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < kPos; ++k) {
-          x[k] = __fadd_rn(__fmul_rn(x[k], sh.up[slot][k] * cq), sh.c[slot][k]);
-          top = fmaxf(top, x[k]);
-        }
-        const float now = sum <= 16384.f ? ref : fmaxf(ref, top - 6.f);
-        keep = exp2f(ref - now);
-        ref = now;
-        l2 = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < kPos; ++k) {
-          x[k] = exp2_fast(min_nan(x[k] - ref, 15.5f));
-          l2.x = fmaf(x[k], sh.inv[slot][k], l2.x);
-        }
       }
       l = l * keep + (l2.x + l2.y);
       if (i > 0 && __any_sync(0xffffffffu, keep != 1.f)) {
@@ -521,9 +515,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_prefix(const __grid_consta
     if (ok) ok = role_wait(&sh.done, 0, &sh.abort, p.status);
     fence_after();
     asm volatile("bar.sync 1, 256;" ::: "memory");        // all products are done: their operands' memory is free
+    // --- the records: outputs as they are, each row's reference and sum.  Through shared memory (word u of row
+    // r at u ^ r, on banks of their own), so that a warp writes whole rows ---
     const bool seen = mine > 0 && ok && (ref != kNoRef || l != 0.f);
-    float4* out = reinterpret_cast<float4*>(smem) + (m * 128 + rt) * (D / 4);
-    float* refs = reinterpret_cast<float*>(smem + S::at_ref);
+    const int64_t slot = (kSplit ? 2 * int64_t(blockIdx.x) : int64_t(blockIdx.x)) * kRows;       // (a record a stream)
+    if ((kSplit ? rt : m * 128 + rt) < rows) pp.sums[slot + m * 128 + rt] = make_float2(seen ? ref : -INFINITY, l);
+    float4* held = reinterpret_cast<float4*>(smem) + (m * 128 + (warp & 3) * 32) * (D / 4);      // the warp's 32 rows
+    const int there = min(max((kSplit ? rows : rows - m * 128) - (warp & 3) * 32, 0), 32);
     if (mine > 0 && ok) {
 #pragma unroll 1
       for (int c = 0; c < C; ++c) {
@@ -533,33 +531,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_prefix(const __grid_consta
         landed();
         defined16(o);
         defined16(o + 16);
-        // dims 4k .. 4k + 3 of the 32 came as columns k, 8 + k, ..; word u of row r at u ^ r, on banks of their own
+        // dims 4k .. 4k + 3 of the 32 came as columns k, 8 + k, ..
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          out[(8 * c + k) ^ (rt & (D / 4 - 1))] = make_float4(o[k], o[8 + k], o[16 + k], o[24 + k]);
+          held[lane * (D / 4) + ((8 * c + k) ^ (lane & (D / 4 - 1)))] = make_float4(o[k], o[8 + k], o[16 + k], o[24 + k]);
       }
-    }
-    refs[m * 128 + rt] = seen ? ref : -INFINITY;
-    refs[256 + m * 128 + rt] = seen ? l : 0.f;
-    asm volatile("bar.sync 1, 256;" ::: "memory");
-    // --- the record: a row a warp, of one stream or of two joined ---
-    const int64_t slot = int64_t(blockIdx.x) * kRows;
-    const float4* held = reinterpret_cast<const float4*>(smem);
-#pragma unroll 2
-    for (int i = warp; i < rows; i += 8) {
-      const float a = refs[i], b = kSplit ? refs[128 + i] : -INFINITY, top = fmaxf(a, b);
-      const float wa = a == -INFINITY ? 0.f : exp2f(a - top), wb = b == -INFINITY ? 0.f : exp2f(b - top);
-      const float total = (a == -INFINITY ? 0.f : wa * refs[256 + i]) + (b == -INFINITY ? 0.f : wb * refs[256 + 128 + i]);
-      const bool any = a != -INFINITY || b != -INFINITY;
-      const float inv = any ? 1.f / total : 0.f;
-      if (lane < D / 4) {
-        const int u = lane ^ (i & (D / 4 - 1));
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (a != -INFINITY) add_scaled(v, wa * inv, held[i * (D / 4) + u]);
-        if (kSplit && b != -INFINITY) add_scaled(v, wb * inv, held[(128 + i) * (D / 4) + u]);
-        reinterpret_cast<float4*>(pp.records + (slot + i) * D)[lane] = v;
+      __syncwarp();
+      float4* out = reinterpret_cast<float4*>(pp.records + (slot + m * 128 + (warp & 3) * 32) * D);
+#pragma unroll 4
+      for (int i = lane; i < there * (D / 4); i += 32) {
+        const int r1 = i / (D / 4), u = i % (D / 4);
+        out[i] = held[r1 * (D / 4) + (u ^ (r1 & (D / 4 - 1)))];
       }
-      if (lane == 0) pp.sums[slot + i] = any ? top + log2f(total) : -INFINITY;
     }
   }
   fence_before();
@@ -605,7 +588,7 @@ cudaError_t launch_attn_groups(const AttnParams& p, int mt, int items, int ctas,
   pp.a.table_pages = p.prefix_pages;
   pp.plans = plans;
   pp.records = records;
-  pp.sums = p.prefix_ref;
+  pp.sums = reinterpret_cast<float2*>(p.prefix_ref);
   pp.ctas = ctas;
   return mt == 1 ? dispatch<true>(pp, items, d, quant_group, dev, s) : dispatch<false>(pp, items, d, quant_group, dev, s);
 }

@@ -2,8 +2,9 @@
 //
 // The passes leave, for every query row, the softmax's output over what they saw and the
 // log2 sum of its weights: the own tokens' in one row, the prefix's in one row or, where
-// it was taken in blocks of rows, in one record for each part of its positions.
-// With sums s_k and outputs o_k the output is sum 2^(s_k - S) o_k, S = log2 sum 2^s_k.
+// it was taken in blocks of rows, in one record for each part of its positions, not yet
+// divided by its sum.  With references s_k, sums l_k and outputs l_k o_k (1 and o_k of a whole
+// row) the output is sum 2^(s_k - S) l_k o_k, S = log2 sum 2^s_k l_k.
 // A warp a row; bound by its reads (fp32 rows that the passes left in L2).
 #include "paged_attn.cuh"
 
@@ -48,9 +49,12 @@ __global__ void __launch_bounds__(kWarps * 32) k_shared_join(const __grid_consta
     const int64_t r = (tok - g.q0) * p.group + head % p.group;
     // (of a seq_begin out of order there may be more items than CTAs and records)
     if (tok >= g.q0 && tok < g.q0 + g.count && g.first + int64_t(g.parts) * g.row_blocks * p.kv_heads <= j.items) {
-      parts = g.parts;
+      // item i has records i, or (streams) 2 i and 2 i + 1
+      const int streams = j.block_rows == 128 ? 2 : 1;
+      const int64_t block = r / j.block_rows;
+      parts = g.parts * streams;
       stride = int64_t(g.row_blocks) * j.block_rows;
-      first = (g.first + int64_t(head / p.group) * parts * g.row_blocks) * j.block_rows + r;
+      first = (g.first + int64_t(head / p.group) * g.parts * g.row_blocks + block) * streams * j.block_rows + r % j.block_rows;
     }
   } else if (group >= 0) {
     const Sequence s = group_of(p, group, j.groups);
@@ -59,13 +63,25 @@ __global__ void __launch_bounds__(kWarps * 32) k_shared_join(const __grid_consta
       first = row;
     }
   }
-  // 32 parts at a time, their sums in the lanes; a part of weight 0 still counts: a NaN in it is seen
+  // Record k of a row: of part k, or (streams) of part k / 2.
+  auto at = [&](int k) {
+    return j.plans && j.block_rows == 128 ? first + (k >> 1) * 2 * stride + (k & 1) * 128 : first + k * stride;
+  };
+  // 32 records at a time, their references and sums in the lanes; one of weight 0 still counts: a NaN in it is seen
   float top = own, sum = with_own ? 1.f : 0.f;
 #pragma unroll 1
   for (int k0 = 0; k0 < parts; k0 += 32) {
     const int n = min(32, parts - k0);
-    const float ref = lane < n ? j.prefix_ref[first + (k0 + lane) * stride] : -INFINITY;
-    const float* rows = j.prefix + (first + k0 * stride) * D;
+    float ref = -INFINITY, l = 1.f;
+    if (lane < n) {
+      if (j.plans) {
+        const float2 s = reinterpret_cast<const float2*>(j.prefix_ref)[at(k0 + lane)];
+        ref = s.x;
+        l = s.y;
+      } else {
+        ref = j.prefix_ref[first];
+      }
+    }
     float now = ref;
 #pragma unroll
     for (int o = 16; o; o /= 2) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, o));
@@ -73,7 +89,7 @@ __global__ void __launch_bounds__(kWarps * 32) k_shared_join(const __grid_consta
     const uint32_t present = __ballot_sync(0xffffffffu, ref != -INFINITY);
     if (!present) continue;
     const float keep = top == -INFINITY ? 0.f : exp2f(top - now), f = ref == -INFINITY ? 0.f : exp2f(ref - now);
-    float more = f;
+    float more = ref == -INFINITY ? 0.f : f * l;
 #pragma unroll
     for (int o = 16; o; o /= 2) more += __shfl_xor_sync(0xffffffffu, more, o);
     sum = top == -INFINITY ? more : fmaf(sum, keep, more);
@@ -82,18 +98,18 @@ __global__ void __launch_bounds__(kWarps * 32) k_shared_join(const __grid_consta
 #pragma unroll 8
     for (int k = 0; k < n; ++k) {
       const float w = __shfl_sync(0xffffffffu, f, k);
-      const float4 v = (present >> k) & 1 ? reinterpret_cast<const float4*>(rows + k * stride * D)[u] : zero;
+      const float4 v = (present >> k) & 1 ? reinterpret_cast<const float4*>(j.prefix + at(k0 + k) * D)[u] : zero;
       add_scaled(a, w, v);
     }
   }
   const bool seen = sum != 0.f;
   const float inv = seen ? 1.f / sum : 0.f;
-  Sequence at{};
-  at.q0 = int(tok);
-  at.count = 1;
+  Sequence self{};
+  self.q0 = int(tok);
+  self.count = 1;
   const int h = head / p.group, r = head % p.group;
-  if (lane < D / 4) store_out(p, at, h, r, lane, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
-  if (lane == 0) store_lse(p, at, h, r, seen ? top + log2f(sum) : -INFINITY);
+  if (lane < D / 4) store_out(p, self, h, r, lane, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+  if (lane == 0) store_lse(p, self, h, r, seen ? top + log2f(sum) : -INFINITY);
 }
 
 }  // namespace
