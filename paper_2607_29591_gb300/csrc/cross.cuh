@@ -172,7 +172,7 @@ inline int cross_tile_tokens(int group) { return 128 / group; }
 constexpr int kRowStates = 64;
 cudaError_t launch_cross_rows(const CrossParams& p, const CrossMaps& maps, int d, int dev, int sms, cudaStream_t s);
 cudaError_t launch_cross_grad(const CrossParams& p, const CrossMaps& maps, int d, int dev, cudaStream_t s);      // cross_grad.cu
-cudaError_t launch_cross_blocks(const CrossParams& p, const CrossMaps& maps, int d, int dev, int sms, cudaStream_t s);
+cudaError_t launch_cross_blocks(const CrossParams& p, const CrossMaps& maps, int d, int dev, cudaStream_t s);
 
 // Rows of any alignment; cross_general.cu.
 cudaError_t launch_cross_general(const CrossParams& p, int d, cudaStream_t s);

@@ -100,7 +100,7 @@ extern "C" reskv_status reskv_cross_attn(const reskv_cross_attn_args* a, void* s
     const bool fast = rows_aligned(a->q, 16) && rows_aligned(a->o, 16) && encode_maps(&maps, a, p, few ? kRowStates : 128);
     return launch_result(!fast ? launch_cross_general(p, a->head_dim, s)
                          : few ? launch_cross_rows(p, maps, a->head_dim, dev, sms, s)
-                               : launch_cross_blocks(p, maps, a->head_dim, dev, sms, s),
+                               : launch_cross_blocks(p, maps, a->head_dim, dev, s),
                          "cross attention");
   });
 }

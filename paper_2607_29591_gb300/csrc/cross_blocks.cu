@@ -452,17 +452,49 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
   if (cs > 1) sync_cluster();                     // nobody leaves while its rows are read
 }
 
+// Clusters of `size` CTAs that run side by side; asked once a device.
 template <int D, bool kF16, bool kSplit>
-cudaError_t launch(const BlocksParams& bp, int64_t items, int dev, cudaStream_t s) {
+int side_by_side(int size, int dev) {
+  static std::atomic<int> known[64][4];
+  const int at = size == 2 ? 1 : size == 4 ? 2 : size == 8 ? 3 : 0;
+  std::atomic<int>* k = dev >= 0 && dev < 64 ? &known[dev][at] : nullptr;
+  int n = k ? k->load(std::memory_order_relaxed) : 0;
+  if (n == 0) {
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = unsigned(size);
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(unsigned(size));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = BlocksSmem<D, kSplit>::bytes;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, reinterpret_cast<const void*>(k_cross_blocks<D, kF16, kSplit>), &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      return 0;
+    }
+    if (k && n > 0) k->store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+template <int D, bool kF16, bool kSplit>
+cudaError_t launch(const BlocksParams& bp, int64_t items, int64_t sure, int64_t tiles, int dev, cudaStream_t s) {
   static std::atomic<uint64_t> raised{0};
   const cudaError_t err = raise_shared(k_cross_blocks<D, kF16, kSplit>, raised, BlocksSmem<D, kSplit>::bytes, dev);
-  return err != cudaSuccess ? err
-                            : launch_clusters(k_cross_blocks<D, kF16, kSplit>, items, bp.cluster, kThreads, BlocksSmem<D, kSplit>::bytes, s, bp);
+  if (err != cudaSuccess) return err;
+  // A cluster for each block where all blocks' clusters run side by side, of two tiles of states a CTA at least
+  // (16 blocks of 32 tiles: 28 us by clusters of 4, 41 of 8, of which 16 do not, 63 alone).
+  BlocksParams l = bp;
+  l.cluster = 1;
+  while (l.cluster < 8 && l.cluster * 4 <= tiles && sure <= side_by_side<D, kF16, kSplit>(2 * l.cluster, dev)) l.cluster *= 2;
+  return launch_clusters(k_cross_blocks<D, kF16, kSplit>, items, l.cluster, kThreads, BlocksSmem<D, kSplit>::bytes, s, l);
 }
 
 }  // namespace
 
-cudaError_t launch_cross_blocks(const CrossParams& p, const CrossMaps& maps, int d, int dev, int sms, cudaStream_t s) {
+cudaError_t launch_cross_blocks(const CrossParams& p, const CrossMaps& maps, int d, int dev, cudaStream_t s) {
   BlocksParams bp{};
   bp.a = p;
   bp.q = maps.q;
@@ -475,15 +507,12 @@ cudaError_t launch_cross_blocks(const CrossParams& p, const CrossMaps& maps, int
   const int64_t blocks = (p.n_tokens / p.batch + block_tokens - 1) / block_tokens;
   const int64_t sure = (blocks > 0 ? blocks : 1) * p.batch * p.kv_heads;           // about as many blocks as there are
   const int64_t items = cross_blocks(p, p.q_begin, p.n_tokens, int(block_tokens));
-  // a cluster for each block where that fills the SMs, of two tiles of states a CTA at least
   const int64_t tiles = (p.n_rows / p.batch + kStates - 1) / kStates;
-  bp.cluster = 1;
-  while (bp.cluster < 8 && sure * bp.cluster * 2 <= sms && bp.cluster * 4 <= tiles) bp.cluster *= 2;
   if (d == 128)
-    return p.f16 ? (split ? launch<128, true, true>(bp, items, dev, s) : launch<128, true, false>(bp, items, dev, s))
-                 : (split ? launch<128, false, true>(bp, items, dev, s) : launch<128, false, false>(bp, items, dev, s));
-  return p.f16 ? (split ? launch<64, true, true>(bp, items, dev, s) : launch<64, true, false>(bp, items, dev, s))
-               : (split ? launch<64, false, true>(bp, items, dev, s) : launch<64, false, false>(bp, items, dev, s));
+    return p.f16 ? (split ? launch<128, true, true>(bp, items, sure, tiles, dev, s) : launch<128, true, false>(bp, items, sure, tiles, dev, s))
+                 : (split ? launch<128, false, true>(bp, items, sure, tiles, dev, s) : launch<128, false, false>(bp, items, sure, tiles, dev, s));
+  return p.f16 ? (split ? launch<64, true, true>(bp, items, sure, tiles, dev, s) : launch<64, true, false>(bp, items, sure, tiles, dev, s))
+               : (split ? launch<64, false, true>(bp, items, sure, tiles, dev, s) : launch<64, false, false>(bp, items, sure, tiles, dev, s));
 }
 
 }  // namespace reskv
