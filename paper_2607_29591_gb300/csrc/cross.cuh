@@ -152,6 +152,42 @@ cudaError_t launch_clusters(K kernel, int64_t blocks, int cluster, int threads, 
   cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, params);
 }
+// Clusters of `size` (2, 4, 8) CTAs of a kernel that run side by side; asked once a device.
+struct SideBySide {
+  std::atomic<int> known[64][4];
+};
+template <typename K>
+int side_by_side(K kernel, SideBySide& kept, int size, int threads, size_t shared, int dev) {
+  const int at = size == 2 ? 1 : size == 4 ? 2 : size == 8 ? 3 : 0;
+  std::atomic<int>* k = dev >= 0 && dev < 64 ? &kept.known[dev][at] : nullptr;
+  int n = k ? k->load(std::memory_order_relaxed) : 0;
+  if (n == 0) {
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = unsigned(size);
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(unsigned(size));
+    cfg.blockDim = dim3(unsigned(threads));
+    cfg.dynamicSmemBytes = shared;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, reinterpret_cast<const void*>(kernel), &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      return 0;
+    }
+    if (k && n > 0) k->store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+// The cluster that shares a block's `tiles`: as large as all `blocks` (about) run side by side, of two tiles a CTA
+// at least.
+template <typename K>
+int cluster_for(K kernel, SideBySide& kept, int64_t blocks, int64_t tiles, int threads, size_t shared, int dev) {
+  int size = 1;
+  while (size < 8 && size * 4 <= tiles && blocks <= side_by_side(kernel, kept, 2 * size, threads, shared, dev)) size *= 2;
+  return size;
+}
 // A kernel's shared memory limit, raised once a device.
 template <typename K>
 cudaError_t raise_shared(K kernel, std::atomic<uint64_t>& raised, int bytes, int dev) {

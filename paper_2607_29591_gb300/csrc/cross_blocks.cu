@@ -452,43 +452,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
   if (cs > 1) sync_cluster();                     // nobody leaves while its rows are read
 }
 
-// Clusters of `size` CTAs that run side by side; asked once a device.
-template <int D, bool kF16, bool kSplit>
-int side_by_side(int size, int dev) {
-  static std::atomic<int> known[64][4];
-  const int at = size == 2 ? 1 : size == 4 ? 2 : size == 8 ? 3 : 0;
-  std::atomic<int>* k = dev >= 0 && dev < 64 ? &known[dev][at] : nullptr;
-  int n = k ? k->load(std::memory_order_relaxed) : 0;
-  if (n == 0) {
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = unsigned(size);
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(unsigned(size));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = BlocksSmem<D, kSplit>::bytes;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&n, reinterpret_cast<const void*>(k_cross_blocks<D, kF16, kSplit>), &cfg) != cudaSuccess) {
-      cudaGetLastError();
-      return 0;
-    }
-    if (k && n > 0) k->store(n, std::memory_order_relaxed);
-  }
-  return n;
-}
-
 template <int D, bool kF16, bool kSplit>
 cudaError_t launch(const BlocksParams& bp, int64_t items, int64_t sure, int64_t tiles, int dev, cudaStream_t s) {
   static std::atomic<uint64_t> raised{0};
   const cudaError_t err = raise_shared(k_cross_blocks<D, kF16, kSplit>, raised, BlocksSmem<D, kSplit>::bytes, dev);
   if (err != cudaSuccess) return err;
-  // A cluster for each block where all blocks' clusters run side by side, of two tiles of states a CTA at least
-  // (16 blocks of 32 tiles: 28 us by clusters of 4, 41 of 8, of which 16 do not, 63 alone).
+  // (16 blocks of 32 tiles: 28 us by clusters of 4, 41 of 8, of which 16 do not run side by side, 63 alone)
+  static SideBySide kept{};
   BlocksParams l = bp;
-  l.cluster = 1;
-  while (l.cluster < 8 && l.cluster * 4 <= tiles && sure <= side_by_side<D, kF16, kSplit>(2 * l.cluster, dev)) l.cluster *= 2;
+  l.cluster = cluster_for(k_cross_blocks<D, kF16, kSplit>, kept, sure, tiles, kThreads, BlocksSmem<D, kSplit>::bytes, dev);
   return launch_clusters(k_cross_blocks<D, kF16, kSplit>, items, l.cluster, kThreads, BlocksSmem<D, kSplit>::bytes, s, l);
 }
 

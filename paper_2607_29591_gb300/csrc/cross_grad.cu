@@ -18,6 +18,9 @@
 // were summed with atomics.  Heads of a KV head are rows of one sum.  P and T are rounded to q's
 // type (half a step of themselves; P times 2^12 in fp16, whose range ends at 2^-24), sums are fp32.
 //
+// Where there are too few blocks for the SMs, a cluster of CTAs shares a block's tiles: each leaves its two
+// sums in shared memory, where the cluster adds them up in order.
+//
 // Roles: warps 0-7 turn S and G into P and T, a row of TMEM a thread, half of its columns each; 8
 // copies; 9 issues products; 10 puts zeros where a last tile's rows are no one's (a product sums
 // over them, times 0, and they may be NaN); 11 (states) the rows' lse and D.
@@ -32,7 +35,7 @@ using namespace tc;
 
 constexpr int kTile = 128;                        // rows and states of a tile
 constexpr int kThreads = 384;
-constexpr int kCopyWarp = 8, kIssueWarp = 9, kTailWarp = 10, kStatsWarp = 11;
+constexpr int kCopyWarp = 8, kIssueWarp = 9, kTailWarp = 10;
 constexpr int kRegsSoftmax = 232, kRegsIssue = 40;
 static_assert((2 * kRegsSoftmax + kRegsIssue) * 128 <= 168 * kThreads, "registers");
 constexpr int kHalf = kTile * 128;                // bytes of 128 rows of 64 elements
@@ -40,7 +43,7 @@ constexpr int kHalf = kTile * 128;                // bytes of 128 rows of 64 ele
 struct GradParams {
   CrossParams a;
   CUtensorMap q, k, v, g;
-  int32_t tile_tokens;
+  int32_t tile_tokens, cluster;
 };
 
 // 64 values in q's type over the first 32 of the 64 columns that they came from; `sum`: and their sum, as rounded
@@ -81,6 +84,38 @@ template <int N>
 __device__ __forceinline__ void store_zeros(uint16_t* y) {
 #pragma unroll 1
   for (int k = 0; k < N / 8; ++k) reinterpret_cast<uint4*>(y)[k] = make_uint4(0, 0, 0, 0);
+}
+
+// N columns from `at` of a thread's TMEM row into its row of fp32 in shared memory, from dim c0 on (word u of row r
+// at u ^ r: rows on banks of their own).
+template <int D, int N>
+__device__ __forceinline__ void leave_columns(uint32_t at, float4* rows, int r, int c0) {
+#pragma unroll 1
+  for (int k0 = 0; k0 < N / 16; ++k0) {
+    float o[16];
+    load16(at + 16 * k0, o);
+    landed();
+    defined16(o);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      rows[r * (D / 4) + ((c0 / 4 + 4 * k0 + k) ^ (r & (D / 4 - 1)))] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+  }
+}
+// Dims 4u .. of row r of all ranks that have tiles (of `all`), in order.
+template <int D>
+__device__ __forceinline__ float4 add_ranks(uint32_t rows, int r, int u, int cs, int all) {
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+  for (int k = 0; k < cs; ++k) {
+    if (int64_t(all) * (k + 1) / cs == int64_t(all) * k / cs) continue;
+    const float4 v = read_cluster4(of_rank(rows + uint32_t(r * (D / 4) + (u ^ (r & (D / 4 - 1)))) * 16, uint32_t(k)));
+    a = make_float4(a.x + v.x, a.y + v.y, a.z + v.z, a.w + v.w);
+  }
+  return a;
+}
+template <bool kF16>
+__device__ __forceinline__ uint2 pack_four(float4 a, float f) {
+  return make_uint2(pack_two<kF16>(a.x * f, a.y * f), pack_two<kF16>(a.z * f, a.w * f));
 }
 
 // Zeros into rows [r0, r1) of a tile in shared memory (one warp).
@@ -155,21 +190,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
   }
   wait_for_previous();
 
-  const int tt = gp.tile_tokens;
+  const int tt = gp.tile_tokens, cs = gp.cluster, rank = cs > 1 ? int(rank_in_cluster()) : 0;
   CrossBlock block;
-  if (!cross_block(p, p.q_begin, p.n_tokens, tt, int(blockIdx.x), lane, block)) return;      // the whole CTA
-  const int h = block.h, t0 = block.first;
+  if (!cross_block(p, p.q_begin, p.n_tokens, tt, int(blockIdx.x) / cs, lane, block)) return;      // the whole cluster
+  const int h = block.h, t0 = block.first, used_rows = tt * p.group;
   const CrossSequence sq = cross_sequence(p, block.b);
-  const int n = (sq.seen + kTile - 1) / kTile, left = sq.seen - (n - 1) * kTile;
-  const bool cut = left < kTile;
+  const int all = (sq.seen + kTile - 1) / kTile;
+  const int first = int(int64_t(all) * rank / cs), n = int(int64_t(all) * (rank + 1) / cs) - first;      // tiles of states
+  const int left = sq.seen - (first + n - 1) * kTile;                 // states of the last
+  const bool cut = n > 0 && left < kTile;
   // a softmax thread's row, and its half of the columns
   const int c = warp >> 2, rt = (warp & 3) * 32 + lane, row_token = rt / p.group, token = t0 + row_token;
   const bool real = warp < 8 && row_token < tt && token < sq.count;
   const int head = h * p.group + rt - row_token * p.group;
   const int64_t at_token = sq.q0 + token;
   uint16_t* const dq = static_cast<uint16_t*>(p.d_q.data) + (real ? at_token * p.d_q.token + head * p.d_q.head + c * (D / 2) : 0);
-  if (n == 0) {                                   // the same for the whole CTA
-    if (real) store_zeros<D / 2>(dq);
+  if (all == 0) {                                 // the same for the whole cluster
+    if (real && rank == 0) store_zeros<D / 2>(dq);
     return;
   }
   if (warp == kIssueWarp) take_columns(smem_u32(&sh.tmem));
@@ -183,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
     if (warp == kCopyWarp) {
       // --- copies: K0 V0 K1 V1 .. ---
-      if (elected()) {
+      if (elected() && n > 0) {
         mbar_arrive_expect_tx(&sh.q, uint32_t(2 * (D / 64) * tt * p.group * 128));
         for (int x = 0; x < D / 64; ++x) {
           copy_box(smem_q + x * kHalf, &gp.q, 64 * x, h * p.group, sq.q0 + t0, &sh.q);
@@ -203,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
           mbar_arrive_expect_tx(bar, S::tile);
 #pragma unroll
           for (int x = 0; x < D / 64; ++x)
-            copy_box(ring + slot * S::tile + x * kHalf, op & 1 ? &gp.v : &gp.k, 64 * x, h, sq.k0 + op / 2 * kTile, bar);
+            copy_box(ring + slot * S::tile + x * kHalf, op & 1 ? &gp.v : &gp.k, 64 * x, h, sq.k0 + (first + op / 2) * kTile, bar);
         }
         __syncwarp();
         copied = op + 1;
@@ -246,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
         }
         __syncwarp();
       };
-      bool ok = role_wait(&sh.q, 0, &sh.abort, p.status) && wait_tile(0);
+      bool ok = n > 0 && role_wait(&sh.q, 0, &sh.abort, p.status) && wait_tile(0);
       if (ok) {
         outer(s_cols, smem_q, tile_of(0), &sh.s);
         ok = wait_tile(1);
@@ -356,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
       fence_before();
       role_arrive(&sh.t);
     }
-    if (ok) ok = role_wait(&sh.done, 0, &sh.abort, p.status);
+    if (ok && n > 0) ok = role_wait(&sh.done, 0, &sh.abort, p.status);
     auto both_halves = [&](float x) {
       sh.sums[c][rt] = x;
       asm volatile("bar.sync 1, 256;" ::: "memory");
@@ -365,8 +402,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
       return x;
     };
     const float lacks = both_halves(more.x + more.y), e = both_halves(rounded.x + rounded.y);
-    if (real && c == 0) p.delta[stat] = delta + lacks;
-    if (ok) {
+    if (cs == 1 && real && c == 0) p.delta[stat] = delta + lacks;
+    if (cs > 1) {
+      // for the join: all products are done, operands' memory is free
+      fence_after();
+      float4* rows = reinterpret_cast<float4*>(smem);
+      if (n > 0) {
+        leave_columns<D, D / 2>(o_cols + lanes + c * (D / 2), rows, rt, c * (D / 2));
+        leave_columns<D, D / 2>(b_cols + lanes + c * (D / 2), rows + kTile * (D / 4), rt, c * (D / 2));
+      }
+      if (c == 0) reinterpret_cast<float4*>(smem + 2 * kTile * D * 4)[rt] = make_float4(delta, lacks, e, 0.f);
+    } else if (ok) {
       fence_after();
       const float back = -e * kDown;
 #pragma unroll 1
@@ -393,6 +439,33 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
   __syncthreads();
   fence_after();
   if (warp == kIssueWarp) give_columns(tmem);
+  if (cs == 1) return;
+  sync_cluster();
+  // --- the join: a row a warp, rows dealt to the cluster's first eight warps (the others have few registers) ---
+#pragma unroll 1
+  for (int r = rank * 8 + warp; warp < 8 && r < used_rows; r += cs * 8) {
+    const int tk = t0 + r / p.group, hd = h * p.group + r % p.group;
+    if (tk >= sq.count) break;
+    const int u = lane < D / 4 ? lane : 0;
+    float lacks = 0.f, e = 0.f, d0 = 0.f;
+#pragma unroll 1
+    for (int k = 0; k < cs; ++k) {
+      const float4 v = read_cluster4(of_rank(smem_q + 2 * kTile * D * 4 + uint32_t(r) * 16, uint32_t(k)));
+      d0 = v.x;
+      lacks += v.y;
+      e += v.z;
+    }
+    const float4 a = add_ranks<D>(smem_q, r, u, cs, all), b = add_ranks<D>(smem_q + kTile * D * 4, r, u, cs, all);
+    const float back = -e * kDown;
+    const int64_t tok = sq.q0 + tk;
+    if (lane < D / 4)
+      reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.d_q.data) + tok * p.d_q.token + hd * p.d_q.head)[u] = pack_four<kF16>(
+          make_float4(fmaf(back, b.x, a.x), fmaf(back, b.y, a.y), fmaf(back, b.z, a.z), fmaf(back, b.w, a.w)), p.scale);
+    if (lane == 0) p.delta[tok * p.heads + hd] = d0 + lacks;
+    __syncwarp();
+  }
+  __syncthreads();
+  sync_cluster();                                 // nobody leaves while its sums are read
 }
 
 // --- states --------------------------------------------------------------------
@@ -438,21 +511,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
   }
   wait_for_previous();
 
+  const int cs = gp.cluster, rank = cs > 1 ? int(rank_in_cluster()) : 0;
   CrossBlock block;
-  if (!cross_block(p, p.kv_begin, p.n_rows, kTile, int(blockIdx.x), lane, block)) return;    // the whole CTA
+  if (!cross_block(p, p.kv_begin, p.n_rows, kTile, int(blockIdx.x) / cs, lane, block)) return;    // the whole cluster
   const int h = block.h, j0 = block.first;
   const CrossSequence sq = cross_sequence(p, block.b);
   const int tt = gp.tile_tokens, used = tt * p.group;                 // rows of a full tile
-  const int n = j0 < sq.seen ? (sq.count + tt - 1) / tt : 0;
-  const int left = (sq.count - (n - 1) * tt) * p.group;               // rows of the last tile
-  const bool cut = left < used;
+  const int all = j0 < sq.seen ? (sq.count + tt - 1) / tt : 0;
+  const int first = int(int64_t(all) * rank / cs), n = int(int64_t(all) * (rank + 1) / cs) - first;      // tiles of rows
+  const int left = min((sq.count - (first + n - 1) * tt) * p.group, used);      // rows of the last
+  const bool cut = n > 0 && left < used;
   // a softmax thread's state; warps 0-3 write dV, 4-7 dK
   const int c = warp >> 2, rt = (warp & 3) * 32 + lane, j = j0 + rt;
   const bool owned = warp < 8 && j < sq.rows;
   const CrossRows& to = c ? p.d_k : p.d_v;
   uint16_t* const out = static_cast<uint16_t*>(to.data) + (owned ? (sq.k0 + j) * to.token + h * to.head : 0);
-  if (n == 0) {                                   // nobody sees them: the same for the whole CTA
-    if (owned) store_zeros<D>(out);
+  if (all == 0) {                                 // nobody sees them: the same for the whole cluster
+    if (owned && rank == 0) store_zeros<D>(out);
     return;
   }
   if (warp == kIssueWarp) take_columns(smem_u32(&sh.tmem));
@@ -470,7 +545,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
     if (warp == kCopyWarp) {
       // --- copies ---
-      if (elected()) {
+      if (elected() && n > 0) {
         mbar_arrive_expect_tx(&sh.kv, 2 * S::tile);
         for (int x = 0; x < D / 64; ++x) {
           copy_box(smem_k + x * kHalf, &gp.k, 64 * x, h, sq.k0 + j0, &sh.kv);
@@ -491,8 +566,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
           const uint32_t dst = ring + stage * 2 * S::tile;
 #pragma unroll
           for (int x = 0; x < D / 64; ++x) {
-            copy_box(dst + x * kHalf, &gp.q, 64 * x, h * p.group, sq.q0 + i * tt, bar);
-            copy_box(dst + S::tile + x * kHalf, &gp.g, 64 * x, h * p.group, sq.q0 + i * tt, bar);
+            copy_box(dst + x * kHalf, &gp.q, 64 * x, h * p.group, sq.q0 + (first + i) * tt, bar);
+            copy_box(dst + S::tile + x * kHalf, &gp.g, 64 * x, h * p.group, sq.q0 + (first + i) * tt, bar);
           }
         }
         __syncwarp();
@@ -532,7 +607,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
         __syncwarp();
       };
       auto q_tile = [&](int i) { return ring + i % kStages * 2 * S::tile; };
-      bool ok = role_wait(&sh.kv, 0, &sh.abort, p.status) && wait_tile(0);
+      bool ok = n > 0 && role_wait(&sh.kv, 0, &sh.abort, p.status) && wait_tile(0);
       if (ok) {
         outer(s_cols, smem_k, q_tile(0), &sh.s);
         outer(g_cols, smem_v, q_tile(0) + S::tile, &sh.g);
@@ -576,7 +651,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
         float l[4], e[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int r = lane + 32 * k, tk = i * tt + r / p.group;
+          const int r = lane + 32 * k, tk = (first + i) * tt + r / p.group;
           const bool here = r < used && tk < sq.count;
           const int64_t at = int64_t(sq.q0 + tk) * p.heads + h * p.group + r % p.group;
           l[k] = here ? p.lse[at] : 0.f;
@@ -655,8 +730,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
       fence_before();
       role_arrive(&sh.t);
     }
-    if (ok) ok = role_wait(&sh.done, 0, &sh.abort, p.status);
-    if (ok) {
+    if (ok && n > 0) ok = role_wait(&sh.done, 0, &sh.abort, p.status);
+    if (cs > 1) {
+      // for the join: all products are done, operands' memory is free
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      fence_after();
+      if (n > 0) leave_columns<D, D>((c ? k_cols : v_cols) + lanes, reinterpret_cast<float4*>(smem) + c * kTile * (D / 4), rt, 0);
+    } else if (ok) {
       fence_after();
       const bool seen = owned && j < sq.seen;
       store_columns<kF16, D>((c ? k_cols : v_cols) + lanes, c ? p.scale : kDown, out, seen);
@@ -667,7 +747,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
   __syncthreads();
   fence_after();
   if (warp == kIssueWarp) give_columns(tmem);
+  if (cs == 1) return;
+  sync_cluster();
+  // --- the join: a row of dV (even) or dK a warp ---
+#pragma unroll 1
+  for (int i = rank * 8 + warp; warp < 8 && i < 2 * kTile; i += cs * 8) {
+    const int which = i & 1, r = i >> 1, row = j0 + r;
+    if (row >= sq.rows) break;
+    const int u = lane < D / 4 ? lane : 0;
+    const float4 a = add_ranks<D>(smem_k + which * kTile * D * 4, r, u, cs, all);
+    const CrossRows& y = which ? p.d_k : p.d_v;
+    const uint2 v = pack_four<kF16>(a, which ? p.scale : kDown);
+    if (lane < D / 4)
+      reinterpret_cast<uint2*>(static_cast<uint16_t*>(y.data) + (sq.k0 + row) * y.token + h * y.head)[u] =
+          row < sq.seen ? v : make_uint2(0u, 0u);
+    __syncwarp();
+  }
+  __syncthreads();
+  sync_cluster();                                 // nobody leaves while its sums are read
 }
+
 
 template <int D, bool kF16>
 cudaError_t both(const GradParams& gp, int dev, cudaStream_t s) {
@@ -675,12 +774,20 @@ cudaError_t both(const GradParams& gp, int dev, cudaStream_t s) {
   const CrossParams& p = gp.a;
   cudaError_t err = raise_shared(k_cross_grad_q<D, kF16>, raised_q, QuerySmem<D>::bytes, dev);
   if (err == cudaSuccess) err = raise_shared(k_cross_grad_kv<D, kF16>, raised_kv, StateSmem<D>::bytes, dev);
-  if (err == cudaSuccess)
-    err = launch_clusters(k_cross_grad_q<D, kF16>, cross_blocks(p, p.q_begin, p.n_tokens, gp.tile_tokens), 1, kThreads,
-                          QuerySmem<D>::bytes, s, gp);
-  if (err == cudaSuccess)
-    err = launch_clusters(k_cross_grad_kv<D, kF16>, cross_blocks(p, p.kv_begin, p.n_rows, kTile), 1, kThreads, StateSmem<D>::bytes,
-                          s, gp);
+  static SideBySide kept_q{}, kept_kv{};
+  const int64_t rows = (p.n_tokens / p.batch + gp.tile_tokens - 1) / gp.tile_tokens, states = (p.n_rows / p.batch + kTile - 1) / kTile;
+  const int64_t units = int64_t(p.batch) * p.kv_heads;                // (tiles of them: on average)
+  GradParams l = gp;
+  if (err == cudaSuccess) {
+    l.cluster = cluster_for(k_cross_grad_q<D, kF16>, kept_q, (rows > 0 ? rows : 1) * units, states, kThreads, QuerySmem<D>::bytes, dev);
+    err = launch_clusters(k_cross_grad_q<D, kF16>, cross_blocks(p, p.q_begin, p.n_tokens, gp.tile_tokens), l.cluster, kThreads,
+                          QuerySmem<D>::bytes, s, l);
+  }
+  if (err == cudaSuccess) {
+    l.cluster = cluster_for(k_cross_grad_kv<D, kF16>, kept_kv, (states > 0 ? states : 1) * units, rows, kThreads, StateSmem<D>::bytes, dev);
+    err = launch_clusters(k_cross_grad_kv<D, kF16>, cross_blocks(p, p.kv_begin, p.n_rows, kTile), l.cluster, kThreads,
+                          StateSmem<D>::bytes, s, l);
+  }
   return err;
 }
 

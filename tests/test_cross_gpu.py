@@ -205,6 +205,12 @@ def test_longer_states():
     Case(12, [70], [1500], 2, 1, 64, "f16").check()
 
 
+@pytest.mark.parametrize("d,dtype", [(128, "bf16"), (64, "f16")])
+@pytest.mark.parametrize("counts,lens", [([3], [3000]), ([20, 3], [2100, 700]), ([700], [60]), ([300, 1], [50, 400]), ([300], [1100])])
+def test_few_blocks_shared_by_clusters(d, dtype, counts, lens):
+    Case(17, counts, lens, 1, 4, d, dtype).check()
+
+
 def test_gradient_against_differences():
     """<d_o, o(q + h u) - o(q - h u)> / 2h along random directions, o from the oracle."""
     c = Case(13, [6], [50], 1, 2, 64, "f16")
