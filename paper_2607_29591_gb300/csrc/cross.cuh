@@ -152,6 +152,28 @@ cudaError_t launch_clusters(K kernel, int64_t blocks, int cluster, int threads, 
   cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, params);
 }
+// sum of weight(i) * source i, i < n in order, those without a bit in `present` left out; at(i): where the lane's four
+// elements of it are.  Eight are asked for at a time: one after the other they take a cluster's latency each.
+template <typename A, typename W>
+__device__ __forceinline__ float4 add_sources(int n, uint32_t present, A at, W weight) {
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+  for (int i0 = 0; i0 < n; i0 += 8) {
+    float4 v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = i0 + j < n && ((present >> (i0 + j)) & 1) ? read_cluster4(at(i0 + j)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float w = weight(i0 + j);             // (0 past the last)
+      a.x = fmaf(w, v[j].x, a.x);
+      a.y = fmaf(w, v[j].y, a.y);
+      a.z = fmaf(w, v[j].z, a.z);
+      a.w = fmaf(w, v[j].w, a.w);
+    }
+  }
+  return a;
+}
+
 // Clusters of `size` (2, 4, 8) CTAs of a kernel that run side by side; asked once a device.
 struct SideBySide {
   std::atomic<int> known[64][4];

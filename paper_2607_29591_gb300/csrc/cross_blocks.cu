@@ -425,19 +425,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
     float total = w == 0.f && sum == sum ? 0.f : w * sum;
 #pragma unroll
     for (int o = 16; o; o /= 2) total += __shfl_xor_sync(0xffffffffu, total, o);
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
     const int u = lane < D / 4 ? lane : 0;
-#pragma unroll 1
-    for (int i = 0; i < sources; ++i) {
-      const float wi = __shfl_sync(0xffffffffu, w, i);
-      if (__shfl_sync(0xffffffffu, ref, i) == -INFINITY) continue;    // a source without states
-      const uint32_t at = at_rows + uint32_t(((kSplit ? i & 1 : rm) * 128 + rr) * (D / 4) + (u ^ (rr & (D / 4 - 1)))) * 16;
-      const float4 v = read_cluster4(of_rank(at, uint32_t(i / kSources)));
-      a.x = fmaf(wi, v.x, a.x);
-      a.y = fmaf(wi, v.y, a.y);
-      a.z = fmaf(wi, v.z, a.z);
-      a.w = fmaf(wi, v.w, a.w);
-    }
+    const float4 a = add_sources(
+        sources, __ballot_sync(0xffffffffu, ref != -INFINITY),
+        [&](int i) {
+          const uint32_t at = at_rows + uint32_t(((kSplit ? i & 1 : rm) * 128 + rr) * (D / 4) + (u ^ (rr & (D / 4 - 1)))) * 16;
+          return of_rank(at, uint32_t(i / kSources));
+        },
+        [&](int i) { return __shfl_sync(0xffffffffu, w, i & 31); });
     const float inv = 1.f / total;
     const int hd = h * p.group + rr - tk * p.group;
     if (lane < D / 4) {

@@ -104,14 +104,11 @@ __device__ __forceinline__ void leave_columns(uint32_t at, float4* rows, int r, 
 // Dims 4u .. of row r of all ranks that have tiles (of `all`), in order.
 template <int D>
 __device__ __forceinline__ float4 add_ranks(uint32_t rows, int r, int u, int cs, int all) {
-  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-  for (int k = 0; k < cs; ++k) {
-    if (int64_t(all) * (k + 1) / cs == int64_t(all) * k / cs) continue;
-    const float4 v = read_cluster4(of_rank(rows + uint32_t(r * (D / 4) + (u ^ (r & (D / 4 - 1)))) * 16, uint32_t(k)));
-    a = make_float4(a.x + v.x, a.y + v.y, a.z + v.z, a.w + v.w);
-  }
-  return a;
+  uint32_t present = 0;
+  for (int k = 0; k < cs; ++k) present |= uint32_t(int64_t(all) * (k + 1) / cs != int64_t(all) * k / cs) << k;
+  return add_sources(
+      cs, present, [&](int k) { return of_rank(rows + uint32_t(r * (D / 4) + (u ^ (r & (D / 4 - 1)))) * 16, uint32_t(k)); },
+      [](int) { return 1.f; });
 }
 template <bool kF16>
 __device__ __forceinline__ uint2 pack_four(float4 a, float f) {
@@ -411,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
         leave_columns<D, D / 2>(o_cols + lanes + c * (D / 2), rows, rt, c * (D / 2));
         leave_columns<D, D / 2>(b_cols + lanes + c * (D / 2), rows + kTile * (D / 4), rt, c * (D / 2));
       }
-      if (c == 0) reinterpret_cast<float4*>(smem + 2 * kTile * D * 4)[rt] = make_float4(delta, lacks, e, 0.f);
+      if (c == 0) reinterpret_cast<float4*>(smem + 2 * kTile * D * 4)[rt] = make_float4(rank == 0 ? delta : 0.f, lacks, e, 0.f);
     } else if (ok) {
       fence_after();
       const float back = -e * kDown;
@@ -447,14 +444,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
     const int tk = t0 + r / p.group, hd = h * p.group + r % p.group;
     if (tk >= sq.count) break;
     const int u = lane < D / 4 ? lane : 0;
-    float lacks = 0.f, e = 0.f, d0 = 0.f;
-#pragma unroll 1
-    for (int k = 0; k < cs; ++k) {
-      const float4 v = read_cluster4(of_rank(smem_q + 2 * kTile * D * 4 + uint32_t(r) * 16, uint32_t(k)));
-      d0 = v.x;
-      lacks += v.y;
-      e += v.z;
-    }
+    // D, sum T and sum T as rounded: of all ranks the last two
+    const float4 s = add_sources(cs, (1u << cs) - 1u, [&](int k) { return of_rank(smem_q + 2 * kTile * D * 4 + uint32_t(r) * 16, uint32_t(k)); },
+                                 [](int) { return 1.f; });
+    const float d0 = s.x, lacks = s.y, e = s.z;
     const float4 a = add_ranks<D>(smem_q, r, u, cs, all), b = add_ranks<D>(smem_q + kTile * D * 4, r, u, cs, all);
     const float back = -e * kDown;
     const int64_t tok = sq.q0 + tk;

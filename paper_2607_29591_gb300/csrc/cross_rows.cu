@@ -285,18 +285,12 @@ __global__ void __launch_bounds__(kThreads) k_cross_rows(const __grid_constant__
       for (int e = 16; e; e /= 2) total += __shfl_xor_sync(0xffffffffu, total, e);
       const uint32_t present = __ballot_sync(0xffffffffu, rf != -INFINITY);
       const int u = lane < D / 4 ? lane : 0;
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-      for (int i = 0; i < sources; ++i) {
-        const float wi = __shfl_sync(0xffffffffu, wt, i);
-        if (!((present >> i) & 1)) continue;
-        const float4 v = read_cluster4(of_rank(ring + uint32_t(((i % kWarps) * kRows + r) * D + ((4 * u + 8 * r) & (D - 1))) * 4,
-                                               uint32_t(i / kWarps)));
-        a.x = fmaf(wi, v.x, a.x);
-        a.y = fmaf(wi, v.y, a.y);
-        a.z = fmaf(wi, v.z, a.z);
-        a.w = fmaf(wi, v.w, a.w);
-      }
+      const float4 a = add_sources(
+          sources, present,
+          [&](int i) {
+            return of_rank(ring + uint32_t(((i % kWarps) * kRows + r) * D + ((4 * u + 8 * r) & (D - 1))) * 4, uint32_t(i / kWarps));
+          },
+          [&](int i) { return __shfl_sync(0xffffffffu, wt, i & 31); });
       const float inv = present ? 1.f / total : 0.f;
       const int64_t tok = sq.q0 + (r0 + r) / p.group;
       const int hd = h * p.group + (r0 + r) % p.group;
