@@ -119,6 +119,11 @@ __device__ __forceinline__ uint32_t rank_in_cluster() {
 __device__ __forceinline__ void sync_cluster() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// The same, or of the block alone: for warps whose code has parted.
+__device__ __forceinline__ void meet(int cluster) {
+  if (cluster > 1) sync_cluster();
+  else asm volatile("barrier.cta.sync 0;" ::: "memory");
+}
 __device__ __forceinline__ uint32_t of_rank(uint32_t local, uint32_t rank) {
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
@@ -152,26 +157,32 @@ cudaError_t launch_clusters(K kernel, int64_t blocks, int cluster, int threads, 
   cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, params);
 }
-// sum of weight(i) * source i, i < n in order, those without a bit in `present` left out; at(i): where the lane's four
-// elements of it are.  Eight are asked for at a time: one after the other they take a cluster's latency each.
-template <typename A, typename W>
-__device__ __forceinline__ float4 add_sources(int n, uint32_t present, A at, W weight) {
-  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+// M sums over sources i < n in order, those without a bit in `present` left out: out[m] = sum weight(m, i) * what
+// lies at at(m, i), four elements a lane.  4 M are asked for at a time: one after the other each
+// takes the cluster's latency (some 0.6 us).
+template <int M, typename A, typename W>
+__device__ __forceinline__ void add_sources(float4 (&out)[M], int n, uint32_t present, A at, W weight) {
+#pragma unroll
+  for (int m = 0; m < M; ++m) out[m] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-  for (int i0 = 0; i0 < n; i0 += 8) {
-    float4 v[8];
+  for (int i0 = 0; i0 < n; i0 += 4) {
+    float4 v[M][4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = i0 + j < n && ((present >> (i0 + j)) & 1) ? read_cluster4(at(i0 + j)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int m = 0; m < M; ++m)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float w = weight(i0 + j);             // (0 past the last)
-      a.x = fmaf(w, v[j].x, a.x);
-      a.y = fmaf(w, v[j].y, a.y);
-      a.z = fmaf(w, v[j].z, a.z);
-      a.w = fmaf(w, v[j].w, a.w);
-    }
+      for (int j = 0; j < 4; ++j)
+        v[m][j] = i0 + j < n && ((present >> (i0 + j)) & 1) ? read_cluster4(at(m, i0 + j)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        const float w = i0 + j < n && ((present >> (i0 + j)) & 1) ? weight(m, i0 + j) : 0.f;
+        out[m].x = fmaf(w, v[m][j].x, out[m].x);
+        out[m].y = fmaf(w, v[m][j].y, out[m].y);
+        out[m].z = fmaf(w, v[m][j].z, out[m].z);
+        out[m].w = fmaf(w, v[m][j].w, out[m].w);
+      }
   }
-  return a;
 }
 
 // Clusters of `size` (2, 4, 8) CTAs of a kernel that run side by side; asked once a device.

@@ -54,7 +54,7 @@ struct BlocksSmem {
   static constexpr int slots = (224 * 1024 - q) / tile > 8 ? 8 : (224 * 1024 - q) / tile;
   static constexpr int bytes = q + slots * tile + 1024;               // on a boundary of 1024
   static constexpr int at_ref = 2 * 128 * D * 4;  // of rows to be joined: outputs, then references and sums
-  static_assert(at_ref + 2 * 256 * 4 <= q + slots * tile, "rows to be joined");
+  static_assert(at_ref + 3 * 256 * 4 <= q + slots * tile, "rows to be joined");
   static_assert(bytes + 1024 + 256 <= 227 * 1024, "shared memory");
 };
 
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
   if (!cross_block(p, p.q_begin, p.n_tokens, block_tokens, int(blockIdx.x) / cs, lane, block)) return;      // the whole cluster
   const int b = block.b, h = block.h, t0 = block.first;
   const CrossSequence sq = cross_sequence(p, b);
-  const bool two = !kSplit && t0 + tt < sq.count;
+  const bool two = !kSplit && t0 + tt < sq.count, joins = kSplit || cs > 1;
   const int all = (sq.seen + kStates - 1) / kStates;
   const int first = int(int64_t(all) * rank / cs), n = int(int64_t(all) * (rank + 1) / cs) - first;      // tiles of states
   const int steps[2] = {kSplit ? (n + 1) / 2 : n, kSplit ? n / 2 : two ? n : 0};
@@ -248,6 +248,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
         role_arrive(&sh.full[slot]);
       }
     }
+    __syncwarp();
+    meet(cs);                                     // the softmax has read what it reads of tensor memory
+    if (warp == kIssueWarp) {
+      fence_after();
+      give_columns(tmem);
+    }
+    if (joins) meet(cs);
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     // --- the softmax, half a row a thread: states 64 c .. 64 c + 63 of a tile.  Both threads of a row look
@@ -393,58 +400,60 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
         refs[256 + m * 128 + rt] = seen ? l : 0.f;
       }
     }
-  }
-  fence_before();
-  __syncthreads();
-  fence_after();
-  if (warp == kIssueWarp) give_columns(tmem);
-  if (cs == 1 && !kSplit) return;
-  if (cs > 1) sync_cluster();
-
-  // --- the join: a row a warp, rows dealt to the cluster's softmax warps (the others have few registers) ---
-  const int rows = kSplit ? 128 : two ? 256 : 128;
-  const uint32_t at_rows = smem_q, at_ref = smem_q + S::at_ref, at_sum = at_ref + 256 * 4;
-  constexpr int kSources = kSplit ? 2 : 1;
-#pragma unroll 1
-  for (int r = rank * kSoftmaxWarps + warp; warp < kSoftmaxWarps && r < rows; r += cs * kSoftmaxWarps) {
-    const int rm = r >> 7, rr = r & 127;          // (split: tile 0's row, of both streams)
-    const int tk = rr / p.group, tok = t0 + rm * tt + tk;
-    if (tk >= tt || tok >= sq.count) continue;
-    // source i: stream i % kSources of rank i / kSources; at most 32 of them
-    const int sources = cs * kSources;
-    float ref = -INFINITY, sum = 0.f;
-    if (lane < sources) {
-      const uint32_t at = uint32_t((kSplit ? lane & 1 : rm) * 128 + rr) * 4, from = uint32_t(lane / kSources);
-      ref = read_cluster(of_rank(at_ref + at, from));
-      sum = read_cluster(of_rank(at_sum + at, from));
-    }
-    float top = ref;
-#pragma unroll
-    for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float w = ref == -INFINITY ? 0.f : exp2f(ref - top);
-    float total = w == 0.f && sum == sum ? 0.f : w * sum;
-#pragma unroll
-    for (int o = 16; o; o /= 2) total += __shfl_xor_sync(0xffffffffu, total, o);
-    const int u = lane < D / 4 ? lane : 0;
-    const float4 a = add_sources(
-        sources, __ballot_sync(0xffffffffu, ref != -INFINITY),
-        [&](int i) {
-          const uint32_t at = at_rows + uint32_t(((kSplit ? i & 1 : rm) * 128 + rr) * (D / 4) + (u ^ (rr & (D / 4 - 1)))) * 16;
-          return of_rank(at, uint32_t(i / kSources));
-        },
-        [&](int i) { return __shfl_sync(0xffffffffu, w, i & 31); });
-    const float inv = 1.f / total;
-    const int hd = h * p.group + rr - tk * p.group;
-    if (lane < D / 4) {
-      uint16_t* y = static_cast<uint16_t*>(p.o.data) + (sq.q0 + tok) * p.o.token + hd * p.o.head;
-      reinterpret_cast<uint2*>(y)[u] = make_uint2(pack_two<kF16>(a.x * inv, a.y * inv), pack_two<kF16>(a.z * inv, a.w * inv));
-    }
-    const float lse = (top + log2f(total)) * 0.693147180559945f;
-    if (lane == 0 && p.lse) p.lse[int64_t(sq.q0 + tok) * p.heads + hd] = lse;
     __syncwarp();
+    fence_before();
+    meet(cs);
+    if (!joins) return;
+    // --- the join: rows dealt to the ranks in runs, sources (streams of all ranks) in order ---
+    constexpr int kSources = kSplit ? 2 : 1;
+    const int rows = kSplit || !two ? 128 : 256, sources = cs * kSources, share = rows / cs, row0 = rank * share;
+    const uint32_t at_ref = smem_q + S::at_ref;
+    float* const weight = reinterpret_cast<float*>(smem + S::at_ref + 2 * 256 * 4);      // [share][sources], < 0: no states
+    auto place = [&](int i, int r) { return uint32_t((kSplit ? i & 1 : r >> 7) * 128 + (r & 127)); };      // of source i's row r
+    auto token_of = [&](int r) { return (r & 127) / p.group < tt ? t0 + (r >> 7) * tt + (r & 127) / p.group : sq.count; };
+    // each source of each row a thread: at most 256; a row's side by side
+    if (tid < share * sources) {
+      const int q = tid / sources, i = tid - q * sources, r = row0 + q;
+      const uint32_t at = place(i, r) * 4, from = uint32_t(i / kSources);
+      const float ref = read_cluster(of_rank(at_ref + at, from)), sum = read_cluster(of_rank(at_ref + 256 * 4 + at, from));
+      const uint32_t group = __activemask();        // whole warps
+      float top = ref;
+      for (int o = 1; o < sources; o *= 2) top = fmaxf(top, __shfl_xor_sync(group, top, o));
+      const float w = ref == -INFINITY ? 0.f : exp2f(ref - top);
+      float total = ref == -INFINITY ? 0.f : w * sum;
+      for (int o = 1; o < sources; o *= 2) total += __shfl_xor_sync(group, total, o);
+      weight[tid] = ref == -INFINITY ? -1.f : w / total;
+      const int tok = token_of(r);
+      if (i == 0 && p.lse && tok < sq.count)
+        p.lse[int64_t(sq.q0 + tok) * p.heads + h * p.group + (r & 127) % p.group] = (top + log2f(total)) * 0.693147180559945f;
+    }
+    asm volatile("bar.sync 9, 512;" ::: "memory");
+    // then a row a warp, four rows at a time
+#pragma unroll 1
+    for (int q = warp * 4; q < share; q += kSoftmaxWarps * 4) {
+      const int u = lane < D / 4 ? lane : 0;
+      auto w_of = [&](int m, int i) { return weight[(q + m) * sources + i]; };
+      float4 a[4];
+      uint32_t present = 0;                         // (of all rows alike)
+      for (int i = 0; i < sources; ++i) present |= uint32_t(!(w_of(0, i) < 0.f)) << i;
+      add_sources(
+          a, sources, present,
+          [&](int m, int i) {
+            const int r = row0 + q + m;
+            return of_rank(smem_q + (place(i, r) * (D / 4) + uint32_t(u ^ (r & (D / 4 - 1)))) * 16, uint32_t(i / kSources));
+          },
+          w_of);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const int r = row0 + q + m, tok = token_of(r), hd = h * p.group + (r & 127) % p.group;
+        if (tok < sq.count && lane < D / 4)
+          reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.o.data) + (sq.q0 + tok) * p.o.token + hd * p.o.head)[u] =
+              make_uint2(pack_two<kF16>(a[m].x, a[m].y), pack_two<kF16>(a[m].z, a[m].w));
+      }
+    }
+    __syncwarp();
+    meet(cs);                                     // nobody leaves while its rows are read
   }
-  __syncthreads();
-  if (cs > 1) sync_cluster();                     // nobody leaves while its rows are read
 }
 
 template <int D, bool kF16, bool kSplit>

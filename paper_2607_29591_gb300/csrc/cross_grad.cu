@@ -101,14 +101,16 @@ __device__ __forceinline__ void leave_columns(uint32_t at, float4* rows, int r, 
       rows[r * (D / 4) + ((c0 / 4 + 4 * k0 + k) ^ (r & (D / 4 - 1)))] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
   }
 }
-// Dims 4u .. of row r of all ranks that have tiles (of `all`), in order.
-template <int D>
-__device__ __forceinline__ float4 add_ranks(uint32_t rows, int r, int u, int cs, int all) {
+// The ranks that have tiles, of `all`.
+__device__ __forceinline__ uint32_t ranks_with_tiles(int cs, int all) {
   uint32_t present = 0;
   for (int k = 0; k < cs; ++k) present |= uint32_t(int64_t(all) * (k + 1) / cs != int64_t(all) * k / cs) << k;
-  return add_sources(
-      cs, present, [&](int k) { return of_rank(rows + uint32_t(r * (D / 4) + (u ^ (r & (D / 4 - 1)))) * 16, uint32_t(k)); },
-      [](int) { return 1.f; });
+  return present;
+}
+// Where rank k has dims 4u .. of row r.
+template <int D>
+__device__ __forceinline__ uint32_t row_of_rank(uint32_t rows, int r, int u, int k) {
+  return of_rank(rows + uint32_t(r * (D / 4) + (u ^ (r & (D / 4 - 1)))) * 16, uint32_t(k));
 }
 template <bool kF16>
 __device__ __forceinline__ uint2 pack_four(float4 a, float f) {
@@ -322,6 +324,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
         role_arrive(&sh.full[slot]);
       }
     }
+    __syncwarp();
+    meet(cs);                                     // the others have read what they read of tensor memory
+    if (warp == kIssueWarp) {
+      fence_after();
+      give_columns(tmem);
+    }
+    if (cs > 1) meet(cs);
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     // --- weights ---
@@ -431,34 +440,38 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
         }
       }
     }
-  }
-  fence_before();
-  __syncthreads();
-  fence_after();
-  if (warp == kIssueWarp) give_columns(tmem);
-  if (cs == 1) return;
-  sync_cluster();
-  // --- the join: a row a warp, rows dealt to the cluster's first eight warps (the others have few registers) ---
-#pragma unroll 1
-  for (int r = rank * 8 + warp; warp < 8 && r < used_rows; r += cs * 8) {
-    const int tk = t0 + r / p.group, hd = h * p.group + r % p.group;
-    if (tk >= sq.count) break;
-    const int u = lane < D / 4 ? lane : 0;
-    // D, sum T and sum T as rounded: of all ranks the last two
-    const float4 s = add_sources(cs, (1u << cs) - 1u, [&](int k) { return of_rank(smem_q + 2 * kTile * D * 4 + uint32_t(r) * 16, uint32_t(k)); },
-                                 [](int) { return 1.f; });
-    const float d0 = s.x, lacks = s.y, e = s.z;
-    const float4 a = add_ranks<D>(smem_q, r, u, cs, all), b = add_ranks<D>(smem_q + kTile * D * 4, r, u, cs, all);
-    const float back = -e * kDown;
-    const int64_t tok = sq.q0 + tk;
-    if (lane < D / 4)
-      reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.d_q.data) + tok * p.d_q.token + hd * p.d_q.head)[u] = pack_four<kF16>(
-          make_float4(fmaf(back, b.x, a.x), fmaf(back, b.y, a.y), fmaf(back, b.z, a.z), fmaf(back, b.w, a.w)), p.scale);
-    if (lane == 0) p.delta[tok * p.heads + hd] = d0 + lacks;
     __syncwarp();
+    fence_before();
+    meet(cs);
+    if (cs == 1) return;
+    // --- the join: rows dealt to the cluster's warps ---
+    const uint32_t present = ranks_with_tiles(cs, all);
+    auto one = [](int, int) { return 1.f; };
+#pragma unroll 1
+    for (int r = 2 * (rank * 8 + warp); r < used_rows; r += 2 * cs * 8) {       // two rows at a time
+      if (t0 + r / p.group >= sq.count) break;
+      const int u = lane < D / 4 ? lane : 0;
+      // D, sum T and sum T as rounded: of all ranks the last two
+      float4 s[2], a[4];
+      add_sources(s, cs, (1u << cs) - 1u, [&](int m, int k) { return of_rank(smem_q + 2 * kTile * D * 4 + uint32_t(r + m) * 16, uint32_t(k)); }, one);
+      add_sources(a, cs, present, [&](int m, int k) { return row_of_rank<D>(smem_q + (m & 1) * kTile * D * 4, r + m / 2, u, k); }, one);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const int tk = t0 + (r + m) / p.group, hd = h * p.group + (r + m) % p.group;
+        if (r + m >= used_rows || tk >= sq.count) continue;
+        const float back = -s[m].z * kDown;
+        const float4 x = a[2 * m], y = a[2 * m + 1];
+        const int64_t tok = sq.q0 + tk;
+        if (lane < D / 4)
+          reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.d_q.data) + tok * p.d_q.token + hd * p.d_q.head)[u] = pack_four<kF16>(
+              make_float4(fmaf(back, y.x, x.x), fmaf(back, y.y, x.y), fmaf(back, y.z, x.z), fmaf(back, y.w, x.w)), p.scale);
+        if (lane == 0) p.delta[tok * p.heads + hd] = s[m].x + s[m].y;
+      }
+      __syncwarp();
+    }
+    __syncwarp();
+    meet(cs);                                     // nobody leaves while its sums are read
   }
-  __syncthreads();
-  sync_cluster();                                 // nobody leaves while its sums are read
 }
 
 // --- states --------------------------------------------------------------------
@@ -660,6 +673,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
         role_arrive(&sh.full[stage]);
       }
     }
+    __syncwarp();
+    meet(cs);                                     // the others have read what they read of tensor memory
+    if (warp == kIssueWarp) {
+      fence_after();
+      give_columns(tmem);
+    }
+    if (cs > 1) meet(cs);
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     // --- weights: rows 64 c .. 64 c + 63 of a tile ---
@@ -735,29 +755,32 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
       store_columns<kF16, D>((c ? k_cols : v_cols) + lanes, c ? p.scale : kDown, out, seen);
       if (owned && !seen) store_zeros<D>(out);
     }
-  }
-  fence_before();
-  __syncthreads();
-  fence_after();
-  if (warp == kIssueWarp) give_columns(tmem);
-  if (cs == 1) return;
-  sync_cluster();
-  // --- the join: a row of dV (even) or dK a warp ---
-#pragma unroll 1
-  for (int i = rank * 8 + warp; warp < 8 && i < 2 * kTile; i += cs * 8) {
-    const int which = i & 1, r = i >> 1, row = j0 + r;
-    if (row >= sq.rows) break;
-    const int u = lane < D / 4 ? lane : 0;
-    const float4 a = add_ranks<D>(smem_k + which * kTile * D * 4, r, u, cs, all);
-    const CrossRows& y = which ? p.d_k : p.d_v;
-    const uint2 v = pack_four<kF16>(a, which ? p.scale : kDown);
-    if (lane < D / 4)
-      reinterpret_cast<uint2*>(static_cast<uint16_t*>(y.data) + (sq.k0 + row) * y.token + h * y.head)[u] =
-          row < sq.seen ? v : make_uint2(0u, 0u);
     __syncwarp();
+    fence_before();
+    meet(cs);
+    if (cs == 1) return;
+    // --- the join ---
+    const uint32_t present = ranks_with_tiles(cs, all);
+#pragma unroll 1
+    for (int r = 2 * (rank * 8 + warp); r < kTile; r += 2 * cs * 8) {           // two rows of both at a time
+      if (j0 + r >= sq.rows) break;
+      const int u = lane < D / 4 ? lane : 0;
+      float4 a[4];
+      add_sources(a, cs, present, [&](int m, int k) { return row_of_rank<D>(smem_k + (m & 1) * kTile * D * 4, r + m / 2, u, k); },
+                  [](int, int) { return 1.f; });
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const int row = j0 + r + m / 2;
+        if (row >= sq.rows || lane >= D / 4) continue;
+        const CrossRows& y = m & 1 ? p.d_k : p.d_v;
+        reinterpret_cast<uint2*>(static_cast<uint16_t*>(y.data) + (sq.k0 + row) * y.token + h * y.head)[u] =
+            row < sq.seen ? pack_four<kF16>(a[m], m & 1 ? p.scale : kDown) : make_uint2(0u, 0u);
+      }
+      __syncwarp();
+    }
+    __syncwarp();
+    meet(cs);                                     // nobody leaves while its sums are read
   }
-  __syncthreads();
-  sync_cluster();                                 // nobody leaves while its sums are read
 }
 
 

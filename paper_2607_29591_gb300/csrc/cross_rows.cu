@@ -34,8 +34,7 @@ struct RowsSmem {
   static constexpr int half = kRowStates * 128;   // 64 dims of a tile
   static constexpr int tile = D / 64 * half;
   static constexpr int stages = D == 128 ? 3 : 4;
-  static constexpr int at_rows = 0;               // the rows to be joined, over the drained ring
-  static constexpr int at_ref = kWarps * 8 * NB * D * 4;
+  static constexpr int at_ref = kWarps * 8 * NB * D * 4;              // behind the rows to be joined, over the drained ring
   static constexpr int bytes = stages * 2 * tile + 1024;
   static_assert(at_ref + 2 * kWarps * 8 * NB * 4 <= stages * 2 * tile, "rows to be joined");
 };
@@ -285,12 +284,14 @@ __global__ void __launch_bounds__(kThreads) k_cross_rows(const __grid_constant__
       for (int e = 16; e; e /= 2) total += __shfl_xor_sync(0xffffffffu, total, e);
       const uint32_t present = __ballot_sync(0xffffffffu, rf != -INFINITY);
       const int u = lane < D / 4 ? lane : 0;
-      const float4 a = add_sources(
-          sources, present,
-          [&](int i) {
+      float4 sums[1];
+      add_sources(
+          sums, sources, present,
+          [&](int, int i) {
             return of_rank(ring + uint32_t(((i % kWarps) * kRows + r) * D + ((4 * u + 8 * r) & (D - 1))) * 4, uint32_t(i / kWarps));
           },
-          [&](int i) { return __shfl_sync(0xffffffffu, wt, i & 31); });
+          [&](int, int i) { return __shfl_sync(0xffffffffu, wt, i); });
+      const float4 a = sums[0];
       const float inv = present ? 1.f / total : 0.f;
       const int64_t tok = sq.q0 + (r0 + r) / p.group;
       const int hd = h * p.group + (r0 + r) % p.group;
