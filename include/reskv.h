@@ -713,6 +713,8 @@ reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_paged_attn_a
  * queries of a sequence of no group see their own tokens alone.  Faults go to kv's and
  * prefix's status words.  Limits and roundings are reskv_paged_attn's; both parts are
  * joined in fp32.
+ * Limits: fewer than 1024 prefixes; n_tokens * heads / 2 + (batch + prefixes) * n_kv_heads below
+ * 2^24.
  *   seq_begin   : device int32 [prefix->batch + 1], ascending; NULL: batch / prefix->batch each
  *   prefix_lens : device int32 [prefix->batch]
  * Workspace as in reskv_paged_attn (the same one may serve both), of at least
@@ -738,7 +740,7 @@ reskv_status reskv_paged_attn_shared(const reskv_paged_kv* kv, const reskv_paged
  * Query tokens of no sequence are neither read nor written.  Logits are sums of exact
  * products in fp32; statistics and sums are fp32.  The softmax weights are rounded to
  * q's type before they meet the values (16 bits or more with up to 16 query rows a
- * sequence and KV head): half a step of a weight, beside the half step of the output.
+ * sequence and KV head on average): half a step of a weight, beside the half step of the output.
  * A fault (q_begin or kv_begin out of order or outside the rows, kv_lens outside the
  * sequence's rows) is reported and the value taken as the nearest.  Rows on 16-byte
  * boundaries (data and strides) take the fast kernels; others a general one, some
@@ -757,7 +759,7 @@ typedef struct reskv_cross_attn_args {
   const int32_t* kv_begin;             /* the same of the rows of k and v; NULL: n_rows / batch */
   const int32_t* kv_lens;              /* device int32 [batch]; NULL: all rows of a sequence */
   int64_t n_tokens, n_rows;            /* n_tokens * heads and n_rows * n_kv_heads below 2^31 */
-  int32_t batch;
+  int32_t batch;                       /* 1..2^24, batch * n_kv_heads at most 2^28 */
   int32_t head_dim;                    /* 64 or 128                            */
   float scale;                         /* 0: 1 / sqrt(head_dim)                */
   uint32_t* status;                    /* device word for faults, or NULL      */
@@ -780,7 +782,8 @@ size_t reskv_cross_attn_workspace(const reskv_cross_attn_args* args);
  * the sums of d_k and d_v over the sequence's queries and the heads of the KV head.  Rows of a
  * sequence behind kv_lens[b], or that no query sees, get d_k = d_v = 0; rows of no sequence are
  * left as they were.  Sums are fp32 in a fixed order (no atomics); p and t are rounded to q's type before
- * the products that sum them.
+ * the products that sum them, t within its range: in fp16 gradients of 2^-24 and less are 0 (scale d_o, as
+ * training in fp16 does).  What the rounding of o takes from D is put back.
  *   d_o, d_q : q's shape and dtype;  d_k, d_v : k's shape and dtype
  */
 reskv_status reskv_cross_attn_backward(const reskv_cross_attn_args* args, const reskv_heads* d_o,

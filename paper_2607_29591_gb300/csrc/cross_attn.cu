@@ -24,7 +24,8 @@ std::string check_cross(const reskv_cross_attn_args* a) {
   if (a->k.n_heads < 1 || a->v.n_heads != a->k.n_heads) return "k and v must have the same heads";
   if (a->q.n_heads % a->k.n_heads || a->q.n_heads / a->k.n_heads > 64)
     return "q's heads must be a multiple of k's, at most 64 per KV head";
-  if (a->batch < 1 || a->batch > (1 << 24)) return "batch must be in [1, 2^24]";
+  if (a->batch < 1 || a->batch > (1 << 24) || int64_t(a->batch) * a->k.n_heads > (1 << 28))
+    return "batch must be in [1, 2^24], batch * n_kv_heads at most 2^28";
   if (a->n_tokens < 0 || double(a->n_tokens) * a->q.n_heads >= double(int64_t(1) << 31))
     return "n_tokens must not be negative, n_tokens * heads below 2^31";
   if (a->n_rows < 0 || double(a->n_rows) * a->k.n_heads >= double(int64_t(1) << 31))

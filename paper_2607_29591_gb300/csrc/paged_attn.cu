@@ -672,7 +672,7 @@ cudaError_t device_sms(int* dev, int* sms) {
   return *sms < 1 ? cudaErrorInvalidDevice : cudaSuccess;
 }
 
-std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a, size_t workspace) {
+std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
   std::string bad = check_paged(kv);
   if (!bad.empty()) return bad;
   if (!a) return "args is NULL";
@@ -692,10 +692,14 @@ std::string check_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a,
     return "n_tokens * heads / 4 + batch * n_kv_heads must be below 2^24";
   if (!a->q_begin && a->n_tokens % kv->batch) return "n_tokens must be a multiple of batch without q_begin";
   if (a->lse && !aligned_to(a->lse, 4)) return "lse must be 4-byte aligned";
-  if (!a->workspace || !aligned_to(a->workspace, 256) || a->workspace_bytes < workspace)
-    return "workspace must be 256-byte aligned and hold the bytes that the call's _workspace() asks for";
   if (!std::isfinite(a->scale) || a->window < 0) return "scale must be finite and window not negative";
   return "";
+}
+
+// Once the rest is fine: `need` goes by it.
+std::string check_workspace(const reskv_paged_attn_args* a, size_t need, const char* name) {
+  if (a->workspace && aligned_to(a->workspace, 256) && a->workspace_bytes >= need) return "";
+  return std::string("workspace must be 256-byte aligned and hold ") + name + "() bytes";
 }
 
 AttnParams attn_params(const reskv_paged_kv* kv, const reskv_paged_attn_args* a) {
@@ -781,7 +785,8 @@ extern "C" size_t reskv_paged_attn_workspace(const reskv_paged_kv* kv, const res
 extern "C" reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_paged_attn_args* a, void* stream) {
   return no_throw([&]() -> reskv_status {
     if (a && a->n_tokens == 0) return RESKV_OK;
-    const std::string bad = check_attn(kv, a, reskv_paged_attn_workspace(kv, a));
+    std::string bad = check_attn(kv, a);
+    if (bad.empty()) bad = check_workspace(a, reskv_paged_attn_workspace(kv, a), "reskv_paged_attn_workspace");
     if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
     const AttnParams p = attn_params(kv, a);
     int dev = 0, sms = 0;
@@ -874,7 +879,7 @@ std::string check_shared(const reskv_paged_kv* kv, const reskv_paged_kv* prefix,
                          const int32_t* prefix_lens, const reskv_paged_attn_args* a) {
   std::string bad = check_paged(prefix);
   if (!bad.empty()) return "the prefix: " + bad;
-  bad = check_attn(kv, a, reskv_paged_attn_shared_workspace(kv, prefix, a));
+  bad = check_attn(kv, a);
   if (!bad.empty()) return bad;
   if (prefix->head_dim != kv->head_dim || prefix->n_kv_heads != kv->n_kv_heads || prefix->quant_group != kv->quant_group ||
       prefix->page_tokens != kv->page_tokens)
@@ -885,7 +890,7 @@ std::string check_shared(const reskv_paged_kv* kv, const reskv_paged_kv* prefix,
   if (prefix->batch >= kMaxBatch) return "fewer than 1024 prefixes a call";
   if ((double(a->n_tokens) * (a->q.n_heads / kv->n_kv_heads) / 2 + kv->batch + prefix->batch) * kv->n_kv_heads >= double(1 << kUnitBits))
     return "n_tokens * heads / 2 + (batch + prefixes) * n_kv_heads must be below 2^24";
-  return "";
+  return check_workspace(a, reskv_paged_attn_shared_workspace(kv, prefix, a), "reskv_paged_attn_shared_workspace");
 }
 
 }  // namespace
@@ -897,7 +902,10 @@ extern "C" size_t reskv_paged_attn_shared_workspace(const reskv_paged_kv* kv, co
       prefix->batch < 1 || prefix->n_kv_heads != kv->n_kv_heads || a->n_tokens < 0 || a->q.n_heads < 1)
     return 0;
   int dev = 0, sms = 0;
-  if (device_sms(&dev, &sms) != cudaSuccess) cudaGetLastError();
+  if (device_sms(&dev, &sms) != cudaSuccess) {
+    cudaGetLastError();
+    sms = 1;                                      // (no call without a device comes to use it)
+  }
   return shared_layout(kv, prefix, a, sms).bytes;
 }
 
