@@ -23,6 +23,7 @@ struct CrossParams {
   const int32_t* kv_lens;
   uint32_t* status;
   int64_t n_tokens, n_rows;
+  int32_t q_each, kv_each;        // tokens and rows of a sequence without q_begin, kv_begin
   int32_t batch, heads, kv_heads, group;
   int32_t f16;
   float scale, scale2;            // of the logits; times log2 e
@@ -34,23 +35,23 @@ struct CrossSequence {
   int k0, rows, seen;
 };
 
-// Range b of `total` things: begin[b] .. begin[b + 1], or equal shares.
-__device__ __forceinline__ void cross_range(const int32_t* begin, int b, int batch, int64_t total, uint32_t* status,
-                                            int& first, int& count) {
+// Range b of `total` things: begin[b] .. begin[b + 1], or `each`.
+__device__ __forceinline__ void cross_range(const int32_t* begin, int b, int each, int64_t total, uint32_t* status, int& first,
+                                            int& count) {
   if (begin) {
     const int b0 = begin[b], b1 = begin[b + 1], n = int(total);
     if (b0 < 0 || b0 > n || b1 < b0 || b1 > n) report_status(status, kStatusBadIndex);
     first = min(max(b0, 0), n);
     count = min(max(b1, first), n) - first;
   } else {
-    count = int(total / batch);
-    first = b * count;
+    count = each;
+    first = b * each;
   }
 }
 __device__ __forceinline__ CrossSequence cross_sequence(const CrossParams& p, int b) {
   CrossSequence s;
-  cross_range(p.q_begin, b, p.batch, p.n_tokens, p.status, s.q0, s.count);
-  cross_range(p.kv_begin, b, p.batch, p.n_rows, p.status, s.k0, s.rows);
+  cross_range(p.q_begin, b, p.q_each, p.n_tokens, p.status, s.q0, s.count);
+  cross_range(p.kv_begin, b, p.kv_each, p.n_rows, p.status, s.k0, s.rows);
   s.seen = s.rows;
   if (p.kv_lens) {
     const int n = p.kv_lens[b];
@@ -60,14 +61,17 @@ __device__ __forceinline__ CrossSequence cross_sequence(const CrossParams& p, in
   return s;
 }
 
-// The block that a CTA takes: of the `count` tokens (or rows) of every sequence, `times` things each,
-// `per` of those a block, for each KV head; blocks of a KV head lie side by side.  One warp; false: no
-// such block.
+// Whether the lengths are the call's own: then a block is found before the kernel before has ended.
+__device__ __forceinline__ bool cross_fixed(const CrossParams& p) { return !p.q_begin && !p.kv_begin && !p.kv_lens; }
+
+// The block that a CTA takes: of the tokens (or rows) of every sequence, begin[b] .. begin[b + 1] of `total` or
+// `each`, `times` things each, `per` of those a block, for each KV head; blocks of a KV head lie side by
+// side.  One warp; false: no such block.
 struct CrossBlock {
   int b, h, first;                // sequence, KV head, first of its things
 };
-__device__ __forceinline__ bool cross_block(const CrossParams& p, const int32_t* begin, int64_t total, int per, int item, int lane,
-                                            CrossBlock& out, int times = 1) {
+__device__ __forceinline__ bool cross_block(const CrossParams& p, const int32_t* begin, int each, int64_t total, int per, int item,
+                                            int lane, CrossBlock& out, int times = 1) {
   int blocks;
   if (begin) {
     bool found = false;
@@ -75,7 +79,7 @@ __device__ __forceinline__ bool cross_block(const CrossParams& p, const int32_t*
     for (int b0 = 0; b0 < p.batch; b0 += 32) {
       int mine = 0, first, count;
       if (b0 + lane < p.batch) {
-        cross_range(begin, b0 + lane, p.batch, total, p.status, first, count);
+        cross_range(begin, b0 + lane, each, total, p.status, first, count);
         mine = (count * times + per - 1) / per;
       }
       int upto = mine * p.kv_heads;
@@ -97,13 +101,17 @@ __device__ __forceinline__ bool cross_block(const CrossParams& p, const int32_t*
     }
     if (!found) return false;
   } else {
-    blocks = (int(total / p.batch) * times + per - 1) / per;
+    blocks = (each * times + per - 1) / per;
     out.b = item / (blocks * p.kv_heads);
     item -= out.b * blocks * p.kv_heads;
   }
   out.h = item / blocks;
   out.first = (item - out.h * blocks) * per;
   return true;
+}
+// Tiles before rank r's, of `all` (below 2^24) that a cluster of 1, 2, 4 or 8 shares.
+__device__ __forceinline__ int tiles_before(int all, int r, int cluster) {
+  return int(uint32_t(all) * uint32_t(r) >> (cluster >> 1) - (cluster >> 3));
 }
 // Blocks that a call may have.
 inline int64_t cross_blocks(const CrossParams& p, const int32_t* begin, int64_t total, int per, int times = 1) {

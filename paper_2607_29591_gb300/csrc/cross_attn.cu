@@ -55,6 +55,8 @@ CrossParams params_of(const reskv_cross_attn_args* a) {
   p.status = a->status;
   p.n_tokens = a->n_tokens;
   p.n_rows = a->n_rows;
+  p.q_each = int32_t(a->n_tokens / a->batch);
+  p.kv_each = int32_t(a->n_rows / a->batch);
   p.batch = a->batch;
   p.heads = a->q.n_heads;
   p.kv_heads = a->k.n_heads;

@@ -94,17 +94,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
     sh.abort = 0;
     fence_mbar_init();
   }
-  wait_for_previous();
+  if (warp == kCopyWarp && elected()) {
+    fetch_map(&bp.q);
+    fetch_map(&bp.k);
+    fetch_map(&bp.v);
+  }
+  const bool fixed = cross_fixed(p);
+  if (!fixed) wait_for_previous();
 
   // the block: tokens t0 .. of sequence b, KV head h
   const int tt = bp.tile_tokens, block_tokens = (kSplit ? 1 : 2) * tt;
   CrossBlock block;
-  if (!cross_block(p, p.q_begin, p.n_tokens, block_tokens, int(blockIdx.x) / cs, lane, block)) return;      // the whole cluster
+  if (!cross_block(p, p.q_begin, p.q_each, p.n_tokens, block_tokens, int(blockIdx.x) / cs, lane, block)) return;      // the whole cluster
   const int b = block.b, h = block.h, t0 = block.first;
   const CrossSequence sq = cross_sequence(p, b);
   const bool two = !kSplit && t0 + tt < sq.count, joins = kSplit || cs > 1;
   const int all = (sq.seen + kStates - 1) / kStates;
-  const int first = int(int64_t(all) * rank / cs), n = int(int64_t(all) * (rank + 1) / cs) - first;      // tiles of states
+  const int first = tiles_before(all, rank, cs), n = tiles_before(all, rank + 1, cs) - first;      // tiles of states
   const int steps[2] = {kSplit ? (n + 1) / 2 : n, kSplit ? n / 2 : two ? n : 0};
   const int left = sq.seen - (first + n - 1) * kStates;               // states of the last tile
   const bool cut = n > 0 && left < kStates;
@@ -115,6 +121,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
   const bool real = warp < kSoftmaxWarps && row_token < tt && token < sq.count;
   const int head = h * p.group + rt - row_token * p.group;
   if (sq.seen == 0) {                             // the same for the whole cluster
+    if (fixed) wait_for_previous();
     if (real && rank == 0 && (m == 0 || !kSplit)) {
       uint16_t* y = static_cast<uint16_t*>(p.o.data) + (sq.q0 + token) * p.o.token + head * p.o.head + c * (D / 2);
 #pragma unroll 1
@@ -124,6 +131,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
     return;
   }
   if (warp == kIssueWarp) take_columns(smem_u32(&sh.tmem));
+  if (fixed) wait_for_previous();
   fence_before();
   __syncthreads();
   fence_after();

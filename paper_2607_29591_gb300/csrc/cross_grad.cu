@@ -104,7 +104,7 @@ __device__ __forceinline__ void leave_columns(uint32_t at, float4* rows, int r, 
 // The ranks that have tiles, of `all`.
 __device__ __forceinline__ uint32_t ranks_with_tiles(int cs, int all) {
   uint32_t present = 0;
-  for (int k = 0; k < cs; ++k) present |= uint32_t(int64_t(all) * (k + 1) / cs != int64_t(all) * k / cs) << k;
+  for (int k = 0; k < cs; ++k) present |= uint32_t(tiles_before(all, k + 1, cs) != tiles_before(all, k, cs)) << k;
   return present;
 }
 // Where rank k has dims 4u .. of row r.
@@ -187,15 +187,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
     sh.abort = 0;
     fence_mbar_init();
   }
-  wait_for_previous();
+  if (warp == kCopyWarp && elected()) {
+    fetch_map(&gp.q);
+    fetch_map(&gp.g);
+    fetch_map(&gp.k);
+    fetch_map(&gp.v);
+  }
+  const bool fixed = cross_fixed(p);
+  if (!fixed) wait_for_previous();
 
   const int tt = gp.tile_tokens, cs = gp.cluster, rank = cs > 1 ? int(rank_in_cluster()) : 0;
   CrossBlock block;
-  if (!cross_block(p, p.q_begin, p.n_tokens, tt, int(blockIdx.x) / cs, lane, block)) return;      // the whole cluster
+  if (!cross_block(p, p.q_begin, p.q_each, p.n_tokens, tt, int(blockIdx.x) / cs, lane, block)) return;      // the whole cluster
   const int h = block.h, t0 = block.first, used_rows = tt * p.group;
   const CrossSequence sq = cross_sequence(p, block.b);
   const int all = (sq.seen + kTile - 1) / kTile;
-  const int first = int(int64_t(all) * rank / cs), n = int(int64_t(all) * (rank + 1) / cs) - first;      // tiles of states
+  const int first = tiles_before(all, rank, cs), n = tiles_before(all, rank + 1, cs) - first;      // tiles of states
   const int left = sq.seen - (first + n - 1) * kTile;                 // states of the last
   const bool cut = n > 0 && left < kTile;
   // a softmax thread's row, and its half of the columns
@@ -205,10 +212,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
   const int64_t at_token = sq.q0 + token;
   uint16_t* const dq = static_cast<uint16_t*>(p.d_q.data) + (real ? at_token * p.d_q.token + head * p.d_q.head + c * (D / 2) : 0);
   if (all == 0) {                                 // the same for the whole cluster
+    if (fixed) wait_for_previous();
     if (real && rank == 0) store_zeros<D / 2>(dq);
     return;
   }
   if (warp == kIssueWarp) take_columns(smem_u32(&sh.tmem));
+  if (fixed) wait_for_previous();
   fence_before();
   __syncthreads();
   fence_after();
@@ -515,16 +524,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
     sh.abort = 0;
     fence_mbar_init();
   }
-  wait_for_previous();
+  if (warp == kCopyWarp && elected()) {
+    fetch_map(&gp.q);
+    fetch_map(&gp.g);
+    fetch_map(&gp.k);
+    fetch_map(&gp.v);
+  }
+  const bool fixed = cross_fixed(p);
+  if (!fixed) wait_for_previous();
 
   const int cs = gp.cluster, rank = cs > 1 ? int(rank_in_cluster()) : 0;
   CrossBlock block;
-  if (!cross_block(p, p.kv_begin, p.n_rows, kTile, int(blockIdx.x) / cs, lane, block)) return;    // the whole cluster
+  if (!cross_block(p, p.kv_begin, p.kv_each, p.n_rows, kTile, int(blockIdx.x) / cs, lane, block)) return;    // the whole cluster
   const int h = block.h, j0 = block.first;
   const CrossSequence sq = cross_sequence(p, block.b);
   const int tt = gp.tile_tokens, used = tt * p.group;                 // rows of a full tile
   const int all = j0 < sq.seen ? (sq.count + tt - 1) / tt : 0;
-  const int first = int(int64_t(all) * rank / cs), n = int(int64_t(all) * (rank + 1) / cs) - first;      // tiles of rows
+  const int first = tiles_before(all, rank, cs), n = tiles_before(all, rank + 1, cs) - first;      // tiles of rows
   const int left = min((sq.count - (first + n - 1) * tt) * p.group, used);      // rows of the last
   const bool cut = n > 0 && left < used;
   // a softmax thread's state; warps 0-3 write dV, 4-7 dK
@@ -533,10 +549,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
   const CrossRows& to = c ? p.d_k : p.d_v;
   uint16_t* const out = static_cast<uint16_t*>(to.data) + (owned ? (sq.k0 + j) * to.token + h * to.head : 0);
   if (all == 0) {                                 // nobody sees them: the same for the whole cluster
+    if (fixed) wait_for_previous();
     if (owned && rank == 0) store_zeros<D>(out);
     return;
   }
   if (warp == kIssueWarp) take_columns(smem_u32(&sh.tmem));
+  if (fixed) wait_for_previous();
   if (used < kTile && warp < 2 * kStages) {       // rows that no copy writes
     clear_rows<D>(smem + S::at_ring + warp * S::tile, used, kTile, lane);
     fence_proxy_async_smem();

@@ -84,16 +84,22 @@ __global__ void __launch_bounds__(kThreads) k_cross_rows(const __grid_constant__
     sh.abort = 0;
     fence_mbar_init();
   }
+  if (warp == kWarps && elected()) {
+    fetch_map(&rp.k);
+    fetch_map(&rp.v);
+  }
   __syncthreads();
-  wait_for_previous();
+  const bool fixed = cross_fixed(p);
+  if (!fixed) wait_for_previous();
   CrossBlock block;
-  if (!cross_block(p, p.q_begin, p.n_tokens, kRows, int(blockIdx.x) / cs, lane, block, p.group)) return;      // the whole cluster
+  if (!cross_block(p, p.q_begin, p.q_each, p.n_tokens, kRows, int(blockIdx.x) / cs, lane, block, p.group)) return;      // the whole cluster
   const int h = block.h, r0 = block.first;
   const CrossSequence sq = cross_sequence(p, block.b);
   const int rows = min(sq.count * p.group - r0, kRows);               // of this block
   const int all = (sq.seen + kRowStates - 1) / kRowStates;
-  const int first = int(int64_t(all) * rank / cs), n = int(int64_t(all) * (rank + 1) / cs) - first;
+  const int first = tiles_before(all, rank, cs), n = tiles_before(all, rank + 1, cs) - first;
   const uint32_t ring = smem_u32(smem);
+  if (fixed) wait_for_previous();
 
   if (warp == kWarps) {
     // --- copies ---

@@ -105,6 +105,9 @@ __device__ __forceinline__ void give_columns(uint32_t tmem) {
   asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
+__device__ __forceinline__ void fetch_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+}
 // Copy of a box of a tensor [tokens, heads, dims] from element (x, head, token), landing on `bar`.
 __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, int x, int head, int token, uint64_t* bar) {
   asm volatile(
