@@ -1,7 +1,7 @@
 // The small calls' way from torch tensors to the C ABI.  A single token's reskv_rope,
 // reskv_paged_append or reskv_paged_gather is bound by the host: reading the tensors
 // attribute by attribute from Python took 4 of a call's 6.7 us, here the whole call
-// takes 2.2 (append 7.3 -> 2.3, gather 4.9 -> 2.0).  Each function looks its tensors
+// takes 2.2 (append 7.3 -> 2.3, gather 4.9 -> 2.0; cross attention 7.0 -> 3.6).  Each function looks its tensors
 // over, fills the ABI's structs and calls.  It returns the call's status, or -1 without
 // having called where an argument is not of the plain kind; the caller's general path
 // then takes the call or says what is wrong with it.
@@ -18,6 +18,8 @@ struct {
   decltype(&reskv_rope) rope;
   decltype(&reskv_paged_append) append;
   decltype(&reskv_paged_gather) gather;
+  decltype(&reskv_cross_attn) cross;
+  decltype(&reskv_cross_attn_backward) cross_backward;
   PyObject* current_stream;       // torch's: device index -> address
 } g{};
 
@@ -122,18 +124,20 @@ int without_gil(F call) {
   return st;
 }
 
-// addresses of the three entries, torch's current-stream function
+// addresses of the entries, torch's current-stream function
 PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 4) return PyErr_Format(PyExc_TypeError, "setup takes 4 arguments");
-  void* f[3];
-  for (int i = 0; i < 3; ++i) {
+  if (n != 6) return PyErr_Format(PyExc_TypeError, "setup takes 6 arguments");
+  void* f[5];
+  for (int i = 0; i < 5; ++i) {
     f[i] = PyLong_AsVoidPtr(a[i]);
     if (PyErr_Occurred()) return nullptr;
   }
   g.rope = reinterpret_cast<decltype(g.rope)>(f[0]);
   g.append = reinterpret_cast<decltype(g.append)>(f[1]);
   g.gather = reinterpret_cast<decltype(g.gather)>(f[2]);
-  g.current_stream = Py_NewRef(a[3]);
+  g.cross = reinterpret_cast<decltype(g.cross)>(f[3]);
+  g.cross_backward = reinterpret_cast<decltype(g.cross_backward)>(f[4]);
+  g.current_stream = Py_NewRef(a[5]);
   Py_RETURN_NONE;
 }
 
@@ -211,11 +215,67 @@ PyObject* gather(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// q, k, v, o, batch, q_begin, kv_begin, kv_lens, scale, lse, status, stream from a on
+bool cross_of(PyObject* const* a, reskv_cross_attn_args* c, void** stream) {
+  const at::Tensor *q = tensor(a[0]), *k = tensor(a[1]);
+  if (!q || !k || q->dim() != 3 || k->dim() != 3 || q->size(2) > INT_MAX || !PyLong_CheckExact(a[4])) return false;
+  const long batch = PyLong_AsLong(a[4]);
+  if (batch < 1 || batch > INT_MAX - 1) return false;
+  *c = reskv_cross_attn_args{};
+  c->n_tokens = q->size(0);
+  c->n_rows = k->size(0);
+  c->batch = int32_t(batch);
+  c->head_dim = int32_t(q->size(2));
+  const int32_t* status = nullptr;
+  const at::Tensor* lse = a[9] == Py_None ? nullptr : tensor(a[9]);
+  if (!heads_of(a[0], c->n_tokens, -1, c->head_dim, &c->q) || !heads_of(a[1], c->n_rows, -1, c->head_dim, &c->k) ||
+      !heads_of(a[2], c->n_rows, c->k.n_heads, c->head_dim, &c->v) || !heads_of(a[3], c->n_tokens, c->q.n_heads, c->head_dim, &c->o) ||
+      (a[5] != Py_None && !ints_of(a[5], batch + 1, &c->q_begin)) || (a[6] != Py_None && !ints_of(a[6], batch + 1, &c->kv_begin)) ||
+      (a[7] != Py_None && !ints_of(a[7], batch, &c->kv_lens)) || (a[10] != Py_None && !ints_of(a[10], 1, &status)) ||
+      (a[9] != Py_None && (!lse || lse->scalar_type() != at::kFloat || !lse->is_contiguous() || lse->numel() != c->n_tokens * c->q.n_heads)))
+    return false;
+  c->lse = lse ? static_cast<float*>(lse->data_ptr()) : nullptr;
+  c->status = reinterpret_cast<uint32_t*>(const_cast<int32_t*>(status));
+  if (a[8] != Py_None) {
+    c->scale = float(PyFloat_AsDouble(a[8]));
+    if (PyErr_Occurred()) return false;
+  }
+  return stream_of(a[11], q->get_device(), stream);
+}
+
+PyObject* cross(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    reskv_cross_attn_args c;
+    void* stream;
+    if (n != 12 || !g.cross || !cross_of(a, &c, &stream)) return -1;
+    return without_gil([&] { return int(g.cross(&c, stream)); });
+  });
+}
+
+// the same, then workspace, d_o, d_q, d_k, d_v
+PyObject* cross_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    reskv_cross_attn_args c;
+    reskv_heads d_o, d_q, d_k, d_v;
+    void* stream;
+    if (n != 17 || !g.cross_backward || !cross_of(a, &c, &stream)) return -1;
+    const at::Tensor* w = tensor(a[12]);
+    if (!w || !w->is_contiguous() || !heads_of(a[13], c.n_tokens, c.q.n_heads, c.head_dim, &d_o) ||
+        !heads_of(a[14], c.n_tokens, c.q.n_heads, c.head_dim, &d_q) || !heads_of(a[15], c.n_rows, c.k.n_heads, c.head_dim, &d_k) ||
+        !heads_of(a[16], c.n_rows, c.k.n_heads, c.head_dim, &d_v))
+      return -1;
+    c.workspace = w->data_ptr();
+    c.workspace_bytes = size_t(w->nbytes());
+    return without_gil([&] { return int(g.cross_backward(&c, &d_o, &d_q, &d_k, &d_v, stream)); });
+  });
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr};
 }
-PyMethodDef methods[] = {method<setup>("setup"), method<rope>("rope"), method<append>("append"), method<gather>("gather"), {}};
+PyMethodDef methods[] = {method<setup>("setup"), method<rope>("rope"), method<append>("append"), method<gather>("gather"),
+                        method<cross>("cross"), method<cross_backward>("cross_backward"), {}};
 PyModuleDef module{PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

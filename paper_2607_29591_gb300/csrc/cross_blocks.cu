@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
       auto issue_s = [&](int s, int op) {
         fence_after();
         if (elected()) {
-          const uint32_t q0 = operand(smem_q + (kSplit ? 0 : s) * S::tile), k0 = operand(ring + op % S::slots * S::tile);
+          const uint32_t q0 = cluster_operand(smem_q + (kSplit ? 0 : s) * S::tile), k0 = cluster_operand(ring + op % S::slots * S::tile);
 #pragma unroll
           for (int k = 0; k < D / 16; ++k)
             multiply<kRows128>(s_cols(s), q0 + (((k / 4) * S::half + (k & 3) * 32) >> 4),

@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
       auto outer = [&](uint32_t d, uint32_t a, uint32_t b, uint64_t* bar) {      // [128 x 128] = A B^T over D dims
         fence_after();
         if (elected()) {
-          const uint32_t a0 = operand(a), b0 = operand(b);
+          const uint32_t a0 = cluster_operand(a), b0 = cluster_operand(b);
 #pragma unroll
           for (int k = 0; k < D / 16; ++k)
             multiply<kRows128, kLogits>(d, a0 + (((k / 4) * kHalf + (k & 3) * 32) >> 4), b0 + (((k / 4) * kHalf + (k & 3) * 32) >> 4),
@@ -611,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
       auto outer = [&](uint32_t d, uint32_t a, uint32_t b, uint64_t* bar) {      // [128 x 128] = A B^T over D dims
         fence_after();
         if (elected()) {
-          const uint32_t a0 = operand(a), b0 = operand(b);
+          const uint32_t a0 = cluster_operand(a), b0 = cluster_operand(b);
 #pragma unroll
           for (int k = 0; k < D / 16; ++k)
             multiply<kRows128, kLogits>(d, a0 + (((k / 4) * kHalf + (k & 3) * 32) >> 4), b0 + (((k / 4) * kHalf + (k & 3) * 32) >> 4),

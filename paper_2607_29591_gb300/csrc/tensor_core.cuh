@@ -14,9 +14,11 @@ namespace tc {
 // word, beside a constant; in the high word the distance of groups of eight rows
 // / 16, version 1 and the swizzle.  Rows of 128 bytes (64 fp16) have the 128-byte
 // swizzle (16-byte word w of row r at w ^ (r & 7)); rows of 32 bytes (one step) the
-// 32-byte swizzle (w at w ^ ((r >> 2) & 1)).  The address is that within the CTA: in a cluster the
-// rank stands above it, where a descriptor has other fields.
-__device__ __forceinline__ uint32_t operand(uint32_t saddr) { return ((saddr & 0x3ffffu) >> 4) | (1u << 16); }
+// 32-byte swizzle (w at w ^ ((r >> 2) & 1)).
+__device__ __forceinline__ uint32_t operand(uint32_t saddr) { return (saddr >> 4) | (1u << 16); }
+// The same in a cluster, where a shared address has the CTA's rank above its 18 bits and a descriptor other
+// fields there (an operand that lies across took its distances from the rank).
+__device__ __forceinline__ uint32_t cluster_operand(uint32_t saddr) { return operand(saddr & 0x3ffffu); }
 constexpr uint32_t kRows128 = (1024 >> 4) | (1u << 14) | (2u << 29);
 // An operand that lies the other way round (a row holds 64 neighbours of the product's rows or
 // columns, for one term of its sums): groups of eight such rows follow each other as above, `next64`

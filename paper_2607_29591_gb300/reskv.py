@@ -613,7 +613,8 @@ def _calls():
         from . import _bind as bind
         if _kinds[2] is not None:
             bind.setup(*(ctypes.cast(f, ctypes.c_void_p).value for f in
-                         (lib.reskv_rope, lib.reskv_paged_append, lib.reskv_paged_gather)), _kinds[2])
+                         (lib.reskv_rope, lib.reskv_paged_append, lib.reskv_paged_gather, lib.reskv_cross_attn,
+                          lib.reskv_cross_attn_backward)), _kinds[2])
             _bind = bind
         _direct = lib
     return _direct
@@ -1002,10 +1003,17 @@ def reskv_cross_attn(q, k, v, o, batch: int = 1, q_begin=None, kv_begin=None, kv
     float32 [T, heads] for ln sum exp, which the gradient needs, or None.  status: int32 [1]
     that begins or lengths outside their range set to 2.
     """
+    if _bind is not None:
+        st = _bind.cross(q, k, v, o, batch, q_begin, kv_begin, kv_lens, scale, lse, status, stream)
+        if st >= 0:
+            return _check(st) if st else None
     a = _cross(q, k, v, o, batch, q_begin, kv_begin, kv_lens, scale, lse, status)
     st = _calls().reskv_cross_attn(a, _stream_of(stream, q))
     if st:
         _check(st)
+
+
+_cross_workspace = {}                            # bytes by (query tokens, heads)
 
 
 def reskv_cross_attn_workspace(n_tokens: int, heads: int) -> int:
@@ -1028,13 +1036,19 @@ def reskv_cross_attn_backward(q, k, v, o, lse, d_o, d_q, d_k, d_v, batch: int = 
     lib = _calls()
     s = _stream_of(stream, q)
     T = q.shape[0]
-    if workspace is None:
-        workspace = _kept_workspace(lib, q, s, reskv_cross_attn_workspace(T, q.shape[1]) if q.dim() == 3 else 0,
-                                    "reskv_cross_attn_workspace()")
-    elif not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous CUDA tensor")
     if lse is None:
         raise ValueError("the gradient needs the lse of reskv_cross_attn")
+    if workspace is None:
+        need = _cross_workspace.get(key := (T, q.shape[1]))
+        if need is None:
+            need = _cross_workspace[key] = reskv_cross_attn_workspace(*key)
+        workspace = _kept_workspace(lib, q, s, need, "reskv_cross_attn_workspace()")
+    elif not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor")
+    if _bind is not None:
+        st = _bind.cross_backward(q, k, v, o, batch, q_begin, kv_begin, kv_lens, scale, lse, status, s, workspace, d_o, d_q, d_k, d_v)
+        if st >= 0:
+            return _check(st) if st else None
     a = _cross(q, k, v, o, batch, q_begin, kv_begin, kv_lens, scale, lse, status, workspace)
     H, d, rows, kv = q.shape[1], q.shape[2], k.shape[0], k.shape[1]
     st = lib.reskv_cross_attn_backward(a, _pack_heads(*_heads(d_o, "d_o", T, H, d)),
