@@ -18,6 +18,10 @@
 // were summed with atomics.  Heads of a KV head are rows of one sum.  P and T are rounded to q's
 // type (half a step of themselves; P times 2^12 in fp16, whose range ends at 2^-24), sums are fp32.
 //
+// Bound by the products: 4 x 2048 tokens of 32 heads over up to 4097 states (1.5 TFLOP in the eight products)
+// 1.07 ms, 1.4 PFLOP/s; without exponentials, sums and roundings 1.0.  A tile's two pairs of products run while
+// the weights of the other pair are formed; tensor memory (S, G and two sums) is full at d = 128.
+//
 // Where there are too few blocks for the SMs, a cluster of CTAs shares a block's tiles: each leaves its two
 // sums in shared memory, where the cluster adds them up in order.
 //

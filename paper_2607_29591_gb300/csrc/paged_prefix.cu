@@ -26,6 +26,12 @@
 // s n + m are rounded to 11 bits, no coarser than the 16-bit types of the output.  Their
 // power of two goes into the weight's exponent (c), and the reference follows the largest
 // logit + c; the sum of the weights takes 2^-c back.  Positions that do not exist have c = -inf.
+//
+// A tile takes 1.4 us with one block of rows or two (some 1700 instructions a scheduler, unpacking and softmax
+// about half each; the products alone 0.75), a CTA some 15 beside its tiles: the plan, the queries, the first
+// tile, and 128 KB of records.  32 sequences of 4 rows behind 131072 positions 185 us, 64 behind 8192 42 with
+// their own tokens beside them.  What runs once is kept in short loops: unrolled, reading the queries took
+// 5 us and all of a CTA's beginning and end 23, for the instructions' sake.
 #include <atomic>
 
 #include "paged_attn.cuh"

@@ -200,6 +200,92 @@ def test_peaked_and_flat_queries(n):
     Case(10, [n], [300], 1, 2, 64, "bf16", scale=-0.3).check()
 
 
+def test_negative_scale_of_either_type():
+    Case(18, [40], [300], 1, 2, 64, "f16", scale=-0.4).check()
+    Case(19, [2], [300], 1, 2, 128, "f16", scale=-0.4).check()
+
+
+@pytest.mark.parametrize("n", [1, 50])
+def test_heads_before_tokens(n):
+    """Rows as [head, token, dim] and with gaps: the same bits as from packed rows."""
+    c = Case(20, [n, n], [200, 131], 2, 4, 128, "bf16", form="padded", pad=200)
+    o, lse = c.forward()
+    grads = c.backward(o, lse)
+    turned = lambda t: t.transpose(0, 1).contiguous().transpose(0, 1)  # noqa: E731
+    wide = lambda t: torch.cat([t, t, t], 2)[:, :, :t.shape[2]]  # noqa: E731
+    for lay in (turned, wide):
+        q, k, v, g = (lay(t) for t in (c.q, c.k, c.v, c.g))
+        o2, lse2 = lay(torch.zeros_like(o)), torch.zeros_like(lse)
+        assert o2.stride() != o.stride() or n == 1
+        R.reskv_cross_attn(q, k, v, o2, lse=lse2, **c.args)
+        assert torch.equal(o2, o) and torch.equal(lse2, lse)
+        out = [lay(torch.zeros_like(t)) for t in grads]
+        R.reskv_cross_attn_backward(q, k, v, o2, lse2, g, *out, **c.args)
+        for a, b in zip(out, grads):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n", [2, 60])
+def test_broadcast_heads(n):
+    """One head of keys and values for all (a head stride of 0), the general path, against the same rows copied."""
+    c = Case(21, [n], [90], 1, 1, 64, "bf16")
+    q = torch.randn((n, 4, 64), device="cuda").bfloat16()
+    one, four = c.k.expand(-1, 4, -1), c.k.repeat(1, 4, 1)
+    a, b = torch.empty_like(q), torch.empty_like(q)
+    R.reskv_cross_attn(q, one, one, a)
+    R.reskv_cross_attn(q, four, four, b)
+    assert float((a.float() - b.float()).abs().max()) <= 2.0 ** -7 * 5            # two roundings each of values within 5
+
+
+def test_no_states_and_no_tokens():
+    q, none = torch.randn((3, 4, 64), device="cuda").half(), torch.empty((0, 2, 64), dtype=torch.float16, device="cuda")
+    o, lse, dq = torch.full_like(q, 7), torch.zeros((3, 4), device="cuda"), torch.full_like(q, 7)
+    R.reskv_cross_attn(q, none, none, o, lse=lse)
+    assert (o == 0).all() and (lse == -np.inf).all()
+    R.reskv_cross_attn_backward(q, none, none, o, lse, q, dq, none, none)
+    assert (dq == 0).all()
+    k = torch.randn((5, 2, 64), device="cuda").half()
+    empty, dk, dv = q[:0], torch.full_like(k, 7), torch.full_like(k, 7)
+    R.reskv_cross_attn(empty, k, k, empty, lse=lse[:0])
+    R.reskv_cross_attn_backward(empty, k, k, empty, lse[:0], empty, empty, dk, dv)
+    assert (dk == 0).all() and (dv == 0).all()
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_offsets_past_32_bits(n):
+    """Rows 2^20 elements apart: 3000 of them reach past 2^31 elements and 2^32 bytes."""
+    c = Case(22, [n], [3000], 1, 2, 128, "bf16", form="equal", pad=3000)
+    o, lse = c.forward()
+    grads = c.backward(o, lse)
+    far = lambda: torch.empty(3000 << 20, dtype=torch.bfloat16, device="cuda").as_strided((3000, 1, 128), (1 << 20, 128, 1))  # noqa: E731
+    k, v, dk, dv = far(), far(), far(), far()
+    k.copy_(c.k)
+    v.copy_(c.v)
+    o2, lse2, dq = torch.empty_like(o), torch.empty_like(lse), torch.empty_like(o)
+    R.reskv_cross_attn(c.q, k, v, o2, lse=lse2)
+    R.reskv_cross_attn_backward(c.q, k, v, o2, lse2, c.g, dq, dk, dv)
+    assert torch.equal(o2, o) and torch.equal(dq, grads[0]) and torch.equal(dk, grads[1]) and torch.equal(dv, grads[2])
+
+
+def test_two_streams_at_once():
+    cases = [Case(23 + i, [n], [700], 2, 2, 128, "bf16") for i, n in enumerate((1, 30, 300))]
+    want = [(c.forward(), c) for c in cases]
+    want = [(f, c.backward(*f)) for f, c in want]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = []
+    for _ in range(4):
+        got = []
+        for c, s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                f = c.forward()
+                got.append((f, c.backward(*f)))
+    torch.cuda.synchronize()
+    for (f, g), (f2, g2) in zip(want, got):
+        for a, b in zip((*f, *g), (*f2, *g2)):
+            assert torch.equal(torch.nan_to_num(a.float()), torch.nan_to_num(b.float()))
+
+
 def test_longer_states():
     Case(11, [1, 2], [3000, 1111], 2, 4, 128, "bf16").check()
     Case(12, [70], [1500], 2, 1, 64, "f16").check()

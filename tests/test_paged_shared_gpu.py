@@ -137,6 +137,113 @@ def test_agrees_with_one_long_sequence():
     assert float((a - b).abs().max()) <= 2.0 ** -16 * 40              # two fp32 results, values within 40
 
 
+@pytest.mark.parametrize("batch", [3, 20])
+def test_long_prefixes(batch):
+    """Many tiles a CTA, for one block of rows and for two."""
+    case(17, [3000], [4 + i for i in range(batch)], [batch], 1, kv=1, per=4, group=64)
+    case(18, [2500, 40], [4 + i for i in range(2 * batch)], [batch, batch], 1, kv=1, per=16, d=64, group=32, dtype="f16")
+
+
+@pytest.mark.parametrize("batch,scale", [(40, 1e-20), (40, 1e9), (3, 1e9)])
+def test_values_and_keys_of_any_size(batch, scale):
+    """Tokens far larger and far smaller than their neighbours, in keys that queries avoid and in values."""
+    rng = np.random.default_rng(19)
+    kv, d, n = 1, 128, 200
+    prefix, _, _, _ = paged(rng, [0], kv, d, 32, 16, extra_pages=13, table_pages=13)
+    prefix.page_table.copy_(torch.arange(13, dtype=torch.int32)[None])
+    own, _, _, _ = paged(rng, [0] * batch, kv, d, 32, 16, extra_pages=batch, table_pages=1)
+    own.page_table.copy_(torch.arange(batch, dtype=torch.int32)[:, None])
+    k, v = rng.standard_normal((2, n, kv, d)).astype(np.float32) * np.float32(scale)
+    k[..., 0], v[7::16] = 0, v[7::16] * 1e8                               # channel 0 alone tells the large keys
+    k[7::16] = 0
+    k[7::16, :, 0] = -60 * scale
+    ints = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    kt, vt = torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda()
+    R.reskv_paged_append(prefix, kt, vt, ints(np.zeros(n)), ints(np.arange(n)))
+    R.reskv_paged_append(own, kt[:batch].contiguous(), vt[:batch].contiguous(), ints(np.arange(batch)), ints(np.zeros(batch)))
+    held = [torch.empty((1, kv, n, d), device="cuda") for _ in range(2)]
+    R.reskv_paged_gather(prefix, ints([n]), *held)
+    mine = [torch.empty((batch, kv, 1, d), device="cuda") for _ in range(2)]
+    R.reskv_paged_gather(own, ints(np.ones(batch)), *mine)
+    q = rng.standard_normal((batch, 2, d)) / scale
+    q[..., 0] = 20 / scale                                                # the large tokens' weights vanish
+    q, q64 = as_type(q, "bf16")
+    o, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    R.reskv_paged_attn_shared(own, prefix, q, ints(np.ones(batch)), ints([n]), o, lse=lse)
+    for kvc in (own, prefix):
+        kvc.check_status()
+    f64 = lambda t: t.double().cpu().numpy()  # noqa: E731
+    for b in range(batch):
+        kk, vv = (np.concatenate([f64(h[0]), f64(m[b])], 1) for h, m in zip(held, mine))
+        ro, rl, xm, _ = co.attend(q64[b:b + 1], kk, vv, d ** -0.5)
+        # in units of the values that count: weights of the large ones are below 2^-100
+        small = np.abs(vv[:, np.abs(vv).max((0, 2)) < 100 * scale]).max()
+        share = 2 * d * 2.0 ** -23 * xm + 2.0 ** -10 + 2.0 ** -16
+        tol = (share * small)[..., None] + HALF_ULP["bf16"] * np.abs(ro) * 1.01 + 2.0 ** -120
+        worst = (np.abs(f64(o)[b:b + 1] - ro) - tol).max() / small
+        assert worst <= 0
+        assert (np.abs(f64(lse)[b:b + 1] - rl) <= d * 2.0 ** -23 * xm + 2.0 ** -12 + 2.0 ** -22 * np.abs(rl)).all()
+
+
+@pytest.mark.parametrize("batch", [3, 24])
+def test_nan_held_in_a_prefix_reaches_its_group_alone(batch):
+    rng = np.random.default_rng(20)
+    ints = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    prefix, _, pages, table = paged(rng, [70, 50], 1, 128, 32, 16)
+    own, _, _, _ = paged(rng, [9] * 2 * batch, 1, 128, 32, 16)
+    bad = torch.zeros((1, 1, 128), device="cuda")
+    bad[..., 40] = float("nan")
+    good = torch.zeros_like(bad)
+    R.reskv_paged_append(prefix, good, bad, ints([1]), ints([33]))
+    q, _ = as_type(rng.standard_normal((2 * batch, 4, 128)), "bf16")
+    o = torch.empty_like(q)
+    R.reskv_paged_attn_shared(own, prefix, q, ints([9] * 2 * batch), ints([70, 50]), o)
+    nan = torch.isnan(o)
+    assert not nan[:batch].any()
+    assert nan[batch:, :, 32:64].all() and not nan[batch:, :, :32].any() and not nan[batch:, :, 64:].any()
+    # behind the prefix's end it is nobody's
+    R.reskv_paged_attn_shared(own, prefix, q, ints([9] * 2 * batch), ints([70, 33]), o)
+    assert not torch.isnan(o).any()
+
+
+@pytest.mark.parametrize("batch", [3, 24])
+def test_pages_past_32_bits(batch):
+    """The same prefix in the first and in the last pages of more than 4 GB."""
+    rng = np.random.default_rng(21)
+    ints = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    near, _, pages, table = paged(rng, [130], 2, 128, 32, 64)
+    own, _, _, _ = paged(rng, [5] * batch, 2, 128, 32, 64)
+    n = (1 << 32) // pages[0].size + 10
+    big = torch.zeros((n, *pages.shape[1:]), dtype=torch.uint8, device="cuda")
+    last = ints([[n - 1, n - 3, n - 2]])
+    big[last[0].long()] = near.pages[near.page_table[0, :3].long()]
+    far = R.PagedKV(big, last, 64, 2, 128, 32)
+    q, _ = as_type(rng.standard_normal((batch, 8, 128)), "f16")
+    a, b = torch.empty_like(q), torch.empty_like(q)
+    R.reskv_paged_attn_shared(own, near, q, ints([5] * batch), ints([130]), a)
+    R.reskv_paged_attn_shared(own, far, q, ints([5] * batch), ints([130]), b)
+    far.check_status()
+    assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("batch", [3, 24])
+def test_any_rows_of_queries_and_outputs(batch):
+    """Strided and unaligned queries and outputs, the same bits."""
+    rng = np.random.default_rng(22)
+    ints = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    prefix, _, _, _ = paged(rng, [100], 2, 64, 32, 16)
+    own, _, _, _ = paged(rng, [5] * batch, 2, 64, 32, 16)
+    q, _ = as_type(rng.standard_normal((batch, 8, 64)), "bf16")
+    want = torch.empty_like(q)
+    R.reskv_paged_attn_shared(own, prefix, q, ints([5] * batch), ints([100]), want)
+    for pad in (1, 8):
+        wide = torch.zeros((batch, 8, 64 + pad), dtype=q.dtype, device="cuda")
+        wide[..., :64] = q
+        out = torch.zeros_like(wide)
+        R.reskv_paged_attn_shared(own, prefix, wide[..., :64], ints([5] * batch), ints([100]), out[..., :64])
+        assert torch.equal(out[..., :64], want) and (out[..., 64:] == 0).all()
+
+
 def test_faults_are_reported_and_bounded():
     rng = np.random.default_rng(15)
     prefix, _, _, _ = paged(rng, [60, 60], 2, 128, 32, 32)
