@@ -76,11 +76,11 @@ struct RowCursor {
   RowBlock k;
   int64_t start;                                  // the unit's first tile among all
 
-  __device__ __forceinline__ void block(const AttnParams& p) {
+  __device__ __forceinline__ void block(const Params<kShared>& p) {
     const int rows = s.count * p.group;
     k = row_block(p, s, r0, min(r0 + R, rows));
   }
-  __device__ void locate(const AttnParams& p, const int64_t* prefix, int64_t x) {
+  __device__ void locate(const Params<kShared>& p, const int64_t* prefix, int64_t x) {
     int lo = 0, hi = p.batch;                     // tiles before lo <= x < tiles before hi
 #pragma unroll 1
     while (hi - lo > 1) {
@@ -103,7 +103,7 @@ struct RowCursor {
     start = x - tile;
   }
   // To the beginning of unit i, which exists.
-  __device__ void locate_unit(const AttnParams& p, const int64_t* prefix, int64_t i) {
+  __device__ void locate_unit(const Params<kShared>& p, const int64_t* prefix, int64_t i) {
     int lo = 0, hi = p.batch;
 #pragma unroll 1
     while (hi - lo > 1) {
@@ -127,7 +127,7 @@ struct RowCursor {
     h = left;
     start += int64_t(h) * k.tiles;
   }
-  __device__ void next(const AttnParams& p, const int64_t* prefix) {
+  __device__ void next(const Params<kShared>& p, const int64_t* prefix) {
     start += k.tiles;
     tile = 0;
     if (++h < p.kv_heads) return;
@@ -173,7 +173,7 @@ __device__ __forceinline__ void copy_tile(void* dst, const void* src, uint32_t b
 }
 
 template <int D, int NG, bool kTwoPlanes, int R, bool kShared>
-__global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __grid_constant__ AttnParams p) {
+__global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __grid_constant__ Params<kShared> p) {
   using S = AttnSmem<D, NG, R>;
   using Cursor = RowCursor<R, kShared>;
   constexpr int kRows = R;
@@ -296,6 +296,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     const int64_t page_bytes = int64_t(p.kv_heads) * tpp * TB;
     const uint8_t* head = p.pages;                // the unit's head in page 0
     int64_t n_pages = p.n_pages;
+    uint32_t* status = p.status;
     const uint8_t* src = head;                    // the next tile
     int in_unit = 0, in_page = 0;                 // tiles left of the unit and of the page, the next one included
     bool ok = false;                              // the page exists
@@ -303,7 +304,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     const int32_t* ask = p.page_table;
     auto turn_page = [&]() {                      // to `page`
       ok = uint32_t(page) < uint32_t(n_pages);
-      if (!ok) report_status(kShared && c.s.all ? p.prefix_status : p.status, kStatusBadIndex);
+      if (!ok) report_status(status, kStatusBadIndex);
       src = head + (ok ? page : 0) * page_bytes;
       in_page = tpp;
       ++ask;
@@ -312,14 +313,14 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     auto begin_unit = [&]() {
       in_unit = c.k.tiles - c.tile;
       const int tile = c.k.first + c.tile, at = tile / tpp, first = tile - at * tpp;
-      if (kShared && c.s.all) {
-        head = p.prefix_data + int64_t(c.h) * tpp * TB;
-        ask = p.prefix_table + int64_t(c.b - p.own) * p.prefix_pages + at;
-        n_pages = p.prefix_n_pages;
+      head = p.pages + int64_t(c.h) * tpp * TB;
+      if constexpr (kShared) {
+        n_pages = c.s.all ? p.prefix_n_pages : p.n_pages;
+        status = c.s.all ? p.prefix_status : p.status;
+        if (c.s.all) head = p.prefix_data + int64_t(c.h) * tpp * TB;
+        ask = c.s.all ? p.prefix_table + int64_t(c.b - p.own) * p.prefix_pages + at : p.page_table + int64_t(c.b) * p.table_pages + at;
       } else {
-        head = p.pages + int64_t(c.h) * tpp * TB;
         ask = p.page_table + int64_t(c.b) * p.table_pages + at;
-        if (kShared) n_pages = p.n_pages;
       }
       page = *ask;
       in_unit += first;                           // as from the page's first tile
@@ -393,8 +394,8 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
         const int u = int(i % (D / 4));
         const int64_t hr = i / (D / 4);
         const int h = int(hr / r1), r = int(hr - int64_t(h) * r1);
-        store_out(p, s, h, r, u, make_float4(0.f, 0.f, 0.f, 0.f));
-        if (u == 0) store_lse(p, s, h, r, -INFINITY);
+        store_out<kShared>(p, s, h, r, u, make_float4(0.f, 0.f, 0.f, 0.f));
+        if (u == 0) store_lse<kShared>(p, s, h, r, -INFINITY);
       }
     }
     if (!active) return;
@@ -476,11 +477,11 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
           const float4 v = make_float4(st.out(b, 0, j), st.out(b, 1, j), st.out(b, 2, j), st.out(b, 3, j));
           const int u = 8 * st.block(b) + st.g;
           if (!unit) *reinterpret_cast<float4*>(rec + r * RS + 4 * u) = v;
-          else if (c.r0 + r < rows) store_out(p, c.s, c.h, c.r0 + r, u, v);
+          else if (c.r0 + r < rows) store_out<kShared>(p, c.s, c.h, c.r0 + r, u, v);
         }
         if (st.g == 0 && st.half == 0) {
           if (!unit) refs[(2 * warp + slot) * kRows + r] = st.ref[j];
-          else if (c.r0 + r < rows) store_lse(p, c.s, c.h, c.r0 + r, st.ref[j]);
+          else if (c.r0 + r < rows) store_lse<kShared>(p, c.s, c.h, c.r0 + r, st.ref[j]);
         }
       }
       if (!unit && lane == 0) info[2 * warp + slot] = RecordInfo{c.start, c.s, c.k.tiles, c.r0, c.h, 1};
@@ -538,8 +539,8 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     }
     a = all_lanes(a, lanes);
     if (!cut(ri)) {
-      if (every == 0) store_out(p, ri.s, ri.h, ri.r0 + row, u, a);
-      if (lane == 0 && u == 0) store_lse(p, ri.s, ri.h, ri.r0 + row, j.ref);
+      if (every == 0) store_out<kShared>(p, ri.s, ri.h, ri.r0 + row, u, a);
+      if (lane == 0 && u == 0) store_lse<kShared>(p, ri.s, ri.h, ri.r0 + row, j.ref);
     } else {
       float* rec = p.partials + (cta * 2 + (ri.start >= c0 ? 1 : 0)) * (RF + kRows);
       if (every == 0) *reinterpret_cast<float4*>(rec + row * RS + 4 * u) = a;
@@ -603,8 +604,8 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
         all = k;
       }
     }
-    if (every2 == 0) store_out(p, ri.s, ri.h, ri.r0 + row2, u2, a);
-    if (lane == 0 && u2 == 0) store_lse(p, ri.s, ri.h, ri.r0 + row2, all.ref);
+    if (every2 == 0) store_out<kShared>(p, ri.s, ri.h, ri.r0 + row2, u2, a);
+    if (lane == 0 && u2 == 0) store_lse<kShared>(p, ri.s, ri.h, ri.r0 + row2, all.ref);
   }
 }
 
@@ -625,7 +626,7 @@ constexpr int kMaxBatch = 1024;                   // of a launch: the cut is wor
 constexpr size_t kTicketBytes = kMaxCtas * 4;
 
 template <int D, int NG, bool kTwoPlanes, int R, bool kShared>
-cudaError_t launch_rows(const AttnParams& p, int dev, int ctas, cudaStream_t s) {
+cudaError_t launch_rows(const Params<kShared>& p, int dev, int ctas, cudaStream_t s) {
   // the kernel's shared memory limit, raised once a device
   static std::atomic<uint64_t> raised{0};
   const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
@@ -640,7 +641,7 @@ cudaError_t launch_rows(const AttnParams& p, int dev, int ctas, cudaStream_t s) 
 }
 
 template <bool kTwoPlanes, int R, bool kShared>
-cudaError_t dispatch_rows(const AttnParams& p, int d, int group, int dev, int ctas, cudaStream_t s) {
+cudaError_t dispatch_rows(const Params<kShared>& p, int d, int group, int dev, int ctas, cudaStream_t s) {
   if (d == 128 && group == 32) return launch_rows<128, 4, kTwoPlanes, R, kShared>(p, dev, ctas, s);
   if (d == 128 && group == 64) return launch_rows<128, 2, kTwoPlanes, R, kShared>(p, dev, ctas, s);
   if (d == 128) return launch_rows<128, 1, kTwoPlanes, R, kShared>(p, dev, ctas, s);
@@ -730,7 +731,6 @@ AttnParams attn_params(const reskv_paged_kv* kv, const reskv_paged_attn_args* a)
   p.q_f16 = a->q.dtype == RESKV_F16;
   p.q_wide = rows_aligned(a->q, 16);
   p.o_wide = rows_aligned(a->o, size_t(4 * dtype_size(a->o.dtype)));
-  p.lse_unit = 0.693147180559945f;
   p.tickets = static_cast<int32_t*>(a->workspace);
   p.partials = reinterpret_cast<float*>(static_cast<char*>(a->workspace) + kTicketBytes);
   return p;
@@ -849,7 +849,7 @@ int own_sms(const reskv_paged_kv* kv, const reskv_paged_kv* prefix, const reskv_
 }
 
 struct SharedLayout {             // of the workspace, in bytes from its start
-  size_t own, own_ref, prefix, prefix_ref, plans, bytes;
+  size_t own, own_lse, prefix, prefix_ref, plans, bytes;
 };
 size_t padded(size_t n) { return (n + 255) / 256 * 256; }
 SharedLayout shared_layout(const reskv_paged_kv* kv, const reskv_paged_kv* prefix, const reskv_paged_attn_args* a, int sms) {
@@ -861,8 +861,8 @@ SharedLayout shared_layout(const reskv_paged_kv* kv, const reskv_paged_kv* prefi
   }
   SharedLayout l{};
   l.own = padded(kTicketBytes + records);
-  l.own_ref = l.own + padded(rows * kv->head_dim * 4);
-  l.prefix = l.own_ref + padded(rows * 4);
+  l.own_lse = l.own + padded(rows * kv->head_dim * 4);
+  l.prefix = l.own_lse + padded(rows * 4);
   size_t held = rows;
   if (prefix_in_blocks(prefix, a)) {
     const int block = 128 * prefix_mt(prefix, a);
@@ -926,13 +926,13 @@ extern "C" reskv_status reskv_paged_attn_shared(const reskv_paged_kv* kv, const 
     const AttnParams call = attn_params(kv, a);
     AttnParams p = call;
     p.o = ws + l.own;
-    p.lse = reinterpret_cast<float*>(ws + l.own_ref);
+    p.lse = reinterpret_cast<float*>(ws + l.own_lse);
     p.o_f32 = p.o_wide = 1;
     p.o_head = kv->head_dim;
     p.o_token = int64_t(p.heads) * kv->head_dim;
-    p.lse_unit = 1.f;
     // the prefix: a group's query tokens are one sequence's that all see all
-    AttnParams g = p;
+    SharedParams g{};
+    static_cast<AttnParams&>(g) = p;
     g.sequences = kv->batch;
     g.seq_begin = seq_begin;
     g.prefix_lens = prefix_lens;
@@ -975,9 +975,8 @@ extern "C" reskv_status reskv_paged_attn_shared(const reskv_paged_kv* kv, const 
     j.a.o_head = call.o_head;
     j.a.o_f32 = call.o_f32;
     j.a.o_wide = call.o_wide;
-    j.a.lse_unit = call.lse_unit;
     j.own = static_cast<const float*>(p.o);
-    j.own_ref = p.lse;
+    j.own_lse = p.lse;
     j.prefix = g.prefix_o;
     j.prefix_ref = g.prefix_ref;
     j.plans = blocks ? plans : nullptr;

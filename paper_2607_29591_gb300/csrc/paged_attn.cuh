@@ -2,6 +2,8 @@
 // and the matrix step of one 16-token tile, shared by the kernels of
 // paged_attn*.cu.
 #pragma once
+#include <type_traits>
+
 #include "paged.cuh"
 #include "warp_mma.cuh"
 
@@ -23,7 +25,10 @@ struct AttnParams {
   int32_t batch, table_pages, page_tokens, kv_heads, heads, group;
   int32_t window, q_f16, o_f32, q_wide, o_wide;
   float scale2;                   // scale * log2 e
-  float lse_unit;                 // what lse holds of a log2 of a sum: ln 2 of it, or all
+};
+
+// The same of a call with a shared prefix.
+struct SharedParams : AttnParams {
   // Prefixes that groups of the call's `sequences` share: behind `own` sequences `batch` holds groups,
   // whose query tokens all see all of the group's positions.  What is the groups':
   int32_t sequences, own;
@@ -37,6 +42,9 @@ struct AttnParams {
   float* prefix_o;                // fp32 rows [token][head][dim], o_head elements each
   float* prefix_ref;              // log2 sums
 };
+
+template <bool kShared>
+using Params = std::conditional_t<kShared, SharedParams, AttnParams>;
 
 // One block of query rows of one sequence: row r of the sequence is query token
 // r / group, head r % group of the KV head.  Its tiles are those any of its rows
@@ -55,7 +63,7 @@ __device__ __forceinline__ int clamp_len(int len, int room, uint32_t* status) {
   return min(max(len, 0), room);
 }
 // Group g's query tokens, those of its sequences.
-__device__ __forceinline__ Sequence group_of(const AttnParams& p, int g, int groups) {
+__device__ __forceinline__ Sequence group_of(const SharedParams& p, int g, int groups) {
   const int members = p.sequences;
   Sequence s;
   int s0, s1;
@@ -81,8 +89,12 @@ __device__ __forceinline__ Sequence group_of(const AttnParams& p, int g, int gro
   return s;
 }
 template <bool kShared = false>
-__device__ __forceinline__ Sequence sequence_of(const AttnParams& p, int b) {
-  if (kShared && b >= p.own) return group_of(p, b - p.own, p.batch - p.own);
+__device__ __forceinline__ Sequence sequence_of(const Params<kShared>& p, int b) {
+  int sequences = p.batch;
+  if constexpr (kShared) {
+    if (b >= p.own) return group_of(p, b - p.own, p.batch - p.own);
+    sequences = p.own;
+  }
   Sequence s;
   if (p.q_begin) {
     const int64_t lo = min(max(int64_t(p.q_begin[b]), int64_t(0)), p.n_tokens);
@@ -90,7 +102,7 @@ __device__ __forceinline__ Sequence sequence_of(const AttnParams& p, int b) {
     s.q0 = int(lo);
     s.count = int(hi - lo);
   } else {
-    s.count = int(p.n_tokens / (kShared ? p.own : p.batch));
+    s.count = int(p.n_tokens / sequences);
     s.q0 = b * s.count;
   }
   s.len = clamp_len(p.lens[b], p.table_pages * p.page_tokens, p.status);           // below 2^31
@@ -119,12 +131,13 @@ __device__ __forceinline__ RowBlock row_block(const AttnParams& p, const Sequenc
 
 // --- outputs -----------------------------------------------------------------
 
-// Output row r of a sequence, dims 4u .. 4u + 3.
-__device__ __forceinline__ void store_out(const AttnParams& p, const Sequence& s, int h, int r, int u, float4 v) {
+// Output row r of a sequence, dims 4u .. 4u + 3.  (kShared: or of a group)
+template <bool kShared = false>
+__device__ __forceinline__ void store_out(const Params<kShared>& p, const Sequence& s, int h, int r, int u, float4 v) {
   const int64_t tok = s.q0 + r / p.group;
   const int64_t at = tok * p.o_token + int64_t(h * p.group + r % p.group) * p.o_head + 4 * u;
   const float f[4] = {v.x, v.y, v.z, v.w};
-  if (s.all) {                                    // fp32 rows [token][head][dim]
+  if constexpr (kShared) if (s.all) {
     *reinterpret_cast<float4*>(p.prefix_o + (tok * p.heads + h * p.group + r % p.group) * p.o_head + 4 * u) = v;
     return;
   }
@@ -151,12 +164,13 @@ __device__ __forceinline__ void store_out(const AttnParams& p, const Sequence& s
   }
 }
 
-__device__ __forceinline__ void store_lse(const AttnParams& p, const Sequence& s, int h, int r, float ref) {
-  if (s.all) {                                    // fp32 rows [token][head][dim]
+template <bool kShared = false>
+__device__ __forceinline__ void store_lse(const Params<kShared>& p, const Sequence& s, int h, int r, float ref) {
+  if constexpr (kShared) if (s.all) {
     p.prefix_ref[(s.q0 + r / p.group) * int64_t(p.heads) + h * p.group + r % p.group] = ref;
     return;
   }
-  if (p.lse) p.lse[(s.q0 + r / p.group) * int64_t(p.heads) + h * p.group + r % p.group] = ref * p.lse_unit;
+  if (p.lse) p.lse[(s.q0 + r / p.group) * int64_t(p.heads) + h * p.group + r % p.group] = ref * 0.693147180559945f;
 }
 // The softmaxes of up to 32 records joined: each lane's weight for its record's
 // output, from their log2 sums (-inf: an empty or no record), the records that are none
@@ -635,7 +649,7 @@ constexpr int kLeastSteps = 4;    // of a part
 
 // One warp; the same in all its lanes: the plan of item `item`'s group.  With `plans`, those of all
 // groups are written there instead.
-__device__ __forceinline__ GroupPlan group_plan(const AttnParams& p, int block_rows, int ctas, int item, int lane,
+__device__ __forceinline__ GroupPlan group_plan(const SharedParams& p, int block_rows, int ctas, int item, int lane,
                                                 GroupPlan* plans = nullptr) {
   auto units_steps = [&](int g, int& units, int& steps) {
     Sequence s{};
@@ -728,14 +742,14 @@ inline int64_t group_items(int64_t rows, int groups, int kv_heads, int block_row
   const int64_t units = (rows / block_rows + groups) * kv_heads;
   return units > ctas ? units : ctas;
 }
-cudaError_t launch_attn_groups(const AttnParams& p, int mt, int items, int ctas, int d, int quant_group, int dev, float* records,
+cudaError_t launch_attn_groups(const SharedParams& p, int mt, int items, int ctas, int d, int quant_group, int dev, float* records,
                                GroupPlan* plans, cudaStream_t s);
-// The softmaxes over the own tokens (fp32 rows in the order of o, log2 sums) and over
-// the prefix (the same, or the records of `plans`) joined into o.
+// The softmaxes over the own tokens (fp32 rows in the order of o, ln of their sums) and over
+// the prefix (the same with log2, or the records of `plans`) joined into o.
 struct SharedJoin {
-  AttnParams a;                   // the call's, with the groups as in the prefix's pass
+  SharedParams a;                 // the call's, with the groups as in the prefix's pass
   const float* own;
-  const float* own_ref;
+  const float* own_lse;
   const float* prefix;
   const float* prefix_ref;
   const GroupPlan* plans;         // NULL: the prefix has rows in the order of o, too

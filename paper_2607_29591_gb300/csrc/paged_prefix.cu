@@ -54,7 +54,7 @@ constexpr int kHalf = 128 * 128;                  // bytes of 128 rows of 64 fp1
 constexpr int kLeastBelow = 60, kLeastExponent = 41;
 
 struct PrefixParams {
-  AttnParams a;
+  SharedParams a;
   GroupPlan* plans;
   float* records;                                 // [record][rows][D]: outputs times their sum; kSplit: two an item
   float2* sums;                                   // [record][rows]: reference (log2) and sum; -inf: nothing seen
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_prefix(const __grid_consta
   using S = PrefixSmem<D, kSplit>;
   constexpr int kRows = 128 * S::tiles, C = D / 32, PG = C / NG, TB = TileShape{D, NG}.bytes();
   constexpr TileShape ts{D, NG};
-  const AttnParams& p = pp.a;
+  const SharedParams& p = pp.a;
   extern __shared__ uint8_t dynamic[];
   uint8_t* smem = dynamic + ((1024u - (smem_u32(dynamic) & 1023u)) & 1023u);
   __shared__ __align__(16) PrefixShared sh;
@@ -583,7 +583,7 @@ cudaError_t dispatch(const PrefixParams& pp, int items, int d, int group, int de
 
 }  // namespace
 
-cudaError_t launch_attn_groups(const AttnParams& p, int mt, int items, int ctas, int d, int quant_group, int dev, float* records,
+cudaError_t launch_attn_groups(const SharedParams& p, int mt, int items, int ctas, int d, int quant_group, int dev, float* records,
                                GroupPlan* plans, cudaStream_t s) {
   PrefixParams pp{};
   pp.a = p;

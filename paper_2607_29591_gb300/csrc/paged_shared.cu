@@ -1,7 +1,7 @@
 // Attention with a shared prefix (reskv_paged_attn_shared): the join of its two passes.
 //
-// The passes leave, for every query row, the softmax's output over what they saw and the
-// log2 sum of its weights: the own tokens' in one row, the prefix's in one row or, where
+// The passes leave, for every query row, the softmax's output over what they saw and the log
+// of the sum of its weights: the own tokens' in one row, the prefix's in one row or, where
 // it was taken in blocks of rows, in one record for each part of its positions, not yet
 // divided by its sum.  With references s_k, sums l_k and outputs l_k o_k (1 and o_k of a whole
 // row) the output is sum 2^(s_k - S) l_k o_k, S = log2 sum 2^s_k l_k.
@@ -26,7 +26,7 @@ __device__ __forceinline__ int range_of(const int32_t* begin, int n, int64_t x) 
 
 template <int D>
 __global__ void __launch_bounds__(kWarps * 32) k_shared_join(const __grid_constant__ SharedJoin j) {
-  const AttnParams& p = j.a;
+  const SharedParams& p = j.a;
   const int lane = threadIdx.x & 31;
   const int64_t row = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
   const int64_t tok = row / p.heads;
@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(kWarps * 32) k_shared_join(const __grid_consta
   const int group = p.seq_begin ? range_of(p.seq_begin, j.groups, seq) : seq / (p.sequences / j.groups);
   const int u = lane < D / 4 ? lane : 0;
   const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-  const float own = j.own_ref[row];
+  const float own = j.own_lse[row] * kLog2e;      // (-inf, NaN: as they are)
   const bool with_own = own != -INFINITY;
   float4 a = with_own ? reinterpret_cast<const float4*>(j.own + row * D)[u] : zero;
   int parts = 0;
