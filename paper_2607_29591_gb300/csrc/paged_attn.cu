@@ -826,7 +826,7 @@ int prefix_mt(const reskv_paged_kv* prefix, const reskv_paged_attn_args* a) {
 
 // SMs of the pass over the own tokens while the prefix has the others; 0: one after the other, with all.  By
 // the times of both (us) with n SMs, as measured, for the tables' room; what is fixed of them is most of it
-// where a prefix has some thousand positions: 64 sequences of 512 behind 8192 67 -> 54 us.
+// where a prefix has some thousand positions: 64 sequences of 512 behind 8192 68 -> 43 us.
 int own_sms(const reskv_paged_kv* kv, const reskv_paged_kv* prefix, const reskv_paged_attn_args* a, int sms) {
   const double rows = double(a->n_tokens) * (a->q.n_heads / kv->n_kv_heads);
   const double tiles = double(kv->table_pages) * kv->page_tokens / kTile * kv->n_kv_heads * kv->batch * std::ceil(rows / kv->batch / 8.0);
