@@ -285,3 +285,42 @@ def test_captured_call_replayed(batch):
     got = o.clone()
     R.reskv_paged_attn_shared(own, prefix, q, lens, plens, o)
     assert torch.equal(got, o)
+
+
+@pytest.mark.parametrize("batch", [3, 40])
+def test_calls_behind_writes_of_all_that_they_read(batch):
+    """Tables, lengths, groups, queries and rows that kernels just before write, call after call without a pause."""
+    rng = np.random.default_rng(23)
+    ints = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    two, _, _, _ = paged(rng, [1504, 1504], 2, 128, 32, 32)
+    own, _, _, _ = paged(rng, [30] * batch, 2, 128, 32, 32)
+    prefix = R.PagedKV(two.pages, two.page_table.clone(), 32, 2, 128, 32)
+    tables = torch.stack([two.page_table, two.page_table.flip(0), two.page_table.roll(1, 1)])
+    steps = 24
+    qs, _ = as_type(rng.standard_normal((steps, batch, 8, 128)), "bf16")
+    rows, _ = as_type(rng.standard_normal((steps, 2, 2, 2, 128)), "bf16")
+    lens, plens = ints(rng.integers(1, 31, (steps, batch))), ints(rng.integers(1, 1505, (steps, 2)))
+    at = ints(np.stack([np.zeros(steps), rng.integers(0, batch + 1, steps), np.full(steps, batch)], 1))
+    q, n, pn, begin = torch.empty_like(qs[0]), torch.empty_like(lens[0]), torch.empty_like(plens[0]), torch.empty_like(at[0])
+    start, last, which = two.pages.clone(), torch.empty_like(plens[0]), ints([0, 1])
+    torch.cuda.synchronize()
+
+    def all_steps(pause):
+        two.pages.copy_(start)
+        outs = torch.full_like(qs, float("nan"))
+        for i in range(steps):
+            for to, source in ((q, qs[i]), (n, lens[i]), (pn, plens[i]), (begin, at[i]), (prefix.page_table, tables[i % 3])):
+                torch.add(source, 0, out=to)
+            torch.sub(pn, 1, out=last)
+            R.reskv_paged_append(prefix, rows[i, 0], rows[i, 1], which, last)
+            pause()
+            R.reskv_paged_attn_shared(own, prefix, q, n, pn, outs[i], seq_begin=begin)
+            pause()
+        own.check_status()
+        prefix.check_status()
+        return outs
+
+    want = all_steps(torch.cuda.synchronize)
+    assert torch.isfinite(want.float()).all()
+    for _ in range(3):
+        assert torch.equal(all_steps(lambda: None), want)
