@@ -807,13 +807,29 @@ extern "C" reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_p
 namespace reskv {
 namespace {
 
+// Units of 8 query rows of all sequences (or groups) of a cache, and their tiles by the tables' room.
+struct FewRows {
+  double units, tiles;
+};
+FewRows few_rows(const reskv_paged_kv* c, const reskv_paged_attn_args* a) {
+  const double rows = double(a->n_tokens) * (a->q.n_heads / c->n_kv_heads);
+  const double units = double(c->batch) * c->n_kv_heads * std::ceil(rows / c->batch / 8.0);
+  return {units, units * (double(c->table_pages) * c->page_tokens / kTile)};
+}
+
 // The prefix in blocks of rows, by the mean rows of a group: as in takes_blocks, but from 32 rows on, us:
 // four groups of 32 rows to 16384 positions 65 against 82, 32 rows of 32768 64 against 70, of 4096 34 against 32;
 // 24 rows of 1000 26 against 21, 16 of 32768 63 against 48.
-constexpr int kPrefixRows = 32;
-bool prefix_in_blocks(const reskv_paged_kv* prefix, const reskv_paged_attn_args* a) {
-  return a->o.dtype != RESKV_F32 && a->scale >= 0.f &&
-         double(a->n_tokens) * a->q.n_heads / prefix->n_kv_heads >= double(kPrefixRows) * prefix->batch;
+// Below 128 rows that is not so where each SM has a unit and a dozen tiles at most, of both passes: one launch
+// ends before two then.  8 KV heads, 4 query heads each, us: 8 sequences of 100 behind 512 23.0 against 18.5,
+// 12 of 60 behind 256 22.5 against 18.0; 8 of 60 behind 1000 (15 tiles) 22.0 against 21.3, behind 4096 27 against
+// 31; 16 of 60 behind 256 (1.3 units) 25 against 27; with one KV head 128 rows of 1000 23.8 against 24.7.
+constexpr int kPrefixRows = 32, kFewTiles = 12;
+bool prefix_in_blocks(const reskv_paged_kv* kv, const reskv_paged_kv* prefix, const reskv_paged_attn_args* a, int sms) {
+  const double rows = double(a->n_tokens) * (a->q.n_heads / prefix->n_kv_heads) / prefix->batch;       // of a group
+  if (a->o.dtype == RESKV_F32 || !(a->scale >= 0.f) || rows < kPrefixRows) return false;
+  const FewRows own = few_rows(kv, a), shared = few_rows(prefix, a);
+  return rows >= 128 || takes_blocks(kv, a) || own.units + shared.units > sms || own.tiles + shared.tiles > double(kFewTiles) * sms;
 }
 // Sequences and groups that one launch of the kernel of few rows holds.
 bool one_launch(const reskv_paged_kv* kv, const reskv_paged_kv* prefix, const reskv_paged_attn_args* a) {
@@ -829,7 +845,7 @@ int prefix_mt(const reskv_paged_kv* prefix, const reskv_paged_attn_args* a) {
 // where a prefix has some thousand positions: 64 sequences of 512 behind 8192 68 -> 43 us.
 int own_sms(const reskv_paged_kv* kv, const reskv_paged_kv* prefix, const reskv_paged_attn_args* a, int sms) {
   const double rows = double(a->n_tokens) * (a->q.n_heads / kv->n_kv_heads);
-  const double tiles = double(kv->table_pages) * kv->page_tokens / kTile * kv->n_kv_heads * kv->batch * std::ceil(rows / kv->batch / 8.0);
+  const double tiles = few_rows(kv, a).tiles;
   const double block = 128.0 * prefix_mt(prefix, a);
   const double steps = double(prefix->table_pages) * prefix->page_tokens / kBlockPos * kv->n_kv_heads * prefix->batch *
                        std::ceil(rows / prefix->batch / block);
@@ -864,7 +880,7 @@ SharedLayout shared_layout(const reskv_paged_kv* kv, const reskv_paged_kv* prefi
   l.own_lse = l.own + padded(rows * kv->head_dim * 4);
   l.prefix = l.own_lse + padded(rows * 4);
   size_t held = rows;
-  if (prefix_in_blocks(prefix, a)) {
+  if (prefix_in_blocks(kv, prefix, a, sms)) {
     const int block = 128 * prefix_mt(prefix, a);
     // rows of records: 128 or 256 of two streams or blocks an item
     held = size_t(group_items(a->n_tokens * (a->q.n_heads / kv->n_kv_heads), prefix->batch, kv->n_kv_heads, block, sms)) * 256;
@@ -943,7 +959,7 @@ extern "C" reskv_status reskv_paged_attn_shared(const reskv_paged_kv* kv, const 
     g.prefix_pages = prefix->table_pages;
     g.prefix_o = reinterpret_cast<float*>(ws + l.prefix);
     g.prefix_ref = reinterpret_cast<float*>(ws + l.prefix_ref);
-    const bool blocks = prefix_in_blocks(prefix, a), fused = !blocks && one_launch(kv, prefix, a);
+    const bool blocks = prefix_in_blocks(kv, prefix, a, sms), fused = !blocks && one_launch(kv, prefix, a);
     const int mt = prefix_mt(prefix, a);
     const int apart = blocks && !takes_blocks(kv, a) ? own_sms(kv, prefix, a, sms) : 0;
     const int items = blocks ? int(group_items(p.n_tokens * p.group, prefix->batch, p.kv_heads, 128 * mt, sms - apart)) : 0;

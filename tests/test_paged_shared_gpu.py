@@ -66,16 +66,16 @@ def case(seed, prefix_lens, lens, members, new, kv=2, per=4, d=128, group=32, pa
 
 @pytest.mark.parametrize("d,group", [(128, 32), (128, 64), (128, 128), (64, 32), (64, 64)])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("batch", [3, 20])
+@pytest.mark.parametrize("batch", [3, 20, 33])
 def test_single_tokens(d, group, dtype, batch):
     lens = [1 + (37 * i) % 90 for i in range(batch)]
     case(1, [150], lens, [batch], 1, d=d, group=group, dtype=dtype)
 
 
 @pytest.mark.parametrize("prefix", [0, 1, 15, 16, 17, 64, 65, 700])
-@pytest.mark.parametrize("batch", [2, 40])
-def test_prefix_lengths(prefix, batch):
-    case(prefix, [prefix], [5 + i for i in range(batch)], [batch], 1, per=2)
+@pytest.mark.parametrize("batch,per", [(2, 2), (40, 2), (40, 4)])
+def test_prefix_lengths(prefix, batch, per):
+    case(prefix, [prefix], [5 + i for i in range(batch)], [batch], 1, per=per)
 
 
 @pytest.mark.parametrize("per", [1, 3, 7, 16])
@@ -88,7 +88,9 @@ def test_head_groups(per, batch):
 def test_several_groups(dtype):
     case(2, [100, 0, 333, 17], [9, 30, 1, 64, 65, 2, 70, 40, 8, 3], [1, 4, 3, 2], 1, dtype=dtype)
     case(3, [100, 0, 333, 17], [9 + i for i in range(70)], [20, 0, 30, 20], 1, dtype=dtype)
+    case(3, [100, 0, 333, 17], [9 + i for i in range(70)], [20, 0, 30, 20], 1, per=8, dtype=dtype)
     case(4, [64, 200], [20] * 40, [20, 20], 1, uniform=True, dtype=dtype)
+    case(4, [64, 200], [20] * 40, [20, 20], 1, per=7, uniform=True, dtype=dtype)
     case(5, [50], [9, 30, 12], [2], 1, dtype=dtype)                    # the last sequence is in no group
 
 
@@ -97,10 +99,13 @@ def test_several_groups(dtype):
 def test_several_tokens(new, batch):
     case(new, [140], [new + 7 * i for i in range(batch)], [batch], new)
     case(new + 1, [140, 30], [new + 7 * i for i in range(batch + 1)], [batch, 1], new, dtype="f16", d=64, group=64)
+    case(new + 2, [140], [new + 7 * i for i in range(batch)], [batch], new, per=64)
 
 
 def test_ragged_queries_and_tokens_before_the_own_ones():
     case(6, [120, 60], [20, 9, 64, 3, 30], [3, 2], None, counts=[2, 0, 7, 3, 1])
+    case(6, [120, 60], [20, 9, 64, 3, 30], [3, 2], None, counts=[2, 0, 7, 3, 1], per=24)
+    case(7, [120, 60], [1, 0, 2], [2, 1], 3, per=32)
     case(7, [120, 60], [1, 0, 2], [2, 1], 3)                            # some stand before their own tokens
     case(8, [0, 60], [1, 0, 2], [2, 1], 3)                              # and see nothing
     case(9, [120], [40] * 4, [4], None, counts=[30, 1, 60, 0])
@@ -137,14 +142,14 @@ def test_agrees_with_one_long_sequence():
     assert float((a - b).abs().max()) <= 2.0 ** -16 * 40              # two fp32 results, values within 40
 
 
-@pytest.mark.parametrize("batch", [3, 20])
+@pytest.mark.parametrize("batch", [3, 20, 33])
 def test_long_prefixes(batch):
     """Many tiles a CTA, for one block of rows and for two."""
     case(17, [3000], [4 + i for i in range(batch)], [batch], 1, kv=1, per=4, group=64)
     case(18, [2500, 40], [4 + i for i in range(2 * batch)], [batch, batch], 1, kv=1, per=16, d=64, group=32, dtype="f16")
 
 
-@pytest.mark.parametrize("batch,scale", [(40, 1e-20), (40, 1e9), (3, 1e9)])
+@pytest.mark.parametrize("batch,scale", [(40, 1e-20), (40, 1e9), (3, 1e9), (64, 1e-20), (64, 1e9)])
 def test_values_and_keys_of_any_size(batch, scale):
     """Tokens far larger and far smaller than their neighbours, in keys that queries avoid and in values."""
     rng = np.random.default_rng(19)
@@ -185,7 +190,7 @@ def test_values_and_keys_of_any_size(batch, scale):
         assert (np.abs(f64(lse)[b:b + 1] - rl) <= d * 2.0 ** -23 * xm + 2.0 ** -12 + 2.0 ** -22 * np.abs(rl)).all()
 
 
-@pytest.mark.parametrize("batch", [3, 24])
+@pytest.mark.parametrize("batch", [3, 24, 40])
 def test_nan_held_in_a_prefix_reaches_its_group_alone(batch):
     rng = np.random.default_rng(20)
     ints = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
@@ -206,7 +211,7 @@ def test_nan_held_in_a_prefix_reaches_its_group_alone(batch):
     assert not torch.isnan(o).any()
 
 
-@pytest.mark.parametrize("batch", [3, 24])
+@pytest.mark.parametrize("batch", [3, 24, 40])
 def test_pages_past_32_bits(batch):
     """The same prefix in the first and in the last pages of more than 4 GB."""
     rng = np.random.default_rng(21)
@@ -226,7 +231,7 @@ def test_pages_past_32_bits(batch):
     assert torch.equal(a, b)
 
 
-@pytest.mark.parametrize("batch", [3, 24])
+@pytest.mark.parametrize("batch", [3, 24, 40])
 def test_any_rows_of_queries_and_outputs(batch):
     """Strided and unaligned queries and outputs, the same bits."""
     rng = np.random.default_rng(22)
@@ -259,7 +264,7 @@ def test_faults_are_reported_and_bounded():
         own.check_status()
 
 
-@pytest.mark.parametrize("batch", [3, 24])
+@pytest.mark.parametrize("batch", [3, 24, 40])
 def test_captured_call_replayed(batch):
     rng = np.random.default_rng(16)
     prefix, _, _, _ = paged(rng, [200], 2, 128, 32, 32)
