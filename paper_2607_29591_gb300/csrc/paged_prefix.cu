@@ -28,10 +28,10 @@
 // logit + c; the sum of the weights takes 2^-c back.  Positions that do not exist have c = -inf.
 //
 // A tile takes 1.4 us with one block of rows or two (some 1700 instructions a scheduler, unpacking and softmax
-// about half each; the products alone 0.75), a CTA some 15 beside its tiles: the plan, the queries, the first
-// tile, and 128 KB of records.  32 sequences of 4 rows behind 131072 positions 185 us, 64 behind 8192 42 with
-// their own tokens beside them.  What runs once is kept in short loops: unrolled, reading the queries took
-// 5 us and all of a CTA's beginning and end 23, for the instructions' sake.
+// about half each; the products alone 0.75), a CTA some 12 beside its tiles: the plan, the queries, the first
+// tile, and 128 KB of records.  32 sequences of 4 rows behind 131072 positions 175 us, 64 behind 8192 42 with
+// their own tokens beside them.  What runs once is kept in short loops: unrolled, all of a CTA's beginning and
+// end took 23 us, for the instructions' sake.
 #include <atomic>
 
 #include "paged_attn.cuh"
@@ -80,6 +80,7 @@ struct PrefixShared {
   GroupPlan plan;
   // per position of a slot: 2^e of its key; log2 of its value's scale (-inf: no such position), and 2^- of that
   alignas(16) float up[4][kPos], c[4][kPos], inv[4][kPos];
+  float cq[128];                                  // of a row: its logits' factor
 };
 
 // 2^(14 - (e - 127)) and its inverse, of a biased exponent 15 <= e <= 254
@@ -374,23 +375,41 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_prefix(const __grid_consta
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     // --- the softmax, a row a thread ---
-    const int m = warp >> 2, rt = (warp & 3) * 32 + lane, r = r0 + (kSplit ? 0 : m * 128) + rt;
-    const bool real = (kSplit ? 0 : m * 128) + rt < rows;
+    const int m = warp >> 2, rt = (warp & 3) * 32 + lane;
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
-    float cq;
+    float cq = 0.f;
     {
-      // The row's query, scaled below 2^8 (128 of them sum up within fp16), in the order of the keys' dims.
+      // The block's queries, to where they will lie: lanes along the rows, 16 bytes each, all under way at once.
+      // (A row a thread, 32 lines a load: 32 sequences behind 131072 positions 180 us for 175.)  Two streams have one block of rows: a half of it each.
+      constexpr int kWords = D / 8, kEach = kSplit ? 16 : 32;
+      auto place = [&](int row, int k) {          // word k (dims 8k .. 8k + 7) of a row of this warp's block
+        return (kSplit ? 0 : m * S::q) + row * 128 + (k >> 3) * kHalf + (((k & 7) ^ (row & 7)) << 4);
+      };
+#pragma unroll 1
+      for (int i = lane / kWords; i < kEach; i += 32 / kWords) {
+        const int own = (warp & 3) * 32 + (kSplit ? m * 16 : 0) + i, k = lane % kWords, at = (kSplit ? 0 : m * 128) + own;
+        uint8_t* const to = smem + place(own, k);
+        const uint16_t* e = static_cast<const uint16_t*>(p.q);
+        if (at < rows) e += (plan.q0 + (r0 + at) / p.group) * p.q_token + int64_t(h * p.group + (r0 + at) % p.group) * p.q_head + 8 * k;
+        if (at < rows && p.q_wide)
+          copy16(smem_u32(to), e);
+        else if (at < rows)
+          *reinterpret_cast<uint4*>(to) = make_uint4(e[0] | uint32_t(e[1]) << 16, e[2] | uint32_t(e[3]) << 16,
+                                                     e[4] | uint32_t(e[5]) << 16, e[6] | uint32_t(e[7]) << 16);
+        else
+          *reinterpret_cast<uint4*>(to) = make_uint4(0u, 0u, 0u, 0u);
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      if (kSplit) asm volatile("bar.sync 1, 256;" ::: "memory");
+      else __syncwarp();
+    }
+    if (!kSplit || m == 0) {
+      // The row's query in place, scaled below 2^8 (128 of them sum up within fp16), in the order of the keys' dims.
       // In short loops, as all code that runs once here is: straight on, every 128 bytes of it are waited for.
-      const uint16_t* src = static_cast<const uint16_t*>(p.q) +
-                            (real ? (plan.q0 + r / p.group) * p.q_token + int64_t(h * p.group + r % p.group) * p.q_head : 0);
+      uint8_t* const row = smem + m * S::q + rt * 128;
+      auto word = [&](int k) { return reinterpret_cast<uint4*>(row + (k >> 3) * kHalf + (((k & 7) ^ (rt & 7)) << 4)); };
       auto eight = [&](int k, float (&x)[8]) {    // dims 8k .. 8k + 7
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (real && p.q_wide) {
-          v = reinterpret_cast<const uint4*>(src)[k];
-        } else if (real) {
-          const uint16_t* e = src + 8 * k;
-          v = make_uint4(e[0] | uint32_t(e[1]) << 16, e[2] | uint32_t(e[3]) << 16, e[4] | uint32_t(e[5]) << 16, e[6] | uint32_t(e[7]) << 16);
-        }
+        const uint4 v = *word(k);
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -409,14 +428,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_prefix(const __grid_consta
       }
       const int e = 134 - min(max(__float_as_int(top) >> 23, 1), 254), e1 = e >> 1, e2 = e - e1;
       const float f1 = __int_as_float((127 + e1) << 23), f2 = __int_as_float((127 + e2) << 23);
-      uint8_t* const row = smem + m * S::q + rt * 128;
       uint8_t* const more = smem + S::at_q_more + m * S::q_more + rt * 32;
-      const bool mine = !kSplit || m == 0;        // (two streams have one block of rows)
       const int turn_word = ((rt >> 2) & 1) << 4;
-      if (mine) {
-        *reinterpret_cast<uint4*>(more) = make_uint4(0u, 0u, 0u, 0u);
-        *reinterpret_cast<uint4*>(more + 16) = make_uint4(0u, 0u, 0u, 0u);
-      }
+      *reinterpret_cast<uint4*>(more) = make_uint4(0u, 0u, 0u, 0u);
+      *reinterpret_cast<uint4*>(more + 16) = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll 1
       for (int n0 = 0; n0 < NG; ++n0) {
         float sum = 0.f;
@@ -431,19 +446,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_prefix(const __grid_consta
             const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&held[j]));
             sum += y.x + y.y;
           }
-          if (mine) *reinterpret_cast<uint4*>(row + (k >> 3) * kHalf + (((k & 7) ^ (rt & 7)) << 4)) = make_uint4(held[0], held[1], held[2], held[3]);
+          *word(k) = make_uint4(held[0], held[1], held[2], held[3]);
         }
         // against the keys' planes: first planes twice, then what they left over
         const __half first_plane = __float2half_rn(sum), rest = __float2half_rn(sum - __half2float(first_plane));
-        if (mine) {
-          __half* at = reinterpret_cast<__half*>(more);
-          at[turn_word / 2 + n0] = first_plane;
-          at[turn_word / 2 + 4 + n0] = first_plane;
-          at[(16 ^ turn_word) / 2 + n0] = rest;
-        }
+        __half* at = reinterpret_cast<__half*>(more);
+        at[turn_word / 2 + n0] = first_plane;
+        at[turn_word / 2 + 4 + n0] = first_plane;
+        at[(16 ^ turn_word) / 2 + n0] = rest;
       }
       cq = p.scale2 * __int_as_float((127 - e1) << 23) * __int_as_float((127 - e2) << 23);
+      if (kSplit) sh.cq[rt] = cq;
       fence_proxy_async_smem();
+    }
+    if (kSplit) {
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      cq = sh.cq[rt];
     }
     role_arrive(&sh.q);
     const int mine = steps[m];
