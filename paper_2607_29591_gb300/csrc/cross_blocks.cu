@@ -25,7 +25,7 @@
 // The reference of a row moves only when a weight passes 2^13; it then lies 6 below the largest logit.
 //
 // Bound by the exponentials between two products of a stream, then by the products: 8 x 1024 tokens of 32 heads
-// over 4096 states, 8 KV heads of 128 (550 GFLOP) 440 us, 1.25 PFLOP/s; without any exponential 365, which
+// over 4096 states, 8 KV heads of 128 (550 GFLOP) 450 us, 1.22 PFLOP/s; without any exponential 365, which
 // is what the products alone take in these tiles.  (P keeps both streams from a second S: the sums of 256 rows
 // and two S fill the tensor memory.)  Weights before their largest logit, 16 at a time in the shadow of the
 // other half's loads, spilled: 546.
@@ -61,7 +61,6 @@ struct BlocksSmem {
   static constexpr int bytes = q + slots * tile + 1024;               // on a boundary of 1024
   static constexpr int at_ref = 2 * 128 * D * 4;  // of rows to be joined: outputs, then references and sums
   static_assert(at_ref + 3 * 256 * 4 <= q + slots * tile, "rows to be joined");
-  static_assert(bytes + 1024 + 256 <= 227 * 1024, "shared memory");
 };
 
 struct BlocksShared {
@@ -69,8 +68,12 @@ struct BlocksShared {
   uint32_t tmem, abort;
   float half[2][128];             // of a row's second half, for the first and back
 };
-// A barrier of two warps.
+static_assert(BlocksSmem<64, false>::bytes + sizeof(BlocksShared) + 16 <= 227 * 1024 && BlocksSmem<64, true>::bytes + sizeof(BlocksShared) + 16 <= 227 * 1024 &&
+                  BlocksSmem<128, false>::bytes + sizeof(BlocksShared) + 16 <= 227 * 1024 && BlocksSmem<128, true>::bytes + sizeof(BlocksShared) + 16 <= 227 * 1024,
+              "shared memory");
+// A barrier of two warps, and one's share of it where it goes no further.
 __device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void pair_leave(int id) { asm volatile("barrier.cta.arrive %0, 64;" ::"r"(id) : "memory"); }
 
 
 template <int D, bool kF16, bool kSplit>
@@ -272,9 +275,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     // --- the softmax, half a row a thread: states 64 c .. 64 c + 63 of a tile.  Both threads of a row look
-    // for its largest logit in all of it, so that they agree without a word.  8 x 1024 tokens over 4096
-    // states, us: with one thread a row, whose 128 exponentials a tile waits for, 523 (without any exponential
-    // 365); with half a row each and a barrier of the two, 478 ---
+    // for its largest logit in all of it and so agree on it; they meet before P goes over S, which both
+    // have looked through.  8 x 1024 tokens over 4096 states, us: with one thread a row, whose 128
+    // exponentials a tile waits for, 523 (without any exponential 365); with half a row each that exchange
+    // their largest logits at a barrier 478; so 450 (465 with an mbarrier for each warp's reading) ---
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
     const int mine = steps[m], pair = 1 + 4 * m + (warp & 3);
     const float f = fabsf(p.scale2);              // (a negative scale is the product's: S = -Q K^T)
@@ -353,22 +357,27 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
       uint32_t w[32];
 #pragma unroll
       for (int k = 0; k < 32; ++k) w[k] = pack_two<kF16>(x[2 * k], x[2 * k + 1]);
+      // (both warps of the rows have read S: what one puts P over was the other's to look through, too)
+      fence_before();
+      pair_sync(pair);
+      fence_after();
       store32(s_cols(m) + lanes + 64 * c, w);
       stored();
       fence_before();
       role_arrive(&sh.p[m]);
     }
+    if (!ok) pair_leave(pair);                    // a wait gave up: the other warp may be at the barrier of a tile
     if (ok && mine > 0) ok = role_wait(&sh.done, 0, &sh.abort, p.status);
     fence_after();
     const bool seen = mine > 0 && ok;
     // the row's sum, of both halves
     if (c == 1) sh.half[m][rt] = l;
-    pair_sync(pair);
+    asm volatile("bar.sync 9, 512;" ::: "memory");
     if (c == 0) {
       l += sh.half[m][rt];
       sh.half[m][rt] = l;
     }
-    pair_sync(pair);
+    asm volatile("bar.sync 9, 512;" ::: "memory");
     l = sh.half[m][rt];
     if (cs == 1 && !kSplit) {
       const float inv = 1.f / l;
