@@ -76,3 +76,44 @@ def gradient(q, k, v, d_o, scale, unit, least):
     for i in range(3):
         tol[i] += unit * (np.abs(out[i]) + tol[i]) + least
     return out, tol
+
+
+def gradient_norms(q, k, v, d_o, scale, unit, least, of_d=None):
+    """d_q, d_k, d_v of one sequence, and for each KV head what the norm of their errors may be.
+
+    Every rounding is taken as an error of its own, evenly spread over half a step (`unit` of the value, `least`
+    at the bottom of the type): its variance is a third of its square, and the squares add up.  t and p
+    are rounded before the products over them (of t in d_q, what all of a row's t lose together is put back: its
+    part along the row's mean key is gone), then the results.  fp32 sums are off by `d` 2^-24 of their absolute
+    sums, far less.  The norm of independent errors lies close to the root of their variance; 2.5 times that is
+    past any one error's largest size (3^0.5 of it), and a gradient with a term left out is beyond it.
+
+    of_d: D = <d_o, o> of [n, H] to be used instead (mistakes to be refused)."""
+    n, H, d = q.shape
+    kv, length, _ = k.shape
+    per = H // kv
+    out = [np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape)]
+    var = np.zeros((3, kv))
+    for h in range(H if length and n else 0):
+        kk, vv, qq, g = k[h // per], v[h // per], q[:, h], d_o[:, h]
+        x = scale * (qq @ kk.T)
+        w = np.exp(x - x.max(1, keepdims=True))
+        p = w / w.sum(1, keepdims=True)
+        D = (g * (p @ vv)).sum(1, keepdims=True) if of_d is None else of_d[:, h, None]
+        dp = g @ vv.T
+        t = p * (dp - D)
+        off = scale * np.sqrt(d) * 2.0 ** -23 * (np.abs(qq) @ np.abs(kk).T)       # of a logit: the weight's share
+        t_var = (unit * t) ** 2 / 3 + least ** 2 / 3 + (off * t) ** 2 + (p * d * 2.0 ** -23) ** 2 * (g * g).sum(1, keepdims=True) * (vv * vv).sum(1)
+        p_var = (unit * p) ** 2 / 3 + least ** 2 / 3 + (off * p) ** 2
+        far = (kk * kk).sum(1) - 2 * (p @ kk) @ kk.T + ((p @ kk) ** 2).sum(1, keepdims=True)      # |k_j - mean k|^2
+        out[0][:, h] = scale * (t @ kk)
+        out[1][h // per] += scale * (t.T @ qq)
+        out[2][h // per] += p.T @ g
+        var[0, h // per] += scale ** 2 * (t_var * np.maximum(far, 0)).sum()
+        var[1, h // per] += scale ** 2 * (t_var * (qq * qq).sum(1, keepdims=True)).sum()
+        var[2, h // per] += (p_var * (g * g).sum(1, keepdims=True)).sum()
+    heads = [out[0].reshape(n, kv, per, d).transpose(1, 0, 2, 3), out[1], out[2]]
+    for i in range(3):
+        for h in range(kv):
+            var[i, h] += unit ** 2 / 3 * (heads[i][h] ** 2).sum() + least ** 2 / 3 * heads[i][h].size
+    return out, 2.5 * np.sqrt(var)

@@ -361,6 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
     sh.sums[c][rt] = delta;
     asm volatile("bar.sync 1, 256;" ::: "memory");
     delta = sh.sums[0][rt] + sh.sums[1][rt];
+    asm volatile("bar.sync 1, 256;" ::: "memory");      // (a rank without tiles comes to its next sums at once)
     const int64_t stat = at_token * p.heads + head;
     const float f = p.scale2, lse2 = real ? fmaf(p.lse[stat], kLog2e, -kUp) : 0.f, down = -delta * kDown;
     float2 more = make_float2(0.f, 0.f), rounded = more;      // sums of T
