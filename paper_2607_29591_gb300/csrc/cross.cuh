@@ -29,6 +29,12 @@ struct CrossParams {
   float scale, scale2;            // of the logits; times log2 e
 };
 
+// Weights are 2^(s f - ref) of a sum of products s, f = scale log2 e, with a reference near the row's largest s f, as
+// fp32 holds it.  One rounding of s f - ref keeps most of a weight's digits, but from 2^26 on s f may lie past the reference
+// by more than the weights' types reach.  So from kFarLogits on, where fp32 sums of products are some 2^-6 off anyway,
+// weights come from s f rounded, as the reference does.  Either way equal sums have equal weights, in whichever tile.
+constexpr float kFarLogits = 65536.f;
+
 // A sequence's query tokens and rows; `seen` of the rows take part.
 struct CrossSequence {
   int q0, count;

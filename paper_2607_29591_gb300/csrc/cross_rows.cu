@@ -192,7 +192,8 @@ __global__ void __launch_bounds__(kThreads) k_cross_rows(const __grid_constant__
           auto weights = [&]() {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              x[j] = exp2_fast(fmaf(s[b][j], f, -ref[b][j & 1]));
+              const float r = ref[b][j & 1];
+              x[j] = exp2_fast(fabsf(r) > kFarLogits ? __fsub_rn(__fmul_rn(s[b][j], f), r) : fmaf(s[b][j], f, -r));
               if (left < 16 && g + (j >> 1) * 8 >= left) x[j] = 0.f;
             }
           };
