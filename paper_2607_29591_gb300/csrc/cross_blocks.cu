@@ -315,6 +315,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
       }
 #pragma unroll
       for (int k = 0; k < 64; k += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(x[k]), "f"(x[k + 1]));
+      if (!real) top = -INFINITY;                   // a row of another sequence, or of nothing, moves no reference
       float keep = 1.f;
       float2 s2[4] = {};
       if (__any_sync(0xffffffffu, fmaf(top, f, -ref) > 13.f)) {
