@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
     const int mine = steps[m], pair = 1 + 4 * m + (warp & 3);
     const float f = fabsf(p.scale2);              // (a negative scale is the product's: S = -Q K^T)
     float ref = kNoReference, l = 0.f;
-    bool ok = true;
+    bool ok = true, far = false;                  // far: logits of any row of the warp
 #pragma unroll 1
     for (int i = 0; i < mine; ++i) {
       ok = role_wait(&sh.s[m], i & 1, &sh.abort, p.status);
@@ -318,12 +318,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
       if (!real) top = -INFINITY;                   // a row of another sequence, or of nothing, moves no reference
       float keep = 1.f;
       float2 s2[4] = {};
-      if (__any_sync(0xffffffffu, fmaf(top, f, -ref) > 13.f)) {
-        // The reference 6 below the row's largest, weights from rounded logits as the reference is: past
-        // 2^26 it may lie many units off the unrounded ones.
+      if (__any_sync(0xffffffffu, (far ? __fsub_rn(__fmul_rn(top, f), ref) : fmaf(top, f, -ref)) > 13.f)) {
+        // the reference 6 below the row's largest (the same rows, and what becomes of them, in both warps)
         const float now = fmaxf(ref, __fmul_rn(top, f) - 6.f);
         keep = exp2f(ref - now);
         ref = now;
+        far = __any_sync(0xffffffffu, fabsf(ref) > kFarLogits && ref != kNoReference);
+      }
+      if (far) {
 #pragma unroll
         for (int k = 0; k < 64; ++k) x[k] = __fsub_rn(__fmul_rn(x[k], f), ref);
       } else {

@@ -26,7 +26,7 @@ def keys_and_queries(size, n, states, winners, d, dtype, seed, kv=1, per=4):
 
 
 SIZES = [("bf16", s) for s in (1e2, 1e4, 1e5, 1e7, 1e8, 3e8, 1e9, 1e10, 1e12, 1e15, 1e20, 1e30)] + [("f16", s) for s in (1e2, 1e4, 3e4)]
-FORMS = [(1, 300, 0), (4, 4000, 0), (3, 300, 1)]
+FORMS = [(1, 300, 0), (4, 4000, 0), (3, 300, 1), (5, 300, 0), (40, 300, 0), (30, 2000, 0), (150, 400, 0)]
 
 
 def place(t, offset):
@@ -67,3 +67,21 @@ def test_rows_near_the_end_of_fp16(n):
     o = torch.empty_like(q)
     R.reskv_cross_attn(q, k, v, o)
     assert torch.equal(o, v[77].expand_as(o))
+
+
+@pytest.mark.parametrize("n", [2, 40])
+@pytest.mark.parametrize("per_unit", [2.0 ** 20, 2.0 ** 23, 2.0 ** 24])
+def test_logits_that_climb_in_small_steps(n, per_unit):
+    """Logits of 2^24 to 2^28 whose tiles' largest climb by some fp32 steps each: one output row is one value's."""
+    states = 1300
+    q = torch.full((n, 2, 64), 1024.0, device="cuda").half()
+    k = torch.zeros((states, 1, 64), device="cuda")
+    k[:, :, 0] = per_unit * 2.0 ** -10                      # 1024 times that each
+    k[:, :, 1] = torch.arange(states, device="cuda")[:, None] / 8.0
+    k = k.clamp(max=60000).half()
+    v = torch.randn((states, 1, 64), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").half()
+    o, lse = torch.empty_like(q), torch.empty((n, 2), device="cuda")
+    for scale in (1.0, 0.5, 0.3):
+        R.reskv_cross_attn(q, k, v, o, scale=scale, lse=lse)
+        assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+        assert float((o.double() - v[-1].double()).abs().max()) <= 2.0 ** -10 * 5      # the last key's logit is 38 above the next's
