@@ -34,6 +34,8 @@ struct CrossParams {
 // by more than the weights' types reach.  So from kFarLogits on, where fp32 sums of products are some 2^-6 off anyway,
 // weights come from s f rounded, as the reference does.  Either way equal sums have equal weights, in whichever tile.
 constexpr float kFarLogits = 65536.f;
+// log2 of a row's sum, less `up`, of its ln: -inf (all logits are) as what leaves every weight 0.
+__device__ __forceinline__ float log2_sum(float lse, float up = 0.f) { return lse == -INFINITY ? 3.0e38f : fmaf(lse, kLog2e, -up); }
 
 // A sequence's query tokens and rows; `seen` of the rows take part.
 struct CrossSequence {

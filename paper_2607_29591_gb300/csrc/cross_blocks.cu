@@ -383,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
     asm volatile("bar.sync 9, 512;" ::: "memory");
     l = sh.half[m][rt];
     if (cs == 1 && !kSplit) {
-      const float inv = 1.f / l;
+      const float inv = l != 0.f ? 1.f / l : 0.f;         // (0: every logit is -inf)
       if (seen) {
         uint16_t* y = static_cast<uint16_t*>(p.o.data) + (sq.q0 + token) * p.o.token + head * p.o.head + c * (D / 2);
 #pragma unroll 1
@@ -402,7 +402,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
             }
           }
         }
-        if (real && p.lse && c == 0) p.lse[int64_t(sq.q0 + token) * p.heads + head] = (ref + log2f(l)) * 0.693147180559945f;
+        if (real && p.lse && c == 0)
+          p.lse[int64_t(sq.q0 + token) * p.heads + head] = l != 0.f ? (ref + log2f(l)) * 0.693147180559945f : -INFINITY;
       }
     } else {
       // for the join: all products are done, operands' memory is free (word u of row r at u ^ r)
@@ -448,10 +449,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
       const float w = ref == -INFINITY ? 0.f : exp2f(ref - top);
       float total = ref == -INFINITY ? 0.f : w * sum;
       for (int o = 1; o < sources; o *= 2) total += __shfl_xor_sync(group, total, o);
-      weight[tid] = ref == -INFINITY ? -1.f : w / total;
+      weight[tid] = ref == -INFINITY ? -1.f : total != 0.f ? w / total : 0.f;
       const int tok = token_of(r);
       if (i == 0 && p.lse && tok < sq.count)
-        p.lse[int64_t(sq.q0 + tok) * p.heads + h * p.group + (r & 127) % p.group] = (top + log2f(total)) * 0.693147180559945f;
+        p.lse[int64_t(sq.q0 + tok) * p.heads + h * p.group + (r & 127) % p.group] = total != 0.f ? (top + log2f(total)) * 0.693147180559945f : -INFINITY;
     }
     asm volatile("bar.sync 9, 512;" ::: "memory");
     // then a row a warp, four rows at a time

@@ -82,17 +82,17 @@ __global__ void __launch_bounds__(kWarps * 32) k_cross(const __grid_constant__ C
       for (int e = 0; e < E; ++e) o[e] *= keep;
       top = x;
     }
-    const float w = exp2f(x - top);
+    const float w = x == -INFINITY ? 0.f : exp2f(x - top);
     l += w;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = fmaf(w, v[e], o[e]);
   }
-  store_row<kF16>(p.o, tok, h, lane, o, s.seen ? 1.f / l : 0.f);
-  if (p.lse && lane == 0) p.lse[tok * p.heads + h] = s.seen ? (top + log2f(l)) * 0.693147180559945f : -INFINITY;
+  store_row<kF16>(p.o, tok, h, lane, o, l != 0.f ? 1.f / l : 0.f);
+  if (p.lse && lane == 0) p.lse[tok * p.heads + h] = l != 0.f ? (top + log2f(l)) * 0.693147180559945f : -INFINITY;
 }
 
 // exp(x - lse) of one logit
-__device__ __forceinline__ float weight(float x2, float lse) { return exp2f(fmaf(lse, -kLog2e, x2)); }
+__device__ __forceinline__ float weight(float x2, float lse) { return exp2f(x2 - log2_sum(lse)); }
 
 template <int D, bool kF16>
 __global__ void __launch_bounds__(kWarps * 32) k_cross_grad_q(const __grid_constant__ CrossParams p) {

@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
     delta = sh.sums[0][rt] + sh.sums[1][rt];
     asm volatile("bar.sync 1, 256;" ::: "memory");      // (a rank without tiles comes to its next sums at once)
     const int64_t stat = at_token * p.heads + head;
-    const float f = p.scale2, lse2 = real ? fmaf(p.lse[stat], kLog2e, -kUp) : 0.f, down = -delta * kDown;
+    const float f = p.scale2, lse2 = real ? log2_sum(p.lse[stat], kUp) : 0.f, down = -delta * kDown;
     float2 more = make_float2(0.f, 0.f), rounded = more;      // sums of T
     bool ok = true;
 #pragma unroll 1
@@ -690,7 +690,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
         if (!ok) break;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          sh.lse2[stage][lane + 32 * k] = fmaf(l[k], kLog2e, -kUp);
+          sh.lse2[stage][lane + 32 * k] = log2_sum(l[k], kUp);
           sh.delta[stage][lane + 32 * k] = e[k] * kDown;
         }
         role_arrive(&sh.full[stage]);
