@@ -772,7 +772,7 @@ typedef struct reskv_cross_attn_args {
 
 reskv_status reskv_cross_attn(const reskv_cross_attn_args* args, void* stream);
 
-/* Workspace bytes of reskv_cross_attn_backward; depends on n_tokens and q's heads. */
+/* Workspace bytes of reskv_cross_attn_backward, 16 a row and 1024; depends on n_tokens and q's heads. */
 size_t reskv_cross_attn_workspace(const reskv_cross_attn_args* args);
 
 /*
@@ -784,6 +784,8 @@ size_t reskv_cross_attn_workspace(const reskv_cross_attn_args* args);
  * left as they were.  Sums are fp32 in a fixed order (no atomics); p and t are rounded to q's type before
  * the products that sum them, t within its range: in fp16 gradients of 2^-24 and less are 0 (scale d_o, as
  * training in fp16 does).  What the rounding of o takes from D is put back.
+ * Logits may be of any size: rows whose |lse| passes 355 (fp32 then holds too few of its digits for a weight) have
+ * their weights' sum formed once more.
  *   d_o, d_q : q's shape and dtype;  d_k, d_v : k's shape and dtype
  */
 reskv_status reskv_cross_attn_backward(const reskv_cross_attn_args* args, const reskv_heads* d_o,

@@ -78,7 +78,7 @@ def gradient(q, k, v, d_o, scale, unit, least):
     return out, tol
 
 
-def gradient_norms(q, k, v, d_o, scale, unit, least, of_d=None):
+def gradient_norms(q, k, v, d_o, scale, unit, least, of_d=None, exact=False):
     """d_q, d_k, d_v of one sequence, and for each KV head what the norm of their errors may be.
 
     Every rounding is taken as an error of its own, evenly spread over half a step (`unit` of the value, `least`
@@ -88,7 +88,8 @@ def gradient_norms(q, k, v, d_o, scale, unit, least, of_d=None):
     sums, far less.  The norm of independent errors lies close to the root of their variance; 2.5 times that is
     past any one error's largest size (3^0.5 of it), and a gradient with a term left out is beyond it.
 
-    of_d: D = <d_o, o> of [n, H] to be used instead (mistakes to be refused)."""
+    of_d: D = <d_o, o> of [n, H] to be used instead (mistakes to be refused).  exact: every partial sum of a
+    logit fits fp32."""
     n, H, d = q.shape
     kv, length, _ = k.shape
     per = H // kv
@@ -102,7 +103,8 @@ def gradient_norms(q, k, v, d_o, scale, unit, least, of_d=None):
         D = (g * (p @ vv)).sum(1, keepdims=True) if of_d is None else of_d[:, h, None]
         dp = g @ vv.T
         t = p * (dp - D)
-        off = scale * np.sqrt(d) * 2.0 ** -23 * (np.abs(qq) @ np.abs(kk).T)       # of a logit: the weight's share
+        # of a logit, the weight's share; 2^-15: the log-sum-exp's up to 2^9
+        off = 2.0 ** -15 + (0 if exact else abs(scale) * np.sqrt(d) * 2.0 ** -23 * (np.abs(qq) @ np.abs(kk).T))
         t_var = (unit * t) ** 2 / 3 + least ** 2 / 3 + (off * t) ** 2 + (p * d * 2.0 ** -23) ** 2 * (g * g).sum(1, keepdims=True) * (vv * vv).sum(1)
         p_var = (unit * p) ** 2 / 3 + least ** 2 / 3 + (off * p) ** 2
         far = (kk * kk).sum(1) - 2 * (p @ kk) @ kk.T + ((p @ kk) ** 2).sum(1, keepdims=True)      # |k_j - mean k|^2

@@ -6,6 +6,7 @@
 #include <atomic>
 
 #include "paged.cuh"
+#include "warp_mma.cuh"
 
 namespace reskv {
 
@@ -17,7 +18,7 @@ struct CrossRows {
 struct CrossParams {
   CrossRows q, k, v, o, d_o, d_q, d_k, d_v;
   float* lse;
-  float* delta;                   // [n_tokens, heads]: <d_o, o> of every row (backward)
+  float4* stats;                  // [n_tokens, heads] (backward): a row's RowShift, and <d_o, o>
   const int32_t* q_begin;
   const int32_t* kv_begin;
   const int32_t* kv_lens;
@@ -36,6 +37,31 @@ struct CrossParams {
 constexpr float kFarLogits = 65536.f;
 // log2 of a row's sum, less `up`, of its ln: -inf (all logits are) as what leaves every weight 0.
 __device__ __forceinline__ float log2_sum(float lse, float up = 0.f) { return lse == -INFINITY ? 3.0e38f : fmaf(lse, kLog2e, -up); }
+
+// The weights of a row in the gradient: 2^((s f - hi) - lo - less), s f - hi rounded once.  The log-sum-exp that
+// the gradient is given will do for hi (with lo = less = 0) up to kFarSum, as log2: it is then off by 2^-15 of a weight.  Past
+// it fp32 has ever fewer of its digits for a weight (at 1e7 none), so the gradient finds the row's largest s f itself:
+// hi and lo are its product in full, less the log2 of the weights' sum beside it.
+constexpr float kFarSum = 512.f;
+__device__ __forceinline__ bool far_sum(float lse) { return fabsf(lse) * kLog2e > kFarSum && fabsf(lse) <= 3.0e38f; }
+struct RowShift {
+  float hi, lo, less;
+  __device__ __forceinline__ float exponent(float s, float f) const { return (fmaf(s, f, -hi) - lo) - less; }
+};
+struct FarSum {
+  float top = -INFINITY;          // the largest s so far, or -s where f < 0
+  float hi = 0.f, lo = 0.f, l = 0.f;          // top f in two parts; sum of the weights beside it
+  bool ok = true;
+  __device__ __forceinline__ float weight(float s, float f) const { return exp2_fast(fmaf(s, f, -hi) - lo); }
+  __device__ __forceinline__ void move(float to, float f) {
+    if (!(to > top)) return;
+    const float before = f < 0.f ? -top : top, now = f < 0.f ? -to : to;
+    hi = __fmul_rn(now, f);
+    lo = fmaf(now, f, -hi);
+    l = top == -INFINITY ? l : l * weight(before, f);
+    top = to;
+  }
+};
 
 // A sequence's query tokens and rows; `seen` of the rows take part.
 struct CrossSequence {

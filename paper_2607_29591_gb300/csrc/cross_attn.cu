@@ -110,7 +110,7 @@ extern "C" reskv_status reskv_cross_attn(const reskv_cross_attn_args* a, void* s
 
 extern "C" size_t reskv_cross_attn_workspace(const reskv_cross_attn_args* a) {
   if (!a || a->n_tokens < 0 || a->q.n_heads < 1) return 0;
-  return kLeftAlone + (size_t(a->n_tokens) * size_t(a->q.n_heads) * 4 + 255) / 256 * 256;
+  return kLeftAlone + (size_t(a->n_tokens) * size_t(a->q.n_heads) * sizeof(float4) + 255) / 256 * 256;
 }
 
 extern "C" reskv_status reskv_cross_attn_backward(const reskv_cross_attn_args* a, const reskv_heads* d_o, const reskv_heads* d_q,
@@ -138,7 +138,7 @@ extern "C" reskv_status reskv_cross_attn_backward(const reskv_cross_attn_args* a
     if (tokens) {
       p.d_o = rows_of(*d_o);
       p.d_q = rows_of(*d_q);
-      p.delta = reinterpret_cast<float*>(static_cast<char*>(a->workspace) + kLeftAlone);
+      p.stats = reinterpret_cast<float4*>(static_cast<char*>(a->workspace) + kLeftAlone);
     }
     if (rows) {
       p.d_k = rows_of(*d_k);

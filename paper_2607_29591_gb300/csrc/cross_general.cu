@@ -91,8 +91,6 @@ __global__ void __launch_bounds__(kWarps * 32) k_cross(const __grid_constant__ C
   if (p.lse && lane == 0) p.lse[tok * p.heads + h] = l != 0.f ? (top + log2f(l)) * 0.693147180559945f : -INFINITY;
 }
 
-// exp(x - lse) of one logit
-__device__ __forceinline__ float weight(float x2, float lse) { return exp2f(x2 - log2_sum(lse)); }
 
 template <int D, bool kF16>
 __global__ void __launch_bounds__(kWarps * 32) k_cross_grad_q(const __grid_constant__ CrossParams p) {
@@ -111,16 +109,30 @@ __global__ void __launch_bounds__(kWarps * 32) k_cross_grad_q(const __grid_const
   load_row<kF16>(o, p.o, tok, h, lane);
   load_row<kF16>(g, p.d_o, tok, h, lane);
   const float delta = dot(o, g), lse = p.lse[tok * p.heads + h];
+  RowShift shift{log2_sum(lse), 0.f, 0.f};
+  if (far_sum(lse)) {
+    FarSum sum;
+#pragma unroll 1
+    for (int j = 0; j < s.seen; ++j) {
+      float k[E];
+      load_row<kF16>(k, p.k, s.k0 + j, h / p.group, lane);
+      const float x = dot(q, k);
+      sum.move(p.scale2 < 0.f ? -x : x, p.scale2);
+      sum.l += sum.weight(x, p.scale2);
+    }
+    shift = RowShift{sum.hi, sum.lo, log2f(sum.l)};
+  }
 #pragma unroll 1
   for (int j = 0; j < s.seen; ++j) {
     float k[E], v[E];
     load_row<kF16>(k, p.k, s.k0 + j, h / p.group, lane);
     load_row<kF16>(v, p.v, s.k0 + j, h / p.group, lane);
-    const float w = weight(dot(q, k) * p.scale2, lse), t = w * (dot(g, v) - delta);
+    const float w = exp2f(shift.exponent(dot(q, k), p.scale2)), t = w * (dot(g, v) - delta);
 #pragma unroll
     for (int e = 0; e < E; ++e) dq[e] = fmaf(t, k[e], dq[e]);
   }
   store_row<kF16>(p.d_q, tok, h, lane, dq, p.scale);
+  if (lane == 0) p.stats[tok * p.heads + h] = make_float4(shift.hi, shift.lo, shift.less, delta);
 }
 
 template <int D, bool kF16>
@@ -143,11 +155,11 @@ __global__ void __launch_bounds__(kWarps * 32) k_cross_grad_kv(const __grid_cons
     for (int64_t i = 0; i < int64_t(s.count) * p.group; ++i) {
       const int64_t tok = s.q0 + i / p.group;
       const int hq = h * p.group + int(i % p.group);
-      float q[E], o[E], g[E];
+      float q[E], g[E];
       load_row<kF16>(q, p.q, tok, hq, lane);
-      load_row<kF16>(o, p.o, tok, hq, lane);
       load_row<kF16>(g, p.d_o, tok, hq, lane);
-      const float w = weight(dot(q, k) * p.scale2, p.lse[tok * p.heads + hq]), t = w * (dot(g, v) - dot(o, g));
+      const float4 stat = p.stats[tok * p.heads + hq];
+      const float w = exp2f(RowShift{stat.x, stat.y, stat.z}.exponent(dot(q, k), p.scale2)), t = w * (dot(g, v) - stat.w);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         dv[e] = fmaf(w, g[e], dv[e]);

@@ -22,6 +22,10 @@
 // 1.07 ms, 1.4 PFLOP/s; without exponentials, sums and roundings 1.0.  A tile's two pairs of products run while
 // the weights of the other pair are formed; tensor memory (S, G and two sums) is full at d = 128.
 //
+// Weights are formed from the log-sum-exp that the forward pass left up to kFarSum.  A block of queries with a row
+// past it first walks the sequence's states for the rows' own sums (S alone, every rank of a cluster all of
+// them), and leaves them for the states' kernel.
+//
 // Where there are too few blocks for the SMs, a cluster of CTAs shares a block's tiles: each leaves its two
 // sums in shared memory, where the cluster adds them up in order.
 //
@@ -40,7 +44,7 @@ using namespace tc;
 constexpr int kTile = 128;                        // rows and states of a tile
 constexpr int kThreads = 384;
 constexpr int kCopyWarp = 8, kIssueWarp = 9, kTailWarp = 10;
-constexpr int kRegsSoftmax = 232, kRegsIssue = 40;
+constexpr int kRegsSoftmax = 224, kRegsIssue = 56;
 static_assert((2 * kRegsSoftmax + kRegsIssue) * 128 <= 168 * kThreads, "registers");
 constexpr int kHalf = kTile * 128;                // bytes of 128 rows of 64 elements
 
@@ -150,6 +154,42 @@ __device__ __forceinline__ float dot8(uint4 a, uint4 b) {
   return s;
 }
 
+// --- rows whose logits are large (RowShift) ---
+// Few calls have any.  What they alone need is in functions of its own: within the kernels' loops, though
+// not run, it cost the others 4 to 6 of 46 us (8 x 512 tokens over 577 states).
+
+// Products s of a thread's row in TMEM, 64 columns, into what f makes their weights' exponents of.
+__noinline__ __device__ void shift_row(uint32_t at, RowShift shift, float f) {
+  const float inv = 1.f / f;
+#pragma unroll 1
+  for (int k0 = 0; k0 < 64; k0 += 16) {
+    float x[16];
+    load16(at + k0, x);
+    landed();
+    defined16(x);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) x[k] = shift.exponent(x[k], f) * inv;
+    store16(at + k0, x);
+  }
+  stored();
+}
+// The same where columns are the rows, with a shift each; a weight is 2^up at most, whatever the last
+// digits of s are in the other order of its factors.
+__noinline__ __device__ void shift_columns(uint32_t at, const float* hi, const float* lo, const float* less, float f, float up) {
+  const float inv = 1.f / f;
+#pragma unroll 1
+  for (int k0 = 0; k0 < 64; k0 += 16) {
+    float x[16];
+    load16(at + k0, x);
+    landed();
+    defined16(x);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) x[k] = min_nan(RowShift{hi[k0 + k], lo[k0 + k], less[k0 + k]}.exponent(x[k], f), up) * inv;
+    store16(at + k0, x);
+  }
+  stored();
+}
+
 // --- queries -------------------------------------------------------------------
 
 template <int D>
@@ -160,10 +200,49 @@ struct QuerySmem {
   static constexpr int bytes = at_ring + slots * tile + 1024;
 };
 struct QueryShared {
-  uint64_t q, full[8], empty[8], s, g, p, t, done, tail;
-  uint32_t tmem, abort;
+  uint64_t q, full[8], empty[8], s, g, p, t, done, tail, mode;
+  uint32_t tmem, abort, far;      // far: of any row; known once `mode` is complete
   float sums[2][kTile];           // D at the beginning, sums of T at the end
 };
+
+// The sums of a row's weights over its half of all tiles' columns, from tile `first` on: states left .. of them from
+// tile 0 on.
+__noinline__ __device__ FarSum far_sums(QueryShared& sh, uint32_t at, int first, int all, int left, float f, uint32_t* status) {
+  FarSum sum;
+#pragma unroll 1
+  for (int i = 0; i < all; ++i) {
+    const int tile = first + i < all ? first + i : first + i - all, upto = left - tile * kTile;
+    sum.ok = role_wait(&sh.s, i & 1, &sh.abort, status);
+    // (the G that came with the first S; its next comes after the last arrival below)
+    if (sum.ok && i == 0) sum.ok = role_wait(&sh.g, 0, &sh.abort, status);
+    if (!sum.ok) break;
+    fence_after();
+    float x[16], top = -INFINITY;
+    auto sixteen = [&](int k0) {
+      load16(at + k0, x);
+      landed();
+      defined16(x);
+    };
+#pragma unroll 1
+    for (int k0 = 0; k0 < 64; k0 += 16) {
+      sixteen(k0);
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (k0 + k < upto) top = fmaxf(top, f < 0.f ? -x[k] : x[k]);
+    }
+    sum.move(top, f);
+#pragma unroll 1
+    for (int k0 = 0; k0 < 64; k0 += 16) {
+      sixteen(k0);
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (k0 + k < upto) sum.l += sum.weight(x[k], f);
+    }
+    fence_before();
+    role_arrive(&sh.p);
+  }
+  return sum;
+}
 
 template <int D, bool kF16>
 __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_constant__ GradParams gp) {
@@ -188,7 +267,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
     mbar_init(&sh.t, 8);
     mbar_init(&sh.done, 1);
     mbar_init(&sh.tail, 1);
-    sh.abort = 0;
+    mbar_init(&sh.mode, 8);
+    sh.abort = sh.far = 0;
     fence_mbar_init();
   }
   if (warp == kCopyWarp && elected()) {
@@ -242,26 +322,33 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
       __syncwarp();
       int copied = 0;
       bool ok = true;
-#pragma unroll 1
-      for (int op = 0; op < 2 * n && ok; ++op) {
+      auto copy = [&](int op, int tile, bool last) {
         const int slot = op % S::slots, turn = op / S::slots;
         if (turn > 0) ok = role_wait(&sh.empty[slot], (turn - 1) & 1, &sh.abort, p.status);
-        if (!ok) break;
+        if (!ok) return;
         if (elected()) {
-          uint64_t* bar = cut && op == 2 * n - 2 ? &sh.tail : &sh.full[slot];
+          uint64_t* bar = last ? &sh.tail : &sh.full[slot];
           mbar_arrive_expect_tx(bar, S::tile);
 #pragma unroll
           for (int x = 0; x < D / 64; ++x)
-            copy_box(ring + slot * S::tile + x * kHalf, op & 1 ? &gp.v : &gp.k, 64 * x, h, sq.k0 + (first + op / 2) * kTile, bar);
+            copy_box(ring + slot * S::tile + x * kHalf, op & 1 ? &gp.v : &gp.k, 64 * x, h, sq.k0 + tile * kTile, bar);
         }
         __syncwarp();
         copied = op + 1;
+      };
+#pragma unroll 1
+      for (int op = 0; op < 2 * n && ok; ++op) copy(op, first + op / 2, cut && op == 2 * n - 2);
+      if (ok && n > 0) ok = role_wait(&sh.mode, 0, &sh.abort, p.status);
+      if (ok && sh.far) {                         // the other ranks' tiles, then the own ones again
+#pragma unroll 1
+        for (int op = 2 * n; op < 2 * (all + n) && ok; ++op)
+          copy(op, op < 2 * all ? (first + op / 2) % all : first + op / 2 - all, cut && op == 2 * (all + n) - 2);
       }
       if (!ok && lane == 0) {                     // a wait gave up: let what is in flight land
         mbar_wait_bounded(&sh.q, 0);
         for (int op = copied > S::slots ? copied - S::slots : 0; op < copied; ++op) {
-          const bool last = cut && op == 2 * n - 2;
-          mbar_wait_bounded(last ? &sh.tail : &sh.full[op % S::slots], last ? 0 : (op / S::slots) & 1);
+          const bool again = op == 2 * (all + n) - 2, last = cut && (op == 2 * n - 2 || again);
+          mbar_wait_bounded(last ? &sh.tail : &sh.full[op % S::slots], last ? again : (op / S::slots) & 1);
         }
       }
       __syncwarp();
@@ -303,26 +390,46 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
       if (ok) {
         outer(g_cols, smem_g, tile_of(1), &sh.g);
         release(1);
+        ok = role_wait(&sh.mode, 0, &sh.abort, p.status);
       }
+      int s0 = 0;                                 // tiles whose logits went to the rows' sums
+      if (ok && sh.far) {
+        s0 = all;
+        // S of every tile, then the own tiles' first products again
 #pragma unroll 1
-      for (int i = 0; i < n && ok; ++i) {
-        ok = role_wait(&sh.p, i & 1, &sh.abort, p.status);
-        if (!ok) break;
-        add_to(b_cols, s_cols, tile_of(2 * i), i > 0);
-        if (i + 1 < n) {
+        for (int i = 0; i < all && ok; ++i) {
+          ok = role_wait(&sh.p, i & 1, &sh.abort, p.status);       // the tile is read
+          if (!ok) break;
+          release(2 * i);
           ok = wait_tile(2 * i + 2);
           if (!ok) break;
           outer(s_cols, smem_q, tile_of(2 * i + 2), &sh.s);
+          ok = wait_tile(2 * i + 3);
+          if (!ok) break;
+          if (i + 1 == all) outer(g_cols, smem_g, tile_of(2 * i + 3), &sh.g);
+          release(2 * i + 3);
+        }
+      }
+#pragma unroll 1
+      for (int i = 0; i < n && ok; ++i) {
+        const int op = 2 * (s0 + i);
+        ok = role_wait(&sh.p, (s0 + i) & 1, &sh.abort, p.status);
+        if (!ok) break;
+        add_to(b_cols, s_cols, tile_of(op), i > 0);
+        if (i + 1 < n) {
+          ok = wait_tile(op + 2);
+          if (!ok) break;
+          outer(s_cols, smem_q, tile_of(op + 2), &sh.s);
         }
         ok = role_wait(&sh.t, i & 1, &sh.abort, p.status);
         if (!ok) break;
-        add_to(o_cols, g_cols, tile_of(2 * i), i > 0);
-        release(2 * i);
+        add_to(o_cols, g_cols, tile_of(op), i > 0);
+        release(op);
         if (i + 1 < n) {
-          ok = wait_tile(2 * i + 3);
+          ok = wait_tile(op + 3);
           if (!ok) break;
-          outer(g_cols, smem_g, tile_of(2 * i + 3), &sh.g);
-          release(2 * i + 3);
+          outer(g_cols, smem_g, tile_of(op + 3), &sh.g);
+          release(op + 3);
         }
       }
       if (elected()) commit(&sh.done);
@@ -330,12 +437,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
       if (!ok) mbar_wait_bounded(&sh.done, 0);
     } else if (warp == kTailWarp && cut) {
       // --- behind the last state: P and T are zero there, keys may be anything ---
-      const int slot = (2 * n - 2) % S::slots;
-      if (role_wait(&sh.tail, 0, &sh.abort, p.status)) {
+      auto clear = [&](int op, uint32_t parity) {
+        const int slot = op % S::slots;
+        if (!role_wait(&sh.tail, parity, &sh.abort, p.status)) return false;
         clear_rows<D>(smem + S::at_ring + slot * S::tile, left, kTile, lane);
         fence_proxy_async_smem();
         role_arrive(&sh.full[slot]);
-      }
+        return true;
+      };
+      if (clear(2 * n - 2, 0) && role_wait(&sh.mode, 0, &sh.abort, p.status) && sh.far) clear(2 * (all + n) - 2, 1);
     }
     __syncwarp();
     meet(cs);                                     // the others have read what they read of tensor memory
@@ -350,6 +460,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
     // D: half of the row's dims each
     float delta = 0.f;
+    const int64_t stat = at_token * p.heads + head;
+    const float lse = real ? p.lse[stat] : 0.f;
     if (real) {
       const uint4* g = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.d_o.data) + at_token * p.d_o.token +
                                                       head * p.d_o.head + c * (D / 2));
@@ -358,20 +470,47 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) delta += dot8<kF16>(g[k], o[k]);
     }
+    const bool far_row = far_sum(lse);
+    if (__any_sync(0xffffffffu, far_row) && lane == 0) *static_cast<volatile uint32_t*>(&sh.far) = 1u;
+    role_arrive(&sh.mode);
     sh.sums[c][rt] = delta;
     asm volatile("bar.sync 1, 256;" ::: "memory");
     delta = sh.sums[0][rt] + sh.sums[1][rt];
+    const bool far = sh.far != 0;
     asm volatile("bar.sync 1, 256;" ::: "memory");      // (a rank without tiles comes to its next sums at once)
-    const int64_t stat = at_token * p.heads + head;
-    const float f = p.scale2, lse2 = real ? log2_sum(p.lse[stat], kUp) : 0.f, down = -delta * kDown;
+    auto both_halves = [&](float x) {
+      sh.sums[c][rt] = x;
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      x = sh.sums[0][rt] + sh.sums[1][rt];
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      return x;
+    };
+    const float f = p.scale2, down = -delta * kDown;
+    RowShift shift{log2_sum(lse, kUp), 0.f, 0.f};
     float2 more = make_float2(0.f, 0.f), rounded = more;      // sums of T
     bool ok = true;
+    if (far && n > 0) {
+      // the rows' sums, over all tiles of the sequence (each rank for itself)
+      FarSum sum = far_sums(sh, s_cols + lanes + 64 * c, first, all, sq.seen - 64 * c, f, p.status);
+      ok = sum.ok;
+      // both halves of the row
+      sh.sums[c][rt] = sum.top;
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      const float top = fmaxf(sh.sums[0][rt], sh.sums[1][rt]);
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      sum.move(top, f);
+      const float l = both_halves(sum.l);
+      if (far_row) shift = RowShift{sum.hi, sum.lo, log2f(l) - kUp};
+    }
+    const int s0 = far ? all : 0, g0 = far ? 1 : 0;       // phases that are over
+    const float lse2 = far ? 0.f : shift.hi;
 #pragma unroll 1
-    for (int i = 0; i < n; ++i) {
+    for (int i = 0; i < n && ok; ++i) {
       const int upto = (i == n - 1 ? left : kTile) - 64 * c;
-      ok = role_wait(&sh.s, i & 1, &sh.abort, p.status);
+      ok = role_wait(&sh.s, (s0 + i) & 1, &sh.abort, p.status);
       if (!ok) break;
       fence_after();
+      if (far) shift_row(s_cols + lanes + 64 * c, shift, f);
       float x[64];
       load64(s_cols + lanes + 64 * c, x);
       landed64(x);
@@ -389,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
       store64<kF16>(s_cols + lanes + 64 * c, x);
       fence_before();
       role_arrive(&sh.p);
-      ok = role_wait(&sh.g, i & 1, &sh.abort, p.status);
+      ok = role_wait(&sh.g, (g0 + i) & 1, &sh.abort, p.status);
       if (!ok) break;
       fence_after();
       float y[64];
@@ -414,15 +553,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
       role_arrive(&sh.t);
     }
     if (ok && n > 0) ok = role_wait(&sh.done, 0, &sh.abort, p.status);
-    auto both_halves = [&](float x) {
-      sh.sums[c][rt] = x;
-      asm volatile("bar.sync 1, 256;" ::: "memory");
-      x = sh.sums[0][rt] + sh.sums[1][rt];
-      asm volatile("bar.sync 1, 256;" ::: "memory");
-      return x;
-    };
     const float lacks = both_halves(more.x + more.y), e = both_halves(rounded.x + rounded.y);
-    if (cs == 1 && real && c == 0) p.delta[stat] = delta + lacks;
+    if (rank == cs - 1 && real && c == 0) p.stats[stat] = make_float4(shift.hi, shift.lo, shift.less, delta + lacks);
     if (cs > 1) {
       // for the join: all products are done, operands' memory is free
       fence_after();
@@ -431,7 +563,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
         leave_columns<D, D / 2>(o_cols + lanes + c * (D / 2), rows, rt, c * (D / 2));
         leave_columns<D, D / 2>(b_cols + lanes + c * (D / 2), rows + kTile * (D / 4), rt, c * (D / 2));
       }
-      if (c == 0) reinterpret_cast<float4*>(smem + 2 * kTile * D * 4)[rt] = make_float4(rank == 0 ? delta : 0.f, lacks, e, 0.f);
+      if (c == 0) reinterpret_cast<float4*>(smem + 2 * kTile * D * 4)[rt] = make_float4(rank == cs - 1 ? delta : 0.f, lacks, e, 0.f);
     } else if (ok) {
       fence_after();
       const float back = -e * kDown;
@@ -479,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
         if (lane < D / 4)
           reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.d_q.data) + tok * p.d_q.token + hd * p.d_q.head)[u] = pack_four<kF16>(
               make_float4(fmaf(back, y.x, x.x), fmaf(back, y.y, x.y), fmaf(back, y.z, x.z), fmaf(back, y.w, x.w)), p.scale);
-        if (lane == 0) p.delta[tok * p.heads + hd] = s[m].x + s[m].y;
+        if (lane == 0) p.stats[tok * p.heads + hd].w = s[m].x + s[m].y;
       }
       __syncwarp();
     }
@@ -500,7 +632,8 @@ struct StateSmem {
 struct StateShared {
   uint64_t kv, full[kStages], empty[kStages], s, g, p, t, done, tail;
   uint32_t tmem, abort;
-  alignas(16) float lse2[kStages][kTile], delta[kStages][kTile];
+  uint32_t far[kStages];          // of any row of the tile
+  alignas(16) float lse2[kStages][kTile], hi[kStages][kTile], lo[kStages][kTile], less[kStages][kTile], delta[kStages][kTile];
 };
 
 template <int D, bool kF16>
@@ -677,22 +810,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
 #pragma unroll 1
       for (int i = 0; i < n && ok; ++i) {
         const int stage = i % kStages;
-        float l[4], e[4];
+        float4 v[4];
+        bool far = false;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int r = lane + 32 * k, tk = (first + i) * tt + r / p.group;
           const bool here = r < used && tk < sq.count;
-          const int64_t at = int64_t(sq.q0 + tk) * p.heads + h * p.group + r % p.group;
-          l[k] = here ? p.lse[at] : 0.f;
-          e[k] = here ? p.delta[at] : 0.f;
+          v[k] = here ? p.stats[int64_t(sq.q0 + tk) * p.heads + h * p.group + r % p.group] : make_float4(0.f, 0.f, 0.f, 0.f);
+          far |= v[k].y != 0.f || v[k].z != 0.f;
         }
+        far = __any_sync(0xffffffffu, far);
         if (i >= kStages) ok = role_wait(&sh.empty[stage], (i / kStages - 1) & 1, &sh.abort, p.status);
         if (!ok) break;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          sh.lse2[stage][lane + 32 * k] = log2_sum(l[k], kUp);
-          sh.delta[stage][lane + 32 * k] = e[k] * kDown;
+          sh.lse2[stage][lane + 32 * k] = far ? 0.f : v[k].x;
+          if (far) {
+            sh.hi[stage][lane + 32 * k] = v[k].x;
+            sh.lo[stage][lane + 32 * k] = v[k].y;
+            sh.less[stage][lane + 32 * k] = v[k].z;
+          }
+          sh.delta[stage][lane + 32 * k] = v[k].w * kDown;
         }
+        if (lane == 0) sh.far[stage] = far;
         role_arrive(&sh.full[stage]);
       }
     }
@@ -713,9 +853,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
     for (int i = 0; i < n; ++i) {
       const int stage = i % kStages, upto = (i == n - 1 ? left : used) - 64 * c;
       // (the tile's barrier also has its sums behind it)
-      ok = role_wait(&sh.full[stage], (i / kStages) & 1, &sh.abort, p.status) && role_wait(&sh.s, i & 1, &sh.abort, p.status);
+      ok = role_wait(&sh.full[stage], (i / kStages) & 1, &sh.abort, p.status);
+      const bool far = sh.far[stage] != 0;
+      ok = ok && role_wait(&sh.s, i & 1, &sh.abort, p.status);
       if (!ok) break;
       fence_after();
+      if (far) shift_columns(s_cols + lanes + 64 * c, &sh.hi[stage][64 * c], &sh.lo[stage][64 * c], &sh.less[stage][64 * c], f, kUp);
       float x[64];
       load64(s_cols + lanes + 64 * c, x);
       landed64(x);
