@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kWarps * 32) k_cross_grad_q(const __grid_const
   const int b = owner(p.q_begin, p.batch, p.n_tokens, tok);
   if (b < 0) return;
   const CrossSequence s = cross_sequence(p, b);
-  float q[E], o[E], g[E], dq[E] = {};
+  float q[E], o[E], g[E], dq[E] = {}, mean[E] = {}, lacks = 0.f;        // sums of T k, P k and T
   load_row<kF16>(q, p.q, tok, h, lane);
   load_row<kF16>(o, p.o, tok, h, lane);
   load_row<kF16>(g, p.d_o, tok, h, lane);
@@ -128,11 +128,18 @@ __global__ void __launch_bounds__(kWarps * 32) k_cross_grad_q(const __grid_const
     load_row<kF16>(k, p.k, s.k0 + j, h / p.group, lane);
     load_row<kF16>(v, p.v, s.k0 + j, h / p.group, lane);
     const float w = exp2f(shift.exponent(dot(q, k), p.scale2)), t = w * (dot(g, v) - delta);
+    lacks += t;
 #pragma unroll
-    for (int e = 0; e < E; ++e) dq[e] = fmaf(t, k[e], dq[e]);
+    for (int e = 0; e < E; ++e) {
+      dq[e] = fmaf(t, k[e], dq[e]);
+      mean[e] = fmaf(w, k[e], mean[e]);
+    }
   }
+  // P sums up to 1, so the sum of T is what D of the rounded o lacks
+#pragma unroll
+  for (int e = 0; e < E; ++e) dq[e] = fmaf(-lacks, mean[e], dq[e]);
   store_row<kF16>(p.d_q, tok, h, lane, dq, p.scale);
-  if (lane == 0) p.stats[tok * p.heads + h] = make_float4(shift.hi, shift.lo, shift.less, delta);
+  if (lane == 0) p.stats[tok * p.heads + h] = make_float4(shift.hi, shift.lo, shift.less, delta + lacks);
 }
 
 template <int D, bool kF16>

@@ -10,7 +10,7 @@ from test_cross_gpu import LEAST, Case
 
 pytestmark = pytest.mark.gpu
 
-FORMS = [([1, 3], [300, 40], 0), ([3], [3000], 0), ([40, 9], [300, 129], 0), ([20, 30], [2100, 700], 0), ([300], [400], 0)]
+FORMS = [([1, 3], [300, 40], 0), ([3], [3000], 0), ([40, 9], [300, 129], 0), ([20, 30], [2100, 700], 0), ([300], [400], 0), ([4, 9], [60, 50], 2)]
 
 
 def offset_case(counts, lens, d, dtype, size, sign, offset, both=False):

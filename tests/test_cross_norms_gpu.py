@@ -26,7 +26,22 @@ def test_queries_akin_to_a_key(n, states, d, dtype):
     for t, r, _ in c.sequences():
         pick = torch.from_numpy(rng.integers(r.start, r.stop, n)).cuda()
         near = c.k[pick].repeat_interleave(c.per, 1)
-        c.q[t] = (0.3 * near.float() + 0.7 * c.q[t].float()).to(c.q.dtype)
+        c.q[t] = (1.5 * near.float() + 0.7 * c.q[t].float()).to(c.q.dtype)
+    c.q64 = c.q.double().cpu().numpy()
+    c.check()
+    check_norms(c)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("offset", [1, 4])
+@pytest.mark.parametrize("n,states,d", [(1, 40, 64), (20, 100, 128), (40, 200, 64)])
+def test_rows_of_any_alignment(n, states, d, offset, dtype):
+    """The same for rows off 16-byte boundaries, with queries akin to a key."""
+    c = Case(53, [n, n], [states, states + 1], 2, 4, d, dtype, offset=offset)
+    rng = np.random.default_rng(n)
+    for t, r, _ in c.sequences():
+        pick = torch.from_numpy(rng.integers(r.start, r.stop, n)).cuda()
+        c.q[t] = (1.5 * c.k[pick].repeat_interleave(c.per, 1).float() + 0.7 * c.q[t].float()).to(c.q.dtype)
     c.q64 = c.q.double().cpu().numpy()
     c.check()
     check_norms(c)
