@@ -852,13 +852,16 @@ def _workspace(device, stream: int, nbytes: int):
     return held
 
 
-def _kept_workspace(lib, t, stream: int, need: int, size: str):
-    """The workspace kept for the tensor's device and the stream, of `need` bytes at least."""
+def _kept_workspace(lib, t, stream: int, need: int, size: str, look_over=None):
+    """The workspace kept for the tensor's device and the stream, of `need` bytes at least.  look_over:
+    called before one is made."""
     if lib.reskv_stream_capturing(stream):
         raise ValueError("a call that is captured into a graph needs workspace=: a zeroed uint8 tensor of "
                          f"{size} bytes, made before the capture")
     held = _workspaces.get((t.get_device(), stream))
     if held is None or held[-1].numel() < need:
+        if look_over is not None:
+            look_over()
         held = _workspace(t.device, stream, need)
     return held[-1]
 
@@ -888,32 +891,35 @@ def reskv_paged_attn(kv: PagedKV, q, lens, o, q_begin=None, scale: Optional[floa
     captured into a graph brings its own.
     """
     lib = _calls()
-    heads, out = q.shape[1] if q.dim() == 3 else 0, o.dtype
+    fields = _attn(kv, q, lens, o, q_begin, scale, window, lse)
     s = _stream_of(stream, q)
     if workspace is None:
-        need = kv.attn_workspace.get((q.shape[0], heads, out))
-        if need is None and out in _dtypes:
-            need = kv.attn_workspace[q.shape[0], heads, out] = reskv_paged_attn_workspace(kv, q.shape[0], heads, out)
-        workspace = _kept_workspace(lib, q, s, need or 0, "reskv_paged_attn_workspace()")
-    st = lib.reskv_paged_attn(kv.address, _attn(kv, q, lens, o, q_begin, scale, window, lse, workspace), s)
+        key = q.shape[0], q.shape[1], o.dtype
+        need = kv.attn_workspace.get(key)
+        if need is None:
+            need = kv.attn_workspace[key] = reskv_paged_attn_workspace(kv, *key)
+        workspace = _kept_workspace(lib, q, s, need, "reskv_paged_attn_workspace()")
+    st = lib.reskv_paged_attn(kv.address, _pack_attn(*fields, *_bytes_of(workspace)), s)
     if st:
         _check(st)
 
 
-def _attn(kv: PagedKV, q, lens, o, q_begin, scale, window, lse, workspace) -> bytes:
-    """A reskv_paged_attn_args' bytes."""
+def _bytes_of(workspace):
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _attn(kv: PagedKV, q, lens, o, q_begin, scale, window, lse):
+    """A reskv_paged_attn_args' fields up to the workspace."""
     T, d, B = q.shape[0], kv.head_dim, kv.batch
     qh = _heads(q, "q", T, None, d)
     oh = _heads(o, "o", T, qh[3], d)
     if lse is not None and lse.numel() != T * qh[3]:
         raise ValueError(f"lse must hold {T * qh[3]} elements, got {lse.numel()}")
-    if not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous CUDA tensor")
-    return _pack_attn(
-        *qh, *oh, 0 if lse is None else _dptr(lse, "torch.float32", "lse").value,
-        0 if q_begin is None else _ints(q_begin, "q_begin", B + 1), _ints(lens, "lens", B), T,
-        0.0 if scale is None else scale, window, workspace.data_ptr(),
-        workspace.numel() * workspace.element_size())
+    return (*qh, *oh, 0 if lse is None else _dptr(lse, "torch.float32", "lse").value,
+            0 if q_begin is None else _ints(q_begin, "q_begin", B + 1), _ints(lens, "lens", B), T,
+            0.0 if scale is None else scale, window)
 
 
 def reskv_paged_attn_workspace(kv: PagedKV, n_tokens: int, heads: int, out_dtype=None) -> int:
@@ -940,16 +946,17 @@ def reskv_paged_attn_shared(kv: PagedKV, prefix: PagedKV, q, lens, prefix_lens, 
     least reskv_paged_attn_shared_workspace() bytes (None: one kept per stream).
     """
     lib = _calls()
+    fields = _attn(kv, q, lens, o, q_begin, scale, 0, lse)
+    seqs = None if seq_begin is None else _ints(seq_begin, "seq_begin", prefix.batch + 1)
+    held = _ints(prefix_lens, "prefix_lens", prefix.batch)
     s = _stream_of(stream, q)
     if workspace is None:
-        key = (q.shape[0], q.shape[1] if q.dim() == 3 else 0, o.dtype, prefix.batch, prefix.table_pages)
+        key = (q.shape[0], q.shape[1], o.dtype, prefix.batch, prefix.table_pages)
         need = kv.attn_workspace.get(key)
-        if need is None and o.dtype in _dtypes:
+        if need is None:
             need = kv.attn_workspace[key] = reskv_paged_attn_shared_workspace(kv, prefix, key[0], key[1], o.dtype)
-        workspace = _kept_workspace(lib, q, s, need or 0, "reskv_paged_attn_shared_workspace()")
-    st = lib.reskv_paged_attn_shared(
-        kv.address, prefix.address, None if seq_begin is None else _ints(seq_begin, "seq_begin", prefix.batch + 1),
-        _ints(prefix_lens, "prefix_lens", prefix.batch), _attn(kv, q, lens, o, q_begin, scale, 0, lse, workspace), s)
+        workspace = _kept_workspace(lib, q, s, need, "reskv_paged_attn_shared_workspace()")
+    st = lib.reskv_paged_attn_shared(kv.address, prefix.address, seqs, held, _pack_attn(*fields, *_bytes_of(workspace)), s)
     if st:
         _check(st)
 
@@ -1034,15 +1041,26 @@ def reskv_cross_attn_backward(q, k, v, o, lse, d_o, d_q, d_k, d_v, batch: int = 
     stream); a call that is captured into a graph brings its own.
     """
     lib = _calls()
-    s = _stream_of(stream, q)
-    T = q.shape[0]
     if lse is None:
         raise ValueError("the gradient needs the lse of reskv_cross_attn")
+
+    def gradients():
+        T, H, d, rows, kv = *q.shape, k.shape[0], k.shape[1]
+        return [_pack_heads(*_heads(t, what, n, h, d)) for t, what, n, h in
+                ((d_o, "d_o", T, H), (d_q, "d_q", T, H), (d_k, "d_k", rows, kv), (d_v, "d_v", rows, kv))]
+
+    def look_over():
+        _cross(q, k, v, o, batch, q_begin, kv_begin, kv_lens, scale, lse, status)
+        gradients()
+
+    if not q.is_cuda or q.dim() != 3:
+        look_over()
+    s = _stream_of(stream, q)
     if workspace is None:
-        need = _cross_workspace.get(key := (T, q.shape[1]))
+        need = _cross_workspace.get(key := (q.shape[0], q.shape[1]))
         if need is None:
             need = _cross_workspace[key] = reskv_cross_attn_workspace(*key)
-        workspace = _kept_workspace(lib, q, s, need, "reskv_cross_attn_workspace()")
+        workspace = _kept_workspace(lib, q, s, need, "reskv_cross_attn_workspace()", look_over)
     elif not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous CUDA tensor")
     if _bind is not None:
@@ -1050,10 +1068,6 @@ def reskv_cross_attn_backward(q, k, v, o, lse, d_o, d_q, d_k, d_v, batch: int = 
         if st >= 0:
             return _check(st) if st else None
     a = _cross(q, k, v, o, batch, q_begin, kv_begin, kv_lens, scale, lse, status, workspace)
-    H, d, rows, kv = q.shape[1], q.shape[2], k.shape[0], k.shape[1]
-    st = lib.reskv_cross_attn_backward(a, _pack_heads(*_heads(d_o, "d_o", T, H, d)),
-                                       _pack_heads(*_heads(d_q, "d_q", T, H, d)),
-                                       _pack_heads(*_heads(d_k, "d_k", rows, kv, d)),
-                                       _pack_heads(*_heads(d_v, "d_v", rows, kv, d)), s)
+    st = lib.reskv_cross_attn_backward(a, *gradients(), s)
     if st:
         _check(st)
