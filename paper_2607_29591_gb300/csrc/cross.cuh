@@ -127,7 +127,7 @@ __device__ __forceinline__ bool cross_block(const CrossParams& p, const int32_t*
       const int l = after ? __ffs(after) - 2 : 31;
       if (step == 1) {
         out.b = lo + l;
-        blocks = (__shfl_sync(0xffffffffu, count, l) * times + per - 1) / per;
+        blocks = ceil_div(__shfl_sync(0xffffffffu, count, l) * times, per);
         item -= __shfl_sync(0xffffffffu, start, l) * p.kv_heads;
         break;
       }
@@ -141,7 +141,7 @@ __device__ __forceinline__ bool cross_block(const CrossParams& p, const int32_t*
     }
     if (item >= blocks * p.kv_heads) return false;
   } else {
-    blocks = (each * times + per - 1) / per;
+    blocks = ceil_div(each * times, per);
     out.b = item / (blocks * p.kv_heads);
     item -= out.b * blocks * p.kv_heads;
   }

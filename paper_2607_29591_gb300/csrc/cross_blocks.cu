@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_blocks(const __grid_const
   const int b = block.b, h = block.h, t0 = block.first;
   const CrossSequence sq = cross_sequence(p, b);
   const bool two = !kSplit && t0 + tt < sq.count, joins = kSplit || cs > 1;
-  const int all = (sq.seen + kStates - 1) / kStates;
+  const int all = ceil_div(sq.seen, kStates);
   const int first = tiles_before(all, rank, cs), n = tiles_before(all, rank + 1, cs) - first;      // tiles of states
   const int steps[2] = {kSplit ? (n + 1) / 2 : n, kSplit ? n / 2 : two ? n : 0};
   const int left = sq.seen - (first + n - 1) * kStates;               // states of the last tile

@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_q(const __grid_const
   if (!cross_block(p, p.q_begin, p.q_each, p.n_tokens, tt, int(blockIdx.x) / cs, lane, block)) return;      // the whole cluster
   const int h = block.h, t0 = block.first, used_rows = tt * p.group;
   const CrossSequence sq = cross_sequence(p, block.b);
-  const int all = (sq.seen + kTile - 1) / kTile;
+  const int all = ceil_div(sq.seen, kTile);
   const int first = tiles_before(all, rank, cs), n = tiles_before(all, rank + 1, cs) - first;      // tiles of states
   const int left = sq.seen - (first + n - 1) * kTile;                 // states of the last
   const bool cut = n > 0 && left < kTile;
@@ -677,7 +677,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_grad_kv(const __grid_cons
   const int h = block.h, j0 = block.first;
   const CrossSequence sq = cross_sequence(p, block.b);
   const int tt = gp.tile_tokens, used = tt * p.group;                 // rows of a full tile
-  const int all = j0 < sq.seen ? (sq.count + tt - 1) / tt : 0;
+  const int all = j0 < sq.seen ? ceil_div(sq.count, tt) : 0;
   const int first = tiles_before(all, rank, cs), n = tiles_before(all, rank + 1, cs) - first;      // tiles of rows
   const int left = min((sq.count - (first + n - 1) * tt) * p.group, used);      // rows of the last
   const bool cut = n > 0 && left < used;

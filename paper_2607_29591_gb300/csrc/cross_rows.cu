@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(kThreads) k_cross_rows(const __grid_constant__
   const int h = block.h, r0 = block.first;
   const CrossSequence sq = cross_sequence(p, block.b);
   const int rows = min(sq.count * p.group - r0, kRows);               // of this block
-  const int all = (sq.seen + kRowStates - 1) / kRowStates;
+  const int all = ceil_div(sq.seen, kRowStates);
   const int first = tiles_before(all, rank, cs), n = tiles_before(all, rank + 1, cs) - first;
   const uint32_t ring = smem_u32(smem);
   if (fixed) wait_for_previous();

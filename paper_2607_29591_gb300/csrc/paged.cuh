@@ -117,6 +117,9 @@ __device__ __forceinline__ void wait_for_previous() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// x / per rounded up, of any x >= 0 (x + per may pass 2^31).
+__device__ __forceinline__ int ceil_div(int x, int per) { return int((uint32_t(x) + uint32_t(per) - 1u) / uint32_t(per)); }
+
 inline int dtype_size(int32_t dtype) { return dtype == RESKV_F32 ? 4 : 2; }
 inline bool dtype_known(int32_t dtype) { return dtype >= RESKV_BF16 && dtype <= RESKV_F32; }
 inline bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }

@@ -656,7 +656,7 @@ __device__ __forceinline__ GroupPlan group_plan(const SharedParams& p, int block
     units = steps = 0;
     if (g >= p.batch) return s;
     s = group_of(p, g, p.batch);
-    steps = (s.len + kBlockPos - 1) / kBlockPos;
+    steps = ceil_div(s.len, kBlockPos);
     if (steps > 0) units = int((int64_t(s.count) * p.group + block_rows - 1) / block_rows) * p.kv_heads;
     return s;
   };

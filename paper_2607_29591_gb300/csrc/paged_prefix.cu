@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_prefix(const __grid_consta
   }
   const int local = int(blockIdx.x) - plan.first, hp = local / plan.row_blocks, part = hp % plan.parts, h = hp / plan.parts;
   const int r0 = (local - hp * plan.row_blocks) * kRows, rows = min(plan.count * p.group - r0, kRows);
-  const int all = (plan.len + kPos - 1) / kPos;
+  const int all = ceil_div(plan.len, kPos);
   const int first = int(int64_t(all) * part / plan.parts), n = int(int64_t(all) * (part + 1) / plan.parts) - first;      // tiles, > 0
   const int steps[2] = {kSplit ? (n + 1) / 2 : n, kSplit ? n / 2 : rows > 128 ? n : 0};
   const uint32_t smem_q = smem_u32(smem);
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_prefix(const __grid_consta
     const bool values = uw & 1;
     const int tpp = p.page_tokens / kTile;
     const int32_t* table = p.page_table + int64_t(plan.group) * p.table_pages;
-    const int tiles = (plan.len + kTile - 1) / kTile;               // cache tiles held
+    const int tiles = ceil_div(plan.len, kTile);                   // cache tiles held
     auto page_of = [&](int i) {                   // of this warp's cache tile of tile i
       const int tile = (first + i) * kSub + sub;
       return i < n && tile < tiles ? __ldg(table + tile / tpp) : -1;
