@@ -787,6 +787,7 @@ size_t reskv_cross_attn_workspace(const reskv_cross_attn_args* args);
  * Logits may be of any size: rows whose |lse| passes 355 (fp32 then holds too few of its digits for a weight) have
  * their weights' sum formed once more.
  *   d_o, d_q : q's shape and dtype;  d_k, d_v : k's shape and dtype
+ * d_q lies over none of q, d_o, k and v, d_k and d_v over neither q nor d_o, and none over another.
  */
 reskv_status reskv_cross_attn_backward(const reskv_cross_attn_args* args, const reskv_heads* d_o,
                                        const reskv_heads* d_q, const reskv_heads* d_k,

@@ -1,6 +1,7 @@
 // Attention to states of another length: the entry points (reskv_cross_attn,
 // reskv_cross_attn_backward), what they refuse and which kernels they take.
 #include <cmath>
+#include <initializer_list>
 
 #include "cross.cuh"
 
@@ -80,6 +81,18 @@ bool encode_maps(CrossMaps* maps, const reskv_cross_attn_args* a, const CrossPar
          encode_heads(&maps->v, a->v, a->n_rows, a->head_dim, 1, box_states);
 }
 
+// Whether a gradient begins where another tensor does that blocks beside its own still read or write (no full look for
+// overlaps; over o, and d_k and d_v over k or v, each block has read its rows before it writes them).
+bool in_the_way(const reskv_cross_attn_args* a, const reskv_heads* d_o, const reskv_heads* d_q, const reskv_heads* d_k,
+                const reskv_heads* d_v, bool tokens, bool rows) {
+  if (tokens && (d_q->data == a->q.data || d_q->data == d_o->data)) return true;
+  if (rows && d_k->data == d_v->data) return true;
+  if (!tokens || !rows) return false;
+  for (const void* x : {d_k->data, d_v->data})
+    if (x == a->q.data || x == d_o->data || x == d_q->data) return true;
+  return d_q->data == a->k.data || d_q->data == a->v.data;
+}
+
 // The kernel of few rows where a sequence and KV head have kFewRows of them on average.
 constexpr int kFewRows = 16;
 
@@ -132,6 +145,8 @@ extern "C" reskv_status reskv_cross_attn_backward(const reskv_cross_attn_args* a
     if (bad.empty() && tokens &&
         (!a->workspace || !aligned_to(a->workspace, 256) || a->workspace_bytes < reskv_cross_attn_workspace(a)))
       bad = "workspace must be 256-byte aligned and hold reskv_cross_attn_workspace() bytes";
+    if (bad.empty() && in_the_way(a, d_o, d_q, d_k, d_v, tokens, rows))
+      bad = "d_q must not lie over q, d_o, k or v, d_k and d_v not over q or d_o, and none over another";
     if (!bad.empty()) return paged_fail(RESKV_ERR_INVALID_ARG, bad);
     if (!tokens && !rows) return RESKV_OK;
     CrossParams p = params_of(a);
