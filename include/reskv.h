@@ -703,16 +703,22 @@ reskv_status reskv_paged_attn(const reskv_paged_kv* kv, const reskv_paged_attn_a
  * positions 0 .. prefix_lens[g] - 1 of row g of prefix->page_table, then, as always, the own
  * positions up to their own.  Query i of n_b stands at own position p = lens[b] - n_b + i; one
  * with p < 0 sees the prefix alone; one that sees nothing gets o = 0.  A prefix's pages are read
- * and unpacked once for 128 or 256 rows (query tokens times heads / n_kv_heads) of a group,
- * not once for every sequence.
+ * and unpacked once for 128 or 256 rows (query tokens times heads / n_kv_heads) of a group
+ * where groups have 32 rows or more on average (128 in small calls), o has 16 bits and scale is
+ * not negative, else once for eight rows; not once for every sequence.
  *
  * kv and prefix have the same head shape, page_tokens and quant_group, and may share their
  * pages.  Positions are the caller's matter (keys are held rotated).  args is
  * reskv_paged_attn's with window 0.  A prefix_lens[g] outside the table is a fault and taken
  * as the nearest; a seq_begin that is out of order or outside [0, batch] likewise; the
  * queries of a sequence of no group see their own tokens alone.  Faults go to kv's and
- * prefix's status words.  Limits and roundings are reskv_paged_attn's; both parts are
- * joined in fp32.
+ * prefix's status words.  Limits and roundings are reskv_paged_attn's.  Where a prefix is taken
+ * for 128 or 256 rows, queries are held in fp16 beside a power of two a row, exactly down to
+ * 2^-21 of the row's largest element and to 2^-32 of it below.  Both parts are joined in fp32 by their
+ * log-sum-exps, each off by 2^-22 of itself at most.
+ * Speed goes by the room of the tables, too, which is what the host knows: SMs are divided between
+ * both parts, and kernels chosen, as if tables were full.  Tables no wider than the longest sequences are
+ * best (64 sequences of up to 512 behind 8192, caches flushed: 48 us; with own tables of 8192 129).
  * Limits: fewer than 1024 prefixes; n_tokens * heads / 2 + (batch + prefixes) * n_kv_heads below
  * 2^24.
  *   seq_begin   : device int32 [prefix->batch + 1], ascending; NULL: batch / prefix->batch each
@@ -738,14 +744,18 @@ reskv_status reskv_paged_attn_shared(const reskv_paged_kv* kv, const reskv_paged
  *
  * Rows that nobody sees (behind kv_lens[b], between sequences) may hold anything, NaN too.
  * Query tokens of no sequence are neither read nor written.  Logits are sums of exact
- * products in fp32; statistics and sums are fp32.  The softmax weights are rounded to
- * q's type before they meet the values (16 bits or more with up to 16 query rows a
+ * products in fp32, of any size (past 45000 rounded once more, to fp32, as x_j log2 e); one of -inf is
+ * a weight of 0, and a query with no other sees nothing.  Statistics and sums are fp32.  The softmax
+ * weights are rounded to q's type before they meet the values (16 bits or more with up to 16 query rows a
  * sequence and KV head on average): half a step of a weight, beside the half step of the output.
  * A fault (q_begin or kv_begin out of order or outside the rows, kv_lens outside the
  * sequence's rows) is reported and the value taken as the nearest.  Rows on 16-byte
  * boundaries (data and strides) take the fast kernels; others a general one, some
  * hundred times slower.
- * The result depends on shapes and lengths, not on the order in which blocks run.
+ * The result depends on shapes and lengths, not on the order in which blocks run, nor on the rows of
+ * other sequences.  (Of begins out of order, which sequences' rows are written is not said.)
+ * The kernel, and how many CTAs share a sequence, goes by the mean of query rows and states a sequence: a
+ * long prompt beside single tokens takes about what two calls take one after the other.
  */
 typedef struct reskv_cross_attn_args {
   reskv_heads q;                       /* [n_tokens, heads, d] bf16 or fp16; heads a multiple

@@ -25,8 +25,8 @@
 // The reference of a row moves only when a weight passes 2^13; it then lies 6 below the largest logit.
 //
 // Bound by the exponentials between two products of a stream, then by the products: 8 x 1024 tokens of 32 heads
-// over 4096 states, 8 KV heads of 128 (550 GFLOP) 450 us, 1.22 PFLOP/s; without any exponential 365, which
-// is what the products alone take in these tiles.  (P keeps both streams from a second S: the sums of 256 rows
+// over 4096 states, 8 KV heads of 128 (550 GFLOP) 450 us, 1.22 PFLOP/s; without any exponential, and
+// without the two threads' barrier, 365, which is what the products alone take in these tiles.  (P keeps both streams from a second S: the sums of 256 rows
 // and two S fill the tensor memory.)  Weights before their largest logit, 16 at a time in the shadow of the
 // other half's loads, spilled: 546.
 #include "cross.cuh"

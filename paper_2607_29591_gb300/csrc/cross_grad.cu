@@ -19,12 +19,13 @@
 // type (half a step of themselves; P times 2^12 in fp16, whose range ends at 2^-24), sums are fp32.
 //
 // Bound by the products: 4 x 2048 tokens of 32 heads over up to 4097 states (1.5 TFLOP in the eight products)
-// 1.07 ms, 1.4 PFLOP/s; without exponentials, sums and roundings 1.0.  A tile's two pairs of products run while
+// 1.10 ms, 1.4 PFLOP/s; without exponentials, sums and roundings 1.0.  A tile's two pairs of products run while
 // the weights of the other pair are formed; tensor memory (S, G and two sums) is full at d = 128.
 //
 // Weights are formed from the log-sum-exp that the forward pass left up to kFarSum.  A block of queries with a row
 // past it first walks the sequence's states for the rows' own sums (S alone, every rank of a cluster all of
-// them), and leaves them for the states' kernel.
+// them), and leaves them for the states' kernel: with queries 100 times as large 4 x 2048 tokens with their forward
+// pass take 2.47 ms for 1.46, 8 x 512 over 577 states 192 us for 125.
 //
 // Where there are too few blocks for the SMs, a cluster of CTAs shares a block's tiles: each leaves its two
 // sums in shared memory, where the cluster adds them up in order.

@@ -13,7 +13,7 @@
 //
 // Three stages of 32 KB (d = 128; two CTAs an SM) keep some 190 KB of an SM's under way: 32 tokens over up
 // to 6400 states of 8 KV heads (534 MB) 90 us, 5.9 TB/s, what is left being the sequences' unequal lengths (64
-// of 2000: 80 us, 6.6 TB/s).  One token over 1500 states 6.0 us, a chain of launch, copies, two products and
+// of 2000: 80 us, 6.6 TB/s).  One token over 1500 states 6.4 us, a chain of launch, copies, two products and
 // the join.
 #include "cross.cuh"
 #include "tensor_core.cuh"

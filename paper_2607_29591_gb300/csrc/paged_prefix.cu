@@ -20,7 +20,8 @@
 //   pv[m]         O holds it                                   (products -> softmax)
 //
 // Any magnitude fits fp16, whatever stands beside it: each position's key and each position's value is divided
-// by a power of two of its own, each query row by one.  Keys enter as s (n - 8), exact in 11
+// by a power of two of its own, each query row by one (its elements are exact down to 2^-21 of the largest, and to
+// 2^-32 of it below).  Keys enter as s (n - 8), exact in 11
 // bits, and m + 8 s in two planes against the sums of the query over its groups, so that logits are
 // sums of exact products; f is the power of two that the logit of a row and position takes.  Values
 // s n + m are rounded to 11 bits, no coarser than the 16-bit types of the output.  Their
