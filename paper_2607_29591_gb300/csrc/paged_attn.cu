@@ -395,7 +395,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
         const int64_t hr = i / (D / 4);
         const int h = int(hr / r1), r = int(hr - int64_t(h) * r1);
         store_out<kShared>(p, s, h, r, u, make_float4(0.f, 0.f, 0.f, 0.f));
-        if (u == 0) store_lse<kShared>(p, s, h, r, -INFINITY);
+        if (u == 0) store_sum<kShared>(p, s, h, r, -INFINITY);
       }
     }
     if (!active) return;
@@ -481,7 +481,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
         }
         if (st.g == 0 && st.half == 0) {
           if (!unit) refs[(2 * warp + slot) * kRows + r] = st.ref[j];
-          else if (c.r0 + r < rows) store_lse<kShared>(p, c.s, c.h, c.r0 + r, st.ref[j]);
+          else if (c.r0 + r < rows) store_sum<kShared>(p, c.s, c.h, c.r0 + r, st.ref[j]);
         }
       }
       if (!unit && lane == 0) info[2 * warp + slot] = RecordInfo{c.start, c.s, c.k.tiles, c.r0, c.h, 1};
@@ -540,7 +540,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
     a = all_lanes(a, lanes);
     if (!cut(ri)) {
       if (every == 0) store_out<kShared>(p, ri.s, ri.h, ri.r0 + row, u, a);
-      if (lane == 0 && u == 0) store_lse<kShared>(p, ri.s, ri.h, ri.r0 + row, j.ref);
+      if (lane == 0 && u == 0) store_sum<kShared>(p, ri.s, ri.h, ri.r0 + row, j.ref);
     } else {
       float* rec = p.partials + (cta * 2 + (ri.start >= c0 ? 1 : 0)) * (RF + kRows);
       if (every == 0) *reinterpret_cast<float4*>(rec + row * RS + 4 * u) = a;
@@ -605,7 +605,7 @@ __global__ void __launch_bounds__((kAttnWarps + 1) * 32, 1) k_attn_rows(const __
       }
     }
     if (every2 == 0) store_out<kShared>(p, ri.s, ri.h, ri.r0 + row2, u2, a);
-    if (lane == 0 && u2 == 0) store_lse<kShared>(p, ri.s, ri.h, ri.r0 + row2, all.ref);
+    if (lane == 0 && u2 == 0) store_sum<kShared>(p, ri.s, ri.h, ri.r0 + row2, all.ref);
   }
 }
 
@@ -993,6 +993,7 @@ extern "C" reskv_status reskv_paged_attn_shared(const reskv_paged_kv* kv, const 
     j.a.o_wide = call.o_wide;
     j.own = static_cast<const float*>(p.o);
     j.own_lse = p.lse;
+    j.own_unit = fused ? 1.f : kLog2e;
     j.prefix = g.prefix_o;
     j.prefix_ref = g.prefix_ref;
     j.plans = blocks ? plans : nullptr;

@@ -164,13 +164,17 @@ __device__ __forceinline__ void store_out(const Params<kShared>& p, const Sequen
   }
 }
 
-template <bool kShared = false>
-__device__ __forceinline__ void store_lse(const Params<kShared>& p, const Sequence& s, int h, int r, float ref) {
-  if constexpr (kShared) if (s.all) {
-    p.prefix_ref[(s.q0 + r / p.group) * int64_t(p.heads) + h * p.group + r % p.group] = ref;
-    return;
-  }
+__device__ __forceinline__ void store_lse(const AttnParams& p, const Sequence& s, int h, int r, float ref) {
   if (p.lse) p.lse[(s.q0 + r / p.group) * int64_t(p.heads) + h * p.group + r % p.group] = ref * 0.693147180559945f;
+}
+// The same, or in a launch of both parts log2 of the sums, for the join: through ln and back, equal keys of a prefix and of
+// the own tokens weighed up to 2 : 1 at logits of 1e7.
+template <bool kShared>
+__device__ __forceinline__ void store_sum(const Params<kShared>& p, const Sequence& s, int h, int r, float ref) {
+  float* to = p.lse;
+  if constexpr (kShared) if (s.all) to = p.prefix_ref;
+  if (to)
+    to[(s.q0 + r / p.group) * int64_t(p.heads) + h * p.group + r % p.group] = kShared ? ref : ref * 0.693147180559945f;
 }
 // The softmaxes of up to 32 records joined: each lane's weight for its record's
 // output, from their log2 sums (-inf: an empty or no record), the records that are none
@@ -744,12 +748,13 @@ inline int64_t group_items(int64_t rows, int groups, int kv_heads, int block_row
 }
 cudaError_t launch_attn_groups(const SharedParams& p, int mt, int items, int ctas, int d, int quant_group, int dev, float* records,
                                GroupPlan* plans, cudaStream_t s);
-// The softmaxes over the own tokens (fp32 rows in the order of o, ln of their sums) and over
+// The softmaxes over the own tokens (fp32 rows in the order of o, and their sums) and over
 // the prefix (the same with log2, or the records of `plans`) joined into o.
 struct SharedJoin {
   SharedParams a;                 // the call's, with the groups as in the prefix's pass
   const float* own;
-  const float* own_lse;
+  const float* own_lse;           // log2 of the sums times `own_unit`
+  float own_unit;
   const float* prefix;
   const float* prefix_ref;
   const GroupPlan* plans;         // NULL: the prefix has rows in the order of o, too

@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(kWarps * 32) k_shared_join(const __grid_consta
   const int u = lane < D / 4 ? lane : 0;
   const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
   // rows are asked for before it is known whether they count: what does not may hold anything
-  const float own = j.own_lse[row] * kLog2e;      // (-inf, NaN: as they are)
+  const float own = j.own_lse[row] * j.own_unit;  // (-inf, NaN: as they are)
   float4 a = reinterpret_cast<const float4*>(j.own + row * D)[u];
   if (group >= 0 && j.plans) {
     const GroupPlan g = j.plans[group];

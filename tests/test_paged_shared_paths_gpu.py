@@ -119,3 +119,33 @@ def test_a_prefix_of_all_positions_that_a_table_may_have(batch):
     ro, rl, _, vm = co.attend(q64, k, v, 64 ** -0.5)
     assert (np.abs(o.double().cpu().numpy() - ro) <= 0.06 * vm[..., None]).all()
     assert (np.abs(lse.double().cpu().numpy() - rl - np.log(many)) <= 0.03).all()
+
+
+@pytest.mark.parametrize("size", [1e1, 1e3, 1e5, 1e6, 1e7, 1e9])
+@pytest.mark.parametrize("batch", [1, 3, 7])
+def test_equal_keys_of_both_parts_share(batch, size):
+    """One key in the prefix and the same as own token, all others far below: one kernel forms both logits, so they are
+    equal, and the output is the mean of both values, each off by 11 bits."""
+    n, d = 300, 128
+    rng = np.random.default_rng(37)
+    prefix, _, _, _ = paged(rng, [0], 1, d, 32, 16, extra_pages=20, table_pages=19)
+    prefix.page_table.copy_(torch.arange(19, dtype=torch.int32)[None])
+    own, _, _, _ = paged(rng, [0] * batch, 1, d, 32, 16, extra_pages=batch, table_pages=1)
+    own.page_table.copy_(torch.arange(batch, dtype=torch.int32)[:, None])
+    k, v = np.full((n, 1, d), -size / d), rng.standard_normal((n, 1, d))
+    ko, vo = np.zeros((batch, 1, d)), rng.standard_normal((batch, 1, d))
+    k[100] = ko[:] = (1 + rng.random(d)) * size / d
+    f32 = lambda x: torch.from_numpy(x.astype(np.float32)).cuda()  # noqa: E731
+    R.reskv_paged_append(prefix, f32(k), f32(v), ints(np.zeros(n)), ints(np.arange(n)))
+    R.reskv_paged_append(own, f32(ko), f32(vo), ints(np.arange(batch)), ints(np.zeros(batch)))
+    held = [torch.empty((1, 1, n, d), device="cuda") for _ in range(2)]
+    mine = [torch.empty((batch, 1, 1, d), device="cuda") for _ in range(2)]
+    R.reskv_paged_gather(prefix, ints([n]), *held)
+    R.reskv_paged_gather(own, ints(np.ones(batch)), *mine)
+    q = (8 + torch.rand((batch, 4, d), device="cuda")).bfloat16()
+    o = torch.empty(q.shape, device="cuda")
+    R.reskv_paged_attn_shared(own, prefix, q, ints(np.ones(batch)), ints([n]), o)
+    a, b = held[1][0, 0, 100], mine[1][:, 0, 0]
+    far = float((q.float() @ (held[0][0, 0, 100] - held[0][0, 0, 0])).min()) * d ** -0.5          # the others' logits below
+    want, rest = (a + b)[:, None] / 2, n * np.exp(-min(far, 100.0)) * float(held[1].abs().max())
+    assert ((o - want).abs() <= 2.0 ** -11 * (a.abs() + b.abs())[:, None] + 2.0 ** -14 + rest).all()
